@@ -137,7 +137,7 @@ def prepare(case, seed):
     if own:
         import paper_2406_03285_amd as rb
         if case["op"] in ("score", "grad"):
-            s["scorer"] = rb.TokenScorer(case["vocab"], DTYPES[case["dtype"]], given=case["given"], top=case.get("top", 0), max_rows=case["rows"])
+            s["scorer"] = rb.TokenScorer(case["vocab"], DTYPES[case["dtype"]], given=case["given"], top=case.get("top", 0))
             if case["op"] == "score":
                 s["out"] = s["scorer"].outputs(case["rows"])
             else:                   # laid out like the logits
