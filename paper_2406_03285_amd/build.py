@@ -1,4 +1,4 @@
-"""Compile the HIP library (csrc/rb.hip and the headers it includes -> librb.so, gfx950 only) in-tree with hipcc."""
+"""Compile the HIP libraries (csrc/rb.hip -> librb.so, csrc/rb_train.hip -> librb_train.so, gfx950 only) in-tree with hipcc."""
 import os
 import subprocess
 import sysconfig
@@ -8,6 +8,8 @@ ROOT = os.path.dirname(HERE)
 SRC = os.path.join(HERE, "csrc", "rb.hip")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(HERE, "librb.so")
+TRAIN_SRC = os.path.join(HERE, "csrc", "rb_train.hip")
+TRAIN_LIB = os.path.join(HERE, "librb_train.so")
 
 HIPCC_FLAGS = [
     "-O3", "-std=c++17", "--offload-arch=gfx950", "-shared", "-fPIC",
@@ -48,12 +50,19 @@ def build_calls(verbose: bool = False) -> None:
     subprocess.run(cmd, check=True)
 
 
-def build(verbose: bool = False) -> str:
+def start_library(src: str, lib: str, verbose: bool = False) -> subprocess.Popen:
     hipcc = os.environ.get("HIPCC", os.path.join(ROCM, "bin", "hipcc"))
-    cmd = [hipcc, *HIPCC_FLAGS, "-I", INCLUDE, SRC, "-o", LIB]
+    cmd = [hipcc, *HIPCC_FLAGS, "-I", INCLUDE, src, "-o", lib]
     if verbose:
         print(" ".join(cmd))
-    subprocess.run(cmd, check=True)
+    return subprocess.Popen(cmd)
+
+
+def build(verbose: bool = False) -> str:
+    compilers = [start_library(SRC, LIB, verbose), start_library(TRAIN_SRC, TRAIN_LIB, verbose)]      # side by side
+    for compiler, status in [(c, c.wait()) for c in compilers]:
+        if status != 0:
+            raise subprocess.CalledProcessError(status, compiler.args)
     build_calls(verbose)
     if os.path.exists(CLIENT_SRC):
         cmd = ["gcc", "-std=c11", "-O2", "-Wall", "-Werror", "-D__HIP_PLATFORM_AMD__", "-I", INCLUDE, "-I", os.path.join(ROCM, "include"),

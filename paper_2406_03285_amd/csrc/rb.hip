@@ -32,6 +32,7 @@
 
 #include "rb.h"
 #include "rb_device.h"
+#include "rb_host.h"
 #include "rb_kernels_general.h"
 #include "rb_kernels_small.h"
 #include "rb_kernels_planned.h"
@@ -109,7 +110,6 @@ constexpr int MAX_DEVICES = 64;
 void* scratch_ptr[MAX_DEVICES] = {};          // device address of `scratch` on each device, once known
 rb_buffer* scratch_holder[MAX_DEVICES] = {};  // the handle that is bound to it
 
-inline bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 inline bool overlap(const void* p, int64_t p_bytes, const void* q, int64_t q_bytes)
 {
     const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
@@ -121,19 +121,6 @@ inline bool in_host_memory(const void* p)
     if (hipPointerGetAttributes(&at, p) == hipSuccess) return at.type == hipMemoryTypeHost;
     (void)hipGetLastError();                      // memory the runtime does not know: taken for the device's
     return false;
-}
-inline size_t round_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
-
-// Launches a kernel; the result is this launch's own.  (`<<<>>>` drops it, and hipGetLastError, asked behind it, also tells of calls of
-// anybody's that have failed on this thread before: a step that runs would be taken for one that does not.)
-template <typename T> struct as_is { using type = T; };
-template <typename... P>
-hipError_t launch(void (*kernel)(P...), dim3 grid, int threads, size_t lds, hipStream_t st, const typename as_is<P>::type&... arguments)
-{
-    void* args[] = {const_cast<void*>(static_cast<const void*>(&arguments))...};
-    const hipError_t e = hipLaunchKernel(reinterpret_cast<const void*>(kernel), grid, dim3((unsigned)threads), args, lds, st);
-    if (e != hipSuccess) (void)hipGetLastError();       // (nor is it left for others)
-    return e;
 }
 
 // How rb_update_sample_many carries out a call: step by step, or several steps per launch planned by one workgroup per

@@ -1,6 +1,7 @@
 /*
  * Native marshalling of the calls a training loop makes: rb_update, rb_sample_augment, rb_update_sample, rb_announce_next,
- * rb_update_sample_many, rb_announce_next_many, rb_pipeline_step_many and rb_pipeline_drain (rb_pipeline_step goes through ctypes).
+ * rb_update_sample_many, rb_announce_next_many, rb_pipeline_step_many and rb_pipeline_drain (rb_pipeline_step goes through ctypes), and of
+ * the training step's rb_scorer_score, rb_scorer_grad and rb_ortho_apply.
  * One `Call` object per function: called with integers, None and tensors in the declared positions it goes straight to the library;
  * anything else (keywords, other number types, wrong argument counts) goes to the Python function it was made with, which says what is
  * accepted and what is not.  A call through ctypes converts every argument through objects of its own: 16 + 16 rows of 12 KB in one call
@@ -8,7 +9,7 @@
  * A call for many steps and its announcement make five arrays of pointers besides: for 20 steps through ctypes 28 us, which pipelines of
  * short steps wait for, and 4.3 so (16 steps of 21 + 7 rows of 44 KB on a stream of their own 54 -> 41 us a call).
  *
- * Built as the extension module paper_2406_03285_amd._calls; it is not linked to librb.so but given the functions' addresses,
+ * Built as the extension module paper_2406_03285_amd._calls; it is not linked to the libraries but given the functions' addresses,
  * so that it calls the library that the binding has loaded.
  */
 #define PY_SSIZE_T_CLEAN
@@ -117,8 +118,10 @@ static PyObject* call(PyObject* self, PyObject* const* args, size_t nargsf, PyOb
     case 3: status = ((int (*)(uint64_t, uint64_t, uint64_t))c->address)(a[0], a[1], a[2]); break;
     case 6: status = ((int (*)(uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t))c->address)(a[0], a[1], a[2], a[3], a[4], a[5]); break;
     case 7: status = ((int (*)(uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t))c->address)(a[0], a[1], a[2], a[3], a[4], a[5], a[6]); break;
+    case 8: status = ((int (*)(uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t))c->address)(a[0], a[1], a[2], a[3], a[4], a[5], a[6], a[7]); break;
     case 10: status = ((int (*)(uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t))c->address)(a[0], a[1], a[2], a[3], a[4], a[5], a[6], a[7], a[8], a[9]); break;
     case 11: status = ((int (*)(uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t))c->address)(a[0], a[1], a[2], a[3], a[4], a[5], a[6], a[7], a[8], a[9], a[10]); break;
+    case 12: status = ((int (*)(uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t))c->address)(a[0], a[1], a[2], a[3], a[4], a[5], a[6], a[7], a[8], a[9], a[10], a[11]); break;
     default:
         status = ((int (*)(uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t))c->address)(
             a[0], a[1], a[2], a[3], a[4], a[5], a[6], a[7], a[8], a[9], a[10], a[11], a[12]);
@@ -144,7 +147,7 @@ static int call_init(PyObject* self, PyObject* args, PyObject* kwargs)
     size_t sequences = 0;
     for (size_t i = 0; i < n; ++i) sequences += layout[i] == 'v';
     const char* stream = strchr(layout, 's');
-    if (address == 0 || n > MAX_ARGS || (k != 2 && k != 3 && k != 6 && k != 7 && k != 10 && k != 11 && k != 13) || strspn(layout, "hpivs") != n ||
+    if (address == 0 || n > MAX_ARGS || (k != 2 && k != 3 && k != 6 && k != 7 && k != 8 && k != 10 && k != 11 && k != 12 && k != 13) || strspn(layout, "hpivs") != n ||
         sequences > MAX_SEQUENCES || (stream != NULL && stream != layout + n - 1) || !PyCallable_Check(general)) {
         PyErr_SetString(PyExc_ValueError, "Call(address, layout, general, rows=False)");
         return -1;

@@ -1,0 +1,527 @@
+// Scores of tokens under rows of logits (rb_scorer_score) and their gradient (rb_scorer_grad).  Included by rb_train.hip only.
+//
+// Score.  A row of logits is read once, 16 bytes per lane and load.  Every lane keeps the running maximum m of what it has seen, s = sum
+// of e^(z - m) and t = sum of e^(z - m) (z - m), rescaled when a tile of 32 elements brings a larger maximum; lanes, wavefronts and
+// workgroups are joined by the same rule, and lse = m + log s, entropy = log s - t / s.
+// Alternatives.  A wavefront keeps its best 64 elements so far as one 64-bit key per lane, sorted: the logit in an order-preserving 32-bit
+// form above the inverted index, so that equal logits order by index and no two keys are equal.  A lane whose tile holds nothing above the
+// smallest key that still counts (which the running maximum tells at no cost) goes on; of the others the tile's elements are read again
+// (they are in the cache), what passes is queued, and a full queue is sorted and merged into the list.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+namespace {
+
+constexpr int SC_WAVE = 64;
+constexpr int SC_TPB = 256;
+constexpr int SC_NWAVE = SC_TPB / SC_WAVE;
+constexpr int SC_LANE_ELEMS = 32;                  // elements of a tile per lane: 4 loads of 8 bfloat16, 8 of 4 binary32
+constexpr int SC_TILE = SC_WAVE * SC_LANE_ELEMS;   // elements of a wavefront's tile
+constexpr int SC_MAX_SPLITS = 64;                  // most workgroups that share a row (the last one's lanes join them)
+constexpr int SC_SPLIT_GROUPS = 1024;              // most workgroups of a launch whose rows are shared
+constexpr float SC_LOG2E = 1.44269504088896340736f;
+constexpr float SC_FLOOR = -200.0f;                // e^-200 is 0 in binary32: what is further below the maximum adds nothing, and 0 * floor is 0
+
+typedef uint32_t sc_vec __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ float sc_neg_inf() { return -__builtin_huge_valf(); }
+__device__ __forceinline__ float sc_nan() { return __builtin_nanf(""); }
+
+template <typename T> struct Logit;
+template <> struct Logit<float> {
+    static constexpr int N = 4;
+    static __device__ __forceinline__ float one(const float* p) { return *p; }
+    static __device__ __forceinline__ void unpack(const sc_vec v, float* z)
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) z[i] = __uint_as_float(v[i]);
+    }
+    static __device__ __forceinline__ float round(float x) { return x; }
+    static __device__ __forceinline__ sc_vec pack(const float* z)
+    {
+        return sc_vec{__float_as_uint(z[0]), __float_as_uint(z[1]), __float_as_uint(z[2]), __float_as_uint(z[3])};
+    }
+};
+struct Bf16 { uint16_t bits; };
+__device__ __forceinline__ uint32_t sc_bf16_bits(float x)      // to nearest, ties to even; NaN stays NaN
+{
+    const uint32_t u = __float_as_uint(x);
+    return (u & 0x7fffffffu) > 0x7f800000u ? (u >> 16) | 0x40u : (u + 0x7fffu + ((u >> 16) & 1u)) >> 16;
+}
+template <> struct Logit<Bf16> {
+    static constexpr int N = 8;
+    static __device__ __forceinline__ float one(const Bf16* p) { return __uint_as_float((uint32_t)p->bits << 16); }
+    static __device__ __forceinline__ void unpack(const sc_vec v, float* z)
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            z[2 * i] = __uint_as_float(v[i] << 16);
+            z[2 * i + 1] = __uint_as_float(v[i] & 0xffff0000u);
+        }
+    }
+    static __device__ __forceinline__ Bf16 round(float x) { return Bf16{(uint16_t)sc_bf16_bits(x)}; }
+    static __device__ __forceinline__ sc_vec pack(const float* z)
+    {
+        sc_vec v;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = sc_bf16_bits(z[2 * i]) | (sc_bf16_bits(z[2 * i + 1]) << 16);
+        return v;
+    }
+};
+
+// A row cut into what lies before the first 16-byte boundary, whole 16-byte vectors, and the rest.
+template <typename T>
+struct RowSpan {
+    int head, vectors, tail;
+    const sc_vec* body;
+    __device__ __forceinline__ RowSpan(const T* row, int vocab)
+    {
+        const int off = (int)((reinterpret_cast<uintptr_t>(row) & 15) / sizeof(T));
+        head = off ? min(Logit<T>::N - off, vocab) : 0;
+        vectors = (vocab - head) / Logit<T>::N;
+        tail = vocab - head - vectors * Logit<T>::N;
+        body = reinterpret_cast<const sc_vec*>(row + head);
+    }
+};
+
+// ---- running maximum and sums ------------------------------------------------
+
+struct Stats {
+    float m, s, t;      // maximum (NaN left out), sum of e^(z - m), sum of e^(z - m) (z - m)
+};
+
+// m as something to subtract: 0 where there is nothing but -inf (every e^(-inf - 0) is 0)
+__device__ __forceinline__ float sc_base(float m) { return m == sc_neg_inf() ? 0.0f : m; }
+
+__device__ __forceinline__ Stats sc_rebase(const Stats a, float m)
+{
+    const float d = fmaxf(a.m - sc_base(m), SC_FLOOR);             // a.m <= m; -inf and NaN (inf - inf) go to the floor
+    const float f = a.m == m ? 1.0f : __builtin_amdgcn_exp2f(d * SC_LOG2E);
+    return Stats{m, a.s * f, f * fmaf(a.s, a.m == m ? 0.0f : d, a.t)};
+}
+
+__device__ __forceinline__ Stats sc_join(const Stats a, const Stats b)
+{
+    const float m = fmaxf(a.m, b.m);
+    const Stats x = sc_rebase(a, m), y = sc_rebase(b, m);
+    return Stats{m, x.s + y.s, x.t + y.t};
+}
+
+__device__ __forceinline__ Stats sc_join_wave(Stats a)
+{
+#pragma unroll
+    for (int d = SC_WAVE / 2; d > 0; d >>= 1)
+        a = sc_join(a, Stats{__shfl_xor(a.m, d), __shfl_xor(a.s, d), __shfl_xor(a.t, d)});
+    return a;
+}
+
+template <int COUNT>
+__device__ __forceinline__ float sc_max(const float* z)
+{
+    float m = z[0];
+#pragma unroll
+    for (int i = 1; i < COUNT; ++i) m = fmaxf(m, z[i]);
+    return m;
+}
+
+template <int COUNT>
+__device__ __forceinline__ void sc_absorb(Stats& a, const float* z, float tile_max)
+{
+    a = sc_rebase(a, fmaxf(a.m, tile_max));
+    const float base = sc_base(a.m);
+    float s0 = 0.0f, s1 = 0.0f, t0 = 0.0f, t1 = 0.0f;
+#pragma unroll
+    for (int i = 0; i < COUNT; ++i) {
+        const float d = z[i] - base, e = __builtin_amdgcn_exp2f(d * SC_LOG2E), c = fmaxf(d, SC_FLOOR);
+        if (i & 1) {
+            s1 += e;
+            t1 = fmaf(e, c, t1);
+        } else {
+            s0 += e;
+            t0 = fmaf(e, c, t0);
+        }
+    }
+    a.s += s0 + s1;
+    a.t += t0 + t1;
+}
+
+// ---- the best elements -------------------------------------------------------
+
+__device__ __forceinline__ uint32_t sc_order(float z)              // orders as the numbers do, -0 as +0
+{
+    const uint32_t u = __float_as_uint(z + 0.0f);
+    return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ float sc_unorder(uint32_t o) { return __uint_as_float(o & 0x80000000u ? o ^ 0x80000000u : ~o); }
+__device__ __forceinline__ uint64_t sc_key(float z, uint32_t index) { return ((uint64_t)sc_order(z) << 32) | (uint32_t)~index; }
+
+template <typename K>
+__device__ __forceinline__ K sc_exchange(K key, int distance, bool keep_larger)
+{
+    const K other = __shfl_xor(key, distance);
+    return (key > other) == keep_larger ? key : other;             // (equal keys: either)
+}
+
+// The wavefront's keys, largest in lane 0.
+template <typename K>
+__device__ __forceinline__ K sc_sort(K key)
+{
+    const int lane = threadIdx.x & (SC_WAVE - 1);
+#pragma unroll
+    for (int k = 2; k <= SC_WAVE; k <<= 1)
+#pragma unroll
+        for (int d = k >> 1; d > 0; d >>= 1) key = sc_exchange(key, d, ((lane & d) == 0) == ((lane & k) == 0));
+    return key;
+}
+
+// The 64 largest of two sorted lists, sorted.
+__device__ __forceinline__ uint64_t sc_merge(uint64_t a, uint64_t b)
+{
+    const int lane = threadIdx.x & (SC_WAVE - 1);
+    b = __shfl(b, SC_WAVE - 1 - lane);
+    uint64_t key = a > b ? a : b;
+#pragma unroll
+    for (int d = SC_WAVE / 2; d > 0; d >>= 1) key = sc_exchange(key, d, (lane & d) == 0);
+    return key;
+}
+
+__device__ __forceinline__ void sc_lds_wait() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
+// A wavefront's list and the queue in LDS before it.
+struct Best {
+    uint64_t list;        // lane i: the (i + 1)-th largest key so far, 0: none
+    uint64_t least;       // the key of the last place that counts: what is not above it is not wanted
+    uint64_t* queue;      // 2 * SC_WAVE keys
+    uint32_t* shared;     // sc_order of a value that the row's result has `top` elements at or above, from any wavefront (null: none)
+    int queued, top;
+
+    __device__ __forceinline__ Best(uint64_t* q, uint32_t* sh, int top_) : list(0), least(0), queue(q), shared(sh), queued(0), top(top_) {}
+
+    __device__ __forceinline__ void merge_first()
+    {
+        const int lane = threadIdx.x & (SC_WAVE - 1);
+        sc_lds_wait();
+        const uint64_t key = lane < queued ? queue[lane] : 0;
+        const uint64_t rest = SC_WAVE + lane < queued ? queue[SC_WAVE + lane] : 0;
+        sc_lds_wait();
+        queue[lane] = rest;
+        queued = max(queued - SC_WAVE, 0);
+        list = sc_merge(list, sc_sort(key));
+        least = __shfl(list, top - 1);
+        if (shared != nullptr && lane == 0) atomicMax(shared, (uint32_t)(least >> 32));
+    }
+    __device__ __forceinline__ void push(uint64_t key, bool wanted)
+    {
+        const uint64_t who = __ballot(wanted && key > least);
+        if (who == 0) return;
+        if (wanted && key > least) queue[queued + __builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0))] = key;
+        queued += __popcll(who);
+        if (queued >= SC_WAVE) merge_first();
+    }
+    __device__ __forceinline__ void flush()
+    {
+        while (queued > 0) merge_first();
+    }
+};
+
+// ---- one row's share of a wavefront ------------------------------------------
+
+// Tiles part, part + parts, ... of the row; the elements at its unaligned ends fall to part 0.
+template <typename T, bool TOP>
+__device__ __forceinline__ void sc_scan(const T* row, int vocab, int part, int parts, Stats& stats, Best& best)
+{
+    constexpr int N = Logit<T>::N, U = SC_LANE_ELEMS / N;
+    const int lane = threadIdx.x & (SC_WAVE - 1);
+    const RowSpan<T> span(row, vocab);
+    const int tiles = (span.vectors + SC_WAVE * U - 1) / (SC_WAVE * U);
+    bool first = true;
+    for (int tile = part; tile < tiles; tile += parts) {
+        const int v0 = tile * (SC_WAVE * U) + lane;
+        sc_vec v[U];
+        if (v0 - lane + SC_WAVE * U <= span.vectors) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) v[u] = span.body[v0 + u * SC_WAVE];
+        } else {
+            uint32_t none = 0xff800000u;                           // -inf, one binary32 or (its upper half, twice) two bfloat16
+            if (sizeof(T) == 2) none = 0xff80ff80u;
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                v[u] = sc_vec{none, none, none, none};
+                if (v0 + u * SC_WAVE < span.vectors) v[u] = span.body[v0 + u * SC_WAVE];
+            }
+        }
+        float z[SC_LANE_ELEMS];
+#pragma unroll
+        for (int u = 0; u < U; ++u) Logit<T>::unpack(v[u], z + u * N);
+        const float tile_max = sc_max<SC_LANE_ELEMS>(z);
+        sc_absorb<SC_LANE_ELEMS>(stats, z, tile_max);
+        if (TOP) {
+            const bool any = v0 < span.vectors;
+            uint32_t least = 0;                                    // what an element has to reach
+            bool look;
+            if (first) {
+                // At least `top` elements reach the top-th largest of the lanes' maxima (fewer lanes than that: all are looked at).
+                least = __shfl(sc_sort(any ? sc_order(tile_max) : 0u), best.top - 1);
+                look = any && sc_order(tile_max) >= least;
+            } else {
+                if (best.shared != nullptr) least = __hip_atomic_load(best.shared, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+                // (an element that only equals the list's last one has a higher index than that)
+                look = any && (best.least == 0 || sc_order(tile_max) > (uint32_t)(best.least >> 32)) && sc_order(tile_max) >= least;
+            }
+            uint64_t who = __ballot(look);
+            while (who != 0) {
+                // lanes 0..31 read the elements of one of them, lanes 32..63 those of the next
+                const int a = __builtin_ctzll(who);
+                who &= who - 1;
+                const int b = who ? __builtin_ctzll(who) : -1;
+                who &= who - 1;
+                const int of = lane < SC_LANE_ELEMS ? a : b, j = lane & (SC_LANE_ELEMS - 1);
+                const int vector = tile * (SC_WAVE * U) + (j / N) * SC_WAVE + of;
+                const bool there = of >= 0 && vector < span.vectors;
+                const int index = span.head + vector * N + j % N;
+                float x = 0.0f;
+                if (there) x = Logit<T>::one(row + index);
+                best.push(sc_key(x, (uint32_t)index), there && sc_order(x) >= least);
+            }
+            if (first) best.flush();
+            first = false;
+        }
+    }
+    if (part == 0 && span.head + span.tail > 0) {
+        const int j = lane < span.head ? lane : lane >= SC_WAVE / 2 && lane - SC_WAVE / 2 < span.tail ? vocab - span.tail + lane - SC_WAVE / 2 : -1;
+        const float x = j >= 0 ? Logit<T>::one(row + j) : sc_neg_inf();
+        sc_absorb<1>(stats, &x, fmaxf(x, sc_neg_inf()));
+        if (TOP) best.push(sc_key(x, (uint32_t)j), j >= 0);
+    }
+    if (TOP) best.flush();
+}
+
+struct ScoreArgs {
+    const void* logits;
+    int64_t stride;                 // elements between rows
+    const int64_t* tokens;
+    float *logp, *lse, *entropy, *top_logp;
+    int64_t* top_ids;
+    uint32_t* counters;             // per row that is shared: workgroups that have left their part (0 between launches)
+    char* partials;                 // per workgroup of a shared row: Stats, then `top` keys
+    int32_t rows, vocab, given, top, splits;
+};
+
+__host__ __device__ inline size_t sc_partial_bytes(int top) { return 16 + 8 * (size_t)top; }
+
+// What a wavefront that knows a whole row writes.
+template <typename T>
+__device__ __forceinline__ void sc_finish(const ScoreArgs& a, const T* z, int64_t row, const Stats st, uint64_t list)
+{
+    const int lane = threadIdx.x & (SC_WAVE - 1);
+    const bool empty = st.m == sc_neg_inf() && st.s == 0.0f;
+    const float log_s = logf(st.s);
+    const float lse = empty ? sc_neg_inf() : st.m + log_s;
+    const bool broken = lse != lse;
+    if (lane == 0) {
+        if (a.lse != nullptr) a.lse[row] = lse;
+        if (a.entropy != nullptr) a.entropy[row] = empty ? 0.0f : broken ? lse : log_s - st.t / st.s;
+    }
+    if (lane < a.given) {
+        const int64_t t = a.tokens[row * a.given + lane];
+        float v = 0.0f;
+        if (t >= 0 && t < a.vocab) {
+            const float x = Logit<T>::one(z + t);
+            v = broken ? lse : x == sc_neg_inf() ? x : (x - st.m) - log_s;      // (x - lse would be off by lse's last bit)
+        }
+        a.logp[row * a.given + lane] = v;
+    }
+    if (lane < a.top) {
+        const float x = sc_unorder((uint32_t)(list >> 32));
+        a.top_logp[row * a.top + lane] = broken ? lse : x == sc_neg_inf() ? x : (x - st.m) - log_s;
+        a.top_ids[row * a.top + lane] = broken ? -1 : (int64_t)(uint32_t)~(uint32_t)list;
+    }
+}
+
+// A wavefront per row (WAVES 1: short rows) or a workgroup per row or per 1 / splits of one (WAVES 4).
+template <typename T, bool TOP, int WAVES>
+__global__ __launch_bounds__(SC_TPB) void rb_score_kernel(const ScoreArgs a)
+{
+    __shared__ uint64_t queues[SC_NWAVE][TOP ? 2 * SC_WAVE : 1];
+    const int wave = threadIdx.x / SC_WAVE, lane = threadIdx.x & (SC_WAVE - 1);
+    Stats st{sc_neg_inf(), 0.0f, 0.0f};
+    if (WAVES == 1) {
+        const int64_t row = (int64_t)blockIdx.x * SC_NWAVE + wave;
+        if (row >= a.rows) return;
+        const T* z = static_cast<const T*>(a.logits) + row * a.stride;
+        Best best(queues[wave], nullptr, a.top);
+        sc_scan<T, TOP>(z, a.vocab, 0, 1, st, best);
+        sc_finish(a, z, row, sc_join_wave(st), best.list);
+        return;
+    }
+    __shared__ uint64_t lists[SC_NWAVE][TOP ? SC_WAVE : 1];
+    __shared__ Stats stats[SC_NWAVE];
+    __shared__ uint32_t shared;
+    const int64_t row = blockIdx.x / (uint32_t)a.splits;
+    const int split = blockIdx.x % (uint32_t)a.splits;
+    const T* z = static_cast<const T*>(a.logits) + row * a.stride;
+    if (TOP) {
+        if (threadIdx.x == 0) shared = 0;
+        __syncthreads();
+    }
+    Best best(queues[wave], TOP ? &shared : nullptr, a.top);
+    sc_scan<T, TOP>(z, a.vocab, split * SC_NWAVE + wave, a.splits * SC_NWAVE, st, best);
+    st = sc_join_wave(st);
+    if (lane == 0) stats[wave] = st;
+    if (TOP) lists[wave][lane] = best.list;
+    __syncthreads();
+    if (wave != 0) return;
+    st = stats[0];
+    uint64_t list = best.list;
+#pragma unroll
+    for (int w = 1; w < SC_NWAVE; ++w) {
+        st = sc_join(st, stats[w]);
+        if (TOP) list = sc_merge(list, lists[w][lane]);
+    }
+    if (a.splits > 1) {
+        // Every workgroup leaves its part; the one that is last to do so joins them, in the order of the parts whoever it is.
+        const size_t bytes = sc_partial_bytes(a.top);
+        char* mine = a.partials + (size_t)blockIdx.x * bytes;
+        if (lane == 0) *reinterpret_cast<Stats*>(mine) = st;
+        if (TOP && lane < a.top) reinterpret_cast<uint64_t*>(mine + 16)[lane] = list;
+        __threadfence();
+        uint32_t before = 0;
+        if (lane == 0) before = __hip_atomic_fetch_add(a.counters + row, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
+        before = __builtin_amdgcn_readfirstlane(before);
+        if (before != (uint32_t)a.splits - 1) return;
+        __threadfence();
+        if (lane == 0) __hip_atomic_store(a.counters + row, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        const char* parts = a.partials + (size_t)row * a.splits * bytes;
+        st = Stats{sc_neg_inf(), 0.0f, 0.0f};
+        if (lane < a.splits) st = *reinterpret_cast<const Stats*>(parts + lane * bytes);
+        st = sc_join_wave(st);
+        if (TOP) {
+            list = 0;
+            for (int p = 0; p < a.splits; ++p) list = sc_merge(list, lane < a.top ? reinterpret_cast<const uint64_t*>(parts + p * bytes + 16)[lane] : 0);
+        }
+    }
+    sc_finish(a, z, row, st, list);
+}
+
+// ---- gradient ----------------------------------------------------------------
+
+struct GradArgs {
+    const void* logits;
+    void* grad;
+    int64_t stride, grad_stride;
+    const int64_t* tokens;
+    const float *lse, *entropy, *grad_logp, *grad_entropy;
+    int32_t vocab, given, chunk;    // chunk: accesses (vectors, or elements) of a row per workgroup
+};
+
+constexpr int GR_MAX_TILES = 32;    // tiles of SC_TPB accesses in a chunk: one bit each says whether a given token is in it
+
+// A workgroup per row (blockIdx.x) and chunk of the row (blockIdx.y).  N elements per access: 16 bytes, or one element where logits and
+// gradient lie differently relative to 16 bytes.  Which of a thread's accesses hold a given token is one word of bits, so that the rest
+// costs one test; the tokens' sums are made in the order in which they were given.
+template <typename T, int N>
+__global__ __launch_bounds__(SC_TPB) void rb_score_grad_kernel(const GradArgs a)
+{
+    __shared__ uint32_t hit[SC_TPB];
+    __shared__ int32_t ids[64];
+    __shared__ float weights[64];
+    const int64_t row = blockIdx.x;
+    const T* z = static_cast<const T*>(a.logits) + row * a.stride;
+    T* dz = static_cast<T*>(a.grad) + row * a.grad_stride;
+    const float lse = a.lse[row];
+    const float h = a.grad_entropy != nullptr ? a.grad_entropy[row] : 0.0f, ent = a.grad_entropy != nullptr ? a.entropy[row] : 0.0f;
+    int head = 0, count = a.vocab, tail = 0;
+    if (N > 1) {
+        const RowSpan<T> span(z, a.vocab);
+        head = span.head;
+        count = span.vectors;
+        tail = span.tail;
+    }
+    const int begin = blockIdx.y * a.chunk, end = min(begin + a.chunk, count);
+    const int lane = threadIdx.x & (SC_WAVE - 1);
+    int id = -1;
+    float w = 0.0f;
+    if (lane < a.given) {
+        const int64_t t = a.tokens[row * a.given + lane];
+        if (t >= 0 && t < a.vocab) {
+            id = (int)t;
+            w = a.grad_logp[row * a.given + lane];
+        }
+    }
+    float sum = w;
+#pragma unroll
+    for (int d = SC_WAVE / 2; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
+    hit[threadIdx.x] = 0;
+    __syncthreads();
+    if (threadIdx.x < 64) {
+        ids[lane] = id;
+        weights[lane] = w;
+        const int at = id < head ? -1 : (id - head) / N;
+        if (id >= 0 && at >= begin && at < end) atomicOr(&hit[(at - begin) % SC_TPB], 1u << ((at - begin) / SC_TPB));
+    }
+    __syncthreads();
+    const uint32_t mine = hit[threadIdx.x];
+    const bool dead = lse == sc_neg_inf();
+    auto value = [&](float x) {
+        const float l = fmaxf(x - lse, SC_FLOOR), p = __builtin_amdgcn_exp2f((x - lse) * SC_LOG2E);
+        return -p * fmaf(h, l + ent, sum);
+    };
+    auto given = [&](int j) {
+        float v = 0.0f;
+        for (int g = 0; g < a.given; ++g)
+            if (ids[g] == j) v += weights[g];
+        return v;
+    };
+    if (N > 1) {
+        constexpr int U = 4;
+        const sc_vec* src = reinterpret_cast<const sc_vec*>(z + head);
+        sc_vec* dst = reinterpret_cast<sc_vec*>(dz + head);
+        int tile = 0;
+        for (int i0 = begin + threadIdx.x; i0 < end; i0 += U * SC_TPB, tile += U) {
+            sc_vec v[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (i0 + u * SC_TPB < end) v[u] = src[i0 + u * SC_TPB];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (i0 + u * SC_TPB >= end) continue;
+                float x[Logit<T>::N];
+                Logit<T>::unpack(v[u], x);
+#pragma unroll
+                for (int i = 0; i < Logit<T>::N; ++i) x[i] = value(x[i]);
+                if ((mine >> (tile + u)) & 1u) {
+                    const int first = head + (i0 + u * SC_TPB) * N;
+#pragma unroll
+                    for (int i = 0; i < Logit<T>::N; ++i) x[i] += given(first + i);
+                }
+                if (dead) {
+#pragma unroll
+                    for (int i = 0; i < Logit<T>::N; ++i) x[i] = 0.0f;
+                }
+                dst[i0 + u * SC_TPB] = Logit<T>::pack(x);
+            }
+        }
+        if (blockIdx.y == 0 && threadIdx.x < head + tail) {
+            const int j = threadIdx.x < head ? threadIdx.x : a.vocab - tail + (int)threadIdx.x - head;
+            const float x = value(Logit<T>::one(z + j)) + given(j);
+            dz[j] = Logit<T>::round(dead ? 0.0f : x);
+        }
+    } else {
+        int tile = 0;
+        for (int i = begin + threadIdx.x; i < end; i += SC_TPB, ++tile) {
+            float x = value(Logit<T>::one(z + i));
+            if ((mine >> tile) & 1u) x += given(i);
+            dz[i] = Logit<T>::round(dead ? 0.0f : x);
+        }
+    }
+}
+
+__global__ __launch_bounds__(SC_TPB) void rb_train_clear_kernel(uint32_t* p, int64_t words)
+{
+    for (int64_t i = (int64_t)blockIdx.x * SC_TPB + threadIdx.x; i < words; i += (int64_t)gridDim.x * SC_TPB) p[i] = 0;
+}
+
+}  // namespace

@@ -1,0 +1,315 @@
+"""Thin binding of the C ABI in include/rb_train.h: what a training program computes at the augmented mini-batch.
+
+As in binding.py every function has the name and argument order of its C counterpart, and the classes only own device memory, keep a
+handle, look at what they are given and raise RbError on a non-zero status.  There is no fallback: if librb_train.so is missing the import fails.
+"""
+import ctypes as C
+import math
+import os
+from typing import NamedTuple, Optional
+
+import torch
+
+from .binding import Call, HERE, RB_BF16, RB_F32, _check, _ptr, _stream
+
+TRAIN_LIB_PATH = os.environ.get("RB_TRAIN_LIBRARY") or os.path.join(HERE, "librb_train.so")   # RB_TRAIN_LIBRARY: another build of the same library
+
+RB_MAX_VOCAB, RB_MAX_ROWS, RB_MAX_GIVEN, RB_MAX_TOP = 1 << 28, 1 << 23, 64, 64
+RB_MAX_DIM, RB_MAX_MATRICES, RB_MAX_ORTHO_STEPS = 65536, 65535, 16
+
+TRAIN_EXPORTS = (
+    "rb_scorer_create", "rb_scorer_query", "rb_scorer_bind", "rb_scorer_score", "rb_scorer_grad", "rb_scorer_destroy",
+    "rb_ortho_create", "rb_ortho_query", "rb_ortho_bind", "rb_ortho_apply", "rb_ortho_step", "rb_ortho_destroy",
+)
+
+__all__ = ["TRAIN_EXPORTS", "TRAIN_LIB_PATH", "RB_MAX_VOCAB", "RB_MAX_ROWS", "RB_MAX_GIVEN", "RB_MAX_TOP", "RB_MAX_DIM", "RB_MAX_MATRICES",
+           "RB_MAX_ORTHO_STEPS", "NEWTON_SCHULZ", "Scores", "TokenScorer", "Orthogonalizer", *TRAIN_EXPORTS]
+
+
+def _load():
+    if not os.path.exists(TRAIN_LIB_PATH):
+        raise ImportError(
+            f"{TRAIN_LIB_PATH} is missing: build it with `python paper_2406_03285_amd/build.py` "
+            "(there is no fallback path)")
+    L = C.CDLL(TRAIN_LIB_PATH)
+    vp, i64, i32, sz, f32 = C.c_void_p, C.c_int64, C.c_int32, C.c_size_t, C.c_float
+    L.rb_scorer_create.argtypes = [C.POINTER(vp), i64, i32, i64, i64]
+    L.rb_scorer_query.argtypes = [vp, C.POINTER(sz)]
+    L.rb_scorer_bind.argtypes = [vp, vp, vp]
+    L.rb_scorer_score.argtypes = [vp, vp, i64, i64, vp, vp, vp, vp, vp, vp, vp]
+    L.rb_scorer_grad.argtypes = [vp, vp, i64, i64, vp, vp, vp, vp, vp, vp, i64, vp]
+    L.rb_scorer_destroy.argtypes = [vp]
+    L.rb_ortho_create.argtypes = [C.POINTER(vp), i64, i64, i64, i32, i32, C.POINTER(f32), i64, f32]
+    L.rb_ortho_query.argtypes = [vp, C.POINTER(sz)]
+    L.rb_ortho_bind.argtypes = [vp, vp]
+    L.rb_ortho_apply.argtypes = [vp, vp, i64, i64, vp, i64, i64, vp]
+    L.rb_ortho_step.argtypes = [vp, vp, i64, i64, vp, i64, i64, vp, f32, f32, i32, f32, f32, vp]
+    L.rb_ortho_destroy.argtypes = [vp]
+    for name in TRAIN_EXPORTS:
+        getattr(L, name).restype = C.c_int
+    return L
+
+
+_L = _load()
+
+
+def _native(general, layout):
+    """As in binding.py: the same function with its usual arguments marshalled natively."""
+    if Call is None:
+        return general
+    return Call(C.cast(getattr(_L, general.__name__), C.c_void_p).value, layout, general)
+
+
+def rb_scorer_create(vocab, dtype, given, top):
+    h = C.c_void_p()
+    rc = _L.rb_scorer_create(C.byref(h), int(vocab), int(dtype), int(given), int(top))
+    return rc, h.value
+
+
+def rb_scorer_query(s):
+    n = C.c_size_t()
+    rc = _L.rb_scorer_query(s, C.byref(n))
+    return rc, n.value
+
+
+def rb_scorer_bind(s, workspace, hip_stream=None):
+    return _L.rb_scorer_bind(s, _ptr(workspace), _stream(hip_stream))
+
+
+def rb_scorer_score(s, logits, rows, row_stride, tokens, logp, lse, entropy, top_logp, top_ids, hip_stream=None):
+    return _L.rb_scorer_score(s, _ptr(logits), int(rows), int(row_stride), _ptr(tokens), _ptr(logp), _ptr(lse), _ptr(entropy),
+                              _ptr(top_logp), _ptr(top_ids), _stream(hip_stream))
+
+
+def rb_scorer_grad(s, logits, rows, row_stride, tokens, lse, entropy, grad_logp, grad_entropy, grad_logits, grad_stride, hip_stream=None):
+    return _L.rb_scorer_grad(s, _ptr(logits), int(rows), int(row_stride), _ptr(tokens), _ptr(lse), _ptr(entropy), _ptr(grad_logp),
+                             _ptr(grad_entropy), _ptr(grad_logits), int(grad_stride), _stream(hip_stream))
+
+
+def rb_scorer_destroy(s):
+    return _L.rb_scorer_destroy(s)
+
+
+def rb_ortho_create(matrices, m, n, dtype, out_dtype, coefficients, eps):
+    """coefficients: a sequence of (a, b, c), one per step."""
+    h = C.c_void_p()
+    flat = [float(v) for abc in coefficients for v in abc]
+    rc = _L.rb_ortho_create(C.byref(h), int(matrices), int(m), int(n), int(dtype), int(out_dtype), (C.c_float * len(flat))(*flat),
+                            len(flat) // 3, float(eps))
+    return rc, h.value
+
+
+def rb_ortho_query(o):
+    n = C.c_size_t()
+    rc = _L.rb_ortho_query(o, C.byref(n))
+    return rc, n.value
+
+
+def rb_ortho_bind(o, workspace):
+    return _L.rb_ortho_bind(o, _ptr(workspace))
+
+
+def rb_ortho_apply(o, update, update_matrix_stride, update_row_stride, out, out_matrix_stride, out_row_stride, hip_stream=None):
+    return _L.rb_ortho_apply(o, _ptr(update), int(update_matrix_stride), int(update_row_stride), _ptr(out), int(out_matrix_stride),
+                             int(out_row_stride), _stream(hip_stream))
+
+
+def rb_ortho_step(o, weight, weight_matrix_stride, weight_row_stride, grad, grad_matrix_stride, grad_row_stride, momentum, lr, beta,
+                  nesterov, weight_decay, scale, hip_stream=None):
+    return _L.rb_ortho_step(o, _ptr(weight), int(weight_matrix_stride), int(weight_row_stride), _ptr(grad), int(grad_matrix_stride),
+                            int(grad_row_stride), _ptr(momentum), float(lr), float(beta), int(nesterov), float(weight_decay),
+                            float(scale), _stream(hip_stream))
+
+
+def rb_ortho_destroy(o):
+    return _L.rb_ortho_destroy(o)
+
+
+rb_scorer_score = _native(rb_scorer_score, "hpiipppppps")
+rb_scorer_grad = _native(rb_scorer_grad, "hpiippppppis")
+rb_ortho_apply = _native(rb_ortho_apply, "hpiipiis")
+
+_CODES = {torch.float32: RB_F32, torch.bfloat16: RB_BF16}
+
+
+class _OnStream:
+    """Calls go to the current stream of the handle's device; a call on another stream than the last one's waits for that, since the two
+    share the workspace (not under capture: a captured call is ordered by its graph)."""
+
+    def _bind_device(self, device):
+        self.device = torch.device(device)
+        if self.device.index is None:
+            self.device = torch.device(self.device.type, torch.cuda.current_device())
+        self._last = torch.cuda.current_stream(self.device)
+
+    def _on_stream(self, call, *args):
+        stream = torch.cuda.current_stream(self.device)
+        if stream != self._last:
+            if not torch.cuda.is_current_stream_capturing():
+                stream.wait_stream(self._last)
+            self._last = stream
+        if torch.cuda.current_device() == self.device.index:
+            return call(*args, stream)
+        with torch.cuda.device(self.device):
+            return call(*args, stream)
+
+
+class Scores(NamedTuple):
+    """What TokenScorer.score gives, binary32 but for the indices; the last two are None without alternatives, logp without given tokens."""
+    logp: Optional[torch.Tensor]           # [rows, given]
+    lse: torch.Tensor                      # [rows]
+    entropy: torch.Tensor                  # [rows]
+    top_logp: Optional[torch.Tensor]       # [rows, top]
+    top_ids: Optional[torch.Tensor]        # [rows, top] int64
+
+
+class TokenScorer(_OnStream):
+    """Log probabilities of given tokens under rows of logits, the rows' entropy and top alternatives, and their gradient.
+
+    scorer = TokenScorer(vocab, torch.bfloat16, given=1, top=8)
+    s = scorer.score(logits, tokens)                # Scores; logits [rows, vocab], rows may be strided; tokens [rows, given] (or [rows])
+    s = scorer(logits, tokens)                      # the same within autograd: s.logp and s.entropy carry gradients
+    """
+
+    def __init__(self, vocab, dtype=torch.float32, given=1, top=0, device="cuda"):
+        rc, self.handle = rb_scorer_create(vocab, _CODES[dtype], given, top)
+        _check(rc, "rb_scorer_create")
+        self.vocab, self.dtype, self.given, self.top = int(vocab), dtype, int(given), int(top)
+        self._bind_device(device)
+        rc, size = rb_scorer_query(self.handle)
+        _check(rc, "rb_scorer_query")
+        self.workspace = torch.empty(size, dtype=torch.uint8, device=self.device)
+        _check(self._on_stream(rb_scorer_bind, self.handle, self.workspace), "rb_scorer_bind")
+
+    def outputs(self, rows):
+        """Tensors for score(..., out=...)."""
+        def new(*shape, dtype=torch.float32):
+            return torch.empty(shape, dtype=dtype, device=self.device)
+        return Scores(new(rows, self.given) if self.given else None, new(rows), new(rows), new(rows, self.top) if self.top else None,
+                      new(rows, self.top, dtype=torch.int64) if self.top else None)
+
+    def _look_at(self, logits, tokens):
+        rows = logits.shape[0]
+        assert logits.dim() == 2 and logits.shape[1] == self.vocab and logits.dtype == self.dtype and logits.device == self.device
+        assert logits.stride(1) == 1 or self.vocab == 1
+        if self.given:
+            assert tokens.dtype == torch.int64 and tokens.is_contiguous() and tokens.device == self.device
+            assert tokens.shape == (rows, self.given) or (self.given == 1 and tokens.shape == (rows,))
+        return rows, max(logits.stride(0), self.vocab) if rows < 2 else logits.stride(0)
+
+    def score(self, logits, tokens=None, out=None):
+        """Scores of every row of logits; into `out` if given (see outputs)."""
+        rows, stride = self._look_at(logits, tokens)
+        if out is None:
+            out = self.outputs(rows)
+        elif rows:
+            for t, shape in zip(out, ((rows, self.given), (rows,), (rows,), (rows, self.top), (rows, self.top))):
+                assert t is None or (t.shape == shape and t.is_contiguous() and t.device == self.device)
+            assert (out.logp is None or out.logp.dtype == torch.float32) and (out.top_ids is None or out.top_ids.dtype == torch.int64)
+        _check(self._on_stream(rb_scorer_score, self.handle, logits, rows, stride, tokens if self.given else None, out.logp, out.lse,
+                               out.entropy, out.top_logp, out.top_ids), "rb_scorer_score")
+        return out
+
+    def grad(self, logits, tokens, lse, entropy, grad_logp, grad_entropy=None, out=None):
+        """The gradient with respect to the logits, from the derivatives with respect to logp [rows, given] and entropy [rows] (or None).
+        out: a tensor shaped as the logits (rows may be strided), which the logits themselves may be."""
+        rows, stride = self._look_at(logits, tokens)
+        if out is None:
+            out = torch.empty((rows, self.vocab), dtype=self.dtype, device=self.device)
+        assert out.shape == (rows, self.vocab) and out.dtype == self.dtype and out.device == self.device and (out.stride(1) == 1 or self.vocab == 1)
+        for t, shape in ((lse, (rows,)), (entropy, (rows,)), (grad_entropy, (rows,)), (grad_logp, (rows, self.given))):
+            if t is not None:
+                assert t.dtype == torch.float32 and t.is_contiguous() and t.device == self.device and t.numel() == math.prod(shape)
+        out_stride = max(out.stride(0), self.vocab) if rows < 2 else out.stride(0)
+        _check(self._on_stream(rb_scorer_grad, self.handle, logits, rows, stride, tokens if self.given else None, lse, entropy,
+                               grad_logp if self.given else None, grad_entropy, out, out_stride), "rb_scorer_grad")
+        return out
+
+    def __call__(self, logits, tokens=None):
+        return Scores(*_Score.apply(logits, tokens, self))
+
+    def close(self):
+        if getattr(self, "handle", None):
+            rb_scorer_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        self.close()
+
+
+class _Score(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, logits, tokens, scorer):
+        s = scorer.score(logits, tokens)
+        ctx.scorer = scorer
+        ctx.set_materialize_grads(False)
+        ctx.save_for_backward(logits, tokens, s.lse, s.entropy)
+        ctx.mark_non_differentiable(*[t for t in (s.lse, s.top_logp, s.top_ids) if t is not None])
+        return tuple(s)
+
+    @staticmethod
+    def backward(ctx, grad_logp, _lse, grad_entropy, _top_logp, _top_ids):
+        logits, tokens, lse, entropy = ctx.saved_tensors
+        scorer = ctx.scorer
+        if grad_logp is None and grad_entropy is None:
+            return None, None, None
+        if grad_logp is None and scorer.given:
+            grad_logp = lse.new_zeros((logits.shape[0], scorer.given))
+        return scorer.grad(logits, tokens, lse, entropy, None if grad_logp is None else grad_logp.contiguous(),
+                           None if grad_entropy is None else grad_entropy.contiguous()), None, None
+
+
+#: The usual coefficients of one Newton-Schulz step: they bring singular values from about 0.01 to 1 near 1 in five steps.
+NEWTON_SCHULZ = (3.4445, -4.7750, 2.0315)
+
+
+class Orthogonalizer(_OnStream):
+    """Updates orthogonalised by Newton-Schulz products, for `batch` matrices of m x n at a time.
+
+    ortho = Orthogonalizer(1024, 4096, dtype=torch.bfloat16, out_dtype=torch.float32)
+    ortho.orthogonalize(update)                                  # [m, n] or [batch, m, n] -> the same of out_dtype
+    ortho.step(weight, grad, momentum, lr=0.02)                  # the optimiser step around it, in place
+    """
+
+    def __init__(self, m, n, batch=1, dtype=torch.float32, out_dtype=None, coefficients=(NEWTON_SCHULZ,) * 5, eps=1e-7, device="cuda"):
+        self.out_dtype = dtype if out_dtype is None else out_dtype
+        rc, self.handle = rb_ortho_create(batch, m, n, _CODES[dtype], _CODES[self.out_dtype], coefficients, eps)
+        _check(rc, "rb_ortho_create")
+        self.m, self.n, self.batch, self.dtype = int(m), int(n), int(batch), dtype
+        self._bind_device(device)
+        rc, size = rb_ortho_query(self.handle)
+        _check(rc, "rb_ortho_query")
+        self.workspace = torch.empty(size, dtype=torch.uint8, device=self.device)
+        _check(rb_ortho_bind(self.handle, self.workspace), "rb_ortho_bind")
+
+    def _strides(self, t, dtype):
+        """(matrix stride, row stride) of a tensor that is looked at first."""
+        assert t.dtype == dtype and t.device == self.device
+        assert t.shape == (self.batch, self.m, self.n) or (self.batch == 1 and t.shape == (self.m, self.n))
+        assert t.stride(-1) == 1 or self.n == 1
+        return (t.stride(0) if t.dim() == 3 and self.batch > 1 else 0), (t.stride(-2) if self.m > 1 else self.n)
+
+    def orthogonalize(self, update, out=None):
+        a = self._strides(update, self.dtype)
+        if out is None:
+            out = torch.empty(update.shape, dtype=self.out_dtype, device=self.device)
+        b = self._strides(out, self.out_dtype)
+        _check(self._on_stream(rb_ortho_apply, self.handle, update, *a, out, *b), "rb_ortho_apply")
+        return out
+
+    def step(self, weight, grad, momentum, lr, beta=0.95, nesterov=True, weight_decay=0.0, scale=None):
+        """momentum <- beta momentum + grad; weight <- (1 - lr weight_decay) weight - lr scale O, O the orthogonalised grad + beta momentum
+        (nesterov) or momentum.  scale: None - sqrt(max(1, m / n))."""
+        w, g = self._strides(weight, self.out_dtype), self._strides(grad, self.dtype)
+        assert momentum.shape == weight.shape and momentum.dtype == torch.float32 and momentum.is_contiguous() and momentum.device == self.device
+        if scale is None:
+            scale = math.sqrt(max(1.0, self.m / self.n))
+        _check(self._on_stream(rb_ortho_step, self.handle, weight, *w, grad, *g, momentum, lr, beta, nesterov, weight_decay, scale), "rb_ortho_step")
+
+    def close(self):
+        if getattr(self, "handle", None):
+            rb_ortho_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        self.close()
