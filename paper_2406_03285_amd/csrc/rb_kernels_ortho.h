@@ -26,8 +26,7 @@ typedef uint32_t ns_vec __attribute__((ext_vector_type(4)));
 constexpr int NS_TPB = 256;
 constexpr int NS_KBLOCK = 32;                  // elements of a block: hi, then lo
 constexpr int NS_KHALVES = 2 * NS_KBLOCK;
-constexpr int NS_TILE = 128;                   // rows and columns of a product's tile
-constexpr int NS_PARTS = 256;                  // partial sums of a norm per matrix
+constexpr int NS_PARTS = 1024;                 // most partial sums of a norm per matrix
 // What is kept is scaled by powers of two, so that lo is a normal binary16 number for elements of the size that occurs, and a singular
 // value of 4 (A: 16, B: 60) is still below 65504.
 constexpr float NS_SCALE_X = 4096.0f, NS_SCALE_A = 2048.0f, NS_SCALE_B = 1024.0f;
@@ -38,6 +37,9 @@ __device__ __forceinline__ void ns_split(float x, _Float16& hi, _Float16& lo)
     lo = (_Float16)(x - (float)hi);
 }
 __device__ __forceinline__ int64_t ns_at(int64_t row, int col, int64_t pitch) { return row * pitch + (col >> 5) * NS_KHALVES + (col & 31); }
+
+// What an update is multiplied by; a zero update stays zero.
+__device__ __forceinline__ double ns_inverse(double norm) { return norm == 0.0 ? 0.0 : (double)NS_SCALE_X / norm; }
 
 template <typename T> __device__ __forceinline__ float ns_load(const T* p);
 template <> __device__ __forceinline__ float ns_load<float>(const float* p) { return *p; }
@@ -58,24 +60,37 @@ struct UpdateArgs {
 };
 
 // First pass over the update: the squares' partial sums (binary64: no square of a binary32 number overflows or vanishes), and the momentum.
+// Elements go to threads in runs of columns of one row; eight rows are on their way at once.
 template <typename T>
 __global__ __launch_bounds__(NS_TPB) void rb_ortho_norm_kernel(const UpdateArgs a, double* parts)
 {
+    constexpr int AT_ONCE = 8;
     __shared__ double sums[NS_TPB / 64];
     const int64_t k = blockIdx.y;
     const T* g = static_cast<const T*>(a.grad) + k * a.matrix_stride;
     float* mom = a.momentum != nullptr ? a.momentum + k * a.m * (int64_t)a.n : nullptr;
     double sum = 0.0;
-    for (int i = blockIdx.x; i < a.m; i += gridDim.x) {
-        for (int j = threadIdx.x; j < a.n; j += NS_TPB) {
-            float u = ns_load(g + i * a.row_stride + j);
-            if (mom != nullptr) {
-                const float v = fmaf(a.beta, mom[(int64_t)i * a.n + j], u);
-                mom[(int64_t)i * a.n + j] = v;
-                u = a.nesterov ? fmaf(a.beta, v, u) : v;
+    const int spans = (a.n + NS_TPB - 1) / NS_TPB;                       // a row in spans of a workgroup's width
+    const int64_t items = (int64_t)((a.m + AT_ONCE - 1) / AT_ONCE) * spans;
+    for (int64_t it = blockIdx.x; it < items; it += gridDim.x) {
+        const int i0 = (int)(it / spans) * AT_ONCE, j = (int)(it % spans) * NS_TPB + threadIdx.x;
+        if (j >= a.n) continue;
+        float u[AT_ONCE];
+#pragma unroll
+        for (int e = 0; e < AT_ONCE; ++e) u[e] = i0 + e < a.m ? ns_load(g + (i0 + e) * a.row_stride + j) : 0.0f;
+        if (mom != nullptr) {
+            float v[AT_ONCE];
+#pragma unroll
+            for (int e = 0; e < AT_ONCE; ++e) v[e] = i0 + e < a.m ? mom[(int64_t)(i0 + e) * a.n + j] : 0.0f;
+#pragma unroll
+            for (int e = 0; e < AT_ONCE; ++e) {
+                v[e] = fmaf(a.beta, v[e], u[e]);
+                if (i0 + e < a.m) mom[(int64_t)(i0 + e) * a.n + j] = v[e];
+                u[e] = a.nesterov ? fmaf(a.beta, v[e], u[e]) : v[e];
             }
-            sum = fma((double)u, (double)u, sum);
         }
+#pragma unroll
+        for (int e = 0; e < AT_ONCE; ++e) sum = fma((double)u[e], (double)u[e], sum);
     }
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
@@ -97,13 +112,15 @@ __global__ __launch_bounds__(NS_TPB) void rb_ortho_split_kernel(const UpdateArgs
     __shared__ float tile[64][65];
     __shared__ double sums[NS_TPB / 64];
     const int64_t k = blockIdx.z;
-    double sum = (int)threadIdx.x < nparts ? parts[k * NS_PARTS + threadIdx.x] : 0.0;
+    double sum = 0.0;
+#pragma unroll
+    for (int i = 0; i < NS_PARTS / NS_TPB; ++i)
+        if ((int)threadIdx.x + i * NS_TPB < nparts) sum += parts[k * NS_PARTS + threadIdx.x + i * NS_TPB];
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
     if ((threadIdx.x & 63) == 0) sums[threadIdx.x / 64] = sum;
     __syncthreads();
-    const double norm = sqrt((sums[0] + sums[1]) + (sums[2] + sums[3])) + (double)a.eps;
-    const double inverse = norm > 0.0 || norm != norm ? (double)NS_SCALE_X / norm : 0.0;      // a zero update stays zero
+    const double inverse = ns_inverse(sqrt((sums[0] + sums[1]) + (sums[2] + sums[3])) + (double)a.eps);
     // the tile in the caller's orientation: rows i0.., columns j0..
     const int r0 = blockIdx.y * 64, c0 = blockIdx.x * 64, i0 = a.tall ? c0 : r0, j0 = a.tall ? r0 : c0;
     const T* g = static_cast<const T*>(a.grad) + k * a.matrix_stride;
@@ -139,6 +156,38 @@ __global__ __launch_bounds__(NS_TPB) void rb_ortho_split_kernel(const UpdateArgs
     }
 }
 
+// Where the result goes.
+struct ResultArgs {
+    void* dst;
+    int64_t matrix_stride, row_stride;      // elements
+    int32_t rows, cols, tall;               // of the kept X, and whether the caller has its transpose
+    int32_t update;                         // dst <- keep * dst - gain * result
+    float keep, gain;
+};
+
+// 16 numbers of a lane to their places: all that is read of them first (an update), then all that is written.
+template <typename OUT>
+__device__ __forceinline__ void ns_result(const ResultArgs& a, OUT* dst, const int* r, const int* c, float* v)
+{
+    int64_t at[16];
+    bool there[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        there[i] = r[i] < a.rows && c[i] < a.cols;
+        at[i] = a.tall ? c[i] * a.row_stride + r[i] : r[i] * a.row_stride + c[i];
+    }
+    if (a.update) {
+        float w[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) w[i] = there[i] ? ns_load(dst + at[i]) : 0.0f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] = a.keep * w[i] - a.gain * v[i];
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+        if (there[i]) ns_store(dst + at[i], v[i]);
+}
+
 enum { NS_GRAM = 0, NS_POLY = 1, NS_APPLY = 2, NS_LAST = 3 };
 
 struct ProductArgs {
@@ -150,146 +199,421 @@ struct ProductArgs {
     _Float16 *out, *out_t;                  // the result and its transpose, as hi and lo
     int64_t out_matrix, out_t_matrix, out_pitch, out_t_pitch;
     float alpha, beta;                      // result = alpha * old + beta * product, in the scales of what is kept
-    // LAST: the caller's result
-    void* dst;
-    int64_t dst_matrix, dst_row;
-    int32_t m, n, tall;                     // of the kept X, and whether the caller has its transpose
-    int32_t update;                         // dst <- keep * dst - gain * result
-    float keep, gain;
+    ResultArgs result;                      // LAST
 };
 
-// C = P Q^T of one tile of 128 x 128; a wavefront has 64 x 64 of it as 2 x 2 blocks of 32 x 32.
-template <int KIND, typename OUT>
-__global__ __launch_bounds__(NS_TPB, 2) void rb_ortho_product_kernel(const ProductArgs a)
+// Asynchronous loads into LDS.  The wavefront's 64 lanes bring 16 bytes each, which land behind each other from `to` on.
+__device__ __forceinline__ void ns_load_to_lds(const char* from, char* to)
 {
-    __shared__ __align__(16) char lds[2][2 * NS_TILE * 128];
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (__attribute__((address_space(3))) void*)to, 16, 0, 0);
+}
+// Waits until at most COUNT of them are on their way and everything read from LDS is there, then for the workgroup's other wavefronts.
+template <int COUNT>
+__device__ __forceinline__ void ns_arrived()
+{
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(COUNT) : "memory");
+}
+
+// Which tile a workgroup has.  Workgroups go to the 8 dies in turn, and each die has its own L2: a die gets tiles that are neighbours, in groups
+// of 8 tile rows walked column by column, so that the panels it reads at a time are few.
+__device__ __forceinline__ int ns_rank(int id, int count)
+{
+    const int die = id & 7, whole = count >> 3, more = count & 7;
+    return die * whole + min(die, more) + (id >> 3);
+}
+constexpr int NS_GROUP = 8;
+__device__ __forceinline__ void ns_tile_of(int t, int rows, int cols, int& ti, int& tj)
+{
+    const int g = t / (NS_GROUP * cols), first = g * NS_GROUP, height = min(NS_GROUP, rows - first);
+    t -= g * NS_GROUP * cols;
+    ti = first + t % height;
+    tj = t / height;
+}
+__device__ __forceinline__ void ns_tile_above(int t, int rows, int& ti, int& tj)          // on and above the diagonal only
+{
+    for (int first = 0;; first += NS_GROUP) {
+        const int height = min(NS_GROUP, rows - first), corner = height * (height + 1) / 2, count = corner + (rows - first - height) * height;
+        if (t < count) {
+            int col = 0;
+            if (t < corner) {
+                while (t > col) t -= ++col;
+                ti = first + t;
+            } else {
+                t -= corner;
+                ti = first + t % height;
+                col = height + t / height;
+            }
+            tj = first + col;
+            return;
+        }
+        t -= count;
+    }
+}
+
+// C = P Q^T of one tile of BM x BN (BM = BN or 2 BN); a wavefront has WM x WN of it in blocks of 32 x 32.  A block of 32 of the summed index
+// is (BM + BN) lines of 128 bytes; STAGES of them are in LDS or on their way there.
+template <int KIND, typename OUT, int BM, int BN, int WM, int WN, int STAGES, int WAVES_PER_SIMD>
+__global__ __launch_bounds__((BM / WM) * (BN / WN) * 64, WAVES_PER_SIMD) void rb_ortho_product_kernel(const ProductArgs a)
+{
+    constexpr int WAVES = (BM / WM) * (BN / WN), MI = WM / 32, MJ = WN / 32;
+    constexpr int STAGE = (BM + BN) * 128, PIECES = (BM + BN) / 8, PER_WAVE = PIECES / WAVES;
+    static_assert(PIECES % WAVES == 0 && BM % 8 == 0, "whole pieces of 8 lines per wavefront");
+    extern __shared__ __align__(16) char lds[];
     const int64_t k = blockIdx.y;
+    constexpr int SUB = BM / BN;
+    const int t = ns_rank(blockIdx.x, gridDim.x);
     int ti, tj;
     if (KIND == NS_GRAM || KIND == NS_POLY) {
-        // tiles on and above the diagonal, row by row
-        int t = blockIdx.x;
-        ti = 0;
-        while (t >= a.tiles_j - ti) {
-            t -= a.tiles_j - ti;
-            ++ti;
-        }
-        tj = ti + t;
+        ns_tile_above(t / SUB, a.tiles_i, ti, tj);
+        tj = tj * SUB + t % SUB;
     } else {
-        ti = blockIdx.x / a.tiles_j;
-        tj = blockIdx.x % a.tiles_j;
+        ns_tile_of(t, a.tiles_i, a.tiles_j, ti, tj);
     }
-    const int wave = threadIdx.x / 64, lane = threadIdx.x & 63;
-    const int wi = (wave >> 1) * 64, wj = (wave & 1) * 64;
-    const int64_t pitch = (int64_t)a.kblocks * NS_KHALVES;
-    const _Float16* p = a.p + k * a.p_matrix + (int64_t)ti * NS_TILE * pitch;
-    const _Float16* q = a.q + k * a.q_matrix + (int64_t)tj * NS_TILE * pitch;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x & 63;
+    const int wi = (wave / (BN / WN)) * WM, wj = (wave % (BN / WN)) * WN;
+    const int64_t pitch = (int64_t)a.kblocks * NS_KHALVES * 2;          // bytes
+    const char* p = reinterpret_cast<const char*>(a.p + k * a.p_matrix) + (int64_t)ti * BM * pitch;
+    const char* q = reinterpret_cast<const char*>(a.q + k * a.q_matrix) + (int64_t)tj * BN * pitch;
 
-    // 2048 pieces of 16 bytes per block of both operands, eight per thread
-    const int piece_row = threadIdx.x / 8, piece = threadIdx.x % 8;
-    const _Float16* src_p = p + piece_row * pitch + piece * 8;
-    const _Float16* src_q = q + piece_row * pitch + piece * 8;
-    const int dst = piece_row * 128 + ((piece ^ (piece_row & 7)) * 16);
-    ns_vec stage_p[4], stage_q[4];
-    auto fetch = [&](int block) {
+    // A piece is 8 lines; the 16-byte part c of line r stands at place c ^ (r & 7) of its line in LDS, so that 8 lanes that read one part of
+    // 8 lines read all banks once.
+    const uint32_t lane_offset = (uint32_t)((lane >> 3) * pitch) + (((lane & 7) ^ (lane >> 3)) * 16);
+    auto fetch = [&](int block, int stage) {
 #pragma unroll
-        for (int s = 0; s < 4; ++s) {
-            stage_p[s] = *reinterpret_cast<const ns_vec*>(src_p + block * NS_KHALVES + s * 32 * pitch);
-            stage_q[s] = *reinterpret_cast<const ns_vec*>(src_q + block * NS_KHALVES + s * 32 * pitch);
-        }
-    };
-    auto put = [&](int to) {
-#pragma unroll
-        for (int s = 0; s < 4; ++s) {
-            *reinterpret_cast<ns_vec*>(lds[to] + dst + s * 32 * 128) = stage_p[s];
-            *reinterpret_cast<ns_vec*>(lds[to] + NS_TILE * 128 + dst + s * 32 * 128) = stage_q[s];
+        for (int i = 0; i < PER_WAVE; ++i) {
+            const int piece = wave * PER_WAVE + i;
+            const char* from = (piece < BM / 8 ? p + (int64_t)piece * 8 * pitch : q + (int64_t)(piece - BM / 8) * 8 * pitch) + (int64_t)block * 128;
+            ns_load_to_lds(from + lane_offset, lds + stage * STAGE + piece * 1024);
         }
     };
 
-    float16v acc[2][2] = {};
-    fetch(0);
-    put(0);
-    __syncthreads();
+    // The fragments of 16 of the summed index: a lane has 8 of them of row lane % 32 of every block, hi and lo.
+    struct Fragments { half8 ph[MI], pl[MI], qh[MJ], ql[MJ]; };
+    const int row = lane & 31;
+    auto read = [&](Fragments& f, int stage, int ks) {
+        const int c = ks * 2 + lane / 32, hi = (c ^ (row & 7)) * 16, lo = ((c + 4) ^ (row & 7)) * 16;
+        const char* at = lds + stage * STAGE;
+#pragma unroll
+        for (int b = 0; b < MI; ++b) {
+            f.ph[b] = *reinterpret_cast<const half8*>(at + (wi + b * 32 + row) * 128 + hi);
+            f.pl[b] = *reinterpret_cast<const half8*>(at + (wi + b * 32 + row) * 128 + lo);
+        }
+#pragma unroll
+        for (int b = 0; b < MJ; ++b) {
+            f.qh[b] = *reinterpret_cast<const half8*>(at + (BM + wj + b * 32 + row) * 128 + hi);
+            f.ql[b] = *reinterpret_cast<const half8*>(at + (BM + wj + b * 32 + row) * 128 + lo);
+        }
+    };
+    float16v acc[MI][MJ] = {};
+    auto multiply = [&](const Fragments& f) {
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+#pragma unroll
+            for (int j = 0; j < MJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f.pl[i], f.qh[j], acc[i][j], 0, 0, 0);
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+#pragma unroll
+            for (int j = 0; j < MJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f.ph[i], f.ql[j], acc[i][j], 0, 0, 0);
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+#pragma unroll
+            for (int j = 0; j < MJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f.ph[i], f.qh[j], acc[i][j], 0, 0, 0);
+    };
+
+    // While the second half of a block is multiplied the next block's first half is read, and its second half while that is multiplied; a block's
+    // place is free for the block STAGES further on as soon as all wavefronts have read its second half.
+#pragma unroll
+    for (int s = 0; s < STAGES; ++s)
+        if (s < a.kblocks) fetch(s, s);
+    if (a.kblocks >= STAGES)
+        ns_arrived<PER_WAVE * (STAGES - 1)>();
+    else
+        ns_arrived<0>();
+    Fragments first, second;
+    read(first, 0, 0);
+    int stage = 0;
     for (int block = 0; block < a.kblocks; ++block) {
-        const bool more = block + 1 < a.kblocks;
-        if (more) fetch(block + 1);
-        const char* at = lds[block & 1];
-#pragma unroll
-        for (int ks = 0; ks < 2; ++ks) {
-            half8 ph[2], pl[2], qh[2], ql[2];
-            const int row = lane & 31, c = ks * 2 + lane / 32;
-            const int hi = ((c ^ (row & 7)) * 16), lo = (((c + 4) ^ (row & 7)) * 16);
-#pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                const char* pr = at + (wi + b * 32 + row) * 128;
-                const char* qr = at + NS_TILE * 128 + (wj + b * 32 + row) * 128;
-                ph[b] = *reinterpret_cast<const half8*>(pr + hi);
-                pl[b] = *reinterpret_cast<const half8*>(pr + lo);
-                qh[b] = *reinterpret_cast<const half8*>(qr + hi);
-                ql[b] = *reinterpret_cast<const half8*>(qr + lo);
-            }
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(pl[i], qh[j], acc[i][j], 0, 0, 0);
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph[i], ql[j], acc[i][j], 0, 0, 0);
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph[i], qh[j], acc[i][j], 0, 0, 0);
-                }
+        read(second, stage, 1);
+        multiply(first);
+        const int next = stage + 1 == STAGES ? 0 : stage + 1;
+        if (block + STAGES < a.kblocks) {
+            ns_arrived<PER_WAVE * (STAGES - 2)>();
+            fetch(block + STAGES, stage);
+        } else {
+            ns_arrived<0>();
         }
-        if (more) put((block + 1) & 1);
-        __syncthreads();
+        if (block + 1 < a.kblocks) read(first, next, 0);
+        multiply(second);
+        stage = next;
     }
 
-    // Block element i of a lane: row 8 (i / 4) + 4 (lane / 32) + i % 4, column lane % 32.
-    const bool mirror = (KIND == NS_GRAM || KIND == NS_POLY) ? ti != tj : true;
-    const _Float16* old = a.old + k * a.old_matrix;
-    _Float16* out = a.out + k * a.out_matrix;
-    _Float16* out_t = a.out_t + k * a.out_t_matrix;
+    // The result.  Block element i of a lane: row 8 (i / 4) + 4 (lane / 32) + i % 4, column lane % 32.  A block of 32 x 32 is 32 lines of 128 bytes
+    // in the kept matrix, and 32 in its transpose: they are put together in LDS (each wavefront has a place of its own, lines 144 bytes apart),
+    // and stored 16 bytes a lane.
+    constexpr int PITCH = 144;
+    static_assert(WAVES * 32 * PITCH <= STAGES * STAGE, "the places fit what the stages leave");
+    char* mine = lds + wave * (32 * PITCH);
+    const int half = lane / 32, col = lane & 31, line = lane >> 3, part = (lane & 7) * 16;
+    const bool mirror = (KIND == NS_GRAM || KIND == NS_POLY) ? tj >= (ti + 1) * SUB : true;
+    // what is added lies transposed (A is symmetric): the four rows of a lane's column are neighbours there
+    // (all of it at once while that is four blocks, a row of blocks at a time of a larger tile, which would not fit the registers)
+    constexpr int AHEAD = KIND == NS_GRAM ? 0 : MI * MJ <= 4 ? MI : 1;
+    ns_vec old[AHEAD ? AHEAD : 1][MJ][4];
+    auto fetch_old = [&](int bi, ns_vec (*to)[4]) {
+        const _Float16* from = a.old + k * a.old_matrix;
 #pragma unroll
-    for (int bi = 0; bi < 2; ++bi)
+        for (int bj = 0; bj < MJ; ++bj)
 #pragma unroll
-        for (int bj = 0; bj < 2; ++bj)
+            for (int l = 0; l < 4; ++l)
+                to[bj][l] = *reinterpret_cast<const ns_vec*>(reinterpret_cast<const char*>(
+                    from + ns_at(tj * BN + wj + bj * 32 + l * 8 + line, ti * BM + wi + bi * 32, a.old_pitch)) + part);
+    };
+#pragma unroll
+    for (int bi = 0; bi < AHEAD; ++bi) fetch_old(bi, old[bi]);
+#pragma unroll
+    for (int bi = 0; bi < MI; ++bi) {
+        if (AHEAD == 1 && bi > 0) fetch_old(bi, old[0]);
+#pragma unroll
+        for (int bj = 0; bj < MJ; ++bj) {
+            const int r0 = ti * BM + wi + bi * 32, c0 = tj * BN + wj + bj * 32;
+            float v[16];
+            if (KIND != NS_GRAM) {
+#pragma unroll
+                for (int l = 0; l < 4; ++l) *reinterpret_cast<ns_vec*>(mine + (l * 8 + line) * PITCH + part) = old[AHEAD > 1 ? bi : 0][bj][l];
+                sc_lds_wait();
+            }
+            half4 hi[4], lo[4];
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
-                const int r = ti * NS_TILE + wi + bi * 32 + g * 8 + (lane / 32) * 4, c = tj * NS_TILE + wj + bj * 32 + (lane & 31);
-                float v[4];
-                half4 hi, lo;
                 if (KIND != NS_GRAM) {
-                    // what is added lies transposed (A is symmetric): four rows of this column are neighbours there
-                    const int64_t o = ns_at(c, r, a.old_pitch);
-                    hi = *reinterpret_cast<const half4*>(old + o);
-                    lo = *reinterpret_cast<const half4*>(old + o + NS_KBLOCK);
+                    hi[g] = *reinterpret_cast<const half4*>(mine + col * PITCH + (g * 8 + half * 4) * 2);
+                    lo[g] = *reinterpret_cast<const half4*>(mine + col * PITCH + (g * 8 + half * 4) * 2 + 64);
                 }
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    v[e] = a.beta * acc[bi][bj][g * 4 + e];
-                    if (KIND != NS_GRAM) v[e] = fmaf(a.alpha, (float)hi[e] + (float)lo[e], v[e]);
+                    v[g * 4 + e] = a.beta * acc[bi][bj][g * 4 + e];
+                    if (KIND != NS_GRAM) v[g * 4 + e] = fmaf(a.alpha, (float)hi[g][e] + (float)lo[g][e], v[g * 4 + e]);
                 }
-                if (KIND == NS_LAST) {
+            }
+            if (KIND == NS_LAST) {
+                // 32 numbers of a row of what the caller has, by half a wavefront
+                if (a.result.tall) {
+                    sc_lds_wait();
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        if (r + e >= a.m || c >= a.n) continue;
-                        OUT* d = static_cast<OUT*>(a.dst) + k * a.dst_matrix + (a.tall ? c * a.dst_row + r + e : (r + e) * a.dst_row + c);
-                        ns_store(d, a.update ? a.keep * ns_load(d) - a.gain * v[e] : v[e]);
-                    }
-                    continue;
+                    for (int g = 0; g < 4; ++g) *reinterpret_cast<float4*>(mine + col * PITCH + (g * 8 + half * 4) * 4) = float4{v[g * 4], v[g * 4 + 1], v[g * 4 + 2], v[g * 4 + 3]};
+                    sc_lds_wait();
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) v[i] = *reinterpret_cast<const float*>(mine + (2 * i + half) * PITCH + col * 4);
+                    sc_lds_wait();
                 }
+                int r[16], c[16];
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    r[i] = r0 + (a.result.tall ? col : (i / 4) * 8 + half * 4 + i % 4);
+                    c[i] = c0 + (a.result.tall ? 2 * i + half : col);
+                }
+                ns_result(a.result, static_cast<OUT*>(a.result.dst) + k * a.result.matrix_stride, r, c, v);
+                continue;
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                _Float16 h, l;
+                ns_split(v[i], h, l);
+                hi[i / 4][i % 4] = h;
+                lo[i / 4][i % 4] = l;
+            }
+            if (mirror) {
+                char* to = reinterpret_cast<char*>(a.out_t + k * a.out_t_matrix + ns_at(c0 + line, r0, a.out_t_pitch)) + part;
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    *reinterpret_cast<half4*>(mine + col * PITCH + (g * 8 + half * 4) * 2) = hi[g];
+                    *reinterpret_cast<half4*>(mine + col * PITCH + (g * 8 + half * 4) * 2 + 64) = lo[g];
+                }
+                sc_lds_wait();
+#pragma unroll
+                for (int l = 0; l < 4; ++l) *reinterpret_cast<ns_vec*>(to + l * 8 * a.out_t_pitch * 2) = *reinterpret_cast<const ns_vec*>(mine + (l * 8 + line) * PITCH + part);
+                sc_lds_wait();
+            }
+            char* to = reinterpret_cast<char*>(a.out + k * a.out_matrix + ns_at(r0 + line, c0, a.out_pitch)) + part;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                _Float16* at = reinterpret_cast<_Float16*>(mine + ((i / 4) * 8 + half * 4 + i % 4) * PITCH) + col;
+                at[0] = hi[i / 4][i % 4];
+                at[NS_KBLOCK] = lo[i / 4][i % 4];
+            }
+            sc_lds_wait();
+#pragma unroll
+            for (int l = 0; l < 4; ++l) *reinterpret_cast<ns_vec*>(to + l * 8 * a.out_pitch * 2) = *reinterpret_cast<const ns_vec*>(mine + (l * 8 + line) * PITCH + part);
+            sc_lds_wait();
+        }
+    }
+}
+
+// A whole matrix of up to P x P by one workgroup, in LDS: X, or A, or B in one half of it, X^T in the other; X itself in registers, a wavefront
+// has 32 x WN of it.  One launch from the update to the result.
+struct SmallArgs {
+    UpdateArgs update;
+    ResultArgs result;
+    int32_t steps;
+    float coefficients[16][3];
+};
+
+template <typename T, typename OUT, int P, int WN>
+__global__ __launch_bounds__(P / 32 * (P / WN) * 64) void rb_ortho_small_kernel(const SmallArgs a)
+{
+    constexpr int WAVES = P / 32 * (P / WN), MJ = WN / 32, LINES = P / 32;
+    extern __shared__ __align__(16) char lds[];
+    __shared__ double sums[WAVES];
+    char* const one = lds;                      // X, A, B: line (row, block of 32 columns), its 16-byte parts at c ^ (row & 7)
+    char* const two = lds + P * LINES * 128;    // X^T
+    const int64_t k = blockIdx.x;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x & 63, half = lane / 32, col = lane & 31;
+    const int wi = wave / (P / WN) * 32, wj = wave % (P / WN) * WN;
+    const UpdateArgs& u = a.update;
+    const int rows = a.result.rows, cols = a.result.cols;
+
+    float x[MJ][16];
+    double sum = 0.0;
+    const T* grad = static_cast<const T*>(u.grad) + k * u.matrix_stride;
+    float* mom = u.momentum != nullptr ? u.momentum + k * u.m * (int64_t)u.n : nullptr;
+#pragma unroll
+    for (int b = 0; b < MJ; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int r = wi + (i / 4) * 8 + half * 4 + i % 4, c = wj + b * 32 + col;
+            const int ci = u.tall ? c : r, cj = u.tall ? r : c;
+            x[b][i] = r < rows && c < cols ? ns_load(grad + ci * u.row_stride + cj) : 0.0f;
+        }
+    if (mom != nullptr) {
+#pragma unroll
+        for (int b = 0; b < MJ; ++b) {
+            float v[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int r = wi + (i / 4) * 8 + half * 4 + i % 4, c = wj + b * 32 + col;
+                const int ci = u.tall ? c : r, cj = u.tall ? r : c;
+                v[i] = r < rows && c < cols ? mom[(int64_t)ci * u.n + cj] : 0.0f;
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int r = wi + (i / 4) * 8 + half * 4 + i % 4, c = wj + b * 32 + col;
+                const int ci = u.tall ? c : r, cj = u.tall ? r : c;
+                v[i] = fmaf(u.beta, v[i], x[b][i]);
+                if (r < rows && c < cols) mom[(int64_t)ci * u.n + cj] = v[i];
+                x[b][i] = u.nesterov ? fmaf(u.beta, v[i], x[b][i]) : v[i];
+            }
+        }
+    }
+#pragma unroll
+    for (int b = 0; b < MJ; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sum = fma((double)x[b][i], (double)x[b][i], sum);
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
+    if (lane == 0) sums[wave] = sum;
+    __syncthreads();
+    sum = 0.0;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) sum += sums[w];
+    const double inverse = ns_inverse(sqrt(sum) + (double)u.eps);
+#pragma unroll
+    for (int b = 0; b < MJ; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[b][i] = (float)((double)x[b][i] * inverse);
+
+    auto part = [&](char* area, int row, int column) {          // of element (row, column): hi; lo is 4 parts on
+        return area + (row * LINES + column / 32) * 128 + (((column % 32 / 8) ^ (row & 7)) * 16) + column % 8 * 2;
+    };
+    auto part_lo = [&](char* area, int row, int column) {
+        return area + (row * LINES + column / 32) * 128 + (((column % 32 / 8 + 4) ^ (row & 7)) * 16) + column % 8 * 2;
+    };
+    // v, scaled already, to the transposed place (4 rows of a column are neighbours there), and to its own
+    auto put = [&](char* across, char* along, const float (*v)[16]) {
+#pragma unroll
+        for (int b = 0; b < MJ; ++b)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const int r = wi + g * 8 + half * 4, c = wj + b * 32 + col;
+                half4 hi, lo;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     _Float16 h, l;
-                    ns_split(v[e], h, l);
+                    ns_split(v[b][g * 4 + e], h, l);
                     hi[e] = h;
                     lo[e] = l;
-                    const int64_t o = ns_at(r + e, c, a.out_pitch);
-                    out[o] = h;
-                    out[o + NS_KBLOCK] = l;
+                    if (along != nullptr) {
+                        *reinterpret_cast<_Float16*>(part(along, r + e, c)) = h;
+                        *reinterpret_cast<_Float16*>(part_lo(along, r + e, c)) = l;
+                    }
                 }
-                if (mirror) {
-                    const int64_t o = ns_at(c, r, a.out_t_pitch);
-                    *reinterpret_cast<half4*>(out_t + o) = hi;
-                    *reinterpret_cast<half4*>(out_t + o + NS_KBLOCK) = lo;
-                }
+                *reinterpret_cast<half4*>(part(across, c, r)) = hi;
+                *reinterpret_cast<half4*>(part_lo(across, c, r)) = lo;
             }
+    };
+    float16v acc[MJ];
+    auto product = [&](const char* p, const char* q, int blocks) {
+#pragma unroll
+        for (int b = 0; b < MJ; ++b) acc[b] = float16v{};
+        for (int ks = 0; ks < 2 * blocks; ++ks) {
+            const int c = (ks & 1) * 2 + half, hi = (c ^ (col & 7)) * 16, lo = ((c + 4) ^ (col & 7)) * 16;
+            const char* pr = p + ((wi + col) * LINES + ks / 2) * 128;
+            const half8 ph = *reinterpret_cast<const half8*>(pr + hi), pl = *reinterpret_cast<const half8*>(pr + lo);
+#pragma unroll
+            for (int b = 0; b < MJ; ++b) {
+                const char* qr = q + ((wj + b * 32 + col) * LINES + ks / 2) * 128;
+                const half8 qh = *reinterpret_cast<const half8*>(qr + hi), ql = *reinterpret_cast<const half8*>(qr + lo);
+                acc[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(pl, qh, acc[b], 0, 0, 0);
+                acc[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph, ql, acc[b], 0, 0, 0);
+                acc[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph, qh, acc[b], 0, 0, 0);
+            }
+        }
+    };
+
+    const int row_blocks = (rows + 31) / 32, col_blocks = (cols + 31) / 32;
+    put(two, one, x);
+    __syncthreads();
+    for (int s = 0; s < a.steps; ++s) {
+        const float ca = a.coefficients[s][0], cb = a.coefficients[s][1], cc = a.coefficients[s][2];
+        float v[MJ][16];
+        product(one, one, col_blocks);                          // A
+#pragma unroll
+        for (int b = 0; b < MJ; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) v[b][i] = acc[b][i] * (NS_SCALE_A / (NS_SCALE_X * NS_SCALE_X));
+        __syncthreads();
+        put(one, nullptr, v);
+        __syncthreads();
+        product(one, one, row_blocks);                          // B = b A + c A A
+#pragma unroll
+        for (int b = 0; b < MJ; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                v[b][i] = fmaf(cb * (NS_SCALE_B / NS_SCALE_A), v[b][i], cc * (NS_SCALE_B / (NS_SCALE_A * NS_SCALE_A)) * acc[b][i]);
+        __syncthreads();
+        put(one, nullptr, v);
+        __syncthreads();
+        product(one, two, row_blocks);                          // X <- a X + B X
+#pragma unroll
+        for (int b = 0; b < MJ; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[b][i] = fmaf(ca, x[b][i], acc[b][i] * (1.0f / NS_SCALE_B));
+        if (s + 1 == a.steps) break;
+        __syncthreads();
+        put(two, one, x);
+        __syncthreads();
+    }
+    OUT* dst = static_cast<OUT*>(a.result.dst) + k * a.result.matrix_stride;
+#pragma unroll
+    for (int b = 0; b < MJ; ++b) {
+        int r[16], c[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            r[i] = wi + (i / 4) * 8 + half * 4 + i % 4;
+            c[i] = wj + b * 32 + col;
+            x[b][i] *= 1.0f / NS_SCALE_X;
+        }
+        ns_result(a.result, dst, r, c, x[b]);
+    }
 }
 
 }  // namespace

@@ -171,42 +171,110 @@ struct rb_ortho {
     float eps;
     bool tall;
     int32_t rows, cols;            // of the kept X: short and long side
-    int32_t prows, pcols;          // padded to whole tiles
+    int32_t small;                 // a workgroup per matrix: its padded side (64, 128), or 0: tiled products
+    int32_t prows, pcols;          // tiled: padded to whole tiles
+    int32_t tile[3];               // of A, of B, of X
     size_t off_x, off_xt[2], off_a, off_b, bytes;
     char* ws;
 };
 
 namespace {
 
-struct OrthoOut {
-    void* dst;
-    int64_t matrix_stride, row_stride;
-    int32_t update;
-    float keep, gain;
-};
-
-template <int KIND>
-hipError_t product(const rb_ortho* o, const ProductArgs& a, bool symmetric, hipStream_t st)
+// Tiles of a product: 64 x 64 by 4 wavefronts, 128 x 128 by 8, 256 x 256 by 8.
+template <int KIND, typename OUT, int BM, int WM, int WN, int STAGES, int WAVES_PER_SIMD>
+hipError_t product_of(const ProductArgs& a, unsigned tiles, unsigned matrices, hipStream_t st)
 {
-    const int64_t tiles = symmetric ? (int64_t)a.tiles_i * (a.tiles_i + 1) / 2 : (int64_t)a.tiles_i * a.tiles_j;
-    const dim3 grid((unsigned)tiles, (unsigned)o->matrices);
-    if (KIND == NS_LAST && o->out_dtype == RB_BF16) return launch(rb_ortho_product_kernel<KIND, Bf16>, grid, NS_TPB, 0, st, a);
-    return launch(rb_ortho_product_kernel<KIND, float>, grid, NS_TPB, 0, st, a);
+    return launch(rb_ortho_product_kernel<KIND, OUT, BM, BM, WM, WN, STAGES, WAVES_PER_SIMD>, dim3(tiles, matrices), BM / WM * (BM / WN) * 64,
+                  (size_t)STAGES * 2 * BM * 128, st, a);
+}
+
+template <int KIND, typename OUT>
+hipError_t product(const rb_ortho* o, ProductArgs a, int tile, bool symmetric, hipStream_t st)
+{
+    a.tiles_i = o->prows / tile;
+    a.tiles_j = (symmetric ? o->prows : o->pcols) / tile;
+    const unsigned tiles = symmetric ? (unsigned)a.tiles_i * (a.tiles_i + 1) / 2 : (unsigned)a.tiles_i * a.tiles_j, n = (unsigned)o->matrices;
+    switch (tile) {
+    case 256: return product_of<KIND, OUT, 256, 128, 64, 2, 2>(a, tiles, n, st);
+    case 128: return product_of<KIND, OUT, 128, 64, 32, 2, 4>(a, tiles, n, st);
+    default: return product_of<KIND, OUT, 64, 32, 32, 3, 3>(a, tiles, n, st);
+    }
+}
+
+// What a product takes, in us, by its tile, measured on 256 compute units: a launch with its epilogue, and a tile's block of 32 of the summed
+// index on a compute unit that has one workgroup (64: 0.25, 128: 0.51, 256: 2.1) or is full (two of 128 together 1.58, 256: 2.65).
+double product_us(int tile, double tiles, int kblocks)
+{
+    const double per = tiles / 256;
+    if (tile == 64) return 5 + kblocks * 0.25 * std::max(1.0, per);
+    if (tile == 128) {
+        const double pairs = std::floor(per / 2), rest = per - 2 * pairs;
+        return 8 + kblocks * (1.58 * pairs + (rest == 0 ? 0 : rest <= 1 ? 0.51 : 1.58));
+    }
+    return 15 + kblocks * (per <= 0.75 ? 2.1 : 2.65 * std::ceil(per));
+}
+
+// The padding and the three products' tiles that take least.
+void choose_tiles(rb_ortho* o)
+{
+    double best = 1e300;
+    for (int pad = 64; pad <= 256; pad *= 2) {
+        const int64_t R = (int64_t)round_up((size_t)o->rows, (size_t)pad), C = (int64_t)round_up((size_t)o->cols, (size_t)pad);
+        double total = 0;
+        int chosen[3] = {};
+        for (int kind = 0; kind < 3; ++kind) {
+            double least = 1e300;
+            for (int tile = 64; tile <= pad; tile *= 2) {
+                const double n = (double)(R / tile), tiles = (double)o->matrices * (kind < 2 ? n * (n + 1) / 2 : n * (double)(C / tile));
+                const double us = product_us(tile, tiles, (int)((kind == 0 ? C : R) / NS_KBLOCK));
+                if (us < least) {
+                    least = us;
+                    chosen[kind] = tile;
+                }
+            }
+            total += least;
+        }
+        if (total < best) {
+            best = total;
+            o->prows = (int32_t)R;
+            o->pcols = (int32_t)C;
+            for (int kind = 0; kind < 3; ++kind) o->tile[kind] = chosen[kind];
+        }
+    }
 }
 
 template <typename T>
 hipError_t first_pass(const rb_ortho* o, const UpdateArgs& u, const KeptArgs& q, hipStream_t st)
 {
     double* parts = reinterpret_cast<double*>(o->ws);
-    const int nparts = std::min<int32_t>(o->m, NS_PARTS);
+    const int64_t items = (int64_t)((o->m + 7) / 8) * ((o->n + NS_TPB - 1) / NS_TPB);
+    const int nparts = (int)std::min<int64_t>(items, NS_PARTS);
     hipError_t e = launch(rb_ortho_norm_kernel<T>, dim3((unsigned)nparts, (unsigned)o->matrices), NS_TPB, 0, st, u, parts);
     if (e != hipSuccess) return e;
     return launch(rb_ortho_split_kernel<T>, dim3((unsigned)(o->pcols / 64), (unsigned)(o->prows / 64), (unsigned)o->matrices), NS_TPB, 0, st, u, q,
                   static_cast<const double*>(parts), nparts);
 }
 
-hipError_t orthogonalize(const rb_ortho* o, const UpdateArgs& u, const OrthoOut& out, hipStream_t st)
+template <typename T, typename OUT>
+hipError_t whole(const rb_ortho* o, const UpdateArgs& u, const ResultArgs& result, hipStream_t st)
 {
+    SmallArgs a{};
+    a.update = u;
+    a.result = result;
+    a.steps = o->steps;
+    for (int s = 0; s < o->steps; ++s)
+        for (int i = 0; i < 3; ++i) a.coefficients[s][i] = o->coefficients[s][i];
+    const size_t lds = (size_t)2 * o->small * o->small * 4;
+    if (o->small == 64) return launch(rb_ortho_small_kernel<T, OUT, 64, 32>, dim3((unsigned)o->matrices), 256, lds, st, a);
+    return launch(rb_ortho_small_kernel<T, OUT, 128, 64>, dim3((unsigned)o->matrices), 512, lds, st, a);
+}
+
+hipError_t orthogonalize(const rb_ortho* o, const UpdateArgs& u, const ResultArgs& result, hipStream_t st)
+{
+    if (o->small) {
+        if (o->dtype == RB_F32) return o->out_dtype == RB_F32 ? whole<float, float>(o, u, result, st) : whole<float, Bf16>(o, u, result, st);
+        return o->out_dtype == RB_F32 ? whole<Bf16, float>(o, u, result, st) : whole<Bf16, Bf16>(o, u, result, st);
+    }
     const int64_t R = o->prows, C = o->pcols;
     _Float16* x = reinterpret_cast<_Float16*>(o->ws + o->off_x);
     _Float16* xt[2] = {reinterpret_cast<_Float16*>(o->ws + o->off_xt[0]), reinterpret_cast<_Float16*>(o->ws + o->off_xt[1])};
@@ -214,19 +282,16 @@ hipError_t orthogonalize(const rb_ortho* o, const UpdateArgs& u, const OrthoOut&
     _Float16* mb = reinterpret_cast<_Float16*>(o->ws + o->off_b);
     const KeptArgs kept{x, xt[0], 2 * R * C, 2 * R * C, (int32_t)R, (int32_t)C};
     hipError_t e = o->dtype == RB_F32 ? first_pass<float>(o, u, kept, st) : first_pass<Bf16>(o, u, kept, st);
-    const int ti = (int)(R / NS_TILE), tj = (int)(C / NS_TILE);
     for (int s = 0; s < o->steps && e == hipSuccess; ++s) {
-        const float *c = o->coefficients[s];
+        const float* c = o->coefficients[s];
         ProductArgs g{};                                   // A = X X^T
         g.p = x; g.q = x; g.p_matrix = g.q_matrix = 2 * R * C;
         g.kblocks = (int32_t)(C / NS_KBLOCK);
-        g.tiles_i = g.tiles_j = ti;
-        g.old = ma;
         g.out = ma; g.out_t = ma;
         g.out_matrix = g.out_t_matrix = 2 * R * R;
         g.out_pitch = g.out_t_pitch = 2 * R;
         g.beta = NS_SCALE_A / (NS_SCALE_X * NS_SCALE_X);
-        if ((e = product<NS_GRAM>(o, g, true, st)) != hipSuccess) break;
+        if ((e = product<NS_GRAM, float>(o, g, o->tile[0], true, st)) != hipSuccess) break;
         ProductArgs p = g;                                 // B = b A + c A A
         p.p = ma; p.q = ma; p.p_matrix = p.q_matrix = 2 * R * R;
         p.kblocks = (int32_t)(R / NS_KBLOCK);
@@ -234,27 +299,24 @@ hipError_t orthogonalize(const rb_ortho* o, const UpdateArgs& u, const OrthoOut&
         p.out = mb; p.out_t = mb;
         p.alpha = c[1] * (NS_SCALE_B / NS_SCALE_A);
         p.beta = c[2] * (NS_SCALE_B / (NS_SCALE_A * NS_SCALE_A));
-        if ((e = product<NS_POLY>(o, p, true, st)) != hipSuccess) break;
+        if ((e = product<NS_POLY, float>(o, p, o->tile[1], true, st)) != hipSuccess) break;
         ProductArgs q{};                                   // X <- a X + B X
         q.p = mb; q.p_matrix = 2 * R * R;
         q.q = xt[s & 1]; q.q_matrix = 2 * R * C;
         q.kblocks = (int32_t)(R / NS_KBLOCK);
-        q.tiles_i = ti; q.tiles_j = tj;
         q.old = xt[s & 1]; q.old_matrix = 2 * R * C; q.old_pitch = 2 * R;
         q.out = x; q.out_matrix = 2 * R * C; q.out_pitch = 2 * C;
         q.out_t = xt[(s + 1) & 1]; q.out_t_matrix = 2 * R * C; q.out_t_pitch = 2 * R;
         q.alpha = c[0];
         q.beta = 1.0f / NS_SCALE_B;
         if (s + 1 < o->steps) {
-            e = product<NS_APPLY>(o, q, false, st);
+            e = product<NS_APPLY, float>(o, q, o->tile[2], false, st);
             continue;
         }
         q.alpha = c[0] / NS_SCALE_X;
         q.beta = 1.0f / (NS_SCALE_B * NS_SCALE_X);
-        q.dst = out.dst; q.dst_matrix = out.matrix_stride; q.dst_row = out.row_stride;
-        q.m = o->rows; q.n = o->cols; q.tall = o->tall;
-        q.update = out.update; q.keep = out.keep; q.gain = out.gain;
-        e = product<NS_LAST>(o, q, false, st);
+        q.result = result;
+        e = o->out_dtype == RB_F32 ? product<NS_LAST, float>(o, q, o->tile[2], false, st) : product<NS_LAST, Bf16>(o, q, o->tile[2], false, st);
     }
     return e;
 }
@@ -279,8 +341,8 @@ int rb_ortho_create(rb_ortho** out, int64_t matrices, int64_t m, int64_t n, int3
     if (steps < 1 || steps > RB_MAX_ORTHO_STEPS || !std::isfinite(eps) || eps < 0.0f) return RB_EINVAL;
     for (int64_t i = 0; i < 3 * steps; ++i)
         if (!std::isfinite(coefficients[i])) return RB_EINVAL;
-    for (int i = 0; i <= 4096; ++i) {                      // where the steps lead the singular values (at most 1 at first)
-        double v = i / 4096.0;
+    for (int i = 0; i <= 1024; ++i) {                      // where the steps lead the singular values (at most 1 at first)
+        double v = i / 1024.0;
         for (int64_t s = 0; s < steps; ++s) {
             const double l = v * v, q = coefficients[3 * s + 1] * l + coefficients[3 * s + 2] * l * l;
             v *= coefficients[3 * s] + q;
@@ -300,16 +362,19 @@ int rb_ortho_create(rb_ortho** out, int64_t matrices, int64_t m, int64_t n, int3
     o->tall = m > n;
     o->rows = (int32_t)std::min(m, n);
     o->cols = (int32_t)std::max(m, n);
-    o->prows = (int32_t)round_up((size_t)o->rows, NS_TILE);
-    o->pcols = (int32_t)round_up((size_t)o->cols, NS_TILE);
-    const size_t kept = (size_t)matrices * o->prows * o->pcols * 4, square = (size_t)matrices * o->prows * o->prows * 4;
-    size_t off = round_up((size_t)matrices * NS_PARTS * sizeof(double), 256);
-    o->off_x = off; off += kept;
-    o->off_xt[0] = off; off += kept;
-    o->off_xt[1] = off; off += kept;
-    o->off_a = off; off += square;
-    o->off_b = off; off += square;
-    o->bytes = off;
+    o->small = o->cols <= 64 ? 64 : o->cols <= 128 ? 128 : 0;
+    o->bytes = 256;
+    if (!o->small) {
+        choose_tiles(o);
+        const size_t kept = (size_t)matrices * o->prows * o->pcols * 4, square = (size_t)matrices * o->prows * o->prows * 4;
+        size_t off = round_up((size_t)matrices * NS_PARTS * sizeof(double), 256);
+        o->off_x = off; off += kept;
+        o->off_xt[0] = off; off += kept;
+        o->off_xt[1] = off; off += kept;
+        o->off_a = off; off += square;
+        o->off_b = off; off += square;
+        o->bytes = off;
+    }
     *out = o;
     return RB_OK;
 }
@@ -336,7 +401,7 @@ int rb_ortho_apply(rb_ortho* o, const void* update, int64_t update_matrix_stride
     if (!strides_fit(o, update_matrix_stride, update_row_stride, false) || !strides_fit(o, out_matrix_stride, out_row_stride, true)) return RB_EINVAL;
     if (!o->ws) return RB_ESTATE;
     UpdateArgs u{update, update_matrix_stride, update_row_stride, nullptr, 0.0f, 0, o->m, o->n, o->tall, o->eps};
-    const OrthoOut w{out, out_matrix_stride, out_row_stride, 0, 0.0f, 0.0f};
+    const ResultArgs w{out, out_matrix_stride, out_row_stride, o->rows, o->cols, o->tall, 0, 0.0f, 0.0f};
     return orthogonalize(o, u, w, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? RB_OK : RB_EHIP;
 }
 
@@ -350,7 +415,8 @@ int rb_ortho_step(rb_ortho* o, void* weight, int64_t weight_matrix_stride, int64
     if (!std::isfinite(lr) || !std::isfinite(beta) || !std::isfinite(weight_decay) || !std::isfinite(scale)) return RB_EINVAL;
     if (!o->ws) return RB_ESTATE;
     UpdateArgs u{grad, grad_matrix_stride, grad_row_stride, momentum, beta, nesterov != 0, o->m, o->n, o->tall, o->eps};
-    const OrthoOut w{weight, weight_matrix_stride, weight_row_stride, 1, (float)(1.0 - (double)lr * weight_decay), (float)((double)lr * scale)};
+    const ResultArgs w{weight, weight_matrix_stride, weight_row_stride, o->rows, o->cols, o->tall, 1, (float)(1.0 - (double)lr * weight_decay),
+                       (float)((double)lr * scale)};
     return orthogonalize(o, u, w, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? RB_OK : RB_EHIP;
 }
 
