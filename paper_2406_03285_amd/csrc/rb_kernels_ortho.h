@@ -8,8 +8,9 @@
 // Every product is P Q^T of two row-major matrices with the summed index contiguous: X and X^T are both kept, A and B are symmetric, and of
 // the symmetric results only the tiles on and above the diagonal are computed, each written to its place and mirrored.
 //
-// A row of a kept matrix is cut into blocks of 32 elements, hi before lo: 128 bytes, one line of memory.  Matrices are padded with zeros
-// to whole tiles, so that products need no bounds.
+// A row of a kept matrix is cut into blocks of 32 elements, hi before lo: 128 bytes, one line of memory.  The matrices have room for whole
+// tiles, so that products need no bounds: what lies beyond the last row and column up to a multiple of 32 is zero (it starts so, and the
+// products keep it so); what lies beyond that is whatever it is, enters no sum and is in no result.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -26,6 +27,7 @@ typedef uint32_t ns_vec __attribute__((ext_vector_type(4)));
 constexpr int NS_TPB = 256;
 constexpr int NS_KBLOCK = 32;                  // elements of a block: hi, then lo
 constexpr int NS_KHALVES = 2 * NS_KBLOCK;
+constexpr int NS_ROWS_AT_ONCE = 4;             // rows a thread of the first pass has on their way
 constexpr int NS_PARTS = 1024;                 // most partial sums of a norm per matrix
 // What is kept is scaled by powers of two, so that lo is a normal binary16 number for elements of the size that occurs, and a singular
 // value of 4 (A: 16, B: 60) is still below 65504.
@@ -59,38 +61,68 @@ struct UpdateArgs {
     float eps;
 };
 
+// V neighbours of a row, V = 4 where all rows of all tensors are whole and aligned vectors, else 1.
+template <typename T, int V> struct Run;
+template <typename T> struct Run<T, 1> {
+    static __device__ __forceinline__ void load(const T* p, float* x) { x[0] = ns_load(p); }
+    static __device__ __forceinline__ void store(T* p, const float* x) { ns_store(p, x[0]); }
+};
+template <> struct Run<float, 4> {
+    static __device__ __forceinline__ void load(const float* p, float* x)
+    {
+        const float4 v = *reinterpret_cast<const float4*>(p);
+        x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
+    }
+    static __device__ __forceinline__ void store(float* p, const float* x) { *reinterpret_cast<float4*>(p) = float4{x[0], x[1], x[2], x[3]}; }
+};
+template <> struct Run<Bf16, 4> {
+    static __device__ __forceinline__ void load(const Bf16* p, float* x)
+    {
+        const uint2 v = *reinterpret_cast<const uint2*>(p);
+        x[0] = __uint_as_float(v.x << 16); x[1] = __uint_as_float(v.x & 0xffff0000u);
+        x[2] = __uint_as_float(v.y << 16); x[3] = __uint_as_float(v.y & 0xffff0000u);
+    }
+};
+
 // First pass over the update: the squares' partial sums (binary64: no square of a binary32 number overflows or vanishes), and the momentum.
-// Elements go to threads in runs of columns of one row; eight rows are on their way at once.
-template <typename T>
+// A thread has V neighbours of a row; some rows are on their way at once.
+template <typename T, int V>
 __global__ __launch_bounds__(NS_TPB) void rb_ortho_norm_kernel(const UpdateArgs a, double* parts)
 {
-    constexpr int AT_ONCE = 8;
+    constexpr int AT_ONCE = NS_ROWS_AT_ONCE;
     __shared__ double sums[NS_TPB / 64];
     const int64_t k = blockIdx.y;
     const T* g = static_cast<const T*>(a.grad) + k * a.matrix_stride;
     float* mom = a.momentum != nullptr ? a.momentum + k * a.m * (int64_t)a.n : nullptr;
     double sum = 0.0;
-    const int spans = (a.n + NS_TPB - 1) / NS_TPB;                       // a row in spans of a workgroup's width
+    // the matrix in pieces of AT_ONCE rows by V NS_TPB columns
+    const int spans = (a.n + V * NS_TPB - 1) / (V * NS_TPB);
     const int64_t items = (int64_t)((a.m + AT_ONCE - 1) / AT_ONCE) * spans;
     for (int64_t it = blockIdx.x; it < items; it += gridDim.x) {
-        const int i0 = (int)(it / spans) * AT_ONCE, j = (int)(it % spans) * NS_TPB + threadIdx.x;
+        const int i0 = (int)(it / spans) * AT_ONCE, j = ((int)(it % spans) * NS_TPB + threadIdx.x) * V;
         if (j >= a.n) continue;
-        float u[AT_ONCE];
+        float u[AT_ONCE][V] = {};
 #pragma unroll
-        for (int e = 0; e < AT_ONCE; ++e) u[e] = i0 + e < a.m ? ns_load(g + (i0 + e) * a.row_stride + j) : 0.0f;
+        for (int e = 0; e < AT_ONCE; ++e)
+            if (i0 + e < a.m) Run<T, V>::load(g + (i0 + e) * a.row_stride + j, u[e]);
         if (mom != nullptr) {
-            float v[AT_ONCE];
+            float v[AT_ONCE][V] = {};
 #pragma unroll
-            for (int e = 0; e < AT_ONCE; ++e) v[e] = i0 + e < a.m ? mom[(int64_t)(i0 + e) * a.n + j] : 0.0f;
+            for (int e = 0; e < AT_ONCE; ++e)
+                if (i0 + e < a.m) Run<float, V>::load(mom + (int64_t)(i0 + e) * a.n + j, v[e]);
 #pragma unroll
             for (int e = 0; e < AT_ONCE; ++e) {
-                v[e] = fmaf(a.beta, v[e], u[e]);
-                if (i0 + e < a.m) mom[(int64_t)(i0 + e) * a.n + j] = v[e];
-                u[e] = a.nesterov ? fmaf(a.beta, v[e], u[e]) : v[e];
+#pragma unroll
+                for (int x = 0; x < V; ++x) v[e][x] = fmaf(a.beta, v[e][x], u[e][x]);
+                if (i0 + e < a.m) Run<float, V>::store(mom + (int64_t)(i0 + e) * a.n + j, v[e]);
+#pragma unroll
+                for (int x = 0; x < V; ++x) u[e][x] = a.nesterov ? fmaf(a.beta, v[e][x], u[e][x]) : v[e][x];
             }
         }
 #pragma unroll
-        for (int e = 0; e < AT_ONCE; ++e) sum = fma((double)u[e], (double)u[e], sum);
+        for (int e = 0; e < AT_ONCE; ++e)
+#pragma unroll
+            for (int x = 0; x < V; ++x) sum = fma((double)u[e][x], (double)u[e][x], sum);
     }
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
@@ -102,16 +134,41 @@ __global__ __launch_bounds__(NS_TPB) void rb_ortho_norm_kernel(const UpdateArgs 
 struct KeptArgs {
     _Float16 *x, *xt;                       // X: rows x 2 cols halves, X^T: cols x 2 rows
     int64_t x_matrix, xt_matrix;            // halves between matrices
+    int64_t x_pitch, xt_pitch;              // halves between rows
     int32_t rows, cols;                     // padded
 };
 
-// Second pass: X and X^T, 64 x 64 elements per workgroup.
-template <typename T>
+// Halves between the rows of a kept matrix of so many columns: an odd number of lines, so that a tile's lines of one block do not all
+// begin at multiples of one power of two.
+__host__ __device__ inline int64_t ns_pitch(int64_t cols) { return (cols / NS_KBLOCK | 1) * NS_KHALVES; }
+
+// Second pass: X and X^T, 64 x 64 elements per workgroup, 8 neighbours of a row per thread and store.
+template <typename T, int V>
 __global__ __launch_bounds__(NS_TPB) void rb_ortho_split_kernel(const UpdateArgs a, const KeptArgs q, const double* parts, int32_t nparts)
 {
+    constexpr int ACROSS = 64 / V, ROWS = NS_TPB / ACROSS, ITEMS = 64 / ROWS;      // threads of a row, rows at a time, how often
     __shared__ float tile[64][65];
     __shared__ double sums[NS_TPB / 64];
     const int64_t k = blockIdx.z;
+    // the tile in the caller's orientation: rows i0.., columns j0..
+    const int r0 = blockIdx.y * 64, c0 = blockIdx.x * 64, i0 = a.tall ? c0 : r0, j0 = a.tall ? r0 : c0;
+    const T* g = static_cast<const T*>(a.grad) + k * a.matrix_stride;
+    const float* mom = a.momentum != nullptr ? a.momentum + k * a.m * (int64_t)a.n : nullptr;
+    const int tx = threadIdx.x % ACROSS * V, ty = threadIdx.x / ACROSS;
+    float u[ITEMS][V] = {};
+#pragma unroll
+    for (int e = 0; e < ITEMS; ++e)
+        if (i0 + ty + e * ROWS < a.m && j0 + tx < a.n) Run<T, V>::load(g + (i0 + ty + e * ROWS) * a.row_stride + j0 + tx, u[e]);
+    if (mom != nullptr) {
+        float v[ITEMS][V] = {};
+#pragma unroll
+        for (int e = 0; e < ITEMS; ++e)
+            if (i0 + ty + e * ROWS < a.m && j0 + tx < a.n) Run<float, V>::load(mom + (int64_t)(i0 + ty + e * ROWS) * a.n + j0 + tx, v[e]);
+#pragma unroll
+        for (int e = 0; e < ITEMS; ++e)
+#pragma unroll
+            for (int x = 0; x < V; ++x) u[e][x] = a.nesterov ? fmaf(a.beta, v[e][x], u[e][x]) : v[e][x];
+    }
     double sum = 0.0;
 #pragma unroll
     for (int i = 0; i < NS_PARTS / NS_TPB; ++i)
@@ -121,38 +178,39 @@ __global__ __launch_bounds__(NS_TPB) void rb_ortho_split_kernel(const UpdateArgs
     if ((threadIdx.x & 63) == 0) sums[threadIdx.x / 64] = sum;
     __syncthreads();
     const double inverse = ns_inverse(sqrt((sums[0] + sums[1]) + (sums[2] + sums[3])) + (double)a.eps);
-    // the tile in the caller's orientation: rows i0.., columns j0..
-    const int r0 = blockIdx.y * 64, c0 = blockIdx.x * 64, i0 = a.tall ? c0 : r0, j0 = a.tall ? r0 : c0;
-    const T* g = static_cast<const T*>(a.grad) + k * a.matrix_stride;
-    const float* mom = a.momentum != nullptr ? a.momentum + k * a.m * (int64_t)a.n : nullptr;
-    const int tx = threadIdx.x & 63, ty = threadIdx.x / 64;
-    for (int y = ty; y < 64; y += NS_TPB / 64) {
-        const int i = i0 + y, j = j0 + tx;
-        float u = 0.0f;
-        if (i < a.m && j < a.n) {
-            u = ns_load(g + i * a.row_stride + j);
-            if (mom != nullptr) {
-                const float v = mom[(int64_t)i * a.n + j];
-                u = a.nesterov ? fmaf(a.beta, v, u) : v;
-            }
-        }
-        tile[y][tx] = (float)((double)u * inverse);
-    }
+#pragma unroll
+    for (int e = 0; e < ITEMS; ++e)
+#pragma unroll
+        for (int x = 0; x < V; ++x) tile[ty + e * ROWS][tx + x] = (float)((double)u[e][x] * inverse);
     __syncthreads();
     // which of the two kept matrices has its rows along the caller's rows
     _Float16* along = a.tall ? q.xt + k * q.xt_matrix : q.x + k * q.x_matrix;
     _Float16* across = a.tall ? q.x + k * q.x_matrix : q.xt + k * q.xt_matrix;
-    const int64_t along_pitch = 2 * (int64_t)(a.tall ? q.rows : q.cols), across_pitch = 2 * (int64_t)(a.tall ? q.cols : q.rows);
-    for (int y = ty; y < 64; y += NS_TPB / 64) {
-        _Float16 hi, lo;
-        ns_split(tile[y][tx], hi, lo);
-        int64_t at = ns_at(i0 + y, j0 + tx, along_pitch);
-        along[at] = hi;
-        along[at + NS_KBLOCK] = lo;
-        ns_split(tile[tx][y], hi, lo);
-        at = ns_at(j0 + y, i0 + tx, across_pitch);
-        across[at] = hi;
-        across[at + NS_KBLOCK] = lo;
+    const int64_t along_pitch = a.tall ? q.xt_pitch : q.x_pitch, across_pitch = a.tall ? q.x_pitch : q.xt_pitch;
+    const int row = threadIdx.x / 4, first = threadIdx.x % 4 * 8;
+#pragma unroll
+    for (int b = 0; b < 64; b += NS_KBLOCK) {
+        half8 hi, lo;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            _Float16 h, l;
+            ns_split(tile[row][b + first + e], h, l);
+            hi[e] = h;
+            lo[e] = l;
+        }
+        _Float16* to = along + ns_at(i0 + row, j0 + b + first, along_pitch);
+        *reinterpret_cast<half8*>(to) = hi;
+        *reinterpret_cast<half8*>(to + NS_KBLOCK) = lo;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            _Float16 h, l;
+            ns_split(tile[b + first + e][row], h, l);
+            hi[e] = h;
+            lo[e] = l;
+        }
+        to = across + ns_at(j0 + row, i0 + b + first, across_pitch);
+        *reinterpret_cast<half8*>(to) = hi;
+        *reinterpret_cast<half8*>(to + NS_KBLOCK) = lo;
     }
 }
 
@@ -193,7 +251,10 @@ enum { NS_GRAM = 0, NS_POLY = 1, NS_APPLY = 2, NS_LAST = 3 };
 struct ProductArgs {
     const _Float16 *p, *q;                  // P: tiles_i * NS_TILE rows, Q: tiles_j * NS_TILE rows, kblocks blocks each
     int64_t p_matrix, q_matrix;             // halves between matrices
+    int64_t p_pitch, q_pitch;               // halves between rows
     int32_t kblocks, tiles_i, tiles_j;
+    int32_t tiles, slices;                  // of one matrix; of the summed index
+    float* sums;                            // of the slices, if there are several
     const _Float16* old;                    // POLY: A; APPLY, LAST: X^T, of which a * X is added
     int64_t old_matrix, old_pitch;
     _Float16 *out, *out_t;                  // the result and its transpose, as hi and lo
@@ -250,40 +311,141 @@ __device__ __forceinline__ void ns_tile_above(int t, int rows, int& ti, int& tj)
     }
 }
 
-// C = P Q^T of one tile of BM x BN (BM = BN or 2 BN); a wavefront has WM x WN of it in blocks of 32 x 32.  A block of 32 of the summed index
-// is (BM + BN) lines of 128 bytes; STAGES of them are in LDS or on their way there.
-template <int KIND, typename OUT, int BM, int BN, int WM, int WN, int STAGES, int WAVES_PER_SIMD>
-__global__ __launch_bounds__((BM / WM) * (BN / WN) * 64, WAVES_PER_SIMD) void rb_ortho_product_kernel(const ProductArgs a)
-{
-    constexpr int WAVES = (BM / WM) * (BN / WN), MI = WM / 32, MJ = WN / 32;
-    constexpr int STAGE = (BM + BN) * 128, PIECES = (BM + BN) / 8, PER_WAVE = PIECES / WAVES;
-    static_assert(PIECES % WAVES == 0 && BM % 8 == 0, "whole pieces of 8 lines per wavefront");
-    extern __shared__ __align__(16) char lds[];
-    const int64_t k = blockIdx.y;
-    constexpr int SUB = BM / BN;
-    const int t = ns_rank(blockIdx.x, gridDim.x);
-    int ti, tj;
-    if (KIND == NS_GRAM || KIND == NS_POLY) {
-        ns_tile_above(t / SUB, a.tiles_i, ti, tj);
-        tj = tj * SUB + t % SUB;
-    } else {
-        ns_tile_of(t, a.tiles_i, a.tiles_j, ti, tj);
-    }
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x & 63;
-    const int wi = (wave / (BN / WN)) * WM, wj = (wave % (BN / WN)) * WN;
-    const int64_t pitch = (int64_t)a.kblocks * NS_KHALVES * 2;          // bytes
-    const char* p = reinterpret_cast<const char*>(a.p + k * a.p_matrix) + (int64_t)ti * BM * pitch;
-    const char* q = reinterpret_cast<const char*>(a.q + k * a.q_matrix) + (int64_t)tj * BN * pitch;
+// ---- a block of 32 x 32 of a result -------------------------------------------
+//
+// Element i of a lane: row 8 (i / 4) + 4 (lane / 32) + i % 4, column lane % 32.  The block is 32 lines of 128 bytes of the kept matrix, and 32 of its
+// transpose: they are put together in LDS (each wavefront has a place of its own, lines 144 bytes apart) and moved 16 bytes a lane.
+constexpr int NS_PLACE_PITCH = 144, NS_PLACE = 32 * NS_PLACE_PITCH;
 
-    // A piece is 8 lines; the 16-byte part c of line r stands at place c ^ (r & 7) of its line in LDS, so that 8 lanes that read one part of
-    // 8 lines read all banks once.
-    const uint32_t lane_offset = (uint32_t)((lane >> 3) * pitch) + (((lane & 7) ^ (lane >> 3)) * 16);
-    auto fetch = [&](int block, int stage) {
+// What is added to the product lies transposed (A is symmetric): the four rows of a lane's column are neighbours there.
+__device__ __forceinline__ void ns_fetch_old(const ProductArgs& a, int64_t k, int r0, int c0, ns_vec* old)
+{
+    const int lane = threadIdx.x & 63, line = lane >> 3, part = (lane & 7) * 16;
+    const _Float16* from = a.old + k * a.old_matrix;
 #pragma unroll
-        for (int i = 0; i < PER_WAVE; ++i) {
-            const int piece = wave * PER_WAVE + i;
-            const char* from = (piece < BM / 8 ? p + (int64_t)piece * 8 * pitch : q + (int64_t)(piece - BM / 8) * 8 * pitch) + (int64_t)block * 128;
-            ns_load_to_lds(from + lane_offset, lds + stage * STAGE + piece * 1024);
+    for (int l = 0; l < 4; ++l)
+        old[l] = *reinterpret_cast<const ns_vec*>(reinterpret_cast<const char*>(from + ns_at(c0 + l * 8 + line, r0, a.old_pitch)) + part);
+}
+
+template <int KIND, typename OUT>
+__device__ __forceinline__ void ns_finish(const ProductArgs& a, int64_t k, int r0, int c0, const float16v& acc, const ns_vec* old, bool mirror, char* mine)
+{
+    const int lane = threadIdx.x & 63, half = lane / 32, col = lane & 31, line = lane >> 3, part = (lane & 7) * 16;
+    float v[16];
+    if (KIND != NS_GRAM) {
+#pragma unroll
+        for (int l = 0; l < 4; ++l) *reinterpret_cast<ns_vec*>(mine + (l * 8 + line) * NS_PLACE_PITCH + part) = old[l];
+        sc_lds_wait();
+    }
+    half4 hi[4], lo[4];
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+        char* const at = mine + col * NS_PLACE_PITCH + (g * 8 + half * 4) * 2;
+        if (KIND != NS_GRAM) {
+            hi[g] = *reinterpret_cast<const half4*>(at);
+            lo[g] = *reinterpret_cast<const half4*>(at + 64);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            v[g * 4 + e] = a.beta * acc[g * 4 + e];
+            if (KIND != NS_GRAM) v[g * 4 + e] = fmaf(a.alpha, (float)hi[g][e] + (float)lo[g][e], v[g * 4 + e]);
+        }
+    }
+    if (KIND == NS_LAST) {
+        // 32 numbers of a row of what the caller has, by half a wavefront
+        const bool tall = a.result.tall != 0;
+        if (tall) {
+            sc_lds_wait();
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+                *reinterpret_cast<float4*>(mine + col * NS_PLACE_PITCH + (g * 8 + half * 4) * 4) = float4{v[g * 4], v[g * 4 + 1], v[g * 4 + 2], v[g * 4 + 3]};
+            sc_lds_wait();
+#pragma unroll
+            for (int i = 0; i < 16; ++i) v[i] = *reinterpret_cast<const float*>(mine + (2 * i + half) * NS_PLACE_PITCH + col * 4);
+        }
+        sc_lds_wait();
+        int r[16], c[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            r[i] = r0 + (tall ? col : (i / 4) * 8 + half * 4 + i % 4);
+            c[i] = c0 + (tall ? 2 * i + half : col);
+        }
+        ns_result(a.result, static_cast<OUT*>(a.result.dst) + k * a.result.matrix_stride, r, c, v);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        _Float16 h, l;
+        ns_split(v[i], h, l);
+        hi[i / 4][i % 4] = h;
+        lo[i / 4][i % 4] = l;
+    }
+    if (mirror) {
+        char* to = reinterpret_cast<char*>(a.out_t + k * a.out_t_matrix + ns_at(c0 + line, r0, a.out_t_pitch)) + part;
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            *reinterpret_cast<half4*>(mine + col * NS_PLACE_PITCH + (g * 8 + half * 4) * 2) = hi[g];
+            *reinterpret_cast<half4*>(mine + col * NS_PLACE_PITCH + (g * 8 + half * 4) * 2 + 64) = lo[g];
+        }
+        sc_lds_wait();
+#pragma unroll
+        for (int l = 0; l < 4; ++l) *reinterpret_cast<ns_vec*>(to + l * 8 * a.out_t_pitch * 2) = *reinterpret_cast<const ns_vec*>(mine + (l * 8 + line) * NS_PLACE_PITCH + part);
+        sc_lds_wait();
+    }
+    char* to = reinterpret_cast<char*>(a.out + k * a.out_matrix + ns_at(r0 + line, c0, a.out_pitch)) + part;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        _Float16* at = reinterpret_cast<_Float16*>(mine + ((i / 4) * 8 + half * 4 + i % 4) * NS_PLACE_PITCH) + col;
+        at[0] = hi[i / 4][i % 4];
+        at[NS_KBLOCK] = lo[i / 4][i % 4];
+    }
+    sc_lds_wait();
+#pragma unroll
+    for (int l = 0; l < 4; ++l) *reinterpret_cast<ns_vec*>(to + l * 8 * a.out_pitch * 2) = *reinterpret_cast<const ns_vec*>(mine + (l * 8 + line) * NS_PLACE_PITCH + part);
+    sc_lds_wait();
+}
+
+// Block b of 32 x 32 of a tile, tile t of slice s: 1024 sums, 16 of a lane as 4 times 4.
+__device__ __forceinline__ float4* ns_sums(const ProductArgs& a, int64_t tile, int slice, int blocks, int b)
+{
+    return reinterpret_cast<float4*>(a.sums) + ((tile * a.slices + slice) * blocks + b) * 256 + (threadIdx.x & 63);
+}
+
+// C = P Q^T of one tile of BM x BM; a wavefront has WM x WN of it in blocks of 32 x 32.  A block of 32 of the summed index is 2 BM lines of 128
+// bytes; STAGES of them are in LDS or on their way there.  Where the tiles are few the summed index is cut into slices, a workgroup each.
+template <int KIND, typename OUT, int BM, int WM, int WN, int STAGES, int WAVES_PER_SIMD>
+__global__ __launch_bounds__((BM / WM) * (BM / WN) * 64, WAVES_PER_SIMD) void rb_ortho_product_kernel(const ProductArgs a)
+{
+    constexpr int BN = BM, WAVES = (BM / WM) * (BN / WN), MI = WM / 32, MJ = WN / 32;
+    constexpr int STAGE = (BM + BN) * 128, PIECES = (BM + BN) / 8, PER_WAVE = PIECES / WAVES;
+    static_assert(PIECES % (4 * WAVES) == 0, "pairs of pieces of 8 lines of either operand per wavefront");
+    extern __shared__ __align__(16) char lds[];
+    const int rank = ns_rank(blockIdx.x, gridDim.x);
+    const int slice = rank % a.slices, tile = rank / a.slices;      // tile: counted over all matrices
+    const int64_t k = tile / a.tiles;
+    int ti, tj;
+    if (KIND == NS_GRAM || KIND == NS_POLY)
+        ns_tile_above(tile - (int)k * a.tiles, a.tiles_i, ti, tj);
+    else
+        ns_tile_of(tile - (int)k * a.tiles, a.tiles_i, a.tiles_j, ti, tj);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x & 63;
+    const int kbegin = (int)((int64_t)a.kblocks * slice / a.slices), kblocks = (int)((int64_t)a.kblocks * (slice + 1) / a.slices) - kbegin;
+    const int wi = (wave / (BN / WN)) * WM, wj = (wave % (BN / WN)) * WN;
+    const char* p = reinterpret_cast<const char*>(a.p + k * a.p_matrix + (int64_t)ti * BM * a.p_pitch) + (int64_t)kbegin * 128;
+    const char* q = reinterpret_cast<const char*>(a.q + k * a.q_matrix + (int64_t)tj * BN * a.q_pitch) + (int64_t)kbegin * 128;
+
+    // A piece is 8 lines; the 16-byte part c of line r stands at place c ^ (r / 2 % 8) of its line in LDS, so that 16 lanes that read one part of
+    // 16 lines read all 64 banks once.  (Of an odd piece r / 2 is 4 more.)
+    const uint32_t place = ((lane & 7) ^ (lane >> 4)) * 16;
+    const uint32_t p_lane = (uint32_t)((lane >> 3) * a.p_pitch * 2), q_lane = (uint32_t)((lane >> 3) * a.q_pitch * 2);
+    auto fetch = [&](int block, int stage) {
+        char* to = lds + stage * STAGE + wave * (PER_WAVE / 2 * 1024);
+        const char* from_p = p + wave * (PER_WAVE / 2 * 16) * a.p_pitch + (int64_t)block * 128;
+        const char* from_q = q + wave * (PER_WAVE / 2 * 16) * a.q_pitch + (int64_t)block * 128;
+#pragma unroll
+        for (int i = 0; i < PER_WAVE / 2; ++i) {
+            ns_load_to_lds(from_p + i * 16 * a.p_pitch + p_lane + (place ^ (i & 1) * 64), to + i * 1024);
+            ns_load_to_lds(from_q + i * 16 * a.q_pitch + q_lane + (place ^ (i & 1) * 64), to + BM * 128 + i * 1024);
         }
     };
 
@@ -291,7 +453,7 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64, WAVES_PER_SIMD) void rb
     struct Fragments { half8 ph[MI], pl[MI], qh[MJ], ql[MJ]; };
     const int row = lane & 31;
     auto read = [&](Fragments& f, int stage, int ks) {
-        const int c = ks * 2 + lane / 32, hi = (c ^ (row & 7)) * 16, lo = ((c + 4) ^ (row & 7)) * 16;
+        const int c = ks * 2 + lane / 32, hi = (c ^ (row / 2 & 7)) * 16, lo = ((c + 4) ^ (row / 2 & 7)) * 16;
         const char* at = lds + stage * STAGE;
 #pragma unroll
         for (int b = 0; b < MI; ++b) {
@@ -324,129 +486,91 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64, WAVES_PER_SIMD) void rb
     // place is free for the block STAGES further on as soon as all wavefronts have read its second half.
 #pragma unroll
     for (int s = 0; s < STAGES; ++s)
-        if (s < a.kblocks) fetch(s, s);
-    if (a.kblocks >= STAGES)
+        if (s < kblocks) fetch(s, s);
+    if (kblocks >= STAGES)
         ns_arrived<PER_WAVE * (STAGES - 1)>();
     else
         ns_arrived<0>();
     Fragments first, second;
     read(first, 0, 0);
     int stage = 0;
-    for (int block = 0; block < a.kblocks; ++block) {
+    for (int block = 0; block < kblocks; ++block) {
         read(second, stage, 1);
         multiply(first);
         const int next = stage + 1 == STAGES ? 0 : stage + 1;
-        if (block + STAGES < a.kblocks) {
+        if (block + STAGES < kblocks) {
             ns_arrived<PER_WAVE * (STAGES - 2)>();
             fetch(block + STAGES, stage);
         } else {
             ns_arrived<0>();
         }
-        if (block + 1 < a.kblocks) read(first, next, 0);
+        if (block + 1 < kblocks) read(first, next, 0);
         multiply(second);
         stage = next;
     }
 
-    // The result.  Block element i of a lane: row 8 (i / 4) + 4 (lane / 32) + i % 4, column lane % 32.  A block of 32 x 32 is 32 lines of 128 bytes
-    // in the kept matrix, and 32 in its transpose: they are put together in LDS (each wavefront has a place of its own, lines 144 bytes apart),
-    // and stored 16 bytes a lane.
-    constexpr int PITCH = 144;
-    static_assert(WAVES * 32 * PITCH <= STAGES * STAGE, "the places fit what the stages leave");
-    char* mine = lds + wave * (32 * PITCH);
-    const int half = lane / 32, col = lane & 31, line = lane >> 3, part = (lane & 7) * 16;
-    const bool mirror = (KIND == NS_GRAM || KIND == NS_POLY) ? tj >= (ti + 1) * SUB : true;
-    // what is added lies transposed (A is symmetric): the four rows of a lane's column are neighbours there
-    // (all of it at once while that is four blocks, a row of blocks at a time of a larger tile, which would not fit the registers)
-    constexpr int AHEAD = KIND == NS_GRAM ? 0 : MI * MJ <= 4 ? MI : 1;
-    ns_vec old[AHEAD ? AHEAD : 1][MJ][4];
-    auto fetch_old = [&](int bi, ns_vec (*to)[4]) {
-        const _Float16* from = a.old + k * a.old_matrix;
+    if (a.slices > 1) {                        // a slice's sums: rb_ortho_join_kernel adds them up
 #pragma unroll
-        for (int bj = 0; bj < MJ; ++bj)
+        for (int i = 0; i < MI; ++i)
 #pragma unroll
-            for (int l = 0; l < 4; ++l)
-                to[bj][l] = *reinterpret_cast<const ns_vec*>(reinterpret_cast<const char*>(
-                    from + ns_at(tj * BN + wj + bj * 32 + l * 8 + line, ti * BM + wi + bi * 32, a.old_pitch)) + part);
-    };
+            for (int j = 0; j < MJ; ++j) {
+                float4* to = ns_sums(a, tile, slice, (BM / 32) * (BM / 32), ((wi / 32) + i) * (BM / 32) + wj / 32 + j);
 #pragma unroll
-    for (int bi = 0; bi < AHEAD; ++bi) fetch_old(bi, old[bi]);
-#pragma unroll
-    for (int bi = 0; bi < MI; ++bi) {
-        if (AHEAD == 1 && bi > 0) fetch_old(bi, old[0]);
-#pragma unroll
-        for (int bj = 0; bj < MJ; ++bj) {
-            const int r0 = ti * BM + wi + bi * 32, c0 = tj * BN + wj + bj * 32;
-            float v[16];
-            if (KIND != NS_GRAM) {
-#pragma unroll
-                for (int l = 0; l < 4; ++l) *reinterpret_cast<ns_vec*>(mine + (l * 8 + line) * PITCH + part) = old[AHEAD > 1 ? bi : 0][bj][l];
-                sc_lds_wait();
+                for (int g = 0; g < 4; ++g) to[g * 64] = float4{acc[i][j][g * 4], acc[i][j][g * 4 + 1], acc[i][j][g * 4 + 2], acc[i][j][g * 4 + 3]};
             }
-            half4 hi[4], lo[4];
+        return;
+    }
+    static_assert(WAVES * NS_PLACE <= STAGES * STAGE, "the wavefronts' places fit what the stages leave");
+    char* mine = lds + wave * NS_PLACE;
+    const bool mirror = (KIND == NS_GRAM || KIND == NS_POLY) ? tj > ti : true;
+    // (what is added: all of it at once while that is four blocks, a row of blocks at a time of a larger tile, which would not fit the registers)
+    constexpr int AHEAD = MI * MJ <= 4 ? MI : 1;
+    ns_vec old[AHEAD][MJ][4];
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                if (KIND != NS_GRAM) {
-                    hi[g] = *reinterpret_cast<const half4*>(mine + col * PITCH + (g * 8 + half * 4) * 2);
-                    lo[g] = *reinterpret_cast<const half4*>(mine + col * PITCH + (g * 8 + half * 4) * 2 + 64);
-                }
+    for (int i = 0; i < MI; ++i) {
+        if (KIND != NS_GRAM && (i == 0 || AHEAD == 1)) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    v[g * 4 + e] = a.beta * acc[bi][bj][g * 4 + e];
-                    if (KIND != NS_GRAM) v[g * 4 + e] = fmaf(a.alpha, (float)hi[g][e] + (float)lo[g][e], v[g * 4 + e]);
-                }
-            }
-            if (KIND == NS_LAST) {
-                // 32 numbers of a row of what the caller has, by half a wavefront
-                if (a.result.tall) {
-                    sc_lds_wait();
+            for (int b = 0; b < AHEAD; ++b)
 #pragma unroll
-                    for (int g = 0; g < 4; ++g) *reinterpret_cast<float4*>(mine + col * PITCH + (g * 8 + half * 4) * 4) = float4{v[g * 4], v[g * 4 + 1], v[g * 4 + 2], v[g * 4 + 3]};
-                    sc_lds_wait();
+                for (int j = 0; j < MJ; ++j) ns_fetch_old(a, k, ti * BM + wi + (i + b) * 32, tj * BN + wj + j * 32, old[b][j]);
+        }
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) v[i] = *reinterpret_cast<const float*>(mine + (2 * i + half) * PITCH + col * 4);
-                    sc_lds_wait();
-                }
-                int r[16], c[16];
+        for (int j = 0; j < MJ; ++j)
+            ns_finish<KIND, OUT>(a, k, ti * BM + wi + i * 32, tj * BN + wj + j * 32, acc[i][j], old[AHEAD == 1 ? 0 : i][j], mirror, mine);
+    }
+}
+
+// The sums of the slices, in their order, and what is left of the product: a wavefront per block of 32 x 32.
+template <int KIND, typename OUT, int BM>
+__global__ __launch_bounds__(NS_TPB) void rb_ortho_join_kernel(const ProductArgs a)
+{
+    __shared__ __align__(16) char places[NS_TPB / 64][NS_PLACE];
+    constexpr int SIDE = BM / 32;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const int64_t item = (int64_t)blockIdx.x * (NS_TPB / 64) + wave, tile = item / (SIDE * SIDE);
+    const int b = (int)(item % (SIDE * SIDE));
+    const int64_t k = tile / a.tiles;
+    int ti, tj;
+    if (KIND == NS_GRAM || KIND == NS_POLY)
+        ns_tile_above((int)(tile - k * a.tiles), a.tiles_i, ti, tj);
+    else
+        ns_tile_of((int)(tile - k * a.tiles), a.tiles_i, a.tiles_j, ti, tj);
+    const int r0 = ti * BM + b / SIDE * 32, c0 = tj * BM + b % SIDE * 32;
+    ns_vec old[4];
+    if (KIND != NS_GRAM) ns_fetch_old(a, k, r0, c0, old);
+    float16v acc = {};
+    for (int s = 0; s < a.slices; ++s) {
+        const float4* from = ns_sums(a, tile, s, SIDE * SIDE, b);
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    r[i] = r0 + (a.result.tall ? col : (i / 4) * 8 + half * 4 + i % 4);
-                    c[i] = c0 + (a.result.tall ? 2 * i + half : col);
-                }
-                ns_result(a.result, static_cast<OUT*>(a.result.dst) + k * a.result.matrix_stride, r, c, v);
-                continue;
-            }
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                _Float16 h, l;
-                ns_split(v[i], h, l);
-                hi[i / 4][i % 4] = h;
-                lo[i / 4][i % 4] = l;
-            }
-            if (mirror) {
-                char* to = reinterpret_cast<char*>(a.out_t + k * a.out_t_matrix + ns_at(c0 + line, r0, a.out_t_pitch)) + part;
-#pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    *reinterpret_cast<half4*>(mine + col * PITCH + (g * 8 + half * 4) * 2) = hi[g];
-                    *reinterpret_cast<half4*>(mine + col * PITCH + (g * 8 + half * 4) * 2 + 64) = lo[g];
-                }
-                sc_lds_wait();
-#pragma unroll
-                for (int l = 0; l < 4; ++l) *reinterpret_cast<ns_vec*>(to + l * 8 * a.out_t_pitch * 2) = *reinterpret_cast<const ns_vec*>(mine + (l * 8 + line) * PITCH + part);
-                sc_lds_wait();
-            }
-            char* to = reinterpret_cast<char*>(a.out + k * a.out_matrix + ns_at(r0 + line, c0, a.out_pitch)) + part;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                _Float16* at = reinterpret_cast<_Float16*>(mine + ((i / 4) * 8 + half * 4 + i % 4) * PITCH) + col;
-                at[0] = hi[i / 4][i % 4];
-                at[NS_KBLOCK] = lo[i / 4][i % 4];
-            }
-            sc_lds_wait();
-#pragma unroll
-            for (int l = 0; l < 4; ++l) *reinterpret_cast<ns_vec*>(to + l * 8 * a.out_pitch * 2) = *reinterpret_cast<const ns_vec*>(mine + (l * 8 + line) * PITCH + part);
-            sc_lds_wait();
+        for (int g = 0; g < 4; ++g) {
+            const float4 v = from[g * 64];
+            acc[g * 4] += v.x;
+            acc[g * 4 + 1] += v.y;
+            acc[g * 4 + 2] += v.z;
+            acc[g * 4 + 3] += v.w;
         }
     }
+    ns_finish<KIND, OUT>(a, k, r0, c0, acc, old, (KIND == NS_GRAM || KIND == NS_POLY) ? tj > ti : true, places[wave]);
 }
 
 // A whole matrix of up to P x P by one workgroup, in LDS: X, or A, or B in one half of it, X^T in the other; X itself in registers, a wavefront
@@ -464,7 +588,7 @@ __global__ __launch_bounds__(P / 32 * (P / WN) * 64) void rb_ortho_small_kernel(
     constexpr int WAVES = P / 32 * (P / WN), MJ = WN / 32, LINES = P / 32;
     extern __shared__ __align__(16) char lds[];
     __shared__ double sums[WAVES];
-    char* const one = lds;                      // X, A, B: line (row, block of 32 columns), its 16-byte parts at c ^ (row & 7)
+    char* const one = lds;                      // X, A, B: line (block of 32 columns, row), its 16-byte parts at c ^ (row / 2 % 8)
     char* const two = lds + P * LINES * 128;    // X^T
     const int64_t k = blockIdx.x;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x & 63, half = lane / 32, col = lane & 31;
@@ -522,10 +646,10 @@ __global__ __launch_bounds__(P / 32 * (P / WN) * 64) void rb_ortho_small_kernel(
         for (int i = 0; i < 16; ++i) x[b][i] = (float)((double)x[b][i] * inverse);
 
     auto part = [&](char* area, int row, int column) {          // of element (row, column): hi; lo is 4 parts on
-        return area + (row * LINES + column / 32) * 128 + (((column % 32 / 8) ^ (row & 7)) * 16) + column % 8 * 2;
+        return area + (column / 32 * P + row) * 128 + (((column % 32 / 8) ^ (row / 2 & 7)) * 16) + column % 8 * 2;
     };
     auto part_lo = [&](char* area, int row, int column) {
-        return area + (row * LINES + column / 32) * 128 + (((column % 32 / 8 + 4) ^ (row & 7)) * 16) + column % 8 * 2;
+        return area + (column / 32 * P + row) * 128 + (((column % 32 / 8 + 4) ^ (row / 2 & 7)) * 16) + column % 8 * 2;
     };
     // v, scaled already, to the transposed place (4 rows of a column are neighbours there), and to its own
     auto put = [&](char* across, char* along, const float (*v)[16]) {
@@ -555,12 +679,12 @@ __global__ __launch_bounds__(P / 32 * (P / WN) * 64) void rb_ortho_small_kernel(
 #pragma unroll
         for (int b = 0; b < MJ; ++b) acc[b] = float16v{};
         for (int ks = 0; ks < 2 * blocks; ++ks) {
-            const int c = (ks & 1) * 2 + half, hi = (c ^ (col & 7)) * 16, lo = ((c + 4) ^ (col & 7)) * 16;
-            const char* pr = p + ((wi + col) * LINES + ks / 2) * 128;
+            const int c = (ks & 1) * 2 + half, hi = (c ^ (col / 2 & 7)) * 16, lo = ((c + 4) ^ (col / 2 & 7)) * 16;
+            const char* pr = p + (ks / 2 * P + wi + col) * 128;
             const half8 ph = *reinterpret_cast<const half8*>(pr + hi), pl = *reinterpret_cast<const half8*>(pr + lo);
 #pragma unroll
             for (int b = 0; b < MJ; ++b) {
-                const char* qr = q + ((wj + b * 32 + col) * LINES + ks / 2) * 128;
+                const char* qr = q + (ks / 2 * P + wj + b * 32 + col) * 128;
                 const half8 qh = *reinterpret_cast<const half8*>(qr + hi), ql = *reinterpret_cast<const half8*>(qr + lo);
                 acc[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(pl, qh, acc[b], 0, 0, 0);
                 acc[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph, ql, acc[b], 0, 0, 0);

@@ -172,87 +172,113 @@ struct rb_ortho {
     bool tall;
     int32_t rows, cols;            // of the kept X: short and long side
     int32_t small;                 // a workgroup per matrix: its padded side (64, 128), or 0: tiled products
-    int32_t prows, pcols;          // tiled: padded to whole tiles
-    int32_t tile[3];               // of A, of B, of X
-    size_t off_x, off_xt[2], off_a, off_b, bytes;
+    int32_t kept_rows, kept_cols;  // tiled: with room for whole tiles of every product
+    int32_t tile[3], slices[3];    // of A, of B, of X
+    size_t off_x, off_xt[2], off_a, off_b, off_sums, bytes;
     char* ws;
 };
 
 namespace {
 
-// Tiles of a product: 64 x 64 by 4 wavefronts, 128 x 128 by 8, 256 x 256 by 8.
-template <int KIND, typename OUT, int BM, int WM, int WN, int STAGES, int WAVES_PER_SIMD>
-hipError_t product_of(const ProductArgs& a, unsigned tiles, unsigned matrices, hipStream_t st)
+enum { OF_A = 0, OF_B = 1, OF_X = 2 };
+
+template <int KIND, typename OUT, int BM, int WM, int WN, int WAVES_PER_SIMD>
+hipError_t product_of(const ProductArgs& a, unsigned tiles, hipStream_t st)
 {
-    return launch(rb_ortho_product_kernel<KIND, OUT, BM, BM, WM, WN, STAGES, WAVES_PER_SIMD>, dim3(tiles, matrices), BM / WM * (BM / WN) * 64,
-                  (size_t)STAGES * 2 * BM * 128, st, a);
+    constexpr int STAGES = BM == 64 ? 3 : 2;
+    const hipError_t e = launch(rb_ortho_product_kernel<KIND, OUT, BM, WM, WN, STAGES, WAVES_PER_SIMD>, dim3(tiles * (unsigned)a.slices),
+                                BM / WM * (BM / WN) * 64, (size_t)STAGES * 2 * BM * 128, st, a);
+    if (e != hipSuccess || a.slices == 1) return e;
+    return launch(rb_ortho_join_kernel<KIND, OUT, BM>, dim3(tiles * (BM / 32) * (BM / 32) / (NS_TPB / 64)), NS_TPB, 0, st, a);
 }
 
 template <int KIND, typename OUT>
-hipError_t product(const rb_ortho* o, ProductArgs a, int tile, bool symmetric, hipStream_t st)
+hipError_t product(const rb_ortho* o, ProductArgs a, int which, hipStream_t st)
 {
-    a.tiles_i = o->prows / tile;
-    a.tiles_j = (symmetric ? o->prows : o->pcols) / tile;
-    const unsigned tiles = symmetric ? (unsigned)a.tiles_i * (a.tiles_i + 1) / 2 : (unsigned)a.tiles_i * a.tiles_j, n = (unsigned)o->matrices;
+    const int tile = o->tile[which];
+    a.tiles_i = (o->rows + tile - 1) / tile;
+    a.tiles_j = which == OF_X ? (o->cols + tile - 1) / tile : a.tiles_i;
+    a.tiles = which == OF_X ? a.tiles_i * a.tiles_j : a.tiles_i * (a.tiles_i + 1) / 2;
+    a.slices = o->slices[which];
+    a.sums = reinterpret_cast<float*>(o->ws + o->off_sums);
+    const unsigned tiles = (unsigned)(a.tiles * o->matrices);
     switch (tile) {
-    case 256: return product_of<KIND, OUT, 256, 128, 64, 2, 2>(a, tiles, n, st);
-    case 128: return product_of<KIND, OUT, 128, 64, 32, 2, 4>(a, tiles, n, st);
-    default: return product_of<KIND, OUT, 64, 32, 32, 3, 3>(a, tiles, n, st);
+    case 256: return product_of<KIND, OUT, 256, 128, 64, 2>(a, tiles, st);
+    case 192: return product_of<KIND, OUT, 192, 96, 96, 1>(a, tiles, st);
+    case 128: return product_of<KIND, OUT, 128, 64, 32, 4>(a, tiles, st);
+    default: return product_of<KIND, OUT, 64, 32, 32, 3>(a, tiles, st);
     }
 }
 
-// What a product takes, in us, by its tile, measured on 256 compute units: a launch with its epilogue, and a tile's block of 32 of the summed
-// index on a compute unit that has one workgroup (64: 0.25, 128: 0.51, 256: 2.1) or is full (two of 128 together 1.58, 256: 2.65).
-double product_us(int tile, double tiles, int kblocks)
+// What a product takes, in us, by its tile and slices: a launch with its ends, and per block of 32 of the summed index what 256 compute units were
+// measured to take, by how many tiles there are per unit (64: 0.23 for one, 0.25 each for more; 128: 0.57 for one while others idle,
+// 0.74, 0.8; 192: 1.2, 1.55 and 256: 1.85, 2.0, 2.5, one at a time).  Slices add a launch that reads what they have written.
+double product_us(int tile, double tiles, int kblocks, int slices)
 {
-    const double per = tiles / 256;
-    if (tile == 64) return 5 + kblocks * 0.25 * std::max(1.0, per);
-    if (tile == 128) {
-        const double pairs = std::floor(per / 2), rest = per - 2 * pairs;
-        return 8 + kblocks * (1.58 * pairs + (rest == 0 ? 0 : rest <= 1 ? 0.51 : 1.58));
-    }
-    return 15 + kblocks * (per <= 0.75 ? 2.1 : 2.65 * std::ceil(per));
+    const double per = tiles * slices / 256, whole = std::floor(per), part = per - whole;
+    const double shared = whole + (part > 0 ? 0.35 + 0.65 * part : 0);       // several at a time: the last of them have the unit to themselves
+    double us = 0;
+    if (tile == 64) us = 5 + kblocks / (double)slices * (per <= 1 ? 0.23 : 0.25 * shared);
+    if (tile == 128) us = 8 + kblocks / (double)slices * (per <= 0.5 ? 0.57 : per <= 1 ? 0.57 + 0.34 * (per - 0.5) : 0.8 * shared);
+    if (tile == 192) us = 12 + kblocks / (double)slices * (per <= 0.5 ? 1.2 : 1.55) * std::ceil(per);
+    if (tile == 256) us = 16 + kblocks / (double)slices * (per <= 0.5 ? 1.85 : per <= 0.75 ? 2.0 : 2.5) * std::ceil(per);
+    return slices == 1 ? us : us + 6 + tiles * slices * tile * tile * 8 / 1e7;
 }
 
-// The padding and the three products' tiles that take least.
+// The tiles and slices that take least, and the room that all products need.
 void choose_tiles(rb_ortho* o)
 {
-    double best = 1e300;
-    for (int pad = 64; pad <= 256; pad *= 2) {
-        const int64_t R = (int64_t)round_up((size_t)o->rows, (size_t)pad), C = (int64_t)round_up((size_t)o->cols, (size_t)pad);
-        double total = 0;
-        int chosen[3] = {};
-        for (int kind = 0; kind < 3; ++kind) {
-            double least = 1e300;
-            for (int tile = 64; tile <= pad; tile *= 2) {
-                const double n = (double)(R / tile), tiles = (double)o->matrices * (kind < 2 ? n * (n + 1) / 2 : n * (double)(C / tile));
-                const double us = product_us(tile, tiles, (int)((kind == 0 ? C : R) / NS_KBLOCK));
-                if (us < least) {
-                    least = us;
-                    chosen[kind] = tile;
-                }
+    int64_t rows = round_up((size_t)o->rows, 64), cols = round_up((size_t)o->cols, 64);
+    size_t sums = 0;
+    for (int which = 0; which < 3; ++which) {
+        double least = 1e300;
+        for (int tile = 64; tile <= 256; tile += 64) {
+            const int64_t n = (o->rows + tile - 1) / tile, m = (o->cols + tile - 1) / tile, tiles = o->matrices * (which == OF_X ? n * m : n * (n + 1) / 2);
+            const int kblocks = ((which == OF_A ? o->cols : o->rows) + NS_KBLOCK - 1) / NS_KBLOCK;
+            for (int slices = 1; slices <= 16 && (slices == 1 || (kblocks / slices >= 8 && tiles * slices <= 512)); ++slices) {
+                const double us = product_us(tile, (double)tiles, kblocks, slices);
+                if (us >= least) continue;
+                least = us;
+                o->tile[which] = tile;
+                o->slices[which] = slices;
             }
-            total += least;
         }
-        if (total < best) {
-            best = total;
-            o->prows = (int32_t)R;
-            o->pcols = (int32_t)C;
-            for (int kind = 0; kind < 3; ++kind) o->tile[kind] = chosen[kind];
-        }
+        const size_t tile = (size_t)o->tile[which], n = (o->rows + tile - 1) / tile, m = (o->cols + tile - 1) / tile;
+        rows = std::max(rows, (int64_t)(n * tile));
+        cols = std::max(cols, (int64_t)((which == OF_X ? m : n) * tile));
+        if (o->slices[which] > 1) sums = std::max(sums, (size_t)o->matrices * (which == OF_X ? n * m : n * (n + 1) / 2) * o->slices[which] * tile * tile * sizeof(float));
     }
+    o->kept_rows = (int32_t)rows;
+    o->kept_cols = (int32_t)cols;
+    const size_t n = (size_t)o->matrices * sizeof(_Float16), xp = (size_t)ns_pitch(cols), tp = (size_t)ns_pitch(rows);
+    size_t off = round_up((size_t)o->matrices * NS_PARTS * sizeof(double), 256);
+    o->off_x = off; off += n * (size_t)rows * xp;
+    o->off_xt[0] = off; off += n * (size_t)cols * tp;
+    o->off_xt[1] = off; off += n * (size_t)cols * tp;
+    o->off_a = off; off += n * (size_t)rows * tp;
+    o->off_b = off; off += n * (size_t)rows * tp;
+    o->off_sums = off; off += sums;
+    o->bytes = off;
+}
+
+template <typename T, int V>
+hipError_t first_passes(const rb_ortho* o, const UpdateArgs& u, const KeptArgs& q, hipStream_t st)
+{
+    double* parts = reinterpret_cast<double*>(o->ws);
+    const int64_t items = (int64_t)((o->m + NS_ROWS_AT_ONCE - 1) / NS_ROWS_AT_ONCE) * ((o->n + V * NS_TPB - 1) / (V * NS_TPB));
+    const int nparts = (int)std::min<int64_t>(items, NS_PARTS);
+    hipError_t e = launch(rb_ortho_norm_kernel<T, V>, dim3((unsigned)nparts, (unsigned)o->matrices), NS_TPB, 0, st, u, parts);
+    if (e != hipSuccess) return e;
+    return launch(rb_ortho_split_kernel<T, V>, dim3((unsigned)(o->cols + 63) / 64, (unsigned)(o->rows + 63) / 64, (unsigned)o->matrices), NS_TPB, 0, st, u, q,
+                  static_cast<const double*>(parts), nparts);
 }
 
 template <typename T>
 hipError_t first_pass(const rb_ortho* o, const UpdateArgs& u, const KeptArgs& q, hipStream_t st)
 {
-    double* parts = reinterpret_cast<double*>(o->ws);
-    const int64_t items = (int64_t)((o->m + 7) / 8) * ((o->n + NS_TPB - 1) / NS_TPB);
-    const int nparts = (int)std::min<int64_t>(items, NS_PARTS);
-    hipError_t e = launch(rb_ortho_norm_kernel<T>, dim3((unsigned)nparts, (unsigned)o->matrices), NS_TPB, 0, st, u, parts);
-    if (e != hipSuccess) return e;
-    return launch(rb_ortho_split_kernel<T>, dim3((unsigned)(o->pcols / 64), (unsigned)(o->prows / 64), (unsigned)o->matrices), NS_TPB, 0, st, u, q,
-                  static_cast<const double*>(parts), nparts);
+    const bool vectors = o->n % 4 == 0 && u.row_stride % 4 == 0 && u.matrix_stride % 4 == 0 && aligned(u.grad, 4 * sizeof(T)) &&
+                         aligned(u.momentum, 16);
+    return vectors ? first_passes<T, 4>(o, u, q, st) : first_passes<T, 1>(o, u, q, st);
 }
 
 template <typename T, typename OUT>
@@ -275,48 +301,49 @@ hipError_t orthogonalize(const rb_ortho* o, const UpdateArgs& u, const ResultArg
         if (o->dtype == RB_F32) return o->out_dtype == RB_F32 ? whole<float, float>(o, u, result, st) : whole<float, Bf16>(o, u, result, st);
         return o->out_dtype == RB_F32 ? whole<Bf16, float>(o, u, result, st) : whole<Bf16, Bf16>(o, u, result, st);
     }
-    const int64_t R = o->prows, C = o->pcols;
+    const int64_t R = o->kept_rows, C = o->kept_cols;
     _Float16* x = reinterpret_cast<_Float16*>(o->ws + o->off_x);
     _Float16* xt[2] = {reinterpret_cast<_Float16*>(o->ws + o->off_xt[0]), reinterpret_cast<_Float16*>(o->ws + o->off_xt[1])};
     _Float16* ma = reinterpret_cast<_Float16*>(o->ws + o->off_a);
     _Float16* mb = reinterpret_cast<_Float16*>(o->ws + o->off_b);
-    const KeptArgs kept{x, xt[0], 2 * R * C, 2 * R * C, (int32_t)R, (int32_t)C};
+    const int64_t xp = ns_pitch(C), tp = ns_pitch(R);     // halves between rows of X; of X^T, A and B
+    const KeptArgs kept{x, xt[0], R * xp, C * tp, xp, tp, (int32_t)R, (int32_t)C};
     hipError_t e = o->dtype == RB_F32 ? first_pass<float>(o, u, kept, st) : first_pass<Bf16>(o, u, kept, st);
     for (int s = 0; s < o->steps && e == hipSuccess; ++s) {
         const float* c = o->coefficients[s];
         ProductArgs g{};                                   // A = X X^T
-        g.p = x; g.q = x; g.p_matrix = g.q_matrix = 2 * R * C;
-        g.kblocks = (int32_t)(C / NS_KBLOCK);
+        g.p = x; g.q = x; g.p_matrix = g.q_matrix = R * xp; g.p_pitch = g.q_pitch = xp;
+        g.kblocks = (o->cols + NS_KBLOCK - 1) / NS_KBLOCK;
         g.out = ma; g.out_t = ma;
-        g.out_matrix = g.out_t_matrix = 2 * R * R;
-        g.out_pitch = g.out_t_pitch = 2 * R;
+        g.out_matrix = g.out_t_matrix = R * tp;
+        g.out_pitch = g.out_t_pitch = tp;
         g.beta = NS_SCALE_A / (NS_SCALE_X * NS_SCALE_X);
-        if ((e = product<NS_GRAM, float>(o, g, o->tile[0], true, st)) != hipSuccess) break;
+        if ((e = product<NS_GRAM, float>(o, g, OF_A, st)) != hipSuccess) break;
         ProductArgs p = g;                                 // B = b A + c A A
-        p.p = ma; p.q = ma; p.p_matrix = p.q_matrix = 2 * R * R;
-        p.kblocks = (int32_t)(R / NS_KBLOCK);
-        p.old = ma; p.old_matrix = 2 * R * R; p.old_pitch = 2 * R;
+        p.p = ma; p.q = ma; p.p_matrix = p.q_matrix = R * tp; p.p_pitch = p.q_pitch = tp;
+        p.kblocks = (o->rows + NS_KBLOCK - 1) / NS_KBLOCK;
+        p.old = ma; p.old_matrix = R * tp; p.old_pitch = tp;
         p.out = mb; p.out_t = mb;
         p.alpha = c[1] * (NS_SCALE_B / NS_SCALE_A);
         p.beta = c[2] * (NS_SCALE_B / (NS_SCALE_A * NS_SCALE_A));
-        if ((e = product<NS_POLY, float>(o, p, o->tile[1], true, st)) != hipSuccess) break;
+        if ((e = product<NS_POLY, float>(o, p, OF_B, st)) != hipSuccess) break;
         ProductArgs q{};                                   // X <- a X + B X
-        q.p = mb; q.p_matrix = 2 * R * R;
-        q.q = xt[s & 1]; q.q_matrix = 2 * R * C;
-        q.kblocks = (int32_t)(R / NS_KBLOCK);
-        q.old = xt[s & 1]; q.old_matrix = 2 * R * C; q.old_pitch = 2 * R;
-        q.out = x; q.out_matrix = 2 * R * C; q.out_pitch = 2 * C;
-        q.out_t = xt[(s + 1) & 1]; q.out_t_matrix = 2 * R * C; q.out_t_pitch = 2 * R;
+        q.p = mb; q.p_matrix = R * tp; q.p_pitch = tp;
+        q.q = xt[s & 1]; q.q_matrix = C * tp; q.q_pitch = tp;
+        q.kblocks = (o->rows + NS_KBLOCK - 1) / NS_KBLOCK;
+        q.old = xt[s & 1]; q.old_matrix = C * tp; q.old_pitch = tp;
+        q.out = x; q.out_matrix = R * xp; q.out_pitch = xp;
+        q.out_t = xt[(s + 1) & 1]; q.out_t_matrix = C * tp; q.out_t_pitch = tp;
         q.alpha = c[0];
         q.beta = 1.0f / NS_SCALE_B;
         if (s + 1 < o->steps) {
-            e = product<NS_APPLY, float>(o, q, o->tile[2], false, st);
+            e = product<NS_APPLY, float>(o, q, OF_X, st);
             continue;
         }
         q.alpha = c[0] / NS_SCALE_X;
         q.beta = 1.0f / (NS_SCALE_B * NS_SCALE_X);
         q.result = result;
-        e = o->out_dtype == RB_F32 ? product<NS_LAST, float>(o, q, o->tile[2], false, st) : product<NS_LAST, Bf16>(o, q, o->tile[2], false, st);
+        e = o->out_dtype == RB_F32 ? product<NS_LAST, float>(o, q, OF_X, st) : product<NS_LAST, Bf16>(o, q, OF_X, st);
     }
     return e;
 }
@@ -364,17 +391,7 @@ int rb_ortho_create(rb_ortho** out, int64_t matrices, int64_t m, int64_t n, int3
     o->cols = (int32_t)std::max(m, n);
     o->small = o->cols <= 64 ? 64 : o->cols <= 128 ? 128 : 0;
     o->bytes = 256;
-    if (!o->small) {
-        choose_tiles(o);
-        const size_t kept = (size_t)matrices * o->prows * o->pcols * 4, square = (size_t)matrices * o->prows * o->prows * 4;
-        size_t off = round_up((size_t)matrices * NS_PARTS * sizeof(double), 256);
-        o->off_x = off; off += kept;
-        o->off_xt[0] = off; off += kept;
-        o->off_xt[1] = off; off += kept;
-        o->off_a = off; off += square;
-        o->off_b = off; off += square;
-        o->bytes = off;
-    }
+    if (!o->small) choose_tiles(o);
     *out = o;
     return RB_OK;
 }
