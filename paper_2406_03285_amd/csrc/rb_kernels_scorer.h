@@ -5,8 +5,8 @@
 // workgroups are joined by the same rule, and lse = m + log s, entropy = log s - t / s.
 // Alternatives.  A wavefront keeps its best 64 elements so far as one 64-bit key per lane, sorted: the logit in an order-preserving 32-bit
 // form above the inverted index, so that equal logits order by index and no two keys are equal.  A lane whose tile holds nothing above the
-// smallest key that still counts (which the running maximum tells at no cost) goes on; of the others the tile's elements are read again
-// (they are in the cache), what passes is queued, and a full queue is sorted and merged into the list.
+// smallest key that still counts (which the running maximum tells at no cost) goes on; the vectors that do are put into LDS, a lane takes
+// one element of them each, what passes is queued, and a full queue is sorted and merged into the list.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -18,10 +18,11 @@ namespace {
 constexpr int SC_WAVE = 64;
 constexpr int SC_TPB = 256;
 constexpr int SC_NWAVE = SC_TPB / SC_WAVE;
+constexpr int SC_MANY_WAVES = 16;                  // of a workgroup that has a row to itself while most of the chip is idle
 constexpr int SC_LANE_ELEMS = 32;                  // elements of a tile per lane: 4 loads of 8 bfloat16, 8 of 4 binary32
 constexpr int SC_TILE = SC_WAVE * SC_LANE_ELEMS;   // elements of a wavefront's tile
 constexpr int SC_MAX_SPLITS = 64;                  // most workgroups that share a row (the last one's lanes join them)
-constexpr int SC_SPLIT_GROUPS = 1024;              // most workgroups of a launch whose rows are shared
+constexpr int SC_SPLIT_GROUPS = 256;               // most workgroups of a launch whose rows are shared
 constexpr float SC_LOG2E = 1.44269504088896340736f;
 constexpr float SC_FLOOR = -200.0f;                // e^-200 is 0 in binary32: what is further below the maximum adds nothing, and 0 * floor is 0
 
@@ -87,6 +88,43 @@ struct RowSpan {
     }
 };
 
+// ---- between lanes -----------------------------------------------------------
+
+// The value of lane ^ D, without a trip through LDS.
+template <int D>
+__device__ __forceinline__ uint32_t sc_xor(uint32_t v)
+{
+    static_assert(D == 1 || D == 2 || D == 4 || D == 8 || D == 16 || D == 32, "a power of two within a wavefront");
+    const int x = (int)v;
+    if constexpr (D == 1) return (uint32_t)__builtin_amdgcn_update_dpp(0, x, 0xB1, 0xf, 0xf, false);             // quad_perm 1 0 3 2
+    if constexpr (D == 2) return (uint32_t)__builtin_amdgcn_update_dpp(0, x, 0x4E, 0xf, 0xf, false);             // quad_perm 2 3 0 1
+    if constexpr (D == 4) return (uint32_t)__builtin_amdgcn_update_dpp(0, __builtin_amdgcn_update_dpp(0, x, 0x141, 0xf, 0xf, false), 0x1B, 0xf, 0xf, false);   // halves of a row mirrored, quads mirrored
+    if constexpr (D == 8) return (uint32_t)__builtin_amdgcn_update_dpp(0, x, 0x128, 0xf, 0xf, false);            // rows of 16 turned by 8
+    if constexpr (D == 16) {
+        const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);      // [0]: odd rows hold the even ones, [1]: even rows the odd ones
+        return threadIdx.x & 16 ? r[0] : r[1];
+    }
+    if constexpr (D == 32) {
+        const auto r = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+        return threadIdx.x & 32 ? r[0] : r[1];
+    }
+}
+template <int D> __device__ __forceinline__ float sc_xor(float v) { return __uint_as_float(sc_xor<D>(__float_as_uint(v))); }
+template <int D> __device__ __forceinline__ uint64_t sc_xor(uint64_t v)
+{
+    return ((uint64_t)sc_xor<D>((uint32_t)(v >> 32)) << 32) | sc_xor<D>((uint32_t)v);
+}
+// Lane i's value in lane 63 - i.
+__device__ __forceinline__ uint64_t sc_reverse(uint64_t v)
+{
+    auto mirror = [](uint32_t x) { return sc_xor<32>(sc_xor<16>((uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x140, 0xf, 0xf, false))); };   // row_mirror
+    return ((uint64_t)mirror((uint32_t)(v >> 32)) << 32) | mirror((uint32_t)v);
+}
+__device__ __forceinline__ uint64_t sc_lane(uint64_t v, int lane)          // the same lane for all
+{
+    return ((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32) | (uint32_t)__builtin_amdgcn_readlane((int)v, lane);
+}
+
 // ---- running maximum and sums ------------------------------------------------
 
 struct Stats {
@@ -110,12 +148,11 @@ __device__ __forceinline__ Stats sc_join(const Stats a, const Stats b)
     return Stats{m, x.s + y.s, x.t + y.t};
 }
 
-__device__ __forceinline__ Stats sc_join_wave(Stats a)
+template <int D>
+__device__ __forceinline__ Stats sc_join_xor(const Stats a) { return sc_join(a, Stats{sc_xor<D>(a.m), sc_xor<D>(a.s), sc_xor<D>(a.t)}); }
+__device__ __forceinline__ Stats sc_join_wave(const Stats a)
 {
-#pragma unroll
-    for (int d = SC_WAVE / 2; d > 0; d >>= 1)
-        a = sc_join(a, Stats{__shfl_xor(a.m, d), __shfl_xor(a.s, d), __shfl_xor(a.t, d)});
-    return a;
+    return sc_join_xor<1>(sc_join_xor<2>(sc_join_xor<4>(sc_join_xor<8>(sc_join_xor<16>(sc_join_xor<32>(a))))));
 }
 
 template <int COUNT>
@@ -158,34 +195,42 @@ __device__ __forceinline__ uint32_t sc_order(float z)              // orders as 
 __device__ __forceinline__ float sc_unorder(uint32_t o) { return __uint_as_float(o & 0x80000000u ? o ^ 0x80000000u : ~o); }
 __device__ __forceinline__ uint64_t sc_key(float z, uint32_t index) { return ((uint64_t)sc_order(z) << 32) | (uint32_t)~index; }
 
-template <typename K>
-__device__ __forceinline__ K sc_exchange(K key, int distance, bool keep_larger)
+template <int D, typename K>
+__device__ __forceinline__ K sc_exchange(K key, bool keep_larger)
 {
-    const K other = __shfl_xor(key, distance);
+    const K other = sc_xor<D>(key);
     return (key > other) == keep_larger ? key : other;             // (equal keys: either)
+}
+
+// Runs of SIZE lanes whose keys rise and then fall (or the other way round), put in order: downwards where `down`.
+template <int SIZE, typename K>
+__device__ __forceinline__ K sc_bitonic(K key, bool down)
+{
+    if constexpr (SIZE > 1) {
+        constexpr int D = SIZE / 2;
+        key = sc_exchange<D>(key, ((threadIdx.x & D) == 0) == down);
+        return sc_bitonic<D>(key, down);
+    }
+    return key;
 }
 
 // The wavefront's keys, largest in lane 0.
 template <typename K>
 __device__ __forceinline__ K sc_sort(K key)
 {
-    const int lane = threadIdx.x & (SC_WAVE - 1);
-#pragma unroll
-    for (int k = 2; k <= SC_WAVE; k <<= 1)
-#pragma unroll
-        for (int d = k >> 1; d > 0; d >>= 1) key = sc_exchange(key, d, ((lane & d) == 0) == ((lane & k) == 0));
-    return key;
+    key = sc_bitonic<2>(key, (threadIdx.x & 2) == 0);
+    key = sc_bitonic<4>(key, (threadIdx.x & 4) == 0);
+    key = sc_bitonic<8>(key, (threadIdx.x & 8) == 0);
+    key = sc_bitonic<16>(key, (threadIdx.x & 16) == 0);
+    key = sc_bitonic<32>(key, (threadIdx.x & 32) == 0);
+    return sc_bitonic<64>(key, true);
 }
 
 // The 64 largest of two sorted lists, sorted.
 __device__ __forceinline__ uint64_t sc_merge(uint64_t a, uint64_t b)
 {
-    const int lane = threadIdx.x & (SC_WAVE - 1);
-    b = __shfl(b, SC_WAVE - 1 - lane);
-    uint64_t key = a > b ? a : b;
-#pragma unroll
-    for (int d = SC_WAVE / 2; d > 0; d >>= 1) key = sc_exchange(key, d, (lane & d) == 0);
-    return key;
+    b = sc_reverse(b);
+    return sc_bitonic<64>(a > b ? a : b, true);
 }
 
 __device__ __forceinline__ void sc_lds_wait() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
@@ -210,7 +255,7 @@ struct Best {
         queue[lane] = rest;
         queued = max(queued - SC_WAVE, 0);
         list = sc_merge(list, sc_sort(key));
-        least = __shfl(list, top - 1);
+        least = sc_lane(list, top - 1);
         if (shared != nullptr && lane == 0) atomicMax(shared, (uint32_t)(least >> 32));
     }
     __device__ __forceinline__ void push(uint64_t key, bool wanted)
@@ -229,9 +274,16 @@ struct Best {
 
 // ---- one row's share of a wavefront ------------------------------------------
 
+constexpr int SC_STAGED = 64;        // vectors of a tile that hold something wanted; of a tile with more the lanes are gone through one by one
+
+struct Staged {
+    sc_vec vectors[SC_STAGED];
+    int32_t numbers[SC_STAGED];
+};
+
 // Tiles part, part + parts, ... of the row; the elements at its unaligned ends fall to part 0.
 template <typename T, bool TOP>
-__device__ __forceinline__ void sc_scan(const T* row, int vocab, int part, int parts, Stats& stats, Best& best)
+__device__ __forceinline__ void sc_scan(const T* row, int vocab, int part, int parts, Stats& stats, Best& best, Staged* staged)
 {
     constexpr int N = Logit<T>::N, U = SC_LANE_ELEMS / N;
     const int lane = threadIdx.x & (SC_WAVE - 1);
@@ -245,49 +297,75 @@ __device__ __forceinline__ void sc_scan(const T* row, int vocab, int part, int p
 #pragma unroll
             for (int u = 0; u < U; ++u) v[u] = span.body[v0 + u * SC_WAVE];
         } else {
-            uint32_t none = 0xff800000u;                           // -inf, one binary32 or (its upper half, twice) two bfloat16
-            if (sizeof(T) == 2) none = 0xff80ff80u;
+            const uint32_t none = sizeof(T) == 2 ? 0xff80ff80u : 0xff800000u;      // -inf: two bfloat16 or one binary32
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 v[u] = sc_vec{none, none, none, none};
                 if (v0 + u * SC_WAVE < span.vectors) v[u] = span.body[v0 + u * SC_WAVE];
             }
         }
-        float z[SC_LANE_ELEMS];
+        float z[SC_LANE_ELEMS], vector_max[U], tile_max = sc_neg_inf();
 #pragma unroll
-        for (int u = 0; u < U; ++u) Logit<T>::unpack(v[u], z + u * N);
-        const float tile_max = sc_max<SC_LANE_ELEMS>(z);
+        for (int u = 0; u < U; ++u) {
+            Logit<T>::unpack(v[u], z + u * N);
+            vector_max[u] = sc_max<N>(z + u * N);
+            tile_max = fmaxf(tile_max, vector_max[u]);
+        }
         sc_absorb<SC_LANE_ELEMS>(stats, z, tile_max);
         if (TOP) {
+            // An element that only equals the list's last one has a higher index than that; one below what another wavefront's list ends with is not wanted.
             const bool any = v0 < span.vectors;
-            uint32_t least = 0;                                    // what an element has to reach
-            bool look;
-            if (first) {
-                // At least `top` elements reach the top-th largest of the lanes' maxima (fewer lanes than that: all are looked at).
-                least = __shfl(sc_sort(any ? sc_order(tile_max) : 0u), best.top - 1);
-                look = any && sc_order(tile_max) >= least;
-            } else {
-                if (best.shared != nullptr) least = __hip_atomic_load(best.shared, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
-                // (an element that only equals the list's last one has a higher index than that)
-                look = any && (best.least == 0 || sc_order(tile_max) > (uint32_t)(best.least >> 32)) && sc_order(tile_max) >= least;
+            uint32_t least = best.least == 0 ? 0 : (uint32_t)(best.least >> 32) + 1;
+            if (best.shared != nullptr) least = max(least, __hip_atomic_load(best.shared, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP));
+            const uint32_t highest = any ? sc_order(tile_max) : 0;
+            uint64_t who = __ballot(any && highest >= least);
+            if (who != 0) {
+                if (first || __popcll(who) > 16) {
+                    // At least `top` elements reach the top-th largest of the lanes' maxima (fewer lanes than that: all are looked at).
+                    least = max(least, (uint32_t)__builtin_amdgcn_readlane((int)sc_sort(highest), best.top - 1));
+                    who = __ballot(any && highest >= least);
+                }
+                int count = 0;
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    const bool hit = v0 + u * SC_WAVE < span.vectors && sc_order(vector_max[u]) >= least;
+                    const uint64_t hits = __ballot(hit);
+                    if (hits != 0) {
+                        const int at = count + __builtin_amdgcn_mbcnt_hi((uint32_t)(hits >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)hits, 0));
+                        if (hit && at < SC_STAGED) {
+                            staged->vectors[at] = v[u];
+                            staged->numbers[at] = v0 + u * SC_WAVE;
+                        }
+                        count += __popcll(hits);
+                    }
+                }
+                if (count <= SC_STAGED) {
+                    sc_lds_wait();
+                    for (int at = lane / N; at - lane / N < count; at += SC_WAVE / N) {
+                        const bool there = at < count;
+                        const int from = there ? at : 0;
+                        const float x = Logit<T>::one(reinterpret_cast<const T*>(&staged->vectors[from]) + lane % N);
+                        best.push(sc_key(x, (uint32_t)(span.head + staged->numbers[from] * N + lane % N)), there && sc_order(x) >= least);
+                    }
+                } else {
+                    while (who != 0) {
+                        // lanes 0..31 read the elements of one of them, lanes 32..63 those of the next
+                        const int a = __builtin_ctzll(who);
+                        who &= who - 1;
+                        const int b = who ? __builtin_ctzll(who) : -1;
+                        who &= who - 1;
+                        const int of = lane < SC_LANE_ELEMS ? a : b, j = lane & (SC_LANE_ELEMS - 1);
+                        const int vector = tile * (SC_WAVE * U) + (j / N) * SC_WAVE + of;
+                        const bool there = of >= 0 && vector < span.vectors;
+                        const int index = span.head + vector * N + j % N;
+                        float x = 0.0f;
+                        if (there) x = Logit<T>::one(row + index);
+                        best.push(sc_key(x, (uint32_t)index), there && sc_order(x) >= least);
+                    }
+                }
+                if (first) best.flush();
+                first = false;
             }
-            uint64_t who = __ballot(look);
-            while (who != 0) {
-                // lanes 0..31 read the elements of one of them, lanes 32..63 those of the next
-                const int a = __builtin_ctzll(who);
-                who &= who - 1;
-                const int b = who ? __builtin_ctzll(who) : -1;
-                who &= who - 1;
-                const int of = lane < SC_LANE_ELEMS ? a : b, j = lane & (SC_LANE_ELEMS - 1);
-                const int vector = tile * (SC_WAVE * U) + (j / N) * SC_WAVE + of;
-                const bool there = of >= 0 && vector < span.vectors;
-                const int index = span.head + vector * N + j % N;
-                float x = 0.0f;
-                if (there) x = Logit<T>::one(row + index);
-                best.push(sc_key(x, (uint32_t)index), there && sc_order(x) >= least);
-            }
-            if (first) best.flush();
-            first = false;
         }
     }
     if (part == 0 && span.head + span.tail > 0) {
@@ -341,24 +419,25 @@ __device__ __forceinline__ void sc_finish(const ScoreArgs& a, const T* z, int64_
     }
 }
 
-// A wavefront per row (WAVES 1: short rows) or a workgroup per row or per 1 / splits of one (WAVES 4).
+// A wavefront per row (WAVES 1, in workgroups of four: short rows), or a workgroup of WAVES per row or per 1 / splits of one.
 template <typename T, bool TOP, int WAVES>
-__global__ __launch_bounds__(SC_TPB) void rb_score_kernel(const ScoreArgs a)
+__global__ __launch_bounds__(WAVES == 1 ? SC_TPB : WAVES * SC_WAVE) void rb_score_kernel(const ScoreArgs a)
 {
-    __shared__ uint64_t queues[SC_NWAVE][TOP ? 2 * SC_WAVE : 1];
-    const int wave = threadIdx.x / SC_WAVE, lane = threadIdx.x & (SC_WAVE - 1);
+    constexpr int LISTS = WAVES == 1 ? SC_NWAVE : WAVES;
+    __shared__ uint64_t queues[LISTS][TOP ? 2 * SC_WAVE : 1];
+    __shared__ Staged staged[TOP ? LISTS : 1];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / SC_WAVE), lane = threadIdx.x & (SC_WAVE - 1);
     Stats st{sc_neg_inf(), 0.0f, 0.0f};
     if (WAVES == 1) {
         const int64_t row = (int64_t)blockIdx.x * SC_NWAVE + wave;
         if (row >= a.rows) return;
         const T* z = static_cast<const T*>(a.logits) + row * a.stride;
         Best best(queues[wave], nullptr, a.top);
-        sc_scan<T, TOP>(z, a.vocab, 0, 1, st, best);
+        sc_scan<T, TOP>(z, a.vocab, 0, 1, st, best, &staged[TOP ? wave : 0]);
         sc_finish(a, z, row, sc_join_wave(st), best.list);
         return;
     }
-    __shared__ uint64_t lists[SC_NWAVE][TOP ? SC_WAVE : 1];
-    __shared__ Stats stats[SC_NWAVE];
+    __shared__ Stats stats[LISTS];
     __shared__ uint32_t shared;
     const int64_t row = blockIdx.x / (uint32_t)a.splits;
     const int split = blockIdx.x % (uint32_t)a.splits;
@@ -368,19 +447,26 @@ __global__ __launch_bounds__(SC_TPB) void rb_score_kernel(const ScoreArgs a)
         __syncthreads();
     }
     Best best(queues[wave], TOP ? &shared : nullptr, a.top);
-    sc_scan<T, TOP>(z, a.vocab, split * SC_NWAVE + wave, a.splits * SC_NWAVE, st, best);
+    sc_scan<T, TOP>(z, a.vocab, split * WAVES + wave, a.splits * WAVES, st, best, &staged[TOP ? wave : 0]);
     st = sc_join_wave(st);
     if (lane == 0) stats[wave] = st;
-    if (TOP) lists[wave][lane] = best.list;
-    __syncthreads();
-    if (wave != 0) return;
-    st = stats[0];
     uint64_t list = best.list;
+    if (TOP) {
+        // half of the lists into the other half, and so on
+        queues[wave][lane] = list;
 #pragma unroll
-    for (int w = 1; w < SC_NWAVE; ++w) {
-        st = sc_join(st, stats[w]);
-        if (TOP) list = sc_merge(list, lists[w][lane]);
+        for (int d = WAVES / 2; d > 0; d >>= 1) {
+            __syncthreads();
+            if (wave < d) {
+                list = sc_merge(list, queues[wave + d][lane]);
+                queues[wave][lane] = list;
+            }
+        }
+    } else {
+        __syncthreads();
     }
+    if (wave != 0) return;
+    st = sc_join_wave(lane < WAVES ? stats[lane] : Stats{sc_neg_inf(), 0.0f, 0.0f});
     if (a.splits > 1) {
         // Every workgroup leaves its part; the one that is last to do so joins them, in the order of the parts whoever it is.
         const size_t bytes = sc_partial_bytes(a.top);
@@ -452,8 +538,12 @@ __global__ __launch_bounds__(SC_TPB) void rb_score_grad_kernel(const GradArgs a)
         }
     }
     float sum = w;
-#pragma unroll
-    for (int d = SC_WAVE / 2; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
+    sum += sc_xor<32>(sum);
+    sum += sc_xor<16>(sum);
+    sum += sc_xor<8>(sum);
+    sum += sc_xor<4>(sum);
+    sum += sc_xor<2>(sum);
+    sum += sc_xor<1>(sum);
     hit[threadIdx.x] = 0;
     __syncthreads();
     if (threadIdx.x < 64) {

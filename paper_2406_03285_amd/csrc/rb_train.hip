@@ -26,10 +26,12 @@ inline int64_t elem_bytes(int32_t dtype) { return dtype == RB_F32 ? 4 : 2; }
 inline size_t scorer_bytes(int32_t top) { return SC_SPLIT_GROUPS * (sizeof(uint32_t) + sc_partial_bytes(top)); }
 
 template <typename T, bool TOP>
-hipError_t score(const ScoreArgs& a, bool wave_per_row, hipStream_t st)
+hipError_t score(const ScoreArgs& a, int waves, hipStream_t st)
 {
-    if (wave_per_row) return launch(rb_score_kernel<T, TOP, 1>, dim3((unsigned)((a.rows + SC_NWAVE - 1) / SC_NWAVE)), SC_TPB, 0, st, a);
-    return launch(rb_score_kernel<T, TOP, SC_NWAVE>, dim3((unsigned)a.rows * (unsigned)a.splits), SC_TPB, 0, st, a);
+    if (waves == 1) return launch(rb_score_kernel<T, TOP, 1>, dim3((unsigned)((a.rows + SC_NWAVE - 1) / SC_NWAVE)), SC_TPB, 0, st, a);
+    const dim3 grid((unsigned)a.rows * (unsigned)a.splits);
+    if (waves == SC_NWAVE) return launch(rb_score_kernel<T, TOP, SC_NWAVE>, grid, SC_TPB, 0, st, a);
+    return launch(rb_score_kernel<T, TOP, SC_MANY_WAVES>, grid, SC_MANY_WAVES * SC_WAVE, 0, st, a);
 }
 
 template <typename T>
@@ -111,14 +113,16 @@ int rb_scorer_score(rb_scorer* s, const void* logits, int64_t rows, int64_t row_
     a.vocab = s->vocab;
     a.given = s->given;
     a.top = s->top;
-    a.splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>({(tiles + SC_NWAVE - 1) / SC_NWAVE, (SC_SPLIT_GROUPS / 2 + rows - 1) / rows, SC_MAX_SPLITS}));
-    const bool wave_per_row = tiles == 1;
+    // One tile is a wavefront's; rows that fill the chip get a workgroup of 4 wavefronts each.  Fewer rows get workgroups of 16, and what has
+    // more than a few tiles for each of these is shared by several workgroups.
+    const int waves = tiles == 1 ? 1 : rows >= 512 || tiles <= SC_NWAVE ? SC_NWAVE : SC_MANY_WAVES;
+    a.splits = waves == SC_MANY_WAVES ? (int32_t)std::max<int64_t>(1, std::min<int64_t>({tiles / (2 * SC_MANY_WAVES), 256 / rows, SC_MAX_SPLITS})) : 1;
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     hipError_t e;
     if (s->dtype == RB_F32)
-        e = s->top ? score<float, true>(a, wave_per_row, st) : score<float, false>(a, wave_per_row, st);
+        e = s->top ? score<float, true>(a, waves, st) : score<float, false>(a, waves, st);
     else
-        e = s->top ? score<Bf16, true>(a, wave_per_row, st) : score<Bf16, false>(a, wave_per_row, st);
+        e = s->top ? score<Bf16, true>(a, waves, st) : score<Bf16, false>(a, waves, st);
     return e == hipSuccess ? RB_OK : RB_EHIP;
 }
 
