@@ -33,10 +33,17 @@ constexpr int NS_PARTS = 1024;                 // most partial sums of a norm pe
 // value of 4 (A: 16, B: 60) is still below 65504.
 constexpr float NS_SCALE_X = 4096.0f, NS_SCALE_A = 2048.0f, NS_SCALE_B = 1024.0f;
 
-__device__ __forceinline__ void ns_split(float x, _Float16& hi, _Float16& lo)
+template <typename H, int N>      // of N neighbours, a vector of N binary16 numbers each (conversions go in pairs)
+__device__ __forceinline__ void ns_split(const float* x, H& hi, H& lo)
 {
-    hi = (_Float16)x;
-    lo = (_Float16)(x - (float)hi);
+    typedef float floats __attribute__((ext_vector_type(N)));
+    floats v, rest;
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = x[i];
+    hi = __builtin_convertvector(v, H);
+#pragma unroll
+    for (int i = 0; i < N; ++i) rest[i] = v[i] - (float)hi[i];
+    lo = __builtin_convertvector(rest, H);
 }
 __device__ __forceinline__ int64_t ns_at(int64_t row, int col, int64_t pitch) { return row * pitch + (col >> 5) * NS_KHALVES + (col & 31); }
 
@@ -191,23 +198,16 @@ __global__ __launch_bounds__(NS_TPB) void rb_ortho_split_kernel(const UpdateArgs
 #pragma unroll
     for (int b = 0; b < 64; b += NS_KBLOCK) {
         half8 hi, lo;
+        float v[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            _Float16 h, l;
-            ns_split(tile[row][b + first + e], h, l);
-            hi[e] = h;
-            lo[e] = l;
-        }
+        for (int e = 0; e < 8; ++e) v[e] = tile[row][b + first + e];
+        ns_split<half8, 8>(v, hi, lo);
         _Float16* to = along + ns_at(i0 + row, j0 + b + first, along_pitch);
         *reinterpret_cast<half8*>(to) = hi;
         *reinterpret_cast<half8*>(to + NS_KBLOCK) = lo;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            _Float16 h, l;
-            ns_split(tile[b + first + e][row], h, l);
-            hi[e] = h;
-            lo[e] = l;
-        }
+        for (int e = 0; e < 8; ++e) v[e] = tile[b + first + e][row];
+        ns_split<half8, 8>(v, hi, lo);
         to = across + ns_at(j0 + row, i0 + b + first, across_pitch);
         *reinterpret_cast<half8*>(to) = hi;
         *reinterpret_cast<half8*>(to + NS_KBLOCK) = lo;
@@ -374,12 +374,7 @@ __device__ __forceinline__ void ns_finish(const ProductArgs& a, int64_t k, int r
         return;
     }
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        _Float16 h, l;
-        ns_split(v[i], h, l);
-        hi[i / 4][i % 4] = h;
-        lo[i / 4][i % 4] = l;
-    }
+    for (int g = 0; g < 4; ++g) ns_split<half4, 4>(v + g * 4, hi[g], lo[g]);
     if (mirror) {
         char* to = reinterpret_cast<char*>(a.out_t + k * a.out_t_matrix + ns_at(c0 + line, r0, a.out_t_pitch)) + part;
 #pragma unroll
@@ -645,50 +640,71 @@ __global__ __launch_bounds__(P / 32 * (P / WN) * 64) void rb_ortho_small_kernel(
 #pragma unroll
         for (int i = 0; i < 16; ++i) x[b][i] = (float)((double)x[b][i] * inverse);
 
-    auto part = [&](char* area, int row, int column) {          // of element (row, column): hi; lo is 4 parts on
-        return area + (column / 32 * P + row) * 128 + (((column % 32 / 8) ^ (row / 2 & 7)) * 16) + column % 8 * 2;
-    };
-    auto part_lo = [&](char* area, int row, int column) {
-        return area + (column / 32 * P + row) * 128 + (((column % 32 / 8 + 4) ^ (row / 2 & 7)) * 16) + column % 8 * 2;
-    };
-    // v, scaled already, to the transposed place (4 rows of a column are neighbours there), and to its own
+    // v, scaled already, to the transposed place (4 rows of a column are neighbours there), and to its own.  The part of a line is the only thing in
+    // bits 4 to 6 of an address, so that its turn by the row is one exclusive or, and what is left of an address a constant.
+    const uint32_t across_at = (uint32_t)((wi / 32 * P + wj + col) * 128 + (col / 2 & 7) * 16 + half * 8);
+    const uint32_t along_at = (uint32_t)((wj / 32 * P + wi + half * 4) * 128 + ((col / 8) ^ (half * 2)) * 16 + col % 8 * 2);
     auto put = [&](char* across, char* along, const float (*v)[16]) {
 #pragma unroll
         for (int b = 0; b < MJ; ++b)
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
-                const int r = wi + g * 8 + half * 4, c = wj + b * 32 + col;
                 half4 hi, lo;
+                ns_split<half4, 4>(v[b] + g * 4, hi, lo);
+                if (along != nullptr) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    _Float16 h, l;
-                    ns_split(v[b][g * 4 + e], h, l);
-                    hi[e] = h;
-                    lo[e] = l;
-                    if (along != nullptr) {
-                        *reinterpret_cast<_Float16*>(part(along, r + e, c)) = h;
-                        *reinterpret_cast<_Float16*>(part_lo(along, r + e, c)) = l;
+                    for (int e = 0; e < 4; ++e) {
+                        const int turn = (g & 1) * 4 + e / 2, off = b * P * 128 + (g * 8 + e) * 128;
+                        *reinterpret_cast<_Float16*>(along + (along_at ^ (turn * 16)) + off) = hi[e];
+                        *reinterpret_cast<_Float16*>(along + (along_at ^ ((turn ^ 4) * 16)) + off) = lo[e];
                     }
                 }
-                *reinterpret_cast<half4*>(part(across, c, r)) = hi;
-                *reinterpret_cast<half4*>(part_lo(across, c, r)) = lo;
+                *reinterpret_cast<half4*>(across + (across_at ^ (g * 16)) + b * 32 * 128) = hi;
+                *reinterpret_cast<half4*>(across + (across_at ^ ((g ^ 4) * 16)) + b * 32 * 128) = lo;
             }
     };
     float16v acc[MJ];
     auto product = [&](const char* p, const char* q, int blocks) {
 #pragma unroll
         for (int b = 0; b < MJ; ++b) acc[b] = float16v{};
-        for (int ks = 0; ks < 2 * blocks; ++ks) {
-            const int c = (ks & 1) * 2 + half, hi = (c ^ (col / 2 & 7)) * 16, lo = ((c + 4) ^ (col / 2 & 7)) * 16;
-            const char* pr = p + (ks / 2 * P + wi + col) * 128;
-            const half8 ph = *reinterpret_cast<const half8*>(pr + hi), pl = *reinterpret_cast<const half8*>(pr + lo);
+        struct Fragments { half8 ph, pl, qh[MJ], ql[MJ]; };
+        auto read = [&](Fragments& f, int block, int ks) {
+            const int at = ks * 2 + half, hi = (at ^ (col / 2 & 7)) * 16, lo = ((at + 4) ^ (col / 2 & 7)) * 16;
+            const char* pr = p + (block * P + wi + col) * 128;
+            f.ph = *reinterpret_cast<const half8*>(pr + hi);
+            f.pl = *reinterpret_cast<const half8*>(pr + lo);
 #pragma unroll
             for (int b = 0; b < MJ; ++b) {
-                const char* qr = q + (ks / 2 * P + wj + b * 32 + col) * 128;
-                const half8 qh = *reinterpret_cast<const half8*>(qr + hi), ql = *reinterpret_cast<const half8*>(qr + lo);
-                acc[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(pl, qh, acc[b], 0, 0, 0);
-                acc[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph, ql, acc[b], 0, 0, 0);
-                acc[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph, qh, acc[b], 0, 0, 0);
+                const char* qr = q + (block * P + wj + b * 32 + col) * 128;
+                f.qh[b] = *reinterpret_cast<const half8*>(qr + hi);
+                f.ql[b] = *reinterpret_cast<const half8*>(qr + lo);
+            }
+        };
+        auto multiply = [&](const Fragments& f) {
+#pragma unroll
+            for (int b = 0; b < MJ; ++b) {
+                acc[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f.pl, f.qh[b], acc[b], 0, 0, 0);
+                acc[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f.ph, f.ql[b], acc[b], 0, 0, 0);
+                acc[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f.ph, f.qh[b], acc[b], 0, 0, 0);
+            }
+        };
+        if (WAVES > 4) {                                        // four wavefronts a SIMD: one multiplies while another reads
+            for (int block = 0; block < blocks; ++block) {
+#pragma unroll
+                for (int ks = 0; ks < 2; ++ks) {
+                    Fragments f;
+                    read(f, block, ks);
+                    multiply(f);
+                }
+            }
+        } else {                                                // one: half of a block is read while the other half is multiplied
+            Fragments first, second;
+            read(first, 0, 0);
+            for (int block = 0; block < blocks; ++block) {
+                read(second, block, 1);
+                multiply(first);
+                if (block + 1 < blocks) read(first, block + 1, 0);
+                multiply(second);
             }
         }
     };

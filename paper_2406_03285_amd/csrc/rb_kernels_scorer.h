@@ -12,6 +12,7 @@
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
+#include <type_traits>
 
 namespace {
 
@@ -47,11 +48,13 @@ template <> struct Logit<float> {
     }
 };
 struct Bf16 { uint16_t bits; };
-__device__ __forceinline__ uint32_t sc_bf16_bits(float x)      // to nearest, ties to even; NaN stays NaN
+typedef __bf16 sc_bf16x2 __attribute__((ext_vector_type(2)));
+typedef float sc_floatx2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t sc_bf16_pair(float a, float b)      // to nearest, ties to even; NaN stays NaN (one instruction)
 {
-    const uint32_t u = __float_as_uint(x);
-    return (u & 0x7fffffffu) > 0x7f800000u ? (u >> 16) | 0x40u : (u + 0x7fffu + ((u >> 16) & 1u)) >> 16;
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector((sc_floatx2{a, b}), sc_bf16x2));
 }
+__device__ __forceinline__ uint32_t sc_bf16_bits(float x) { return sc_bf16_pair(x, x) & 0xffffu; }
 template <> struct Logit<Bf16> {
     static constexpr int N = 8;
     static __device__ __forceinline__ float one(const Bf16* p) { return __uint_as_float((uint32_t)p->bits << 16); }
@@ -68,7 +71,7 @@ template <> struct Logit<Bf16> {
     {
         sc_vec v;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = sc_bf16_bits(z[2 * i]) | (sc_bf16_bits(z[2 * i + 1]) << 16);
+        for (int i = 0; i < 4; ++i) v[i] = sc_bf16_pair(z[2 * i], z[2 * i + 1]);
         return v;
     }
 };
@@ -390,9 +393,26 @@ struct ScoreArgs {
 
 __host__ __device__ inline size_t sc_partial_bytes(int top) { return 16 + 8 * (size_t)top; }
 
-// What a wavefront that knows a whole row writes.
+// The logit of the lane's given token, fetched before the row is gone through.
+struct Given {
+    float logit;
+    bool there;
+};
 template <typename T>
-__device__ __forceinline__ void sc_finish(const ScoreArgs& a, const T* z, int64_t row, const Stats st, uint64_t list)
+__device__ __forceinline__ Given sc_given(const ScoreArgs& a, const T* z, int64_t row)
+{
+    Given g{0.0f, false};
+    const int lane = threadIdx.x & (SC_WAVE - 1);
+    if (lane < a.given) {
+        const int64_t t = a.tokens[row * a.given + lane];
+        g.there = t >= 0 && t < a.vocab;
+        if (g.there) g.logit = Logit<T>::one(z + t);
+    }
+    return g;
+}
+
+// What a wavefront that knows a whole row writes.
+__device__ __forceinline__ void sc_finish(const ScoreArgs& a, int64_t row, const Stats st, uint64_t list, const Given& given)
 {
     const int lane = threadIdx.x & (SC_WAVE - 1);
     const bool empty = st.m == sc_neg_inf() && st.s == 0.0f;
@@ -404,13 +424,8 @@ __device__ __forceinline__ void sc_finish(const ScoreArgs& a, const T* z, int64_
         if (a.entropy != nullptr) a.entropy[row] = empty ? 0.0f : broken ? lse : log_s - st.t / st.s;
     }
     if (lane < a.given) {
-        const int64_t t = a.tokens[row * a.given + lane];
-        float v = 0.0f;
-        if (t >= 0 && t < a.vocab) {
-            const float x = Logit<T>::one(z + t);
-            v = broken ? lse : x == sc_neg_inf() ? x : (x - st.m) - log_s;      // (x - lse would be off by lse's last bit)
-        }
-        a.logp[row * a.given + lane] = v;
+        const float x = given.logit;
+        a.logp[row * a.given + lane] = !given.there ? 0.0f : broken ? lse : x == sc_neg_inf() ? x : (x - st.m) - log_s;      // (x - lse would be off by lse's last bit)
     }
     if (lane < a.top) {
         const float x = sc_unorder((uint32_t)(list >> 32));
@@ -433,8 +448,9 @@ __global__ __launch_bounds__(WAVES == 1 ? SC_TPB : WAVES * SC_WAVE) void rb_scor
         if (row >= a.rows) return;
         const T* z = static_cast<const T*>(a.logits) + row * a.stride;
         Best best(queues[wave], nullptr, a.top);
+        const Given given = sc_given(a, z, row);
         sc_scan<T, TOP>(z, a.vocab, 0, 1, st, best, &staged[TOP ? wave : 0]);
-        sc_finish(a, z, row, sc_join_wave(st), best.list);
+        sc_finish(a, row, sc_join_wave(st), best.list, given);
         return;
     }
     __shared__ Stats stats[LISTS];
@@ -447,6 +463,8 @@ __global__ __launch_bounds__(WAVES == 1 ? SC_TPB : WAVES * SC_WAVE) void rb_scor
         __syncthreads();
     }
     Best best(queues[wave], TOP ? &shared : nullptr, a.top);
+    Given given{};
+    if (wave == 0) given = sc_given(a, z, row);
     sc_scan<T, TOP>(z, a.vocab, split * WAVES + wave, a.splits * WAVES, st, best, &staged[TOP ? wave : 0]);
     st = sc_join_wave(st);
     if (lane == 0) stats[wave] = st;
@@ -489,7 +507,7 @@ __global__ __launch_bounds__(WAVES == 1 ? SC_TPB : WAVES * SC_WAVE) void rb_scor
             for (int p = 0; p < a.splits; ++p) list = sc_merge(list, lane < a.top ? reinterpret_cast<const uint64_t*>(parts + p * bytes + 16)[lane] : 0);
         }
     }
-    sc_finish(a, z, row, st, list);
+    sc_finish(a, row, st, list, given);
 }
 
 // ---- gradient ----------------------------------------------------------------
@@ -508,7 +526,7 @@ constexpr int GR_MAX_TILES = 32;    // tiles of SC_TPB accesses in a chunk: one 
 // A workgroup per row (blockIdx.x) and chunk of the row (blockIdx.y).  N elements per access: 16 bytes, or one element where logits and
 // gradient lie differently relative to 16 bytes.  Which of a thread's accesses hold a given token is one word of bits, so that the rest
 // costs one test; the tokens' sums are made in the order in which they were given.
-template <typename T, int N>
+template <typename T, int N, bool ENTROPY>
 __global__ __launch_bounds__(SC_TPB) void rb_score_grad_kernel(const GradArgs a)
 {
     __shared__ uint32_t hit[SC_TPB];
@@ -518,7 +536,7 @@ __global__ __launch_bounds__(SC_TPB) void rb_score_grad_kernel(const GradArgs a)
     const T* z = static_cast<const T*>(a.logits) + row * a.stride;
     T* dz = static_cast<T*>(a.grad) + row * a.grad_stride;
     const float lse = a.lse[row];
-    const float h = a.grad_entropy != nullptr ? a.grad_entropy[row] : 0.0f, ent = a.grad_entropy != nullptr ? a.entropy[row] : 0.0f;
+    const float h = ENTROPY ? a.grad_entropy[row] : 0.0f, entropy = ENTROPY ? a.entropy[row] : 0.0f;
     int head = 0, count = a.vocab, tail = 0;
     if (N > 1) {
         const RowSpan<T> span(z, a.vocab);
@@ -555,16 +573,21 @@ __global__ __launch_bounds__(SC_TPB) void rb_score_grad_kernel(const GradArgs a)
     __syncthreads();
     const uint32_t mine = hit[threadIdx.x];
     const bool dead = lse == sc_neg_inf();
+    const float rest = fmaf(h, entropy, sum);
     auto value = [&](float x) {
-        const float l = fmaxf(x - lse, SC_FLOOR), p = __builtin_amdgcn_exp2f((x - lse) * SC_LOG2E);
-        return -p * fmaf(h, l + ent, sum);
+        const float d = x - lse, p = __builtin_amdgcn_exp2f(d * SC_LOG2E);
+        return -p * (ENTROPY ? fmaf(h, fmaxf(d, SC_FLOOR), rest) : sum);
     };
-    auto given = [&](int j) {
-        float v = 0.0f;
-        for (int g = 0; g < a.given; ++g)
-            if (ids[g] == j) v += weights[g];
-        return v;
+    // what is given for COUNT elements from `first` on
+    auto given = [&](float* x, int first, auto count) {
+        for (int g = 0; g < a.given; ++g) {
+            const int at = ids[g] - first;
+            const float v = weights[g];
+#pragma unroll
+            for (int i = 0; i < decltype(count)::value; ++i) x[i] += at == i ? v : 0.0f;
+        }
     };
+    using One = std::integral_constant<int, 1>;
     if (N > 1) {
         constexpr int U = 4;
         const sc_vec* src = reinterpret_cast<const sc_vec*>(z + head);
@@ -582,11 +605,7 @@ __global__ __launch_bounds__(SC_TPB) void rb_score_grad_kernel(const GradArgs a)
                 Logit<T>::unpack(v[u], x);
 #pragma unroll
                 for (int i = 0; i < Logit<T>::N; ++i) x[i] = value(x[i]);
-                if ((mine >> (tile + u)) & 1u) {
-                    const int first = head + (i0 + u * SC_TPB) * N;
-#pragma unroll
-                    for (int i = 0; i < Logit<T>::N; ++i) x[i] += given(first + i);
-                }
+                if ((mine >> (tile + u)) & 1u) given(x, head + (i0 + u * SC_TPB) * N, std::integral_constant<int, Logit<T>::N>());
                 if (dead) {
 #pragma unroll
                     for (int i = 0; i < Logit<T>::N; ++i) x[i] = 0.0f;
@@ -596,14 +615,15 @@ __global__ __launch_bounds__(SC_TPB) void rb_score_grad_kernel(const GradArgs a)
         }
         if (blockIdx.y == 0 && threadIdx.x < head + tail) {
             const int j = threadIdx.x < head ? threadIdx.x : a.vocab - tail + (int)threadIdx.x - head;
-            const float x = value(Logit<T>::one(z + j)) + given(j);
+            float x = value(Logit<T>::one(z + j));
+            given(&x, j, One());
             dz[j] = Logit<T>::round(dead ? 0.0f : x);
         }
     } else {
         int tile = 0;
         for (int i = begin + threadIdx.x; i < end; i += SC_TPB, ++tile) {
             float x = value(Logit<T>::one(z + i));
-            if ((mine >> tile) & 1u) x += given(i);
+            if ((mine >> tile) & 1u) given(&x, i, One());
             dz[i] = Logit<T>::round(dead ? 0.0f : x);
         }
     }

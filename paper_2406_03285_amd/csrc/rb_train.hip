@@ -44,8 +44,8 @@ hipError_t score_grad(GradArgs& a, int64_t rows, bool vectors, hipStream_t st)
     const int64_t per = std::min<int64_t>(GR_MAX_TILES, std::max<int64_t>(4, (tiles + want - 1) / want));
     a.chunk = (int32_t)(per * SC_TPB);
     const dim3 grid((unsigned)rows, (unsigned)std::max<int64_t>(1, (tiles + per - 1) / per));
-    if (vectors) return launch(rb_score_grad_kernel<T, Logit<T>::N>, grid, SC_TPB, 0, st, a);
-    return launch(rb_score_grad_kernel<T, 1>, grid, SC_TPB, 0, st, a);
+    if (vectors) return launch(a.grad_entropy ? rb_score_grad_kernel<T, Logit<T>::N, true> : rb_score_grad_kernel<T, Logit<T>::N, false>, grid, SC_TPB, 0, st, a);
+    return launch(a.grad_entropy ? rb_score_grad_kernel<T, 1, true> : rb_score_grad_kernel<T, 1, false>, grid, SC_TPB, 0, st, a);
 }
 
 }  // namespace
@@ -115,7 +115,7 @@ int rb_scorer_score(rb_scorer* s, const void* logits, int64_t rows, int64_t row_
     a.top = s->top;
     // One tile is a wavefront's; rows that fill the chip get a workgroup of 4 wavefronts each.  Fewer rows get workgroups of 16, and what has
     // more than a few tiles for each of these is shared by several workgroups.
-    const int waves = tiles == 1 ? 1 : rows >= 512 || tiles <= SC_NWAVE ? SC_NWAVE : SC_MANY_WAVES;
+    const int waves = tiles == 1 || (tiles <= 8 && rows >= 4096) ? 1 : rows >= 512 || tiles <= SC_NWAVE ? SC_NWAVE : SC_MANY_WAVES;
     a.splits = waves == SC_MANY_WAVES ? (int32_t)std::max<int64_t>(1, std::min<int64_t>({tiles / (2 * SC_MANY_WAVES), 256 / rows, SC_MAX_SPLITS})) : 1;
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     hipError_t e;
@@ -296,7 +296,7 @@ hipError_t whole(const rb_ortho* o, const UpdateArgs& u, const ResultArgs& resul
         for (int i = 0; i < 3; ++i) a.coefficients[s][i] = o->coefficients[s][i];
     const size_t lds = (size_t)2 * o->small * o->small * 4;
     if (o->small == 64) return launch(rb_ortho_small_kernel<T, OUT, 64, 32>, dim3((unsigned)o->matrices), 256, lds, st, a);
-    return launch(rb_ortho_small_kernel<T, OUT, 128, 64>, dim3((unsigned)o->matrices), 512, lds, st, a);
+    return launch(rb_ortho_small_kernel<T, OUT, 128, 32>, dim3((unsigned)o->matrices), 1024, lds, st, a);
 }
 
 hipError_t orthogonalize(const rb_ortho* o, const UpdateArgs& u, const ResultArgs& result, hipStream_t st)

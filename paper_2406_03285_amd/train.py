@@ -129,6 +129,12 @@ rb_scorer_score = _native(rb_scorer_score, "hpiipppppps")
 rb_scorer_grad = _native(rb_scorer_grad, "hpiippppppis")
 rb_ortho_apply = _native(rb_ortho_apply, "hpiipiis")
 
+try:
+    from torch._C import _cuda_getCurrentRawStream as _current_stream      # (the address alone: a Stream object takes the host some us)
+except ImportError:
+    def _current_stream(index):
+        return torch.cuda.current_stream(index).cuda_stream
+
 _CODES = {torch.float32: RB_F32, torch.bfloat16: RB_BF16}
 
 
@@ -141,13 +147,20 @@ class _OnStream:
         if self.device.index is None:
             self.device = torch.device(self.device.type, torch.cuda.current_device())
         self._last = torch.cuda.current_stream(self.device)
+        self._last_address = self._last.cuda_stream
 
-    def _on_stream(self, call, *args):
-        stream = torch.cuda.current_stream(self.device)
-        if stream != self._last:
+    def _current(self):
+        """Address of the stream that a call goes to."""
+        address = _current_stream(self.device.index)
+        if address != self._last_address:
+            stream = torch.cuda.current_stream(self.device)
             if not torch.cuda.is_current_stream_capturing():
                 stream.wait_stream(self._last)
-            self._last = stream
+            self._last, self._last_address = stream, address
+        return address
+
+    def _on_stream(self, call, *args):
+        stream = self._current()
         if torch.cuda.current_device() == self.device.index:
             return call(*args, stream)
         with torch.cuda.device(self.device):
@@ -188,40 +201,58 @@ class TokenScorer(_OnStream):
         return Scores(new(rows, self.given) if self.given else None, new(rows), new(rows), new(rows, self.top) if self.top else None,
                       new(rows, self.top, dtype=torch.int64) if self.top else None)
 
-    def _look_at(self, logits, tokens):
-        rows = logits.shape[0]
-        assert logits.dim() == 2 and logits.shape[1] == self.vocab and logits.dtype == self.dtype and logits.device == self.device
-        assert logits.stride(1) == 1 or self.vocab == 1
-        if self.given:
-            assert tokens.dtype == torch.int64 and tokens.is_contiguous() and tokens.device == self.device
-            assert tokens.shape == (rows, self.given) or (self.given == 1 and tokens.shape == (rows,))
-        return rows, max(logits.stride(0), self.vocab) if rows < 2 else logits.stride(0)
+    def _rows(self, logits, what):
+        """(rows, elements between them) of a tensor of the logits' form, looked at first."""
+        shape = logits.shape
+        assert len(shape) == 2 and shape[1] == self.vocab and logits.dtype == self.dtype and logits.device == self.device, what
+        stride, step = logits.stride()
+        assert step == 1 or self.vocab == 1, what
+        return shape[0], stride if shape[0] > 1 else max(stride, self.vocab)
+
+    def _small(self, t, shape, dtype, what):
+        assert t.shape == shape and t.dtype == dtype and t.is_contiguous() and t.device == self.device, what
+
+    def _tokens(self, tokens, rows):
+        if not self.given:
+            return None
+        self._small(tokens, (rows,) if self.given == 1 and tokens.dim() == 1 else (rows, self.given), torch.int64, "tokens")
+        return tokens
 
     def score(self, logits, tokens=None, out=None):
         """Scores of every row of logits; into `out` if given (see outputs)."""
-        rows, stride = self._look_at(logits, tokens)
+        rows, stride = self._rows(logits, "logits")
+        tokens = self._tokens(tokens, rows)
         if out is None:
             out = self.outputs(rows)
-        elif rows:
-            for t, shape in zip(out, ((rows, self.given), (rows,), (rows,), (rows, self.top), (rows, self.top))):
-                assert t is None or (t.shape == shape and t.is_contiguous() and t.device == self.device)
-            assert (out.logp is None or out.logp.dtype == torch.float32) and (out.top_ids is None or out.top_ids.dtype == torch.int64)
-        _check(self._on_stream(rb_scorer_score, self.handle, logits, rows, stride, tokens if self.given else None, out.logp, out.lse,
-                               out.entropy, out.top_logp, out.top_ids), "rb_scorer_score")
+        else:
+            if self.given:
+                self._small(out.logp, (rows, self.given), torch.float32, "out.logp")
+            if self.top:
+                self._small(out.top_logp, (rows, self.top), torch.float32, "out.top_logp")
+                self._small(out.top_ids, (rows, self.top), torch.int64, "out.top_ids")
+            for t in (out.lse, out.entropy):
+                if t is not None:
+                    self._small(t, (rows,), torch.float32, "out.lse, out.entropy")
+        _check(self._on_stream(rb_scorer_score, self.handle, logits, rows, stride, tokens, out.logp if self.given else None, out.lse,
+                               out.entropy, out.top_logp if self.top else None, out.top_ids if self.top else None), "rb_scorer_score")
         return out
 
     def grad(self, logits, tokens, lse, entropy, grad_logp, grad_entropy=None, out=None):
         """The gradient with respect to the logits, from the derivatives with respect to logp [rows, given] and entropy [rows] (or None).
         out: a tensor shaped as the logits (rows may be strided), which the logits themselves may be."""
-        rows, stride = self._look_at(logits, tokens)
+        rows, stride = self._rows(logits, "logits")
+        tokens = self._tokens(tokens, rows)
         if out is None:
             out = torch.empty((rows, self.vocab), dtype=self.dtype, device=self.device)
-        assert out.shape == (rows, self.vocab) and out.dtype == self.dtype and out.device == self.device and (out.stride(1) == 1 or self.vocab == 1)
-        for t, shape in ((lse, (rows,)), (entropy, (rows,)), (grad_entropy, (rows,)), (grad_logp, (rows, self.given))):
-            if t is not None:
-                assert t.dtype == torch.float32 and t.is_contiguous() and t.device == self.device and t.numel() == math.prod(shape)
-        out_stride = max(out.stride(0), self.vocab) if rows < 2 else out.stride(0)
-        _check(self._on_stream(rb_scorer_grad, self.handle, logits, rows, stride, tokens if self.given else None, lse, entropy,
+        out_rows, out_stride = self._rows(out, "out")
+        assert out_rows == rows, "out"
+        self._small(lse, (rows,), torch.float32, "lse")
+        if self.given:
+            self._small(grad_logp, (rows,) if self.given == 1 and grad_logp.dim() == 1 else (rows, self.given), torch.float32, "grad_logp")
+        if grad_entropy is not None:
+            self._small(entropy, (rows,), torch.float32, "entropy")
+            self._small(grad_entropy, (rows,), torch.float32, "grad_entropy")
+        _check(self._on_stream(rb_scorer_grad, self.handle, logits, rows, stride, tokens, lse, None if grad_entropy is None else entropy,
                                grad_logp if self.given else None, grad_entropy, out, out_stride), "rb_scorer_grad")
         return out
 
