@@ -153,3 +153,36 @@ def test_one_matrix_of_a_batch_does_not_touch_another():
     one = rb.Orthogonalizer(150, 90)
     for i in range(4):
         assert torch.equal(one.orthogonalize(u[i]), whole[i])
+
+
+def on_the_gpu(g, coefficients, eps):
+    """ref.orthogonal for large matrices: the same products in binary64 on the GPU."""
+    x = (g.t() if g.shape[0] > g.shape[1] else g).double().contiguous()
+    x = x / (torch.linalg.vector_norm(x) + eps)
+    for a, b, c in coefficients:
+        p = x @ x.t().contiguous()
+        x = a * x + (b * p + c * (p @ p)) @ x
+    return x.t() if g.shape[0] > g.shape[1] else x
+
+
+@pytest.mark.parametrize("batch,m,n", [
+    (1, 1000, 1100), (3, 520, 777), (1, 2048, 2048), (1, 1700, 3000), (2, 1100, 1300), (1, 2048, 10016), (1, 6000, 1500), (1, 4096, 4096), (1, 3900, 4200),
+    (1, 260, 20000), (70, 130, 150), (300, 129, 140)])
+def test_every_tile_and_slicing(batch, m, n):
+    """Sizes on both sides of where larger tiles, and slices of a long summed index, are the faster ones."""
+    g = torch.Generator(device="cuda").manual_seed(m)
+    u = torch.randn((batch, m, n), generator=g, device="cuda") + torch.randn((batch, m, 4), generator=g, device="cuda") @ torch.randn((batch, 4, n), generator=g, device="cuda")
+    o = rb.Orthogonalizer(m, n, batch=batch)
+    got = o.orthogonalize(u)
+    assert torch.equal(o.orthogonalize(u), got)
+    for i in {0, batch // 2, batch - 1}:
+        want = on_the_gpu(u[i], FIVE, 1e-7)
+        assert torch.linalg.vector_norm(got[i] - want) <= ref.orthogonal_bound(FIVE) * torch.linalg.vector_norm(want)
+    if batch == 1:
+        w = torch.randn((m, n), generator=g, device="cuda").to(BF16)
+        mom = torch.zeros((m, n), device="cuda")
+        before = w.double()
+        rb.Orthogonalizer(m, n, out_dtype=BF16).step(w, u[0], mom, lr=0.5, beta=0.5, nesterov=False, weight_decay=0.5, scale=1.0)
+        want = 0.75 * before - 0.5 * on_the_gpu(u[0], FIVE, 1e-7)
+        off = torch.linalg.vector_norm(w.double() - want)
+        assert off <= 2.0 ** -9 * torch.linalg.vector_norm(want) + ref.orthogonal_bound(FIVE) * torch.linalg.vector_norm(want - 0.75 * before)
