@@ -178,7 +178,8 @@ struct rb_ortho {
     int32_t small;                 // a workgroup per matrix: its padded side (64, 128), or 0: tiled products
     int32_t kept_rows, kept_cols;  // tiled: with room for whole tiles of every product
     int32_t tile[3], slices[3];    // of A, of B, of X
-    size_t off_x, off_xt[2], off_a, off_b, off_sums, bytes;
+    int32_t block;                 // steps that are made on A before X is multiplied (1: none)
+    size_t off_x, off_xt[2], off_square[5], off_sums, bytes;
     char* ws;
 };
 
@@ -229,20 +230,44 @@ double product_us(int tile, double tiles, int kblocks, int slices)
     return slices == 1 ? us : us + 6 + tiles * slices * tile * tile * 8 / 1e7;
 }
 
-// The tiles and slices that take least, and the room that all products need.
+constexpr int NS_BLOCK = 3;      // most steps made on A before X is multiplied
+
+// Whether the products of a block's P stay within what is kept (60 in NS_SCALE_B).
+bool blocks_fit(const rb_ortho* o)
+{
+    for (int i = 0; i <= 1024; ++i) {
+        double v = i / 1024.0, r = 1.0;
+        int blocks = (o->steps + NS_BLOCK - 1) / NS_BLOCK;
+        for (int s = 0, n = 0; s < o->steps; s += n, --blocks) {
+            n = (o->steps - s + blocks - 1) / blocks;
+            r = 1.0;
+            for (int k = s; k < s + n; ++k) {
+                const float* c = o->coefficients[k];
+                const double l = v * v, p = c[0] + c[1] * l + c[2] * l * l;
+                v *= p;
+                r *= p;
+                if (!(std::fabs(p) <= 60.0) || !(std::fabs(r) <= 60.0)) return false;
+            }
+        }
+    }
+    return true;
+}
+
+// The tiles and slices that take least, whether steps are made on A, and the room that all products need.
 void choose_tiles(rb_ortho* o)
 {
     int64_t rows = round_up((size_t)o->rows, 64), cols = round_up((size_t)o->cols, 64);
     size_t sums = 0;
+    double us[3];
     for (int which = 0; which < 3; ++which) {
-        double least = 1e300;
+        us[which] = 1e300;
         for (int tile = 64; tile <= 256; tile += 64) {
             const int64_t n = (o->rows + tile - 1) / tile, m = (o->cols + tile - 1) / tile, tiles = o->matrices * (which == OF_X ? n * m : n * (n + 1) / 2);
             const int kblocks = ((which == OF_A ? o->cols : o->rows) + NS_KBLOCK - 1) / NS_KBLOCK;
             for (int slices = 1; slices <= 16 && (slices == 1 || (kblocks / slices >= 8 && tiles * slices <= 512)); ++slices) {
-                const double us = product_us(tile, (double)tiles, kblocks, slices);
-                if (us >= least) continue;
-                least = us;
+                const double t = product_us(tile, (double)tiles, kblocks, slices);
+                if (t >= us[which]) continue;
+                us[which] = t;
                 o->tile[which] = tile;
                 o->slices[which] = slices;
             }
@@ -252,6 +277,10 @@ void choose_tiles(rb_ortho* o)
         cols = std::max(cols, (int64_t)((which == OF_X ? m : n) * tile));
         if (o->slices[which] > 1) sums = std::max(sums, (size_t)o->matrices * (which == OF_X ? n * m : n * (n + 1) / 2) * o->slices[which] * tile * tile * sizeof(float));
     }
+    // a block of n steps: A, n B, n - 1 times the two of A and the one of R, and R X, instead of n times A, B, B X
+    const int blocks = (o->steps + NS_BLOCK - 1) / NS_BLOCK;
+    const double by_blocks = blocks * (us[OF_A] + us[OF_X]) + (o->steps + 3 * (o->steps - blocks)) * us[OF_B];
+    o->block = by_blocks < o->steps * (us[OF_A] + us[OF_B] + us[OF_X]) && blocks_fit(o) ? NS_BLOCK : 1;
     o->kept_rows = (int32_t)rows;
     o->kept_cols = (int32_t)cols;
     const size_t n = (size_t)o->matrices * sizeof(_Float16), xp = (size_t)ns_pitch(cols), tp = (size_t)ns_pitch(rows);
@@ -259,8 +288,10 @@ void choose_tiles(rb_ortho* o)
     o->off_x = off; off += n * (size_t)rows * xp;
     o->off_xt[0] = off; off += n * (size_t)cols * tp;
     o->off_xt[1] = off; off += n * (size_t)cols * tp;
-    o->off_a = off; off += n * (size_t)rows * tp;
-    o->off_b = off; off += n * (size_t)rows * tp;
+    for (int i = 0; i < 5; ++i) {                          // A, B (P); of blocks also P A and two R
+        o->off_square[i] = off;
+        if (i < 2 || o->block > 1) off += n * (size_t)rows * tp;
+    }
     o->off_sums = off; off += sums;
     o->bytes = off;
 }
@@ -306,46 +337,68 @@ hipError_t orthogonalize(const rb_ortho* o, const UpdateArgs& u, const ResultArg
         return o->out_dtype == RB_F32 ? whole<Bf16, float>(o, u, result, st) : whole<Bf16, Bf16>(o, u, result, st);
     }
     const int64_t R = o->kept_rows, C = o->kept_cols;
-    _Float16* x = reinterpret_cast<_Float16*>(o->ws + o->off_x);
-    _Float16* xt[2] = {reinterpret_cast<_Float16*>(o->ws + o->off_xt[0]), reinterpret_cast<_Float16*>(o->ws + o->off_xt[1])};
-    _Float16* ma = reinterpret_cast<_Float16*>(o->ws + o->off_a);
-    _Float16* mb = reinterpret_cast<_Float16*>(o->ws + o->off_b);
-    const int64_t xp = ns_pitch(C), tp = ns_pitch(R);     // halves between rows of X; of X^T, A and B
+    const int64_t xp = ns_pitch(C), tp = ns_pitch(R);     // halves between rows of X; of X^T and the squares
+    auto place = [&](size_t off) { return reinterpret_cast<_Float16*>(o->ws + off); };
+    _Float16 *const x = place(o->off_x), *const xt[2] = {place(o->off_xt[0]), place(o->off_xt[1])};
     const KeptArgs kept{x, xt[0], R * xp, C * tp, xp, tp, (int32_t)R, (int32_t)C};
     hipError_t e = o->dtype == RB_F32 ? first_pass<float>(o, u, kept, st) : first_pass<Bf16>(o, u, kept, st);
-    for (int s = 0; s < o->steps && e == hipSuccess; ++s) {
-        const float* c = o->coefficients[s];
-        ProductArgs g{};                                   // A = X X^T
+    // to <- beta * p q^T of two squares that commute (symmetric), + alpha * old + diagonal
+    auto square = [&](_Float16* to, const _Float16* p, const _Float16* q, float beta) {
+        ProductArgs a{};
+        a.p = p; a.q = q; a.p_matrix = a.q_matrix = R * tp; a.p_pitch = a.q_pitch = tp;
+        a.kblocks = (o->rows + NS_KBLOCK - 1) / NS_KBLOCK;
+        a.out = to; a.out_t = to; a.out_matrix = a.out_t_matrix = R * tp; a.out_pitch = a.out_t_pitch = tp;
+        a.beta = beta;
+        return a;
+    };
+    _Float16 *const ma = place(o->off_square[0]), *const mb = place(o->off_square[1]);
+    int blocks = (o->steps + o->block - 1) / o->block;
+    for (int s = 0, n = 0, now = 0; s < o->steps && e == hipSuccess; s += n, now ^= 1, --blocks) {
+        n = (o->steps - s + blocks - 1) / blocks;          // steps of this block: as even as it goes, longer ones first
+        ProductArgs g = square(ma, nullptr, nullptr, NS_SCALE_A / (NS_SCALE_X * NS_SCALE_X));                       // A = X X^T
         g.p = x; g.q = x; g.p_matrix = g.q_matrix = R * xp; g.p_pitch = g.q_pitch = xp;
         g.kblocks = (o->cols + NS_KBLOCK - 1) / NS_KBLOCK;
-        g.out = ma; g.out_t = ma;
-        g.out_matrix = g.out_t_matrix = R * tp;
-        g.out_pitch = g.out_t_pitch = tp;
-        g.beta = NS_SCALE_A / (NS_SCALE_X * NS_SCALE_X);
         if ((e = product<NS_GRAM, float>(o, g, OF_A, st)) != hipSuccess) break;
-        ProductArgs p = g;                                 // B = b A + c A A
-        p.p = ma; p.q = ma; p.p_matrix = p.q_matrix = R * tp; p.p_pitch = p.q_pitch = tp;
-        p.kblocks = (o->rows + NS_KBLOCK - 1) / NS_KBLOCK;
-        p.old = ma; p.old_matrix = R * tp; p.old_pitch = tp;
-        p.out = mb; p.out_t = mb;
-        p.alpha = c[1] * (NS_SCALE_B / NS_SCALE_A);
-        p.beta = c[2] * (NS_SCALE_B / (NS_SCALE_A * NS_SCALE_A));
-        if ((e = product<NS_POLY, float>(o, p, OF_B, st)) != hipSuccess) break;
-        ProductArgs q{};                                   // X <- a X + B X
-        q.p = mb; q.p_matrix = R * tp; q.p_pitch = tp;
-        q.q = xt[s & 1]; q.q_matrix = C * tp; q.q_pitch = tp;
+        // B = b A + c A A and then a X + B X; or, of a block, P = a I + B, and R X
+        const _Float16* left_of_x = mb;
+        for (int i = 0; i < n && e == hipSuccess; ++i) {
+            const float* c = o->coefficients[s + i];
+            _Float16* const to = n > 1 && i == 0 ? place(o->off_square[3]) : mb;
+            ProductArgs p = square(to, ma, ma, c[2] * (NS_SCALE_B / (NS_SCALE_A * NS_SCALE_A)));
+            p.old = ma; p.old_matrix = R * tp; p.old_pitch = tp;
+            p.alpha = c[1] * (NS_SCALE_B / NS_SCALE_A);
+            p.diagonal = n > 1 ? c[0] * NS_SCALE_B : 0.0f;
+            if ((e = product<NS_POLY, float>(o, p, OF_B, st)) != hipSuccess || n == 1) break;
+            if (i > 0) {                                   // R <- P R
+                _Float16* const r = place(o->off_square[3 + (i & 1)]);
+                if ((e = product<NS_GRAM, float>(o, square(r, to, left_of_x, 1.0f / NS_SCALE_B), OF_B, st)) != hipSuccess) break;
+                left_of_x = r;
+            } else {
+                left_of_x = to;
+            }
+            if (i + 1 == n) break;
+            _Float16* const t = place(o->off_square[2]);   // A <- P (P A)
+            if ((e = product<NS_GRAM, float>(o, square(t, to, ma, 1.0f / NS_SCALE_B), OF_B, st)) != hipSuccess) break;
+            e = product<NS_GRAM, float>(o, square(ma, to, t, 1.0f / NS_SCALE_B), OF_B, st);
+        }
+        if (e != hipSuccess) break;
+        ProductArgs q{};
+        q.p = left_of_x; q.p_matrix = R * tp; q.p_pitch = tp;
+        q.q = xt[now]; q.q_matrix = C * tp; q.q_pitch = tp;
         q.kblocks = (o->rows + NS_KBLOCK - 1) / NS_KBLOCK;
-        q.old = xt[s & 1]; q.old_matrix = C * tp; q.old_pitch = tp;
+        if (n == 1) {
+            q.old = xt[now]; q.old_matrix = C * tp; q.old_pitch = tp;
+            q.alpha = o->coefficients[s][0];
+        }
         q.out = x; q.out_matrix = R * xp; q.out_pitch = xp;
-        q.out_t = xt[(s + 1) & 1]; q.out_t_matrix = C * tp; q.out_t_pitch = tp;
-        q.alpha = c[0];
+        q.out_t = xt[now ^ 1]; q.out_t_matrix = C * tp; q.out_t_pitch = tp;
         q.beta = 1.0f / NS_SCALE_B;
-        if (s + 1 < o->steps) {
+        if (s + n < o->steps) {
             e = product<NS_APPLY, float>(o, q, OF_X, st);
             continue;
         }
-        q.alpha = c[0] / NS_SCALE_X;
-        q.beta = 1.0f / (NS_SCALE_B * NS_SCALE_X);
+        q.alpha /= NS_SCALE_X;
+        q.beta /= NS_SCALE_X;
         q.result = result;
         e = o->out_dtype == RB_F32 ? product<NS_LAST, float>(o, q, OF_X, st) : product<NS_LAST, Bf16>(o, q, OF_X, st);
     }
