@@ -5,8 +5,8 @@
 // workgroups are joined by the same rule, and lse = m + log s, entropy = log s - t / s.
 // Alternatives.  A wavefront keeps its best 64 elements so far as one 64-bit key per lane, sorted: the logit in an order-preserving 32-bit
 // form above the inverted index, so that equal logits order by index and no two keys are equal.  A lane whose tile holds nothing above the
-// smallest key that still counts (which the running maximum tells at no cost) goes on; the vectors that do are put into LDS, a lane takes
-// one element of them each, what passes is queued, and a full queue is sorted and merged into the list.
+// smallest key that still counts (which the running maximum tells at no cost) goes on; the others put their tile into LDS, half a wavefront
+// looks at one of them at a time, what passes is queued, and a full queue is sorted and merged into the list.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -217,16 +217,17 @@ __device__ __forceinline__ K sc_bitonic(K key, bool down)
     return key;
 }
 
-// The wavefront's keys, largest in lane 0.
+// The keys of the wavefront's first `count` lanes, largest in lane 0; the others' are 0.
 template <typename K>
-__device__ __forceinline__ K sc_sort(K key)
+__device__ __forceinline__ K sc_sort(K key, int count)
 {
     key = sc_bitonic<2>(key, (threadIdx.x & 2) == 0);
     key = sc_bitonic<4>(key, (threadIdx.x & 4) == 0);
     key = sc_bitonic<8>(key, (threadIdx.x & 8) == 0);
     key = sc_bitonic<16>(key, (threadIdx.x & 16) == 0);
-    key = sc_bitonic<32>(key, (threadIdx.x & 32) == 0);
-    return sc_bitonic<64>(key, true);
+    if (count > 16) key = sc_bitonic<32>(key, (threadIdx.x & 32) == 0);
+    if (count > 32) key = sc_bitonic<64>(key, true);
+    return key;
 }
 
 // The 64 largest of two sorted lists, sorted.
@@ -238,28 +239,48 @@ __device__ __forceinline__ uint64_t sc_merge(uint64_t a, uint64_t b)
 
 __device__ __forceinline__ void sc_lds_wait() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 
-// A wavefront's list and the queue in LDS before it.
+// A wavefront's list and the queue in LDS before it.  WAVES that share a row tell each other what they hold: the value that `share` of a
+// wavefront's elements reach.  WAVES * share >= top elements reach the least of these, and what is below that is wanted by none.
+template <int WAVES>
 struct Best {
     uint64_t list;        // lane i: the (i + 1)-th largest key so far, 0: none
     uint64_t least;       // the key of the last place that counts: what is not above it is not wanted
     uint64_t* queue;      // 2 * SC_WAVE keys
-    uint32_t* shared;     // sc_order of a value that the row's result has `top` elements at or above, from any wavefront (null: none)
-    int queued, top;
+    uint32_t* told;       // sc_order of the values, one per wavefront, 0: nothing told yet
+    int queued, top, share;
 
-    __device__ __forceinline__ Best(uint64_t* q, uint32_t* sh, int top_) : list(0), least(0), queue(q), shared(sh), queued(0), top(top_) {}
+    __device__ __forceinline__ Best(uint64_t* q, uint32_t* told_, int top_)
+        : list(0), least(0), queue(q), told(told_), queued(0), top(top_), share((top_ + WAVES - 1) / WAVES) {}
 
+    __device__ __forceinline__ void tell(uint32_t order)
+    {
+        if (WAVES > 1 && (threadIdx.x & (SC_WAVE - 1)) == 0) __hip_atomic_store(told + threadIdx.x / SC_WAVE, order, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+    }
+    // sc_order of the least value that is still wanted: above the list's last (an element that equals it comes with a higher index), and what all reach
+    __device__ __forceinline__ uint32_t wanted() const
+    {
+        const uint32_t own = least == 0 ? 0 : (uint32_t)(least >> 32) + 1;
+        if (WAVES == 1) return own;
+        uint32_t all = __hip_atomic_load(told + threadIdx.x % WAVES, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+        if (WAVES > 1) all = min(all, sc_xor<1>(all));
+        if (WAVES > 2) all = min(all, sc_xor<2>(all));
+        if (WAVES > 4) all = min(all, sc_xor<4>(all));
+        if (WAVES > 8) all = min(all, sc_xor<8>(all));
+        return max(own, (uint32_t)__builtin_amdgcn_readfirstlane((int)all));
+    }
     __device__ __forceinline__ void merge_first()
     {
-        const int lane = threadIdx.x & (SC_WAVE - 1);
+        const int lane = threadIdx.x & (SC_WAVE - 1), now = min(queued, SC_WAVE);
         sc_lds_wait();
-        const uint64_t key = lane < queued ? queue[lane] : 0;
+        uint64_t key = lane < queued ? queue[lane] : 0;
         const uint64_t rest = SC_WAVE + lane < queued ? queue[SC_WAVE + lane] : 0;
         sc_lds_wait();
         queue[lane] = rest;
         queued = max(queued - SC_WAVE, 0);
-        list = sc_merge(list, sc_sort(key));
+        key = sc_sort(key, now);
+        list = sc_lane(list, 0) == 0 ? key : sc_merge(list, key);
         least = sc_lane(list, top - 1);
-        if (shared != nullptr && lane == 0) atomicMax(shared, (uint32_t)(least >> 32));
+        if (WAVES > 1) tell((uint32_t)(sc_lane(list, share - 1) >> 32));
     }
     __device__ __forceinline__ void push(uint64_t key, bool wanted)
     {
@@ -277,22 +298,24 @@ struct Best {
 
 // ---- one row's share of a wavefront ------------------------------------------
 
-constexpr int SC_STAGED = 64;        // vectors of a tile that hold something wanted; of a tile with more the lanes are gone through one by one
+constexpr int SC_STAGED = 16;        // lanes whose elements are in LDS at a time
 
+template <typename T>
 struct Staged {
-    sc_vec vectors[SC_STAGED];
-    int32_t numbers[SC_STAGED];
+    T elements[SC_STAGED][SC_LANE_ELEMS];
+    int32_t lanes[SC_STAGED];
 };
 
 // Tiles part, part + parts, ... of the row; the elements at its unaligned ends fall to part 0.
-template <typename T, bool TOP>
-__device__ __forceinline__ void sc_scan(const T* row, int vocab, int part, int parts, Stats& stats, Best& best, Staged* staged)
+template <typename T, bool TOP, int WAVES>
+__device__ __forceinline__ void sc_scan(const T* row, int vocab, int part, int parts, Stats& stats, Best<WAVES>& best, Staged<T>* staged)
 {
     constexpr int N = Logit<T>::N, U = SC_LANE_ELEMS / N;
     const int lane = threadIdx.x & (SC_WAVE - 1);
     const RowSpan<T> span(row, vocab);
     const int tiles = (span.vectors + SC_WAVE * U - 1) / (SC_WAVE * U);
     bool first = true;
+    if (TOP && WAVES > 1 && part >= tiles) __syncthreads();        // a wavefront without a tile tells nothing, and is met all the same
     for (int tile = part; tile < tiles; tile += parts) {
         const int v0 = tile * (SC_WAVE * U) + lane;
         sc_vec v[U];
@@ -307,63 +330,46 @@ __device__ __forceinline__ void sc_scan(const T* row, int vocab, int part, int p
                 if (v0 + u * SC_WAVE < span.vectors) v[u] = span.body[v0 + u * SC_WAVE];
             }
         }
-        float z[SC_LANE_ELEMS], vector_max[U], tile_max = sc_neg_inf();
+        float z[SC_LANE_ELEMS];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            Logit<T>::unpack(v[u], z + u * N);
-            vector_max[u] = sc_max<N>(z + u * N);
-            tile_max = fmaxf(tile_max, vector_max[u]);
-        }
+        for (int u = 0; u < U; ++u) Logit<T>::unpack(v[u], z + u * N);
+        const float tile_max = sc_max<SC_LANE_ELEMS>(z);
         sc_absorb<SC_LANE_ELEMS>(stats, z, tile_max);
         if (TOP) {
-            // An element that only equals the list's last one has a higher index than that; one below what another wavefront's list ends with is not wanted.
             const bool any = v0 < span.vectors;
-            uint32_t least = best.least == 0 ? 0 : (uint32_t)(best.least >> 32) + 1;
-            if (best.shared != nullptr) least = max(least, __hip_atomic_load(best.shared, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP));
+            const bool meet = WAVES > 1 && first;                  // (all wavefronts meet once, behind their first tile)
+            uint32_t least = meet ? 0 : best.wanted();
             const uint32_t highest = any ? sc_order(tile_max) : 0;
             uint64_t who = __ballot(any && highest >= least);
             if (who != 0) {
                 if (first || __popcll(who) > 16) {
                     // At least `top` elements reach the top-th largest of the lanes' maxima (fewer lanes than that: all are looked at).
-                    least = max(least, (uint32_t)__builtin_amdgcn_readlane((int)sc_sort(highest), best.top - 1));
+                    const uint32_t sorted = sc_sort(highest, SC_WAVE);
+                    least = max(least, (uint32_t)__builtin_amdgcn_readlane((int)sorted, best.top - 1));
+                    if (meet) {
+                        best.tell((uint32_t)__builtin_amdgcn_readlane((int)sorted, best.share - 1));
+                        __syncthreads();
+                        least = max(least, best.wanted());
+                    }
                     who = __ballot(any && highest >= least);
                 }
-                int count = 0;
+                while (who != 0) {
+                    // the first lanes of them put their elements into LDS; then half a wavefront looks at one lane's
+                    const int rank = __builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0));
+                    const bool mine = ((who >> lane) & 1) != 0 && rank < SC_STAGED;
+                    if (mine) {
 #pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    const bool hit = v0 + u * SC_WAVE < span.vectors && sc_order(vector_max[u]) >= least;
-                    const uint64_t hits = __ballot(hit);
-                    if (hits != 0) {
-                        const int at = count + __builtin_amdgcn_mbcnt_hi((uint32_t)(hits >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)hits, 0));
-                        if (hit && at < SC_STAGED) {
-                            staged->vectors[at] = v[u];
-                            staged->numbers[at] = v0 + u * SC_WAVE;
-                        }
-                        count += __popcll(hits);
+                        for (int u = 0; u < U; ++u) *reinterpret_cast<sc_vec*>(&staged->elements[rank][u * N]) = v[u];
+                        staged->lanes[rank] = lane;
                     }
-                }
-                if (count <= SC_STAGED) {
+                    const int count = min(__popcll(who), SC_STAGED);
+                    who &= ~__ballot(mine);
                     sc_lds_wait();
-                    for (int at = lane / N; at - lane / N < count; at += SC_WAVE / N) {
-                        const bool there = at < count;
-                        const int from = there ? at : 0;
-                        const float x = Logit<T>::one(reinterpret_cast<const T*>(&staged->vectors[from]) + lane % N);
-                        best.push(sc_key(x, (uint32_t)(span.head + staged->numbers[from] * N + lane % N)), there && sc_order(x) >= least);
-                    }
-                } else {
-                    while (who != 0) {
-                        // lanes 0..31 read the elements of one of them, lanes 32..63 those of the next
-                        const int a = __builtin_ctzll(who);
-                        who &= who - 1;
-                        const int b = who ? __builtin_ctzll(who) : -1;
-                        who &= who - 1;
-                        const int of = lane < SC_LANE_ELEMS ? a : b, j = lane & (SC_LANE_ELEMS - 1);
-                        const int vector = tile * (SC_WAVE * U) + (j / N) * SC_WAVE + of;
-                        const bool there = of >= 0 && vector < span.vectors;
-                        const int index = span.head + vector * N + j % N;
-                        float x = 0.0f;
-                        if (there) x = Logit<T>::one(row + index);
-                        best.push(sc_key(x, (uint32_t)index), there && sc_order(x) >= least);
+                    for (int at = lane / SC_LANE_ELEMS; at - lane / SC_LANE_ELEMS < count; at += 2) {
+                        const int from = min(at, count - 1), e = lane & (SC_LANE_ELEMS - 1);
+                        const int vector = tile * (SC_WAVE * U) + e / N * SC_WAVE + staged->lanes[from];
+                        const float x = Logit<T>::one(&staged->elements[from][e]);
+                        best.push(sc_key(x, (uint32_t)(span.head + vector * N + e % N)), at < count && vector < span.vectors && sc_order(x) >= least);
                     }
                 }
                 if (first) best.flush();
@@ -440,32 +446,32 @@ __global__ __launch_bounds__(WAVES == 1 ? SC_TPB : WAVES * SC_WAVE) void rb_scor
 {
     constexpr int LISTS = WAVES == 1 ? SC_NWAVE : WAVES;
     __shared__ uint64_t queues[LISTS][TOP ? 2 * SC_WAVE : 1];
-    __shared__ Staged staged[TOP ? LISTS : 1];
+    __shared__ __align__(16) Staged<T> staged[TOP ? LISTS : 1];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / SC_WAVE), lane = threadIdx.x & (SC_WAVE - 1);
     Stats st{sc_neg_inf(), 0.0f, 0.0f};
     if (WAVES == 1) {
         const int64_t row = (int64_t)blockIdx.x * SC_NWAVE + wave;
         if (row >= a.rows) return;
         const T* z = static_cast<const T*>(a.logits) + row * a.stride;
-        Best best(queues[wave], nullptr, a.top);
+        Best<1> best(queues[wave], nullptr, a.top);
         const Given given = sc_given(a, z, row);
-        sc_scan<T, TOP>(z, a.vocab, 0, 1, st, best, &staged[TOP ? wave : 0]);
+        sc_scan<T, TOP, 1>(z, a.vocab, 0, 1, st, best, &staged[TOP ? wave : 0]);
         sc_finish(a, row, sc_join_wave(st), best.list, given);
         return;
     }
     __shared__ Stats stats[LISTS];
-    __shared__ uint32_t shared;
+    __shared__ uint32_t told[WAVES];
     const int64_t row = blockIdx.x / (uint32_t)a.splits;
     const int split = blockIdx.x % (uint32_t)a.splits;
     const T* z = static_cast<const T*>(a.logits) + row * a.stride;
     if (TOP) {
-        if (threadIdx.x == 0) shared = 0;
+        if (threadIdx.x < WAVES) told[threadIdx.x] = 0;
         __syncthreads();
     }
-    Best best(queues[wave], TOP ? &shared : nullptr, a.top);
+    Best<WAVES> best(queues[wave], told, a.top);
     Given given{};
     if (wave == 0) given = sc_given(a, z, row);
-    sc_scan<T, TOP>(z, a.vocab, split * WAVES + wave, a.splits * WAVES, st, best, &staged[TOP ? wave : 0]);
+    sc_scan<T, TOP, WAVES>(z, a.vocab, split * WAVES + wave, a.splits * WAVES, st, best, &staged[TOP ? wave : 0]);
     st = sc_join_wave(st);
     if (lane == 0) stats[wave] = st;
     uint64_t list = best.list;

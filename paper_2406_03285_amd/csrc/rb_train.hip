@@ -30,6 +30,7 @@ hipError_t score(const ScoreArgs& a, int waves, hipStream_t st)
 {
     if (waves == 1) return launch(rb_score_kernel<T, TOP, 1>, dim3((unsigned)((a.rows + SC_NWAVE - 1) / SC_NWAVE)), SC_TPB, 0, st, a);
     const dim3 grid((unsigned)a.rows * (unsigned)a.splits);
+    if (waves == 2) return launch(rb_score_kernel<T, TOP, 2>, grid, 2 * SC_WAVE, 0, st, a);
     if (waves == SC_NWAVE) return launch(rb_score_kernel<T, TOP, SC_NWAVE>, grid, SC_TPB, 0, st, a);
     return launch(rb_score_kernel<T, TOP, SC_MANY_WAVES>, grid, SC_MANY_WAVES * SC_WAVE, 0, st, a);
 }
@@ -113,9 +114,10 @@ int rb_scorer_score(rb_scorer* s, const void* logits, int64_t rows, int64_t row_
     a.vocab = s->vocab;
     a.given = s->given;
     a.top = s->top;
-    // One tile is a wavefront's; rows that fill the chip get a workgroup of 4 wavefronts each.  Fewer rows get workgroups of 16, and what has
-    // more than a few tiles for each of these is shared by several workgroups.
-    const int waves = tiles == 1 || (tiles <= 8 && rows >= 4096) ? 1 : rows >= 512 || tiles <= SC_NWAVE ? SC_NWAVE : SC_MANY_WAVES;
+    // Wavefronts per row: one tile is a wavefront's.  Rows that fill the chip get few, since each has a list of its own to sort and join (2048
+    // rows of 50001 with 16 alternatives: 63 us with one, 51 with two, 58 with four), and four when they are long.  Fewer rows get 16, and
+    // what has more than a few tiles for each of these is shared by several workgroups.
+    const int waves = tiles == 1 || (tiles <= 8 && rows >= 4096) ? 1 : tiles <= 32 && rows >= 2048 ? 2 : rows >= 512 || tiles <= SC_NWAVE ? SC_NWAVE : SC_MANY_WAVES;
     a.splits = waves == SC_MANY_WAVES ? (int32_t)std::max<int64_t>(1, std::min<int64_t>({tiles / (2 * SC_MANY_WAVES), 256 / rows, SC_MAX_SPLITS})) : 1;
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     hipError_t e;
