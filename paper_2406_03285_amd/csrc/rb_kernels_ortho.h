@@ -250,11 +250,16 @@ __device__ __forceinline__ void ns_result(const ResultArgs& a, OUT* at, int64_t 
 
 enum { NS_GRAM = 0, NS_POLY = 1, NS_APPLY = 2, NS_LAST = 3 };
 
+// What the first instructions of a product need: as arguments in front of the structure it is in registers when a wavefront starts.
+struct Operands {
+    const _Float16 *p, *q;                  // P: tiles_i tiles of rows, Q: tiles_j
+    int32_t p_lines, q_lines;               // lines of 128 bytes between rows
+    uint32_t p_matrix, q_matrix;            // lines between matrices
+    int32_t kblocks;                        // of the summed index
+};
+
 struct ProductArgs {
-    const _Float16 *p, *q;                  // P: tiles_i * NS_TILE rows, Q: tiles_j * NS_TILE rows, kblocks blocks each
-    int64_t p_matrix, q_matrix;             // halves between matrices
-    int64_t p_pitch, q_pitch;               // halves between rows
-    int32_t kblocks, tiles_i, tiles_j;
+    int32_t tiles_i, tiles_j;
     int32_t tiles, slices;                  // of one matrix; of the summed index
     float* sums;                            // of the slices, if there are several
     const _Float16* old;                    // POLY: A; APPLY, LAST: X^T, of which a * X is added (null: nothing is)
@@ -286,12 +291,21 @@ __device__ __forceinline__ int ns_rank(int id, int count)
     return die * whole + min(die, more) + (id >> 3);
 }
 constexpr int NS_GROUP = 8;
+__device__ __forceinline__ void ns_in_group(int t, int height, int& row, int& col)          // (divisions take long where little else is to be done)
+{
+    if (height == NS_GROUP) {
+        row = t % NS_GROUP;
+        col = t / NS_GROUP;
+    } else {
+        col = (int)((uint32_t)t / (uint32_t)height);
+        row = t - col * height;
+    }
+}
 __device__ __forceinline__ void ns_tile_of(int t, int rows, int cols, int& ti, int& tj)
 {
-    const int g = t / (NS_GROUP * cols), first = g * NS_GROUP, height = min(NS_GROUP, rows - first);
-    t -= g * NS_GROUP * cols;
-    ti = first + t % height;
-    tj = t / height;
+    const int g = rows <= NS_GROUP ? 0 : (int)((uint32_t)t / (uint32_t)(NS_GROUP * cols)), first = g * NS_GROUP;
+    ns_in_group(t - first * cols, min(NS_GROUP, rows - first), ti, tj);
+    ti += first;
 }
 __device__ __forceinline__ void ns_tile_above(int t, int rows, int& ti, int& tj)          // on and above the diagonal only
 {
@@ -303,15 +317,26 @@ __device__ __forceinline__ void ns_tile_above(int t, int rows, int& ti, int& tj)
                 while (t > col) t -= ++col;
                 ti = first + t;
             } else {
-                t -= corner;
-                ti = first + t % height;
-                col = height + t / height;
+                ns_in_group(t - corner, height, ti, col);
+                ti += first;
+                col += height;
             }
             tj = first + col;
             return;
         }
         t -= count;
     }
+}
+// Matrix, tile and slice of the `rank`-th workgroup.
+__device__ __forceinline__ void ns_share(int rank, int tiles, int slices, int& tile, int& slice, int& k)
+{
+    tile = rank;
+    slice = k = 0;
+    if (slices > 1) {
+        tile = (int)((uint32_t)rank / (uint32_t)slices);
+        slice = rank - tile * slices;
+    }
+    if (tile >= tiles) k = (int)((uint32_t)tile / (uint32_t)tiles);
 }
 
 // ---- a block of 32 x 32 of a result -------------------------------------------
@@ -419,40 +444,46 @@ __device__ __forceinline__ float4* ns_sums(const ProductArgs& a, int64_t tile, i
 // C = P Q^T of one tile of BM x BM; a wavefront has WM x WN of it in blocks of 32 x 32.  A block of 32 of the summed index is 2 BM lines of 128
 // bytes; STAGES of them are in LDS or on their way there.  Where the tiles are few the summed index is cut into slices, a workgroup each.
 template <int KIND, typename OUT, int BM, int WM, int WN, int STAGES, int WAVES_PER_SIMD>
-__global__ __launch_bounds__((BM / WM) * (BM / WN) * 64, WAVES_PER_SIMD) void rb_ortho_product_kernel(const ProductArgs a)
+__global__ __launch_bounds__((BM / WM) * (BM / WN) * 64, WAVES_PER_SIMD) void rb_ortho_product_kernel(
+    const _Float16* of_p, const _Float16* of_q, int32_t p_lines, int32_t q_lines, uint32_t p_matrix, uint32_t q_matrix, int32_t all_blocks,
+    int32_t tiles_i, int32_t tiles_j, int32_t tiles, int32_t slices, const ProductArgs a)
 {
     constexpr int BN = BM, WAVES = (BM / WM) * (BN / WN), MI = WM / 32, MJ = WN / 32;
     constexpr int STAGE = (BM + BN) * 128, PIECES = (BM + BN) / 8, PER_WAVE = PIECES / WAVES;
     static_assert(PIECES % (4 * WAVES) == 0, "pairs of pieces of 8 lines of either operand per wavefront");
     extern __shared__ __align__(16) char lds[];
-    const int rank = ns_rank(blockIdx.x, gridDim.x);
-    const int slice = rank % a.slices, tile = rank / a.slices;      // tile: counted over all matrices
-    const int64_t k = tile / a.tiles;
-    int ti, tj;
+    int tile, slice, k, ti, tj;                                    // tile: counted over all matrices
+    ns_share(ns_rank(blockIdx.x, gridDim.x), tiles, slices, tile, slice, k);
     if (KIND == NS_GRAM || KIND == NS_POLY)
-        ns_tile_above(tile - (int)k * a.tiles, a.tiles_i, ti, tj);
+        ns_tile_above(tile - k * tiles, tiles_i, ti, tj);
     else
-        ns_tile_of(tile - (int)k * a.tiles, a.tiles_i, a.tiles_j, ti, tj);
+        ns_tile_of(tile - k * tiles, tiles_i, tiles_j, ti, tj);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x & 63;
-    const int kbegin = (int)((int64_t)a.kblocks * slice / a.slices), kblocks = (int)((int64_t)a.kblocks * (slice + 1) / a.slices) - kbegin;
+    int kbegin = 0, kblocks = all_blocks;
+    if (slices > 1) {
+        kbegin = (int)((uint32_t)(all_blocks * slice) / (uint32_t)slices);
+        kblocks = (int)((uint32_t)(all_blocks * (slice + 1)) / (uint32_t)slices) - kbegin;
+    }
     const int wi = (wave / (BN / WN)) * WM, wj = (wave % (BN / WN)) * WN;
-    const char* p = reinterpret_cast<const char*>(a.p + k * a.p_matrix + (int64_t)ti * BM * a.p_pitch) + (int64_t)kbegin * 128;
-    const char* q = reinterpret_cast<const char*>(a.q + k * a.q_matrix + (int64_t)tj * BN * a.q_pitch) + (int64_t)kbegin * 128;
 
     // A piece is 8 lines; the 16-byte part c of line r stands at place c ^ (r / 2 % 8) of its line in LDS, so that 16 lanes that read one part of
-    // 16 lines read all 64 banks once.  (Of an odd piece r / 2 is 4 more.)
-    const uint32_t place = ((lane & 7) ^ (lane >> 4)) * 16;
-    const uint32_t p_lane = (uint32_t)((lane >> 3) * a.p_pitch * 2), q_lane = (uint32_t)((lane >> 3) * a.q_pitch * 2);
+    // 16 lines read all 64 banks once.  (Of an odd piece r / 2 is 4 more.)  A wavefront fetches neighbouring pieces of both operands.
+    constexpr int HALF = PER_WAVE / 2;
+    const char* p = reinterpret_cast<const char*>(of_p) + ((int64_t)p_matrix * k + (int64_t)(ti * BM + wave * HALF * 8) * p_lines + kbegin) * 128;
+    const char* q = reinterpret_cast<const char*>(of_q) + ((int64_t)q_matrix * k + (int64_t)(tj * BN + wave * HALF * 8) * q_lines + kbegin) * 128;
+    const uint32_t place = ((lane & 7) ^ (lane >> 4)) * 16, p_lane = (lane >> 3) * p_lines * 128, q_lane = (lane >> 3) * q_lines * 128;
     auto fetch = [&](int block, int stage) {
-        char* to = lds + stage * STAGE + wave * (PER_WAVE / 2 * 1024);
-        const char* from_p = p + wave * (PER_WAVE / 2 * 16) * a.p_pitch + (int64_t)block * 128;
-        const char* from_q = q + wave * (PER_WAVE / 2 * 16) * a.q_pitch + (int64_t)block * 128;
+        char* to = lds + stage * STAGE + wave * (HALF * 1024);
 #pragma unroll
-        for (int i = 0; i < PER_WAVE / 2; ++i) {
-            ns_load_to_lds(from_p + i * 16 * a.p_pitch + p_lane + (place ^ (i & 1) * 64), to + i * 1024);
-            ns_load_to_lds(from_q + i * 16 * a.q_pitch + q_lane + (place ^ (i & 1) * 64), to + BM * 128 + i * 1024);
+        for (int i = 0; i < HALF; ++i) {
+            ns_load_to_lds(p + (int64_t)(i * 8 * p_lines + block) * 128 + (p_lane + (place ^ (i & 1) * 64)), to + i * 1024);
+            ns_load_to_lds(q + (int64_t)(i * 8 * q_lines + block) * 128 + (q_lane + (place ^ (i & 1) * 64)), to + BM * 128 + i * 1024);
         }
     };
+    // what is added to a single block is on its way before anything else (the wait for the first stage is one for it too)
+    constexpr bool EARLY = KIND != NS_GRAM && MI * MJ == 1;
+    ns_vec early[4];
+    if (EARLY) ns_fetch_old(a, k, ti * BM + wi, tj * BN + wj, early);
 
     // The fragments of 16 of the summed index: a lane has 8 of them of row lane % 32 of every block, hi and lo.
     struct Fragments { half8 ph[MI], pl[MI], qh[MJ], ql[MJ]; };
@@ -514,7 +545,7 @@ __global__ __launch_bounds__((BM / WM) * (BM / WN) * 64, WAVES_PER_SIMD) void rb
         stage = next;
     }
 
-    if (a.slices > 1) {                        // a slice's sums: rb_ortho_join_kernel adds them up
+    if (slices > 1) {                          // a slice's sums: rb_ortho_join_kernel adds them up
 #pragma unroll
         for (int i = 0; i < MI; ++i)
 #pragma unroll
@@ -533,7 +564,7 @@ __global__ __launch_bounds__((BM / WM) * (BM / WN) * 64, WAVES_PER_SIMD) void rb
     ns_vec old[AHEAD][MJ][4];
 #pragma unroll
     for (int i = 0; i < MI; ++i) {
-        if (KIND != NS_GRAM && (i == 0 || AHEAD == 1)) {
+        if (KIND != NS_GRAM && !EARLY && (i == 0 || AHEAD == 1)) {
 #pragma unroll
             for (int b = 0; b < AHEAD; ++b)
 #pragma unroll
@@ -541,7 +572,7 @@ __global__ __launch_bounds__((BM / WM) * (BM / WN) * 64, WAVES_PER_SIMD) void rb
         }
 #pragma unroll
         for (int j = 0; j < MJ; ++j)
-            ns_finish<KIND, OUT>(a, k, ti * BM + wi + i * 32, tj * BN + wj + j * 32, acc[i][j], old[AHEAD == 1 ? 0 : i][j], mirror, mine);
+            ns_finish<KIND, OUT>(a, k, ti * BM + wi + i * 32, tj * BN + wj + j * 32, acc[i][j], EARLY ? early : old[AHEAD == 1 ? 0 : i][j], mirror, mine);
     }
 }
 

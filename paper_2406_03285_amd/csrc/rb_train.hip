@@ -190,17 +190,18 @@ namespace {
 enum { OF_A = 0, OF_B = 1, OF_X = 2 };
 
 template <int KIND, typename OUT, int BM, int WM, int WN, int WAVES_PER_SIMD>
-hipError_t product_of(const ProductArgs& a, unsigned tiles, hipStream_t st)
+hipError_t product_of(const Operands& o, const ProductArgs& a, unsigned tiles, hipStream_t st)
 {
     constexpr int STAGES = BM == 64 ? 3 : 2;
     const hipError_t e = launch(rb_ortho_product_kernel<KIND, OUT, BM, WM, WN, STAGES, WAVES_PER_SIMD>, dim3(tiles * (unsigned)a.slices),
-                                BM / WM * (BM / WN) * 64, (size_t)STAGES * 2 * BM * 128, st, a);
+                                BM / WM * (BM / WN) * 64, (size_t)STAGES * 2 * BM * 128, st, o.p, o.q, o.p_lines, o.q_lines, o.p_matrix, o.q_matrix,
+                                o.kblocks, a.tiles_i, a.tiles_j, a.tiles, a.slices, a);
     if (e != hipSuccess || a.slices == 1) return e;
     return launch(rb_ortho_join_kernel<KIND, OUT, BM>, dim3(tiles * (BM / 32) * (BM / 32) / (NS_TPB / 64)), NS_TPB, 0, st, a);
 }
 
 template <int KIND, typename OUT>
-hipError_t product(const rb_ortho* o, ProductArgs a, int which, hipStream_t st)
+hipError_t product(const rb_ortho* o, const Operands& of, ProductArgs a, int which, hipStream_t st)
 {
     const int tile = o->tile[which];
     a.tiles_i = (o->rows + tile - 1) / tile;
@@ -210,10 +211,10 @@ hipError_t product(const rb_ortho* o, ProductArgs a, int which, hipStream_t st)
     a.sums = reinterpret_cast<float*>(o->ws + o->off_sums);
     const unsigned tiles = (unsigned)(a.tiles * o->matrices);
     switch (tile) {
-    case 256: return product_of<KIND, OUT, 256, 128, 64, 2>(a, tiles, st);
-    case 192: return product_of<KIND, OUT, 192, 96, 96, 1>(a, tiles, st);
-    case 128: return product_of<KIND, OUT, 128, 64, 32, 4>(a, tiles, st);
-    default: return product_of<KIND, OUT, 64, 32, 32, 3>(a, tiles, st);
+    case 256: return product_of<KIND, OUT, 256, 128, 64, 2>(of, a, tiles, st);
+    case 192: return product_of<KIND, OUT, 192, 96, 96, 1>(of, a, tiles, st);
+    case 128: return product_of<KIND, OUT, 128, 64, 32, 4>(of, a, tiles, st);
+    default: return product_of<KIND, OUT, 64, 32, 32, 3>(of, a, tiles, st);
     }
 }
 
@@ -344,11 +345,13 @@ hipError_t orthogonalize(const rb_ortho* o, const UpdateArgs& u, const ResultArg
     _Float16 *const x = place(o->off_x), *const xt[2] = {place(o->off_xt[0]), place(o->off_xt[1])};
     const KeptArgs kept{x, xt[0], R * xp, C * tp, xp, tp, (int32_t)R, (int32_t)C};
     hipError_t e = o->dtype == RB_F32 ? first_pass<float>(o, u, kept, st) : first_pass<Bf16>(o, u, kept, st);
-    // to <- beta * p q^T of two squares that commute (symmetric), + alpha * old + diagonal
-    auto square = [&](_Float16* to, const _Float16* p, const _Float16* q, float beta) {
+    const int by_rows = (o->rows + NS_KBLOCK - 1) / NS_KBLOCK, by_cols = (o->cols + NS_KBLOCK - 1) / NS_KBLOCK;
+    const int32_t xl = (int32_t)(xp / NS_KHALVES), tl = (int32_t)(tp / NS_KHALVES);
+    const uint32_t x_matrix = (uint32_t)(R * xl), t_matrix = (uint32_t)(C * tl), square_matrix = (uint32_t)(R * tl);
+    // to <- beta * p q^T of two squares that commute: symmetric
+    auto squares = [&](const _Float16* p, const _Float16* q) { return Operands{p, q, tl, tl, square_matrix, square_matrix, by_rows}; };
+    auto to_square = [&](_Float16* to, float beta) {
         ProductArgs a{};
-        a.p = p; a.q = q; a.p_matrix = a.q_matrix = R * tp; a.p_pitch = a.q_pitch = tp;
-        a.kblocks = (o->rows + NS_KBLOCK - 1) / NS_KBLOCK;
         a.out = to; a.out_t = to; a.out_matrix = a.out_t_matrix = R * tp; a.out_pitch = a.out_t_pitch = tp;
         a.beta = beta;
         return a;
@@ -357,37 +360,33 @@ hipError_t orthogonalize(const rb_ortho* o, const UpdateArgs& u, const ResultArg
     int blocks = (o->steps + o->block - 1) / o->block;
     for (int s = 0, n = 0, now = 0; s < o->steps && e == hipSuccess; s += n, now ^= 1, --blocks) {
         n = (o->steps - s + blocks - 1) / blocks;          // steps of this block: as even as it goes, longer ones first
-        ProductArgs g = square(ma, nullptr, nullptr, NS_SCALE_A / (NS_SCALE_X * NS_SCALE_X));                       // A = X X^T
-        g.p = x; g.q = x; g.p_matrix = g.q_matrix = R * xp; g.p_pitch = g.q_pitch = xp;
-        g.kblocks = (o->cols + NS_KBLOCK - 1) / NS_KBLOCK;
-        if ((e = product<NS_GRAM, float>(o, g, OF_A, st)) != hipSuccess) break;
+        // A = X X^T
+        e = product<NS_GRAM, float>(o, Operands{x, x, xl, xl, x_matrix, x_matrix, by_cols}, to_square(ma, NS_SCALE_A / (NS_SCALE_X * NS_SCALE_X)), OF_A, st);
         // B = b A + c A A and then a X + B X; or, of a block, P = a I + B, and R X
         const _Float16* left_of_x = mb;
         for (int i = 0; i < n && e == hipSuccess; ++i) {
             const float* c = o->coefficients[s + i];
             _Float16* const to = n > 1 && i == 0 ? place(o->off_square[3]) : mb;
-            ProductArgs p = square(to, ma, ma, c[2] * (NS_SCALE_B / (NS_SCALE_A * NS_SCALE_A)));
+            ProductArgs p = to_square(to, c[2] * (NS_SCALE_B / (NS_SCALE_A * NS_SCALE_A)));
             p.old = ma; p.old_matrix = R * tp; p.old_pitch = tp;
             p.alpha = c[1] * (NS_SCALE_B / NS_SCALE_A);
             p.diagonal = n > 1 ? c[0] * NS_SCALE_B : 0.0f;
-            if ((e = product<NS_POLY, float>(o, p, OF_B, st)) != hipSuccess || n == 1) break;
+            if ((e = product<NS_POLY, float>(o, squares(ma, ma), p, OF_B, st)) != hipSuccess || n == 1) break;
             if (i > 0) {                                   // R <- P R
                 _Float16* const r = place(o->off_square[3 + (i & 1)]);
-                if ((e = product<NS_GRAM, float>(o, square(r, to, left_of_x, 1.0f / NS_SCALE_B), OF_B, st)) != hipSuccess) break;
+                if ((e = product<NS_GRAM, float>(o, squares(to, left_of_x), to_square(r, 1.0f / NS_SCALE_B), OF_B, st)) != hipSuccess) break;
                 left_of_x = r;
             } else {
                 left_of_x = to;
             }
             if (i + 1 == n) break;
             _Float16* const t = place(o->off_square[2]);   // A <- P (P A)
-            if ((e = product<NS_GRAM, float>(o, square(t, to, ma, 1.0f / NS_SCALE_B), OF_B, st)) != hipSuccess) break;
-            e = product<NS_GRAM, float>(o, square(ma, to, t, 1.0f / NS_SCALE_B), OF_B, st);
+            if ((e = product<NS_GRAM, float>(o, squares(to, ma), to_square(t, 1.0f / NS_SCALE_B), OF_B, st)) != hipSuccess) break;
+            e = product<NS_GRAM, float>(o, squares(to, t), to_square(ma, 1.0f / NS_SCALE_B), OF_B, st);
         }
         if (e != hipSuccess) break;
+        const Operands of{left_of_x, xt[now], tl, tl, square_matrix, t_matrix, by_rows};
         ProductArgs q{};
-        q.p = left_of_x; q.p_matrix = R * tp; q.p_pitch = tp;
-        q.q = xt[now]; q.q_matrix = C * tp; q.q_pitch = tp;
-        q.kblocks = (o->rows + NS_KBLOCK - 1) / NS_KBLOCK;
         if (n == 1) {
             q.old = xt[now]; q.old_matrix = C * tp; q.old_pitch = tp;
             q.alpha = o->coefficients[s][0];
@@ -396,13 +395,13 @@ hipError_t orthogonalize(const rb_ortho* o, const UpdateArgs& u, const ResultArg
         q.out_t = xt[now ^ 1]; q.out_t_matrix = C * tp; q.out_t_pitch = tp;
         q.beta = 1.0f / NS_SCALE_B;
         if (s + n < o->steps) {
-            e = product<NS_APPLY, float>(o, q, OF_X, st);
+            e = product<NS_APPLY, float>(o, of, q, OF_X, st);
             continue;
         }
         q.alpha /= NS_SCALE_X;
         q.beta /= NS_SCALE_X;
         q.result = result;
-        e = o->out_dtype == RB_F32 ? product<NS_LAST, float>(o, q, OF_X, st) : product<NS_LAST, Bf16>(o, q, OF_X, st);
+        e = o->out_dtype == RB_F32 ? product<NS_LAST, float>(o, of, q, OF_X, st) : product<NS_LAST, Bf16>(o, of, q, OF_X, st);
     }
     return e;
 }
