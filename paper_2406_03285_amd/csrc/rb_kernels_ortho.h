@@ -110,9 +110,9 @@ __global__ __launch_bounds__(NS_TPB) void rb_ortho_norm_kernel(const UpdateArgs 
     double sum = 0.0;
     // the matrix in pieces of AT_ONCE rows by V NS_TPB columns
     const int spans = (a.n + V * NS_TPB - 1) / (V * NS_TPB);
-    const int64_t items = (int64_t)((a.m + AT_ONCE - 1) / AT_ONCE) * spans;
-    for (int64_t it = blockIdx.x; it < items; it += gridDim.x) {
-        const int i0 = (int)(it / spans) * AT_ONCE, j = ((int)(it % spans) * NS_TPB + threadIdx.x) * V;
+    const int items = (a.m + AT_ONCE - 1) / AT_ONCE * spans;             // (at most 2^14 * 2^8)
+    for (int it = blockIdx.x; it < items; it += gridDim.x) {
+        const int i0 = (int)((uint32_t)it / (uint32_t)spans) * AT_ONCE, j = ((int)((uint32_t)it % (uint32_t)spans) * NS_TPB + threadIdx.x) * V;
         if (j >= a.n) continue;
         float u[AT_ONCE][V] = {};
 #pragma unroll

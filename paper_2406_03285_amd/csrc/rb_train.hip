@@ -22,6 +22,7 @@ struct rb_scorer {
 
 namespace {
 
+constexpr int64_t MAX_STRIDE = INT64_MAX / RB_MAX_ROWS / 8;      // of rows of logits: no offset passes 64 bits
 inline int64_t elem_bytes(int32_t dtype) { return dtype == RB_F32 ? 4 : 2; }
 inline size_t scorer_bytes(int32_t top) { return SC_SPLIT_GROUPS * (sizeof(uint32_t) + sc_partial_bytes(top)); }
 
@@ -91,7 +92,7 @@ int rb_scorer_bind(rb_scorer* s, void* workspace, void* hip_stream)
 int rb_scorer_score(rb_scorer* s, const void* logits, int64_t rows, int64_t row_stride, const int64_t* tokens, float* logp, float* lse,
                     float* entropy, float* top_logp, int64_t* top_ids, void* hip_stream)
 {
-    if (!s || rows < 0 || rows > RB_MAX_ROWS || row_stride < s->vocab) return RB_EINVAL;
+    if (!s || rows < 0 || rows > RB_MAX_ROWS || row_stride < s->vocab || row_stride > MAX_STRIDE) return RB_EINVAL;
     if (!logits || !aligned(logits, (size_t)elem_bytes(s->dtype))) return RB_EINVAL;
     if (s->given > 0 && (!tokens || !logp)) return RB_EINVAL;
     if (s->top > 0 && (!top_logp || !top_ids)) return RB_EINVAL;
@@ -132,7 +133,8 @@ int rb_scorer_grad(rb_scorer* s, const void* logits, int64_t rows, int64_t row_s
                    const float* entropy, const float* grad_logp, const float* grad_entropy, void* grad_logits, int64_t grad_stride,
                    void* hip_stream)
 {
-    if (!s || rows < 0 || rows > RB_MAX_ROWS || row_stride < s->vocab || grad_stride < s->vocab) return RB_EINVAL;
+    if (!s || rows < 0 || rows > RB_MAX_ROWS || row_stride < s->vocab || grad_stride < s->vocab || row_stride > MAX_STRIDE || grad_stride > MAX_STRIDE)
+        return RB_EINVAL;
     const int64_t size = elem_bytes(s->dtype);
     if (!logits || !grad_logits || !lse || !aligned(logits, (size_t)size) || !aligned(grad_logits, (size_t)size)) return RB_EINVAL;
     if (s->given > 0 && (!tokens || !grad_logp)) return RB_EINVAL;
@@ -187,15 +189,32 @@ struct rb_ortho {
 
 namespace {
 
+// A kernel that asks for more dynamic LDS than it gets by default: allowed once per kernel and device.
+template <auto kernel>
+hipError_t allow_lds(size_t bytes)
+{
+    static bool allowed[64] = {};
+    int dev = 0;
+    if (bytes <= 65536) return hipSuccess;
+    if (hipGetDevice(&dev) != hipSuccess) return hipErrorInvalidDevice;
+    if (dev >= 0 && dev < 64 && allowed[dev]) return hipSuccess;
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    if (e == hipSuccess && dev >= 0 && dev < 64) allowed[dev] = true;
+    return e;
+}
+
 enum { OF_A = 0, OF_B = 1, OF_X = 2 };
 
 template <int KIND, typename OUT, int BM, int WM, int WN, int WAVES_PER_SIMD>
 hipError_t product_of(const Operands& o, const ProductArgs& a, unsigned tiles, hipStream_t st)
 {
     constexpr int STAGES = BM == 64 ? 3 : 2;
-    const hipError_t e = launch(rb_ortho_product_kernel<KIND, OUT, BM, WM, WN, STAGES, WAVES_PER_SIMD>, dim3(tiles * (unsigned)a.slices),
-                                BM / WM * (BM / WN) * 64, (size_t)STAGES * 2 * BM * 128, st, o.p, o.q, o.p_lines, o.q_lines, o.p_matrix, o.q_matrix,
-                                o.kblocks, a.tiles_i, a.tiles_j, a.tiles, a.slices, a);
+    constexpr size_t LDS = (size_t)STAGES * 2 * BM * 128;
+    constexpr auto kernel = rb_ortho_product_kernel<KIND, OUT, BM, WM, WN, STAGES, WAVES_PER_SIMD>;
+    hipError_t e = allow_lds<kernel>(LDS);
+    if (e != hipSuccess) return e;
+    e = launch(kernel, dim3(tiles * (unsigned)a.slices), BM / WM * (BM / WN) * 64, LDS, st, o.p, o.q, o.p_lines, o.q_lines, o.p_matrix, o.q_matrix,
+               o.kblocks, a.tiles_i, a.tiles_j, a.tiles, a.slices, a);
     if (e != hipSuccess || a.slices == 1) return e;
     return launch(rb_ortho_join_kernel<KIND, OUT, BM>, dim3(tiles * (BM / 32) * (BM / 32) / (NS_TPB / 64)), NS_TPB, 0, st, a);
 }
@@ -330,7 +349,9 @@ hipError_t whole(const rb_ortho* o, const UpdateArgs& u, const ResultArgs& resul
         for (int i = 0; i < 3; ++i) a.coefficients[s][i] = o->coefficients[s][i];
     const size_t lds = (size_t)2 * o->small * o->small * 4;
     if (o->small == 64) return launch(rb_ortho_small_kernel<T, OUT, 64, 32>, dim3((unsigned)o->matrices), 256, lds, st, a);
-    return launch(rb_ortho_small_kernel<T, OUT, 128, 32>, dim3((unsigned)o->matrices), 1024, lds, st, a);
+    constexpr auto kernel = rb_ortho_small_kernel<T, OUT, 128, 32>;
+    const hipError_t e = allow_lds<kernel>(lds);
+    return e != hipSuccess ? e : launch(kernel, dim3((unsigned)o->matrices), 1024, lds, st, a);
 }
 
 hipError_t orthogonalize(const rb_ortho* o, const UpdateArgs& u, const ResultArgs& result, hipStream_t st)

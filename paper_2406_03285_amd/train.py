@@ -233,6 +233,8 @@ class TokenScorer(_OnStream):
             for t in (out.lse, out.entropy):
                 if t is not None:
                     self._small(t, (rows,), torch.float32, "out.lse, out.entropy")
+        if rows == 0:
+            return out
         _check(self._on_stream(rb_scorer_score, self.handle, logits, rows, stride, tokens, out.logp if self.given else None, out.lse,
                                out.entropy, out.top_logp if self.top else None, out.top_ids if self.top else None), "rb_scorer_score")
         return out
@@ -252,6 +254,8 @@ class TokenScorer(_OnStream):
         if grad_entropy is not None:
             self._small(entropy, (rows,), torch.float32, "entropy")
             self._small(grad_entropy, (rows,), torch.float32, "grad_entropy")
+        if rows == 0:
+            return out
         _check(self._on_stream(rb_scorer_grad, self.handle, logits, rows, stride, tokens, lse, None if grad_entropy is None else entropy,
                                grad_logp if self.given else None, grad_entropy, out, out_stride), "rb_scorer_grad")
         return out
@@ -279,6 +283,7 @@ class _Score(torch.autograd.Function):
         return tuple(s)
 
     @staticmethod
+    @torch.autograd.function.once_differentiable
     def backward(ctx, grad_logp, _lse, grad_entropy, _top_logp, _top_ids):
         logits, tokens, lse, entropy = ctx.saved_tensors
         scorer = ctx.scorer
@@ -336,6 +341,7 @@ class Orthogonalizer(_OnStream):
         if scale is None:
             scale = math.sqrt(max(1.0, self.m / self.n))
         _check(self._on_stream(rb_ortho_step, self.handle, weight, *w, grad, *g, momentum, lr, beta, nesterov, weight_decay, scale), "rb_ortho_step")
+        torch.autograd.graph.increment_version((weight, momentum))      # (autograd tells of tensors it has saved that were changed since)
 
     def close(self):
         if getattr(self, "handle", None):

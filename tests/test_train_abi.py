@@ -83,3 +83,44 @@ def test_ortho_calls_refuse():
                 dict(wrs=9), dict(gms=-1), dict(grs=9), dict(lr=NAN), dict(beta=INF), dict(weight_decay=NAN), dict(scale=-INF)):
         assert rb.rb_ortho_step(*{**good, **bad}.values(), STREAM) == rb.RB_EINVAL, bad
     assert rb.rb_ortho_destroy(o) == rb.RB_OK and rb.rb_ortho_destroy(None) == rb.RB_OK
+
+
+@pytest.mark.parametrize("compiler", [["gcc", "-std=c11"], ["g++", "-std=c++17"]])
+def test_header_is_c_and_cpp(compiler, tmp_path):
+    import subprocess
+    src = tmp_path / ("t.c" if compiler[0] == "gcc" else "t.cpp")
+    src.write_text("#include \"rb_train.h\"\nint f(rb_scorer *s) { return rb_scorer_destroy(s); }\n")
+    subprocess.run([*compiler, "-Wall", "-Werror", "-fsyntax-only", "-I", os.path.join(ROOT, "include"), str(src)], check=True)
+
+
+@pytest.mark.parametrize("name", ["rb_scorer_score", "rb_scorer_grad", "rb_ortho_apply"])
+def test_native_marshalling_passes_what_ctypes_passes(name):
+    """Streams, tensors, None and numbers, and what goes to the Python function instead."""
+    import inspect
+
+    import torch
+
+    from paper_2406_03285_amd import binding, train
+    native = getattr(train, name)
+    if binding.Call is None:
+        pytest.skip("no native marshalling was built")
+    general = native.__wrapped__
+    names = list(inspect.signature(general).parameters)
+    kinds = "".join("h" if n in ("s", "o") else "s" if n == "hip_stream" else "i" if n == "rows" or n.endswith("stride") else "p" for n in names)
+    assert {"rb_scorer_score": 11, "rb_scorer_grad": 12, "rb_ortho_apply": 8}[name] == len(kinds)
+    seen = []
+    entry = C.CFUNCTYPE(C.c_int, *[C.c_uint64] * len(kinds))(lambda *a: seen.append(a) or 3)
+    there = binding.Call(C.cast(entry, C.c_void_p).value, kinds, lambda *a: ("general", a))
+
+    class Stream:
+        cuda_stream = 77
+
+    t = torch.zeros(4)
+    args = [{"h": 2 ** 46, "p": t, "i": 5 + i, "s": Stream()}[k] for i, k in enumerate(kinds)]
+    assert there(*args) == 3
+    assert seen == [tuple({"h": 2 ** 46, "p": t.data_ptr(), "i": 5 + i, "s": 77}[k] for i, k in enumerate(kinds))]
+    assert there(*args[:-1]) == 3 and seen[1] == seen[0][:-1] + (0,)              # the stream left out: null
+    args[kinds.index("p")] = None
+    assert there(*args) == 3 and seen[2][kinds.index("p")] == 0
+    args[kinds.index("i")] = 2.5
+    assert there(*args)[0] == "general"
