@@ -609,8 +609,105 @@ __global__ __launch_bounds__(NS_TPB) void rb_ortho_join_kernel(const ProductArgs
     ns_finish<KIND, OUT>(a, k, r0, c0, acc, old, (KIND == NS_GRAM || KIND == NS_POLY) ? tj > ti : true, places[wave]);
 }
 
-// A whole matrix of up to P x P by one workgroup, in LDS: X, or A, or B in one half of it, X^T in the other; X itself in registers, a wavefront
-// has 32 x WN of it.  One launch from the update to the result.
+// ---- matrices of up to P x P in the LDS of one workgroup ------------------------
+//
+// A wavefront per block of 32 x 32 of the result, whose element i of a lane is as above.  A matrix is P * P / 32 lines of 128 bytes, line (block of
+// 32 columns, row), its 16-byte parts at c ^ (row / 2 % 8).
+template <int P>
+struct LdsMatrices {
+    static constexpr int WAVES = (P / 32) * (P / 32), BYTES = P * P * 4;
+    int lane, half, col, wi, wj;
+    uint32_t across_at, along_at;
+
+    __device__ __forceinline__ LdsMatrices()
+    {
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+        lane = threadIdx.x & 63;
+        half = lane / 32;
+        col = lane & 31;
+        wi = wave / (P / 32) * 32;
+        wj = wave % (P / 32) * 32;
+        // The part of a line is the only thing in bits 4 to 6 of an address, so that its turn by the row is one exclusive or, and what is left of
+        // an address a constant.
+        across_at = (uint32_t)((wi / 32 * P + wj + col) * 128 + (col / 2 & 7) * 16 + half * 8);
+        along_at = (uint32_t)((wj / 32 * P + wi + half * 4) * 128 + ((col / 8) ^ (half * 2)) * 16 + col % 8 * 2);
+    }
+    __device__ __forceinline__ int row(int i) const { return wi + (i / 4) * 8 + half * 4 + i % 4; }
+    __device__ __forceinline__ int column() const { return wj + col; }
+
+    // v, scaled already, to the transposed place (4 rows of a column are neighbours there) and, unless null, to its own.
+    __device__ __forceinline__ void put(char* across, char* along, const float* v) const
+    {
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            half4 hi, lo;
+            ns_split<half4, 4>(v + g * 4, hi, lo);
+            if (along != nullptr) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int turn = (g & 1) * 4 + e / 2, off = (g * 8 + e) * 128;
+                    *reinterpret_cast<_Float16*>(along + (along_at ^ (turn * 16)) + off) = hi[e];
+                    *reinterpret_cast<_Float16*>(along + (along_at ^ ((turn ^ 4) * 16)) + off) = lo[e];
+                }
+            }
+            *reinterpret_cast<half4*>(across + (across_at ^ (g * 16))) = hi;
+            *reinterpret_cast<half4*>(across + (across_at ^ ((g ^ 4) * 16))) = lo;
+        }
+    }
+    // The same where another wavefront may still be reading, for all to read.
+    __device__ __forceinline__ void replace(char* across, char* along, const float* v) const
+    {
+        __syncthreads();
+        put(across, along, v);
+        __syncthreads();
+    }
+
+    struct Fragments { half8 ph, pl, qh, ql; };
+    __device__ __forceinline__ void read(Fragments& f, const char* p, const char* q, int block, int ks) const
+    {
+        const int at = ks * 2 + half, hi = (at ^ (col / 2 & 7)) * 16, lo = ((at + 4) ^ (col / 2 & 7)) * 16;
+        const char* pr = p + (block * P + wi + col) * 128;
+        const char* qr = q + (block * P + wj + col) * 128;
+        f.ph = *reinterpret_cast<const half8*>(pr + hi);
+        f.pl = *reinterpret_cast<const half8*>(pr + lo);
+        f.qh = *reinterpret_cast<const half8*>(qr + hi);
+        f.ql = *reinterpret_cast<const half8*>(qr + lo);
+    }
+    static __device__ __forceinline__ void multiply(const Fragments& f, float16v& acc)
+    {
+        acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(f.pl, f.qh, acc, 0, 0, 0);
+        acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(f.ph, f.ql, acc, 0, 0, 0);
+        acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(f.ph, f.qh, acc, 0, 0, 0);
+    }
+    // The wavefront's block of P Q^T over so many blocks of 32 of the summed index.
+    __device__ __forceinline__ float16v product(const char* p, const char* q, int blocks) const
+    {
+        float16v acc = {};
+        if (WAVES > 4) {                                        // four wavefronts a SIMD: one multiplies while another reads
+            for (int block = 0; block < blocks; ++block) {
+#pragma unroll
+                for (int ks = 0; ks < 2; ++ks) {
+                    Fragments f;
+                    read(f, p, q, block, ks);
+                    multiply(f, acc);
+                }
+            }
+        } else {                                                // one: half of a block is read while the other half is multiplied
+            Fragments first, second;
+            read(first, p, q, 0, 0);
+            for (int block = 0; block < blocks; ++block) {
+                read(second, p, q, block, 1);
+                multiply(first, acc);
+                if (block + 1 < blocks) read(first, p, q, block + 1, 0);
+                multiply(second, acc);
+            }
+        }
+        return acc;
+    }
+};
+
+// A whole matrix of up to P x P: X, or A, or B in one half of the LDS, X^T in the other; X itself in registers.  One launch from the update to the
+// result.  The products need 19 us at 128 x 128 and five steps, the rest is the conversions and barriers between them (43 us in all).
 struct SmallArgs {
     UpdateArgs update;
     ResultArgs result;
@@ -618,181 +715,145 @@ struct SmallArgs {
     float coefficients[16][3];
 };
 
-template <typename T, typename OUT, int P, int WN>
-__global__ __launch_bounds__(P / 32 * (P / WN) * 64) void rb_ortho_small_kernel(const SmallArgs a)
+template <typename T, typename OUT, int P>
+__global__ __launch_bounds__(LdsMatrices<P>::WAVES * 64) void rb_ortho_small_kernel(const SmallArgs a)
 {
-    constexpr int WAVES = P / 32 * (P / WN), MJ = WN / 32, LINES = P / 32;
     extern __shared__ __align__(16) char lds[];
-    __shared__ double sums[WAVES];
-    char* const one = lds;                      // X, A, B: line (block of 32 columns, row), its 16-byte parts at c ^ (row / 2 % 8)
-    char* const two = lds + P * LINES * 128;    // X^T
+    __shared__ double sums[LdsMatrices<P>::WAVES];
+    const LdsMatrices<P> mat;
+    char* const one = lds;                                      // X, A, B
+    char* const two = lds + LdsMatrices<P>::BYTES;              // X^T
     const int64_t k = blockIdx.x;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x & 63, half = lane / 32, col = lane & 31;
-    const int wi = wave / (P / WN) * 32, wj = wave % (P / WN) * WN;
     const UpdateArgs& u = a.update;
-    const int rows = a.result.rows, cols = a.result.cols;
+    const int rows = a.result.rows, cols = a.result.cols, c = mat.column();
 
-    float x[MJ][16];
-    double sum = 0.0;
+    float x[16];
     const T* grad = static_cast<const T*>(u.grad) + k * u.matrix_stride;
     float* mom = u.momentum != nullptr ? u.momentum + k * u.m * (int64_t)u.n : nullptr;
+    // the place of the lane's element i in the caller's tensors
+    auto at = [&](int i, int64_t stride) { return u.tall ? c * stride + mat.row(i) : mat.row(i) * stride + c; };
+    auto there = [&](int i) { return mat.row(i) < rows && c < cols; };
 #pragma unroll
-    for (int b = 0; b < MJ; ++b)
+    for (int i = 0; i < 16; ++i) x[i] = there(i) ? ns_load(grad + at(i, u.row_stride)) : 0.0f;
+    if (mom != nullptr) {
+        float v[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] = there(i) ? mom[at(i, u.n)] : 0.0f;
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-            const int r = wi + (i / 4) * 8 + half * 4 + i % 4, c = wj + b * 32 + col;
-            const int ci = u.tall ? c : r, cj = u.tall ? r : c;
-            x[b][i] = r < rows && c < cols ? ns_load(grad + ci * u.row_stride + cj) : 0.0f;
-        }
-    if (mom != nullptr) {
-#pragma unroll
-        for (int b = 0; b < MJ; ++b) {
-            float v[16];
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const int r = wi + (i / 4) * 8 + half * 4 + i % 4, c = wj + b * 32 + col;
-                const int ci = u.tall ? c : r, cj = u.tall ? r : c;
-                v[i] = r < rows && c < cols ? mom[(int64_t)ci * u.n + cj] : 0.0f;
-            }
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const int r = wi + (i / 4) * 8 + half * 4 + i % 4, c = wj + b * 32 + col;
-                const int ci = u.tall ? c : r, cj = u.tall ? r : c;
-                v[i] = fmaf(u.beta, v[i], x[b][i]);
-                if (r < rows && c < cols) mom[(int64_t)ci * u.n + cj] = v[i];
-                x[b][i] = u.nesterov ? fmaf(u.beta, v[i], x[b][i]) : v[i];
-            }
+            v[i] = fmaf(u.beta, v[i], x[i]);
+            if (there(i)) mom[at(i, u.n)] = v[i];
+            x[i] = u.nesterov ? fmaf(u.beta, v[i], x[i]) : v[i];
         }
     }
+    double sum = 0.0;
 #pragma unroll
-    for (int b = 0; b < MJ; ++b)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) sum = fma((double)x[b][i], (double)x[b][i], sum);
+    for (int i = 0; i < 16; ++i) sum = fma((double)x[i], (double)x[i], sum);
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
-    if (lane == 0) sums[wave] = sum;
+    if (mat.lane == 0) sums[threadIdx.x / 64] = sum;
     __syncthreads();
     sum = 0.0;
 #pragma unroll
-    for (int w = 0; w < WAVES; ++w) sum += sums[w];
+    for (int w = 0; w < LdsMatrices<P>::WAVES; ++w) sum += sums[w];
     const double inverse = ns_inverse(sqrt(sum) + (double)u.eps);
 #pragma unroll
-    for (int b = 0; b < MJ; ++b)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) x[b][i] = (float)((double)x[b][i] * inverse);
-
-    // v, scaled already, to the transposed place (4 rows of a column are neighbours there), and to its own.  The part of a line is the only thing in
-    // bits 4 to 6 of an address, so that its turn by the row is one exclusive or, and what is left of an address a constant.
-    const uint32_t across_at = (uint32_t)((wi / 32 * P + wj + col) * 128 + (col / 2 & 7) * 16 + half * 8);
-    const uint32_t along_at = (uint32_t)((wj / 32 * P + wi + half * 4) * 128 + ((col / 8) ^ (half * 2)) * 16 + col % 8 * 2);
-    auto put = [&](char* across, char* along, const float (*v)[16]) {
-#pragma unroll
-        for (int b = 0; b < MJ; ++b)
-#pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                half4 hi, lo;
-                ns_split<half4, 4>(v[b] + g * 4, hi, lo);
-                if (along != nullptr) {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int turn = (g & 1) * 4 + e / 2, off = b * P * 128 + (g * 8 + e) * 128;
-                        *reinterpret_cast<_Float16*>(along + (along_at ^ (turn * 16)) + off) = hi[e];
-                        *reinterpret_cast<_Float16*>(along + (along_at ^ ((turn ^ 4) * 16)) + off) = lo[e];
-                    }
-                }
-                *reinterpret_cast<half4*>(across + (across_at ^ (g * 16)) + b * 32 * 128) = hi;
-                *reinterpret_cast<half4*>(across + (across_at ^ ((g ^ 4) * 16)) + b * 32 * 128) = lo;
-            }
-    };
-    float16v acc[MJ];
-    auto product = [&](const char* p, const char* q, int blocks) {
-#pragma unroll
-        for (int b = 0; b < MJ; ++b) acc[b] = float16v{};
-        struct Fragments { half8 ph, pl, qh[MJ], ql[MJ]; };
-        auto read = [&](Fragments& f, int block, int ks) {
-            const int at = ks * 2 + half, hi = (at ^ (col / 2 & 7)) * 16, lo = ((at + 4) ^ (col / 2 & 7)) * 16;
-            const char* pr = p + (block * P + wi + col) * 128;
-            f.ph = *reinterpret_cast<const half8*>(pr + hi);
-            f.pl = *reinterpret_cast<const half8*>(pr + lo);
-#pragma unroll
-            for (int b = 0; b < MJ; ++b) {
-                const char* qr = q + (block * P + wj + b * 32 + col) * 128;
-                f.qh[b] = *reinterpret_cast<const half8*>(qr + hi);
-                f.ql[b] = *reinterpret_cast<const half8*>(qr + lo);
-            }
-        };
-        auto multiply = [&](const Fragments& f) {
-#pragma unroll
-            for (int b = 0; b < MJ; ++b) {
-                acc[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f.pl, f.qh[b], acc[b], 0, 0, 0);
-                acc[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f.ph, f.ql[b], acc[b], 0, 0, 0);
-                acc[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f.ph, f.qh[b], acc[b], 0, 0, 0);
-            }
-        };
-        if (WAVES > 4) {                                        // four wavefronts a SIMD: one multiplies while another reads
-            for (int block = 0; block < blocks; ++block) {
-#pragma unroll
-                for (int ks = 0; ks < 2; ++ks) {
-                    Fragments f;
-                    read(f, block, ks);
-                    multiply(f);
-                }
-            }
-        } else {                                                // one: half of a block is read while the other half is multiplied
-            Fragments first, second;
-            read(first, 0, 0);
-            for (int block = 0; block < blocks; ++block) {
-                read(second, block, 1);
-                multiply(first);
-                if (block + 1 < blocks) read(first, block + 1, 0);
-                multiply(second);
-            }
-        }
-    };
+    for (int i = 0; i < 16; ++i) x[i] = (float)((double)x[i] * inverse);
 
     const int row_blocks = (rows + 31) / 32, col_blocks = (cols + 31) / 32;
-    put(two, one, x);
+    mat.put(two, one, x);
     __syncthreads();
     for (int s = 0; s < a.steps; ++s) {
         const float ca = a.coefficients[s][0], cb = a.coefficients[s][1], cc = a.coefficients[s][2];
-        float v[MJ][16];
-        product(one, one, col_blocks);                          // A
+        float v[16];
+        float16v acc = mat.product(one, one, col_blocks);       // A
 #pragma unroll
-        for (int b = 0; b < MJ; ++b)
+        for (int i = 0; i < 16; ++i) v[i] = acc[i] * (NS_SCALE_A / (NS_SCALE_X * NS_SCALE_X));
+        mat.replace(one, nullptr, v);
+        acc = mat.product(one, one, row_blocks);                // B = b A + c A A
 #pragma unroll
-            for (int i = 0; i < 16; ++i) v[b][i] = acc[b][i] * (NS_SCALE_A / (NS_SCALE_X * NS_SCALE_X));
-        __syncthreads();
-        put(one, nullptr, v);
-        __syncthreads();
-        product(one, one, row_blocks);                          // B = b A + c A A
+        for (int i = 0; i < 16; ++i)
+            v[i] = fmaf(cb * (NS_SCALE_B / NS_SCALE_A), v[i], cc * (NS_SCALE_B / (NS_SCALE_A * NS_SCALE_A)) * acc[i]);
+        mat.replace(one, nullptr, v);
+        acc = mat.product(one, two, row_blocks);                // X <- a X + B X
 #pragma unroll
-        for (int b = 0; b < MJ; ++b)
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
-                v[b][i] = fmaf(cb * (NS_SCALE_B / NS_SCALE_A), v[b][i], cc * (NS_SCALE_B / (NS_SCALE_A * NS_SCALE_A)) * acc[b][i]);
-        __syncthreads();
-        put(one, nullptr, v);
-        __syncthreads();
-        product(one, two, row_blocks);                          // X <- a X + B X
-#pragma unroll
-        for (int b = 0; b < MJ; ++b)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) x[b][i] = fmaf(ca, x[b][i], acc[b][i] * (1.0f / NS_SCALE_B));
-        if (s + 1 == a.steps) break;
-        __syncthreads();
-        put(two, one, x);
-        __syncthreads();
+        for (int i = 0; i < 16; ++i) x[i] = fmaf(ca, x[i], acc[i] * (1.0f / NS_SCALE_B));
+        if (s + 1 < a.steps) mat.replace(two, one, x);
     }
     OUT* dst = static_cast<OUT*>(a.result.dst) + k * a.result.matrix_stride;
+    const int r = mat.row(0);
 #pragma unroll
-    for (int b = 0; b < MJ; ++b) {
-        const int r = wi + half * 4, c = wj + b * 32 + col;
+    for (int i = 0; i < 16; ++i) x[i] *= 1.0f / NS_SCALE_X;
+    if (!a.result.tall)
+        ns_result<StepRows>(a.result, dst + r * a.result.row_stride + c, a.result.row_stride, c < cols ? rows - r : 0, x);
+    else
+        ns_result<StepRows>(a.result, dst + c * a.result.row_stride + r, 1, c < cols ? rows - r : 0, x);
+}
+
+// A block of steps on A alone, of a short side of up to P: R, the product of the steps' P = a I + b A + c A A, from A.  A launch instead of nine or five
+// of a few microseconds each.
+struct StepsArgs {
+    const _Float16* a;
+    _Float16* r;
+    int64_t matrix, pitch;      // halves between matrices, and between rows, of both
+    int32_t rows, steps;
+    float coefficients[3][3];
+};
+
+template <int P>
+__global__ __launch_bounds__(LdsMatrices<P>::WAVES * 64) void rb_ortho_steps_kernel(const StepsArgs a)
+{
+    extern __shared__ __align__(16) char lds[];
+    const LdsMatrices<P> mat;
+    char* const one = lds;                                      // A, P A, R
+    char* const two = lds + LdsMatrices<P>::BYTES;              // P
+    const int c = mat.column(), blocks = (a.rows + 31) / 32;
+    const _Float16* from = a.a + blockIdx.x * a.matrix + ns_at(c, mat.row(0), a.pitch);          // (A is symmetric)
+    float m[16], p[16], r[16];                                  // A, P, R
 #pragma unroll
-        for (int i = 0; i < 16; ++i) x[b][i] *= 1.0f / NS_SCALE_X;
-        if (!a.result.tall)
-            ns_result<StepRows>(a.result, dst + r * a.result.row_stride + c, a.result.row_stride, c < cols ? rows - r : 0, x[b]);
-        else
-            ns_result<StepRows>(a.result, dst + c * a.result.row_stride + r, 1, c < cols ? rows - r : 0, x[b]);
+    for (int g = 0; g < 4; ++g) {
+        const half4 hi = *reinterpret_cast<const half4*>(from + g * 8), lo = *reinterpret_cast<const half4*>(from + g * 8 + NS_KBLOCK);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) m[g * 4 + e] = mat.row(g * 4 + e) < a.rows && c < a.rows ? (float)hi[e] + (float)lo[e] : 0.0f;
+    }
+    mat.put(one, nullptr, m);
+    __syncthreads();
+    for (int s = 0; s < a.steps; ++s) {
+        const float ca = a.coefficients[s][0], cb = a.coefficients[s][1], cc = a.coefficients[s][2];
+        float16v acc = mat.product(one, one, blocks);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            p[i] = fmaf(cb * (NS_SCALE_B / NS_SCALE_A), m[i], cc * (NS_SCALE_B / (NS_SCALE_A * NS_SCALE_A)) * acc[i]);
+            if (mat.row(i) == c) p[i] += ca * NS_SCALE_B;
+        }
+        mat.replace(two, nullptr, p);
+        if (s + 1 < a.steps) {                                  // P A, then A <- P (P A)
+            acc = mat.product(two, one, blocks);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) m[i] = acc[i] * (1.0f / NS_SCALE_B);
+            mat.replace(one, nullptr, m);
+            acc = mat.product(two, one, blocks);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) m[i] = acc[i] * (1.0f / NS_SCALE_B);
+        }
+        if (s == 0) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) r[i] = p[i];
+        } else {                                                // R <- P R
+            mat.replace(one, nullptr, r);
+            acc = mat.product(two, one, blocks);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) r[i] = acc[i] * (1.0f / NS_SCALE_B);
+        }
+        if (s + 1 < a.steps) mat.replace(one, nullptr, m);
+    }
+    _Float16* to = a.r + blockIdx.x * a.matrix + ns_at(c, mat.row(0), a.pitch);
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+        half4 hi, lo;
+        ns_split<half4, 4>(r + g * 4, hi, lo);
+        *reinterpret_cast<half4*>(to + g * 8) = hi;
+        *reinterpret_cast<half4*>(to + g * 8 + NS_KBLOCK) = lo;
     }
 }
 

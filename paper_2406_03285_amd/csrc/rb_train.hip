@@ -301,7 +301,9 @@ void choose_tiles(rb_ortho* o)
     }
     // a block of n steps: A, n B, n - 1 times the two of A and the one of R, and R X, instead of n times A, B, B X
     const int blocks = (o->steps + NS_BLOCK - 1) / NS_BLOCK;
-    const double by_blocks = blocks * (us[OF_A] + us[OF_X]) + (o->steps + 3 * (o->steps - blocks)) * us[OF_B];
+    const int squares = o->steps + 3 * (o->steps - blocks);
+    const double in_squares = o->rows > 128 ? squares * us[OF_B] : blocks * 5 + squares * (o->rows <= 64 ? 0.9 : 2.3) * (double)((o->matrices + 255) / 256);
+    const double by_blocks = blocks * (us[OF_A] + us[OF_X]) + in_squares;
     o->block = by_blocks < o->steps * (us[OF_A] + us[OF_B] + us[OF_X]) && blocks_fit(o) ? NS_BLOCK : 1;
     o->kept_rows = (int32_t)rows;
     o->kept_cols = (int32_t)cols;
@@ -312,7 +314,7 @@ void choose_tiles(rb_ortho* o)
     o->off_xt[1] = off; off += n * (size_t)cols * tp;
     for (int i = 0; i < 5; ++i) {                          // A, B (P); of blocks also P A and two R
         o->off_square[i] = off;
-        if (i < 2 || o->block > 1) off += n * (size_t)rows * tp;
+        if (i < 2 || (o->block > 1 && o->rows > 128)) off += n * (size_t)rows * tp;
     }
     o->off_sums = off; off += sums;
     o->bytes = off;
@@ -348,10 +350,27 @@ hipError_t whole(const rb_ortho* o, const UpdateArgs& u, const ResultArgs& resul
     for (int s = 0; s < o->steps; ++s)
         for (int i = 0; i < 3; ++i) a.coefficients[s][i] = o->coefficients[s][i];
     const size_t lds = (size_t)2 * o->small * o->small * 4;
-    if (o->small == 64) return launch(rb_ortho_small_kernel<T, OUT, 64, 32>, dim3((unsigned)o->matrices), 256, lds, st, a);
-    constexpr auto kernel = rb_ortho_small_kernel<T, OUT, 128, 32>;
+    if (o->small == 64) return launch(rb_ortho_small_kernel<T, OUT, 64>, dim3((unsigned)o->matrices), 256, lds, st, a);
+    constexpr auto kernel = rb_ortho_small_kernel<T, OUT, 128>;
     const hipError_t e = allow_lds<kernel>(lds);
     return e != hipSuccess ? e : launch(kernel, dim3((unsigned)o->matrices), 1024, lds, st, a);
+}
+
+// R of a block of n steps, from A, of short sides that fit one workgroup.
+hipError_t steps_in_lds(const rb_ortho* o, const _Float16* a, _Float16* r, int64_t pitch, int s, int n, hipStream_t st)
+{
+    StepsArgs g{};
+    g.a = a;
+    g.r = r;
+    g.matrix = o->kept_rows * pitch;
+    g.pitch = pitch;
+    g.rows = o->rows;
+    g.steps = n;
+    for (int i = 0; i < n; ++i)
+        for (int k = 0; k < 3; ++k) g.coefficients[i][k] = o->coefficients[s + i][k];
+    if (o->rows <= 64) return launch(rb_ortho_steps_kernel<64>, dim3((unsigned)o->matrices), 256, 2 * LdsMatrices<64>::BYTES, st, g);
+    const hipError_t e = allow_lds<rb_ortho_steps_kernel<128>>(2 * LdsMatrices<128>::BYTES);
+    return e != hipSuccess ? e : launch(rb_ortho_steps_kernel<128>, dim3((unsigned)o->matrices), 1024, 2 * LdsMatrices<128>::BYTES, st, g);
 }
 
 hipError_t orthogonalize(const rb_ortho* o, const UpdateArgs& u, const ResultArgs& result, hipStream_t st)
@@ -385,7 +404,9 @@ hipError_t orthogonalize(const rb_ortho* o, const UpdateArgs& u, const ResultArg
         e = product<NS_GRAM, float>(o, Operands{x, x, xl, xl, x_matrix, x_matrix, by_cols}, to_square(ma, NS_SCALE_A / (NS_SCALE_X * NS_SCALE_X)), OF_A, st);
         // B = b A + c A A and then a X + B X; or, of a block, P = a I + B, and R X
         const _Float16* left_of_x = mb;
-        for (int i = 0; i < n && e == hipSuccess; ++i) {
+        const bool in_lds = n > 1 && o->rows <= 128;
+        if (in_lds && e == hipSuccess) e = steps_in_lds(o, ma, mb, tp, s, n, st);
+        for (int i = 0; i < n && !in_lds && e == hipSuccess; ++i) {
             const float* c = o->coefficients[s + i];
             _Float16* const to = n > 1 && i == 0 ? place(o->off_square[3]) : mb;
             ProductArgs p = to_square(to, c[2] * (NS_SCALE_B / (NS_SCALE_A * NS_SCALE_A)));
