@@ -3,6 +3,8 @@
 // Score.  A row of logits is read once, 16 bytes per lane and load.  Every lane keeps the running maximum m of what it has seen, s = sum
 // of e^(z - m) and t = sum of e^(z - m) (z - m), rescaled when a tile of 32 elements brings a larger maximum; lanes, wavefronts and
 // workgroups are joined by the same rule, and lse = m + log s, entropy = log s - t / s.
+// Bound by HBM without alternatives (8192 x 131072 bfloat16: 368 us, 5.8 TB/s; 8.7 vector instructions per logit), by vector instructions with them
+// (2048 x 50001 with 16: 51 us, 4.0 TB/s, 14.4 per logit; 5120 x 10000 binary32 with 5: 40 us, 5.2 TB/s).
 // Alternatives.  A wavefront keeps its best 64 elements so far as one 64-bit key per lane, sorted: the logit in an order-preserving 32-bit
 // form above the inverted index, so that equal logits order by index and no two keys are equal.  A lane whose tile holds nothing above the
 // smallest key that still counts (which the running maximum tells at no cost) goes on; the others put their tile into LDS, half a wavefront
@@ -529,6 +531,7 @@ struct GradArgs {
 
 constexpr int GR_MAX_TILES = 32;    // tiles of SC_TPB accesses in a chunk: one bit each says whether a given token is in it
 
+// Bound by HBM: each logit read once, each gradient written once (8192 x 131072 bfloat16: 814 us, 5.3 TB/s; 1024 x 50001 with 17 given tokens: 38 us).
 // A workgroup per row (blockIdx.x) and chunk of the row (blockIdx.y).  N elements per access: 16 bytes, or one element where logits and
 // gradient lie differently relative to 16 bytes.  Which of a thread's accesses hold a given token is one word of bits, so that the rest
 // costs one test; the tokens' sums are made in the order in which they were given.

@@ -186,3 +186,38 @@ def test_every_tile_and_slicing(batch, m, n):
         want = 0.75 * before - 0.5 * on_the_gpu(u[0], FIVE, 1e-7)
         off = torch.linalg.vector_norm(w.double() - want)
         assert off <= 2.0 ** -9 * torch.linalg.vector_norm(want) + ref.orthogonal_bound(FIVE) * torch.linalg.vector_norm(want - 0.75 * before)
+
+
+@pytest.mark.parametrize("batch,m,n", [(2, 40, 50), (1, 100, 128), (1, 33, 70), (3, 50, 700), (2, 97, 300), (1, 130, 140), (2, 200, 333), (1, 300, 2500), (1, 1999, 1700)])
+def test_what_the_workspace_held_does_not_matter(batch, m, n):
+    """Room beyond the last row and column is never read into a sum: the workspace starts full of NaN."""
+    u = update(batch, m, n, F32, seed=3)
+    o = rb.Orthogonalizer(m, n, batch=batch)
+    o.workspace.fill_(0xFF)
+    got = o.orthogonalize(u)
+    assert torch.isfinite(got).all()
+    o.workspace.random_(0, 256)
+    assert torch.equal(o.orthogonalize(u), got)
+    for i in range(batch):
+        want = on_the_gpu(u[i], FIVE, 1e-7)
+        assert torch.linalg.vector_norm(got[i] - want) <= ref.orthogonal_bound(FIVE) * torch.linalg.vector_norm(want)
+
+
+@pytest.mark.parametrize("steps", [1, 2, 3, 4, 6, 7])
+@pytest.mark.parametrize("m,n", [(60, 2000), (2100, 110), (200, 3000)])
+def test_blocks_of_steps(m, n, steps):
+    """A long side: steps are made on the short side's square in blocks of up to three."""
+    u = update(1, m, n, F32, seed=steps)[0]
+    coefficients = (rb.NEWTON_SCHULZ,) * steps
+    got = rb.Orthogonalizer(m, n, coefficients=coefficients).orthogonalize(u)
+    want = on_the_gpu(u, coefficients, 1e-7)
+    assert torch.linalg.vector_norm(got - want) <= ref.orthogonal_bound(coefficients) * torch.linalg.vector_norm(want)
+
+
+def test_blocks_that_would_not_fit_are_not_made():
+    """Three steps that raise small values by more than 60 go one by one."""
+    coefficients = ((4.0, -10.2, 7.1),) * 3                 # 64 at small values, and nowhere beyond 2
+    u = update(1, 48, 3000, F32, seed=5)[0]
+    got = rb.Orthogonalizer(48, 3000, coefficients=coefficients).orthogonalize(u)
+    want = on_the_gpu(u, coefficients, 1e-7)
+    assert torch.linalg.vector_norm(got - want) <= ref.orthogonal_bound(coefficients) * torch.linalg.vector_norm(want)

@@ -227,3 +227,18 @@ def test_rows_far_apart():
     t, w = tokens_for(3, vocab, 1), torch.ones((3, 1), device="cuda")
     near = scorer.grad(z.contiguous(), t, got.lse, got.entropy, w)
     assert torch.equal(scorer.grad(z, t, got.lse, got.entropy, w, out=z), near)
+
+
+@pytest.mark.parametrize("rows,vocab", [(1, 200000), (3, 131075), (100, 70000), (2, 66000)])
+def test_rows_shared_by_workgroups(rows, vocab):
+    """What the parts of an earlier call left does not matter, and the counters are back at nothing."""
+    z, t = make(rows, vocab, BF16, seed=rows), tokens_for(rows, vocab, 2)
+    scorer = rb.TokenScorer(vocab, BF16, given=2, top=40)
+    first = scorer.score(z, t)
+    counters = scorer.workspace[:1024].view(torch.int32)
+    assert (counters == 0).all()
+    scorer.workspace[1024:].fill_(0xFF)
+    for a, b in zip(first, scorer.score(z, t)):
+        assert torch.equal(a, b)
+    assert (counters == 0).all()
+    check_score(z, t, 40)
