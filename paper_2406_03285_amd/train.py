@@ -135,6 +135,12 @@ except ImportError:
     def _current_stream(index):
         return torch.cuda.current_stream(index).cuda_stream
 
+
+def _fits(t, dtype, index, shape):
+    """Whether t is a contiguous tensor of that type and shape on the device of that index."""
+    return t.dtype is dtype and t.get_device() == index and t.shape == shape and t.is_contiguous()
+
+
 _CODES = {torch.float32: RB_F32, torch.bfloat16: RB_BF16}
 
 
@@ -146,25 +152,21 @@ class _OnStream:
         self.device = torch.device(device)
         if self.device.index is None:
             self.device = torch.device(self.device.type, torch.cuda.current_device())
+        self._index = self.device.index
         self._last = torch.cuda.current_stream(self.device)
         self._last_address = self._last.cuda_stream
 
-    def _current(self):
-        """Address of the stream that a call goes to."""
-        address = _current_stream(self.device.index)
+    def _on_stream(self, call, *args):
+        address = _current_stream(self._index)
         if address != self._last_address:
             stream = torch.cuda.current_stream(self.device)
             if not torch.cuda.is_current_stream_capturing():
                 stream.wait_stream(self._last)
             self._last, self._last_address = stream, address
-        return address
-
-    def _on_stream(self, call, *args):
-        stream = self._current()
-        if torch.cuda.current_device() == self.device.index:
-            return call(*args, stream)
+        if torch.cuda.current_device() == self._index:
+            return call(*args, address)
         with torch.cuda.device(self.device):
-            return call(*args, stream)
+            return call(*args, address)
 
 
 class Scores(NamedTuple):
@@ -174,6 +176,10 @@ class Scores(NamedTuple):
     entropy: torch.Tensor                  # [rows]
     top_logp: Optional[torch.Tensor]       # [rows, top]
     top_ids: Optional[torch.Tensor]        # [rows, top] int64
+
+
+class _Outputs(Scores):
+    """Scores' tensors that TokenScorer.outputs has made: `scorer` and `rows` say for what."""
 
 
 class TokenScorer(_OnStream):
@@ -195,69 +201,69 @@ class TokenScorer(_OnStream):
         _check(self._on_stream(rb_scorer_bind, self.handle, self.workspace), "rb_scorer_bind")
 
     def outputs(self, rows):
-        """Tensors for score(..., out=...)."""
+        """Tensors for score(..., out=...), which looks at these no further."""
         def new(*shape, dtype=torch.float32):
             return torch.empty(shape, dtype=dtype, device=self.device)
-        return Scores(new(rows, self.given) if self.given else None, new(rows), new(rows), new(rows, self.top) if self.top else None,
-                      new(rows, self.top, dtype=torch.int64) if self.top else None)
+        out = _Outputs(new(rows, self.given) if self.given else None, new(rows), new(rows), new(rows, self.top) if self.top else None,
+                       new(rows, self.top, dtype=torch.int64) if self.top else None)
+        out.scorer, out.rows = self, rows
+        return out
 
     def _rows(self, logits, what):
         """(rows, elements between them) of a tensor of the logits' form, looked at first."""
-        shape = logits.shape
-        assert len(shape) == 2 and shape[1] == self.vocab and logits.dtype == self.dtype and logits.device == self.device, what
-        stride, step = logits.stride()
+        shape, (stride, step) = logits.shape, logits.stride()
+        assert len(shape) == 2 and shape[1] == self.vocab and logits.dtype == self.dtype and logits.get_device() == self._index, what
         assert step == 1 or self.vocab == 1, what
         return shape[0], stride if shape[0] > 1 else max(stride, self.vocab)
 
-    def _small(self, t, shape, dtype, what):
-        assert t.shape == shape and t.dtype == dtype and t.is_contiguous() and t.device == self.device, what
-
-    def _tokens(self, tokens, rows):
-        if not self.given:
-            return None
-        self._small(tokens, (rows,) if self.given == 1 and tokens.dim() == 1 else (rows, self.given), torch.int64, "tokens")
-        return tokens
+    def _given(self, t, rows, dtype, what):
+        """A tensor of given tokens' form: [rows, given], or [rows] of one."""
+        assert _fits(t, dtype, self._index, (rows, self.given)) or (self.given == 1 and _fits(t, dtype, self._index, (rows,))), what
+        return t
 
     def score(self, logits, tokens=None, out=None):
         """Scores of every row of logits; into `out` if given (see outputs)."""
         rows, stride = self._rows(logits, "logits")
-        tokens = self._tokens(tokens, rows)
+        if self.given:
+            self._given(tokens, rows, torch.int64, "tokens")
         if out is None:
             out = self.outputs(rows)
-        else:
-            if self.given:
-                self._small(out.logp, (rows, self.given), torch.float32, "out.logp")
-            if self.top:
-                self._small(out.top_logp, (rows, self.top), torch.float32, "out.top_logp")
-                self._small(out.top_ids, (rows, self.top), torch.int64, "out.top_ids")
-            for t in (out.lse, out.entropy):
-                if t is not None:
-                    self._small(t, (rows,), torch.float32, "out.lse, out.entropy")
+        elif type(out) is not _Outputs or out.scorer is not self or out.rows != rows:
+            f32, index = torch.float32, self._index
+            assert out.lse is None or _fits(out.lse, f32, index, (rows,)), "out.lse"
+            assert out.entropy is None or _fits(out.entropy, f32, index, (rows,)), "out.entropy"
+            assert not self.given or _fits(out.logp, f32, index, (rows, self.given)), "out.logp"
+            assert not self.top or (_fits(out.top_logp, f32, index, (rows, self.top)) and _fits(out.top_ids, torch.int64, index, (rows, self.top))), "out.top"
         if rows == 0:
             return out
-        _check(self._on_stream(rb_scorer_score, self.handle, logits, rows, stride, tokens, out.logp if self.given else None, out.lse,
-                               out.entropy, out.top_logp if self.top else None, out.top_ids if self.top else None), "rb_scorer_score")
+        logp, lse, entropy, top_logp, top_ids = out
+        _check(self._on_stream(rb_scorer_score, self.handle, logits, rows, stride, tokens if self.given else None, logp if self.given else None, lse,
+                               entropy, top_logp if self.top else None, top_ids if self.top else None), "rb_scorer_score")
         return out
 
     def grad(self, logits, tokens, lse, entropy, grad_logp, grad_entropy=None, out=None):
         """The gradient with respect to the logits, from the derivatives with respect to logp [rows, given] and entropy [rows] (or None).
         out: a tensor shaped as the logits (rows may be strided), which the logits themselves may be."""
         rows, stride = self._rows(logits, "logits")
-        tokens = self._tokens(tokens, rows)
         if out is None:
             out = torch.empty((rows, self.vocab), dtype=self.dtype, device=self.device)
         out_rows, out_stride = self._rows(out, "out")
         assert out_rows == rows, "out"
-        self._small(lse, (rows,), torch.float32, "lse")
+        assert _fits(lse, torch.float32, self._index, (rows,)), "lse"
         if self.given:
-            self._small(grad_logp, (rows,) if self.given == 1 and grad_logp.dim() == 1 else (rows, self.given), torch.float32, "grad_logp")
-        if grad_entropy is not None:
-            self._small(entropy, (rows,), torch.float32, "entropy")
-            self._small(grad_entropy, (rows,), torch.float32, "grad_entropy")
+            self._given(tokens, rows, torch.int64, "tokens")
+            self._given(grad_logp, rows, torch.float32, "grad_logp")
+        else:
+            tokens = grad_logp = None
+        if grad_entropy is None:
+            entropy = None
+        else:
+            assert _fits(entropy, torch.float32, self._index, (rows,)), "entropy"
+            assert _fits(grad_entropy, torch.float32, self._index, (rows,)), "grad_entropy"
         if rows == 0:
             return out
-        _check(self._on_stream(rb_scorer_grad, self.handle, logits, rows, stride, tokens, lse, None if grad_entropy is None else entropy,
-                               grad_logp if self.given else None, grad_entropy, out, out_stride), "rb_scorer_grad")
+        _check(self._on_stream(rb_scorer_grad, self.handle, logits, rows, stride, tokens, lse, entropy, grad_logp, grad_entropy, out, out_stride),
+               "rb_scorer_grad")
         return out
 
     def __call__(self, logits, tokens=None):
