@@ -116,10 +116,14 @@ int rb_scorer_score(rb_scorer* s, const void* logits, int64_t rows, int64_t row_
     a.given = s->given;
     a.top = s->top;
     // Wavefronts per row: one tile is a wavefront's.  Rows that fill the chip get few, since each has a list of its own to sort and join (2048
-    // rows of 50001 with 16 alternatives: 63 us with one, 51 with two, 58 with four), and four when they are long.  Fewer rows get 16, and
-    // what has more than a few tiles for each of these is shared by several workgroups.
+    // rows of 50001 with 16 alternatives: 63 us with one, 51 with two, 58 with four), and four when they are long.  Fewer rows get 16.
     const int waves = tiles == 1 || (tiles <= 8 && rows >= 4096) ? 1 : tiles <= 32 && rows >= 2048 ? 2 : rows >= 512 || tiles <= SC_NWAVE ? SC_NWAVE : SC_MANY_WAVES;
-    a.splits = waves == SC_MANY_WAVES ? (int32_t)std::max<int64_t>(1, std::min<int64_t>({tiles / (2 * SC_MANY_WAVES), 256 / rows, SC_MAX_SPLITS})) : 1;
+    // Rows shared by workgroups: what the last one waits for (the others' parts have to reach memory) costs more with every workgroup, so the
+    // more rows, the more tiles for each wavefront: one, two, and four from 33 rows (bfloat16, 20 alternatives, unshared and shared: one row
+    // of 131072 20.0 and 13.2 us, 16 rows of 131072 20.7 and 18.0, 64 rows of 262144 34.5 and 26.3; at two tiles each 64 rows of 131072
+    // without alternatives would take 15.3 us, not 11.4).
+    const int64_t each = rows > 32 ? 4 : rows > 8 ? 2 : 1, splits = waves == SC_MANY_WAVES ? tiles / (each * SC_MANY_WAVES) : 1;
+    a.splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>({splits, SC_SPLIT_GROUPS / rows, SC_MAX_SPLITS}));
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     hipError_t e;
     if (s->dtype == RB_F32)
