@@ -5,11 +5,12 @@
 // rounded to one 16-bit number would leave errors of per cents; so an operand is kept as the sum of two binary16 numbers (hi + lo, 22
 // bits), a product is three matrix instructions (hi hi + hi lo + lo hi; lo lo is below the last bit), and sums are binary32.
 //
-// Where one side is much the longer one, most of the work is in the two products with X.  Then up to three steps are made on A alone: a step
+// Where one side is much the longer one, most of the work is in the two products with X.  Then steps are made in pairs on A alone: a step
 // multiplies X from the left by P = a I + b A + c A A, and A, a polynomial of the same symmetric matrix, by P twice; R, the product of the
-// block's P, is applied to X at its end.  That is 9 symmetric products of the short side for three steps instead of two more A and two more B X.
-// More than three steps would let A's rounding errors grow (by a^2 a step); with three, and two, results are as exact as with the plain form
-// in binary32 (1.3e-6 against 1.8e-6 at 200 x 1000, simulated).
+// pair's P, is applied to X at its end.  That is 5 symmetric products of the short side for two steps instead of 2, one more A and one more B X.
+// Three steps at a time would let A's rounding errors grow once more by a^2, which they do where a few directions are much stronger than the
+// rest (errors of 3 to 20 times those of the plain form in binary32 were measured); in pairs they stay within 1.7 times, and from 200 rows on at or
+// below the plain form's.
 //
 // Every product is P Q^T of two row-major matrices with the summed index contiguous: X and X^T are both kept, A and B are symmetric, and of
 // the symmetric results only the tiles on and above the diagonal are computed, each written to its place and mirrored.
@@ -793,63 +794,61 @@ __global__ __launch_bounds__(LdsMatrices<P>::WAVES * 64) void rb_ortho_small_ker
         ns_result<StepRows>(a.result, dst + c * a.result.row_stride + r, 1, c < cols ? rows - r : 0, x);
 }
 
-// A block of steps on A alone, of a short side of up to P: R, the product of the steps' P = a I + b A + c A A, from A.  A launch instead of nine or five
-// of a few microseconds each.
-struct StepsArgs {
+// Two steps on A alone, of a short side of up to P: R = P2 P1 with P = a I + b A + c A A, the second of P1 A P1.  A launch instead of five of a few
+// microseconds each.  What is put is there transposed, so a product's operands are the other way round: P1 A P1 and P2 P1 as they are
+// written.  P1 P1 A and P1 P2 would be the same but for their rounding errors, which P1 multiplies by up to a a and by a in the weak singular
+// directions (results of up to twice the error).
+struct PairArgs {
     const _Float16* a;
     _Float16* r;
     int64_t matrix, pitch;      // halves between matrices, and between rows, of both
-    int32_t rows, steps;
-    float coefficients[3][3];
+    int32_t rows;
+    float coefficients[2][3];
 };
 
 template <int P>
-__global__ __launch_bounds__(LdsMatrices<P>::WAVES * 64) void rb_ortho_steps_kernel(const StepsArgs a)
+__global__ __launch_bounds__(LdsMatrices<P>::WAVES * 64) void rb_ortho_pair_kernel(const PairArgs a)
 {
     extern __shared__ __align__(16) char lds[];
     const LdsMatrices<P> mat;
-    char* const one = lds;                                      // A, P A, R
-    char* const two = lds + LdsMatrices<P>::BYTES;              // P
+    char* const one = lds;                                      // A, P1 A, P1 A P1, P1
+    char* const two = lds + LdsMatrices<P>::BYTES;              // P1, P2
     const int c = mat.column(), blocks = (a.rows + 31) / 32;
     const _Float16* from = a.a + blockIdx.x * a.matrix + ns_at(c, mat.row(0), a.pitch);          // (A is symmetric)
-    float m[16], p[16], r[16];                                  // A, P, R
+    float m[16], p[16], r[16];                                  // A, the step's P, the first P and R
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
         const half4 hi = *reinterpret_cast<const half4*>(from + g * 8), lo = *reinterpret_cast<const half4*>(from + g * 8 + NS_KBLOCK);
 #pragma unroll
         for (int e = 0; e < 4; ++e) m[g * 4 + e] = mat.row(g * 4 + e) < a.rows && c < a.rows ? (float)hi[e] + (float)lo[e] : 0.0f;
     }
-    mat.put(one, nullptr, m);
-    __syncthreads();
-    for (int s = 0; s < a.steps; ++s) {
-        const float ca = a.coefficients[s][0], cb = a.coefficients[s][1], cc = a.coefficients[s][2];
-        float16v acc = mat.product(one, one, blocks);
+    auto polynomial = [&](const float* k, const float16v& acc) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-            p[i] = fmaf(cb * (NS_SCALE_B / NS_SCALE_A), m[i], cc * (NS_SCALE_B / (NS_SCALE_A * NS_SCALE_A)) * acc[i]);
-            if (mat.row(i) == c) p[i] += ca * NS_SCALE_B;
+            p[i] = fmaf(k[1] * (NS_SCALE_B / NS_SCALE_A), m[i], k[2] * (NS_SCALE_B / (NS_SCALE_A * NS_SCALE_A)) * acc[i]);
+            if (mat.row(i) == c) p[i] += k[0] * NS_SCALE_B;
         }
-        mat.replace(two, nullptr, p);
-        if (s + 1 < a.steps) {                                  // P A, then A <- P (P A)
-            acc = mat.product(two, one, blocks);
+    };
+    auto of_p = [&](float* to, const float16v& acc) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) m[i] = acc[i] * (1.0f / NS_SCALE_B);
-            mat.replace(one, nullptr, m);
-            acc = mat.product(two, one, blocks);
+        for (int i = 0; i < 16; ++i) to[i] = acc[i] * (1.0f / NS_SCALE_B);
+    };
+    mat.put(one, nullptr, m);
+    __syncthreads();
+    polynomial(a.coefficients[0], mat.product(one, one, blocks));
+    mat.replace(two, nullptr, p);
+    of_p(m, mat.product(one, two, blocks));
+    mat.replace(one, nullptr, m);
+    of_p(m, mat.product(two, one, blocks));
+    mat.replace(one, nullptr, m);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) m[i] = acc[i] * (1.0f / NS_SCALE_B);
-        }
-        if (s == 0) {
-#pragma unroll
-            for (int i = 0; i < 16; ++i) r[i] = p[i];
-        } else {                                                // R <- P R
-            mat.replace(one, nullptr, r);
-            acc = mat.product(two, one, blocks);
-#pragma unroll
-            for (int i = 0; i < 16; ++i) r[i] = acc[i] * (1.0f / NS_SCALE_B);
-        }
-        if (s + 1 < a.steps) mat.replace(one, nullptr, m);
-    }
+    for (int i = 0; i < 16; ++i) r[i] = p[i];
+    polynomial(a.coefficients[1], mat.product(one, one, blocks));
+    __syncthreads();
+    mat.put(two, nullptr, p);
+    mat.put(one, nullptr, r);
+    __syncthreads();
+    of_p(r, mat.product(one, two, blocks));
     _Float16* to = a.r + blockIdx.x * a.matrix + ns_at(c, mat.row(0), a.pitch);
 #pragma unroll
     for (int g = 0; g < 4; ++g) {

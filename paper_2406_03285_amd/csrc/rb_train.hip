@@ -186,8 +186,8 @@ struct rb_ortho {
     int32_t small;                 // a workgroup per matrix: its padded side (64, 128), or 0: tiled products
     int32_t kept_rows, kept_cols;  // tiled: with room for whole tiles of every product
     int32_t tile[3], slices[3];    // of A, of B, of X
-    int32_t block;                 // steps that are made on A before X is multiplied (1: none)
-    size_t off_x, off_xt[2], off_square[5], off_sums, bytes;
+    bool pairs;                    // two steps are made on A before X is multiplied
+    size_t off_x, off_xt[2], off_square[4], off_sums, bytes;
     char* ws;
 };
 
@@ -256,30 +256,23 @@ double product_us(int tile, double tiles, int kblocks, int slices)
     return slices == 1 ? us : us + 6 + tiles * slices * tile * tile * 8 / 1e7;
 }
 
-constexpr int NS_BLOCK = 3;      // most steps made on A before X is multiplied
-
-// Whether the products of a block's P stay within what is kept (60 in NS_SCALE_B).
-bool blocks_fit(const rb_ortho* o)
+// Whether P of every step, and of every pair the product of both, stay within what is kept (60 in NS_SCALE_B).
+bool pairs_fit(const rb_ortho* o)
 {
     for (int i = 0; i <= 1024; ++i) {
-        double v = i / 1024.0, r = 1.0;
-        int blocks = (o->steps + NS_BLOCK - 1) / NS_BLOCK;
-        for (int s = 0, n = 0; s < o->steps; s += n, --blocks) {
-            n = (o->steps - s + blocks - 1) / blocks;
-            r = 1.0;
-            for (int k = s; k < s + n; ++k) {
-                const float* c = o->coefficients[k];
-                const double l = v * v, p = c[0] + c[1] * l + c[2] * l * l;
-                v *= p;
-                r *= p;
-                if (!(std::fabs(p) <= 60.0) || !(std::fabs(r) <= 60.0)) return false;
-            }
+        double v = i / 1024.0, first = 1.0;
+        for (int s = 0; s < o->steps; ++s) {
+            const float* c = o->coefficients[s];
+            const double l = v * v, p = c[0] + c[1] * l + c[2] * l * l;
+            v *= p;
+            if (!(std::fabs(p) <= 60.0) || (s % 2 != 0 && !(std::fabs(first * p) <= 60.0))) return false;
+            first = p;
         }
     }
     return true;
 }
 
-// The tiles and slices that take least, whether steps are made on A, and the room that all products need.
+// The tiles and slices that take least, whether pairs of steps are made on A, and the room that all products need.
 void choose_tiles(rb_ortho* o)
 {
     int64_t rows = round_up((size_t)o->rows, 64), cols = round_up((size_t)o->cols, 64);
@@ -303,12 +296,9 @@ void choose_tiles(rb_ortho* o)
         cols = std::max(cols, (int64_t)((which == OF_X ? m : n) * tile));
         if (o->slices[which] > 1) sums = std::max(sums, (size_t)o->matrices * (which == OF_X ? n * m : n * (n + 1) / 2) * o->slices[which] * tile * tile * sizeof(float));
     }
-    // a block of n steps: A, n B, n - 1 times the two of A and the one of R, and R X, instead of n times A, B, B X
-    const int blocks = (o->steps + NS_BLOCK - 1) / NS_BLOCK;
-    const int squares = o->steps + 3 * (o->steps - blocks);
-    const double in_squares = o->rows > 128 ? squares * us[OF_B] : blocks * 5 + squares * (o->rows <= 64 ? 0.9 : 2.3) * (double)((o->matrices + 255) / 256);
-    const double by_blocks = blocks * (us[OF_A] + us[OF_X]) + in_squares;
-    o->block = by_blocks < o->steps * (us[OF_A] + us[OF_B] + us[OF_X]) && blocks_fit(o) ? NS_BLOCK : 1;
+    // two steps: A, five squares (in LDS: 0.9 or 2.3 us each, and 5 for the launch) and R X instead of twice A, B and B X
+    const double five = o->rows > 128 ? 5 * us[OF_B] : 5 + 5 * (o->rows <= 64 ? 0.9 : 2.3) * (double)((o->matrices + 255) / 256);
+    o->pairs = o->steps > 1 && five < us[OF_A] + 2 * us[OF_B] + us[OF_X] && pairs_fit(o);
     o->kept_rows = (int32_t)rows;
     o->kept_cols = (int32_t)cols;
     const size_t n = (size_t)o->matrices * sizeof(_Float16), xp = (size_t)ns_pitch(cols), tp = (size_t)ns_pitch(rows);
@@ -316,9 +306,9 @@ void choose_tiles(rb_ortho* o)
     o->off_x = off; off += n * (size_t)rows * xp;
     o->off_xt[0] = off; off += n * (size_t)cols * tp;
     o->off_xt[1] = off; off += n * (size_t)cols * tp;
-    for (int i = 0; i < 5; ++i) {                          // A, B (P); of blocks also P A and two R
+    for (int i = 0; i < 4; ++i) {                          // A, B (P); of pairs also the first P and what P A and R share
         o->off_square[i] = off;
-        if (i < 2 || (o->block > 1 && o->rows > 128)) off += n * (size_t)rows * tp;
+        if (i < 2 || (o->pairs && o->rows > 128)) off += n * (size_t)rows * tp;
     }
     o->off_sums = off; off += sums;
     o->bytes = off;
@@ -360,21 +350,20 @@ hipError_t whole(const rb_ortho* o, const UpdateArgs& u, const ResultArgs& resul
     return e != hipSuccess ? e : launch(kernel, dim3((unsigned)o->matrices), 1024, lds, st, a);
 }
 
-// R of a block of n steps, from A, of short sides that fit one workgroup.
-hipError_t steps_in_lds(const rb_ortho* o, const _Float16* a, _Float16* r, int64_t pitch, int s, int n, hipStream_t st)
+// R of steps s and s + 1, from A, of short sides that fit one workgroup.
+hipError_t pair_in_lds(const rb_ortho* o, const _Float16* a, _Float16* r, int64_t pitch, int s, hipStream_t st)
 {
-    StepsArgs g{};
+    PairArgs g{};
     g.a = a;
     g.r = r;
     g.matrix = o->kept_rows * pitch;
     g.pitch = pitch;
     g.rows = o->rows;
-    g.steps = n;
-    for (int i = 0; i < n; ++i)
+    for (int i = 0; i < 2; ++i)
         for (int k = 0; k < 3; ++k) g.coefficients[i][k] = o->coefficients[s + i][k];
-    if (o->rows <= 64) return launch(rb_ortho_steps_kernel<64>, dim3((unsigned)o->matrices), 256, 2 * LdsMatrices<64>::BYTES, st, g);
-    const hipError_t e = allow_lds<rb_ortho_steps_kernel<128>>(2 * LdsMatrices<128>::BYTES);
-    return e != hipSuccess ? e : launch(rb_ortho_steps_kernel<128>, dim3((unsigned)o->matrices), 1024, 2 * LdsMatrices<128>::BYTES, st, g);
+    if (o->rows <= 64) return launch(rb_ortho_pair_kernel<64>, dim3((unsigned)o->matrices), 256, 2 * LdsMatrices<64>::BYTES, st, g);
+    const hipError_t e = allow_lds<rb_ortho_pair_kernel<128>>(2 * LdsMatrices<128>::BYTES);
+    return e != hipSuccess ? e : launch(rb_ortho_pair_kernel<128>, dim3((unsigned)o->matrices), 1024, 2 * LdsMatrices<128>::BYTES, st, g);
 }
 
 hipError_t orthogonalize(const rb_ortho* o, const UpdateArgs& u, const ResultArgs& result, hipStream_t st)
@@ -401,34 +390,31 @@ hipError_t orthogonalize(const rb_ortho* o, const UpdateArgs& u, const ResultArg
         return a;
     };
     _Float16 *const ma = place(o->off_square[0]), *const mb = place(o->off_square[1]);
-    int blocks = (o->steps + o->block - 1) / o->block;
-    for (int s = 0, n = 0, now = 0; s < o->steps && e == hipSuccess; s += n, now ^= 1, --blocks) {
-        n = (o->steps - s + blocks - 1) / blocks;          // steps of this block: as even as it goes, longer ones first
+    // to <- b A + c A A of step s, and P of a pair's: a I too
+    auto polynomial = [&](int s, bool whole, _Float16* to) {
+        const float* c = o->coefficients[s];
+        ProductArgs p = to_square(to, c[2] * (NS_SCALE_B / (NS_SCALE_A * NS_SCALE_A)));
+        p.old = ma; p.old_matrix = R * tp; p.old_pitch = tp;
+        p.alpha = c[1] * (NS_SCALE_B / NS_SCALE_A);
+        p.diagonal = whole ? c[0] * NS_SCALE_B : 0.0f;
+        return product<NS_POLY, float>(o, squares(ma, ma), p, OF_B, st);
+    };
+    for (int s = 0, n = 0, now = 0; s < o->steps && e == hipSuccess; s += n, now ^= 1) {
+        n = o->pairs && s + 1 < o->steps ? 2 : 1;
         // A = X X^T
         e = product<NS_GRAM, float>(o, Operands{x, x, xl, xl, x_matrix, x_matrix, by_cols}, to_square(ma, NS_SCALE_A / (NS_SCALE_X * NS_SCALE_X)), OF_A, st);
-        // B = b A + c A A and then a X + B X; or, of a block, P = a I + B, and R X
+        // B and then a X + B X; or, of a pair, R and R X
         const _Float16* left_of_x = mb;
-        const bool in_lds = n > 1 && o->rows <= 128;
-        if (in_lds && e == hipSuccess) e = steps_in_lds(o, ma, mb, tp, s, n, st);
-        for (int i = 0; i < n && !in_lds && e == hipSuccess; ++i) {
-            const float* c = o->coefficients[s + i];
-            _Float16* const to = n > 1 && i == 0 ? place(o->off_square[3]) : mb;
-            ProductArgs p = to_square(to, c[2] * (NS_SCALE_B / (NS_SCALE_A * NS_SCALE_A)));
-            p.old = ma; p.old_matrix = R * tp; p.old_pitch = tp;
-            p.alpha = c[1] * (NS_SCALE_B / NS_SCALE_A);
-            p.diagonal = n > 1 ? c[0] * NS_SCALE_B : 0.0f;
-            if ((e = product<NS_POLY, float>(o, squares(ma, ma), p, OF_B, st)) != hipSuccess || n == 1) break;
-            if (i > 0) {                                   // R <- P R
-                _Float16* const r = place(o->off_square[3 + (i & 1)]);
-                if ((e = product<NS_GRAM, float>(o, squares(to, left_of_x), to_square(r, 1.0f / NS_SCALE_B), OF_B, st)) != hipSuccess) break;
-                left_of_x = r;
-            } else {
-                left_of_x = to;
-            }
-            if (i + 1 == n) break;
-            _Float16* const t = place(o->off_square[2]);   // A <- P (P A)
-            if ((e = product<NS_GRAM, float>(o, squares(to, ma), to_square(t, 1.0f / NS_SCALE_B), OF_B, st)) != hipSuccess) break;
-            e = product<NS_GRAM, float>(o, squares(to, t), to_square(ma, 1.0f / NS_SCALE_B), OF_B, st);
+        if (n == 1 && e == hipSuccess) e = polynomial(s, false, mb);
+        if (n == 2 && o->rows <= 128 && e == hipSuccess) e = pair_in_lds(o, ma, mb, tp, s, st);
+        if (n == 2 && o->rows > 128) {
+            _Float16 *const first = place(o->off_square[2]), *const t = place(o->off_square[3]);
+            if (e == hipSuccess) e = polynomial(s, true, first);
+            if (e == hipSuccess) e = product<NS_GRAM, float>(o, squares(first, ma), to_square(t, 1.0f / NS_SCALE_B), OF_B, st);       // A <- P (P A)
+            if (e == hipSuccess) e = product<NS_GRAM, float>(o, squares(first, t), to_square(ma, 1.0f / NS_SCALE_B), OF_B, st);
+            if (e == hipSuccess) e = polynomial(s + 1, true, mb);
+            if (e == hipSuccess) e = product<NS_GRAM, float>(o, squares(mb, first), to_square(t, 1.0f / NS_SCALE_B), OF_B, st);      // R
+            left_of_x = t;
         }
         if (e != hipSuccess) break;
         const Operands of{left_of_x, xt[now], tl, tl, square_matrix, t_matrix, by_rows};

@@ -206,7 +206,7 @@ def test_what_the_workspace_held_does_not_matter(batch, m, n):
 @pytest.mark.parametrize("steps", [1, 2, 3, 4, 6, 7])
 @pytest.mark.parametrize("m,n", [(60, 2000), (2100, 110), (200, 3000)])
 def test_blocks_of_steps(m, n, steps):
-    """A long side: steps are made on the short side's square in blocks of up to three."""
+    """A long side: steps are made on the short side's square in pairs."""
     u = update(1, m, n, F32, seed=steps)[0]
     coefficients = (rb.NEWTON_SCHULZ,) * steps
     got = rb.Orthogonalizer(m, n, coefficients=coefficients).orthogonalize(u)
@@ -214,9 +214,27 @@ def test_blocks_of_steps(m, n, steps):
     assert torch.linalg.vector_norm(got - want) <= ref.orthogonal_bound(coefficients) * torch.linalg.vector_norm(want)
 
 
-def test_blocks_that_would_not_fit_are_not_made():
-    """Three steps that raise small values by more than 60 go one by one."""
-    coefficients = ((4.0, -10.2, 7.1),) * 3                 # 64 at small values, and nowhere beyond 2
+@pytest.mark.parametrize("m,n", [(40, 1000), (621, 63), (128, 8000), (5000, 200)])
+@pytest.mark.parametrize("strong", [1.0, 4.0, 20.0])
+def test_strong_directions_cost_the_weak_ones_no_precision(m, n, strong):
+    """A few directions much stronger than the rest.  Where two steps are made on A, what is rounded in A is carried through P A P: in a weak
+    direction that is a (3.44) times the strong ones' gain, near 1, more than in the plain form in binary32, whose own error is the scale."""
+    rng = np.random.default_rng(m + int(strong))
+    u = rng.standard_normal((m, n)) + 0.5 * strong * rng.standard_normal((m, 8)) @ rng.standard_normal((8, n))
+    u = torch.tensor(u.astype(np.float32), device="cuda")
+    got = rb.Orthogonalizer(m, n, coefficients=FIVE).orthogonalize(u)
+    want, plain = on_the_gpu(u, FIVE, 1e-7), u / torch.linalg.vector_norm(u)
+    plain = plain if m <= n else plain.t().contiguous()
+    for a, b, c in FIVE:
+        s = plain @ plain.t().contiguous()
+        plain = a * plain + (b * s + c * (s @ s)) @ plain
+    plain = plain if m <= n else plain.t()
+    assert torch.linalg.vector_norm(got - want) <= 4.0 * torch.linalg.vector_norm(plain - want)
+
+
+@pytest.mark.parametrize("coefficients", [((4.0, -10.2, 7.1),) * 3, ((19.5, -78.0, 62.4), (5.0, -1.3149, 0.069157))])
+def test_blocks_that_would_not_fit_are_not_made(coefficients):
+    """Steps that raise small values much, by 4 each and by 19.5 and 5: pairs that raise them by more than 60 are not made."""
     u = update(1, 48, 3000, F32, seed=5)[0]
     got = rb.Orthogonalizer(48, 3000, coefficients=coefficients).orthogonalize(u)
     want = on_the_gpu(u, coefficients, 1e-7)
