@@ -144,6 +144,9 @@ def _fits(t, dtype, index, shape):
 _CODES = {torch.float32: RB_F32, torch.bfloat16: RB_BF16}
 
 
+_written = torch.autograd.graph.increment_version       # tells autograd, which may have saved them, of tensors that a call has written
+
+
 class _OnStream:
     """Calls go to the current stream of the handle's device; a call on another stream than the last one's waits for that, since the two
     share the workspace (not under capture: a captured call is ordered by its graph)."""
@@ -226,6 +229,7 @@ class TokenScorer(_OnStream):
         rows, stride = self._rows(logits, "logits")
         if self.given:
             self._given(tokens, rows, torch.int64, "tokens")
+        theirs = out is not None
         if out is None:
             out = self.outputs(rows)
         elif type(out) is not _Outputs or out.scorer is not self or out.rows != rows:
@@ -237,14 +241,20 @@ class TokenScorer(_OnStream):
         if rows == 0:
             return out
         logp, lse, entropy, top_logp, top_ids = out
-        _check(self._on_stream(rb_scorer_score, self.handle, logits, rows, stride, tokens if self.given else None, logp if self.given else None, lse,
-                               entropy, top_logp if self.top else None, top_ids if self.top else None), "rb_scorer_score")
+        if not self.given:
+            tokens = logp = None
+        if not self.top:
+            top_logp = top_ids = None
+        _check(self._on_stream(rb_scorer_score, self.handle, logits, rows, stride, tokens, logp, lse, entropy, top_logp, top_ids), "rb_scorer_score")
+        if theirs:
+            _written([t for t in (logp, lse, entropy, top_logp, top_ids) if t is not None])
         return out
 
     def grad(self, logits, tokens, lse, entropy, grad_logp, grad_entropy=None, out=None):
         """The gradient with respect to the logits, from the derivatives with respect to logp [rows, given] and entropy [rows] (or None).
         out: a tensor shaped as the logits (rows may be strided), which the logits themselves may be."""
         rows, stride = self._rows(logits, "logits")
+        theirs = out is not None
         if out is None:
             out = torch.empty((rows, self.vocab), dtype=self.dtype, device=self.device)
         out_rows, out_stride = self._rows(out, "out")
@@ -264,6 +274,8 @@ class TokenScorer(_OnStream):
             return out
         _check(self._on_stream(rb_scorer_grad, self.handle, logits, rows, stride, tokens, lse, entropy, grad_logp, grad_entropy, out, out_stride),
                "rb_scorer_grad")
+        if theirs:
+            _written(out)
         return out
 
     def __call__(self, logits, tokens=None):
@@ -333,10 +345,13 @@ class Orthogonalizer(_OnStream):
 
     def orthogonalize(self, update, out=None):
         a = self._strides(update, self.dtype)
+        theirs = out is not None
         if out is None:
             out = torch.empty(update.shape, dtype=self.out_dtype, device=self.device)
         b = self._strides(out, self.out_dtype)
         _check(self._on_stream(rb_ortho_apply, self.handle, update, *a, out, *b), "rb_ortho_apply")
+        if theirs:
+            _written(out)
         return out
 
     def step(self, weight, grad, momentum, lr, beta=0.95, nesterov=True, weight_decay=0.0, scale=None):
@@ -347,7 +362,7 @@ class Orthogonalizer(_OnStream):
         if scale is None:
             scale = math.sqrt(max(1.0, self.m / self.n))
         _check(self._on_stream(rb_ortho_step, self.handle, weight, *w, grad, *g, momentum, lr, beta, nesterov, weight_decay, scale), "rb_ortho_step")
-        torch.autograd.graph.increment_version((weight, momentum))      # (autograd tells of tensors it has saved that were changed since)
+        _written((weight, momentum))
 
     def close(self):
         if getattr(self, "handle", None):
