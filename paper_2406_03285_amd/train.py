@@ -149,7 +149,8 @@ _written = torch.autograd.graph.increment_version       # tells autograd, which 
 
 class _OnStream:
     """Calls go to the current stream of the handle's device; a call on another stream than the last one's waits for that, since the two
-    share the workspace (not under capture: a captured call is ordered by its graph)."""
+    share the workspace (not under capture: a captured call is ordered by its graph).  The allocator is told of every stream that the workspace was
+    used on, so that it is not another tensor's before these are done with it."""
 
     def _bind_device(self, device):
         self.device = torch.device(device)
@@ -165,6 +166,7 @@ class _OnStream:
             stream = torch.cuda.current_stream(self.device)
             if not torch.cuda.is_current_stream_capturing():
                 stream.wait_stream(self._last)
+            self.workspace.record_stream(stream)
             self._last, self._last_address = stream, address
         if torch.cuda.current_device() == self._index:
             return call(*args, address)

@@ -76,3 +76,61 @@ def test_backward_refuses_logits_that_a_call_has_overwritten():
     s.grad(z.detach(), torch.zeros((5, 1), dtype=torch.int64), row, row, torch.zeros((5, 1)), row, out=z.detach())
     with pytest.raises(RuntimeError, match="modified by an inplace operation"):
         y.backward()
+
+
+# ---- streams -------------------------------------------------------------------
+
+class Stream:
+    """A stream of a device that keeps what it was told to wait for."""
+
+    def __init__(self, address):
+        self.cuda_stream, self.waited = address, []
+
+    def wait_stream(self, other):
+        self.waited.append(other)
+
+
+class Workspace:
+    def __init__(self):
+        self.used_on = []
+
+    def record_stream(self, stream):
+        self.used_on.append(stream)
+
+
+class Device:
+    """The current stream, and whether it is being captured into a graph."""
+
+    def __init__(self, monkeypatch):
+        self.stream, self.capturing = Stream(0), False
+        monkeypatch.undo()                               # (the calls go through _on_stream here)
+        monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+        monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: self.stream)
+        monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: self.capturing)
+        monkeypatch.setattr(train, "_current_stream", lambda index: self.stream.cuda_stream)
+
+    def handle(self):
+        h = train._OnStream()
+        h._bind_device("cuda:0")
+        h.workspace = Workspace()
+        return h
+
+    def call(self, h, stream, capturing=False):
+        self.stream, self.capturing = stream, capturing
+        assert h._on_stream(lambda *args: args, 1, 2) == (1, 2, stream.cuda_stream)
+
+
+def test_the_workspace_is_kept_for_every_stream_that_it_was_used_on(monkeypatch):
+    """It was allocated on the handle's first stream: given back with the handle, it may be that stream's next tensor while another stream's
+    kernels still use it, unless the allocator knows of these."""
+    d = Device(monkeypatch)
+    a, b, c = d.stream, Stream(7), Stream(9)
+    h = d.handle()
+    d.call(h, a)
+    assert h.workspace.used_on == []
+    d.call(h, b)
+    d.call(h, b)
+    d.call(h, c)
+    d.call(h, a)
+    assert h.workspace.used_on[:2] == [b, c]
+    assert b.waited == [a] and c.waited == [b] and a.waited == [c]
