@@ -149,8 +149,9 @@ _written = torch.autograd.graph.increment_version       # tells autograd, which 
 
 class _OnStream:
     """Calls go to the current stream of the handle's device; a call on another stream than the last one's waits for that, since the two
-    share the workspace (not under capture: a captured call is ordered by its graph).  The allocator is told of every stream that the workspace was
-    used on, so that it is not another tensor's before these are done with it."""
+    share the workspace.  The allocator is told of every stream that the workspace was used on, so that it is not another tensor's before these are
+    done with it.  A captured call is ordered by its graph: whoever replays it orders the replays and the handle's other calls, and keeps the
+    handle as long as the graph."""
 
     def _bind_device(self, device):
         self.device = torch.device(device)
@@ -162,10 +163,9 @@ class _OnStream:
 
     def _on_stream(self, call, *args):
         address = _current_stream(self._index)
-        if address != self._last_address:
+        if address != self._last_address and not torch.cuda.is_current_stream_capturing():
             stream = torch.cuda.current_stream(self.device)
-            if not torch.cuda.is_current_stream_capturing():
-                stream.wait_stream(self._last)
+            stream.wait_stream(self._last)
             self.workspace.record_stream(stream)
             self._last, self._last_address = stream, address
         if torch.cuda.current_device() == self._index:

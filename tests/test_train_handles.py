@@ -59,3 +59,25 @@ def test_calls_on_streams_in_turn_and_a_handle_that_is_dropped_behind_them():
     for k in range(3):
         assert torch.equal(out[k], want[k])
         assert all(torch.equal(a, b) for a, b in zip(outs[k], wanted[k]))
+
+
+def test_calls_before_and_behind_a_capture():
+    """A call on a stream, a capture, a call on a third stream: the third's waits for the first's."""
+    o = rb.Orthogonalizer(700, 900)
+    u = [torch.randn((700, 900), generator=torch.Generator("cuda").manual_seed(k), device="cuda") for k in range(2)]
+    want = [o.orthogonalize(x) for x in u]
+    out, captured = [torch.empty_like(x) for x in want], torch.empty_like(want[0])
+    one, two = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        o.orthogonalize(u[0], out=captured)
+    for _ in range(3):
+        with torch.cuda.stream(one):
+            o.orthogonalize(u[0], out=out[0])
+        with torch.cuda.stream(two):
+            o.orthogonalize(u[1], out=out[1])
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out[0], want[0]) and torch.equal(out[1], want[1]) and torch.equal(captured, want[0])

@@ -134,3 +134,18 @@ def test_the_workspace_is_kept_for_every_stream_that_it_was_used_on(monkeypatch)
     d.call(h, a)
     assert h.workspace.used_on[:2] == [b, c]
     assert b.waited == [a] and c.waited == [b] and a.waited == [c]
+
+
+def test_a_captured_call_does_not_make_the_handle_forget_the_stream_before(monkeypatch):
+    """Eager work on b, then a capture, then eager work on c: that has to wait for b's, which the capture's stream knows nothing of."""
+    d = Device(monkeypatch)
+    a, b, c, capture = d.stream, Stream(7), Stream(9), Stream(11)
+    h = d.handle()
+    d.call(h, b)
+    d.call(h, capture, capturing=True)
+    assert capture.waited == [] and capture not in h.workspace.used_on
+    d.call(h, c)
+    assert c.waited == [b]
+    d.call(h, capture, capturing=True)
+    d.call(h, c)
+    assert c.waited == [b]
