@@ -184,7 +184,8 @@ class Scores(NamedTuple):
 
 
 class _Outputs(Scores):
-    """Scores' tensors that TokenScorer.outputs has made: `scorer` and `rows` say for what."""
+    """Scores' tensors that TokenScorer.outputs has made: `scorer` and `rows` say for what (of one that was changed since: for none)."""
+    scorer = rows = None
 
 
 class TokenScorer(_OnStream):

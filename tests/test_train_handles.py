@@ -61,8 +61,8 @@ def test_calls_on_streams_in_turn_and_a_handle_that_is_dropped_behind_them():
         assert all(torch.equal(a, b) for a, b in zip(outs[k], wanted[k]))
 
 
-def test_calls_before_and_behind_a_capture():
-    """A call on a stream, a capture, a call on a third stream: the third's waits for the first's."""
+def test_calls_on_streams_in_turn_behind_a_capture():
+    """Calls on two streams in turn behind a capture, and replays between them."""
     o = rb.Orthogonalizer(700, 900)
     u = [torch.randn((700, 900), generator=torch.Generator("cuda").manual_seed(k), device="cuda") for k in range(2)]
     want = [o.orthogonalize(x) for x in u]

@@ -149,3 +149,21 @@ def test_a_captured_call_does_not_make_the_handle_forget_the_stream_before(monke
     d.call(h, capture, capturing=True)
     d.call(h, c)
     assert c.waited == [b]
+
+
+# ---- what is given as out ------------------------------------------------------
+
+def test_outputs_of_which_some_are_left_out_or_exchanged():
+    s = scorer_of(11, 1, 2)
+    z, t = torch.zeros((5, 11)), torch.zeros((5, 1), dtype=torch.int64)
+    lse = torch.zeros(5)
+    out = s.outputs(5)._replace(lse=lse, entropy=None)
+    assert s.score(z, t, out=out) is out
+    assert CALLED[-1][5:9] == (out.logp, lse, None, out.top_logp)
+    for wrong in (dict(lse=torch.zeros(6)), dict(logp=torch.zeros((5, 1), dtype=torch.float64)), dict(top_ids=torch.zeros((5, 2)))):
+        with pytest.raises(AssertionError, match="out"):
+            s.score(z, t, out=s.outputs(5)._replace(**wrong))
+    with pytest.raises(AssertionError, match="out"):
+        s.score(z, t, out=s.outputs(4))
+    with pytest.raises(AssertionError, match="out"):
+        s.score(z, t, out=scorer_of(11, 2, 2).outputs(5))
