@@ -165,3 +165,32 @@ def test_what_is_not_a_number_is_in_all_of_its_matrix_and_in_no_other(m, n, valu
     u[1, m // 2, n - 1] = value
     got = o.orthogonalize(u)
     assert torch.isnan(got[1]).all() and torch.equal(got[0], want[0]) and torch.equal(got[2], want[2])
+
+
+# ---- pairs of steps of other coefficients --------------------------------------
+
+MADE, NOT_MADE = ((4.0, -10.2, 7.1),) * 3, ((19.5, -78.0, 62.4), (5.0, -1.3149, 0.069157))
+
+
+def workspace(coefficients, m=200, n=3000):
+    rc, o = rb.rb_ortho_create(1, m, n, rb.RB_F32, rb.RB_F32, coefficients, 0.0)
+    assert rc == rb.RB_OK
+    rc, size = rb.rb_ortho_query(o)
+    rb.rb_ortho_destroy(o)
+    return size
+
+
+def test_which_pairs_are_made():
+    """A pair wants room for two more squares.  4 * 4 = 16 is kept, 19.5 * 5 = 97.5 would be beyond what a square's scale leaves (60)."""
+    one = workspace(FIVE[:1])
+    assert workspace(FIVE) > one and workspace(MADE) > one
+    assert workspace(NOT_MADE) == one
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("m,n", [(48, 3000), (200, 3000), (3000, 110)])
+@pytest.mark.parametrize("coefficients", [MADE, NOT_MADE])
+def test_steep_steps_are_as_near_as_those_of_binary32(m, n, coefficients):
+    u = updates(1, m, n)[0]
+    off, plain = errors(rb.Orthogonalizer(m, n, coefficients=coefficients).orthogonalize(u), u, coefficients)
+    assert off <= 4.0 * plain, off / plain
