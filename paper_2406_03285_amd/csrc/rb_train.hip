@@ -115,9 +115,13 @@ int rb_scorer_score(rb_scorer* s, const void* logits, int64_t rows, int64_t row_
     a.vocab = s->vocab;
     a.given = s->given;
     a.top = s->top;
-    // Wavefronts per row: one tile is a wavefront's.  Rows that fill the chip get few, since each has a list of its own to sort and join (2048
-    // rows of 50001 with 16 alternatives: 63 us with one, 51 with two, 58 with four), and four when they are long.  Fewer rows get 16.
-    const int waves = tiles == 1 || (tiles <= 8 && rows >= 4096) ? 1 : tiles <= 32 && rows >= 2048 ? 2 : rows >= 512 || tiles <= SC_NWAVE ? SC_NWAVE : SC_MANY_WAVES;
+    // Wavefronts per row: one tile is a wavefront's.  Rows that fill the chip get few, since each has a list of its own to sort and join, and four when
+    // they are long.  Two where there are more rows than 7 workgroups of four on each of 256 compute units (bfloat16, 50001 with 16 alternatives, two
+    // and four: 1700 rows 48.6 and 47.8 us, 1750 48.3 and 48.2, 1800 48.1 and 50.2, 2500 57.5 and 62.4; of 10000 1800 rows 18.8 and 22.4; without
+    // alternatives 50001 1750 33.4 and 31.9, 1900 34.8 and 34.9).  Binary32 rows are twice the bytes, which long ones wait for rather than for lists (1800
+    // rows of 10000 with 16 21.0 and 23.6, of 20000 32.1 and 33.3, of 30001 43.3 and 41.5; 3000 of 65000 152 and 144).  Fewer rows get 16.
+    const bool two = rows > 7 * 256 && tiles <= (s->dtype == RB_BF16 ? 32 : 12);
+    const int waves = tiles == 1 || (tiles <= 8 && rows >= 4096) ? 1 : two ? 2 : rows >= 512 || tiles <= SC_NWAVE ? SC_NWAVE : SC_MANY_WAVES;
     // Rows shared by workgroups: what the last one waits for (the others' parts have to reach memory) costs more with every workgroup, so the
     // more rows, the more tiles for each wavefront: one, two, and four from 33 rows (bfloat16, 20 alternatives, unshared and shared: one row
     // of 131072 20.0 and 13.2 us, 16 rows of 131072 20.7 and 18.0, 64 rows of 262144 34.5 and 26.3; at two tiles each 64 rows of 131072
