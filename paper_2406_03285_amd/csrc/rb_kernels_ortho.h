@@ -2,8 +2,8 @@
 //
 // X = G / (|G| + eps), short side first; per step A = X X^T, B = b A + c A A, X <- a X + B X.  The iteration multiplies a small singular
 // value by a (3.4 in the usual coefficients) in every step, and a rounding error in its direction as well: by 140 in four steps.  Operands
-// rounded to one 16-bit number would leave errors of per cents; so an operand is kept as the sum of two binary16 numbers (hi + lo, 22
-// bits), a product is three matrix instructions (hi hi + hi lo + lo hi; lo lo is below the last bit), and sums are binary32.
+// rounded to one 16-bit number would leave errors of per cents; so an operand is kept as the sum of two binary16 numbers (hi + lo: 22
+// bits, as far as binary16's range goes), a product is three matrix instructions (hi hi + hi lo + lo hi; lo lo is below the last bit), and sums are binary32.
 //
 // Where one side is much the longer one, most of the work is in the two products with X.  Then steps are made in pairs on A alone: a step
 // multiplies X from the left by P = a I + b A + c A A, and A, a polynomial of the same symmetric matrix, by P twice; R, the product of the
@@ -36,8 +36,8 @@ constexpr int NS_KBLOCK = 32;                  // elements of a block: hi, then 
 constexpr int NS_KHALVES = 2 * NS_KBLOCK;
 constexpr int NS_ROWS_AT_ONCE = 4;             // rows a thread of the first pass has on their way
 constexpr int NS_PARTS = 1024;                 // most partial sums of a norm per matrix
-// What is kept is scaled by powers of two, so that lo is a normal binary16 number for elements of the size that occurs, and a singular
-// value of 4 (A: 16, B: 60) is still below 65504.
+// What is kept is scaled by powers of two so that a singular value of 4 (A: 16, B: 60) is still below 65504.  lo is a normal binary16 number, and the sum
+// has its 22 bits, for elements of X from 2^-14 on (of 4096 x 4096 a typical one is 2^-12); below, it goes in steps of 2^-24 over the scale.
 constexpr float NS_SCALE_X = 4096.0f, NS_SCALE_A = 2048.0f, NS_SCALE_B = 1024.0f;
 
 template <typename H, int N>      // of N neighbours, a vector of N binary16 numbers each (conversions go in pairs)

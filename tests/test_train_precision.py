@@ -194,3 +194,19 @@ def test_steep_steps_are_as_near_as_those_of_binary32(m, n, coefficients):
     u = updates(1, m, n)[0]
     off, plain = errors(rb.Orthogonalizer(m, n, coefficients=coefficients).orthogonalize(u), u, coefficients)
     assert off <= 4.0 * plain, off / plain
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("m,n", [(100, 100), (256, 256), (1500, 200), (1000, 1100)])
+@pytest.mark.parametrize("norm", [1.0, 1e-7, 1e-9, 1e-11])
+def test_updates_smaller_than_eps(m, n, norm):
+    """X is G / (|G| + eps), and its steps are those of |G| + eps: a small update is like small rows of a larger one."""
+    u = updates(1, m, n)[0]
+    u *= norm / torch.linalg.vector_norm(u)
+    got = rb.Orthogonalizer(m, n, coefficients=FIVE, eps=1e-7).orthogonalize(u).double()
+    want = iteration(u, torch.float64, FIVE)
+    size = torch.linalg.vector_norm(want, dim=1)
+    off = torch.linalg.vector_norm(got - want, dim=1) / size
+    plain = (torch.linalg.vector_norm(iteration(u, torch.float32, FIVE) - want, dim=1) / size).max()
+    r = torch.linalg.vector_norm(u.double(), dim=1) / (torch.linalg.vector_norm(u.double()) + 1e-7)
+    assert (off <= 4.0 * plain + 2.0 ** -36 * (n ** 0.5 + 64) / r).all()
