@@ -8,7 +8,9 @@
 // Alternatives.  A wavefront keeps its best 64 elements so far as one 64-bit key per lane, sorted: the logit in an order-preserving 32-bit
 // form above the inverted index, so that equal logits order by index and no two keys are equal.  A lane whose tile holds nothing above the
 // smallest key that still counts (which the running maximum tells at no cost) goes on; the others put their tile into LDS, half a wavefront
-// looks at one of them at a time, what passes is queued, and a full queue is sorted and merged into the list.
+// looks at one of them at a time, what passes is queued, and a full queue is sorted and merged into the list.  So the time depends on the order of
+// the logits: of rows that rise along their indices all pass (20 from end to end; 2048 x 50001 bfloat16 with 16: 114 us; one row of 32000 with 20: 15.8
+// for 10.1; 5120 x 10000 binary32 with 5: 43); falling or equal ones take less than random ones (40 and 43 for 2048 x 50001).
 #pragma once
 
 #include <hip/hip_runtime.h>

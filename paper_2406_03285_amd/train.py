@@ -194,6 +194,7 @@ class TokenScorer(_OnStream):
     scorer = TokenScorer(vocab, torch.bfloat16, given=1, top=8)
     s = scorer.score(logits, tokens)                # Scores; logits [rows, vocab], rows may be strided; tokens [rows, given] (or [rows])
     s = scorer(logits, tokens)                      # the same within autograd: s.logp and s.entropy carry gradients
+                                                    # (s.lse, s.top_logp and s.top_ids carry none: what a loss adds of them changes no gradient)
     """
 
     def __init__(self, vocab, dtype=torch.float32, given=1, top=0, device="cuda"):
@@ -255,7 +256,8 @@ class TokenScorer(_OnStream):
 
     def grad(self, logits, tokens, lse, entropy, grad_logp, grad_entropy=None, out=None):
         """The gradient with respect to the logits, from the derivatives with respect to logp [rows, given] and entropy [rows] (or None).
-        out: a tensor shaped as the logits (rows may be strided), which the logits themselves may be."""
+        out: a tensor shaped as the logits (rows may be strided), which the logits themselves may be.  Without it the rows lie behind each other, as in
+        backward: where those of the logits lie otherwise relative to 16 bytes, a tensor laid out like the logits is written faster."""
         rows, stride = self._rows(logits, "logits")
         theirs = out is not None
         if out is None:
