@@ -3,6 +3,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 #include <cstdint>
 #include <new>
@@ -201,7 +202,7 @@ namespace {
 template <auto kernel>
 hipError_t allow_lds(size_t bytes)
 {
-    static bool allowed[64] = {};
+    static std::atomic<bool> allowed[64] = {};      // (handles of several host threads)
     int dev = 0;
     if (bytes <= 65536) return hipSuccess;
     if (hipGetDevice(&dev) != hipSuccess) return hipErrorInvalidDevice;
