@@ -1,4 +1,4 @@
-"""Compile the HIP libraries (csrc/rb.hip -> librb.so, csrc/rb_train.hip -> librb_train.so, gfx950 only) in-tree with hipcc."""
+"""Compile the HIP libraries (csrc/rb.hip -> librb.so, rb_train.hip -> librb_train.so, rb_block.hip -> librb_block.so, gfx950 only) in-tree with hipcc."""
 import os
 import subprocess
 import sysconfig
@@ -10,6 +10,8 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(HERE, "librb.so")
 TRAIN_SRC = os.path.join(HERE, "csrc", "rb_train.hip")
 TRAIN_LIB = os.path.join(HERE, "librb_train.so")
+BLOCK_SRC = os.path.join(HERE, "csrc", "rb_block.hip")
+BLOCK_LIB = os.path.join(HERE, "librb_block.so")
 
 HIPCC_FLAGS = [
     "-O3", "-std=c++17", "--offload-arch=gfx950", "-shared", "-fPIC",
@@ -59,7 +61,7 @@ def start_library(src: str, lib: str, verbose: bool = False) -> subprocess.Popen
 
 
 def build(verbose: bool = False) -> str:
-    compilers = [start_library(SRC, LIB, verbose), start_library(TRAIN_SRC, TRAIN_LIB, verbose)]      # side by side
+    compilers = [start_library(src, lib, verbose) for src, lib in ((SRC, LIB), (TRAIN_SRC, TRAIN_LIB), (BLOCK_SRC, BLOCK_LIB))]      # side by side
     for compiler, status in [(c, c.wait()) for c in compilers]:
         if status != 0:
             raise subprocess.CalledProcessError(status, compiler.args)

@@ -1,0 +1,421 @@
+// What a block of a model computes between its matrix products, for gfx950 (MI355X): the C ABI of include/rb_block.h (host side); the kernels are
+// in rb_kernels_norm.h (dropout, layer norm) and rb_kernels_attention.h (attention of packed documents).
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstdint>
+#include <new>
+
+#include "rb_host.h"
+#include "rb_kernels_norm.h"
+#include "rb_kernels_attention.h"
+#include "rb_block.h"
+
+namespace {
+
+constexpr int64_t MAX_STRIDE = int64_t(1) << 36;       // of rows and positions, in elements: no offset passes 64 bits
+inline bool known(int32_t dtype) { return dtype == RB_F32 || dtype == RB_BF16; }
+inline int64_t elem_bytes(int32_t dtype) { return dtype == RB_F32 ? 4 : 2; }
+
+bool drop_of(const rb_drop* d, Drop& to)
+{
+    to = Drop{};
+    if (!d) return true;
+    if (!(d->p >= 0.0 && d->p <= 1.0)) return false;
+    to.seed_lo = (uint32_t)d->seed;
+    to.seed_hi = (uint32_t)(d->seed >> 32);
+    to.step_lo = (uint32_t)d->step;
+    to.step_hi = (uint32_t)(d->step >> 32);
+    to.least = (uint32_t)std::nearbyint(d->p * 65536.0);
+    to.scale = to.least == 65536 ? 0.0f : (float)(65536.0 / (65536.0 - to.least));
+    return true;
+}
+
+}  // namespace
+
+// ---- dropout ---------------------------------------------------------------------
+extern "C" int rb_dropout(const void* x, int64_t x_stride, int64_t rows, int64_t width, int32_t dtype, const rb_drop* drop, void* out, int64_t out_stride,
+                          void* hip_stream)
+{
+    DropoutArgs a{};
+    if (!x || !out || !drop || !known(dtype) || rows < 0 || rows > RB_MAX_NORM_ROWS || width < 1 || width > RB_MAX_DROP_WIDTH) return RB_EINVAL;
+    if (!aligned(x, (size_t)elem_bytes(dtype)) || !aligned(out, (size_t)elem_bytes(dtype))) return RB_EINVAL;
+    if (x_stride < width || out_stride < width || x_stride > MAX_STRIDE || out_stride > MAX_STRIDE || !drop_of(drop, a.drop)) return RB_EINVAL;
+    if (x == out && x_stride != out_stride && rows > 1) return RB_EINVAL;
+    if (rows == 0) return RB_OK;
+    a.x = x;
+    a.out = out;
+    a.x_stride = x_stride;
+    a.out_stride = out_stride;
+    a.rows = (int32_t)rows;
+    a.width = (int32_t)width;
+    a.pieces = (int32_t)((width + NM_PIECE - 1) / NM_PIECE);
+    a.at_once = std::max(1, NM_TPB / a.pieces);
+    a.blocks = (a.pieces + NM_TPB - 1) / NM_TPB;
+    a.items = (rows + a.at_once - 1) / a.at_once * a.blocks;
+    const dim3 grid((unsigned)std::min<int64_t>(a.items, 1 << 20));
+    hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    const hipError_t e = dtype == RB_F32 ? launch(rb_dropout_kernel<float>, grid, NM_TPB, 0, st, a) : launch(rb_dropout_kernel<Bf16>, grid, NM_TPB, 0, st, a);
+    return e == hipSuccess ? RB_OK : RB_EHIP;
+}
+
+// ---- layer norm ------------------------------------------------------------------
+struct rb_norm {
+    int32_t width, dtype, weight_dtype;
+    float eps;
+    float* sums;       // workspace
+};
+
+namespace {
+
+constexpr int64_t NM_FUSED_WIDTH = 8192;       // longest rows whose sums over rows stay in registers beside them
+
+inline bool rows_fit(const rb_norm* n, const rb_rows* r)
+{
+    return r && r->data && aligned(r->data, (size_t)elem_bytes(n->dtype)) && r->stride >= n->width && r->stride <= MAX_STRIDE;
+}
+// what is written in place has to lie as what is read
+inline bool apart_or_alike(const rb_rows* a, const rb_rows* b, int64_t rows) { return !a || !b || !a->data || a->data != b->data || a->stride == b->stride || rows <= 1; }
+
+// Workgroups of a grid that goes through `rows` rows, `at_once` each: enough to fill the chip `per_unit` times.
+inline unsigned norm_groups(int64_t rows, int at_once, int per_unit)
+{
+    return (unsigned)std::min<int64_t>((rows + at_once - 1) / at_once, 256 * per_unit);
+}
+
+template <typename T, int LANES, int PARTS>
+hipError_t norm_forward(const NormArgs& a, hipStream_t st)
+{
+    constexpr int TPB = std::max(LANES, NM_TPB);
+    return launch(rb_norm_kernel<T, LANES, PARTS>, dim3(norm_groups(a.rows, TPB / LANES, 8)), TPB, 0, st, a);
+}
+
+template <typename T, int LANES, int PARTS>
+hipError_t norm_grad(const NormGradArgs& a, unsigned groups, hipStream_t st)
+{
+    constexpr int TPB = std::max(LANES, NM_TPB);
+    if constexpr (LANES * PARTS * NM_PIECE <= NM_FUSED_WIDTH) {
+        if (a.sums) return launch(rb_norm_grad_kernel<T, LANES, PARTS, true>, dim3(groups), TPB, 0, st, a);
+    }
+    return launch(rb_norm_grad_kernel<T, LANES, PARTS, false>, dim3(norm_groups(a.rows, TPB / LANES, 8)), TPB, 0, st, a);
+}
+
+// Lanes of a row and pieces of a lane, by the row's length: `of` is called with both.
+template <typename Of>
+hipError_t by_width(int32_t width, const Of& of)
+{
+    if (width <= 128) return of(std::integral_constant<int, 16>(), std::integral_constant<int, 1>());
+    if (width <= 512) return of(std::integral_constant<int, 64>(), std::integral_constant<int, 1>());
+    if (width <= 1024) return of(std::integral_constant<int, 64>(), std::integral_constant<int, 2>());
+    if (width <= 2048) return of(std::integral_constant<int, 64>(), std::integral_constant<int, 4>());
+    if (width <= 4096) return of(std::integral_constant<int, 256>(), std::integral_constant<int, 2>());
+    if (width <= 8192) return of(std::integral_constant<int, 256>(), std::integral_constant<int, 4>());
+    if (width <= 32768) return of(std::integral_constant<int, 1024>(), std::integral_constant<int, 4>());
+    return of(std::integral_constant<int, 1024>(), std::integral_constant<int, 8>());
+}
+inline int rows_at_once(int32_t width) { return width <= 128 ? NM_TPB / 16 : width <= 2048 ? NM_TPB / 64 : 1; }
+
+}  // namespace
+
+extern "C" {
+
+int rb_norm_create(rb_norm** out, int64_t width, int32_t dtype, int32_t weight_dtype, float eps)
+{
+    if (!out) return RB_EINVAL;
+    *out = nullptr;
+    if (width < 1 || width > RB_MAX_NORM_WIDTH || !known(dtype) || !known(weight_dtype) || !std::isfinite(eps) || !(eps > 0.0f)) return RB_EINVAL;
+    rb_norm* n = new (std::nothrow) rb_norm();
+    if (!n) return RB_ENOMEM;
+    n->width = (int32_t)width;
+    n->dtype = dtype;
+    n->weight_dtype = weight_dtype;
+    n->eps = eps;
+    *out = n;
+    return RB_OK;
+}
+
+int rb_norm_query(const rb_norm* n, size_t* workspace_bytes)
+{
+    if (!n || !workspace_bytes) return RB_EINVAL;
+    *workspace_bytes = (size_t)2 * NM_MAX_GROUPS * n->width * sizeof(float);
+    return RB_OK;
+}
+
+int rb_norm_bind(rb_norm* n, void* workspace)
+{
+    if (!n || !workspace || !aligned(workspace, 256)) return RB_EINVAL;
+    n->sums = static_cast<float*>(workspace);
+    return RB_OK;
+}
+
+int rb_norm_forward(rb_norm* n, const rb_rows* x, const rb_rows* residual, const rb_drop* drop, int64_t rows, const void* weight, const void* bias,
+                    const rb_rows* total, const rb_rows* y, float* mean, float* rstd, void* hip_stream)
+{
+    if (!n || rows < 0 || rows > RB_MAX_NORM_ROWS || !rows_fit(n, x) || !rows_fit(n, y) || (residual && !rows_fit(n, residual))) return RB_EINVAL;
+    const bool sum = residual || drop;
+    if (sum != (total && total->data) || (sum && !rows_fit(n, total))) return RB_EINVAL;
+    const size_t size = (size_t)elem_bytes(n->weight_dtype);
+    if (!weight || !aligned(weight, size) || !aligned(bias, size) || !aligned(mean, 4) || !aligned(rstd, 4)) return RB_EINVAL;
+    if (!apart_or_alike(y, x, rows) || (sum && (total->data == y->data || !apart_or_alike(total, x, rows) || !apart_or_alike(total, residual, rows)))) return RB_EINVAL;
+    if (residual && y->data == residual->data && rows > 0) return RB_EINVAL;
+    NormArgs a{};
+    if (!drop_of(drop, a.drop)) return RB_EINVAL;
+    if (rows == 0) return RB_OK;
+    a.x = x->data;
+    a.x_stride = x->stride;
+    if (residual) {
+        a.residual = residual->data;
+        a.residual_stride = residual->stride;
+    }
+    if (sum) {
+        a.total = total->data;
+        a.total_stride = total->stride;
+    }
+    a.y = y->data;
+    a.y_stride = y->stride;
+    a.weight = weight;
+    a.bias = bias;
+    a.mean = mean;
+    a.rstd = rstd;
+    a.rows = (int32_t)rows;
+    a.width = n->width;
+    a.eps = n->eps;
+    a.wide_weights = n->weight_dtype == RB_F32;
+    a.drops = drop != nullptr;
+    hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    const hipError_t e = by_width(n->width, [&](auto lanes, auto parts) {
+        return n->dtype == RB_F32 ? norm_forward<float, lanes(), parts()>(a, st) : norm_forward<Bf16, lanes(), parts()>(a, st);
+    });
+    return e == hipSuccess ? RB_OK : RB_EHIP;
+}
+
+int rb_norm_grad(rb_norm* n, const rb_rows* grad_y, const rb_rows* total, const rb_rows* grad_total, const float* mean, const float* rstd, const rb_drop* drop,
+                 int64_t rows, const void* weight, const rb_rows* grad_sum, const rb_rows* grad_x, void* grad_weight, void* grad_bias, void* hip_stream)
+{
+    if (!n || rows < 0 || rows > RB_MAX_NORM_ROWS || !rows_fit(n, grad_y) || !rows_fit(n, total) || !rows_fit(n, grad_sum)) return RB_EINVAL;
+    if ((grad_total && !rows_fit(n, grad_total)) || (drop != nullptr) != (grad_x && grad_x->data) || (drop && !rows_fit(n, grad_x))) return RB_EINVAL;
+    const size_t size = (size_t)elem_bytes(n->weight_dtype);
+    if (!mean || !rstd || !weight || !aligned(mean, 4) || !aligned(rstd, 4) || !aligned(weight, size) || !aligned(grad_weight, size) || !aligned(grad_bias, size))
+        return RB_EINVAL;
+    if (!apart_or_alike(grad_sum, grad_y, rows) || !apart_or_alike(grad_sum, grad_total, rows) || grad_sum->data == total->data) return RB_EINVAL;
+    if (drop && (grad_x->data == grad_sum->data || grad_x->data == total->data || !apart_or_alike(grad_x, grad_y, rows) || !apart_or_alike(grad_x, grad_total, rows)))
+        return RB_EINVAL;
+    NormGradArgs a{};
+    if (!drop_of(drop, a.drop)) return RB_EINVAL;
+    const bool wanted = grad_weight || grad_bias;
+    if (wanted && !n->sums) return RB_ESTATE;
+    a.grad_y = grad_y->data;
+    a.grad_y_stride = grad_y->stride;
+    a.total = total->data;
+    a.total_stride = total->stride;
+    if (grad_total) {
+        a.grad_total = grad_total->data;
+        a.grad_total_stride = grad_total->stride;
+    }
+    a.grad_sum = grad_sum->data;
+    a.grad_sum_stride = grad_sum->stride;
+    if (drop) {
+        a.grad_x = grad_x->data;
+        a.grad_x_stride = grad_x->stride;
+    }
+    a.weight = weight;
+    a.mean = mean;
+    a.rstd = rstd;
+    a.sums = wanted ? n->sums : nullptr;
+    a.rows = (int32_t)rows;
+    a.width = n->width;
+    a.wide_weights = n->weight_dtype == RB_F32;
+    a.drops = drop != nullptr;
+    hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    hipError_t e = hipSuccess;
+    unsigned groups = norm_groups(rows, rows_at_once(n->width), NM_MAX_GROUPS / 256);
+    if (wanted && n->width > NM_FUSED_WIDTH) {       // (before grad_y may be overwritten)
+        const dim3 grid(groups, (unsigned)(n->width + NM_TPB * NM_PIECE - 1) / (NM_TPB * NM_PIECE));
+        if (rows > 0) e = n->dtype == RB_F32 ? launch(rb_norm_columns_kernel<float>, grid, NM_TPB, 0, st, a) : launch(rb_norm_columns_kernel<Bf16>, grid, NM_TPB, 0, st, a);
+    }
+    if (e == hipSuccess && rows > 0)
+        e = by_width(n->width, [&](auto lanes, auto parts) {
+            return n->dtype == RB_F32 ? norm_grad<float, lanes(), parts()>(a, groups, st) : norm_grad<Bf16, lanes(), parts()>(a, groups, st);
+        });
+    if (e == hipSuccess && wanted) {
+        const dim3 grid((unsigned)(n->width + 63) / 64, 2);
+        e = n->weight_dtype == RB_F32
+                ? launch(rb_norm_join_kernel<float>, grid, 1024, 0, st, n->sums, (int)groups, (int)n->width, static_cast<float*>(grad_weight), static_cast<float*>(grad_bias))
+                : launch(rb_norm_join_kernel<Bf16>, grid, 1024, 0, st, n->sums, (int)groups, (int)n->width, static_cast<Bf16*>(grad_weight), static_cast<Bf16*>(grad_bias));
+    }
+    return e == hipSuccess ? RB_OK : RB_EHIP;
+}
+
+int rb_norm_destroy(rb_norm* n)
+{
+    delete n;
+    return RB_OK;
+}
+
+}  // extern "C"
+
+// ---- attention of packed documents -----------------------------------------------
+struct rb_attention {
+    int32_t heads, kv_heads, dim, max_tokens;
+    bool causal;
+    ScoreOf score;
+    bool cap;
+    size_t off_lse2, off_delta, bytes;
+    char* ws;
+};
+
+namespace {
+
+bool heads_fit(const rb_attention* a, const rb_heads* t, bool written)
+{
+    if (!t || !t->data || !aligned(t->data, 16) || t->token_stride % 8 != 0 || t->head_stride % 8 != 0) return false;
+    if (t->token_stride < 0 || t->head_stride < 0 || t->token_stride > MAX_STRIDE || t->head_stride > (int64_t(1) << 48)) return false;
+    return !written || (t->token_stride >= a->dim && t->head_stride >= a->dim);
+}
+HeadRows rows_of(const rb_heads* t) { return HeadRows{static_cast<Bf16*>(t->data), t->token_stride, t->head_stride}; }
+
+bool documents_fit(const rb_documents* d)
+{
+    if (!d || !d->offsets || d->count < 0 || d->count > RB_MAX_DOCUMENTS) return false;
+    return aligned(d->offsets, 8) && aligned(d->lengths, 8) && aligned(d->prefixes, 8);
+}
+
+hipError_t find_spans(const rb_attention* a, const rb_documents* d, int64_t tokens, hipStream_t st)
+{
+    const SpanArgs s{d->offsets, d->lengths, d->prefixes, d->count, reinterpret_cast<Spans*>(a->ws), (int32_t)tokens, a->causal};
+    return launch(rb_spans_kernel, dim3((unsigned)(tokens + AT_TPB - 1) / AT_TPB), AT_TPB, 0, st, s);
+}
+
+AttentionArgs attention_args(const rb_attention* a, const rb_heads* q, const rb_heads* k, const rb_heads* v, int64_t tokens, const float* slopes)
+{
+    AttentionArgs g{};
+    g.q = rows_of(q);
+    g.k = rows_of(k);
+    g.v = rows_of(v);
+    g.spans = reinterpret_cast<const Spans*>(a->ws);
+    g.slopes = slopes;
+    g.score = a->score;
+    g.tokens = (int32_t)tokens;
+    g.dim = a->dim;
+    g.heads = a->heads;
+    g.group = a->heads / a->kv_heads;
+    g.tiles = (int32_t)((tokens + AT_ROWS - 1) / AT_ROWS);
+    return g;
+}
+
+// The kernel of a head's size, with or without a cap and slopes: `of` is called with these three.
+template <typename Of>
+hipError_t by_form(const rb_attention* a, bool slopes, const Of& of)
+{
+    using D64 = std::integral_constant<int, 64>;
+    using D128 = std::integral_constant<int, 128>;
+    auto with = [&](auto dim) {
+        if (a->cap) return slopes ? of(dim, std::true_type(), std::true_type()) : of(dim, std::true_type(), std::false_type());
+        return slopes ? of(dim, std::false_type(), std::true_type()) : of(dim, std::false_type(), std::false_type());
+    };
+    return a->dim <= 64 ? with(D64()) : with(D128());
+}
+
+}  // namespace
+
+extern "C" {
+
+int rb_attention_create(rb_attention** out, int64_t heads, int64_t kv_heads, int64_t head_dim, int64_t max_tokens, int32_t causal, float scale, float cap)
+{
+    if (!out) return RB_EINVAL;
+    *out = nullptr;
+    if (heads < 1 || heads > RB_MAX_HEADS || kv_heads < 1 || heads % kv_heads != 0) return RB_EINVAL;
+    if (head_dim < 8 || head_dim > RB_MAX_HEAD_DIM || head_dim % 8 != 0 || max_tokens < 1 || max_tokens > RB_MAX_TOKENS || heads * max_tokens > RB_MAX_HEAD_ROWS) return RB_EINVAL;
+    if (!std::isfinite(scale) || !(scale > 0.0f) || !std::isfinite(cap) || cap < 0.0f) return RB_EINVAL;
+    rb_attention* a = new (std::nothrow) rb_attention();
+    if (!a) return RB_ENOMEM;
+    a->heads = (int32_t)heads;
+    a->kv_heads = (int32_t)kv_heads;
+    a->dim = (int32_t)head_dim;
+    a->max_tokens = (int32_t)max_tokens;
+    a->causal = causal != 0;
+    a->cap = cap > 0.0f;
+    a->score.scale = scale;
+    a->score.to_log2 = (a->cap ? cap : scale) * AT_LOG2E;
+    a->score.per_cap = a->cap ? scale / cap : 0.0f;
+    size_t off = round_up((size_t)max_tokens * sizeof(Spans), 256);
+    a->off_lse2 = off; off += round_up((size_t)heads * (size_t)max_tokens * sizeof(float), 256);
+    a->off_delta = off; off += round_up((size_t)heads * (size_t)max_tokens * sizeof(float), 256);
+    a->bytes = off;
+    *out = a;
+    return RB_OK;
+}
+
+int rb_attention_query(const rb_attention* a, size_t* workspace_bytes)
+{
+    if (!a || !workspace_bytes) return RB_EINVAL;
+    *workspace_bytes = a->bytes;
+    return RB_OK;
+}
+
+int rb_attention_bind(rb_attention* a, void* workspace)
+{
+    if (!a || !workspace || !aligned(workspace, 256)) return RB_EINVAL;
+    a->ws = static_cast<char*>(workspace);
+    return RB_OK;
+}
+
+int rb_attention_forward(rb_attention* a, const rb_heads* q, const rb_heads* k, const rb_heads* v, int64_t tokens, const rb_documents* documents,
+                         const float* slopes, const rb_heads* out, float* lse, void* hip_stream)
+{
+    if (!a || tokens < 0 || tokens > a->max_tokens || !documents_fit(documents) || !aligned(slopes, 4) || !aligned(lse, 4)) return RB_EINVAL;
+    if (!heads_fit(a, q, false) || !heads_fit(a, k, false) || !heads_fit(a, v, false) || !heads_fit(a, out, true)) return RB_EINVAL;
+    if (!a->ws) return RB_ESTATE;
+    if (tokens == 0) return RB_OK;
+    hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    AttentionArgs g = attention_args(a, q, k, v, tokens, slopes);
+    g.out = rows_of(out);
+    g.lse = lse;
+    hipError_t e = find_spans(a, documents, tokens, st);
+    if (e == hipSuccess)
+        e = by_form(a, slopes != nullptr, [&](auto dim, auto cap, auto lowered) {
+            return launch(rb_attend_kernel<dim(), cap(), lowered()>, dim3((unsigned)(g.tiles * g.heads)), AT_TPB, 0, st, g);
+        });
+    return e == hipSuccess ? RB_OK : RB_EHIP;
+}
+
+int rb_attention_grad(rb_attention* a, const rb_heads* q, const rb_heads* k, const rb_heads* v, int64_t tokens, const rb_documents* documents,
+                      const float* slopes, const rb_heads* out, const float* lse, const rb_heads* grad_out, const rb_heads* grad_q, const rb_heads* grad_k,
+                      const rb_heads* grad_v, void* hip_stream)
+{
+    if (!a || tokens < 0 || tokens > a->max_tokens || !documents_fit(documents) || !aligned(slopes, 4) || !lse || !aligned(lse, 4)) return RB_EINVAL;
+    if (!heads_fit(a, q, false) || !heads_fit(a, k, false) || !heads_fit(a, v, false) || !heads_fit(a, out, false) || !heads_fit(a, grad_out, false)) return RB_EINVAL;
+    if (!heads_fit(a, grad_q, true) || !heads_fit(a, grad_k, true) || !heads_fit(a, grad_v, true)) return RB_EINVAL;
+    if (!a->ws) return RB_ESTATE;
+    if (tokens == 0) return RB_OK;
+    hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    AttentionArgs g = attention_args(a, q, k, v, tokens, slopes);
+    float *const lse2 = reinterpret_cast<float*>(a->ws + a->off_lse2), *const delta = reinterpret_cast<float*>(a->ws + a->off_delta);
+    g.out = rows_of(out);
+    g.lse = const_cast<float*>(lse);
+    g.grad_out = rows_of(grad_out);
+    g.grad_q = rows_of(grad_q);
+    g.grad_k = rows_of(grad_k);
+    g.grad_v = rows_of(grad_v);
+    g.lse2 = lse2;
+    g.delta = delta;
+    hipError_t e = find_spans(a, documents, tokens, st);
+    const int64_t rows = tokens * a->heads;
+    if (e == hipSuccess) e = launch(rb_attend_delta_kernel, dim3((unsigned)std::min<int64_t>((rows + AT_TPB / 16 - 1) / (AT_TPB / 16), 1 << 20)), AT_TPB, 0, st, g, lse2, delta);
+    if (e == hipSuccess)
+        e = by_form(a, slopes != nullptr, [&](auto dim, auto cap, auto lowered) {
+            const hipError_t first = launch(rb_attend_grad_kv_kernel<dim(), cap(), lowered()>, dim3((unsigned)(g.tiles * a->kv_heads)), AT_TPB, 0, st, g);
+            if (first != hipSuccess) return first;
+            return launch(rb_attend_grad_q_kernel<dim(), cap(), lowered()>, dim3((unsigned)(g.tiles * g.heads)), AT_TPB, 0, st, g);
+        });
+    return e == hipSuccess ? RB_OK : RB_EHIP;
+}
+
+int rb_attention_destroy(rb_attention* a)
+{
+    delete a;
+    return RB_OK;
+}
+
+}  // extern "C"

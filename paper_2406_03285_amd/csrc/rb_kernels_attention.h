@@ -1,0 +1,697 @@
+// Attention of packed documents (rb_attention_forward) and its gradients (rb_attention_grad).  Included by rb_block.hip only.
+//
+// Masks.  What a position sees - its document up to itself, or the prefix, or all of the document - is one interval of positions, and so is what sees
+// it.  A first small kernel finds both for every position; the others compare with them and know no documents.  Tiles that every row of a wavefront sees whole
+// are not compared at all, tiles that none sees are passed over.
+//
+// Products.  Matrix instructions of 32 x 32 x 16 give a lane 16 elements of one column, in rows 8 (i / 4) + 4 (lane / 32) + i % 4.  The scores are made
+// transposed (keys x queries), so that a lane has one query: maximum and sum of the softmax are its own but for one exchange with lane ^ 32.  The next
+// product sums over the keys, and may take them in any order as long as both operands do: the lane's elements, rounded to bfloat16, are that
+// operand as they are, and the other one (values, transposed) is read from LDS in the same order by transposing reads.  The gradients of keys
+// and values have keys for columns (a lane has one key) and sum over queries in the same way.
+//
+// LDS.  Tiles are 64 rows of 128 or 256 bytes, loaded straight into LDS, 16 bytes a lane; the 16-byte pieces of a row are permuted by the row's number so
+// that both the reads of rows (one piece each of 32 rows) and the transposing reads (four neighbouring pieces of eight rows) meet all banks.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "rb_lanes.h"
+
+namespace {
+
+constexpr int AT_TPB = 256;
+constexpr int AT_WAVES = AT_TPB / 64;
+constexpr int AT_BLOCK = 32;                       // rows of a wavefront
+constexpr int AT_ROWS = AT_WAVES * AT_BLOCK;       // rows of a workgroup
+constexpr int AT_TILE = 64;                        // rows that are in LDS at a time
+constexpr float AT_LOG2E = 1.44269504088896340736f;
+constexpr float AT_LN2 = 0.69314718055994530942f;
+
+typedef __bf16 at_bf8 __attribute__((ext_vector_type(8)));
+typedef float at_acc __attribute__((ext_vector_type(16)));
+typedef short at_s4 __attribute__((ext_vector_type(4)));
+typedef short at_s8 __attribute__((ext_vector_type(8)));
+
+struct HeadRows {
+    Bf16* data;
+    int64_t token, head;       // strides in elements
+    __device__ __forceinline__ Bf16* at(int64_t t, int64_t h) const { return data + t * token + h * head; }
+};
+
+struct Span { int32_t lo, hi; };
+struct Spans { Span sees, seen; };      // of a position: what it sees, and what sees it
+
+struct SpanArgs {
+    const int64_t *offsets, *lengths, *prefixes;
+    int64_t count;
+    Spans* spans;
+    int32_t tokens, causal;
+};
+
+// Of position t.  Its document is the last one that begins at or before it (those behind that one with the same begin are empty).  Positions
+// in no document get empty intervals at themselves, so that neighbouring positions' intervals still rise.  Whatever the numbers are, intervals
+// lie within the positions there are, and one that is not empty holds t.
+__host__ __device__ inline Spans at_spans_of(const SpanArgs& a, int32_t t)
+{
+    auto lower = [](int64_t x, int64_t y) { return x < y ? x : y; };
+    auto higher = [](int64_t x, int64_t y) { return x < y ? y : x; };
+    int64_t low = 0, high = a.count;               // first document that begins behind t
+    while (low < high) {
+        const int64_t mid = (low + high) / 2;
+        if (a.offsets[mid] <= t) low = mid + 1;
+        else high = mid;
+    }
+    Spans s{{t, t}, {t, t}};
+    if (low == 0) return s;
+    const int64_t d = low - 1, begin = higher(a.offsets[d], 0);
+    int64_t end = lower(a.offsets[d + 1], a.tokens);
+    if (a.lengths) end = lower(end, begin + lower(higher(a.lengths[d], 0), a.tokens));
+    if (t >= end) return s;
+    const int64_t prefix = a.prefixes ? begin + lower(higher(a.prefixes[d], 0), end - begin) : begin;
+    s.sees.lo = (int32_t)begin;
+    s.sees.hi = (int32_t)(a.causal ? higher((int64_t)t + 1, prefix) : end);
+    s.seen.lo = (int32_t)(a.causal && t >= prefix ? t : begin);
+    s.seen.hi = (int32_t)end;
+    return s;
+}
+
+// A thread per position.
+__global__ void __launch_bounds__(AT_TPB) rb_spans_kernel(SpanArgs a)
+{
+    const int t = blockIdx.x * AT_TPB + threadIdx.x;
+    if (t < a.tokens) a.spans[t] = at_spans_of(a, t);
+}
+
+// ---- tiles in LDS --------------------------------------------------------------
+
+// Where piece c (16 bytes) of row r of a tile lies: in place c ^ at_turn(r) of the row.
+template <int D>
+__device__ __forceinline__ int at_turn(int r)
+{
+    return D == 128 ? ((r & 3) << 2) | ((r >> 2) & 3) : (((r >> 1) & 1) << 2) | ((r >> 2) & 3);
+}
+
+// A lane's part in bringing tiles of 64 rows: the same pieces of every tile.
+template <int D>
+struct Bring {
+    static constexpr int PIECES = D / 8, LOADS = AT_TILE * PIECES / AT_TPB, STEP = AT_TILE / LOADS;
+    int row, piece, wave;
+    __device__ __forceinline__ Bring(int wave_) : wave(wave_)
+    {
+        const int lane = threadIdx.x & 63;
+        row = (wave * 64 + lane) / PIECES;
+        piece = (lane % PIECES) ^ at_turn<D>(row);
+    }
+    // Rows first .. first + 63 of `from`, no further than row `last`.  (Pieces behind the head's last number are left as they are: 0.)
+    __device__ __forceinline__ void operator()(const Bf16* from, int64_t stride, int first, int last, int dim, char* tile) const
+    {
+        if (piece * 8 >= dim) return;
+#pragma unroll
+        for (int j = 0; j < LOADS; ++j) {
+            const Bf16* p = from + (int64_t)min(first + j * STEP + row, last) * stride + piece * 8;
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)p,
+                                             (__attribute__((address_space(3))) void*)(tile + (j * AT_WAVES + wave) * 1024), 16, 0, 0);
+        }
+    }
+};
+
+// 64 binary32 numbers behind each other (one wavefront).
+__device__ __forceinline__ void at_bring_numbers(const float* from, int first, int last, float* to)
+{
+    const float* p = from + min(first + (int)(threadIdx.x & 63), last);
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)p, (__attribute__((address_space(3))) void*)to, 4, 0, 0);
+}
+
+// Waits until a wavefront's loads into LDS and its reads from there are done, then for the workgroup's other wavefronts.
+__device__ __forceinline__ void at_arrived() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+// What a lane reads of tiles: rows (an operand whose rows are the tile's, summed over the head's numbers) and columns (one whose rows are the head's
+// numbers, summed over the tile's rows in the order of a result's elements).
+template <int D>
+struct Reads {
+    int row_at, row_turn, col_at, col_turn;
+    __device__ __forceinline__ Reads()
+    {
+        const int lane = threadIdx.x & 63, half = lane / 32, r = lane & 31;
+        row_at = r * D * 2;
+        row_turn = half ^ at_turn<D>(r);
+        // 16 lanes read four rows of 16 numbers; lane i gets column i of them
+        const int i = lane & 15, c = (lane >> 4) & 1, rr = 4 * half + i / 4;
+        col_at = rr * D * 2 + (i & 1) * 8;
+        col_turn = (2 * c + (i & 3) / 2) ^ at_turn<D>(rr);
+    }
+    // numbers 16 s + 8 (lane / 32) .. of row 32 b + lane % 32
+    __device__ __forceinline__ at_bf8 rows(const char* tile, int b, int s) const
+    {
+        return *reinterpret_cast<const at_bf8*>(tile + b * 32 * D * 2 + row_at + ((row_turn ^ (2 * s)) << 4));
+    }
+    // number 32 n + lane % 32 of the rows 16 c + 4 (lane / 32) .. + 3 and 8 behind these
+    __device__ __forceinline__ at_bf8 columns(const char* tile, int n, int c) const
+    {
+        typedef __attribute__((address_space(3))) at_s4* place;
+        const char* const first = tile + c * 16 * D * 2 + col_at;
+        const int turn = col_turn ^ (4 * n);
+        const at_s4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((place)(first + (turn << 4)));
+        const at_s4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((place)(first + 8 * D * 2 + ((turn ^ 2) << 4)));
+        return __builtin_bit_cast(at_bf8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+    }
+};
+
+__device__ __forceinline__ at_acc at_mma(at_bf8 a, at_bf8 b, at_acc c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+
+// Elements 8 c .. 8 c + 7 of a lane as an operand.
+__device__ __forceinline__ at_bf8 at_pack(const at_acc& v, int c)
+{
+    sc_vec w;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = sc_bf16_pair(v[8 * c + 2 * i], v[8 * c + 2 * i + 1]);
+    return __builtin_bit_cast(at_bf8, w);
+}
+
+// The head's numbers 16 s + 8 (lane / 32) .. of one row, as operands.
+template <int D>
+__device__ __forceinline__ void at_own(const Bf16* row, int dim, at_bf8 (&f)[D / 16])
+{
+    const int half = (threadIdx.x >> 5) & 1;
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s) {
+        const int first = 16 * s + 8 * half;
+        f[s] = first < dim ? *reinterpret_cast<const at_bf8*>(row + first) : at_bf8{};
+    }
+}
+
+// ---- products with what may be masked --------------------------------------------
+//
+// 0 times an infinity or a NaN is no 0: where a tile has both what is masked (a factor of 0) and numbers that are not finite, those are
+// replaced by 0, and products with 1 where something is seen tell where they belong.
+
+__device__ __forceinline__ uint32_t at_not_finite(at_bf8 v)         // not 0 if one of them is
+{
+    const sc_vec w = __builtin_bit_cast(sc_vec, v);
+    uint32_t found = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) found |= (w[i] & 0x7f807f80u) + 0x00800080u;       // (an exponent of ones carries into the sign's place)
+    return found & 0x80008000u;
+}
+
+__device__ __forceinline__ void at_sort_out(at_bf8 v, at_bf8& finite, at_bf8& up, at_bf8& down)
+{
+    at_s8 w = __builtin_bit_cast(at_s8, v), u, d;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const uint16_t x = (uint16_t)w[i];
+        const bool special = (x & 0x7f80) == 0x7f80, nan = special && (x & 0x7f);
+        u[i] = special && (nan || !(x & 0x8000)) ? 0x3f80 : 0;
+        d[i] = special && (nan || (x & 0x8000)) ? 0x3f80 : 0;
+        if (special) w[i] = 0;
+    }
+    finite = __builtin_bit_cast(at_bf8, w);
+    up = __builtin_bit_cast(at_bf8, u);
+    down = __builtin_bit_cast(at_bf8, d);
+}
+
+// sum[n] += columns of the tile's rows 16 (c0 + c) .. times factors[c], for the head's numbers 32 n ...  seen: which factors count, a bit each.
+template <int D, int C>
+__device__ __forceinline__ void at_add(at_acc (&sum)[D / 32], const at_bf8 (&factors)[C], const Reads<D>& reads, const char* tile, int c0, bool masked, const uint32_t (&seen)[C])
+{
+    if (masked) {
+        uint32_t found = 0;
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int n = 0; n < D / 32; ++n) found |= at_not_finite(reads.columns(tile, n, c0 + c));
+        if (__any(found != 0)) {
+#pragma unroll
+            for (int n = 0; n < D / 32; ++n) {
+                at_acc ups{}, downs{};
+#pragma unroll
+                for (int c = 0; c < C; ++c) {
+                    at_bf8 finite, up, down;
+                    at_sort_out(reads.columns(tile, n, c0 + c), finite, up, down);
+                    at_s8 one;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) one[i] = (seen[c] >> i) & 1 ? 0x3f80 : 0;
+                    sum[n] = at_mma(finite, factors[c], sum[n]);
+                    ups = at_mma(up, __builtin_bit_cast(at_bf8, one), ups);
+                    downs = at_mma(down, __builtin_bit_cast(at_bf8, one), downs);
+                }
+#pragma unroll
+                for (int i = 0; i < 16; ++i) sum[n][i] += (ups[i] > 0.0f ? -sc_neg_inf() : 0.0f) + (downs[i] > 0.0f ? sc_neg_inf() : 0.0f);
+            }
+            return;
+        }
+    }
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int n = 0; n < D / 32; ++n) sum[n] = at_mma(reads.columns(tile, n, c0 + c), factors[c], sum[n]);
+}
+
+// ---- scores ------------------------------------------------------------------
+
+struct ScoreOf {
+    float scale, to_log2;      // of a product; of a score in base 2: scale * log2 e without a cap, cap * log2 e with one
+    float per_cap;             // scale / cap
+};
+
+// tanh within some 2^-23: (near 0 by its series, x^9 left out: 2^-32 of it at 1/8)
+__device__ __forceinline__ float at_tanh(float x)
+{
+    const float x2 = x * x;
+    const float near = x * fmaf(x2, fmaf(x2, fmaf(x2, -17.0f / 315, 2.0f / 15), -1.0f / 3), 1.0f);
+    const float e = __builtin_amdgcn_exp2f(x * (2 * AT_LOG2E));
+    const float far = 1.0f - 2.0f * __builtin_amdgcn_rcpf(e + 1.0f);
+    return fabsf(x) < 0.125f ? near : far;
+}
+
+// A score in base 2 of a product; `slope` becomes the cap's derivative.
+template <bool CAP>
+__device__ __forceinline__ float at_score(const ScoreOf& of, float product, float& slope)
+{
+    if (!CAP) return product * of.to_log2;
+    const float t = at_tanh(product * of.per_cap);
+    slope = 1.0f - t * t;
+    return t * of.to_log2;
+}
+
+struct AttentionArgs {
+    HeadRows q, k, v;
+    const Spans* spans;
+    const float* slopes;
+    ScoreOf score;
+    int32_t tokens, dim, heads, group;     // group: heads of queries to one of keys
+    int32_t tiles;
+    // forward: written; gradients: read
+    HeadRows out;
+    float* lse;
+    // gradients
+    HeadRows grad_out, grad_q, grad_k, grad_v;
+    const float *lse2, *delta;             // [heads][tokens]: lse in base 2 (+inf where nothing is seen); the sum of grad_out * out
+};
+
+// Which tile and head the workgroup has.  Workgroups go to the 8 dies in turn; a die gets neighbours - the heads of a group, then tiles of one
+// head of keys - whose keys it then finds in its own L2.  Tiles are taken from both ends in turn: the first ones of a causal document see little, the last all.
+__device__ __forceinline__ void at_place(int id, int count, int tiles, int inner, int& tile, int& head)
+{
+    const int die = id & 7, whole = count >> 3, more = count & 7;
+    const int rank = die * whole + min(die, more) + (id >> 3);
+    const int outer = rank / inner, in = rank - outer * inner;
+    const int t = outer % tiles, kv = outer / tiles;
+    tile = t & 1 ? t / 2 : tiles - 1 - t / 2;
+    head = kv * inner + in;
+}
+
+__device__ __forceinline__ int at_lowest(int v)
+{
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) v = min(v, __shfl_xor(v, d));
+    return __builtin_amdgcn_readfirstlane(v);
+}
+__device__ __forceinline__ int at_highest(int v) { return -at_lowest(-v); }
+
+// What a wavefront's rows see: all of it lies in [lo, hi), and [all_lo, all_hi) is seen by every row that sees anything.
+struct Reach {
+    int lo, hi, all_lo, all_hi;
+    __device__ __forceinline__ Reach(Span s)
+    {
+        const bool any = s.lo < s.hi;
+        lo = at_lowest(any ? s.lo : INT32_MAX);
+        hi = at_highest(any ? s.hi : 0);
+        all_lo = at_highest(any ? s.lo : 0);
+        all_hi = at_lowest(any ? s.hi : INT32_MAX);
+    }
+    __device__ __forceinline__ bool meets(int first) const { return first < hi && first + AT_TILE > lo; }
+    __device__ __forceinline__ bool whole(int first) const { return first >= all_lo && first + AT_TILE <= all_hi; }
+};
+
+// [lo, hi) of what the rows first .. first + 127 see (SEEN: of what sees them).
+template <bool SEEN>
+__device__ __forceinline__ void at_range(const Spans* spans, int first, int tokens, int& lo, int& hi)
+{
+    const int lane = threadIdx.x & 63;
+    lo = INT32_MAX;
+    hi = 0;
+#pragma unroll
+    for (int i = 0; i < AT_ROWS / 64; ++i) {
+        const int t = first + i * 64 + lane;
+        if (t < tokens) {
+            const Span s = SEEN ? spans[t].seen : spans[t].sees;
+            if (s.lo < s.hi) {
+                lo = min(lo, s.lo);
+                hi = max(hi, s.hi);
+            }
+        }
+    }
+    lo = at_lowest(lo);
+    hi = at_highest(hi);
+}
+
+template <int D>
+__device__ __forceinline__ void at_clear(char* lds, int bytes, int dim)
+{
+    if (dim == D) return;
+    for (int i = threadIdx.x * 16; i < bytes; i += AT_TPB * 16) *reinterpret_cast<sc_vec*>(lds + i) = sc_vec{0, 0, 0, 0};
+    __syncthreads();
+}
+
+// Row `t` of a result from its numbers 32 n + 8 (i / 4) + 4 (lane / 32) + i % 4.
+template <int D>
+__device__ __forceinline__ void at_store(Bf16* row, int dim, const at_acc (&v)[D / 32], float factor, bool zero)
+{
+    const int half = (threadIdx.x >> 5) & 1;
+#pragma unroll
+    for (int n = 0; n < D / 32; ++n)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const int first = 32 * n + 8 * g + 4 * half;
+            if (first >= dim) continue;
+            uint2 w{0, 0};
+            if (!zero) w = uint2{sc_bf16_pair(v[n][4 * g] * factor, v[n][4 * g + 1] * factor), sc_bf16_pair(v[n][4 * g + 2] * factor, v[n][4 * g + 3] * factor)};
+            *reinterpret_cast<uint2*>(row + first) = w;
+        }
+}
+
+// ---- forward -------------------------------------------------------------------
+
+template <int D, bool CAP, bool SLOPES>
+__global__ void __launch_bounds__(AT_TPB, 2) rb_attend_kernel(AttentionArgs a)
+{
+    __shared__ __align__(1024) char lds[2][2][AT_TILE * D * 2];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x & 63, half = lane / 32;
+    int tile, head;
+    at_place(blockIdx.x, gridDim.x, a.tiles, a.group, tile, head);
+    const int kv = head / a.group;
+    int lo, hi;
+    at_range<false>(a.spans, tile * AT_ROWS, a.tokens, lo, hi);
+    const int row = tile * AT_ROWS + wave * AT_BLOCK + (lane & 31);
+    const Span mine = row < a.tokens ? a.spans[row].sees : Span{0, 0};
+    const Reach reach(mine);
+    const int last = a.tokens - 1;
+    const Bf16 *const keys = a.k.at(0, kv), *const values = a.v.at(0, kv);
+    const float slope2 = SLOPES ? a.slopes[head] * AT_LOG2E : 0.0f;
+    at_bf8 q[D / 16];
+    at_own<D>(a.q.at(min(row, last), head), a.dim, q);
+    at_clear<D>(&lds[0][0][0], sizeof(lds), a.dim);
+    const Bring<D> bring(wave);
+    const Reads<D> reads;
+    at_acc o[D / 32]{};
+    float m = sc_neg_inf(), l = 0.0f;               // maximum (base 2) and this lane's part of the sum
+    const int count = (hi - lo + AT_TILE - 1) / AT_TILE;        // (nothing seen: lo > hi, no tiles)
+    if (lo < hi) {
+        bring(keys, a.k.token, lo, last, a.dim, lds[0][0]);
+        bring(values, a.v.token, lo, last, a.dim, lds[0][1]);
+    }
+    for (int i = 0; lo < hi && i < count; ++i) {
+        const int first = lo + i * AT_TILE;
+        at_arrived();
+        if (i + 1 < count) {
+            bring(keys, a.k.token, first + AT_TILE, last, a.dim, lds[(i + 1) & 1][0]);
+            bring(values, a.v.token, first + AT_TILE, last, a.dim, lds[(i + 1) & 1][1]);
+        }
+        if (!reach.meets(first)) continue;
+        const char *const kt = lds[i & 1][0], *const vt = lds[i & 1][1];
+        at_acc s[2]{};
+#pragma unroll
+        for (int n = 0; n < D / 16; ++n)
+#pragma unroll
+            for (int b = 0; b < 2; ++b) s[b] = at_mma(reads.rows(kt, b, n), q[n], s[b]);
+        const bool masked = !reach.whole(first);
+        uint32_t seen[4] = {~0u, ~0u, ~0u, ~0u};
+        float most = sc_neg_inf();
+        if (CAP || SLOPES) {
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    float slope;
+                    s[b][e] = at_score<CAP>(a.score, s[b][e], slope);
+                    if (SLOPES) s[b][e] -= slope2 * fabsf((float)(row - first - 32 * b - 8 * (e / 4) - 4 * half - e % 4));
+                }
+        }
+        if (masked) {
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                seen[c] = 0;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const int key = first + 16 * c + 8 * (e / 4) + 4 * half + e % 4;
+                    const bool there = key >= mine.lo && key < mine.hi;
+                    s[c / 2][c % 2 * 8 + e] = there ? s[c / 2][c % 2 * 8 + e] : sc_neg_inf();
+                    seen[c] |= there ? 1u << e : 0u;
+                }
+            }
+        }
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) most = fmaxf(most, s[b][e]);
+        if (!CAP && !SLOPES) most *= a.score.to_log2;
+        most = fmaxf(most, sc_xor<32>(most));
+        if (__any(most > m)) {
+            const float now = fmaxf(m, most);
+            const float factor = now == sc_neg_inf() ? 1.0f : __builtin_amdgcn_exp2f(m - now);
+            l *= factor;
+#pragma unroll
+            for (int n = 0; n < D / 32; ++n)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) o[n][e] *= factor;
+            m = now;
+        }
+        const float base = m == sc_neg_inf() ? 0.0f : m;
+        at_bf8 p[4];
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                s[b][e] = __builtin_amdgcn_exp2f(CAP || SLOPES ? s[b][e] - base : fmaf(s[b][e], a.score.to_log2, -base));
+                l += s[b][e];
+            }
+            p[2 * b] = at_pack(s[b], 0);
+            p[2 * b + 1] = at_pack(s[b], 1);
+        }
+        at_add<D, 4>(o, p, reads, vt, 0, masked, seen);
+    }
+    if (row >= a.tokens) return;
+    l += sc_xor<32>(l);
+    const bool empty = mine.lo >= mine.hi;
+    at_store<D>(a.out.at(row, head), a.dim, o, 1.0f / l, empty);
+    if (a.lse && half == 0) a.lse[(int64_t)head * a.tokens + row] = empty ? sc_neg_inf() : (m + __log2f(l)) * AT_LN2;
+}
+
+// ---- gradients -----------------------------------------------------------------
+
+// What the gradients need of every row of every head: lse in base 2, and the sum of grad_out * out.  16 lanes a row.
+__global__ void __launch_bounds__(AT_TPB) rb_attend_delta_kernel(AttentionArgs a, float* lse2, float* delta)
+{
+    const int64_t rows = (int64_t)a.heads * a.tokens;
+    const int first = (threadIdx.x & 15) * 8;
+    for (int64_t at = (int64_t)blockIdx.x * (AT_TPB / 16) + threadIdx.x / 16; at < rows; at += (int64_t)gridDim.x * (AT_TPB / 16)) {       // (whole groups of 16 lanes)
+        const int t = (int)(at / a.heads), h = (int)(at - (int64_t)t * a.heads);
+        float sum = 0.0f;
+        if (first < a.dim) {
+            const sc_vec x = *reinterpret_cast<const sc_vec*>(a.out.at(t, h) + first), y = *reinterpret_cast<const sc_vec*>(a.grad_out.at(t, h) + first);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                sum = fmaf(__uint_as_float(x[i] << 16), __uint_as_float(y[i] << 16), sum);
+                sum = fmaf(__uint_as_float(x[i] & 0xffff0000u), __uint_as_float(y[i] & 0xffff0000u), sum);
+            }
+        }
+        sum += sc_xor<1>(sum);
+        sum += sc_xor<2>(sum);
+        sum += sc_xor<4>(sum);
+        sum += sc_xor<8>(sum);
+        if (first == 0) {
+            const Span s = a.spans[t].sees;
+            const int64_t to = (int64_t)h * a.tokens + t;
+            delta[to] = sum;
+            lse2[to] = s.lo < s.hi ? a.lse[to] * AT_LOG2E : -sc_neg_inf();
+        }
+    }
+}
+
+// p and ds of one element.
+template <bool CAP, bool SLOPES>
+__device__ __forceinline__ void at_slope(const ScoreOf& of, float product, float dp, float lse2, float delta, float lowered, float& p, float& ds)
+{
+    float slope = 1.0f;
+    if (CAP || SLOPES) {
+        float s = at_score<CAP>(of, product, slope);
+        if (SLOPES) s -= lowered;
+        p = __builtin_amdgcn_exp2f(s - lse2);
+    } else {
+        p = __builtin_amdgcn_exp2f(fmaf(product, of.to_log2, -lse2));
+    }
+    ds = p * (dp - delta);
+    if (CAP) ds *= slope;
+}
+
+// Of queries: as forward, with the scores made again.
+template <int D, bool CAP, bool SLOPES>
+__global__ void __launch_bounds__(AT_TPB, 2) rb_attend_grad_q_kernel(AttentionArgs a)
+{
+    __shared__ __align__(1024) char lds[2][2][AT_TILE * D * 2];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x & 63, half = lane / 32;
+    int tile, head;
+    at_place(blockIdx.x, gridDim.x, a.tiles, a.group, tile, head);
+    const int kv = head / a.group;
+    int lo, hi;
+    at_range<false>(a.spans, tile * AT_ROWS, a.tokens, lo, hi);
+    const int row = tile * AT_ROWS + wave * AT_BLOCK + (lane & 31);
+    const Span mine = row < a.tokens ? a.spans[row].sees : Span{0, 0};
+    const Reach reach(mine);
+    const int last = a.tokens - 1, r = min(row, last);
+    const Bf16 *const keys = a.k.at(0, kv), *const values = a.v.at(0, kv);
+    const float slope2 = SLOPES ? a.slopes[head] * AT_LOG2E : 0.0f;
+    at_bf8 q[D / 16], go[D / 16];
+    at_own<D>(a.q.at(r, head), a.dim, q);
+    at_own<D>(a.grad_out.at(r, head), a.dim, go);
+    const float lse2 = a.lse2[(int64_t)head * a.tokens + r], delta = a.delta[(int64_t)head * a.tokens + r];
+    at_clear<D>(&lds[0][0][0], sizeof(lds), a.dim);
+    const Bring<D> bring(wave);
+    const Reads<D> reads;
+    at_acc dq[D / 32]{};
+    const int count = (hi - lo + AT_TILE - 1) / AT_TILE;
+    if (lo < hi) {
+        bring(keys, a.k.token, lo, last, a.dim, lds[0][0]);
+        bring(values, a.v.token, lo, last, a.dim, lds[0][1]);
+    }
+    for (int i = 0; lo < hi && i < count; ++i) {
+        const int first = lo + i * AT_TILE;
+        at_arrived();
+        if (i + 1 < count) {
+            bring(keys, a.k.token, first + AT_TILE, last, a.dim, lds[(i + 1) & 1][0]);
+            bring(values, a.v.token, first + AT_TILE, last, a.dim, lds[(i + 1) & 1][1]);
+        }
+        if (!reach.meets(first)) continue;
+        const char *const kt = lds[i & 1][0], *const vt = lds[i & 1][1];
+        const bool masked = !reach.whole(first);
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            at_acc s{}, dp{};
+#pragma unroll
+            for (int n = 0; n < D / 16; ++n) {
+                s = at_mma(reads.rows(kt, b, n), q[n], s);
+                dp = at_mma(reads.rows(vt, b, n), go[n], dp);
+            }
+            uint32_t seen[2] = {~0u, ~0u};
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                float p, ds;
+                at_slope<CAP, SLOPES>(a.score, s[e], dp[e], lse2, delta,
+                                      SLOPES ? slope2 * fabsf((float)(row - first - 32 * b - 8 * (e / 4) - 4 * half - e % 4)) : 0.0f, p, ds);
+                s[e] = ds;
+            }
+            if (masked) {
+                seen[0] = seen[1] = 0;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const int key = first + 32 * b + 8 * (e / 4) + 4 * half + e % 4;
+                    const bool there = key >= mine.lo && key < mine.hi;
+                    s[e] = there ? s[e] : 0.0f;
+                    seen[e / 8] |= there ? 1u << (e % 8) : 0u;
+                }
+            }
+            const at_bf8 f[2] = {at_pack(s, 0), at_pack(s, 1)};
+            at_add<D, 2>(dq, f, reads, kt, 2 * b, masked, seen);
+        }
+    }
+    if (row >= a.tokens) return;
+    at_store<D>(a.grad_q.at(row, head), a.dim, dq, a.score.scale, mine.lo >= mine.hi);
+}
+
+// Of keys and values: a workgroup has 128 of one head, and goes through the queries of all the heads that read it.
+template <int D, bool CAP, bool SLOPES>
+__global__ void __launch_bounds__(AT_TPB, 1) rb_attend_grad_kv_kernel(AttentionArgs a)
+{
+    __shared__ __align__(1024) char lds[2][2][AT_TILE * D * 2];
+    __shared__ __align__(1024) float numbers[2][2][AT_TILE];          // lse in base 2 and delta of the tile's queries
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x & 63, half = lane / 32;
+    int tile, kv;
+    at_place(blockIdx.x, gridDim.x, a.tiles, 1, tile, kv);
+    int lo, hi;
+    at_range<true>(a.spans, tile * AT_ROWS, a.tokens, lo, hi);
+    const int row = tile * AT_ROWS + wave * AT_BLOCK + (lane & 31);
+    const Span mine = row < a.tokens ? a.spans[row].seen : Span{0, 0};
+    const Reach reach(mine);
+    const int last = a.tokens - 1;
+    at_bf8 k[D / 16], v[D / 16];
+    at_own<D>(a.k.at(min(row, last), kv), a.dim, k);
+    at_own<D>(a.v.at(min(row, last), kv), a.dim, v);
+    at_clear<D>(&lds[0][0][0], sizeof(lds), a.dim);
+    const Bring<D> bring(wave);
+    const Reads<D> reads;
+    auto fetch = [&](int head, int first, int buffer) {
+        bring(a.q.at(0, head), a.q.token, first, last, a.dim, lds[buffer][0]);
+        bring(a.grad_out.at(0, head), a.grad_out.token, first, last, a.dim, lds[buffer][1]);
+        if (wave == 0) at_bring_numbers(a.lse2 + (int64_t)head * a.tokens, first, last, numbers[buffer][0]);
+        if (wave == 1) at_bring_numbers(a.delta + (int64_t)head * a.tokens, first, last, numbers[buffer][1]);
+    };
+    at_acc dk[D / 32]{}, dv[D / 32]{};
+    int head = kv * a.group, first = lo, left = lo < hi ? (hi - lo + AT_TILE - 1) / AT_TILE * a.group : 0;
+    if (left) fetch(head, first, 0);
+    for (int buffer = 0; left > 0; --left, buffer ^= 1) {
+        int next_head = head, next = first + AT_TILE;
+        if (next >= hi) {
+            next = lo;
+            ++next_head;
+        }
+        at_arrived();
+        if (left > 1) fetch(next_head, next, buffer ^ 1);
+        if (reach.meets(first)) {
+            const char *const qt = lds[buffer][0], *const gt = lds[buffer][1];
+            const bool masked = !reach.whole(first);
+            const float slope2 = SLOPES ? a.slopes[head] * AT_LOG2E : 0.0f;
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                at_acc s{}, dp{};
+#pragma unroll
+                for (int n = 0; n < D / 16; ++n) {
+                    s = at_mma(reads.rows(qt, b, n), k[n], s);
+                    dp = at_mma(reads.rows(gt, b, n), v[n], dp);
+                }
+                uint32_t seen[2] = {~0u, ~0u};
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const float4 lse2 = *reinterpret_cast<const float4*>(&numbers[buffer][0][32 * b + 8 * g + 4 * half]);
+                    const float4 delta = *reinterpret_cast<const float4*>(&numbers[buffer][1][32 * b + 8 * g + 4 * half]);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int e = 4 * g + i;
+                        const float lse2_i = i == 0 ? lse2.x : i == 1 ? lse2.y : i == 2 ? lse2.z : lse2.w;
+                        const float delta_i = i == 0 ? delta.x : i == 1 ? delta.y : i == 2 ? delta.z : delta.w;
+                        float p, ds;
+                        at_slope<CAP, SLOPES>(a.score, s[e], dp[e], lse2_i, delta_i,
+                                              SLOPES ? slope2 * fabsf((float)(row - first - 32 * b - 8 * g - 4 * half - i)) : 0.0f, p, ds);
+                        s[e] = p;
+                        dp[e] = ds;
+                    }
+                }
+                if (masked) {
+                    seen[0] = seen[1] = 0;
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const int query = first + 32 * b + 8 * (e / 4) + 4 * half + e % 4;
+                        const bool there = query >= mine.lo && query < mine.hi;
+                        s[e] = there ? s[e] : 0.0f;
+                        dp[e] = there ? dp[e] : 0.0f;
+                        seen[e / 8] |= there ? 1u << (e % 8) : 0u;
+                    }
+                }
+                const at_bf8 p[2] = {at_pack(s, 0), at_pack(s, 1)}, ds[2] = {at_pack(dp, 0), at_pack(dp, 1)};
+                at_add<D, 2>(dv, p, reads, gt, 2 * b, masked, seen);
+                at_add<D, 2>(dk, ds, reads, qt, 2 * b, masked, seen);
+            }
+        }
+        head = next_head;
+        first = next;
+    }
+    if (row >= a.tokens) return;
+    const bool empty = mine.lo >= mine.hi;
+    at_store<D>(a.grad_k.at(row, kv), a.dim, dk, a.score.scale, empty);
+    at_store<D>(a.grad_v.at(row, kv), a.dim, dv, 1.0f, empty);
+}
+
+}  // namespace

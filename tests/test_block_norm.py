@@ -1,0 +1,269 @@
+"""Layer norm, dropout and their gradients (include/rb_block.h) on the GPU against a plain statement in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+import block_reference as ref
+import paper_2406_03285_amd as rb
+
+pytestmark = pytest.mark.gpu
+F32, BF16 = torch.float32, torch.bfloat16
+D = rb.Drop(0.2, 0xFEDCBA9876543210, (7 << 32) + 9)
+
+
+def make(rows, width, dtype, pad=0, offset=0, seed=0, spread=1.0, mean=0.0):
+    """[rows, width] in rows of width + pad, the first one `offset` elements behind a 16-byte boundary."""
+    g = torch.Generator().manual_seed(seed + 31 * width + rows)
+    x = (torch.randn((rows, width), generator=g) * spread + mean).to(dtype)
+    whole = torch.full((rows * (width + pad) + offset + 16,), 7.0, dtype=dtype, device="cuda")
+    view = whole[offset:offset + rows * (width + pad)].view(rows, width + pad)[:, :width]
+    view.copy_(x)
+    return view
+
+
+def weights(width, dtype, seed=0):
+    g = torch.Generator().manual_seed(seed + width)
+    return (1 + 0.3 * torch.randn(width, generator=g)).to(dtype).cuda(), (0.2 * torch.randn(width, generator=g)).to(dtype).cuda()
+
+
+def near(have, want, off, what):
+    have = ref.to64(have)
+    assert torch.isfinite(have).all(), what
+    assert ((have - want).abs() <= off).all(), (what, ((have - want).abs() / off).max())
+
+
+def check(x, residual, drop, weight, bias, eps=1e-5):
+    rows, width = x.shape
+    dtype, weight_dtype = x.dtype, weight.dtype
+    n = rb.LayerNorm(width, dtype, weight_dtype=weight_dtype, eps=eps)
+    got = n.forward(x, weight, bias, residual=residual, drop=drop)
+    total = ref.to64(x)
+    if residual is not None or drop is not None:
+        total = ref.drop(total, drop)
+        exact = total if residual is None else total + ref.to64(residual)
+        # the product is rounded, then the sum
+        near(got.total, exact, ref.HALF[dtype] * exact.abs() * 1.01 + 2 * ref.F32_HALF * (total.abs() + exact.abs()), "total")
+        total = ref.to64(got.total)
+    else:
+        assert got.total is None
+    w64, b64 = ref.to64(weight), ref.to64(bias)
+    y, mean, rstd = ref.norm(total, w64, b64, eps)
+    off_y, off_mean, off_rstd = ref.norm_bounds(total, w64, b64, eps, dtype)
+    near(got.y, y, off_y, "y")
+    near(got.mean, mean, off_mean, "mean")
+    near(got.rstd, rstd, off_rstd, "rstd")
+    # gradients, from the statistics as they are
+    gy, gt = make(rows, width, dtype, seed=3), make(rows, width, dtype, seed=4) if got.total is not None else None
+    g = n.grad(gy, x if got.total is None else got.total, weight, got.mean, got.rstd, grad_total=gt, drop=drop, bias=bias is not None)
+    args = (ref.to64(gy), total, ref.to64(gt), ref.to64(got.mean), ref.to64(got.rstd), w64)
+    d, gw, gb = ref.norm_grad(*args)
+    off_d, off_w, off_b = ref.norm_grad_bounds(*args, dtype, weight_dtype)
+    near(g.total, d, off_d, "grad total")
+    near(g.weight, gw, off_w, "grad weight")
+    if bias is not None:
+        near(g.bias, gb, off_b, "grad bias")
+    if drop is None:
+        assert g.x is None
+    else:
+        f = ref.kept(rows, width, drop)
+        have = ref.to64(g.x)
+        assert (have[f == 0] == 0).all()
+        near(g.x, d * f, off_d * f * (1 + ref.HALF[dtype]) + 2 * ref.F32_HALF * (d * f).abs(), "grad x")
+    again = n.grad(gy, x if got.total is None else got.total, weight, got.mean, got.rstd, grad_total=gt, drop=drop, bias=bias is not None)
+    assert all(a is b is None or torch.equal(a, b) for a, b in zip(g, again))
+    return n, got, g
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("width", [1, 2, 7, 8, 9, 63, 64, 127, 128, 129, 200, 511, 512, 513, 1000, 1024, 1025, 2047, 2048, 2049, 4096, 4097, 5003, 8192, 8193, 10007,
+                                   32768, 32769, 65536])
+def test_rows_of_any_length(width, dtype):
+    w, b = weights(width, F32)
+    check(make(5, width, dtype, mean=0.7), None, None, w, b)
+    check(make(18, width, dtype), make(18, width, dtype, seed=1, spread=3.0, mean=-1.0), D, w, b)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("weight_dtype", [F32, BF16])
+@pytest.mark.parametrize("residual,drop,bias", [(False, False, False), (True, False, True), (False, True, True), (True, True, False)])
+def test_what_may_be_left_out(residual, drop, bias, weight_dtype, dtype):
+    for width in (100, 1500, 9001):
+        w, b = weights(width, weight_dtype)
+        check(make(33, width, dtype), make(33, width, dtype, seed=1) if residual else None, D if drop else None, w, b if bias else None)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("pad,offset", [(0, 1), (1, 0), (3, 2), (5, 7), (8, 3), (40, 0)])
+def test_rows_that_lie_anyhow(pad, offset, dtype):
+    for width in (5, 131, 2051):
+        w, b = weights(width + 1, F32)
+        x, r = make(7, width, dtype, pad, offset), make(7, width, dtype, offset, pad, seed=1)
+        check(x, r, D, w[1:], b[1:])                      # (weights not at 16 bytes)
+        n = rb.LayerNorm(width, dtype, weight_dtype=F32)
+        want = n.forward(x, w[1:], b[1:], residual=r, drop=D)
+        into = rb.Normed(make(7, width, dtype, pad, offset), make(7, width, dtype, 2, 1), want.mean.clone(), want.rstd.clone())
+        whole = into.y._base
+        n.forward(x, w[1:], b[1:], residual=r, drop=D, out=into)
+        assert torch.equal(into.y, want.y) and torch.equal(into.total, want.total)
+        into.y.fill_(7.0)
+        assert (whole == 7.0).all()                       # (nothing around it was written)
+
+
+@pytest.mark.parametrize("rows", [1, 15, 16, 17, 511, 513, 4099, 20011])
+def test_any_number_of_rows(rows):
+    for width in (24, 300):
+        w, b = weights(width, F32)
+        check(make(rows, width, BF16), make(rows, width, BF16, seed=1), D, w, b)
+
+
+def test_many_rows_of_every_form():
+    for width, rows in ((1024, 3001), (2048, 2500), (4096, 1300), (8000, 700), (20000, 600)):
+        w, b = weights(width, F32)
+        check(make(rows, width, F32), None, None, w, b)
+
+
+def test_results_in_place():
+    for dtype in (F32, BF16):
+        for width in (70, 3000, 9000):
+            w, b = weights(width, F32)
+            x, r, gy, gt = (make(19, width, dtype, seed=s) for s in range(4))
+            n = rb.LayerNorm(width, dtype, weight_dtype=F32)
+            o = n.forward(x, w, b, residual=r, drop=D)
+            g = n.grad(gy, o.total, w, o.mean, o.rstd, grad_total=gt, drop=D)
+            x2, r2 = x.clone(), r.clone()
+            o2 = n.forward(x2, w, b, residual=r2, drop=D, out=rb.Normed(x2, r2, o.mean.clone(), None))
+            assert torch.equal(x2, o.y) and torch.equal(r2, o.total) and torch.equal(o2.mean, o.mean)
+            gy2, gt2 = gy.clone(), gt.clone()
+            n.grad(gy2, o.total, w, o.mean, o.rstd, grad_total=gt2, drop=D, out=rb.NormGrads(gy2, gt2, torch.empty_like(w), torch.empty_like(b)))
+            assert torch.equal(gy2, g.total) and torch.equal(gt2, g.x)
+            gt3 = gt.clone()
+            g3 = n.grad(gy, o.total, w, o.mean, o.rstd, grad_total=gt3, drop=D, out=rb.NormGrads(gt3, gy.clone(), torch.empty_like(w), None))
+            assert torch.equal(gt3, g.total) and torch.equal(g3.x, g.x) and torch.equal(g3.weight, g.weight)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("width", [50, 700, 5000, 20000])
+def test_rows_that_are_equal_far_or_not_numbers(width, dtype):
+    x = make(9, width, dtype)
+    x[0] = 3.25
+    x[1] = 0.0
+    x[2, width // 2] = float("nan")
+    x[3, 0] = float("inf")
+    x[4, -1] = -float("inf")
+    x[5] = x[5] * 1e-3 + 1e4
+    x[6] = x[6] * 1e-12
+    w, b = weights(width, dtype)
+    n = rb.LayerNorm(width, dtype, eps=1e-5)
+    o = n.forward(x, w, b)
+    assert torch.equal(o.y[0], b) and torch.equal(o.y[1], b)
+    assert torch.isnan(o.y[2:5]).all() and torch.isnan(o.rstd[2:5]).all()
+    rest = [5, 6, 7, 8]
+    want, _, _ = ref.norm(ref.to64(x)[rest], ref.to64(w), ref.to64(b), 1e-5)
+    off, _, _ = ref.norm_bounds(ref.to64(x)[rest], ref.to64(w), ref.to64(b), 1e-5, dtype)
+    near(o.y[rest], want, off, "y")
+    g = n.grad(make(9, width, dtype, seed=2), x, w, o.mean, o.rstd)
+    assert torch.isfinite(g.total[[0, 1, *rest]].float()).all() and torch.isnan(g.total[2:5]).all() and torch.isnan(g.weight).any()
+    with pytest.raises(rb.RbError):                       # (the deviation of a row of equal elements is what rounding leaves: eps has to be more than 0)
+        rb.LayerNorm(width, dtype, eps=0.0)
+
+
+def test_gradient_against_differences():
+    """Autograd through the calls - residual, dropout, weight, bias, y and total both used - against central differences in 64 bits."""
+    rows, width = 4, 13
+    x, r = make(rows, width, F32), make(rows, width, F32, seed=1, spread=2.0)
+    w, b = weights(width, F32)
+    cy, ct = make(rows, width, F32, seed=5), make(rows, width, F32, seed=6)
+    leaves = [t.clone().requires_grad_() for t in (x, w, b, r)]
+    n = rb.LayerNorm(width, F32)
+    o = n(*leaves[:3], residual=leaves[3], drop=D)
+    assert not o.mean.requires_grad
+    ((o.y * cy).sum() + (o.total * ct).sum()).backward()
+
+    def loss(x, w, b, r):
+        total = ref.drop(x, D) + r
+        return (ref.norm(total, w, b, 1e-5)[0] * ref.to64(cy)).sum() + (total * ref.to64(ct)).sum()
+
+    at = [ref.to64(t) for t in (x, w, b, r)]
+    for n_, (t, leaf) in enumerate(zip(at, leaves)):
+        for i in np.ndindex(*t.shape):
+            e = torch.zeros_like(t)
+            e[i] = 1e-5
+            up, down = (loss(*[y + f * e if m == n_ else y for m, y in enumerate(at)]) for f in (1, -1))
+            # differences: third derivatives (under 100) times 1e-10 / 6 and 1e-15 |loss| / 1e-5; binary32: 200 half steps of terms under 10 that are scaled by rstd and 1.25
+            assert abs(float(up - down) / 2e-5 - float(leaf.grad[i])) < 2e-4, (n_, i)
+
+
+def test_gradients_of_one_of_both_and_of_shared_inputs():
+    x, w = make(6, 40, BF16), weights(40, F32)[0]
+    n = rb.LayerNorm(40, BF16, weight_dtype=F32)
+    x1 = x.clone().requires_grad_()
+    o = n(x1, w, residual=x1)                             # the same tensor twice
+    o.y.float().sum().backward()
+    one = n.grad(torch.ones_like(x), o.total.detach(), w, o.mean, o.rstd, bias=False).total
+    assert torch.equal(x1.grad, one + one)
+    x2 = x.clone().requires_grad_()
+    o = n(x2, w, residual=x.clone(), drop=D)
+    (o.total.float() * 2).sum().backward()                # y is not used
+    assert torch.equal(x2.grad.double().cpu(), ref.drop(torch.full((6, 40), 2.0, dtype=torch.float64), D).to(torch.bfloat16).double())
+    x3 = x.clone().requires_grad_()
+    n(x3, w).y.sum().backward()                           # gradients that are broadcast
+    assert torch.equal(x3.grad, n.grad(torch.ones_like(x), x, w, *n.forward(x, w)[2:], bias=False).total)
+
+
+# ---- dropout -------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("p", [0.0, 1e-6, 0.1, 0.5, 0.999, 1.0])
+@pytest.mark.parametrize("rows,width,pad,offset", [(1, 1, 0, 0), (3, 7, 0, 1), (5, 8, 3, 0), (40, 9, 0, 0), (300, 16, 0, 0), (17, 255, 1, 3), (9, 2048, 0, 0), (3, 5001, 9, 0),
+                                                    (2, 40003, 0, 5)])
+def test_dropout(rows, width, pad, offset, p, dtype):
+    x = make(rows, width, dtype, pad, offset)
+    d = rb.Drop(p, 2 ** 64 - 5, 2 ** 40 + 3)
+    got = rb.dropout(x, d)
+    f = ref.kept(rows, width, d)
+    want = ref.to64(x) * f
+    have = ref.to64(got)
+    assert (have[f == 0] == 0).all()
+    # the scale is given in binary32: one product, rounded once to the type (twice where binary32 comes between)
+    assert ((have - want).abs() <= want.abs() * (ref.HALF[dtype] + ref.F32_HALF) * 1.01).all()
+    if p == 0.0:
+        assert torch.equal(got, x)
+    y = x.clone()
+    assert rb.dropout(y, d, out=y) is y and torch.equal(y, got)
+    z = torch.full((rows, width + 3), 7.0, dtype=dtype, device="cuda")
+    rb.dropout(x, d, out=z[:, :width])
+    assert torch.equal(z[:, :width], got) and (z[:, width:] == 7.0).all()
+
+
+def test_dropout_keeps_as_many_as_it_should_and_forgets_what_it_drops():
+    for p in (0.1, 0.5, 0.9):
+        x = torch.ones((512, 4096), device="cuda")
+        y = rb.dropout(x, rb.Drop(p, 1, 2))
+        n, kept = x.numel(), int((y > 0).sum())
+        q = 1 - round(p * 65536) / 65536
+        assert abs(kept - n * q) < 6 * (n * q * (1 - q)) ** 0.5              # six deviations
+        for other in (rb.Drop(p, 1, 3), rb.Drop(p, 2, 2), rb.Drop(p, 1 + (1 << 32), 2), rb.Drop(p, 1, 2 + (1 << 32))):
+            both = int(((y > 0) & (rb.dropout(x, other) > 0)).sum())
+            assert abs(both - n * q * q) < 6 * (n * q * q * (1 - q * q)) ** 0.5
+    x = torch.full((3, 1000), float("nan"), device="cuda")
+    y = rb.dropout(x, D)
+    f = ref.kept(3, 1000, D)
+    assert (y.cpu()[f == 0] == 0).all() and torch.isnan(y.cpu()[f > 0]).all()
+    assert (rb.dropout(x, rb.Drop(1.0, 1, 2)) == 0).all()
+
+
+def test_dropouts_gradient_is_the_same_call():
+    x = make(20, 333, BF16).requires_grad_()
+    y = rb.dropout(x, D)
+    c = make(20, 333, BF16, seed=2)
+    y.backward(c)
+    assert torch.equal(x.grad, rb.dropout(c, D))
+    x.grad = None
+    rb.dropout(x, D).sum().backward()                     # a gradient that is broadcast
+    assert torch.equal(x.grad, rb.dropout(torch.ones_like(c), D))
+    with pytest.raises(AssertionError):
+        rb.dropout(x, D, out=torch.empty_like(x))
+    # the mask is that of layer norm's sum
+    n = rb.LayerNorm(333, BF16)
+    w = torch.ones(333, dtype=BF16, device="cuda")
+    assert torch.equal(n.forward(c, w, drop=D).total, rb.dropout(c, D))
