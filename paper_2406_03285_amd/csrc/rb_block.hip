@@ -260,7 +260,7 @@ struct rb_attention {
     int32_t heads, kv_heads, dim, max_tokens;
     bool causal;
     ScoreOf score;
-    bool cap;
+    int form;                  // of the scores
     size_t off_lse2, off_delta, bytes;
     char* ws;
 };
@@ -304,17 +304,19 @@ AttentionArgs attention_args(const rb_attention* a, const rb_heads* q, const rb_
     return g;
 }
 
-// The kernel of a head's size, with or without a cap and slopes: `of` is called with these three.
+// The kernel of a head's size, the scores' form and slopes: `of` is called with these three.
 template <typename Of>
 hipError_t by_form(const rb_attention* a, bool slopes, const Of& of)
 {
-    using D64 = std::integral_constant<int, 64>;
-    using D128 = std::integral_constant<int, 128>;
     auto with = [&](auto dim) {
-        if (a->cap) return slopes ? of(dim, std::true_type(), std::true_type()) : of(dim, std::true_type(), std::false_type());
-        return slopes ? of(dim, std::false_type(), std::true_type()) : of(dim, std::false_type(), std::false_type());
+        using Plain = std::integral_constant<int, AT_PLAIN>;
+        using Capped = std::integral_constant<int, AT_CAPPED>;
+        using HighCap = std::integral_constant<int, AT_HIGH_CAP>;
+        if (a->form == AT_PLAIN) return slopes ? of(dim, Plain(), std::true_type()) : of(dim, Plain(), std::false_type());
+        if (a->form == AT_CAPPED) return slopes ? of(dim, Capped(), std::true_type()) : of(dim, Capped(), std::false_type());
+        return of(dim, HighCap(), std::true_type());       // (slopes of 0)
     };
-    return a->dim <= 64 ? with(D64()) : with(D128());
+    return a->dim <= 64 ? with(std::integral_constant<int, 64>()) : with(std::integral_constant<int, 128>());
 }
 
 }  // namespace
@@ -335,10 +337,10 @@ int rb_attention_create(rb_attention** out, int64_t heads, int64_t kv_heads, int
     a->dim = (int32_t)head_dim;
     a->max_tokens = (int32_t)max_tokens;
     a->causal = causal != 0;
-    a->cap = cap > 0.0f;
+    a->form = cap == 0.0f ? AT_PLAIN : cap <= AT_LOW_CAP ? AT_CAPPED : AT_HIGH_CAP;
     a->score.scale = scale;
-    a->score.to_log2 = (a->cap ? cap : scale) * AT_LOG2E;
-    a->score.per_cap = a->cap ? scale / cap : 0.0f;
+    a->score.to_log2 = (cap == 0.0f ? scale : cap) * AT_LOG2E;
+    a->score.to_tanh = cap == 0.0f ? 0.0f : scale / cap * (a->form == AT_CAPPED ? 2 * AT_LOG2E : 1.0f);
     size_t off = round_up((size_t)max_tokens * sizeof(Spans), 256);
     a->off_lse2 = off; off += round_up((size_t)heads * (size_t)max_tokens * sizeof(float), 256);
     a->off_delta = off; off += round_up((size_t)heads * (size_t)max_tokens * sizeof(float), 256);
@@ -374,8 +376,8 @@ int rb_attention_forward(rb_attention* a, const rb_heads* q, const rb_heads* k, 
     g.lse = lse;
     hipError_t e = find_spans(a, documents, tokens, st);
     if (e == hipSuccess)
-        e = by_form(a, slopes != nullptr, [&](auto dim, auto cap, auto lowered) {
-            return launch(rb_attend_kernel<dim(), cap(), lowered()>, dim3((unsigned)(g.tiles * g.heads)), AT_TPB, 0, st, g);
+        e = by_form(a, slopes != nullptr, [&](auto dim, auto form, auto lowered) {
+            return launch(rb_attend_kernel<dim(), form(), lowered()>, dim3((unsigned)(g.tiles * g.heads)), AT_TPB, 0, st, g);
         });
     return e == hipSuccess ? RB_OK : RB_EHIP;
 }
@@ -400,14 +402,15 @@ int rb_attention_grad(rb_attention* a, const rb_heads* q, const rb_heads* k, con
     g.grad_v = rows_of(grad_v);
     g.lse2 = lse2;
     g.delta = delta;
+    g.lse_less = a->form == AT_CAPPED ? a->score.to_log2 : 0.0f;
     hipError_t e = find_spans(a, documents, tokens, st);
     const int64_t rows = tokens * a->heads;
     if (e == hipSuccess) e = launch(rb_attend_delta_kernel, dim3((unsigned)std::min<int64_t>((rows + AT_TPB / 16 - 1) / (AT_TPB / 16), 1 << 20)), AT_TPB, 0, st, g, lse2, delta);
     if (e == hipSuccess)
-        e = by_form(a, slopes != nullptr, [&](auto dim, auto cap, auto lowered) {
-            const hipError_t first = launch(rb_attend_grad_kv_kernel<dim(), cap(), lowered()>, dim3((unsigned)(g.tiles * a->kv_heads)), AT_TPB, 0, st, g);
+        e = by_form(a, slopes != nullptr, [&](auto dim, auto form, auto lowered) {
+            const hipError_t first = launch(rb_attend_grad_kv_kernel<dim(), form(), lowered()>, dim3((unsigned)(g.tiles * a->kv_heads)), AT_TPB, 0, st, g);
             if (first != hipSuccess) return first;
-            return launch(rb_attend_grad_q_kernel<dim(), cap(), lowered()>, dim3((unsigned)(g.tiles * g.heads)), AT_TPB, 0, st, g);
+            return launch(rb_attend_grad_q_kernel<dim(), form(), lowered()>, dim3((unsigned)(g.tiles * g.heads)), AT_TPB, 0, st, g);
         });
     return e == hipSuccess ? RB_OK : RB_EHIP;
 }

@@ -17,6 +17,7 @@
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
+#include <type_traits>
 
 #include "rb_lanes.h"
 
@@ -94,27 +95,37 @@ __device__ __forceinline__ int at_turn(int r)
     return D == 128 ? ((r & 3) << 2) | ((r >> 2) & 3) : (((r >> 1) & 1) << 2) | ((r >> 2) & 3);
 }
 
-// A lane's part in bringing tiles of 64 rows: the same pieces of every tile.
+// A lane's part in bringing tiles of 64 rows of a tensor: the same pieces of every tile.
 template <int D>
 struct Bring {
     static constexpr int PIECES = D / 8, LOADS = AT_TILE * PIECES / AT_TPB, STEP = AT_TILE / LOADS;
     int row, piece, wave;
-    __device__ __forceinline__ Bring(int wave_) : wave(wave_)
+    bool there;                // (pieces behind the head's last number are left as they are: 0)
+    __device__ __forceinline__ Bring(int wave_, int dim) : wave(wave_)
     {
         const int lane = threadIdx.x & 63;
         row = (wave * 64 + lane) / PIECES;
         piece = (lane % PIECES) ^ at_turn<D>(row);
+        there = piece * 8 < dim;
     }
-    // Rows first .. first + 63 of `from`, no further than row `last`.  (Pieces behind the head's last number are left as they are: 0.)
-    __device__ __forceinline__ void operator()(const Bf16* from, int64_t stride, int first, int last, int dim, char* tile) const
+    // Where the lane's piece of a tile's first rows is, relative to the tile's first row.
+    __device__ __forceinline__ int64_t offset(int64_t stride) const { return row * stride + piece * 8; }
+    // Rows first .. first + 63 of the tensor that begins at `from`, no further than row `last`.
+    __device__ __forceinline__ void operator()(const Bf16* from, int64_t stride, int64_t offset, int first, int last, char* tile) const
     {
-        if (piece * 8 >= dim) return;
+        if (!there) return;
+        if (first + AT_TILE <= last + 1) {
+            const Bf16* base = from + first * stride;
 #pragma unroll
-        for (int j = 0; j < LOADS; ++j) {
-            const Bf16* p = from + (int64_t)min(first + j * STEP + row, last) * stride + piece * 8;
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)p,
-                                             (__attribute__((address_space(3))) void*)(tile + (j * AT_WAVES + wave) * 1024), 16, 0, 0);
+            for (int j = 0; j < LOADS; ++j) one(base + j * STEP * stride + offset, tile, j);
+        } else {
+#pragma unroll
+            for (int j = 0; j < LOADS; ++j) one(from + (int64_t)min(first + j * STEP + row, last) * stride + piece * 8, tile, j);
         }
+    }
+    __device__ __forceinline__ void one(const Bf16* p, char* tile, int j) const
+    {
+        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)p, (__attribute__((address_space(3))) void*)(tile + (j * AT_WAVES + wave) * 1024), 16, 0, 0);
     }
 };
 
@@ -183,81 +194,75 @@ __device__ __forceinline__ void at_own(const Bf16* row, int dim, at_bf8 (&f)[D /
     }
 }
 
-// ---- products with what may be masked --------------------------------------------
-//
-// 0 times an infinity or a NaN is no 0: where a tile has both what is masked (a factor of 0) and numbers that are not finite, those are
-// replaced by 0, and products with 1 where something is seen tell where they belong.
-
-__device__ __forceinline__ uint32_t at_not_finite(at_bf8 v)         // not 0 if one of them is
-{
-    const sc_vec w = __builtin_bit_cast(sc_vec, v);
-    uint32_t found = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) found |= (w[i] & 0x7f807f80u) + 0x00800080u;       // (an exponent of ones carries into the sign's place)
-    return found & 0x80008000u;
-}
-
-__device__ __forceinline__ void at_sort_out(at_bf8 v, at_bf8& finite, at_bf8& up, at_bf8& down)
-{
-    at_s8 w = __builtin_bit_cast(at_s8, v), u, d;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const uint16_t x = (uint16_t)w[i];
-        const bool special = (x & 0x7f80) == 0x7f80, nan = special && (x & 0x7f);
-        u[i] = special && (nan || !(x & 0x8000)) ? 0x3f80 : 0;
-        d[i] = special && (nan || (x & 0x8000)) ? 0x3f80 : 0;
-        if (special) w[i] = 0;
-    }
-    finite = __builtin_bit_cast(at_bf8, w);
-    up = __builtin_bit_cast(at_bf8, u);
-    down = __builtin_bit_cast(at_bf8, d);
-}
-
-// sum[n] += columns of the tile's rows 16 (c0 + c) .. times factors[c], for the head's numbers 32 n ...  seen: which factors count, a bit each.
+// sum[n] += columns of the tile's rows 16 (c0 + c) .. times factors[c], for the head's numbers 32 n ..
 template <int D, int C>
-__device__ __forceinline__ void at_add(at_acc (&sum)[D / 32], const at_bf8 (&factors)[C], const Reads<D>& reads, const char* tile, int c0, bool masked, const uint32_t (&seen)[C])
+__device__ __forceinline__ void at_add(at_acc (&sum)[D / 32], const at_bf8 (&factors)[C], const Reads<D>& reads, const char* tile, int c0)
 {
-    if (masked) {
-        uint32_t found = 0;
-#pragma unroll
-        for (int c = 0; c < C; ++c)
-#pragma unroll
-            for (int n = 0; n < D / 32; ++n) found |= at_not_finite(reads.columns(tile, n, c0 + c));
-        if (__any(found != 0)) {
-#pragma unroll
-            for (int n = 0; n < D / 32; ++n) {
-                at_acc ups{}, downs{};
-#pragma unroll
-                for (int c = 0; c < C; ++c) {
-                    at_bf8 finite, up, down;
-                    at_sort_out(reads.columns(tile, n, c0 + c), finite, up, down);
-                    at_s8 one;
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) one[i] = (seen[c] >> i) & 1 ? 0x3f80 : 0;
-                    sum[n] = at_mma(finite, factors[c], sum[n]);
-                    ups = at_mma(up, __builtin_bit_cast(at_bf8, one), ups);
-                    downs = at_mma(down, __builtin_bit_cast(at_bf8, one), downs);
-                }
-#pragma unroll
-                for (int i = 0; i < 16; ++i) sum[n][i] += (ups[i] > 0.0f ? -sc_neg_inf() : 0.0f) + (downs[i] > 0.0f ? sc_neg_inf() : 0.0f);
-            }
-            return;
-        }
-    }
 #pragma unroll
     for (int c = 0; c < C; ++c)
 #pragma unroll
         for (int n = 0; n < D / 32; ++n) sum[n] = at_mma(reads.columns(tile, n, c0 + c), factors[c], sum[n]);
 }
 
-// ---- scores ------------------------------------------------------------------
+// ---- what is not finite where something is masked --------------------------------
+//
+// A masked factor is 0, and 0 times an infinity or a NaN is no 0.  So in tiles of which a row of the workgroup does not see all, the workgroup
+// makes what is not finite 0 before it is multiplied by factors, and notes the rows it was in: who sees one of them makes up for it.
 
-struct ScoreOf {
-    float scale, to_log2;      // of a product; of a score in base 2: scale * log2 e without a cap, cap * log2 e with one
-    float per_cap;             // scale / cap
+struct Noted {
+    uint32_t rows[2][2];       // of this tile and the next, 64 bits each
 };
 
-// tanh within some 2^-23: (near 0 by its series, x^9 left out: 2^-32 of it at 1/8)
+// The pieces of a tile that the thread has brought.  (Between two waits for the workgroup.)
+template <int D>
+__device__ __forceinline__ void at_make_finite(char* tile, int wave, uint32_t (&noted)[2])
+{
+#pragma unroll
+    for (int j = 0; j < Bring<D>::LOADS; ++j) {
+        const int at = (j * AT_WAVES + wave) * 64 + (threadIdx.x & 63);
+        sc_vec w = *reinterpret_cast<const sc_vec*>(tile + at * 16);
+        uint32_t found = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) found |= (w[i] & 0x7f807f80u) + 0x00800080u;       // (an exponent of ones carries into the sign's place)
+        if (found & 0x80008000u) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t m = (((w[i] & 0x7f807f80u) + 0x00800080u) >> 15) & 0x00010001u;
+                w[i] &= ~((m << 16) - m);
+            }
+            *reinterpret_cast<sc_vec*>(tile + at * 16) = w;
+            const int row = at / Bring<D>::PIECES;
+            atomicOr(&noted[row / 32], 1u << (row % 32));
+        }
+    }
+}
+__device__ __forceinline__ void at_wait_for_all() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+// The noted rows among from .. to - 1.
+__device__ __forceinline__ uint64_t at_noted(const uint32_t (&noted)[2], int from, int to)
+{
+    const uint64_t rows = (uint64_t)noted[1] << 32 | noted[0];
+    const int f = min(max(from, 0), 64), t = min(max(to, 0), 64);
+    const uint64_t below_to = t == 64 ? ~0ull : (1ull << t) - 1, below_from = f == 64 ? ~0ull : (1ull << f) - 1;
+    return rows & below_to & ~below_from;
+}
+
+// ---- scores ------------------------------------------------------------------
+//
+// All in base 2.  With r = 1 / (1 + e^2x), tanh x = 1 - 2 r to within 2^-22 (and its slope 4 r (1 - r)), so that a capped score is off by cap * 2^-22 at
+// most: less than what rounding e^score to bfloat16 puts in for caps of up to 32, where more is not worth it.  There the cap is also the maximum
+// that the softmax needs: e^(score - cap) is at least e^-64 for what lies next to a position, and its sums are normal numbers.  Larger caps have
+// scores that are exact near 0, too, and a running maximum.
+enum { AT_PLAIN = 0, AT_CAPPED = 1, AT_HIGH_CAP = 2 };
+constexpr float AT_LOW_CAP = 32.0f;
+
+struct ScoreOf {
+    float scale;               // of a product
+    float to_log2;             // plain: scale * log2 e; else cap * log2 e
+    float to_tanh;             // 2 log2 e scale / cap: 2^(to_tanh * product) = e^2x; of a high cap: scale / cap
+};
+
+// tanh within some 2^-23 of itself (its series near 0: x^9 left out, 2^-32 of it at 1/8).
 __device__ __forceinline__ float at_tanh(float x)
 {
     const float x2 = x * x;
@@ -267,12 +272,18 @@ __device__ __forceinline__ float at_tanh(float x)
     return fabsf(x) < 0.125f ? near : far;
 }
 
-// A score in base 2 of a product; `slope` becomes the cap's derivative.
-template <bool CAP>
+// A score (of AT_CAPPED: less the cap) in base 2, and the cap's slope.
+template <int FORM>
 __device__ __forceinline__ float at_score(const ScoreOf& of, float product, float& slope)
 {
-    if (!CAP) return product * of.to_log2;
-    const float t = at_tanh(product * of.per_cap);
+    if (FORM == AT_PLAIN) return product * of.to_log2;
+    if (FORM == AT_CAPPED) {
+        const float r = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(product * of.to_tanh));
+        const float four = 4.0f * r;
+        slope = fmaf(-four, r, four);
+        return r * (-2.0f * of.to_log2);
+    }
+    const float t = at_tanh(product * of.to_tanh);
     slope = 1.0f - t * t;
     return t * of.to_log2;
 }
@@ -289,7 +300,8 @@ struct AttentionArgs {
     float* lse;
     // gradients
     HeadRows grad_out, grad_q, grad_k, grad_v;
-    const float *lse2, *delta;             // [heads][tokens]: lse in base 2 (+inf where nothing is seen); the sum of grad_out * out
+    const float *lse2, *delta;             // [heads][tokens]: lse in base 2, less lse_less (+inf where nothing is seen); the sum of grad_out * out
+    float lse_less;                        // what scores are less by: of AT_CAPPED the cap
 };
 
 // Which tile and head the workgroup has.  Workgroups go to the 8 dies in turn; a die gets neighbours - the heads of a group, then tiles of one
@@ -312,41 +324,48 @@ __device__ __forceinline__ int at_lowest(int v)
 }
 __device__ __forceinline__ int at_highest(int v) { return -at_lowest(-v); }
 
-// What a wavefront's rows see: all of it lies in [lo, hi), and [all_lo, all_hi) is seen by every row that sees anything.
+// What rows see: all of it lies in [lo, hi), and [all_lo, all_hi) is seen by every row that sees anything.
 struct Reach {
     int lo, hi, all_lo, all_hi;
-    __device__ __forceinline__ Reach(Span s)
+    __device__ __forceinline__ void join(Span s)
     {
-        const bool any = s.lo < s.hi;
-        lo = at_lowest(any ? s.lo : INT32_MAX);
-        hi = at_highest(any ? s.hi : 0);
-        all_lo = at_highest(any ? s.lo : 0);
-        all_hi = at_lowest(any ? s.hi : INT32_MAX);
+        if (s.lo >= s.hi) return;
+        lo = min(lo, s.lo);
+        hi = max(hi, s.hi);
+        all_lo = max(all_lo, s.lo);
+        all_hi = min(all_hi, s.hi);
+    }
+    __device__ __forceinline__ void share()            // of all lanes
+    {
+        lo = at_lowest(lo);
+        hi = at_highest(hi);
+        all_lo = at_highest(all_lo);
+        all_hi = at_lowest(all_hi);
     }
     __device__ __forceinline__ bool meets(int first) const { return first < hi && first + AT_TILE > lo; }
     __device__ __forceinline__ bool whole(int first) const { return first >= all_lo && first + AT_TILE <= all_hi; }
 };
+__device__ __forceinline__ Reach at_reach(Span s)      // of the wavefront's rows, one a lane
+{
+    Reach r{INT32_MAX, 0, 0, INT32_MAX};
+    r.join(s);
+    r.share();
+    return r;
+}
 
-// [lo, hi) of what the rows first .. first + 127 see (SEEN: of what sees them).
+// The same of the workgroup's rows first .. first + 127 (SEEN: of what sees them).
 template <bool SEEN>
-__device__ __forceinline__ void at_range(const Spans* spans, int first, int tokens, int& lo, int& hi)
+__device__ __forceinline__ Reach at_reach(const Spans* spans, int first, int tokens)
 {
     const int lane = threadIdx.x & 63;
-    lo = INT32_MAX;
-    hi = 0;
+    Reach r{INT32_MAX, 0, 0, INT32_MAX};
 #pragma unroll
     for (int i = 0; i < AT_ROWS / 64; ++i) {
         const int t = first + i * 64 + lane;
-        if (t < tokens) {
-            const Span s = SEEN ? spans[t].seen : spans[t].sees;
-            if (s.lo < s.hi) {
-                lo = min(lo, s.lo);
-                hi = max(hi, s.hi);
-            }
-        }
+        if (t < tokens) r.join(SEEN ? spans[t].seen : spans[t].sees);
     }
-    lo = at_lowest(lo);
-    hi = at_highest(hi);
+    r.share();
+    return r;
 }
 
 template <int D>
@@ -376,109 +395,144 @@ __device__ __forceinline__ void at_store(Bf16* row, int dim, const at_acc (&v)[D
 
 // ---- forward -------------------------------------------------------------------
 
-template <int D, bool CAP, bool SLOPES>
+template <int D, int FORM, bool SLOPES>
 __global__ void __launch_bounds__(AT_TPB, 2) rb_attend_kernel(AttentionArgs a)
 {
     __shared__ __align__(1024) char lds[2][2][AT_TILE * D * 2];
+    __shared__ Noted noted;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x & 63, half = lane / 32;
     int tile, head;
     at_place(blockIdx.x, gridDim.x, a.tiles, a.group, tile, head);
     const int kv = head / a.group;
-    int lo, hi;
-    at_range<false>(a.spans, tile * AT_ROWS, a.tokens, lo, hi);
+    const Reach all = at_reach<false>(a.spans, tile * AT_ROWS, a.tokens);
     const int row = tile * AT_ROWS + wave * AT_BLOCK + (lane & 31);
     const Span mine = row < a.tokens ? a.spans[row].sees : Span{0, 0};
-    const Reach reach(mine);
+    const Reach reach = at_reach(mine);
     const int last = a.tokens - 1;
     const Bf16 *const keys = a.k.at(0, kv), *const values = a.v.at(0, kv);
-    const float slope2 = SLOPES ? a.slopes[head] * AT_LOG2E : 0.0f;
+    const float slope2 = SLOPES && a.slopes ? a.slopes[head] * AT_LOG2E : 0.0f;
     at_bf8 q[D / 16];
     at_own<D>(a.q.at(min(row, last), head), a.dim, q);
+    if (threadIdx.x < 4) noted.rows[threadIdx.x / 2][threadIdx.x % 2] = 0;
     at_clear<D>(&lds[0][0][0], sizeof(lds), a.dim);
-    const Bring<D> bring(wave);
+    const Bring<D> bring(wave, a.dim);
     const Reads<D> reads;
+    const int64_t k_offset = bring.offset(a.k.token), v_offset = bring.offset(a.v.token);
     at_acc o[D / 32]{};
-    float m = sc_neg_inf(), l = 0.0f;               // maximum (base 2) and this lane's part of the sum
-    const int count = (hi - lo + AT_TILE - 1) / AT_TILE;        // (nothing seen: lo > hi, no tiles)
-    if (lo < hi) {
-        bring(keys, a.k.token, lo, last, a.dim, lds[0][0]);
-        bring(values, a.v.token, lo, last, a.dim, lds[0][1]);
-    }
-    for (int i = 0; lo < hi && i < count; ++i) {
-        const int first = lo + i * AT_TILE;
-        at_arrived();
-        if (i + 1 < count) {
-            bring(keys, a.k.token, first + AT_TILE, last, a.dim, lds[(i + 1) & 1][0]);
-            bring(values, a.v.token, first + AT_TILE, last, a.dim, lds[(i + 1) & 1][1]);
-        }
-        if (!reach.meets(first)) continue;
-        const char *const kt = lds[i & 1][0], *const vt = lds[i & 1][1];
+    float m = sc_neg_inf(), l = 0.0f;               // maximum (base 2), and this lane's part of the sum
+
+    auto step = [&](bool masked, int first, const char* kt, const char* vt) {
         at_acc s[2]{};
 #pragma unroll
         for (int n = 0; n < D / 16; ++n)
 #pragma unroll
             for (int b = 0; b < 2; ++b) s[b] = at_mma(reads.rows(kt, b, n), q[n], s[b]);
-        const bool masked = !reach.whole(first);
-        uint32_t seen[4] = {~0u, ~0u, ~0u, ~0u};
-        float most = sc_neg_inf();
-        if (CAP || SLOPES) {
+        const int from = mine.lo - first, to = mine.hi - first;        // what the lane's row sees of the tile
+        constexpr bool SCORED = FORM != AT_PLAIN || SLOPES;            // (plain products are scaled in the exponent's own instruction)
+        const float away = (float)(row - first - 4 * half);
+        if (SCORED) {
 #pragma unroll
             for (int b = 0; b < 2; ++b)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
+                    const int key = 32 * b + 8 * (e / 4) + e % 4;
                     float slope;
-                    s[b][e] = at_score<CAP>(a.score, s[b][e], slope);
-                    if (SLOPES) s[b][e] -= slope2 * fabsf((float)(row - first - 32 * b - 8 * (e / 4) - 4 * half - e % 4));
+                    s[b][e] = at_score<FORM>(a.score, s[b][e], slope);
+                    if (SLOPES) s[b][e] = fmaf(-slope2, fabsf(away - (float)key), s[b][e]);
                 }
         }
         if (masked) {
+            asm volatile("");       // (a branch: few tiles need it)
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                seen[c] = 0;
+            for (int b = 0; b < 2; ++b)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const int key = first + 16 * c + 8 * (e / 4) + 4 * half + e % 4;
-                    const bool there = key >= mine.lo && key < mine.hi;
-                    s[c / 2][c % 2 * 8 + e] = there ? s[c / 2][c % 2 * 8 + e] : sc_neg_inf();
-                    seen[c] |= there ? 1u << e : 0u;
+                for (int e = 0; e < 16; ++e) {
+                    const int key = 32 * b + 8 * (e / 4) + 4 * half + e % 4;
+                    s[b][e] = key >= from && key < to ? s[b][e] : sc_neg_inf();
                 }
+        }
+        float base = 0.0f;
+        if (FORM != AT_CAPPED) {
+            float most = sc_neg_inf();
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) most = fmaxf(most, s[b][e]);
+            if (!SCORED) most *= a.score.to_log2;
+            most = fmaxf(most, sc_xor<32>(most));
+            // a maximum that is a little too small does as well: sums up to 2^8 times as large
+            if (__any(most > m + 8.0f)) {
+                const float now = fmaxf(m, most);
+                const float factor = now == sc_neg_inf() ? 1.0f : __builtin_amdgcn_exp2f(m - now);
+                l *= factor;
+#pragma unroll
+                for (int n = 0; n < D / 32; ++n)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) o[n][e] *= factor;
+                m = now;
             }
+            base = m == sc_neg_inf() ? 0.0f : m;
         }
-#pragma unroll
-        for (int b = 0; b < 2; ++b)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) most = fmaxf(most, s[b][e]);
-        if (!CAP && !SLOPES) most *= a.score.to_log2;
-        most = fmaxf(most, sc_xor<32>(most));
-        if (__any(most > m)) {
-            const float now = fmaxf(m, most);
-            const float factor = now == sc_neg_inf() ? 1.0f : __builtin_amdgcn_exp2f(m - now);
-            l *= factor;
-#pragma unroll
-            for (int n = 0; n < D / 32; ++n)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) o[n][e] *= factor;
-            m = now;
-        }
-        const float base = m == sc_neg_inf() ? 0.0f : m;
         at_bf8 p[4];
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
-                s[b][e] = __builtin_amdgcn_exp2f(CAP || SLOPES ? s[b][e] - base : fmaf(s[b][e], a.score.to_log2, -base));
+                s[b][e] = __builtin_amdgcn_exp2f(!SCORED ? fmaf(s[b][e], a.score.to_log2, -base) : FORM == AT_CAPPED ? s[b][e] : s[b][e] - base);
                 l += s[b][e];
             }
             p[2 * b] = at_pack(s[b], 0);
             p[2 * b + 1] = at_pack(s[b], 1);
         }
-        at_add<D, 4>(o, p, reads, vt, 0, masked, seen);
+        at_add<D, 4>(o, p, reads, vt, 0);
+    };
+
+    const int count = all.lo < all.hi ? (all.hi - all.lo + AT_TILE - 1) / AT_TILE : 0;
+    if (count > 0) {
+        bring(keys, a.k.token, k_offset, all.lo, last, lds[0][0]);
+        bring(values, a.v.token, v_offset, all.lo, last, lds[0][1]);
+    }
+    for (int i = 0; i < count; ++i) {
+        const int first = all.lo + i * AT_TILE, now = i & 1;
+        at_arrived();
+        if (threadIdx.x < 2) noted.rows[now ^ 1][threadIdx.x] = 0;
+        if (i + 1 < count) {
+            bring(keys, a.k.token, k_offset, first + AT_TILE, last, lds[now ^ 1][0]);
+            bring(values, a.v.token, v_offset, first + AT_TILE, last, lds[now ^ 1][1]);
+        }
+        const bool all_see = all.whole(first);
+        if (!all_see) {
+            at_make_finite<D>(lds[now][1], wave, noted.rows[now]);
+            at_wait_for_all();
+        }
+        if (!reach.meets(first)) continue;
+        step(!reach.whole(first), first, lds[now][0], lds[now][1]);
+        if (!all_see && (noted.rows[now][0] | noted.rows[now][1]) != 0) {
+            // what was not finite and is seen, from where the tile came from
+            const uint64_t rows = at_noted(noted.rows[now], 0, 64), mine_of = at_noted(noted.rows[now], mine.lo - first, mine.hi - first);
+#pragma unroll 1
+            for (uint64_t left = rows; left; left &= left - 1) {
+                const int r = __builtin_ctzll(left);
+                const bool seen = mine_of >> r & 1;
+                const Bf16* const from = values + (int64_t)min(first + r, last) * a.v.token + 4 * half;
+#pragma unroll
+                for (int n = 0; n < D / 32; ++n)
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) {
+                        uint2 w{0, 0};
+                        if (32 * n + 8 * g < a.dim) w = *reinterpret_cast<const uint2*>(from + 32 * n + 8 * g);
+                        const uint32_t x[4] = {w.x << 16, w.x & 0xffff0000u, w.y << 16, w.y & 0xffff0000u};
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) o[n][4 * g + e] += seen && (x[e] & 0x7f800000u) == 0x7f800000u ? __uint_as_float(x[e]) : 0.0f;
+                    }
+            }
+        }
     }
     if (row >= a.tokens) return;
     l += sc_xor<32>(l);
     const bool empty = mine.lo >= mine.hi;
     at_store<D>(a.out.at(row, head), a.dim, o, 1.0f / l, empty);
-    if (a.lse && half == 0) a.lse[(int64_t)head * a.tokens + row] = empty ? sc_neg_inf() : (m + __log2f(l)) * AT_LN2;
+    if (a.lse && half == 0) a.lse[(int64_t)head * a.tokens + row] = empty ? sc_neg_inf() : ((FORM == AT_CAPPED ? a.score.to_log2 : m) + __log2f(l)) * AT_LN2;
 }
 
 // ---- gradients -----------------------------------------------------------------
@@ -507,67 +561,57 @@ __global__ void __launch_bounds__(AT_TPB) rb_attend_delta_kernel(AttentionArgs a
             const Span s = a.spans[t].sees;
             const int64_t to = (int64_t)h * a.tokens + t;
             delta[to] = sum;
-            lse2[to] = s.lo < s.hi ? a.lse[to] * AT_LOG2E : -sc_neg_inf();
+            lse2[to] = s.lo < s.hi ? a.lse[to] * AT_LOG2E - a.lse_less : -sc_neg_inf();
         }
     }
 }
 
-// p and ds of one element.
-template <bool CAP, bool SLOPES>
-__device__ __forceinline__ void at_slope(const ScoreOf& of, float product, float dp, float lse2, float delta, float lowered, float& p, float& ds)
+// p and ds of one element; less: lse in base 2 (of AT_CAPPED: less the cap) and what the score is lowered by.
+template <int FORM, bool SLOPES>
+__device__ __forceinline__ void at_slope(const ScoreOf& of, float product, float dp, float less, float delta, float& p, float& ds)
 {
     float slope = 1.0f;
-    if (CAP || SLOPES) {
-        float s = at_score<CAP>(of, product, slope);
-        if (SLOPES) s -= lowered;
-        p = __builtin_amdgcn_exp2f(s - lse2);
+    if (FORM != AT_PLAIN) {
+        const float s = at_score<FORM>(of, product, slope);
+        p = __builtin_amdgcn_exp2f(s - less);
     } else {
-        p = __builtin_amdgcn_exp2f(fmaf(product, of.to_log2, -lse2));
+        p = __builtin_amdgcn_exp2f(fmaf(product, of.to_log2, -less));
     }
     ds = p * (dp - delta);
-    if (CAP) ds *= slope;
+    if (FORM != AT_PLAIN) ds *= slope;
 }
 
 // Of queries: as forward, with the scores made again.
-template <int D, bool CAP, bool SLOPES>
+template <int D, int FORM, bool SLOPES>
 __global__ void __launch_bounds__(AT_TPB, 2) rb_attend_grad_q_kernel(AttentionArgs a)
 {
     __shared__ __align__(1024) char lds[2][2][AT_TILE * D * 2];
+    __shared__ Noted noted;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x & 63, half = lane / 32;
     int tile, head;
     at_place(blockIdx.x, gridDim.x, a.tiles, a.group, tile, head);
     const int kv = head / a.group;
-    int lo, hi;
-    at_range<false>(a.spans, tile * AT_ROWS, a.tokens, lo, hi);
+    const Reach all = at_reach<false>(a.spans, tile * AT_ROWS, a.tokens);
     const int row = tile * AT_ROWS + wave * AT_BLOCK + (lane & 31);
     const Span mine = row < a.tokens ? a.spans[row].sees : Span{0, 0};
-    const Reach reach(mine);
+    const Reach reach = at_reach(mine);
     const int last = a.tokens - 1, r = min(row, last);
     const Bf16 *const keys = a.k.at(0, kv), *const values = a.v.at(0, kv);
-    const float slope2 = SLOPES ? a.slopes[head] * AT_LOG2E : 0.0f;
+    const float slope2 = SLOPES && a.slopes ? a.slopes[head] * AT_LOG2E : 0.0f;
     at_bf8 q[D / 16], go[D / 16];
     at_own<D>(a.q.at(r, head), a.dim, q);
     at_own<D>(a.grad_out.at(r, head), a.dim, go);
     const float lse2 = a.lse2[(int64_t)head * a.tokens + r], delta = a.delta[(int64_t)head * a.tokens + r];
+    if (threadIdx.x < 4) noted.rows[threadIdx.x / 2][threadIdx.x % 2] = 0;
     at_clear<D>(&lds[0][0][0], sizeof(lds), a.dim);
-    const Bring<D> bring(wave);
+    const Bring<D> bring(wave, a.dim);
     const Reads<D> reads;
+    const int64_t k_offset = bring.offset(a.k.token), v_offset = bring.offset(a.v.token);
     at_acc dq[D / 32]{};
-    const int count = (hi - lo + AT_TILE - 1) / AT_TILE;
-    if (lo < hi) {
-        bring(keys, a.k.token, lo, last, a.dim, lds[0][0]);
-        bring(values, a.v.token, lo, last, a.dim, lds[0][1]);
-    }
-    for (int i = 0; lo < hi && i < count; ++i) {
-        const int first = lo + i * AT_TILE;
-        at_arrived();
-        if (i + 1 < count) {
-            bring(keys, a.k.token, first + AT_TILE, last, a.dim, lds[(i + 1) & 1][0]);
-            bring(values, a.v.token, first + AT_TILE, last, a.dim, lds[(i + 1) & 1][1]);
-        }
-        if (!reach.meets(first)) continue;
-        const char *const kt = lds[i & 1][0], *const vt = lds[i & 1][1];
-        const bool masked = !reach.whole(first);
+
+    auto step = [&](bool masked, int first, const char* kt, const char* vt) {
+        const int from = mine.lo - first, to = mine.hi - first;
+        const float away = (float)(row - first - 4 * half);
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
             at_acc s{}, dp{};
@@ -576,122 +620,152 @@ __global__ void __launch_bounds__(AT_TPB, 2) rb_attend_grad_q_kernel(AttentionAr
                 s = at_mma(reads.rows(kt, b, n), q[n], s);
                 dp = at_mma(reads.rows(vt, b, n), go[n], dp);
             }
-            uint32_t seen[2] = {~0u, ~0u};
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
+                const int key = 32 * b + 8 * (e / 4) + e % 4;
                 float p, ds;
-                at_slope<CAP, SLOPES>(a.score, s[e], dp[e], lse2, delta,
-                                      SLOPES ? slope2 * fabsf((float)(row - first - 32 * b - 8 * (e / 4) - 4 * half - e % 4)) : 0.0f, p, ds);
+                at_slope<FORM, SLOPES>(a.score, s[e], dp[e], SLOPES ? fmaf(slope2, fabsf(away - (float)key), lse2) : lse2, delta, p, ds);
                 s[e] = ds;
             }
             if (masked) {
-                seen[0] = seen[1] = 0;
+            asm volatile("");       // (a branch: few tiles need it)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
-                    const int key = first + 32 * b + 8 * (e / 4) + 4 * half + e % 4;
-                    const bool there = key >= mine.lo && key < mine.hi;
-                    s[e] = there ? s[e] : 0.0f;
-                    seen[e / 8] |= there ? 1u << (e % 8) : 0u;
+                    const int key = 32 * b + 8 * (e / 4) + 4 * half + e % 4;
+                    s[e] = key >= from && key < to ? s[e] : 0.0f;
                 }
             }
             const at_bf8 f[2] = {at_pack(s, 0), at_pack(s, 1)};
-            at_add<D, 2>(dq, f, reads, kt, 2 * b, masked, seen);
+            at_add<D, 2>(dq, f, reads, kt, 2 * b);
         }
+    };
+
+    bool lost = false;                              // the row sees a key that is not finite
+    const int count = all.lo < all.hi ? (all.hi - all.lo + AT_TILE - 1) / AT_TILE : 0;
+    if (count > 0) {
+        bring(keys, a.k.token, k_offset, all.lo, last, lds[0][0]);
+        bring(values, a.v.token, v_offset, all.lo, last, lds[0][1]);
+    }
+    for (int i = 0; i < count; ++i) {
+        const int first = all.lo + i * AT_TILE, now = i & 1;
+        at_arrived();
+        if (threadIdx.x < 2) noted.rows[now ^ 1][threadIdx.x] = 0;
+        if (i + 1 < count) {
+            bring(keys, a.k.token, k_offset, first + AT_TILE, last, lds[now ^ 1][0]);
+            bring(values, a.v.token, v_offset, first + AT_TILE, last, lds[now ^ 1][1]);
+        }
+        if (!all.whole(first)) {
+            at_make_finite<D>(lds[now][0], wave, noted.rows[now]);
+            at_wait_for_all();
+            lost |= at_noted(noted.rows[now], mine.lo - first, mine.hi - first) != 0;
+        }
+        if (reach.meets(first)) step(!reach.whole(first), first, lds[now][0], lds[now][1]);
     }
     if (row >= a.tokens) return;
-    at_store<D>(a.grad_q.at(row, head), a.dim, dq, a.score.scale, mine.lo >= mine.hi);
+    at_store<D>(a.grad_q.at(row, head), a.dim, dq, lost ? sc_nan() : a.score.scale, mine.lo >= mine.hi);
 }
 
 // Of keys and values: a workgroup has 128 of one head, and goes through the queries of all the heads that read it.
-template <int D, bool CAP, bool SLOPES>
+template <int D, int FORM, bool SLOPES>
 __global__ void __launch_bounds__(AT_TPB, 1) rb_attend_grad_kv_kernel(AttentionArgs a)
 {
     __shared__ __align__(1024) char lds[2][2][AT_TILE * D * 2];
+    __shared__ Noted noted;
     __shared__ __align__(1024) float numbers[2][2][AT_TILE];          // lse in base 2 and delta of the tile's queries
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x & 63, half = lane / 32;
     int tile, kv;
     at_place(blockIdx.x, gridDim.x, a.tiles, 1, tile, kv);
-    int lo, hi;
-    at_range<true>(a.spans, tile * AT_ROWS, a.tokens, lo, hi);
+    const Reach all = at_reach<true>(a.spans, tile * AT_ROWS, a.tokens);
     const int row = tile * AT_ROWS + wave * AT_BLOCK + (lane & 31);
     const Span mine = row < a.tokens ? a.spans[row].seen : Span{0, 0};
-    const Reach reach(mine);
+    const Reach reach = at_reach(mine);
     const int last = a.tokens - 1;
     at_bf8 k[D / 16], v[D / 16];
     at_own<D>(a.k.at(min(row, last), kv), a.dim, k);
     at_own<D>(a.v.at(min(row, last), kv), a.dim, v);
+    if (threadIdx.x < 4) noted.rows[threadIdx.x / 2][threadIdx.x % 2] = 0;
     at_clear<D>(&lds[0][0][0], sizeof(lds), a.dim);
-    const Bring<D> bring(wave);
+    const Bring<D> bring(wave, a.dim);
     const Reads<D> reads;
+    const int64_t q_offset = bring.offset(a.q.token), g_offset = bring.offset(a.grad_out.token);
     auto fetch = [&](int head, int first, int buffer) {
-        bring(a.q.at(0, head), a.q.token, first, last, a.dim, lds[buffer][0]);
-        bring(a.grad_out.at(0, head), a.grad_out.token, first, last, a.dim, lds[buffer][1]);
+        bring(a.q.at(0, head), a.q.token, q_offset, first, last, lds[buffer][0]);
+        bring(a.grad_out.at(0, head), a.grad_out.token, g_offset, first, last, lds[buffer][1]);
         if (wave == 0) at_bring_numbers(a.lse2 + (int64_t)head * a.tokens, first, last, numbers[buffer][0]);
         if (wave == 1) at_bring_numbers(a.delta + (int64_t)head * a.tokens, first, last, numbers[buffer][1]);
     };
     at_acc dk[D / 32]{}, dv[D / 32]{};
-    int head = kv * a.group, first = lo, left = lo < hi ? (hi - lo + AT_TILE - 1) / AT_TILE * a.group : 0;
+
+    auto step = [&](bool masked, int first, int head, int buffer) {
+        const char *const qt = lds[buffer][0], *const gt = lds[buffer][1];
+        const float slope2 = SLOPES && a.slopes ? a.slopes[head] * AT_LOG2E : 0.0f;
+        const int from = mine.lo - first, to = mine.hi - first;
+        const float away = (float)(row - first - 4 * half);
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            at_acc s{}, dp{};
+#pragma unroll
+            for (int n = 0; n < D / 16; ++n) {
+                s = at_mma(reads.rows(qt, b, n), k[n], s);
+                dp = at_mma(reads.rows(gt, b, n), v[n], dp);
+            }
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const float4 lse2 = *reinterpret_cast<const float4*>(&numbers[buffer][0][32 * b + 8 * g + 4 * half]);
+                const float4 delta = *reinterpret_cast<const float4*>(&numbers[buffer][1][32 * b + 8 * g + 4 * half]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int e = 4 * g + i, query = 32 * b + 8 * g + i;
+                    const float less = i == 0 ? lse2.x : i == 1 ? lse2.y : i == 2 ? lse2.z : lse2.w;
+                    const float delta_i = i == 0 ? delta.x : i == 1 ? delta.y : i == 2 ? delta.z : delta.w;
+                    float p, ds;
+                    at_slope<FORM, SLOPES>(a.score, s[e], dp[e], SLOPES ? fmaf(slope2, fabsf(away - (float)query), less) : less, delta_i, p, ds);
+                    s[e] = p;
+                    dp[e] = ds;
+                }
+            }
+            if (masked) {
+            asm volatile("");       // (a branch: few tiles need it)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const int query = 32 * b + 8 * (e / 4) + 4 * half + e % 4;
+                    const bool seen = query >= from && query < to;
+                    s[e] = seen ? s[e] : 0.0f;
+                    dp[e] = seen ? dp[e] : 0.0f;
+                }
+            }
+            const at_bf8 p[2] = {at_pack(s, 0), at_pack(s, 1)}, ds[2] = {at_pack(dp, 0), at_pack(dp, 1)};
+            at_add<D, 2>(dv, p, reads, gt, 2 * b);
+            at_add<D, 2>(dk, ds, reads, qt, 2 * b);
+        }
+    };
+
+    bool lost = false;                              // seen by a query that is not finite, or whose gradient is not
+    int head = kv * a.group, first = all.lo, left = all.lo < all.hi ? (all.hi - all.lo + AT_TILE - 1) / AT_TILE * a.group : 0;
     if (left) fetch(head, first, 0);
-    for (int buffer = 0; left > 0; --left, buffer ^= 1) {
+    for (int now = 0; left > 0; --left, now ^= 1) {
         int next_head = head, next = first + AT_TILE;
-        if (next >= hi) {
-            next = lo;
+        if (next >= all.hi) {
+            next = all.lo;
             ++next_head;
         }
         at_arrived();
-        if (left > 1) fetch(next_head, next, buffer ^ 1);
-        if (reach.meets(first)) {
-            const char *const qt = lds[buffer][0], *const gt = lds[buffer][1];
-            const bool masked = !reach.whole(first);
-            const float slope2 = SLOPES ? a.slopes[head] * AT_LOG2E : 0.0f;
-#pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                at_acc s{}, dp{};
-#pragma unroll
-                for (int n = 0; n < D / 16; ++n) {
-                    s = at_mma(reads.rows(qt, b, n), k[n], s);
-                    dp = at_mma(reads.rows(gt, b, n), v[n], dp);
-                }
-                uint32_t seen[2] = {~0u, ~0u};
-#pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    const float4 lse2 = *reinterpret_cast<const float4*>(&numbers[buffer][0][32 * b + 8 * g + 4 * half]);
-                    const float4 delta = *reinterpret_cast<const float4*>(&numbers[buffer][1][32 * b + 8 * g + 4 * half]);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int e = 4 * g + i;
-                        const float lse2_i = i == 0 ? lse2.x : i == 1 ? lse2.y : i == 2 ? lse2.z : lse2.w;
-                        const float delta_i = i == 0 ? delta.x : i == 1 ? delta.y : i == 2 ? delta.z : delta.w;
-                        float p, ds;
-                        at_slope<CAP, SLOPES>(a.score, s[e], dp[e], lse2_i, delta_i,
-                                              SLOPES ? slope2 * fabsf((float)(row - first - 32 * b - 8 * g - 4 * half - i)) : 0.0f, p, ds);
-                        s[e] = p;
-                        dp[e] = ds;
-                    }
-                }
-                if (masked) {
-                    seen[0] = seen[1] = 0;
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        const int query = first + 32 * b + 8 * (e / 4) + 4 * half + e % 4;
-                        const bool there = query >= mine.lo && query < mine.hi;
-                        s[e] = there ? s[e] : 0.0f;
-                        dp[e] = there ? dp[e] : 0.0f;
-                        seen[e / 8] |= there ? 1u << (e % 8) : 0u;
-                    }
-                }
-                const at_bf8 p[2] = {at_pack(s, 0), at_pack(s, 1)}, ds[2] = {at_pack(dp, 0), at_pack(dp, 1)};
-                at_add<D, 2>(dv, p, reads, gt, 2 * b, masked, seen);
-                at_add<D, 2>(dk, ds, reads, qt, 2 * b, masked, seen);
-            }
+        if (threadIdx.x < 2) noted.rows[now ^ 1][threadIdx.x] = 0;
+        if (left > 1) fetch(next_head, next, now ^ 1);
+        if (!all.whole(first)) {
+            at_make_finite<D>(lds[now][0], wave, noted.rows[now]);
+            at_make_finite<D>(lds[now][1], wave, noted.rows[now]);
+            at_wait_for_all();
+            lost |= at_noted(noted.rows[now], mine.lo - first, mine.hi - first) != 0;
         }
+        if (reach.meets(first)) step(!reach.whole(first), first, head, now);
         head = next_head;
         first = next;
     }
     if (row >= a.tokens) return;
     const bool empty = mine.lo >= mine.hi;
-    at_store<D>(a.grad_k.at(row, kv), a.dim, dk, a.score.scale, empty);
-    at_store<D>(a.grad_v.at(row, kv), a.dim, dv, 1.0f, empty);
+    at_store<D>(a.grad_k.at(row, kv), a.dim, dk, lost ? sc_nan() : a.score.scale, empty);
+    at_store<D>(a.grad_v.at(row, kv), a.dim, dv, lost ? sc_nan() : 1.0f, empty);
 }
 
 }  // namespace
