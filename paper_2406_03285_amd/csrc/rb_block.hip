@@ -261,11 +261,29 @@ struct rb_attention {
     bool causal;
     ScoreOf score;
     int form;                  // of the scores
-    size_t off_lse2, off_delta, bytes;
+    size_t off_lse2, off_delta, off_sums, bytes;
     char* ws;
 };
 
 namespace {
+
+// Workgroups that the gradients of keys and values are cut into at least, where there are heads enough.
+constexpr int64_t AT_KEY_GROUPS = 512;
+
+// Into how many parts the heads of queries that read one head of keys are cut.
+inline int key_parts(const rb_attention* a, int64_t tiles)
+{
+    const int64_t group = a->heads / a->kv_heads, groups = tiles * a->kv_heads;
+    return (int)std::min<int64_t>(group, (AT_KEY_GROUPS + groups - 1) / groups);
+}
+
+// Heads of one die that take turns (0: dies have no heads of their own): those that read the same keys.
+inline int inner_heads(int64_t heads, int64_t group)
+{
+    if (heads % 8 != 0) return 0;
+    const int64_t of_die = heads / 8;
+    return (int)(of_die % group == 0 ? group : group % of_die == 0 ? of_die : 1);
+}
 
 bool heads_fit(const rb_attention* a, const rb_heads* t, bool written)
 {
@@ -301,6 +319,7 @@ AttentionArgs attention_args(const rb_attention* a, const rb_heads* q, const rb_
     g.heads = a->heads;
     g.group = a->heads / a->kv_heads;
     g.tiles = (int32_t)((tokens + AT_ROWS - 1) / AT_ROWS);
+    g.inner = inner_heads(a->heads, g.group);
     return g;
 }
 
@@ -344,6 +363,10 @@ int rb_attention_create(rb_attention** out, int64_t heads, int64_t kv_heads, int
     size_t off = round_up((size_t)max_tokens * sizeof(Spans), 256);
     a->off_lse2 = off; off += round_up((size_t)heads * (size_t)max_tokens * sizeof(float), 256);
     a->off_delta = off; off += round_up((size_t)heads * (size_t)max_tokens * sizeof(float), 256);
+    a->off_sums = off;
+    // (most workgroups of a launch whose groups are cut into parts, with one part more than would be needed)
+    const size_t tiles = ((size_t)max_tokens + AT_ROWS - 1) / AT_ROWS;
+    if (heads > kv_heads) off += std::min((size_t)heads * tiles, (size_t)2 * AT_KEY_GROUPS) * AT_ROWS * 2 * (head_dim <= 64 ? 64 : 128) * sizeof(float);
     a->bytes = off;
     *out = a;
     return RB_OK;
@@ -403,13 +426,22 @@ int rb_attention_grad(rb_attention* a, const rb_heads* q, const rb_heads* k, con
     g.lse2 = lse2;
     g.delta = delta;
     g.lse_less = a->form == AT_CAPPED ? a->score.to_log2 : 0.0f;
+    const int parts = key_parts(a, g.tiles);
+    AttentionArgs of_keys = g;
+    of_keys.shares = a->kv_heads * parts;
+    of_keys.inner = inner_heads(of_keys.shares, parts);
+    of_keys.sums = parts > 1 ? reinterpret_cast<float*>(a->ws + a->off_sums) : nullptr;
     hipError_t e = find_spans(a, documents, tokens, st);
     const int64_t rows = tokens * a->heads;
     if (e == hipSuccess) e = launch(rb_attend_delta_kernel, dim3((unsigned)std::min<int64_t>((rows + AT_TPB / 16 - 1) / (AT_TPB / 16), 1 << 20)), AT_TPB, 0, st, g, lse2, delta);
     if (e == hipSuccess)
         e = by_form(a, slopes != nullptr, [&](auto dim, auto form, auto lowered) {
-            const hipError_t first = launch(rb_attend_grad_kv_kernel<dim(), form(), lowered()>, dim3((unsigned)(g.tiles * a->kv_heads)), AT_TPB, 0, st, g);
-            if (first != hipSuccess) return first;
+            hipError_t r = launch(rb_attend_grad_kv_kernel<dim(), form(), lowered()>, dim3((unsigned)(g.tiles * of_keys.shares)), AT_TPB, 0, st, of_keys);
+            if (r == hipSuccess && parts > 1) {
+                const int64_t threads = (int64_t)a->kv_heads * tokens * (2 * dim() / 4);
+                r = launch(rb_attend_join_kernel<dim()>, dim3((unsigned)std::min<int64_t>((threads + AT_TPB - 1) / AT_TPB, 1 << 16)), AT_TPB, 0, st, of_keys);
+            }
+            if (r != hipSuccess) return r;
             return launch(rb_attend_grad_q_kernel<dim(), form(), lowered()>, dim3((unsigned)(g.tiles * g.heads)), AT_TPB, 0, st, g);
         });
     return e == hipSuccess ? RB_OK : RB_EHIP;

@@ -294,7 +294,9 @@ struct AttentionArgs {
     const float* slopes;
     ScoreOf score;
     int32_t tokens, dim, heads, group;     // group: heads of queries to one of keys
-    int32_t tiles;
+    int32_t tiles, inner;
+    int32_t shares;                        // gradients of keys: heads of keys, times the parts that a group is cut into
+    float* sums;                           // of the parts: [shares][tokens][2][D]; null: groups are not cut
     // forward: written; gradients: read
     HeadRows out;
     float* lse;
@@ -304,16 +306,23 @@ struct AttentionArgs {
     float lse_less;                        // what scores are less by: of AT_CAPPED the cap
 };
 
-// Which tile and head the workgroup has.  Workgroups go to the 8 dies in turn; a die gets neighbours - the heads of a group, then tiles of one
-// head of keys - whose keys it then finds in its own L2.  Tiles are taken from both ends in turn: the first ones of a causal document see little, the last all.
-__device__ __forceinline__ void at_place(int id, int count, int tiles, int inner, int& tile, int& head)
+// Which tile and head the workgroup has.  Workgroups go to the 8 dies in turn, and each die has its own L2: a die gets heads of its own (where their number
+// allows it), those that read the same keys at a time.  `inner` of them take turns; their longest tiles come first: the last of a causal document for
+// queries, the first for keys (UP).
+template <bool UP>
+__device__ __forceinline__ void at_place(int id, int tiles, int heads, int inner, int& tile, int& head)
 {
-    const int die = id & 7, whole = count >> 3, more = count & 7;
-    const int rank = die * whole + min(die, more) + (id >> 3);
-    const int outer = rank / inner, in = rank - outer * inner;
-    const int t = outer % tiles, kv = outer / tiles;
-    tile = t & 1 ? t / 2 : tiles - 1 - t / 2;
-    head = kv * inner + in;
+    int t;
+    if (inner > 0) {
+        const int die = id & 7, i = id >> 3, outer = i / inner;
+        const int round = outer / tiles;
+        t = outer - round * tiles;
+        head = die * (heads >> 3) + round * inner + (i - outer * inner);
+    } else {
+        t = id / heads;
+        head = id - t * heads;
+    }
+    tile = UP ? t : tiles - 1 - t;
 }
 
 __device__ __forceinline__ int at_lowest(int v)
@@ -393,6 +402,21 @@ __device__ __forceinline__ void at_store(Bf16* row, int dim, const at_acc (&v)[D
         }
 }
 
+// The same unrounded.
+template <int D>
+__device__ __forceinline__ void at_store_sum(float* row, const at_acc (&v)[D / 32], float factor, bool zero)
+{
+    const int half = (threadIdx.x >> 5) & 1;
+#pragma unroll
+    for (int n = 0; n < D / 32; ++n)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            float4 w{0.0f, 0.0f, 0.0f, 0.0f};
+            if (!zero) w = float4{v[n][4 * g] * factor, v[n][4 * g + 1] * factor, v[n][4 * g + 2] * factor, v[n][4 * g + 3] * factor};
+            *reinterpret_cast<float4*>(row + 32 * n + 8 * g + 4 * half) = w;
+        }
+}
+
 // ---- forward -------------------------------------------------------------------
 
 template <int D, int FORM, bool SLOPES>
@@ -402,7 +426,7 @@ __global__ void __launch_bounds__(AT_TPB, 2) rb_attend_kernel(AttentionArgs a)
     __shared__ Noted noted;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x & 63, half = lane / 32;
     int tile, head;
-    at_place(blockIdx.x, gridDim.x, a.tiles, a.group, tile, head);
+    at_place<false>(blockIdx.x, a.tiles, a.heads, a.inner, tile, head);
     const int kv = head / a.group;
     const Reach all = at_reach<false>(a.spans, tile * AT_ROWS, a.tokens);
     const int row = tile * AT_ROWS + wave * AT_BLOCK + (lane & 31);
@@ -589,7 +613,7 @@ __global__ void __launch_bounds__(AT_TPB, 2) rb_attend_grad_q_kernel(AttentionAr
     __shared__ Noted noted;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x & 63, half = lane / 32;
     int tile, head;
-    at_place(blockIdx.x, gridDim.x, a.tiles, a.group, tile, head);
+    at_place<false>(blockIdx.x, a.tiles, a.heads, a.inner, tile, head);
     const int kv = head / a.group;
     const Reach all = at_reach<false>(a.spans, tile * AT_ROWS, a.tokens);
     const int row = tile * AT_ROWS + wave * AT_BLOCK + (lane & 31);
@@ -673,8 +697,11 @@ __global__ void __launch_bounds__(AT_TPB, 1) rb_attend_grad_kv_kernel(AttentionA
     __shared__ Noted noted;
     __shared__ __align__(1024) float numbers[2][2][AT_TILE];          // lse in base 2 and delta of the tile's queries
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x & 63, half = lane / 32;
-    int tile, kv;
-    at_place(blockIdx.x, gridDim.x, a.tiles, 1, tile, kv);
+    // one workgroup's share of the queries' heads: all of the group, or a part of it
+    int tile, share;
+    at_place<true>(blockIdx.x, a.tiles, a.shares, a.inner, tile, share);
+    const int parts = a.shares / (a.heads / a.group), kv = share / parts, part = share - kv * parts;
+    const int head_from = kv * a.group + a.group * part / parts, head_to = kv * a.group + a.group * (part + 1) / parts;
     const Reach all = at_reach<true>(a.spans, tile * AT_ROWS, a.tokens);
     const int row = tile * AT_ROWS + wave * AT_BLOCK + (lane & 31);
     const Span mine = row < a.tokens ? a.spans[row].seen : Span{0, 0};
@@ -741,7 +768,7 @@ __global__ void __launch_bounds__(AT_TPB, 1) rb_attend_grad_kv_kernel(AttentionA
     };
 
     bool lost = false;                              // seen by a query that is not finite, or whose gradient is not
-    int head = kv * a.group, first = all.lo, left = all.lo < all.hi ? (all.hi - all.lo + AT_TILE - 1) / AT_TILE * a.group : 0;
+    int head = head_from, first = all.lo, left = all.lo < all.hi ? (all.hi - all.lo + AT_TILE - 1) / AT_TILE * (head_to - head_from) : 0;
     if (left) fetch(head, first, 0);
     for (int now = 0; left > 0; --left, now ^= 1) {
         int next_head = head, next = first + AT_TILE;
@@ -764,8 +791,37 @@ __global__ void __launch_bounds__(AT_TPB, 1) rb_attend_grad_kv_kernel(AttentionA
     }
     if (row >= a.tokens) return;
     const bool empty = mine.lo >= mine.hi;
+    if (a.sums) {
+        float* const to = a.sums + ((int64_t)share * a.tokens + row) * (2 * D);
+        at_store_sum<D>(to, dk, lost ? sc_nan() : a.score.scale, empty);
+        at_store_sum<D>(to + D, dv, lost ? sc_nan() : 1.0f, empty);
+        return;
+    }
     at_store<D>(a.grad_k.at(row, kv), a.dim, dk, lost ? sc_nan() : a.score.scale, empty);
     at_store<D>(a.grad_v.at(row, kv), a.dim, dv, lost ? sc_nan() : 1.0f, empty);
+}
+
+// Gradients of keys and values from the parts' sums: a thread has four numbers of a row of one head.
+template <int D>
+__global__ void __launch_bounds__(AT_TPB) rb_attend_join_kernel(AttentionArgs a)
+{
+    const int kv_heads = a.heads / a.group, parts = a.shares / kv_heads;
+    const int64_t count = (int64_t)kv_heads * a.tokens * (2 * D / 4);
+    for (int64_t at = (int64_t)blockIdx.x * AT_TPB + threadIdx.x; at < count; at += (int64_t)gridDim.x * AT_TPB) {
+        const int64_t line = at / (2 * D / 4);
+        const int kv = (int)(line / a.tokens), t = (int)(line - (int64_t)kv * a.tokens), first = (int)(at % (2 * D / 4)) * 4;
+        float4 s{0.0f, 0.0f, 0.0f, 0.0f};
+        for (int p = 0; p < parts; ++p) {
+            const float4 v = *reinterpret_cast<const float4*>(a.sums + ((int64_t)(kv * parts + p) * a.tokens + t) * (2 * D) + first);
+            s.x += v.x;
+            s.y += v.y;
+            s.z += v.z;
+            s.w += v.w;
+        }
+        const int column = first % D;
+        if (column < a.dim)
+            *reinterpret_cast<uint2*>((first < D ? a.grad_k : a.grad_v).at(t, kv) + column) = uint2{sc_bf16_pair(s.x, s.y), sc_bf16_pair(s.z, s.w)};
+    }
 }
 
 }  // namespace
