@@ -267,14 +267,18 @@ struct rb_attention {
 
 namespace {
 
-// Workgroups that the gradients of keys and values are cut into at least, where there are heads enough.
-constexpr int64_t AT_KEY_GROUPS = 512;
+// Workgroups that the gradients of keys and values are cut into at least.
+constexpr int64_t AT_KEY_GROUPS = 512, AT_MAX_PARTS = 16;
 
-// Into how many parts the heads of queries that read one head of keys are cut.
-inline int key_parts(const rb_attention* a, int64_t tiles)
+// Into how many parts the queries of a head of keys are cut: until all units have two workgroups; and twice as many where documents are long and causal
+// (by their mean length), since the first keys' workgroups take twice the mean.
+inline int key_parts(const rb_attention* a, int64_t tokens, int64_t documents)
 {
-    const int64_t group = a->heads / a->kv_heads, groups = tiles * a->kv_heads;
-    return (int)std::min<int64_t>(group, (AT_KEY_GROUPS + groups - 1) / groups);
+    const int64_t groups = (tokens + AT_ROWS - 1) / AT_ROWS * a->kv_heads;
+    const int64_t wanted = a->causal && tokens >= documents * 2048 ? 2 * AT_KEY_GROUPS : AT_KEY_GROUPS;
+    // (a part of less than 4 tiles of queries would not be worth its sums)
+    const int64_t most = std::min<int64_t>(AT_MAX_PARTS, std::max<int64_t>(1, tokens / std::max<int64_t>(documents, 1) * (a->heads / a->kv_heads) / (4 * AT_BLOCK)));
+    return (int)std::min<int64_t>(most, (wanted + groups - 1) / groups);
 }
 
 // Heads of one die that take turns (0: dies have no heads of their own): those that read the same keys.
@@ -364,9 +368,9 @@ int rb_attention_create(rb_attention** out, int64_t heads, int64_t kv_heads, int
     a->off_lse2 = off; off += round_up((size_t)heads * (size_t)max_tokens * sizeof(float), 256);
     a->off_delta = off; off += round_up((size_t)heads * (size_t)max_tokens * sizeof(float), 256);
     a->off_sums = off;
-    // (most workgroups of a launch whose groups are cut into parts, with one part more than would be needed)
+    // (parts > 1: workgroups are less than what is wanted and one more of each)
     const size_t tiles = ((size_t)max_tokens + AT_ROWS - 1) / AT_ROWS;
-    if (heads > kv_heads) off += std::min((size_t)heads * tiles, (size_t)2 * AT_KEY_GROUPS) * AT_ROWS * 2 * (head_dim <= 64 ? 64 : 128) * sizeof(float);
+    off += std::min((size_t)AT_MAX_PARTS * kv_heads * tiles, (size_t)4 * AT_KEY_GROUPS) * AT_ROWS * 2 * (head_dim <= 64 ? 64 : 128) * sizeof(float);
     a->bytes = off;
     *out = a;
     return RB_OK;
@@ -426,7 +430,7 @@ int rb_attention_grad(rb_attention* a, const rb_heads* q, const rb_heads* k, con
     g.lse2 = lse2;
     g.delta = delta;
     g.lse_less = a->form == AT_CAPPED ? a->score.to_log2 : 0.0f;
-    const int parts = key_parts(a, g.tiles);
+    const int parts = key_parts(a, tokens, documents->count);
     AttentionArgs of_keys = g;
     of_keys.shares = a->kv_heads * parts;
     of_keys.inner = inner_heads(of_keys.shares, parts);

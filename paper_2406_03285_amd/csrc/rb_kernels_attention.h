@@ -95,10 +95,10 @@ __device__ __forceinline__ int at_turn(int r)
     return D == 128 ? ((r & 3) << 2) | ((r >> 2) & 3) : (((r >> 1) & 1) << 2) | ((r >> 2) & 3);
 }
 
-// A lane's part in bringing tiles of 64 rows of a tensor: the same pieces of every tile.
-template <int D>
+// A lane's part in bringing tiles of ROWS rows of a tensor: the same pieces of every tile.
+template <int D, int ROWS = AT_TILE>
 struct Bring {
-    static constexpr int PIECES = D / 8, LOADS = AT_TILE * PIECES / AT_TPB, STEP = AT_TILE / LOADS;
+    static constexpr int PIECES = D / 8, LOADS = ROWS * PIECES / AT_TPB, STEP = ROWS / LOADS;
     int row, piece, wave;
     bool there;                // (pieces behind the head's last number are left as they are: 0)
     __device__ __forceinline__ Bring(int wave_, int dim) : wave(wave_)
@@ -110,11 +110,11 @@ struct Bring {
     }
     // Where the lane's piece of a tile's first rows is, relative to the tile's first row.
     __device__ __forceinline__ int64_t offset(int64_t stride) const { return row * stride + piece * 8; }
-    // Rows first .. first + 63 of the tensor that begins at `from`, no further than row `last`.
+    // Rows first .. first + ROWS - 1 of the tensor that begins at `from`, no further than row `last`.
     __device__ __forceinline__ void operator()(const Bf16* from, int64_t stride, int64_t offset, int first, int last, char* tile) const
     {
         if (!there) return;
-        if (first + AT_TILE <= last + 1) {
+        if (first + ROWS <= last + 1) {
             const Bf16* base = from + first * stride;
 #pragma unroll
             for (int j = 0; j < LOADS; ++j) one(base + j * STEP * stride + offset, tile, j);
@@ -129,10 +129,10 @@ struct Bring {
     }
 };
 
-// 64 binary32 numbers behind each other (one wavefront).
+// 32 binary32 numbers of a lane half each, to places behind one another.
 __device__ __forceinline__ void at_bring_numbers(const float* from, int first, int last, float* to)
 {
-    const float* p = from + min(first + (int)(threadIdx.x & 63), last);
+    const float* p = from + min(first + (int)(threadIdx.x & 31), last);
     __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)p, (__attribute__((address_space(3))) void*)to, 4, 0, 0);
 }
 
@@ -214,11 +214,11 @@ struct Noted {
 };
 
 // The pieces of a tile that the thread has brought.  (Between two waits for the workgroup.)
-template <int D>
+template <int D, int ROWS = AT_TILE>
 __device__ __forceinline__ void at_make_finite(char* tile, int wave, uint32_t (&noted)[2])
 {
 #pragma unroll
-    for (int j = 0; j < Bring<D>::LOADS; ++j) {
+    for (int j = 0; j < Bring<D, ROWS>::LOADS; ++j) {
         const int at = (j * AT_WAVES + wave) * 64 + (threadIdx.x & 63);
         sc_vec w = *reinterpret_cast<const sc_vec*>(tile + at * 16);
         uint32_t found = 0;
@@ -231,7 +231,7 @@ __device__ __forceinline__ void at_make_finite(char* tile, int wave, uint32_t (&
                 w[i] &= ~((m << 16) - m);
             }
             *reinterpret_cast<sc_vec*>(tile + at * 16) = w;
-            const int row = at / Bring<D>::PIECES;
+            const int row = at / Bring<D, ROWS>::PIECES;
             atomicOr(&noted[row / 32], 1u << (row % 32));
         }
     }
@@ -295,8 +295,8 @@ struct AttentionArgs {
     ScoreOf score;
     int32_t tokens, dim, heads, group;     // group: heads of queries to one of keys
     int32_t tiles, inner;
-    int32_t shares;                        // gradients of keys: heads of keys, times the parts that a group is cut into
-    float* sums;                           // of the parts: [shares][tokens][2][D]; null: groups are not cut
+    int32_t shares;                        // gradients of keys: heads of keys, times the parts that their queries are cut into
+    float* sums;                           // of the parts: [shares][tokens][2][D]; null: there is one
     // forward: written; gradients: read
     HeadRows out;
     float* lse;
@@ -312,12 +312,13 @@ struct AttentionArgs {
 template <bool UP>
 __device__ __forceinline__ void at_place(int id, int tiles, int heads, int inner, int& tile, int& head)
 {
+    const int i = id >> 3;
     int t;
     if (inner > 0) {
-        const int die = id & 7, i = id >> 3, outer = i / inner;
+        const int outer = i / inner;
         const int round = outer / tiles;
         t = outer - round * tiles;
-        head = die * (heads >> 3) + round * inner + (i - outer * inner);
+        head = (id & 7) * (heads >> 3) + round * inner + (i - outer * inner);
     } else {
         t = id / heads;
         head = id - t * heads;
@@ -351,8 +352,8 @@ struct Reach {
         all_lo = at_highest(all_lo);
         all_hi = at_lowest(all_hi);
     }
-    __device__ __forceinline__ bool meets(int first) const { return first < hi && first + AT_TILE > lo; }
-    __device__ __forceinline__ bool whole(int first) const { return first >= all_lo && first + AT_TILE <= all_hi; }
+    __device__ __forceinline__ bool meets(int first, int rows = AT_TILE) const { return first < hi && first + rows > lo; }
+    __device__ __forceinline__ bool whole(int first, int rows = AT_TILE) const { return first >= all_lo && first + rows <= all_hi; }
 };
 __device__ __forceinline__ Reach at_reach(Span s)      // of the wavefront's rows, one a lane
 {
@@ -691,35 +692,36 @@ __global__ void __launch_bounds__(AT_TPB, 2) rb_attend_grad_q_kernel(AttentionAr
 
 // Of keys and values: a workgroup has 128 of one head, and goes through the queries of all the heads that read it.
 template <int D, int FORM, bool SLOPES>
-__global__ void __launch_bounds__(AT_TPB, 1) rb_attend_grad_kv_kernel(AttentionArgs a)
+__global__ void __launch_bounds__(AT_TPB, 2) rb_attend_grad_kv_kernel(AttentionArgs a)
 {
-    __shared__ __align__(1024) char lds[2][2][AT_TILE * D * 2];
+    constexpr int ROWS = AT_BLOCK;                  // queries at a time
+    __shared__ __align__(1024) char lds[2][2][ROWS * D * 2];
+    __shared__ __align__(1024) char own[AT_ROWS / AT_TILE][AT_TILE * D * 2];       // the workgroup's values
     __shared__ Noted noted;
-    __shared__ __align__(1024) float numbers[2][2][AT_TILE];          // lse in base 2 and delta of the tile's queries
+    __shared__ __align__(1024) float numbers[2][AT_TILE];          // lse in base 2 and delta of the tile's queries
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x & 63, half = lane / 32;
-    // one workgroup's share of the queries' heads: all of the group, or a part of it
+    // one workgroup's share: a head of keys, and all of its queries or a part of them
     int tile, share;
     at_place<true>(blockIdx.x, a.tiles, a.shares, a.inner, tile, share);
     const int parts = a.shares / (a.heads / a.group), kv = share / parts, part = share - kv * parts;
-    const int head_from = kv * a.group + a.group * part / parts, head_to = kv * a.group + a.group * (part + 1) / parts;
     const Reach all = at_reach<true>(a.spans, tile * AT_ROWS, a.tokens);
     const int row = tile * AT_ROWS + wave * AT_BLOCK + (lane & 31);
     const Span mine = row < a.tokens ? a.spans[row].seen : Span{0, 0};
     const Reach reach = at_reach(mine);
     const int last = a.tokens - 1;
-    at_bf8 k[D / 16], v[D / 16];
+    at_bf8 k[D / 16];
     at_own<D>(a.k.at(min(row, last), kv), a.dim, k);
-    at_own<D>(a.v.at(min(row, last), kv), a.dim, v);
     if (threadIdx.x < 4) noted.rows[threadIdx.x / 2][threadIdx.x % 2] = 0;
     at_clear<D>(&lds[0][0][0], sizeof(lds), a.dim);
-    const Bring<D> bring(wave, a.dim);
+    at_clear<D>(&own[0][0], sizeof(own), a.dim);
+    const Bring<D, ROWS> bring(wave, a.dim);
+    const Bring<D> bring_own(wave, a.dim);
     const Reads<D> reads;
     const int64_t q_offset = bring.offset(a.q.token), g_offset = bring.offset(a.grad_out.token);
     auto fetch = [&](int head, int first, int buffer) {
         bring(a.q.at(0, head), a.q.token, q_offset, first, last, lds[buffer][0]);
         bring(a.grad_out.at(0, head), a.grad_out.token, g_offset, first, last, lds[buffer][1]);
-        if (wave == 0) at_bring_numbers(a.lse2 + (int64_t)head * a.tokens, first, last, numbers[buffer][0]);
-        if (wave == 1) at_bring_numbers(a.delta + (int64_t)head * a.tokens, first, last, numbers[buffer][1]);
+        if (wave == 0) at_bring_numbers((lane < 32 ? a.lse2 : a.delta) + (int64_t)head * a.tokens, first, last, numbers[buffer]);
     };
     at_acc dk[D / 32]{}, dv[D / 32]{};
 
@@ -728,21 +730,20 @@ __global__ void __launch_bounds__(AT_TPB, 1) rb_attend_grad_kv_kernel(AttentionA
         const float slope2 = SLOPES && a.slopes ? a.slopes[head] * AT_LOG2E : 0.0f;
         const int from = mine.lo - first, to = mine.hi - first;
         const float away = (float)(row - first - 4 * half);
-#pragma unroll
-        for (int b = 0; b < 2; ++b) {
+        {
             at_acc s{}, dp{};
 #pragma unroll
             for (int n = 0; n < D / 16; ++n) {
-                s = at_mma(reads.rows(qt, b, n), k[n], s);
-                dp = at_mma(reads.rows(gt, b, n), v[n], dp);
+                s = at_mma(reads.rows(qt, 0, n), k[n], s);
+                dp = at_mma(reads.rows(gt, 0, n), reads.rows(own[wave / 2], wave % 2, n), dp);
             }
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
-                const float4 lse2 = *reinterpret_cast<const float4*>(&numbers[buffer][0][32 * b + 8 * g + 4 * half]);
-                const float4 delta = *reinterpret_cast<const float4*>(&numbers[buffer][1][32 * b + 8 * g + 4 * half]);
+                const float4 lse2 = *reinterpret_cast<const float4*>(&numbers[buffer][8 * g + 4 * half]);
+                const float4 delta = *reinterpret_cast<const float4*>(&numbers[buffer][32 + 8 * g + 4 * half]);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const int e = 4 * g + i, query = 32 * b + 8 * g + i;
+                    const int e = 4 * g + i, query = 8 * g + i;
                     const float less = i == 0 ? lse2.x : i == 1 ? lse2.y : i == 2 ? lse2.z : lse2.w;
                     const float delta_i = i == 0 ? delta.x : i == 1 ? delta.y : i == 2 ? delta.z : delta.w;
                     float p, ds;
@@ -755,23 +756,30 @@ __global__ void __launch_bounds__(AT_TPB, 1) rb_attend_grad_kv_kernel(AttentionA
             asm volatile("");       // (a branch: few tiles need it)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
-                    const int query = 32 * b + 8 * (e / 4) + 4 * half + e % 4;
+                    const int query = 8 * (e / 4) + 4 * half + e % 4;
                     const bool seen = query >= from && query < to;
                     s[e] = seen ? s[e] : 0.0f;
                     dp[e] = seen ? dp[e] : 0.0f;
                 }
             }
             const at_bf8 p[2] = {at_pack(s, 0), at_pack(s, 1)}, ds[2] = {at_pack(dp, 0), at_pack(dp, 1)};
-            at_add<D, 2>(dv, p, reads, gt, 2 * b);
-            at_add<D, 2>(dk, ds, reads, qt, 2 * b);
+            at_add<D, 2>(dv, p, reads, gt, 0);
+            at_add<D, 2>(dk, ds, reads, qt, 0);
         }
     };
 
     bool lost = false;                              // seen by a query that is not finite, or whose gradient is not
-    int head = head_from, first = all.lo, left = all.lo < all.hi ? (all.hi - all.lo + AT_TILE - 1) / AT_TILE * (head_to - head_from) : 0;
-    if (left) fetch(head, first, 0);
+    // tiles of queries, head by head; from where and how many
+    const int tiles = all.lo < all.hi ? (all.hi - all.lo + ROWS - 1) / ROWS : 0;
+    const int from = (int)((int64_t)tiles * a.group * part / parts), skipped = tiles > 0 ? from / tiles : 0;
+    int head = kv * a.group + skipped, first = all.lo + (from - skipped * tiles) * ROWS, left = (int)((int64_t)tiles * a.group * (part + 1) / parts) - from;
+    if (left) {
+        for (int i = 0; i < AT_ROWS / AT_TILE; ++i)
+            bring_own(a.v.at(0, kv), a.v.token, bring_own.offset(a.v.token), min(tile * AT_ROWS + i * AT_TILE, last), last, own[i]);
+        fetch(head, first, 0);
+    }
     for (int now = 0; left > 0; --left, now ^= 1) {
-        int next_head = head, next = first + AT_TILE;
+        int next_head = head, next = first + ROWS;
         if (next >= all.hi) {
             next = all.lo;
             ++next_head;
@@ -779,13 +787,13 @@ __global__ void __launch_bounds__(AT_TPB, 1) rb_attend_grad_kv_kernel(AttentionA
         at_arrived();
         if (threadIdx.x < 2) noted.rows[now ^ 1][threadIdx.x] = 0;
         if (left > 1) fetch(next_head, next, now ^ 1);
-        if (!all.whole(first)) {
-            at_make_finite<D>(lds[now][0], wave, noted.rows[now]);
-            at_make_finite<D>(lds[now][1], wave, noted.rows[now]);
+        if (!all.whole(first, ROWS)) {
+            at_make_finite<D, ROWS>(lds[now][0], wave, noted.rows[now]);
+            at_make_finite<D, ROWS>(lds[now][1], wave, noted.rows[now]);
             at_wait_for_all();
             lost |= at_noted(noted.rows[now], mine.lo - first, mine.hi - first) != 0;
         }
-        if (reach.meets(first)) step(!reach.whole(first), first, head, now);
+        if (reach.meets(first, ROWS)) step(!reach.whole(first, ROWS), first, head, now);
         head = next_head;
         first = next;
     }
