@@ -29,6 +29,7 @@ constexpr int AT_BLOCK = 32;                       // rows of a wavefront
 constexpr int AT_ROWS = AT_WAVES * AT_BLOCK;       // rows of a workgroup
 constexpr int AT_TILE = 64;                        // rows that are in LDS at a time
 constexpr float AT_LOG2E = 1.44269504088896340736f;
+constexpr int AT_NEAR_OFFSETS = 2048;              // offsets of documents that are kept in LDS
 constexpr float AT_LN2 = 0.69314718055994530942f;
 
 typedef __bf16 at_bf8 __attribute__((ext_vector_type(8)));
@@ -79,10 +80,16 @@ __host__ __device__ inline Spans at_spans_of(const SpanArgs& a, int32_t t)
     return s;
 }
 
-// A thread per position.
+// A thread per position.  The offsets are looked through in LDS where they fit (24 documents of 8192 positions: 5.0 -> us).
 __global__ void __launch_bounds__(AT_TPB) rb_spans_kernel(SpanArgs a)
 {
+    __shared__ int64_t near[AT_NEAR_OFFSETS];
     const int t = blockIdx.x * AT_TPB + threadIdx.x;
+    if (a.count < AT_NEAR_OFFSETS) {
+        for (int i = threadIdx.x; i <= a.count; i += AT_TPB) near[i] = a.offsets[i];
+        __syncthreads();
+        a.offsets = near;
+    }
     if (t < a.tokens) a.spans[t] = at_spans_of(a, t);
 }
 
@@ -93,6 +100,17 @@ template <int D>
 __device__ __forceinline__ int at_turn(int r)
 {
     return D == 128 ? ((r & 3) << 2) | ((r >> 2) & 3) : (((r >> 1) & 1) << 2) | ((r >> 2) & 3);
+}
+
+// Asynchronous loads into LDS: the wavefront's lanes bring BYTES each, which land behind each other from `to` on (the same for all of them).  Written
+// out, since for the builtin the compiler has every later read from LDS wait for all of them, also of the tile that is complete; at_arrived waits.
+// (There are no registers that such a load writes.)
+template <int BYTES>
+__device__ __forceinline__ void at_load_to_lds(const void* from, const void* to)
+{
+    const uint32_t place = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)to);
+    if constexpr (BYTES == 16) asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(place) : "memory", "m0");
+    else asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(from), "s"(place) : "memory", "m0");
 }
 
 // A lane's part in bringing tiles of ROWS rows of a tensor: the same pieces of every tile.
@@ -123,17 +141,13 @@ struct Bring {
             for (int j = 0; j < LOADS; ++j) one(from + (int64_t)min(first + j * STEP + row, last) * stride + piece * 8, tile, j);
         }
     }
-    __device__ __forceinline__ void one(const Bf16* p, char* tile, int j) const
-    {
-        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)p, (__attribute__((address_space(3))) void*)(tile + (j * AT_WAVES + wave) * 1024), 16, 0, 0);
-    }
+    __device__ __forceinline__ void one(const Bf16* p, char* tile, int j) const { at_load_to_lds<16>(p, tile + (j * AT_WAVES + wave) * 1024); }
 };
 
 // 32 binary32 numbers of a lane half each, to places behind one another.
 __device__ __forceinline__ void at_bring_numbers(const float* from, int first, int last, float* to)
 {
-    const float* p = from + min(first + (int)(threadIdx.x & 31), last);
-    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)p, (__attribute__((address_space(3))) void*)to, 4, 0, 0);
+    at_load_to_lds<4>(from + min(first + (int)(threadIdx.x & 31), last), to);
 }
 
 // Waits until a wavefront's loads into LDS and its reads from there are done, then for the workgroup's other wavefronts.
@@ -182,26 +196,47 @@ __device__ __forceinline__ at_bf8 at_pack(const at_acc& v, int c)
     return __builtin_bit_cast(at_bf8, w);
 }
 
-// The head's numbers 16 s + 8 (lane / 32) .. of one row, as operands.
+// The wavefront's 32 of the workgroup's 128 rows in two tiles, as operands.
 template <int D>
-__device__ __forceinline__ void at_own(const Bf16* row, int dim, at_bf8 (&f)[D / 16])
+__device__ __forceinline__ void at_own(const Reads<D>& reads, const char (&tiles)[2][AT_TILE * D * 2], int wave, at_bf8 (&f)[D / 16])
 {
-    const int half = (threadIdx.x >> 5) & 1;
 #pragma unroll
-    for (int s = 0; s < D / 16; ++s) {
-        const int first = 16 * s + 8 * half;
-        f[s] = first < dim ? *reinterpret_cast<const at_bf8*>(row + first) : at_bf8{};
-    }
+    for (int n = 0; n < D / 16; ++n) f[n] = reads.rows(tiles[wave / 2], wave % 2, n);
+}
+// The workgroup's 128 rows into two tiles.
+template <int D>
+__device__ __forceinline__ void at_bring_own(const Bring<D>& bring, const Bf16* from, int64_t stride, int tile, int last, char (&tiles)[2][AT_TILE * D * 2])
+{
+#pragma unroll
+    for (int i = 0; i < 2; ++i) bring(from, stride, bring.offset(stride), min(tile * AT_ROWS + i * AT_TILE, last), last, tiles[i]);
 }
 
-// sum[n] += columns of the tile's rows 16 (c0 + c) .. times factors[c], for the head's numbers 32 n ..
-template <int D, int C>
+// sum[n] += columns of the tile's rows 16 (c0 + c) .. times factors[c], for the head's numbers 32 n ..  AHEAD: the next columns are on their way while the last
+// ones are multiplied (left to itself the compiler waits for each; where it has no registers left that is better, the other wavefront fills in).
+template <int D, int C, bool AHEAD>
 __device__ __forceinline__ void at_add(at_acc (&sum)[D / 32], const at_bf8 (&factors)[C], const Reads<D>& reads, const char* tile, int c0)
 {
+    if constexpr (!AHEAD) {
 #pragma unroll
-    for (int c = 0; c < C; ++c)
+        for (int c = 0; c < C; ++c)
 #pragma unroll
-        for (int n = 0; n < D / 32; ++n) sum[n] = at_mma(reads.columns(tile, n, c0 + c), factors[c], sum[n]);
+            for (int n = 0; n < D / 32; ++n) sum[n] = at_mma(reads.columns(tile, n, c0 + c), factors[c], sum[n]);
+        return;
+    }
+    at_bf8 v[2][D / 32];
+#pragma unroll
+    for (int n = 0; n < D / 32; ++n) v[0][n] = reads.columns(tile, n, c0);
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        if (c + 1 < C) {
+#pragma unroll
+            for (int n = 0; n < D / 32; ++n) v[(c + 1) & 1][n] = reads.columns(tile, n, c0 + c + 1);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int n = 0; n < D / 32; ++n) sum[n] = at_mma(v[c & 1][n], factors[c], sum[n]);
+        __builtin_amdgcn_sched_barrier(0);
+    }
 }
 
 // ---- what is not finite where something is masked --------------------------------
@@ -326,10 +361,15 @@ __device__ __forceinline__ void at_place(int id, int tiles, int heads, int inner
     tile = UP ? t : tiles - 1 - t;
 }
 
+// Of all lanes.
 __device__ __forceinline__ int at_lowest(int v)
 {
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) v = min(v, __shfl_xor(v, d));
+    v = min(v, (int)sc_xor<1>((uint32_t)v));
+    v = min(v, (int)sc_xor<2>((uint32_t)v));
+    v = min(v, (int)sc_xor<4>((uint32_t)v));
+    v = min(v, (int)sc_xor<8>((uint32_t)v));
+    v = min(v, (int)sc_xor<16>((uint32_t)v));
+    v = min(v, (int)sc_xor<32>((uint32_t)v));
     return __builtin_amdgcn_readfirstlane(v);
 }
 __device__ __forceinline__ int at_highest(int v) { return -at_lowest(-v); }
@@ -386,21 +426,29 @@ __device__ __forceinline__ void at_clear(char* lds, int bytes, int dim)
     __syncthreads();
 }
 
-// Row `t` of a result from its numbers 32 n + 8 (i / 4) + 4 (lane / 32) + i % 4.
+// 32 rows of a result, of which a lane has one (lane % 32) with its numbers 32 n + 8 (i / 4) + 4 (lane / 32) + i % 4: through LDS (`place`, the wavefront's own),
+// so that whole rows go to memory (eight bytes a lane at a time cost a quarter of the time of short documents).
 template <int D>
-__device__ __forceinline__ void at_store(Bf16* row, int dim, const at_acc (&v)[D / 32], float factor, bool zero)
+__device__ __forceinline__ void at_store(char* place, Bf16* first, int64_t stride, int rows, int dim, const at_acc (&v)[D / 32], float factor, bool zero)
 {
-    const int half = (threadIdx.x >> 5) & 1;
+    const int lane = threadIdx.x & 63, half = lane / 32, r = lane & 31;
+    char* const mine = place + r * D * 2 + half * 8;
+    const int turn = at_turn<D>(r);
 #pragma unroll
     for (int n = 0; n < D / 32; ++n)
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
-            const int first = 32 * n + 8 * g + 4 * half;
-            if (first >= dim) continue;
             uint2 w{0, 0};
             if (!zero) w = uint2{sc_bf16_pair(v[n][4 * g] * factor, v[n][4 * g + 1] * factor), sc_bf16_pair(v[n][4 * g + 2] * factor, v[n][4 * g + 3] * factor)};
-            *reinterpret_cast<uint2*>(row + first) = w;
+            *reinterpret_cast<uint2*>(mine + (((4 * n + g) ^ turn) << 4)) = w;
         }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+    for (int j = 0; j < D / 16; ++j) {
+        const int at = j * 64 + lane, row = at / (D / 8), piece = at % (D / 8);
+        const sc_vec w = *reinterpret_cast<const sc_vec*>(place + row * D * 2 + ((piece ^ at_turn<D>(row)) << 4));
+        if (row < rows && piece * 8 < dim) *reinterpret_cast<sc_vec*>(first + row * stride + piece * 8) = w;
+    }
 }
 
 // The same unrounded.
@@ -437,7 +485,6 @@ __global__ void __launch_bounds__(AT_TPB, 2) rb_attend_kernel(AttentionArgs a)
     const Bf16 *const keys = a.k.at(0, kv), *const values = a.v.at(0, kv);
     const float slope2 = SLOPES && a.slopes ? a.slopes[head] * AT_LOG2E : 0.0f;
     at_bf8 q[D / 16];
-    at_own<D>(a.q.at(min(row, last), head), a.dim, q);
     if (threadIdx.x < 4) noted.rows[threadIdx.x / 2][threadIdx.x % 2] = 0;
     at_clear<D>(&lds[0][0][0], sizeof(lds), a.dim);
     const Bring<D> bring(wave, a.dim);
@@ -448,10 +495,26 @@ __global__ void __launch_bounds__(AT_TPB, 2) rb_attend_kernel(AttentionArgs a)
 
     auto step = [&](bool masked, int first, const char* kt, const char* vt) {
         at_acc s[2]{};
+        at_bf8 f[2][2][2];                          // pieces of the keys, two ahead
 #pragma unroll
-        for (int n = 0; n < D / 16; ++n)
+        for (int n = 0; n < 2; ++n)
 #pragma unroll
-            for (int b = 0; b < 2; ++b) s[b] = at_mma(reads.rows(kt, b, n), q[n], s[b]);
+            for (int b = 0; b < 2; ++b) f[0][n][b] = reads.rows(kt, b, n);
+#pragma unroll
+        for (int n = 0; n < D / 16; n += 2) {
+            if (n + 2 < D / 16) {
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int b = 0; b < 2; ++b) f[(n / 2 + 1) & 1][i][b] = reads.rows(kt, b, n + 2 + i);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int b = 0; b < 2; ++b) s[b] = at_mma(f[(n / 2) & 1][i][b], q[n + i], s[b]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
         const int from = mine.lo - first, to = mine.hi - first;        // what the lane's row sees of the tile
         constexpr bool SCORED = FORM != AT_PLAIN || SLOPES;            // (plain products are scaled in the exponent's own instruction)
         const float away = (float)(row - first - 4 * half);
@@ -509,13 +572,17 @@ __global__ void __launch_bounds__(AT_TPB, 2) rb_attend_kernel(AttentionArgs a)
             p[2 * b] = at_pack(s[b], 0);
             p[2 * b + 1] = at_pack(s[b], 1);
         }
-        at_add<D, 4>(o, p, reads, vt, 0);
+        at_add<D, 4, true>(o, p, reads, vt, 0);
     };
 
     const int count = all.lo < all.hi ? (all.hi - all.lo + AT_TILE - 1) / AT_TILE : 0;
     if (count > 0) {
+        at_bring_own<D>(bring, a.q.at(0, head), a.q.token, tile, last, lds[1]);
         bring(keys, a.k.token, k_offset, all.lo, last, lds[0][0]);
         bring(values, a.v.token, v_offset, all.lo, last, lds[0][1]);
+        at_arrived();
+        at_own<D>(reads, lds[1], wave, q);
+        at_wait_for_all();
     }
     for (int i = 0; i < count; ++i) {
         const int first = all.lo + i * AT_TILE, now = i & 1;
@@ -553,11 +620,13 @@ __global__ void __launch_bounds__(AT_TPB, 2) rb_attend_kernel(AttentionArgs a)
             }
         }
     }
-    if (row >= a.tokens) return;
     l += sc_xor<32>(l);
     const bool empty = mine.lo >= mine.hi;
-    at_store<D>(a.out.at(row, head), a.dim, o, 1.0f / l, empty);
-    if (a.lse && half == 0) a.lse[(int64_t)head * a.tokens + row] = empty ? sc_neg_inf() : ((FORM == AT_CAPPED ? a.score.to_log2 : m) + __log2f(l)) * AT_LN2;
+    const int start = tile * AT_ROWS + wave * AT_BLOCK;
+    at_wait_for_all();                              // (the tiles are read)
+    at_store<D>(&lds[0][0][0] + wave * AT_BLOCK * D * 2, a.out.at(start, head), a.out.token, a.tokens - start, a.dim, o, 1.0f / l, empty);
+    if (a.lse && half == 0 && row < a.tokens)
+        a.lse[(int64_t)head * a.tokens + row] = empty ? sc_neg_inf() : ((FORM == AT_CAPPED ? a.score.to_log2 : m) + __log2f(l)) * AT_LN2;
 }
 
 // ---- gradients -----------------------------------------------------------------
@@ -624,8 +693,6 @@ __global__ void __launch_bounds__(AT_TPB, 2) rb_attend_grad_q_kernel(AttentionAr
     const Bf16 *const keys = a.k.at(0, kv), *const values = a.v.at(0, kv);
     const float slope2 = SLOPES && a.slopes ? a.slopes[head] * AT_LOG2E : 0.0f;
     at_bf8 q[D / 16], go[D / 16];
-    at_own<D>(a.q.at(r, head), a.dim, q);
-    at_own<D>(a.grad_out.at(r, head), a.dim, go);
     const float lse2 = a.lse2[(int64_t)head * a.tokens + r], delta = a.delta[(int64_t)head * a.tokens + r];
     if (threadIdx.x < 4) noted.rows[threadIdx.x / 2][threadIdx.x % 2] = 0;
     at_clear<D>(&lds[0][0][0], sizeof(lds), a.dim);
@@ -661,13 +728,19 @@ __global__ void __launch_bounds__(AT_TPB, 2) rb_attend_grad_q_kernel(AttentionAr
                 }
             }
             const at_bf8 f[2] = {at_pack(s, 0), at_pack(s, 1)};
-            at_add<D, 2>(dq, f, reads, kt, 2 * b);
+            at_add<D, 2, false>(dq, f, reads, kt, 2 * b);
         }
     };
 
     bool lost = false;                              // the row sees a key that is not finite
     const int count = all.lo < all.hi ? (all.hi - all.lo + AT_TILE - 1) / AT_TILE : 0;
     if (count > 0) {
+        at_bring_own<D>(bring, a.q.at(0, head), a.q.token, tile, last, lds[0]);
+        at_bring_own<D>(bring, a.grad_out.at(0, head), a.grad_out.token, tile, last, lds[1]);
+        at_arrived();
+        at_own<D>(reads, lds[0], wave, q);
+        at_own<D>(reads, lds[1], wave, go);
+        at_wait_for_all();
         bring(keys, a.k.token, k_offset, all.lo, last, lds[0][0]);
         bring(values, a.v.token, v_offset, all.lo, last, lds[0][1]);
     }
@@ -686,8 +759,10 @@ __global__ void __launch_bounds__(AT_TPB, 2) rb_attend_grad_q_kernel(AttentionAr
         }
         if (reach.meets(first)) step(!reach.whole(first), first, lds[now][0], lds[now][1]);
     }
-    if (row >= a.tokens) return;
-    at_store<D>(a.grad_q.at(row, head), a.dim, dq, lost ? sc_nan() : a.score.scale, mine.lo >= mine.hi);
+    const int start = tile * AT_ROWS + wave * AT_BLOCK;
+    at_wait_for_all();
+    at_store<D>(&lds[0][0][0] + wave * AT_BLOCK * D * 2, a.grad_q.at(start, head), a.grad_q.token, a.tokens - start, a.dim, dq, lost ? sc_nan() : a.score.scale,
+                mine.lo >= mine.hi);
 }
 
 // Of keys and values: a workgroup has 128 of one head, and goes through the queries of all the heads that read it.
@@ -695,7 +770,7 @@ template <int D, int FORM, bool SLOPES>
 __global__ void __launch_bounds__(AT_TPB, 2) rb_attend_grad_kv_kernel(AttentionArgs a)
 {
     constexpr int ROWS = AT_BLOCK;                  // queries at a time
-    __shared__ __align__(1024) char lds[2][2][ROWS * D * 2];
+    __shared__ __align__(1024) char lds[2][2][ROWS * D * 2];           // queries and their gradients; first the workgroup's keys
     __shared__ __align__(1024) char own[AT_ROWS / AT_TILE][AT_TILE * D * 2];       // the workgroup's values
     __shared__ Noted noted;
     __shared__ __align__(1024) float numbers[2][AT_TILE];          // lse in base 2 and delta of the tile's queries
@@ -710,7 +785,6 @@ __global__ void __launch_bounds__(AT_TPB, 2) rb_attend_grad_kv_kernel(AttentionA
     const Reach reach = at_reach(mine);
     const int last = a.tokens - 1;
     at_bf8 k[D / 16];
-    at_own<D>(a.k.at(min(row, last), kv), a.dim, k);
     if (threadIdx.x < 4) noted.rows[threadIdx.x / 2][threadIdx.x % 2] = 0;
     at_clear<D>(&lds[0][0][0], sizeof(lds), a.dim);
     at_clear<D>(&own[0][0], sizeof(own), a.dim);
@@ -763,8 +837,8 @@ __global__ void __launch_bounds__(AT_TPB, 2) rb_attend_grad_kv_kernel(AttentionA
                 }
             }
             const at_bf8 p[2] = {at_pack(s, 0), at_pack(s, 1)}, ds[2] = {at_pack(dp, 0), at_pack(dp, 1)};
-            at_add<D, 2>(dv, p, reads, gt, 0);
-            at_add<D, 2>(dk, ds, reads, qt, 0);
+            at_add<D, 2, false>(dv, p, reads, gt, 0);
+            at_add<D, 2, false>(dk, ds, reads, qt, 0);
         }
     };
 
@@ -774,8 +848,13 @@ __global__ void __launch_bounds__(AT_TPB, 2) rb_attend_grad_kv_kernel(AttentionA
     const int from = (int)((int64_t)tiles * a.group * part / parts), skipped = tiles > 0 ? from / tiles : 0;
     int head = kv * a.group + skipped, first = all.lo + (from - skipped * tiles) * ROWS, left = (int)((int64_t)tiles * a.group * (part + 1) / parts) - from;
     if (left) {
-        for (int i = 0; i < AT_ROWS / AT_TILE; ++i)
-            bring_own(a.v.at(0, kv), a.v.token, bring_own.offset(a.v.token), min(tile * AT_ROWS + i * AT_TILE, last), last, own[i]);
+        static_assert(sizeof(lds) == sizeof(own), "keys fit where the queries will be");
+        char(&keys)[2][AT_TILE * D * 2] = reinterpret_cast<char(&)[2][AT_TILE * D * 2]>(lds);
+        at_bring_own<D>(bring_own, a.v.at(0, kv), a.v.token, tile, last, own);
+        at_bring_own<D>(bring_own, a.k.at(0, kv), a.k.token, tile, last, keys);
+        at_arrived();
+        at_own<D>(reads, keys, wave, k);
+        at_wait_for_all();
         fetch(head, first, 0);
     }
     for (int now = 0; left > 0; --left, now ^= 1) {
@@ -797,16 +876,19 @@ __global__ void __launch_bounds__(AT_TPB, 2) rb_attend_grad_kv_kernel(AttentionA
         head = next_head;
         first = next;
     }
-    if (row >= a.tokens) return;
     const bool empty = mine.lo >= mine.hi;
     if (a.sums) {
+        if (row >= a.tokens) return;
         float* const to = a.sums + ((int64_t)share * a.tokens + row) * (2 * D);
         at_store_sum<D>(to, dk, lost ? sc_nan() : a.score.scale, empty);
         at_store_sum<D>(to + D, dv, lost ? sc_nan() : 1.0f, empty);
         return;
     }
-    at_store<D>(a.grad_k.at(row, kv), a.dim, dk, lost ? sc_nan() : a.score.scale, empty);
-    at_store<D>(a.grad_v.at(row, kv), a.dim, dv, lost ? sc_nan() : 1.0f, empty);
+    const int start = tile * AT_ROWS + wave * AT_BLOCK;
+    char* const place = &own[0][0] + wave * AT_BLOCK * D * 2;
+    at_wait_for_all();
+    at_store<D>(place, a.grad_k.at(start, kv), a.grad_k.token, a.tokens - start, a.dim, dk, lost ? sc_nan() : a.score.scale, empty);
+    at_store<D>(place, a.grad_v.at(start, kv), a.grad_v.token, a.tokens - start, a.dim, dv, lost ? sc_nan() : 1.0f, empty);
 }
 
 // Gradients of keys and values from the parts' sums: a thread has four numbers of a row of one head.
