@@ -23,7 +23,7 @@ extern "C" {
 #endif
 
 #define RB_MAX_NORM_ROWS (1 << 23)     /* most rows of a call of rb_norm_* and rb_dropout         */
-#define RB_MAX_NORM_WIDTH 65536        /* longest row of rb_norm                                  */
+#define RB_MAX_NORM_WIDTH 32768        /* longest row of rb_norm                                  */
 #define RB_MAX_DROP_WIDTH (1 << 27)    /* longest row of rb_dropout                               */
 #define RB_MAX_HEADS 1024              /* most heads of queries                                   */
 #define RB_MAX_HEAD_DIM 128            /* longest row of a head                                   */

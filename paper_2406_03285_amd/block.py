@@ -14,7 +14,7 @@ from .train import _CODES, _OnStream, _current_stream, _fits, _written
 
 BLOCK_LIB_PATH = os.environ.get("RB_BLOCK_LIBRARY") or os.path.join(HERE, "librb_block.so")   # RB_BLOCK_LIBRARY: another build of the same library
 
-RB_MAX_NORM_ROWS, RB_MAX_NORM_WIDTH, RB_MAX_DROP_WIDTH = 1 << 23, 65536, 1 << 27
+RB_MAX_NORM_ROWS, RB_MAX_NORM_WIDTH, RB_MAX_DROP_WIDTH = 1 << 23, 32768, 1 << 27
 RB_MAX_HEADS, RB_MAX_HEAD_DIM, RB_MAX_TOKENS, RB_MAX_HEAD_ROWS, RB_MAX_DOCUMENTS = 1024, 128, 1 << 22, 1 << 30, 1 << 22
 
 BLOCK_EXPORTS = (

@@ -69,7 +69,7 @@ struct rb_norm {
 
 namespace {
 
-constexpr int64_t NM_FUSED_WIDTH = 8192;       // longest rows whose sums over rows stay in registers beside them
+constexpr int64_t NM_FUSED_WIDTH = 16384;      // longest rows whose sums over rows stay in registers beside them
 
 inline bool rows_fit(const rb_norm* n, const rb_rows* r)
 {
@@ -78,43 +78,75 @@ inline bool rows_fit(const rb_norm* n, const rb_rows* r)
 // what is written in place has to lie as what is read
 inline bool apart_or_alike(const rb_rows* a, const rb_rows* b, int64_t rows) { return !a || !b || !a->data || a->data != b->data || a->stride == b->stride || rows <= 1; }
 
-// Workgroups of a grid that goes through `rows` rows, `at_once` each: enough to fill the chip `per_unit` times.
-inline unsigned norm_groups(int64_t rows, int at_once, int per_unit)
+// Workgroups of a grid that goes through `rows` rows: as many as the chip holds at once.
+inline unsigned norm_groups(int64_t rows, int lanes, int waves_per_simd)
 {
-    return (unsigned)std::min<int64_t>((rows + at_once - 1) / at_once, 256 * per_unit);
+    const int threads = nm_threads(lanes), at_once = threads / lanes;
+    return (unsigned)std::min<int64_t>((rows + at_once - 1) / at_once, 256 * std::max(1, waves_per_simd * 4 * 64 / threads));
 }
 
 template <typename T, int LANES, int PARTS>
 hipError_t norm_forward(const NormArgs& a, hipStream_t st)
 {
-    constexpr int TPB = std::max(LANES, NM_TPB);
-    return launch(rb_norm_kernel<T, LANES, PARTS>, dim3(norm_groups(a.rows, TPB / LANES, 8)), TPB, 0, st, a);
+    const dim3 grid(norm_groups(a.rows, LANES, nm_waves<T>(LANES, PARTS)));
+    return launch(a.total ? rb_norm_kernel<T, LANES, PARTS, true> : rb_norm_kernel<T, LANES, PARTS, false>, grid, nm_threads(LANES), 0, st, a);
 }
 
-template <typename T, int LANES, int PARTS>
-hipError_t norm_grad(const NormGradArgs& a, unsigned groups, hipStream_t st)
-{
-    constexpr int TPB = std::max(LANES, NM_TPB);
-    if constexpr (LANES * PARTS * NM_PIECE <= NM_FUSED_WIDTH) {
-        if (a.sums) return launch(rb_norm_grad_kernel<T, LANES, PARTS, true>, dim3(groups), TPB, 0, st, a);
-    }
-    return launch(rb_norm_grad_kernel<T, LANES, PARTS, false>, dim3(norm_groups(a.rows, TPB / LANES, 8)), TPB, 0, st, a);
-}
+template <int N> using Int = std::integral_constant<int, N>;
 
-// Lanes of a row and pieces of a lane, by the row's length: `of` is called with both.
+// Lanes of a row and pieces of a lane, by the row's length, which ends in the last part: `of` is called with both.
 template <typename Of>
-hipError_t by_width(int32_t width, const Of& of)
+auto forward_by_width(int32_t width, const Of& of)
 {
-    if (width <= 128) return of(std::integral_constant<int, 16>(), std::integral_constant<int, 1>());
-    if (width <= 512) return of(std::integral_constant<int, 64>(), std::integral_constant<int, 1>());
-    if (width <= 1024) return of(std::integral_constant<int, 64>(), std::integral_constant<int, 2>());
-    if (width <= 2048) return of(std::integral_constant<int, 64>(), std::integral_constant<int, 4>());
-    if (width <= 4096) return of(std::integral_constant<int, 256>(), std::integral_constant<int, 2>());
-    if (width <= 8192) return of(std::integral_constant<int, 256>(), std::integral_constant<int, 4>());
-    if (width <= 32768) return of(std::integral_constant<int, 1024>(), std::integral_constant<int, 4>());
-    return of(std::integral_constant<int, 1024>(), std::integral_constant<int, 8>());
+    if (width <= 128) return of(Int<16>(), Int<1>());
+    if (width <= 256) return of(Int<16>(), Int<2>());
+    if (width <= 512) return of(Int<64>(), Int<1>());
+    if (width <= 1024) return of(Int<64>(), Int<2>());
+    if (width <= 1536) return of(Int<64>(), Int<3>());
+    if (width <= 2048) return of(Int<64>(), Int<4>());
+    if (width <= 4096) return of(Int<256>(), Int<2>());
+    if (width <= 6144) return of(Int<256>(), Int<3>());
+    if (width <= 8192) return of(Int<512>(), Int<2>());
+    if (width <= 16384) return of(Int<1024>(), Int<2>());
+    if (width <= 24576) return of(Int<1024>(), Int<3>());
+    return of(Int<1024>(), Int<4>());
 }
-inline int rows_at_once(int32_t width) { return width <= 128 ? NM_TPB / 16 : width <= 2048 ? NM_TPB / 64 : 1; }
+// The gradients' sums and rows ahead take more registers: fewer pieces of a lane, of binary32 all the more.
+template <typename Of>
+auto grad_by_width(int32_t width, const Of& of)
+{
+    if (width <= 128) return of(Bf16(), Int<16>(), Int<1>());
+    if (width <= 256) return of(Bf16(), Int<16>(), Int<2>());
+    if (width <= 384) return of(Bf16(), Int<16>(), Int<3>());
+    if (width <= 512) return of(Bf16(), Int<64>(), Int<1>());
+    if (width <= 1024) return of(Bf16(), Int<64>(), Int<2>());
+    if (width <= 1536) return of(Bf16(), Int<64>(), Int<3>());
+    if (width <= 2048) return of(Bf16(), Int<256>(), Int<1>());
+    if (width <= 4096) return of(Bf16(), Int<256>(), Int<2>());
+    if (width <= 6144) return of(Bf16(), Int<256>(), Int<3>());
+    if (width <= 8192) return of(Bf16(), Int<512>(), Int<2>());
+    if (width <= 12288) return of(Bf16(), Int<512>(), Int<3>());
+    if (width <= 16384) return of(Bf16(), Int<512>(), Int<4>());
+    if (width <= 24576) return of(Bf16(), Int<1024>(), Int<3>());
+    return of(Bf16(), Int<1024>(), Int<4>());
+}
+template <typename Of>
+auto grad_by_width_wide(int32_t width, const Of& of)
+{
+    if (width <= 128) return of(float(), Int<16>(), Int<1>());
+    if (width <= 256) return of(float(), Int<16>(), Int<2>());
+    if (width <= 512) return of(float(), Int<64>(), Int<1>());
+    if (width <= 1024) return of(float(), Int<64>(), Int<2>());
+    if (width <= 2048) return of(float(), Int<256>(), Int<1>());
+    if (width <= 4096) return of(float(), Int<256>(), Int<2>());
+    if (width <= 8192) return of(float(), Int<512>(), Int<2>());
+    if (width <= 12288) return of(float(), Int<512>(), Int<3>());
+    if (width <= 16384) return of(float(), Int<512>(), Int<4>());
+    if (width <= 24576) return of(float(), Int<1024>(), Int<3>());
+    return of(float(), Int<1024>(), Int<4>());
+}
+template <typename Of>
+auto grad_form(const rb_norm* n, const Of& of) { return n->dtype == RB_F32 ? grad_by_width_wide(n->width, of) : grad_by_width(n->width, of); }
 
 }  // namespace
 
@@ -184,7 +216,7 @@ int rb_norm_forward(rb_norm* n, const rb_rows* x, const rb_rows* residual, const
     a.wide_weights = n->weight_dtype == RB_F32;
     a.drops = drop != nullptr;
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
-    const hipError_t e = by_width(n->width, [&](auto lanes, auto parts) {
+    const hipError_t e = forward_by_width(n->width, [&](auto lanes, auto parts) {
         return n->dtype == RB_F32 ? norm_forward<float, lanes(), parts()>(a, st) : norm_forward<Bf16, lanes(), parts()>(a, st);
     });
     return e == hipSuccess ? RB_OK : RB_EHIP;
@@ -204,7 +236,8 @@ int rb_norm_grad(rb_norm* n, const rb_rows* grad_y, const rb_rows* total, const 
     NormGradArgs a{};
     if (!drop_of(drop, a.drop)) return RB_EINVAL;
     const bool wanted = grad_weight || grad_bias;
-    if (wanted && !n->sums) return RB_ESTATE;
+    if (!n->sums) return RB_ESTATE;
+    if (rows == 0 && !wanted) return RB_OK;
     a.grad_y = grad_y->data;
     a.grad_y_stride = grad_y->stride;
     a.total = total->data;
@@ -222,21 +255,22 @@ int rb_norm_grad(rb_norm* n, const rb_rows* grad_y, const rb_rows* total, const 
     a.weight = weight;
     a.mean = mean;
     a.rstd = rstd;
-    a.sums = wanted ? n->sums : nullptr;
+    a.sums = n->sums;
     a.rows = (int32_t)rows;
     a.width = n->width;
     a.wide_weights = n->weight_dtype == RB_F32;
     a.drops = drop != nullptr;
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     hipError_t e = hipSuccess;
-    unsigned groups = norm_groups(rows, rows_at_once(n->width), NM_MAX_GROUPS / 256);
+    const unsigned groups = grad_form(n, [&](auto, auto lanes, auto) { return norm_groups(rows, std::min(lanes(), 512), NM_SUM_WAVES); });
     if (wanted && n->width > NM_FUSED_WIDTH) {       // (before grad_y may be overwritten)
         const dim3 grid(groups, (unsigned)(n->width + NM_TPB * NM_PIECE - 1) / (NM_TPB * NM_PIECE));
         if (rows > 0) e = n->dtype == RB_F32 ? launch(rb_norm_columns_kernel<float>, grid, NM_TPB, 0, st, a) : launch(rb_norm_columns_kernel<Bf16>, grid, NM_TPB, 0, st, a);
     }
     if (e == hipSuccess && rows > 0)
-        e = by_width(n->width, [&](auto lanes, auto parts) {
-            return n->dtype == RB_F32 ? norm_grad<float, lanes(), parts()>(a, groups, st) : norm_grad<Bf16, lanes(), parts()>(a, groups, st);
+        e = grad_form(n, [&](auto type, auto lanes, auto parts) {
+            const dim3 grid(lanes() <= 512 ? groups : norm_groups(rows, lanes(), 4));
+            return launch(rb_norm_grad_kernel<decltype(type), lanes(), parts()>, grid, nm_threads(lanes()), 0, st, a);
         });
     if (e == hipSuccess && wanted) {
         const dim3 grid((unsigned)(n->width + 63) / 64, 2);

@@ -23,69 +23,98 @@ constexpr int NM_MAX_GROUPS = 512;                 // most workgroups whose sums
 
 // ---- numbers -------------------------------------------------------------------
 
-// Pieces of a row at any alignment (the hardware's 16-byte accesses take any address); the last one of a row may be shorter.
-template <typename T> __device__ __forceinline__ void nm_load(const T* p, int there, float (&v)[8]);
-template <> __device__ __forceinline__ void nm_load<float>(const float* p, int there, float (&v)[8])
-{
-    if (there >= 8) {
-        memcpy(v, p, 32);
-        return;
+// Eight numbers of a row as they lie in memory, at any alignment (the hardware's accesses of 16 bytes take any address).
+template <typename T> struct Piece;
+template <> struct Piece<float> {
+    float v[8];
+    __device__ __forceinline__ float get(int i) const { return v[i]; }
+    __device__ __forceinline__ void set(const float (&x)[8])
+    {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = x[i];
     }
+    __device__ __forceinline__ void load(const float* p) { memcpy(v, p, 32); }
+    __device__ __forceinline__ void store(float* p) const { memcpy(p, v, 32); }
+    __device__ __forceinline__ void put(float* p, float x) const { *p = x; }
+    __device__ __forceinline__ void keep()
+    {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = i < there ? p[i] : 0.0f;
-}
-template <> __device__ __forceinline__ void nm_load<Bf16>(const Bf16* p, int there, float (&v)[8])
-{
-    if (there >= 8) {
-        sc_vec w;
-        memcpy(&w, p, 16);
+        for (int i = 0; i < 8; ++i) asm volatile("" : "+v"(v[i]));
+    }
+};
+template <> struct Piece<Bf16> {
+    sc_vec w;
+    __device__ __forceinline__ float get(int i) const { return __uint_as_float(i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16); }
+    __device__ __forceinline__ void set(const float (&x)[8])
+    {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            v[2 * i] = __uint_as_float(w[i] << 16);
-            v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+        for (int i = 0; i < 4; ++i) w[i] = sc_bf16_pair(x[2 * i], x[2 * i + 1]);
+    }
+    __device__ __forceinline__ void load(const Bf16* p) { memcpy(&w, p, 16); }
+    __device__ __forceinline__ void store(Bf16* p) const { memcpy(p, &w, 16); }
+    __device__ __forceinline__ void put(Bf16* p, float x) const { p->bits = (uint16_t)sc_bf16_bits(x); }
+    // From here on the numbers are taken apart anew (otherwise the compiler keeps all of them as binary32 beside the row).
+    __device__ __forceinline__ void keep() { asm volatile("" : "+v"(w)); }
+};
+
+__device__ __forceinline__ float nm_number(float x) { return x; }
+__device__ __forceinline__ float nm_number(Bf16 x) { return __uint_as_float((uint32_t)x.bits << 16); }
+
+// A row's pieces: lane `lane` of LANES has the pieces p * LANES + lane, p < PARTS, and the row ends among those of the last part.  Where it does not end with
+// a piece, the last one is the row's last eight numbers: the first `skip` of them are another lane's too, which makes the same of them; sums leave them out
+// here.  (Lanes behind the row's end have its last eight numbers as well, and skip all.)  Rows of less than eight numbers come one by one.
+template <int LANES, int PARTS>
+struct Row {
+    int width, lane, skip, last;       // of the last part: where it is
+    __device__ __forceinline__ Row(int width_, int lane_) : width(width_), lane(lane_)
+    {
+        const int column = ((PARTS - 1) * LANES + lane) * NM_PIECE;
+        last = max(min(column, width - NM_PIECE), 0);
+        skip = column < width ? column - last : NM_PIECE;
+    }
+    __device__ __forceinline__ bool tiny() const { return LANES == 16 && PARTS == 1 && width < NM_PIECE; }
+    __device__ __forceinline__ int column(int p) const { return p < PARTS - 1 ? (p * LANES + lane) * NM_PIECE : last; }
+    __device__ __forceinline__ bool counts(int p, int i) const { return p < PARTS - 1 || (i >= skip && (LANES != 16 || PARTS != 1 || i < width)); }
+    template <typename T>
+    __device__ __forceinline__ void load(const T* row, int p, Piece<T>& x) const
+    {
+        if (tiny()) {
+            float v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = i < width ? nm_number(row[i]) : 0.0f;
+            x.set(v);
+        } else {
+            x.load(row + column(p));
         }
-        return;
     }
+    template <typename T>
+    __device__ __forceinline__ void store(T* row, int p, const Piece<T>& x) const
+    {
+        if (p == PARTS - 1 && skip == NM_PIECE) return;
+        if (tiny()) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = i < there ? __uint_as_float((uint32_t)p[i].bits << 16) : 0.0f;
-}
-
-__device__ __forceinline__ void nm_store(float* p, int there, const float (&v)[8])
-{
-    if (there >= 8) {
-        memcpy(p, v, 32);
-        return;
+            for (int i = 0; i < 7; ++i)
+                if (i < width) x.put(row + i, x.get(i));
+        } else {
+            x.store(row + column(p));
+        }
     }
+    // Weights are binary32 or bfloat16, as the handle says (the same for all lanes).
+    __device__ __forceinline__ void weights(const void* w, bool wide, int p, float (&v)[8]) const
+    {
+        if (wide) {
+            Piece<float> x;
+            load(static_cast<const float*>(w), p, x);
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-        if (i < there) p[i] = v[i];
-}
-__device__ __forceinline__ void nm_store(Bf16* p, int there, const float (&v)[8])
-{
-    if (there >= 8) {
-        sc_vec w;
+            for (int i = 0; i < 8; ++i) v[i] = x.get(i);
+        } else {
+            Piece<Bf16> x;
+            load(static_cast<const Bf16*>(w), p, x);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = sc_bf16_pair(v[2 * i], v[2 * i + 1]);
-        memcpy(p, &w, 16);
-        return;
+            for (int i = 0; i < 8; ++i) v[i] = x.get(i);
+        }
     }
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-        if (i < there) p[i].bits = (uint16_t)sc_bf16_bits(v[i]);
-}
-
-template <typename T> __device__ __forceinline__ float nm_round(float x)
-{
-    if constexpr (std::is_same_v<T, float>) return x;
-    else return __uint_as_float(sc_bf16_bits(x) << 16);
-}
-
-// Weights are binary32 or bfloat16, as the handle says (the same for all lanes).
-__device__ __forceinline__ void nm_weights(const void* w, bool wide, int column, int there, float (&v)[8])
-{
-    if (wide) nm_load(static_cast<const float*>(w) + column, there, v);
-    else nm_load(static_cast<const Bf16*>(w) + column, there, v);
-}
+};
 
 // ---- dropout -------------------------------------------------------------------
 
@@ -95,10 +124,9 @@ struct Drop {
     float scale;
 };
 
-// Which of the eight elements of a piece stay: Philox4x32-10 (Salmon et al., SC'11) of the row and the piece, 16 bits an element.
-__device__ __forceinline__ void nm_drop(const Drop& d, uint32_t row, uint32_t piece, float (&v)[8])
+// Philox4x32-10 (Salmon et al., SC'11) of a row and a piece of it, 16 bits an element.
+__device__ __forceinline__ void nm_draw(const Drop& d, uint32_t row, uint32_t piece, uint32_t (&x)[4])
 {
-    if (d.least == 0) return;
     uint32_t x0 = row, x1 = 0x80000000u | piece, x2 = d.step_lo, x3 = d.step_hi, ka = d.seed_lo, kb = d.seed_hi;
 #pragma unroll
     for (int i = 0; i < 10; ++i) {
@@ -110,7 +138,31 @@ __device__ __forceinline__ void nm_drop(const Drop& d, uint32_t row, uint32_t pi
         ka += 0x9E3779B9u;
         kb += 0xBB67AE85u;
     }
-    const uint32_t x[4] = {x0, x1, x2, x3};
+    x[0] = x0; x[1] = x1; x[2] = x2; x[3] = x3;
+}
+
+// What stays of the eight numbers from `column` on.  Those of a row's end may be parts of two pieces (ENDS: it may be the end).
+template <bool ENDS>
+__device__ __forceinline__ void nm_drop(const Drop& d, uint32_t row, int column, float (&v)[8])
+{
+    if (d.least == 0) return;
+    uint32_t x[4];
+    nm_draw(d, row, (uint32_t)column / NM_PIECE, x);
+    const int by = column % NM_PIECE;
+    if (ENDS && __any(by != 0)) {
+        uint32_t more[4];
+        nm_draw(d, row, (uint32_t)column / NM_PIECE + 1, more);
+        // the sixteen halves move down by as many as the first number is behind its piece's begin
+        const bool one = by & 1, two = by & 2, four = by & 4;
+        const uint32_t a0 = one ? x[0] >> 16 | x[1] << 16 : x[0], a1 = one ? x[1] >> 16 | x[2] << 16 : x[1], a2 = one ? x[2] >> 16 | x[3] << 16 : x[2];
+        const uint32_t a3 = one ? x[3] >> 16 | more[0] << 16 : x[3], a4 = one ? more[0] >> 16 | more[1] << 16 : more[0];
+        const uint32_t a5 = one ? more[1] >> 16 | more[2] << 16 : more[1], a6 = one ? more[2] >> 16 | more[3] << 16 : more[2];
+        const uint32_t b0 = two ? a1 : a0, b1 = two ? a2 : a1, b2 = two ? a3 : a2, b3 = two ? a4 : a3, b4 = two ? a5 : a4, b5 = two ? a6 : a5;
+        x[0] = four ? b2 : b0;
+        x[1] = four ? b3 : b1;
+        x[2] = four ? b4 : b2;
+        x[3] = four ? b5 : b3;
+    }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         v[2 * i] = (x[i] & 0xffffu) >= d.least ? v[2 * i] * d.scale : 0.0f;
@@ -140,13 +192,31 @@ __global__ void __launch_bounds__(NM_TPB) rb_dropout_kernel(DropoutArgs a)
     for (int64_t item = blockIdx.x; item < a.items; item += gridDim.x) {
         const int64_t line = item / a.blocks;
         const int64_t row = line * a.at_once + r;
-        const int piece = (int)(item - line * a.blocks) * NM_TPB + p;
+        const int piece = (int)(item - line * a.blocks) * NM_TPB + p, column = piece * NM_PIECE;
         if (row >= a.rows || piece >= a.pieces) continue;
-        const int there = a.width - piece * NM_PIECE;
+        const T* const from = static_cast<const T*>(a.x) + row * a.x_stride + column;
+        T* const to = static_cast<T*>(a.out) + row * a.out_stride + column;
+        const int there = a.width - column;
+        Piece<T> x;
         float v[8];
-        nm_load(static_cast<const T*>(a.x) + row * a.x_stride + piece * NM_PIECE, there, v);
-        nm_drop(a.drop, (uint32_t)row, (uint32_t)piece, v);
-        nm_store(static_cast<T*>(a.out) + row * a.out_stride + piece * NM_PIECE, there, v);
+        if (there >= NM_PIECE) {
+            x.load(from);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = i < there ? nm_number(from[i]) : 0.0f;
+            x.set(v);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = x.get(i);
+        nm_drop<false>(a.drop, (uint32_t)row, column, v);
+        x.set(v);
+        if (there >= NM_PIECE) {
+            x.store(to);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 7; ++i)
+                if (i < there) x.put(to + i, x.get(i));
+        }
     }
 }
 
@@ -172,7 +242,7 @@ __device__ __forceinline__ void nm_sum(float (&v)[N], float* places)
         if ((threadIdx.x & 63) == 0)
 #pragma unroll
             for (int i = 0; i < N; ++i) places[threadIdx.x / 64 * N + i] = v[i];
-        __syncthreads();
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");       // (not for what is on its way from memory)
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             v[i] = 0.0f;
@@ -195,125 +265,166 @@ struct NormArgs {
     Drop drop;
 };
 
-template <typename T, int LANES, int PARTS>
-__global__ void __launch_bounds__(LANES > NM_TPB ? LANES : NM_TPB) rb_norm_kernel(NormArgs a)
+// Wavefronts that share a SIMD, so how many workgroups of how many threads a grid that fills the chip once has.
+constexpr int nm_threads(int lanes) { return lanes > NM_TPB ? lanes : NM_TPB; }
+template <typename T>
+constexpr int nm_waves(int lanes, int parts)
 {
-    constexpr int TPB = LANES > NM_TPB ? LANES : NM_TPB, ROWS = TPB / LANES;
-    constexpr bool KEPT = PARTS <= 4 && LANES <= NM_TPB;       // weights stay in registers between rows
+    const int registers = parts * (int)sizeof(T) / 2;      // of a row, by fours
+    return lanes > 512 || registers <= 2 ? 4 : registers <= 4 ? 3 : 2;
+}
+
+// A workgroup goes through rows that are the grid's width apart; the next row is on its way while one is worked on.  What is kept of a row is as it lies in
+// memory (the sum is rounded to that type anyway).  SUMMED: there is a residual or dropout.  The sum is stored when all of the row has been read (a lane that
+// has numbers of another one reads them in its own time).
+template <typename T, int LANES, int PARTS, bool SUMMED>
+__global__ void __launch_bounds__(nm_threads(LANES), nm_waves<T>(LANES, PARTS)) rb_norm_kernel(NormArgs a)
+{
+    constexpr int ROWS = nm_threads(LANES) / LANES;
+    constexpr bool KEPT = PARTS * sizeof(T) <= 4;              // weights stay in registers between rows
     __shared__ float places[2][2][32];
-    const int lane = threadIdx.x % LANES;
+    const Row<LANES, PARTS> of(a.width, threadIdx.x % LANES);
+    const int line = threadIdx.x / LANES;
+    Piece<T> x[PARTS], next[PARTS], next_r[SUMMED ? PARTS : 1];
+    auto row_of = [&](int64_t first) { return min(first + line, (int64_t)a.rows - 1); };       // (of the last rows some are made twice, alike)
+    auto fetch = [&](int64_t row) {
+#pragma unroll
+        for (int p = 0; p < PARTS; ++p) of.load(static_cast<const T*>(a.x) + row * a.x_stride, p, next[p]);
+        if (SUMMED && a.residual) {
+#pragma unroll
+            for (int p = 0; p < PARTS; ++p) of.load(static_cast<const T*>(a.residual) + row * a.residual_stride, p, next_r[p]);
+        }
+    };
+    int64_t first = (int64_t)blockIdx.x * ROWS;
+    fetch(row_of(first));
     float w[KEPT ? PARTS : 1][8], b[KEPT ? PARTS : 1][8];
+    auto fetch_weights = [&](int p, float (&ww)[8], float (&bb)[8]) {
+        of.weights(a.weight, a.wide_weights, p, ww);
+        if (a.bias) of.weights(a.bias, a.wide_weights, p, bb);
+        else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) bb[i] = 0.0f;
+        }
+    };
     if constexpr (KEPT) {
 #pragma unroll
-        for (int p = 0; p < PARTS; ++p) {
-            const int piece = p * LANES + lane, there = a.width - piece * NM_PIECE;
-            nm_weights(a.weight, a.wide_weights, piece * NM_PIECE, there, w[p]);
-            if (a.bias) nm_weights(a.bias, a.wide_weights, piece * NM_PIECE, there, b[p]);
-            else
-                for (int i = 0; i < 8; ++i) b[p][i] = 0.0f;
-        }
+        for (int p = 0; p < PARTS; ++p) fetch_weights(p, w[p], b[p]);
     }
-    int turn = 0;
-    for (int64_t first = (int64_t)blockIdx.x * ROWS; first < a.rows; first += (int64_t)gridDim.x * ROWS, turn ^= 1) {
-        const int64_t row = min(first + threadIdx.x / LANES, (int64_t)a.rows - 1);       // (of the last rows some are made twice, alike)
-        const bool mine = first + threadIdx.x / LANES < a.rows;
-        float v[PARTS][8];
+    const float width = (float)a.width;
+    for (int turn = 0; first < a.rows; first += (int64_t)gridDim.x * ROWS, turn ^= 1) {
+        const int64_t row = row_of(first);
+        const bool mine = first + line < a.rows;
         float sum[1] = {0.0f};
+        // part by part: all parts' draws side by side would not fit
 #pragma unroll
         for (int p = 0; p < PARTS; ++p) {
-            const int piece = p * LANES + lane, there = a.width - piece * NM_PIECE;
-            nm_load(static_cast<const T*>(a.x) + row * a.x_stride + piece * NM_PIECE, there, v[p]);
-        }
-        if (a.total) {
+            x[p] = next[p];
+            if constexpr (SUMMED) {
+                float v[8];
 #pragma unroll
-            for (int p = 0; p < PARTS; ++p) {
-                const int piece = p * LANES + lane, there = a.width - piece * NM_PIECE;
-                if (a.drops) nm_drop(a.drop, (uint32_t)row, (uint32_t)piece, v[p]);
-                if (a.residual) {
-                    float r[8];
-                    nm_load(static_cast<const T*>(a.residual) + row * a.residual_stride + piece * NM_PIECE, there, r);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) v[p][i] += r[i];
+                for (int i = 0; i < 8; ++i) v[i] = x[p].get(i);
+                if (a.drops) {
+                    if (p == PARTS - 1) nm_drop<true>(a.drop, (uint32_t)row, of.column(p), v);
+                    else nm_drop<false>(a.drop, (uint32_t)row, of.column(p), v);
                 }
+                if (a.residual) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) v[p][i] = nm_round<T>(v[p][i]);
-                if (mine) nm_store(static_cast<T*>(a.total) + row * a.total_stride + piece * NM_PIECE, there, v[p]);
+                    for (int i = 0; i < 8; ++i) v[i] += next_r[p].get(i);
+                }
+                x[p].set(v);
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum[0] += of.counts(p, i) ? x[p].get(i) : 0.0f;
+            x[p].keep();
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if (first + (int64_t)gridDim.x * ROWS < a.rows) fetch(row_of(first + (int64_t)gridDim.x * ROWS));
+        nm_sum<LANES>(sum, places[turn][0]);
+        if constexpr (SUMMED) {
+            if (mine) {
+#pragma unroll
+                for (int p = 0; p < PARTS; ++p) of.store(static_cast<T*>(a.total) + row * a.total_stride, p, x[p]);
             }
         }
-#pragma unroll
-        for (int p = 0; p < PARTS; ++p)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) sum[0] += v[p][i];
-        nm_sum<LANES>(sum, places[turn][0]);
-        const float width = (float)a.width;
-        float mean = sum[0] / width;
+        const float mean = sum[0] / width;
         float off[2] = {0.0f, 0.0f};               // sums of the differences and of their squares
 #pragma unroll
         for (int p = 0; p < PARTS; ++p) {
-            const int there = a.width - (p * LANES + lane) * NM_PIECE;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const float d = i < there ? v[p][i] - mean : 0.0f;
-                v[p][i] = d;
+                const float d = of.counts(p, i) ? x[p].get(i) - mean : 0.0f;
                 off[0] += d;
                 off[1] = fmaf(d, d, off[1]);
             }
+            x[p].keep();
         }
         nm_sum<LANES>(off, places[turn][1]);
         const float more = off[0] / width;
-        const float rstd = 1.0f / sqrtf(fmaxf(fmaf(-more, more, off[1] / width), 0.0f) + a.eps);
-        mean += more;
-        if (mine && lane == 0) {
-            if (a.mean) a.mean[row] = mean;
-            if (a.rstd) a.rstd[row] = off[1] != off[1] ? off[1] : rstd;
+        float rstd = 1.0f / sqrtf(fmaxf(fmaf(-more, more, off[1] / width), 0.0f) + a.eps);
+        if (off[1] != off[1]) rstd = off[1];       // (a NaN is none of fmaxf's)
+        if (mine && of.lane == 0) {
+            if (a.mean) a.mean[row] = mean + more;
+            if (a.rstd) a.rstd[row] = rstd;
         }
 #pragma unroll
         for (int p = 0; p < PARTS; ++p) {
-            const int piece = p * LANES + lane, there = a.width - piece * NM_PIECE;
             float out[8], ww[8], bb[8];
-            if constexpr (!KEPT) {
-                nm_weights(a.weight, a.wide_weights, piece * NM_PIECE, there, ww);
-                if (a.bias) nm_weights(a.bias, a.wide_weights, piece * NM_PIECE, there, bb);
-                else
-                    for (int i = 0; i < 8; ++i) bb[i] = 0.0f;
-            }
+            if constexpr (!KEPT) fetch_weights(p, ww, bb);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const float h = (v[p][i] - more) * rstd;
+                const float h = (x[p].get(i) - mean - more) * rstd;        // (the mean as two numbers: rows far from 0)
                 if constexpr (KEPT) out[i] = fmaf(h, w[p][i], b[p][i]);
                 else out[i] = fmaf(h, ww[i], bb[i]);
             }
-            if (mine) nm_store(static_cast<T*>(a.y) + row * a.y_stride + piece * NM_PIECE, there, out);
+            Piece<T> y;
+            y.set(out);
+            if (mine) of.store(static_cast<T*>(a.y) + row * a.y_stride, p, y);
         }
     }
 }
 
 // ---- gradients -----------------------------------------------------------------
 
+constexpr int NM_SUM_WAVES = 2;
+
 struct NormGradArgs {
     const void *grad_y, *total, *grad_total, *weight;
     const float *mean, *rstd;
     void *grad_sum, *grad_x;
-    float* sums;                       // [2][groups][width]: of the weight's and of the bias's gradient; null: none is wanted
+    float* sums;                       // [2][groups][width]: of the weight's and of the bias's gradient
     int64_t grad_y_stride, total_stride, grad_total_stride, grad_sum_stride, grad_x_stride;
     int32_t rows, width;
     bool wide_weights, drops;
     Drop drop;
 };
 
-// SUMS: the weights' gradients are summed on the way.
-template <typename T, int LANES, int PARTS, bool SUMS>
-__global__ void __launch_bounds__(LANES > NM_TPB ? LANES : NM_TPB) rb_norm_grad_kernel(NormGradArgs a)
+// As forward; the gradients of the next row's y and that row are on their way while one is worked on.  SUMS: the weights' gradients are summed on the way (of rows
+// that leave room for the sums).
+template <typename T, int LANES, int PARTS>
+__global__ void __launch_bounds__(nm_threads(LANES), LANES > 512 ? 4 : NM_SUM_WAVES) rb_norm_grad_kernel(NormGradArgs a)
 {
-    constexpr int TPB = LANES > NM_TPB ? LANES : NM_TPB, ROWS = TPB / LANES;
-    constexpr bool KEPT = PARTS <= 4 && LANES <= NM_TPB;
+    constexpr bool SUMS = LANES <= 512;
+    constexpr int TPB = nm_threads(LANES), ROWS = TPB / LANES;
+    constexpr bool KEPT = SUMS && PARTS * sizeof(T) <= (sizeof(T) == 2 ? 6 : 8);       // weights stay in registers between rows
     __shared__ float places[2][32];
-    const int lane = threadIdx.x % LANES;
+    const Row<LANES, PARTS> of(a.width, threadIdx.x % LANES);
+    const int line = threadIdx.x / LANES;
+    Piece<T> next_y[PARTS], next_t[PARTS];
+    auto row_of = [&](int64_t first) { return min(first + line, (int64_t)a.rows - 1); };
+    auto fetch = [&](int64_t row) {
+#pragma unroll
+        for (int p = 0; p < PARTS; ++p) {
+            of.load(static_cast<const T*>(a.grad_y) + row * a.grad_y_stride, p, next_y[p]);
+            of.load(static_cast<const T*>(a.total) + row * a.total_stride, p, next_t[p]);
+        }
+    };
+    int64_t first = (int64_t)blockIdx.x * ROWS;
+    fetch(row_of(first));
     float w[KEPT ? PARTS : 1][8];
     float gw[SUMS ? PARTS : 1][8], gb[SUMS ? PARTS : 1][8];
     if constexpr (KEPT) {
 #pragma unroll
-        for (int p = 0; p < PARTS; ++p) nm_weights(a.weight, a.wide_weights, (p * LANES + lane) * NM_PIECE, a.width - (p * LANES + lane) * NM_PIECE, w[p]);
+        for (int p = 0; p < PARTS; ++p) of.weights(a.weight, a.wide_weights, p, w[p]);
     }
     if constexpr (SUMS) {
 #pragma unroll
@@ -321,62 +432,77 @@ __global__ void __launch_bounds__(LANES > NM_TPB ? LANES : NM_TPB) rb_norm_grad_
 #pragma unroll
             for (int i = 0; i < 8; ++i) gw[p][i] = gb[p][i] = 0.0f;
     }
-    int turn = 0;
-    for (int64_t first = (int64_t)blockIdx.x * ROWS; first < a.rows; first += (int64_t)gridDim.x * ROWS, turn ^= 1) {
-        const int64_t row = min(first + threadIdx.x / LANES, (int64_t)a.rows - 1);
-        const bool mine = first + threadIdx.x / LANES < a.rows;
+    for (int turn = 0; first < a.rows; first += (int64_t)gridDim.x * ROWS, turn ^= 1) {
+        const int64_t row = row_of(first);
+        const bool mine = first + line < a.rows;
         const float mean = a.mean[row], rstd = a.rstd[row];
-        float g[PARTS][8], h[PARTS][8];
-        float sum[2] = {0.0f, 0.0f};
+        Piece<T> y[PARTS], t[PARTS], more[PARTS];
+        if (a.grad_total) {
 #pragma unroll
-        for (int p = 0; p < PARTS; ++p) {
-            const int piece = p * LANES + lane, there = a.width - piece * NM_PIECE;
-            nm_load(static_cast<const T*>(a.grad_y) + row * a.grad_y_stride + piece * NM_PIECE, there, g[p]);
-            nm_load(static_cast<const T*>(a.total) + row * a.total_stride + piece * NM_PIECE, there, h[p]);
+            for (int p = 0; p < PARTS; ++p) of.load(static_cast<const T*>(a.grad_total) + row * a.grad_total_stride, p, more[p]);
         }
-#pragma unroll
-        for (int p = 0; p < PARTS; ++p) {
-            const int piece = p * LANES + lane, there = a.width - piece * NM_PIECE;
+        float sum[2] = {0.0f, 0.0f};
+        auto part = [&](int p, float (&g)[8], float (&h)[8]) {       // grad_y * weight and the normalised row
             float ww[8];
-            if constexpr (!KEPT) nm_weights(a.weight, a.wide_weights, piece * NM_PIECE, there, ww);
+            if constexpr (!KEPT) of.weights(a.weight, a.wide_weights, p, ww);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                h[p][i] = i < there ? (h[p][i] - mean) * rstd : 0.0f;
-                if constexpr (SUMS) {
-                    if (mine) {
-                        gw[p][i] = fmaf(g[p][i], h[p][i], gw[p][i]);
-                        gb[p][i] += g[p][i];
-                    }
-                }
-                if constexpr (KEPT) g[p][i] *= w[p][i];
-                else g[p][i] *= ww[i];
-                sum[0] += g[p][i];
-                sum[1] = fmaf(g[p][i], h[p][i], sum[1]);
+                h[i] = (t[p].get(i) - mean) * rstd;
+                if constexpr (KEPT) g[i] = y[p].get(i) * w[p][i];
+                else g[i] = y[p].get(i) * ww[i];
             }
+        };
+#pragma unroll
+        for (int p = 0; p < PARTS; ++p) {
+            float g[8], h[8];
+            y[p] = next_y[p];
+            t[p] = next_t[p];
+            part(p, g, h);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const bool counts = of.counts(p, i);
+                if constexpr (SUMS) {
+                    const bool adds = counts && (ROWS == 1 || mine);
+                    gw[p][i] += adds ? y[p].get(i) * h[i] : 0.0f;
+                    gb[p][i] += adds ? y[p].get(i) : 0.0f;
+                }
+                sum[0] += counts ? g[i] : 0.0f;
+                sum[1] += counts ? g[i] * h[i] : 0.0f;
+            }
+            y[p].keep();
+            t[p].keep();
+            __builtin_amdgcn_sched_barrier(0);
         }
+        if (first + (int64_t)gridDim.x * ROWS < a.rows) fetch(row_of(first + (int64_t)gridDim.x * ROWS));
+        if (a.grad_total) more[PARTS - 1].keep();          // (has been read before any lane may write there)
         nm_sum<LANES>(sum, places[turn]);
         const float c0 = sum[0] / (float)a.width, c1 = sum[1] / (float)a.width;
 #pragma unroll
         for (int p = 0; p < PARTS; ++p) {
-            const int piece = p * LANES + lane, there = a.width - piece * NM_PIECE;
-            float d[8];
+            float g[8], h[8], d[8];
+            part(p, g, h);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) d[i] = rstd * (g[p][i] - c0 - h[p][i] * c1);
+            for (int i = 0; i < 8; ++i) d[i] = rstd * (g[i] - c0 - h[i] * c1);
             if (a.grad_total) {
-                float r[8];
-                nm_load(static_cast<const T*>(a.grad_total) + row * a.grad_total_stride + piece * NM_PIECE, there, r);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) d[i] += r[i];
+                for (int i = 0; i < 8; ++i) d[i] += more[p].get(i);
             }
-            if (mine) nm_store(static_cast<T*>(a.grad_sum) + row * a.grad_sum_stride + piece * NM_PIECE, there, d);
+            Piece<T> out;
+            out.set(d);
+            if (mine) of.store(static_cast<T*>(a.grad_sum) + row * a.grad_sum_stride, p, out);
             if (a.drops) {
-                nm_drop(a.drop, (uint32_t)row, (uint32_t)piece, d);
-                if (mine) nm_store(static_cast<T*>(a.grad_x) + row * a.grad_x_stride + piece * NM_PIECE, there, d);
+                if (p == PARTS - 1) nm_drop<true>(a.drop, (uint32_t)row, of.column(p), d);
+                else nm_drop<false>(a.drop, (uint32_t)row, of.column(p), d);
+                out.set(d);
+                if (mine) of.store(static_cast<T*>(a.grad_x) + row * a.grad_x_stride, p, out);
             }
+            __builtin_amdgcn_sched_barrier(0);
         }
     }
     if constexpr (SUMS) {
         // the workgroup's rows together, and its sums to memory
+        float* const to_w = a.sums + (int64_t)blockIdx.x * a.width;
+        float* const to_b = a.sums + ((int64_t)gridDim.x + blockIdx.x) * a.width;
         if constexpr (ROWS > 1) {
             __shared__ float join[ROWS][LANES * PARTS * 8];
             for (int which = 0; which < 2; ++which) {
@@ -384,22 +510,25 @@ __global__ void __launch_bounds__(LANES > NM_TPB ? LANES : NM_TPB) rb_norm_grad_
 #pragma unroll
                 for (int p = 0; p < PARTS; ++p)
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) join[threadIdx.x / LANES][(p * LANES + lane) * 8 + i] = which ? gb[p][i] : gw[p][i];
+                    for (int i = 0; i < 8; ++i)
+                        if (of.counts(p, i)) join[line][of.column(p) + i] = which ? gb[p][i] : gw[p][i];
                 __syncthreads();
                 for (int c = threadIdx.x; c < a.width; c += TPB) {
                     float s = 0.0f;
 #pragma unroll
                     for (int r = 0; r < ROWS; ++r) s += join[r][c];
-                    a.sums[((int64_t)which * gridDim.x + blockIdx.x) * a.width + c] = s;
+                    (which ? to_b : to_w)[c] = s;
                 }
             }
         } else {
 #pragma unroll
-            for (int p = 0; p < PARTS; ++p) {
-                const int column = (p * LANES + lane) * NM_PIECE, there = a.width - column;
-                nm_store(a.sums + (int64_t)blockIdx.x * a.width + column, there, gw[p]);
-                nm_store(a.sums + ((int64_t)gridDim.x + blockIdx.x) * a.width + column, there, gb[p]);
-            }
+            for (int p = 0; p < PARTS; ++p)
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (of.counts(p, i)) {
+                        to_w[of.column(p) + i] = gw[p][i];
+                        to_b[of.column(p) + i] = gb[p][i];
+                    }
         }
     }
 }
@@ -408,22 +537,27 @@ __global__ void __launch_bounds__(LANES > NM_TPB ? LANES : NM_TPB) rb_norm_grad_
 template <typename T>
 __global__ void __launch_bounds__(NM_TPB) rb_norm_columns_kernel(NormGradArgs a)
 {
-    const int column = (blockIdx.y * NM_TPB + threadIdx.x) * NM_PIECE, there = a.width - column;
-    if (there <= 0) return;
+    const int column = (blockIdx.y * NM_TPB + threadIdx.x) * NM_PIECE;
+    if (column >= a.width) return;
+    const int last = min(column, a.width - NM_PIECE);          // (the row's last piece as Row says)
     float gw[8] = {}, gb[8] = {};
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
         const float mean = a.mean[row], rstd = a.rstd[row];
-        float g[8], h[8];
-        nm_load(static_cast<const T*>(a.grad_y) + row * a.grad_y_stride + column, there, g);
-        nm_load(static_cast<const T*>(a.total) + row * a.total_stride + column, there, h);
+        Piece<T> y, t;
+        y.load(static_cast<const T*>(a.grad_y) + row * a.grad_y_stride + last);
+        t.load(static_cast<const T*>(a.total) + row * a.total_stride + last);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            gw[i] = fmaf(g[i], (h[i] - mean) * rstd, gw[i]);
-            gb[i] += g[i];
+            gw[i] = fmaf(y.get(i), (t.get(i) - mean) * rstd, gw[i]);
+            gb[i] += y.get(i);
         }
     }
-    nm_store(a.sums + (int64_t)blockIdx.x * a.width + column, there, gw);
-    nm_store(a.sums + ((int64_t)gridDim.x + blockIdx.x) * a.width + column, there, gb);
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (last + i >= column) {
+            a.sums[(int64_t)blockIdx.x * a.width + last + i] = gw[i];
+            a.sums[((int64_t)gridDim.x + blockIdx.x) * a.width + last + i] = gb[i];
+        }
 }
 
 // The workgroups' sums together: 64 columns of a workgroup, 16 parts of the groups for each.

@@ -83,7 +83,6 @@ def test_norm_calls_refuse():
     good = dict(n=n, grad_y=rows(P), total=rows(2 * P), grad_total=rows(3 * P), mean=4 * P, rstd=5 * P, drop=d, rows=2, weight=6 * P, grad_sum=rows(7 * P), grad_x=rows(8 * P),
                 grad_weight=10 * P, grad_bias=11 * P)
     assert rb.rb_norm_grad(*good.values(), STREAM) == rb.RB_ESTATE                 # never bound
-    assert rb.rb_norm_grad(*{**good, **dict(rows=0, grad_weight=None, grad_bias=None)}.values(), STREAM) == rb.RB_OK
     refused(rb.rb_norm_grad, good, (
         dict(n=None), dict(rows=-1), dict(rows=rb.RB_MAX_NORM_ROWS + 1), dict(drop=bad_d), dict(drop=None), dict(grad_x=None), dict(mean=None), dict(rstd=None), dict(mean=P + 2),
         dict(rstd=P + 1), dict(weight=None), dict(weight=P + 1), dict(grad_weight=P + 2), dict(grad_bias=P + 1), dict(grad_sum=rows(2 * P)), dict(grad_x=rows(2 * P)),

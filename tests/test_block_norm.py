@@ -75,8 +75,8 @@ def check(x, residual, drop, weight, bias, eps=1e-5):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
-@pytest.mark.parametrize("width", [1, 2, 7, 8, 9, 63, 64, 127, 128, 129, 200, 511, 512, 513, 1000, 1024, 1025, 2047, 2048, 2049, 4096, 4097, 5003, 8192, 8193, 10007,
-                                   32768, 32769, 65536])
+@pytest.mark.parametrize("width", [1, 2, 7, 8, 9, 63, 64, 127, 128, 129, 200, 511, 512, 513, 1000, 1024, 1025, 1536, 1537, 2047, 2048, 2049, 4096, 4097, 5003, 6144, 6145,
+                                   8192, 8193, 10007, 12289, 16383, 16385, 24576, 24577, 32763, 32768])
 def test_rows_of_any_length(width, dtype):
     w, b = weights(width, F32)
     check(make(5, width, dtype, mean=0.7), None, None, w, b)
