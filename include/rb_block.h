@@ -160,9 +160,12 @@ int rb_attention_forward(rb_attention *a, const rb_heads *q, const rb_heads *k, 
 
 /*
  * Gradients with respect to q, k and v of a loss with the derivative grad_out of out; out and lse are rb_attention_forward's for the same arguments.  With p =
- * e^(s - lse), dp = grad_out[i] . v[j], ds = p * (dp - grad_out[i] . out[i]), times the cap's slope and scale:
+ * e^(s - lse), dp = grad_out[i] . v[j], ds = p * (dp - sum of p * dp), times the cap's slope and scale:
  *   grad_v[j] = sum over i of p grad_out[i],  grad_q[i] = sum over j of ds k[j],  grad_k[j] = sum over i of ds q[i]
  * (of keys and values over their heads of queries too), sums in binary32, p and ds rounded to bfloat16 for these products, results rounded to bfloat16.
+ * The sum of p * dp is made in binary32 from the first value grad_out[i] . out[i] on, so that out's rounding does not matter.
+ * What a position does not see, or is not seen by, has no influence on its gradients; where it sees or is seen by a q, k, v or grad_out that is not finite, they
+ * are not finite (which of their numbers is not specified).
  * Positions that belong to no document have gradients 0.  What is written overlaps nothing.  (The slopes have no gradient.)
  * RB_EINVAL, RB_ESTATE: as above.
  */

@@ -471,16 +471,18 @@ int rb_attention_grad(rb_attention* a, const rb_heads* q, const rb_heads* k, con
     of_keys.sums = parts > 1 ? reinterpret_cast<float*>(a->ws + a->off_sums) : nullptr;
     hipError_t e = find_spans(a, documents, tokens, st);
     const int64_t rows = tokens * a->heads;
-    if (e == hipSuccess) e = launch(rb_attend_delta_kernel, dim3((unsigned)std::min<int64_t>((rows + AT_TPB / 16 - 1) / (AT_TPB / 16), 1 << 20)), AT_TPB, 0, st, g, lse2, delta);
+    if (e == hipSuccess) e = launch(rb_attend_delta_kernel, dim3((unsigned)std::min<int64_t>((rows + AT_TPB / 16 - 1) / (AT_TPB / 16), 1 << 20)), AT_TPB, 0, st, g, lse2);
     if (e == hipSuccess)
         e = by_form(a, slopes != nullptr, [&](auto dim, auto form, auto lowered) {
-            hipError_t r = launch(rb_attend_grad_kv_kernel<dim(), form(), lowered()>, dim3((unsigned)(g.tiles * of_keys.shares)), AT_TPB, 0, st, of_keys);
+            // (of queries first: it makes delta exact)
+            hipError_t r = launch(rb_attend_grad_q_kernel<dim(), form(), lowered()>, dim3((unsigned)(g.tiles * g.heads)), AT_TPB, 0, st, g);
+            if (r == hipSuccess)
+                r = launch(rb_attend_grad_kv_kernel<dim(), form(), lowered()>, dim3((unsigned)(g.tiles * of_keys.shares)), AT_TPB, 0, st, of_keys);
             if (r == hipSuccess && parts > 1) {
                 const int64_t threads = (int64_t)a->kv_heads * tokens * (2 * dim() / 4);
                 r = launch(rb_attend_join_kernel<dim()>, dim3((unsigned)std::min<int64_t>((threads + AT_TPB - 1) / AT_TPB, 1 << 16)), AT_TPB, 0, st, of_keys);
             }
-            if (r != hipSuccess) return r;
-            return launch(rb_attend_grad_q_kernel<dim(), form(), lowered()>, dim3((unsigned)(g.tiles * g.heads)), AT_TPB, 0, st, g);
+            return r;
         });
     return e == hipSuccess ? RB_OK : RB_EHIP;
 }

@@ -337,7 +337,8 @@ struct AttentionArgs {
     float* lse;
     // gradients
     HeadRows grad_out, grad_q, grad_k, grad_v;
-    const float *lse2, *delta;             // [heads][tokens]: lse in base 2, less lse_less (+inf where nothing is seen); the sum of grad_out * out
+    const float* lse2;                     // [heads][tokens]: lse in base 2, less lse_less (+inf where nothing is seen)
+    float* delta;                          // [heads][tokens]: the sum of grad_out * out; then of p dp
     float lse_less;                        // what scores are less by: of AT_CAPPED the cap
 };
 
@@ -632,7 +633,7 @@ __global__ void __launch_bounds__(AT_TPB, 2) rb_attend_kernel(AttentionArgs a)
 // ---- gradients -----------------------------------------------------------------
 
 // What the gradients need of every row of every head: lse in base 2, and the sum of grad_out * out.  16 lanes a row.
-__global__ void __launch_bounds__(AT_TPB) rb_attend_delta_kernel(AttentionArgs a, float* lse2, float* delta)
+__global__ void __launch_bounds__(AT_TPB) rb_attend_delta_kernel(AttentionArgs a, float* lse2)
 {
     const int64_t rows = (int64_t)a.heads * a.tokens;
     const int first = (threadIdx.x & 15) * 8;
@@ -654,32 +655,34 @@ __global__ void __launch_bounds__(AT_TPB) rb_attend_delta_kernel(AttentionArgs a
         if (first == 0) {
             const Span s = a.spans[t].sees;
             const int64_t to = (int64_t)h * a.tokens + t;
-            delta[to] = sum;
+            a.delta[to] = sum;
             lse2[to] = s.lo < s.hi ? a.lse[to] * AT_LOG2E - a.lse_less : -sc_neg_inf();
         }
     }
 }
 
-// p and ds of one element; less: lse in base 2 (of AT_CAPPED: less the cap) and what the score is lowered by.
-template <int FORM, bool SLOPES>
-__device__ __forceinline__ void at_slope(const ScoreOf& of, float product, float dp, float less, float delta, float& p, float& ds)
+// p of one element and the cap's slope; less: lse in base 2 (of AT_CAPPED: less the cap) and what the score is lowered by.
+template <int FORM>
+__device__ __forceinline__ void at_weight(const ScoreOf& of, float product, float less, float& p, float& slope)
 {
-    float slope = 1.0f;
-    if (FORM != AT_PLAIN) {
-        const float s = at_score<FORM>(of, product, slope);
-        p = __builtin_amdgcn_exp2f(s - less);
-    } else {
-        p = __builtin_amdgcn_exp2f(fmaf(product, of.to_log2, -less));
-    }
-    ds = p * (dp - delta);
-    if (FORM != AT_PLAIN) ds *= slope;
+    slope = 1.0f;
+    if (FORM == AT_PLAIN) p = __builtin_amdgcn_exp2f(fmaf(product, of.to_log2, -less));
+    else p = __builtin_amdgcn_exp2f(at_score<FORM>(of, product, slope) - less);
 }
 
 // Of queries: as forward, with the scores made again.
+//
+// ds = p (dp - delta), delta the sum of p dp; where attention is sharp that is a small difference, and delta = grad_out . out of an out that was rounded to
+// bfloat16 puts an error of p times 2^-9 |grad_out . out| into it (5 times what rounding the results does, in short documents).  So delta is summed up again from
+// p dp, unrounded, as its difference `off` from that first value; and since that is known at the end only, sums of p k are kept beside those of
+// ds k: the gradient is the sum of p (dp - first - off) k.  The keys' kernel gets the better delta.  (A fourth product beside three, that shares its operand; a
+// pass of its own over the keys would be two.)
 template <int D, int FORM, bool SLOPES>
 __global__ void __launch_bounds__(AT_TPB, 2) rb_attend_grad_q_kernel(AttentionArgs a)
 {
-    __shared__ __align__(1024) char lds[2][2][AT_TILE * D * 2];
+    constexpr int ROWS = AT_BLOCK;                  // keys at a time
+    __shared__ __align__(1024) char lds[2][2][ROWS * D * 2];           // keys and values; first the workgroup's queries
+    __shared__ __align__(1024) char own[AT_ROWS / AT_TILE][AT_TILE * D * 2];       // the gradients of the workgroup's results
     __shared__ Noted noted;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x & 63, half = lane / 32;
     int tile, head;
@@ -692,77 +695,96 @@ __global__ void __launch_bounds__(AT_TPB, 2) rb_attend_grad_q_kernel(AttentionAr
     const int last = a.tokens - 1, r = min(row, last);
     const Bf16 *const keys = a.k.at(0, kv), *const values = a.v.at(0, kv);
     const float slope2 = SLOPES && a.slopes ? a.slopes[head] * AT_LOG2E : 0.0f;
-    at_bf8 q[D / 16], go[D / 16];
     const float lse2 = a.lse2[(int64_t)head * a.tokens + r], delta = a.delta[(int64_t)head * a.tokens + r];
     if (threadIdx.x < 4) noted.rows[threadIdx.x / 2][threadIdx.x % 2] = 0;
     at_clear<D>(&lds[0][0][0], sizeof(lds), a.dim);
-    const Bring<D> bring(wave, a.dim);
+    at_clear<D>(&own[0][0], sizeof(own), a.dim);
+    const Bring<D, ROWS> bring(wave, a.dim);
+    const Bring<D> bring_own(wave, a.dim);
     const Reads<D> reads;
     const int64_t k_offset = bring.offset(a.k.token), v_offset = bring.offset(a.v.token);
-    at_acc dq[D / 32]{};
+    at_bf8 q[D / 16];
+    at_acc dq[D / 32]{}, pk[D / 32]{};
+    float off = 0.0f;
 
     auto step = [&](bool masked, int first, const char* kt, const char* vt) {
         const int from = mine.lo - first, to = mine.hi - first;
         const float away = (float)(row - first - 4 * half);
+        at_acc s{}, dp{};
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
-            at_acc s{}, dp{};
-#pragma unroll
-            for (int n = 0; n < D / 16; ++n) {
-                s = at_mma(reads.rows(kt, b, n), q[n], s);
-                dp = at_mma(reads.rows(vt, b, n), go[n], dp);
-            }
+        for (int n = 0; n < D / 16; ++n) {
+            s = at_mma(reads.rows(kt, 0, n), q[n], s);
+            dp = at_mma(reads.rows(vt, 0, n), reads.rows(own[wave / 2], wave % 2, n), dp);
+        }
+        at_acc w;                                   // p, times the cap's slope
+        auto elements = [&](auto masked_) {
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
-                const int key = 32 * b + 8 * (e / 4) + e % 4;
-                float p, ds;
-                at_slope<FORM, SLOPES>(a.score, s[e], dp[e], SLOPES ? fmaf(slope2, fabsf(away - (float)key), lse2) : lse2, delta, p, ds);
-                s[e] = ds;
-            }
-            if (masked) {
-            asm volatile("");       // (a branch: few tiles need it)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const int key = 32 * b + 8 * (e / 4) + 4 * half + e % 4;
-                    s[e] = key >= from && key < to ? s[e] : 0.0f;
+                const int key = 8 * (e / 4) + e % 4;
+                float p, slope;
+                at_weight<FORM>(a.score, s[e], SLOPES ? fmaf(slope2, fabsf(away - (float)key), lse2) : lse2, p, slope);
+                float ds = p * (dp[e] - delta);
+                if (masked_()) {
+                    const bool seen = key + 4 * half >= from && key + 4 * half < to;
+                    p = seen ? p : 0.0f;
+                    ds = seen ? ds : 0.0f;
                 }
+                off += ds;
+                s[e] = FORM == AT_PLAIN ? ds : ds * slope;
+                w[e] = FORM == AT_PLAIN ? p : p * slope;
             }
-            const at_bf8 f[2] = {at_pack(s, 0), at_pack(s, 1)};
-            at_add<D, 2, false>(dq, f, reads, kt, 2 * b);
-        }
+        };
+        if (masked) elements(std::true_type());
+        else elements(std::false_type());
+        const at_bf8 f[2] = {at_pack(s, 0), at_pack(s, 1)}, g[2] = {at_pack(w, 0), at_pack(w, 1)};
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+#pragma unroll
+            for (int n = 0; n < D / 32; ++n) {
+                const at_bf8 column = reads.columns(kt, n, c);
+                dq[n] = at_mma(column, f[c], dq[n]);
+                pk[n] = at_mma(column, g[c], pk[n]);
+            }
     };
 
     bool lost = false;                              // the row sees a key that is not finite
-    const int count = all.lo < all.hi ? (all.hi - all.lo + AT_TILE - 1) / AT_TILE : 0;
+    const int count = all.lo < all.hi ? (all.hi - all.lo + ROWS - 1) / ROWS : 0;
     if (count > 0) {
-        at_bring_own<D>(bring, a.q.at(0, head), a.q.token, tile, last, lds[0]);
-        at_bring_own<D>(bring, a.grad_out.at(0, head), a.grad_out.token, tile, last, lds[1]);
+        static_assert(sizeof(lds) == sizeof(own), "queries fit where the keys will be");
+        char(&queries)[2][AT_TILE * D * 2] = reinterpret_cast<char(&)[2][AT_TILE * D * 2]>(lds);
+        at_bring_own<D>(bring_own, a.grad_out.at(0, head), a.grad_out.token, tile, last, own);
+        at_bring_own<D>(bring_own, a.q.at(0, head), a.q.token, tile, last, queries);
         at_arrived();
-        at_own<D>(reads, lds[0], wave, q);
-        at_own<D>(reads, lds[1], wave, go);
+        at_own<D>(reads, queries, wave, q);
         at_wait_for_all();
         bring(keys, a.k.token, k_offset, all.lo, last, lds[0][0]);
         bring(values, a.v.token, v_offset, all.lo, last, lds[0][1]);
     }
     for (int i = 0; i < count; ++i) {
-        const int first = all.lo + i * AT_TILE, now = i & 1;
+        const int first = all.lo + i * ROWS, now = i & 1;
         at_arrived();
         if (threadIdx.x < 2) noted.rows[now ^ 1][threadIdx.x] = 0;
         if (i + 1 < count) {
-            bring(keys, a.k.token, k_offset, first + AT_TILE, last, lds[now ^ 1][0]);
-            bring(values, a.v.token, v_offset, first + AT_TILE, last, lds[now ^ 1][1]);
+            bring(keys, a.k.token, k_offset, first + ROWS, last, lds[now ^ 1][0]);
+            bring(values, a.v.token, v_offset, first + ROWS, last, lds[now ^ 1][1]);
         }
-        if (!all.whole(first)) {
-            at_make_finite<D>(lds[now][0], wave, noted.rows[now]);
+        if (!all.whole(first, ROWS)) {
+            at_make_finite<D, ROWS>(lds[now][0], wave, noted.rows[now]);
             at_wait_for_all();
             lost |= at_noted(noted.rows[now], mine.lo - first, mine.hi - first) != 0;
         }
-        if (reach.meets(first)) step(!reach.whole(first), first, lds[now][0], lds[now][1]);
+        if (reach.meets(first, ROWS)) step(!reach.whole(first, ROWS), first, lds[now][0], lds[now][1]);
     }
+    off += sc_xor<32>(off);
+    const bool empty = mine.lo >= mine.hi;
+    if (half == 0 && row < a.tokens && !empty) a.delta[(int64_t)head * a.tokens + row] = delta + off;
+#pragma unroll
+    for (int n = 0; n < D / 32; ++n)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) dq[n][e] = fmaf(-off, pk[n][e], dq[n][e]);
     const int start = tile * AT_ROWS + wave * AT_BLOCK;
     at_wait_for_all();
-    at_store<D>(&lds[0][0][0] + wave * AT_BLOCK * D * 2, a.grad_q.at(start, head), a.grad_q.token, a.tokens - start, a.dim, dq, lost ? sc_nan() : a.score.scale,
-                mine.lo >= mine.hi);
+    at_store<D>(&lds[0][0][0] + wave * AT_BLOCK * D * 2, a.grad_q.at(start, head), a.grad_q.token, a.tokens - start, a.dim, dq, lost ? sc_nan() : a.score.scale, empty);
 }
 
 // Of keys and values: a workgroup has 128 of one head, and goes through the queries of all the heads that read it.
@@ -820,10 +842,11 @@ __global__ void __launch_bounds__(AT_TPB, 2) rb_attend_grad_kv_kernel(AttentionA
                     const int e = 4 * g + i, query = 8 * g + i;
                     const float less = i == 0 ? lse2.x : i == 1 ? lse2.y : i == 2 ? lse2.z : lse2.w;
                     const float delta_i = i == 0 ? delta.x : i == 1 ? delta.y : i == 2 ? delta.z : delta.w;
-                    float p, ds;
-                    at_slope<FORM, SLOPES>(a.score, s[e], dp[e], SLOPES ? fmaf(slope2, fabsf(away - (float)query), less) : less, delta_i, p, ds);
+                    float p, slope;
+                    at_weight<FORM>(a.score, s[e], SLOPES ? fmaf(slope2, fabsf(away - (float)query), less) : less, p, slope);
+                    const float ds = p * (dp[e] - delta_i);
                     s[e] = p;
-                    dp[e] = ds;
+                    dp[e] = FORM == AT_PLAIN ? ds : ds * slope;
                 }
             }
             if (masked) {

@@ -156,7 +156,8 @@ def attend(q, k, v, scale, cap, slopes, mask):
 
 
 def attend_grad(q, k, v, out, lse, grad_out, scale, cap, slopes, mask):
-    """Gradients of q, k, v by the formula from given out and lse, and their bounds."""
+    """Gradients of q, k, v by the formula from given lse, and their bounds.  Out is where the sum of p dp begins: what that is off by (`away`) takes part in what is
+    rounded on the way."""
     u, heads, tokens, dim = F32_HALF, q.shape[1], q.shape[0], q.shape[2]
     kv = k.shape[1]
     k, v = spread(k, heads), spread(v, heads)
@@ -167,20 +168,30 @@ def attend_grad(q, k, v, out, lse, grad_out, scale, cap, slopes, mask):
     p = torch.where(mask, (s - lse[:, :, None]).exp(), 0.0)
     off_p = p * (2 * off_s + 4 * u * (lse.abs()[:, :, None] + 1))
     dp, dp_size = torch.einsum("ihd,jhd->hij", grad_out, v), torch.einsum("ihd,jhd->hij", grad_out.abs(), v.abs())
-    delta, delta_size = (grad_out * out).sum(2).t()[:, :, None], (grad_out * out).abs().sum(2).t()[:, :, None]
+    first, first_size = (grad_out * out).sum(2).t()[:, :, None], (grad_out * out).abs().sum(2).t()[:, :, None]
+    # sum of p (dp - first) over what is seen, p as it was computed: the weights add up to 1 only within the bound of lse, which makes of `first` no more than that
+    away = (p * (dp - first)).sum(2, keepdim=True)
+    delta = first + away
+    off_dp = (dim + 4) * u * (dp_size + first_size)
+    off_delta = (off_p * (dp - first).abs() + p * off_dp + (tokens + 8) * u * p * (dp - first).abs()).sum(2, keepdim=True) + 4 * u * delta.abs()
     ds = p * (dp - delta) * slope
     # the cap's slope 1 - t^2 is off by some 2^-22 where it is of size 1, and by that much of 1 where it is small
-    off_ds = off_p * (dp - delta).abs() * slope + p * slope * ((dim + 4) * u * (dp_size + delta_size)) + (16 * u * p * (dp - delta).abs() if cap else 0.0) + 4 * u * ds.abs()
+    off_slope = 16 * u if cap else 0.0
+    off_ds = off_p * (dp - delta).abs() * slope + p * slope * (off_dp + off_delta) + off_slope * p * (dp - delta).abs() + 4 * u * ds.abs()
+    aside = p * away.abs() * slope                     # what is added to ds before it is rounded, and taken away again
+    off_aside = (off_p * slope + off_slope * p) * away.abs() + 4 * u * aside
     def rounded(x, off):           # x was rounded to bfloat16
         return off * (1 + BF16_HALF) + x.abs() * BF16_HALF
-    off_p, off_ds = rounded(p, off_p), rounded(ds, off_ds)
+    off_w = rounded(p, off_p)
+    off_of_q = rounded(ds.abs() + aside, off_ds + off_aside) + rounded(aside, off_aside)
+    off_of_k = rounded(ds, off_ds)
     many = (tokens * heads + 16) * u
     def joined(x):
         return x.unflatten(1, (kv, heads // kv)).sum(2)
     dq = torch.einsum("hij,jhd->ihd", ds, k) * scale
     dk = joined(torch.einsum("hij,ihd->jhd", ds, q)) * scale
     dv = joined(torch.einsum("hij,ihd->jhd", p, grad_out))
-    b_q = torch.einsum("hij,jhd->ihd", off_ds + many * ds.abs(), k.abs()) * scale
-    b_k = joined(torch.einsum("hij,ihd->jhd", off_ds + many * ds.abs(), q.abs())) * scale
-    b_v = joined(torch.einsum("hij,ihd->jhd", off_p + many * p, grad_out.abs()))
+    b_q = torch.einsum("hij,jhd->ihd", off_of_q + many * (ds.abs() + 2 * aside), k.abs()) * scale
+    b_k = joined(torch.einsum("hij,ihd->jhd", off_of_k + many * ds.abs(), q.abs())) * scale
+    b_v = joined(torch.einsum("hij,ihd->jhd", off_w + many * p, grad_out.abs()))
     return (dq, dk, dv), tuple(b * (1 + BF16_HALF) + x.abs() * BF16_HALF * (1 + BF16_HALF) + 2.0 ** -130 for x, b in ((dq, b_q), (dk, b_k), (dv, b_v)))

@@ -194,9 +194,9 @@ def test_gradient_against_differences(cap, slopes, prefixes):
     d64, low64, scale = ref.to64(d), ref.to64(low), dim ** -0.5
     exact, lse, _, _ = ref.attend(*at, scale, cap, low64, mask)
     _, off = ref.attend_grad(*at, exact, lse, d64, scale, cap, low64, mask)
-    # the sum of grad_out * out is of out as it was rounded (and computed): off by its half steps and the weights' (4 of them for both), times p, over what ds goes to
+    # (the bound is of an out that is exact: the call's is off by the weights' and its own half steps, which go on as `aside` does)
     some = torch.einsum("ihd->hi", (d64 * exact).abs() + d64.abs() * 0.5 * exact.abs().max()) * 4 * ref.BF16_HALF
-    reach = 4 * scale * some.max() * max(float(x.abs().max()) for x in at)
+    reach = 4 * ref.BF16_HALF * scale * some.max() * max(float(x.abs().max()) for x in at)
     g = np.random.RandomState(0)
     for n, (x, leaf, o) in enumerate(zip(at, leaves, off)):
         for _ in range(60):
