@@ -5,11 +5,12 @@ what they are given and raise RbError on a non-zero status.  There is no fallbac
 """
 import ctypes as C
 import os
+import struct
 from typing import NamedTuple, Optional
 
 import torch
 
-from .binding import HERE, _check, _ptr, _stream
+from .binding import Call, HERE, _check, _ptr, _stream
 from .train import _CODES, _OnStream, _current_stream, _fits, _written
 
 BLOCK_LIB_PATH = os.environ.get("RB_BLOCK_LIBRARY") or os.path.join(HERE, "librb_block.so")   # RB_BLOCK_LIBRARY: another build of the same library
@@ -50,7 +51,7 @@ def _load():
             "(there is no fallback path)")
     L = C.CDLL(BLOCK_LIB_PATH)
     vp, i64, i32, sz, f32 = C.c_void_p, C.c_int64, C.c_int32, C.c_size_t, C.c_float
-    rows, heads, drop, docs = C.POINTER(RbRows), C.POINTER(RbHeads), C.POINTER(RbDrop), C.POINTER(RbDocuments)
+    rows = heads = drop = docs = vp            # (addresses of structures)
     L.rb_dropout.argtypes = [vp, i64, i64, i64, i32, drop, vp, i64, vp]
     L.rb_norm_create.argtypes = [C.POINTER(vp), i64, i32, i32, f32]
     L.rb_norm_query.argtypes = [vp, C.POINTER(sz)]
@@ -72,10 +73,20 @@ def _load():
 _L = _load()
 
 
-# Structures are passed as such (RbRows, RbHeads, RbDrop, RbDocuments), or None.
+def _at(structure):
+    """The address of RbRows, RbHeads, RbDrop or RbDocuments, which an address itself may stand for (None: null)."""
+    return C.addressof(structure) if isinstance(structure, C.Structure) else structure
+
+
+def _native(general, layout):
+    """As in binding.py: the same function with its usual arguments - here structures by their addresses - marshalled natively."""
+    if Call is None:
+        return general
+    return Call(C.cast(getattr(_L, general.__name__), C.c_void_p).value, layout, general)
+
 
 def rb_dropout(x, x_stride, rows, width, dtype, drop, out, out_stride, hip_stream=None):
-    return _L.rb_dropout(_ptr(x), int(x_stride), int(rows), int(width), int(dtype), drop, _ptr(out), int(out_stride), _stream(hip_stream))
+    return _L.rb_dropout(_ptr(x), int(x_stride), int(rows), int(width), int(dtype), _at(drop), _ptr(out), int(out_stride), _stream(hip_stream))
 
 
 def rb_norm_create(width, dtype, weight_dtype, eps):
@@ -95,12 +106,12 @@ def rb_norm_bind(n, workspace):
 
 
 def rb_norm_forward(n, x, residual, drop, rows, weight, bias, total, y, mean, rstd, hip_stream=None):
-    return _L.rb_norm_forward(n, x, residual, drop, int(rows), _ptr(weight), _ptr(bias), total, y, _ptr(mean), _ptr(rstd), _stream(hip_stream))
+    return _L.rb_norm_forward(n, _at(x), _at(residual), _at(drop), int(rows), _ptr(weight), _ptr(bias), _at(total), _at(y), _ptr(mean), _ptr(rstd), _stream(hip_stream))
 
 
 def rb_norm_grad(n, grad_y, total, grad_total, mean, rstd, drop, rows, weight, grad_sum, grad_x, grad_weight, grad_bias, hip_stream=None):
-    return _L.rb_norm_grad(n, grad_y, total, grad_total, _ptr(mean), _ptr(rstd), drop, int(rows), _ptr(weight), grad_sum, grad_x, _ptr(grad_weight),
-                           _ptr(grad_bias), _stream(hip_stream))
+    return _L.rb_norm_grad(n, _at(grad_y), _at(total), _at(grad_total), _ptr(mean), _ptr(rstd), _at(drop), int(rows), _ptr(weight), _at(grad_sum), _at(grad_x),
+                           _ptr(grad_weight), _ptr(grad_bias), _stream(hip_stream))
 
 
 def rb_norm_destroy(n):
@@ -124,15 +135,36 @@ def rb_attention_bind(a, workspace):
 
 
 def rb_attention_forward(a, q, k, v, tokens, documents, slopes, out, lse, hip_stream=None):
-    return _L.rb_attention_forward(a, q, k, v, int(tokens), documents, _ptr(slopes), out, _ptr(lse), _stream(hip_stream))
+    return _L.rb_attention_forward(a, _at(q), _at(k), _at(v), int(tokens), _at(documents), _ptr(slopes), _at(out), _ptr(lse), _stream(hip_stream))
 
 
 def rb_attention_grad(a, q, k, v, tokens, documents, slopes, out, lse, grad_out, grad_q, grad_k, grad_v, hip_stream=None):
-    return _L.rb_attention_grad(a, q, k, v, int(tokens), documents, _ptr(slopes), out, _ptr(lse), grad_out, grad_q, grad_k, grad_v, _stream(hip_stream))
+    return _L.rb_attention_grad(a, _at(q), _at(k), _at(v), int(tokens), _at(documents), _ptr(slopes), _at(out), _ptr(lse), _at(grad_out), _at(grad_q), _at(grad_k),
+                                _at(grad_v), _stream(hip_stream))
 
 
 def rb_attention_destroy(a):
     return _L.rb_attention_destroy(a)
+
+
+rb_dropout = _native(rb_dropout, "piiiihpis")
+rb_norm_forward = _native(rb_norm_forward, "hhhhipphhpps")
+rb_norm_grad = _native(rb_norm_grad, "hhhhpphiphhpps")
+rb_attention_forward = _native(rb_attention_forward, "hhhhihphps")
+rb_attention_grad = _native(rb_attention_grad, "hhhhihphphhhhs")
+
+
+class _Structures:
+    """Memory for the structures of a handle's calls, which are read before a call returns."""
+
+    def __init__(self, layout):
+        self._pack = struct.Struct(layout)
+        self._memory = C.create_string_buffer(self._pack.size)
+        self.address = C.addressof(self._memory)
+
+    def fill(self, *values):
+        self._pack.pack_into(self._memory, 0, *values)
+        return self.address
 
 
 # ---- dropout -------------------------------------------------------------------
@@ -156,19 +188,20 @@ def _rows_of(t, width, dtype, index, what):
 
 
 def _drop_rows(x, drop, out):
-    rows, stride = _rows_of(x, x.shape[-1], x.dtype, x.get_device(), "x")
-    assert x.is_cuda and x.dtype in _CODES, "x"
-    out_rows, out_stride = _rows_of(out, x.shape[1], x.dtype, x.get_device(), "out")
+    index, dtype = x.get_device(), x.dtype
+    assert index >= 0 and dtype in _CODES, "x"
+    rows, stride = _rows_of(x, x.shape[-1], dtype, index, "x")
+    width = x.shape[1]
+    out_rows, out_stride = (rows, stride) if out is x else _rows_of(out, width, dtype, index, "out")
     assert out_rows == rows, "out"
     if rows == 0:
         return out
-    index = x.get_device()
-    args = (x, stride, rows, x.shape[1], _CODES[x.dtype], drop.structure(), out, out_stride)
+    structure = drop.structure()
     if torch.cuda.current_device() == index:
-        rc = rb_dropout(*args, _current_stream(index))
+        rc = rb_dropout(x, stride, rows, width, _CODES[dtype], C.addressof(structure), out, out_stride, _current_stream(index))
     else:
         with torch.cuda.device(index):
-            rc = rb_dropout(*args, _current_stream(index))
+            rc = rb_dropout(x, stride, rows, width, _CODES[dtype], C.addressof(structure), out, out_stride, _current_stream(index))
     _check(rc, "rb_dropout")
     return out
 
@@ -216,6 +249,18 @@ class NormGrads(NamedTuple):
     bias: Optional[torch.Tensor]
 
 
+class _NormOutputs(Normed):
+    """Normed's tensors that LayerNorm.outputs has made: `norm` and `rows` say for what (of one that was changed since: for none)."""
+    norm = rows = None
+
+
+class _NormGradients(NormGrads):
+    norm = rows = None
+
+
+_M64 = 2 ** 64 - 1
+
+
 class LayerNorm(_OnStream):
     """Layer norm of rows, alone or of residual + dropout(x), and its gradients.  One handle serves all layers of a width (it holds no weights).
 
@@ -234,27 +279,30 @@ class LayerNorm(_OnStream):
         _check(rc, "rb_norm_query")
         self.workspace = torch.empty(size, dtype=torch.uint8, device=self.device)
         _check(rb_norm_bind(self.handle, self.workspace), "rb_norm_bind")
+        self._structures = _Structures("=QqQqQqQqQqdQQ")       # five rb_rows, one rb_drop
 
     def _new(self, *shape, dtype=None):
         return torch.empty(shape, dtype=dtype or self.dtype, device=self.device)
 
     def outputs(self, rows, total=False):
-        """Tensors for forward(..., out=...)."""
+        """Tensors for forward(..., out=...), which looks at these no further."""
         f32 = torch.float32
-        return Normed(self._new(rows, self.width), self._new(rows, self.width) if total else None, self._new(rows, dtype=f32), self._new(rows, dtype=f32))
+        out = _NormOutputs(self._new(rows, self.width), self._new(rows, self.width) if total else None, self._new(rows, dtype=f32), self._new(rows, dtype=f32))
+        out.norm, out.rows = self, rows
+        return out
 
     def gradients(self, rows, bias=True, drop=False):
-        """Tensors for grad(..., out=...)."""
-        return NormGrads(self._new(rows, self.width), self._new(rows, self.width) if drop else None, self._new(self.width, dtype=self.weight_dtype),
-                         self._new(self.width, dtype=self.weight_dtype) if bias else None)
+        """Tensors for grad(..., out=...), which looks at these no further."""
+        out = _NormGradients(self._new(rows, self.width), self._new(rows, self.width) if drop else None, self._new(self.width, dtype=self.weight_dtype),
+                             self._new(self.width, dtype=self.weight_dtype) if bias else None)
+        out.norm, out.rows = self, rows
+        return out
 
     def _rows(self, t, rows, what):
-        """The structure of a tensor of rows (None of none)."""
-        if t is None:
-            return None
+        """Elements between the rows of a tensor that is looked at first."""
         n, stride = _rows_of(t, self.width, self.dtype, self._index, what)
         assert n == rows, what
-        return RbRows(t.data_ptr(), stride)
+        return stride
 
     def _weights(self, t, what):
         assert t is None or _fits(t, self.weight_dtype, self._index, (self.width,)), what
@@ -262,18 +310,30 @@ class LayerNorm(_OnStream):
 
     def forward(self, x, weight, bias=None, residual=None, drop=None, out=None):
         """Normed of x, or of residual + dropout(x); into `out` if given (see outputs; its y or total may be x, its total the residual)."""
-        rows = x.shape[0]
+        rows, width = x.shape[0], self.width
         theirs, sums = out is not None, residual is not None or drop is not None
         if out is None:
             out = self.outputs(rows, total=sums)
-        assert (out.total is not None) == sums, "out.total"
-        for t, name in ((out.mean, "out.mean"), (out.rstd, "out.rstd")):
-            assert t is None or _fits(t, torch.float32, self._index, (rows,)), name
-        args = (self._rows(x, rows, "x"), self._rows(residual, rows, "residual"), None if drop is None else drop.structure(), rows, self._weights(weight, "weight"),
-                self._weights(bias, "bias"), self._rows(out.total, rows, "out.total"), self._rows(out.y, rows, "out.y"), out.mean, out.rstd)
+        assert (out[1] is not None) == sums, "out.total"
+        y, total, mean, rstd = out
+        if type(out) is _NormOutputs and out.norm is self and out.rows == rows:
+            y_stride = total_stride = width
+        else:
+            y_stride = self._rows(y, rows, "out.y")
+            total_stride = self._rows(total, rows, "out.total") if sums else 0
+            for t, name in ((mean, "out.mean"), (rstd, "out.rstd")):
+                assert t is None or _fits(t, torch.float32, self._index, (rows,)), name
+        x_stride = self._rows(x, rows, "x")
+        self._weights(weight, "weight")
+        self._weights(bias, "bias")
+        residual_stride = 0 if residual is None else self._rows(residual, rows, "residual")
         if rows == 0:
             return out
-        _check(self._on_stream(rb_norm_forward, self.handle, *args), "rb_norm_forward")
+        p, seed, step = (0.0, 0, 0) if drop is None else drop
+        at = self._structures.fill(x.data_ptr(), x_stride, 0 if residual is None else residual.data_ptr(), residual_stride, total.data_ptr() if sums else 0, total_stride,
+                                   y.data_ptr(), y_stride, 0, 0, p, seed & _M64, step & _M64)
+        _check(self._on_stream(rb_norm_forward, self.handle, at, None if residual is None else at + 16, None if drop is None else at + 80, rows, weight, bias,
+                               at + 32 if sums else None, at + 48, mean, rstd), "rb_norm_forward")
         if theirs:
             _written([t for t in out if t is not None])
         return out
@@ -281,22 +341,33 @@ class LayerNorm(_OnStream):
     def grad(self, grad_y, total, weight, mean, rstd, grad_total=None, drop=None, bias=True, out=None):
         """NormGrads from the derivatives with respect to y and (or None) total; total: forward's, or x where that was None.  bias: whether that gradient is
         wanted; into `out` if given (see gradients; its total or x may be grad_y or grad_total, its weight or bias None)."""
-        rows = total.shape[0]
+        rows, width = total.shape[0], self.width
         theirs = out is not None
         if out is None:
             out = self.gradients(rows, bias=bias, drop=drop is not None)
-        assert (out.x is not None) == (drop is not None), "out.x"
+        assert (out[1] is not None) == (drop is not None), "out.x"
+        g_total, g_x, g_weight, g_bias = out
+        if type(out) is _NormGradients and out.norm is self and out.rows == rows:
+            g_stride = x_stride = width
+        else:
+            g_stride = self._rows(g_total, rows, "out.total")
+            x_stride = 0 if g_x is None else self._rows(g_x, rows, "out.x")
+            self._weights(g_weight, "out.weight")
+            self._weights(g_bias, "out.bias")
+        strides = self._rows(grad_y, rows, "grad_y"), self._rows(total, rows, "total"), 0 if grad_total is None else self._rows(grad_total, rows, "grad_total")
+        self._weights(weight, "weight")
         for t, name in ((mean, "mean"), (rstd, "rstd")):
             assert _fits(t, torch.float32, self._index, (rows,)), name
         if rows == 0:
-            for t in (out.weight, out.bias):
+            for t in (g_weight, g_bias):
                 if t is not None:
                     t.zero_()
             return out
-        args = (self._rows(grad_y, rows, "grad_y"), self._rows(total, rows, "total"), self._rows(grad_total, rows, "grad_total"), mean, rstd,
-                None if drop is None else drop.structure(), rows, self._weights(weight, "weight"), self._rows(out.total, rows, "out.total"),
-                self._rows(out.x, rows, "out.x"), self._weights(out.weight, "out.weight"), self._weights(out.bias, "out.bias"))
-        _check(self._on_stream(rb_norm_grad, self.handle, *args), "rb_norm_grad")
+        p, seed, step = (0.0, 0, 0) if drop is None else drop
+        at = self._structures.fill(grad_y.data_ptr(), strides[0], total.data_ptr(), strides[1], 0 if grad_total is None else grad_total.data_ptr(), strides[2],
+                                   g_total.data_ptr(), g_stride, 0 if g_x is None else g_x.data_ptr(), x_stride, p, seed & _M64, step & _M64)
+        _check(self._on_stream(rb_norm_grad, self.handle, at, at + 16, None if grad_total is None else at + 32, mean, rstd, None if drop is None else at + 80, rows, weight,
+                               at + 48, None if g_x is None else at + 64, g_weight, g_bias), "rb_norm_grad")
         if theirs:
             _written([t for t in out if t is not None])
         return out
@@ -334,12 +405,8 @@ class _Norm(torch.autograd.Function):
             grad_y = torch.zeros(total.shape, dtype=norm.dtype, device=norm.device)
         grad_y, grad_total = (t if t is None or (t.stride(1) == 1 and t.stride(0) >= t.shape[1]) else t.contiguous() for t in (grad_y, grad_total))
         wanted = ctx.needs_input_grad
-        rows = total.shape[0]
-        new = norm.gradients(rows, bias=ctx.bias and wanted[2], drop=ctx.drop is not None)
-        if not wanted[1]:
-            new = new._replace(weight=None)
-        g = norm.grad(grad_y, total, weight, mean, rstd, grad_total, ctx.drop, out=new)
-        return g.total if ctx.drop is None else g.x, g.weight, g.bias, g.total if ctx.residual else None, None, None
+        g = norm.grad(grad_y, total, weight, mean, rstd, grad_total, ctx.drop, bias=ctx.bias and wanted[2])
+        return g.total if ctx.drop is None else g.x, g.weight if wanted[1] else None, g.bias, g.total if ctx.residual else None, None, None
 
 
 # ---- attention of packed documents -------------------------------------------------
@@ -353,8 +420,17 @@ class Documents(NamedTuple):
 
 
 class Attended(NamedTuple):
+    """What DocumentAttention.forward gives."""
     out: torch.Tensor                      # [tokens, heads, head_dim], bfloat16
     lse: torch.Tensor                      # [heads, tokens], binary32
+
+
+class _AttendedOutputs(Attended):
+    """Attended's tensors that DocumentAttention.outputs has made: `attention` and `tokens` say for what."""
+    attention = tokens = None
+
+
+_NO_HEADS = (0, 0, 0) * 4
 
 
 class DocumentAttention(_OnStream):
@@ -377,25 +453,30 @@ class DocumentAttention(_OnStream):
         _check(rc, "rb_attention_query")
         self.workspace = torch.empty(size, dtype=torch.uint8, device=self.device)
         _check(rb_attention_bind(self.handle, self.workspace), "rb_attention_bind")
+        self._structures = _Structures("=" + "Qqq" * 8 + "QQQq")       # eight rb_heads, one rb_documents
 
     def outputs(self, tokens):
-        """Tensors for forward(..., out=...)."""
-        return Attended(torch.empty((tokens, self.heads, self.head_dim), dtype=torch.bfloat16, device=self.device),
-                        torch.empty((self.heads, tokens), dtype=torch.float32, device=self.device))
+        """Tensors for forward(..., out=...), which looks at these no further."""
+        out = _AttendedOutputs(torch.empty((tokens, self.heads, self.head_dim), dtype=torch.bfloat16, device=self.device),
+                               torch.empty((self.heads, tokens), dtype=torch.float32, device=self.device))
+        out.attention, out.tokens = self, tokens
+        return out
 
     def _heads(self, t, tokens, heads, what):
-        assert t.shape == (tokens, heads, self.head_dim) and t.dtype == torch.bfloat16 and t.get_device() == self._index, what
+        """The structure's numbers of a tensor that is looked at first."""
+        assert t.shape == (tokens, heads, self.head_dim) and t.dtype is torch.bfloat16 and t.get_device() == self._index, what
         a, b, step = t.stride()
         assert step == 1, what
         # (strides that are never used may be anything)
-        return RbHeads(t.data_ptr(), a if tokens > 1 else max(heads, 1) * self.head_dim, b if heads > 1 else self.head_dim)
+        return t.data_ptr(), a if tokens > 1 else heads * self.head_dim, b if heads > 1 else self.head_dim
 
     def _documents(self, d):
-        count, index = d.offsets.shape[0] - 1, self._index
-        assert count >= 0 and _fits(d.offsets, torch.int64, index, (count + 1,)), "documents.offsets"
-        assert d.lengths is None or _fits(d.lengths, torch.int64, index, (count,)), "documents.lengths"
-        assert d.prefixes is None or _fits(d.prefixes, torch.int64, index, (count,)), "documents.prefixes"
-        return RbDocuments(d.offsets.data_ptr(), None if d.lengths is None else d.lengths.data_ptr(), None if d.prefixes is None else d.prefixes.data_ptr(), count)
+        offsets, lengths, prefixes = d
+        count, index, i64 = offsets.shape[0] - 1, self._index, torch.int64
+        assert count >= 0 and _fits(offsets, i64, index, (count + 1,)), "documents.offsets"
+        assert lengths is None or _fits(lengths, i64, index, (count,)), "documents.lengths"
+        assert prefixes is None or _fits(prefixes, i64, index, (count,)), "documents.prefixes"
+        return offsets.data_ptr(), 0 if lengths is None else lengths.data_ptr(), 0 if prefixes is None else prefixes.data_ptr(), count
 
     def _slopes(self, slopes):
         assert slopes is None or _fits(slopes, torch.float32, self._index, (self.heads,)), "slopes"
@@ -403,34 +484,42 @@ class DocumentAttention(_OnStream):
 
     def forward(self, q, k, v, documents, slopes=None, out=None):
         """Attended; into `out` if given (see outputs; its lse may be None)."""
-        tokens = q.shape[0]
+        tokens, heads, kv = q.shape[0], self.heads, self.kv_heads
         theirs = out is not None
         if out is None:
             out = self.outputs(tokens)
-        assert out.lse is None or _fits(out.lse, torch.float32, self._index, (self.heads, tokens)), "out.lse"
-        args = (self._heads(q, tokens, self.heads, "q"), self._heads(k, tokens, self.kv_heads, "k"), self._heads(v, tokens, self.kv_heads, "v"), tokens,
-                self._documents(documents), self._slopes(slopes), self._heads(out.out, tokens, self.heads, "out.out"), out.lse)
+        result, lse = out
+        if type(out) is _AttendedOutputs and out.attention is self and out.tokens == tokens:
+            to = result.data_ptr(), heads * self.head_dim, self.head_dim
+        else:
+            assert lse is None or _fits(lse, torch.float32, self._index, (heads, tokens)), "out.lse"
+            to = self._heads(result, tokens, heads, "out.out")
+        at = self._structures.fill(*self._heads(q, tokens, heads, "q"), *self._heads(k, tokens, kv, "k"), *self._heads(v, tokens, kv, "v"), *to, *_NO_HEADS,
+                                   *self._documents(documents))
+        self._slopes(slopes)
         if tokens == 0:
             return out
-        _check(self._on_stream(rb_attention_forward, self.handle, *args), "rb_attention_forward")
+        _check(self._on_stream(rb_attention_forward, self.handle, at, at + 24, at + 48, tokens, at + 192, slopes, at + 72, lse), "rb_attention_forward")
         if theirs:
             _written([t for t in out if t is not None])
         return out
 
     def grad(self, q, k, v, documents, out_, lse, grad_out, slopes=None, out=None):
         """The gradients of q, k and v from the derivatives with respect to out; out_, lse: forward's.  Into the three tensors `out` if given."""
-        tokens = q.shape[0]
+        tokens, heads, kv = q.shape[0], self.heads, self.kv_heads
         theirs = out is not None
         if out is None:
-            out = tuple(torch.empty((tokens, n, self.head_dim), dtype=torch.bfloat16, device=self.device) for n in (self.heads, self.kv_heads, self.kv_heads))
-        assert _fits(lse, torch.float32, self._index, (self.heads, tokens)), "lse"
-        args = (self._heads(q, tokens, self.heads, "q"), self._heads(k, tokens, self.kv_heads, "k"), self._heads(v, tokens, self.kv_heads, "v"), tokens,
-                self._documents(documents), self._slopes(slopes), self._heads(out_, tokens, self.heads, "out_"), lse,
-                self._heads(grad_out, tokens, self.heads, "grad_out"), self._heads(out[0], tokens, self.heads, "out[0]"),
-                self._heads(out[1], tokens, self.kv_heads, "out[1]"), self._heads(out[2], tokens, self.kv_heads, "out[2]"))
+            out = tuple(torch.empty((tokens, n, self.head_dim), dtype=torch.bfloat16, device=self.device) for n in (heads, kv, kv))
+        assert _fits(lse, torch.float32, self._index, (heads, tokens)), "lse"
+        at = self._structures.fill(*self._heads(q, tokens, heads, "q"), *self._heads(k, tokens, kv, "k"), *self._heads(v, tokens, kv, "v"),
+                                   *self._heads(out_, tokens, heads, "out_"), *self._heads(grad_out, tokens, heads, "grad_out"),
+                                   *self._heads(out[0], tokens, heads, "out[0]"), *self._heads(out[1], tokens, kv, "out[1]"), *self._heads(out[2], tokens, kv, "out[2]"),
+                                   *self._documents(documents))
+        self._slopes(slopes)
         if tokens == 0:
             return out
-        _check(self._on_stream(rb_attention_grad, self.handle, *args), "rb_attention_grad")
+        _check(self._on_stream(rb_attention_grad, self.handle, at, at + 24, at + 48, tokens, at + 192, slopes, at + 72, lse, at + 96, at + 120, at + 144, at + 168),
+               "rb_attention_grad")
         if theirs:
             _written(list(out))
         return out

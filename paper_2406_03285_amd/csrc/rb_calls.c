@@ -2,7 +2,8 @@
  * Native marshalling of the calls a training loop makes: rb_update, rb_sample_augment, rb_update_sample, rb_announce_next,
  * rb_update_sample_many, rb_announce_next_many, rb_pipeline_step_many and rb_pipeline_drain (rb_pipeline_step goes through ctypes), and of
  * the training step's rb_scorer_score, rb_scorer_grad and rb_ortho_apply (rb_ortho_step, which takes floats as well as integers and pointers, goes
- * through ctypes: 7 us of the host, 2 more than rb_ortho_apply, where the smallest takes the device 14).
+ * through ctypes: 7 us of the host, 2 more than rb_ortho_apply, where the smallest takes the device 14), and of what its blocks compute: rb_dropout,
+ * rb_norm_forward, rb_norm_grad, rb_attention_forward and rb_attention_grad (whose structures go by their addresses).
  * One `Call` object per function: called with integers, None and tensors in the declared positions it goes straight to the library;
  * anything else (keywords, other number types, wrong argument counts) goes to the Python function it was made with, which says what is
  * accepted and what is not.  A call through ctypes converts every argument through objects of its own: 16 + 16 rows of 12 KB in one call
@@ -19,7 +20,7 @@
 #include <stdint.h>
 #include <string.h>
 
-#define MAX_ARGS 12
+#define MAX_ARGS 14
 #define MAX_STEPS 64            /* longer sequences go to the Python function */
 #define MAX_SEQUENCES 4
 
@@ -120,12 +121,17 @@ static PyObject* call(PyObject* self, PyObject* const* args, size_t nargsf, PyOb
     case 6: status = ((int (*)(uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t))c->address)(a[0], a[1], a[2], a[3], a[4], a[5]); break;
     case 7: status = ((int (*)(uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t))c->address)(a[0], a[1], a[2], a[3], a[4], a[5], a[6]); break;
     case 8: status = ((int (*)(uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t))c->address)(a[0], a[1], a[2], a[3], a[4], a[5], a[6], a[7]); break;
+    case 9: status = ((int (*)(uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t))c->address)(a[0], a[1], a[2], a[3], a[4], a[5], a[6], a[7], a[8]); break;
     case 10: status = ((int (*)(uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t))c->address)(a[0], a[1], a[2], a[3], a[4], a[5], a[6], a[7], a[8], a[9]); break;
     case 11: status = ((int (*)(uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t))c->address)(a[0], a[1], a[2], a[3], a[4], a[5], a[6], a[7], a[8], a[9], a[10]); break;
     case 12: status = ((int (*)(uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t))c->address)(a[0], a[1], a[2], a[3], a[4], a[5], a[6], a[7], a[8], a[9], a[10], a[11]); break;
-    default:
+    case 13:
         status = ((int (*)(uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t))c->address)(
             a[0], a[1], a[2], a[3], a[4], a[5], a[6], a[7], a[8], a[9], a[10], a[11], a[12]);
+        break;
+    default:
+        status = ((int (*)(uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t))c->address)(
+            a[0], a[1], a[2], a[3], a[4], a[5], a[6], a[7], a[8], a[9], a[10], a[11], a[12], a[13]);
         break;
     }
     Py_END_ALLOW_THREADS
@@ -148,7 +154,7 @@ static int call_init(PyObject* self, PyObject* args, PyObject* kwargs)
     size_t sequences = 0;
     for (size_t i = 0; i < n; ++i) sequences += layout[i] == 'v';
     const char* stream = strchr(layout, 's');
-    if (address == 0 || n > MAX_ARGS || (k != 2 && k != 3 && k != 6 && k != 7 && k != 8 && k != 10 && k != 11 && k != 12 && k != 13) || strspn(layout, "hpivs") != n ||
+    if (address == 0 || n > MAX_ARGS || (k != 2 && k != 3 && !(k >= 6 && k <= 14)) || strspn(layout, "hpivs") != n ||
         sequences > MAX_SEQUENCES || (stream != NULL && stream != layout + n - 1) || !PyCallable_Check(general)) {
         PyErr_SetString(PyExc_ValueError, "Call(address, layout, general, rows=False)");
         return -1;

@@ -1,7 +1,8 @@
 // Attention of packed documents (rb_attention_forward) and its gradients (rb_attention_grad).  Included by rb_block.hip only.
 //
 // Masks.  What a position sees - its document up to itself, or the prefix, or all of the document - is one interval of positions, and so is what sees
-// it.  A first small kernel finds both for every position; the others compare with them and know no documents.  Tiles that every row of a wavefront sees whole
+// it.  A workgroup of the forward pass finds those of its rows in LDS (of many documents a small kernel finds them first), the first kernel of the gradients
+// those of all positions; what follows compares with them and knows no documents.  Tiles that every row of a wavefront sees whole
 // are not compared at all, tiles that none sees are passed over.
 //
 // Products.  Matrix instructions of 32 x 32 x 16 give a lane 16 elements of one column, in rows 8 (i / 4) + 4 (lane / 32) + i % 4.  The scores are made
@@ -29,7 +30,7 @@ constexpr int AT_BLOCK = 32;                       // rows of a wavefront
 constexpr int AT_ROWS = AT_WAVES * AT_BLOCK;       // rows of a workgroup
 constexpr int AT_TILE = 64;                        // rows that are in LDS at a time
 constexpr float AT_LOG2E = 1.44269504088896340736f;
-constexpr int AT_NEAR_OFFSETS = 2048;              // offsets of documents that are kept in LDS
+constexpr int AT_NEAR_OFFSETS = 2048;              // offsets of documents that a workgroup looks through in LDS
 constexpr float AT_LN2 = 0.69314718055994530942f;
 
 typedef __bf16 at_bf8 __attribute__((ext_vector_type(8)));
@@ -80,16 +81,10 @@ __host__ __device__ inline Spans at_spans_of(const SpanArgs& a, int32_t t)
     return s;
 }
 
-// A thread per position.  The offsets are looked through in LDS where they fit (24 documents of 8192 positions: 5.0 -> us).
+// A thread per position.
 __global__ void __launch_bounds__(AT_TPB) rb_spans_kernel(SpanArgs a)
 {
-    __shared__ int64_t near[AT_NEAR_OFFSETS];
     const int t = blockIdx.x * AT_TPB + threadIdx.x;
-    if (a.count < AT_NEAR_OFFSETS) {
-        for (int i = threadIdx.x; i <= a.count; i += AT_TPB) near[i] = a.offsets[i];
-        __syncthreads();
-        a.offsets = near;
-    }
     if (t < a.tokens) a.spans[t] = at_spans_of(a, t);
 }
 
@@ -325,7 +320,8 @@ __device__ __forceinline__ float at_score(const ScoreOf& of, float product, floa
 
 struct AttentionArgs {
     HeadRows q, k, v;
-    const Spans* spans;
+    const Spans* spans;                    // null: from the documents
+    SpanArgs documents;
     const float* slopes;
     ScoreOf score;
     int32_t tokens, dim, heads, group;     // group: heads of queries to one of keys
@@ -378,6 +374,7 @@ __device__ __forceinline__ int at_highest(int v) { return -at_lowest(-v); }
 // What rows see: all of it lies in [lo, hi), and [all_lo, all_hi) is seen by every row that sees anything.
 struct Reach {
     int lo, hi, all_lo, all_hi;
+    static __device__ __forceinline__ Reach nothing() { return Reach{INT32_MAX, 0, 0, INT32_MAX}; }
     __device__ __forceinline__ void join(Span s)
     {
         if (s.lo >= s.hi) return;
@@ -398,7 +395,7 @@ struct Reach {
 };
 __device__ __forceinline__ Reach at_reach(Span s)      // of the wavefront's rows, one a lane
 {
-    Reach r{INT32_MAX, 0, 0, INT32_MAX};
+    Reach r = Reach::nothing();
     r.join(s);
     r.share();
     return r;
@@ -409,7 +406,7 @@ template <bool SEEN>
 __device__ __forceinline__ Reach at_reach(const Spans* spans, int first, int tokens)
 {
     const int lane = threadIdx.x & 63;
-    Reach r{INT32_MAX, 0, 0, INT32_MAX};
+    Reach r = Reach::nothing();
 #pragma unroll
     for (int i = 0; i < AT_ROWS / 64; ++i) {
         const int t = first + i * 64 + lane;
@@ -478,10 +475,26 @@ __global__ void __launch_bounds__(AT_TPB, 2) rb_attend_kernel(AttentionArgs a)
     int tile, head;
     at_place<false>(blockIdx.x, a.tiles, a.heads, a.inner, tile, head);
     const int kv = head / a.group;
-    const Reach all = at_reach<false>(a.spans, tile * AT_ROWS, a.tokens);
     const int row = tile * AT_ROWS + wave * AT_BLOCK + (lane & 31);
-    const Span mine = row < a.tokens ? a.spans[row].sees : Span{0, 0};
+    Span* const spans = reinterpret_cast<Span*>(&lds[0][0][0]);            // of the workgroup's rows, before the tiles come
+    if (a.spans == nullptr) {
+        int64_t* const near = reinterpret_cast<int64_t*>(&lds[0][0][0] + AT_ROWS * sizeof(Span));
+        for (int i = threadIdx.x; i <= a.documents.count; i += AT_TPB) near[i] = a.documents.offsets[i];
+        __syncthreads();
+        a.documents.offsets = near;
+    }
+    if (threadIdx.x < AT_ROWS) {
+        const int t = tile * AT_ROWS + threadIdx.x;
+        spans[threadIdx.x] = t >= a.tokens ? Span{0, 0} : a.spans ? a.spans[t].sees : at_spans_of(a.documents, t).sees;
+    }
+    __syncthreads();
+    const Span mine = spans[wave * AT_BLOCK + (lane & 31)];
+    Reach all = Reach::nothing();
+#pragma unroll
+    for (int i = 0; i < AT_ROWS / 64; ++i) all.join(spans[i * 64 + lane]);
+    all.share();
     const Reach reach = at_reach(mine);
+    __syncthreads();
     const int last = a.tokens - 1;
     const Bf16 *const keys = a.k.at(0, kv), *const values = a.v.at(0, kv);
     const float slope2 = SLOPES && a.slopes ? a.slopes[head] * AT_LOG2E : 0.0f;
@@ -632,7 +645,7 @@ __global__ void __launch_bounds__(AT_TPB, 2) rb_attend_kernel(AttentionArgs a)
 
 // ---- gradients -----------------------------------------------------------------
 
-// What the gradients need of every row of every head: lse in base 2, and the sum of grad_out * out.  16 lanes a row.
+// What the gradients need: the positions' intervals, and of every row of every head lse in base 2 and the sum of grad_out * out.  16 lanes a row.
 __global__ void __launch_bounds__(AT_TPB) rb_attend_delta_kernel(AttentionArgs a, float* lse2)
 {
     const int64_t rows = (int64_t)a.heads * a.tokens;
@@ -653,10 +666,11 @@ __global__ void __launch_bounds__(AT_TPB) rb_attend_delta_kernel(AttentionArgs a
         sum += sc_xor<4>(sum);
         sum += sc_xor<8>(sum);
         if (first == 0) {
-            const Span s = a.spans[t].sees;
+            const Spans s = at_spans_of(a.documents, t);
+            if (h == 0) a.documents.spans[t] = s;
             const int64_t to = (int64_t)h * a.tokens + t;
             a.delta[to] = sum;
-            lse2[to] = s.lo < s.hi ? a.lse[to] * AT_LOG2E - a.lse_less : -sc_neg_inf();
+            lse2[to] = s.sees.lo < s.sees.hi ? a.lse[to] * AT_LOG2E - a.lse_less : -sc_neg_inf();
         }
     }
 }
