@@ -183,7 +183,7 @@ def _rows_of(t, width, dtype, index, what):
     """(rows, elements between them) of a tensor of rows, looked at first."""
     shape, (stride, step) = t.shape, t.stride()
     assert len(shape) == 2 and shape[1] == width and t.dtype == dtype and t.get_device() == index, what
-    assert step == 1 or width == 1, what
+    assert step == 1 or width == 1 or shape[0] == 0, what
     return shape[0], stride if shape[0] > 1 else max(stride, width)
 
 
@@ -466,7 +466,7 @@ class DocumentAttention(_OnStream):
         """The structure's numbers of a tensor that is looked at first."""
         assert t.shape == (tokens, heads, self.head_dim) and t.dtype is torch.bfloat16 and t.get_device() == self._index, what
         a, b, step = t.stride()
-        assert step == 1, what
+        assert step == 1 or tokens == 0, what
         # (strides that are never used may be anything)
         return t.data_ptr(), a if tokens > 1 else heads * self.head_dim, b if heads > 1 else self.head_dim
 
