@@ -353,6 +353,7 @@ AttentionArgs attention_args(const rb_attention* a, const rb_heads* q, const rb_
     g.group = a->heads / a->kv_heads;
     g.tiles = (int32_t)((tokens + AT_ROWS - 1) / AT_ROWS);
     g.inner = inner_heads(a->heads, g.group);
+    g.ranked = d->count > 1 && tokens >= 192 * d->count && g.tiles > 1 && g.tiles <= AT_RANKED;
     return g;
 }
 
@@ -432,7 +433,7 @@ int rb_attention_forward(rb_attention* a, const rb_heads* q, const rb_heads* k, 
     g.lse = lse;
     // one launch where a workgroup can look through the documents itself (9 documents of 160 positions: 11.3 -> 7.9 us)
     hipError_t e = hipSuccess;
-    if (documents->count < AT_NEAR_OFFSETS) g.spans = nullptr;
+    if (documents->count < AT_NEAR_OFFSETS) g.spans = nullptr;       // (with many documents tiles take turns as they lie)
     else e = launch(rb_spans_kernel, dim3((unsigned)(tokens + AT_TPB - 1) / AT_TPB), AT_TPB, 0, st, g.documents);
     if (e == hipSuccess)
         e = by_form(a, slopes != nullptr, [&](auto dim, auto form, auto lowered) {
@@ -467,8 +468,9 @@ int rb_attention_grad(rb_attention* a, const rb_heads* q, const rb_heads* k, con
     of_keys.shares = a->kv_heads * parts;
     of_keys.inner = inner_heads(of_keys.shares, parts);
     of_keys.sums = parts > 1 ? reinterpret_cast<float*>(a->ws + a->off_sums) : nullptr;
-    const int64_t rows = tokens * a->heads;
-    hipError_t e = launch(rb_attend_delta_kernel, dim3((unsigned)std::min<int64_t>((rows + AT_TPB / 16 - 1) / (AT_TPB / 16), 1 << 20)), AT_TPB, 0, st, g, lse2);
+    const int64_t blocks = (tokens + AT_POSITIONS - 1) / AT_POSITIONS;
+    const dim3 delta_grid((unsigned)blocks, (unsigned)std::min<int64_t>((a->heads + AT_ONCE - 1) / AT_ONCE, (1024 + blocks - 1) / blocks));
+    hipError_t e = launch(rb_attend_delta_kernel, delta_grid, AT_TPB, 0, st, g, lse2);
     if (e == hipSuccess)
         e = by_form(a, slopes != nullptr, [&](auto dim, auto form, auto lowered) {
             // (of queries first: it makes delta exact)

@@ -54,23 +54,32 @@ struct SpanArgs {
     int32_t tokens, causal;
 };
 
+// How many documents begin at or before position t.
+template <typename Offsets>
+__host__ __device__ inline int64_t at_begun(Offsets offsets, int64_t count, int32_t t)
+{
+    int64_t low = 0, high = count;
+    while (low < high) {
+        const int64_t mid = (low + high) / 2;
+        if (offsets[mid] <= t) low = mid + 1;
+        else high = mid;
+    }
+    return low;
+}
+
 // Of position t.  Its document is the last one that begins at or before it (those behind that one with the same begin are empty).  Positions
 // in no document get empty intervals at themselves, so that neighbouring positions' intervals still rise.  Whatever the numbers are, intervals
 // lie within the positions there are, and one that is not empty holds t.
-__host__ __device__ inline Spans at_spans_of(const SpanArgs& a, int32_t t)
+template <typename Offsets>
+__host__ __device__ inline Spans at_spans_of(const SpanArgs& a, Offsets offsets, int32_t t)
 {
     auto lower = [](int64_t x, int64_t y) { return x < y ? x : y; };
     auto higher = [](int64_t x, int64_t y) { return x < y ? y : x; };
-    int64_t low = 0, high = a.count;               // first document that begins behind t
-    while (low < high) {
-        const int64_t mid = (low + high) / 2;
-        if (a.offsets[mid] <= t) low = mid + 1;
-        else high = mid;
-    }
     Spans s{{t, t}, {t, t}};
-    if (low == 0) return s;
-    const int64_t d = low - 1, begin = higher(a.offsets[d], 0);
-    int64_t end = lower(a.offsets[d + 1], a.tokens);
+    const int64_t d = at_begun(offsets, a.count, t) - 1;
+    if (d < 0) return s;
+    const int64_t begin = higher(offsets[d], 0);
+    int64_t end = lower(offsets[d + 1], a.tokens);
     if (a.lengths) end = lower(end, begin + lower(higher(a.lengths[d], 0), a.tokens));
     if (t >= end) return s;
     const int64_t prefix = a.prefixes ? begin + lower(higher(a.prefixes[d], 0), end - begin) : begin;
@@ -85,7 +94,7 @@ __host__ __device__ inline Spans at_spans_of(const SpanArgs& a, int32_t t)
 __global__ void __launch_bounds__(AT_TPB) rb_spans_kernel(SpanArgs a)
 {
     const int t = blockIdx.x * AT_TPB + threadIdx.x;
-    if (t < a.tokens) a.spans[t] = at_spans_of(a, t);
+    if (t < a.tokens) a.spans[t] = at_spans_of(a, a.offsets, t);
 }
 
 // ---- tiles in LDS --------------------------------------------------------------
@@ -326,6 +335,7 @@ struct AttentionArgs {
     ScoreOf score;
     int32_t tokens, dim, heads, group;     // group: heads of queries to one of keys
     int32_t tiles, inner;
+    bool ranked;                           // tiles take turns by what they see, not by where they are
     int32_t shares;                        // gradients of keys: heads of keys, times the parts that their queries are cut into
     float* sums;                           // of the parts: [shares][tokens][2][D]; null: there is one
     // forward: written; gradients: read
@@ -355,65 +365,76 @@ __device__ __forceinline__ void at_place(int id, int tiles, int heads, int inner
         t = id / heads;
         head = id - t * heads;
     }
-    tile = UP ? t : tiles - 1 - t;
+    tile = UP ? t : tiles - 1 - t;             // (the turn's, where tiles are ranked)
 }
 
-// Of all lanes.
-__device__ __forceinline__ int at_lowest(int v)
-{
-    v = min(v, (int)sc_xor<1>((uint32_t)v));
-    v = min(v, (int)sc_xor<2>((uint32_t)v));
-    v = min(v, (int)sc_xor<4>((uint32_t)v));
-    v = min(v, (int)sc_xor<8>((uint32_t)v));
-    v = min(v, (int)sc_xor<16>((uint32_t)v));
-    v = min(v, (int)sc_xor<32>((uint32_t)v));
-    return __builtin_amdgcn_readfirstlane(v);
-}
-__device__ __forceinline__ int at_highest(int v) { return -at_lowest(-v); }
-
-// What rows see: all of it lies in [lo, hi), and [all_lo, all_hi) is seen by every row that sees anything.
+// What rows see: all of it lies in [lo, hi), and [all_lo, all_hi) is seen by every row that sees anything.  Intervals of rows behind one another rise, so the
+// first and the last row that see anything tell.  (Where documents cannot be, what comes of it is unspecified, and within the positions like every interval.)
 struct Reach {
     int lo, hi, all_lo, all_hi;
-    static __device__ __forceinline__ Reach nothing() { return Reach{INT32_MAX, 0, 0, INT32_MAX}; }
-    __device__ __forceinline__ void join(Span s)
-    {
-        if (s.lo >= s.hi) return;
-        lo = min(lo, s.lo);
-        hi = max(hi, s.hi);
-        all_lo = max(all_lo, s.lo);
-        all_hi = min(all_hi, s.hi);
-    }
-    __device__ __forceinline__ void share()            // of all lanes
-    {
-        lo = at_lowest(lo);
-        hi = at_highest(hi);
-        all_lo = at_highest(all_lo);
-        all_hi = at_lowest(all_hi);
-    }
+    __device__ __forceinline__ Reach(Span first, Span last, bool any) : lo(any ? first.lo : 0), hi(any ? last.hi : 0), all_lo(any ? last.lo : 0), all_hi(any ? first.hi : 0) {}
     __device__ __forceinline__ bool meets(int first, int rows = AT_TILE) const { return first < hi && first + rows > lo; }
     __device__ __forceinline__ bool whole(int first, int rows = AT_TILE) const { return first >= all_lo && first + rows <= all_hi; }
+    __device__ __forceinline__ int tiles(int rows) const { return lo < hi ? (hi - lo + rows - 1) / rows : 0; }
 };
-__device__ __forceinline__ Reach at_reach(Span s)      // of the wavefront's rows, one a lane
+__device__ __forceinline__ Span at_lane(Span s, int lane) { return Span{__builtin_amdgcn_readlane(s.lo, lane), __builtin_amdgcn_readlane(s.hi, lane)}; }
+// Of the wavefront's rows, one a lane and the same 32 in both halves.
+__device__ __forceinline__ Reach at_reach(Span s)
 {
-    Reach r = Reach::nothing();
-    r.join(s);
-    r.share();
-    return r;
+    const uint64_t some = __ballot(s.lo < s.hi);
+    const int first = some ? __builtin_ctzll(some) : 0, last = some ? 63 - __builtin_clzll(some) : 0;
+    return Reach(at_lane(s, first), at_lane(s, last), some != 0);
 }
-
-// The same of the workgroup's rows first .. first + 127 (SEEN: of what sees them).
+// Of the workgroup's rows: those of its lanes, `low`, and the 64 behind them, `high`.
+static_assert(AT_ROWS == 128, "two a lane");
+__device__ __forceinline__ Reach at_reach(Span low, Span high)
+{
+    const uint64_t in_low = __ballot(low.lo < low.hi), in_high = __ballot(high.lo < high.hi);
+    const Span first = in_low ? at_lane(low, __builtin_ctzll(in_low)) : at_lane(high, in_high ? __builtin_ctzll(in_high) : 0);
+    const Span last = in_high ? at_lane(high, 63 - __builtin_clzll(in_high)) : at_lane(low, in_low ? 63 - __builtin_clzll(in_low) : 0);
+    return Reach(first, last, (in_low | in_high) != 0);
+}
+// The same from all positions' intervals (SEEN: of what sees the rows).
 template <bool SEEN>
 __device__ __forceinline__ Reach at_reach(const Spans* spans, int first, int tokens)
 {
-    const int lane = threadIdx.x & 63;
-    Reach r = Reach::nothing();
-#pragma unroll
-    for (int i = 0; i < AT_ROWS / 64; ++i) {
-        const int t = first + i * 64 + lane;
-        if (t < tokens) r.join(SEEN ? spans[t].seen : spans[t].sees);
+    const int t = first + (threadIdx.x & 63), u = t + 64;
+    const Span none{0, 0};
+    const Span low = t < tokens ? SEEN ? spans[t].seen : spans[t].sees : none, high = u < tokens ? SEEN ? spans[u].seen : spans[u].sees : none;
+    return at_reach(low, high);
+}
+
+// The tile whose turn it is where there are several documents: the one with the turn's place among all, by what its rows see (or are seen by), the longest first.
+// `lengths`: of all tiles, one a thread (at most AT_RANKED; 24 documents in 8192 positions: 87 -> us).
+constexpr int AT_RANKED = AT_TPB;
+__device__ __forceinline__ int at_ranked(int turn, int tiles, int length, char* lds)
+{
+    int* const lengths = reinterpret_cast<int*>(lds);
+    int* const found = lengths + AT_RANKED;
+    lengths[threadIdx.x] = (int)threadIdx.x < tiles ? length : -1;
+    __syncthreads();
+    int before = 0;
+    for (int i = 0; i < tiles; i += 4) {
+        const int4 l = *reinterpret_cast<const int4*>(lengths + i);
+        before += l.x > length || (l.x == length && i < (int)threadIdx.x);
+        before += l.y > length || (l.y == length && i + 1 < (int)threadIdx.x);
+        before += l.z > length || (l.z == length && i + 2 < (int)threadIdx.x);
+        before += l.w > length || (l.w == length && i + 3 < (int)threadIdx.x);
     }
-    r.share();
-    return r;
+    if ((int)threadIdx.x < tiles && before == turn) *found = threadIdx.x;
+    __syncthreads();
+    const int tile = __builtin_amdgcn_readfirstlane(*found);
+    __syncthreads();
+    return tile;
+}
+// How far the first and the last of a tile's rows reach.
+__device__ __forceinline__ int at_length(Span first, Span last) { return max(last.hi - first.lo, 0); }
+template <bool SEEN>
+__device__ __forceinline__ int at_ranked_by_spans(const Spans* spans, int turn, int tiles, int tokens, char* lds)
+{
+    const int first = min((int)threadIdx.x, tiles - 1) * AT_ROWS, last = min(first + AT_ROWS, tokens) - 1;
+    const int length = SEEN ? at_length(spans[first].seen, spans[last].seen) : at_length(spans[first].sees, spans[last].sees);
+    return at_ranked(turn, tiles, length, lds);
 }
 
 template <int D>
@@ -475,25 +496,31 @@ __global__ void __launch_bounds__(AT_TPB, 2) rb_attend_kernel(AttentionArgs a)
     int tile, head;
     at_place<false>(blockIdx.x, a.tiles, a.heads, a.inner, tile, head);
     const int kv = head / a.group;
-    const int row = tile * AT_ROWS + wave * AT_BLOCK + (lane & 31);
-    Span* const spans = reinterpret_cast<Span*>(&lds[0][0][0]);            // of the workgroup's rows, before the tiles come
+    // what the workgroup's rows see, in LDS before the tiles come
+    Span* const spans = reinterpret_cast<Span*>(&lds[0][0][0]);
     if (a.spans == nullptr) {
+        static_assert(AT_ROWS * sizeof(Span) + AT_NEAR_OFFSETS * 8 + (AT_RANKED + 1) * 4 <= sizeof(lds), "intervals, offsets, ranks");
         int64_t* const near = reinterpret_cast<int64_t*>(&lds[0][0][0] + AT_ROWS * sizeof(Span));
         for (int i = threadIdx.x; i <= a.documents.count; i += AT_TPB) near[i] = a.documents.offsets[i];
         __syncthreads();
-        a.documents.offsets = near;
-    }
-    if (threadIdx.x < AT_ROWS) {
+        if (a.ranked) {
+            const int first = min((int)threadIdx.x, a.tiles - 1) * AT_ROWS, end = min(first + AT_ROWS, a.tokens);
+            const int64_t d = at_begun(near, a.documents.count, first);
+            const int length = end - (d > 0 ? (int)min(max(near[d - 1], (int64_t)0), (int64_t)a.tokens) : first);
+            tile = at_ranked(a.tiles - 1 - tile, a.tiles, length, reinterpret_cast<char*>(near + AT_NEAR_OFFSETS));
+        }
+        if (threadIdx.x < AT_ROWS) {
+            const int t = tile * AT_ROWS + threadIdx.x;
+            spans[threadIdx.x] = t < a.tokens ? at_spans_of(a.documents, near, t).sees : Span{0, 0};
+        }
+    } else if (threadIdx.x < AT_ROWS) {
         const int t = tile * AT_ROWS + threadIdx.x;
-        spans[threadIdx.x] = t >= a.tokens ? Span{0, 0} : a.spans ? a.spans[t].sees : at_spans_of(a.documents, t).sees;
+        spans[threadIdx.x] = t < a.tokens ? a.spans[t].sees : Span{0, 0};
     }
     __syncthreads();
+    const int row = tile * AT_ROWS + wave * AT_BLOCK + (lane & 31);
     const Span mine = spans[wave * AT_BLOCK + (lane & 31)];
-    Reach all = Reach::nothing();
-#pragma unroll
-    for (int i = 0; i < AT_ROWS / 64; ++i) all.join(spans[i * 64 + lane]);
-    all.share();
-    const Reach reach = at_reach(mine);
+    const Reach all = at_reach(spans[lane], spans[64 + lane]), reach = at_reach(mine);
     __syncthreads();
     const int last = a.tokens - 1;
     const Bf16 *const keys = a.k.at(0, kv), *const values = a.v.at(0, kv);
@@ -589,7 +616,7 @@ __global__ void __launch_bounds__(AT_TPB, 2) rb_attend_kernel(AttentionArgs a)
         at_add<D, 4, true>(o, p, reads, vt, 0);
     };
 
-    const int count = all.lo < all.hi ? (all.hi - all.lo + AT_TILE - 1) / AT_TILE : 0;
+    const int count = all.tiles(AT_TILE);
     if (count > 0) {
         at_bring_own<D>(bring, a.q.at(0, head), a.q.token, tile, last, lds[1]);
         bring(keys, a.k.token, k_offset, all.lo, last, lds[0][0]);
@@ -645,32 +672,46 @@ __global__ void __launch_bounds__(AT_TPB, 2) rb_attend_kernel(AttentionArgs a)
 
 // ---- gradients -----------------------------------------------------------------
 
-// What the gradients need: the positions' intervals, and of every row of every head lse in base 2 and the sum of grad_out * out.  16 lanes a row.
+// What the gradients need: the positions' intervals, and of every row of every head lse in base 2 and the sum of grad_out * out.  A workgroup has 16 positions, 16
+// lanes each, and goes through its part of the heads, four at a time.
+constexpr int AT_POSITIONS = AT_TPB / 16, AT_ONCE = 4;
 __global__ void __launch_bounds__(AT_TPB) rb_attend_delta_kernel(AttentionArgs a, float* lse2)
 {
-    const int64_t rows = (int64_t)a.heads * a.tokens;
-    const int first = (threadIdx.x & 15) * 8;
-    for (int64_t at = (int64_t)blockIdx.x * (AT_TPB / 16) + threadIdx.x / 16; at < rows; at += (int64_t)gridDim.x * (AT_TPB / 16)) {       // (whole groups of 16 lanes)
-        const int t = (int)(at / a.heads), h = (int)(at - (int64_t)t * a.heads);
-        float sum = 0.0f;
-        if (first < a.dim) {
-            const sc_vec x = *reinterpret_cast<const sc_vec*>(a.out.at(t, h) + first), y = *reinterpret_cast<const sc_vec*>(a.grad_out.at(t, h) + first);
+    __shared__ Spans found[AT_POSITIONS];
+    const int start = blockIdx.x * AT_POSITIONS, of = threadIdx.x / 16, t = min(start + of, a.tokens - 1), first = (threadIdx.x & 15) * 8;
+    if (threadIdx.x < AT_POSITIONS && start + (int)threadIdx.x < a.tokens) {
+        found[threadIdx.x] = at_spans_of(a.documents, a.documents.offsets, start + threadIdx.x);
+        if (blockIdx.y == 0) a.documents.spans[start + threadIdx.x] = found[threadIdx.x];
+    }
+    const int from_head = a.heads * blockIdx.y / gridDim.y, to_head = a.heads * (blockIdx.y + 1) / gridDim.y;
+    for (int h0 = from_head; h0 < to_head; h0 += AT_ONCE) {
+        sc_vec x[AT_ONCE], y[AT_ONCE];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                sum = fmaf(__uint_as_float(x[i] << 16), __uint_as_float(y[i] << 16), sum);
-                sum = fmaf(__uint_as_float(x[i] & 0xffff0000u), __uint_as_float(y[i] & 0xffff0000u), sum);
-            }
+        for (int i = 0; i < AT_ONCE; ++i) {
+            const int h = min(h0 + i, to_head - 1), from = first < a.dim ? first : 0;
+            x[i] = *reinterpret_cast<const sc_vec*>(a.out.at(t, h) + from);
+            y[i] = *reinterpret_cast<const sc_vec*>(a.grad_out.at(t, h) + from);
         }
-        sum += sc_xor<1>(sum);
-        sum += sc_xor<2>(sum);
-        sum += sc_xor<4>(sum);
-        sum += sc_xor<8>(sum);
-        if (first == 0) {
-            const Spans s = at_spans_of(a.documents, t);
-            if (h == 0) a.documents.spans[t] = s;
-            const int64_t to = (int64_t)h * a.tokens + t;
-            a.delta[to] = sum;
-            lse2[to] = s.sees.lo < s.sees.hi ? a.lse[to] * AT_LOG2E - a.lse_less : -sc_neg_inf();
+        if (h0 == from_head) __syncthreads();
+#pragma unroll
+        for (int i = 0; i < AT_ONCE; ++i) {
+            float sum = 0.0f;
+#pragma unroll
+            for (int n = 0; n < 4; ++n) {
+                sum = fmaf(__uint_as_float(x[i][n] << 16), __uint_as_float(y[i][n] << 16), sum);
+                sum = fmaf(__uint_as_float(x[i][n] & 0xffff0000u), __uint_as_float(y[i][n] & 0xffff0000u), sum);
+            }
+            if (first >= a.dim) sum = 0.0f;
+            sum += sc_xor<1>(sum);
+            sum += sc_xor<2>(sum);
+            sum += sc_xor<4>(sum);
+            sum += sc_xor<8>(sum);
+            if (first == 0 && start + of < a.tokens && h0 + i < to_head) {
+                const Span s = found[of].sees;
+                const int64_t to = (int64_t)(h0 + i) * a.tokens + t;
+                a.delta[to] = sum;
+                lse2[to] = s.lo < s.hi ? a.lse[to] * AT_LOG2E - a.lse_less : -sc_neg_inf();
+            }
         }
     }
 }
@@ -701,6 +742,7 @@ __global__ void __launch_bounds__(AT_TPB, 2) rb_attend_grad_q_kernel(AttentionAr
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x & 63, half = lane / 32;
     int tile, head;
     at_place<false>(blockIdx.x, a.tiles, a.heads, a.inner, tile, head);
+    if (a.ranked) tile = at_ranked_by_spans<false>(a.spans, a.tiles - 1 - tile, a.tiles, a.tokens, &lds[0][0][0]);
     const int kv = head / a.group;
     const Reach all = at_reach<false>(a.spans, tile * AT_ROWS, a.tokens);
     const int row = tile * AT_ROWS + wave * AT_BLOCK + (lane & 31);
@@ -762,7 +804,7 @@ __global__ void __launch_bounds__(AT_TPB, 2) rb_attend_grad_q_kernel(AttentionAr
     };
 
     bool lost = false;                              // the row sees a key that is not finite
-    const int count = all.lo < all.hi ? (all.hi - all.lo + ROWS - 1) / ROWS : 0;
+    const int count = all.tiles(ROWS);
     if (count > 0) {
         static_assert(sizeof(lds) == sizeof(own), "queries fit where the keys will be");
         char(&queries)[2][AT_TILE * D * 2] = reinterpret_cast<char(&)[2][AT_TILE * D * 2]>(lds);
@@ -815,6 +857,7 @@ __global__ void __launch_bounds__(AT_TPB, 2) rb_attend_grad_kv_kernel(AttentionA
     int tile, share;
     at_place<true>(blockIdx.x, a.tiles, a.shares, a.inner, tile, share);
     const int parts = a.shares / (a.heads / a.group), kv = share / parts, part = share - kv * parts;
+    if (a.ranked) tile = at_ranked_by_spans<true>(a.spans, tile, a.tiles, a.tokens, &lds[0][0][0]);
     const Reach all = at_reach<true>(a.spans, tile * AT_ROWS, a.tokens);
     const int row = tile * AT_ROWS + wave * AT_BLOCK + (lane & 31);
     const Span mine = row < a.tokens ? a.spans[row].seen : Span{0, 0};
@@ -881,7 +924,7 @@ __global__ void __launch_bounds__(AT_TPB, 2) rb_attend_grad_kv_kernel(AttentionA
 
     bool lost = false;                              // seen by a query that is not finite, or whose gradient is not
     // tiles of queries, head by head; from where and how many
-    const int tiles = all.lo < all.hi ? (all.hi - all.lo + ROWS - 1) / ROWS : 0;
+    const int tiles = all.tiles(ROWS);
     const int from = (int)((int64_t)tiles * a.group * part / parts), skipped = tiles > 0 ? from / tiles : 0;
     int head = kv * a.group + skipped, first = all.lo + (from - skipped * tiles) * ROWS, left = (int)((int64_t)tiles * a.group * (part + 1) / parts) - from;
     if (left) {

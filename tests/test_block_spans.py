@@ -20,7 +20,7 @@ extern "C" void spans_of(const int64_t* offsets, const int64_t* lengths, const i
 {
     const SpanArgs a{offsets, lengths, prefixes, count, nullptr, tokens, causal};
     for (int32_t t = 0; t < tokens; ++t) {
-        const Spans s = at_spans_of(a, t);
+        const Spans s = at_spans_of(a, a.offsets, t);
         out[4 * t] = s.sees.lo; out[4 * t + 1] = s.sees.hi; out[4 * t + 2] = s.seen.lo; out[4 * t + 3] = s.seen.hi;
     }
 }
