@@ -326,7 +326,7 @@ inline int inner_heads(int64_t heads, int64_t group)
 bool heads_fit(const rb_attention* a, const rb_heads* t, bool written)
 {
     if (!t || !t->data || !aligned(t->data, 16) || t->token_stride % 8 != 0 || t->head_stride % 8 != 0) return false;
-    if (t->token_stride < 0 || t->head_stride < 0 || t->token_stride > MAX_STRIDE || t->head_stride > (int64_t(1) << 48)) return false;
+    if (t->token_stride < 0 || t->head_stride < 0 || t->token_stride > AT_MAX_STRIDE || t->head_stride > (int64_t(1) << 48)) return false;
     return !written || (t->token_stride >= a->dim && t->head_stride >= a->dim);
 }
 HeadRows rows_of(const rb_heads* t) { return HeadRows{static_cast<Bf16*>(t->data), t->token_stride, t->head_stride}; }

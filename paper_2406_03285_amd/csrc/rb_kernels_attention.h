@@ -30,6 +30,7 @@ constexpr int AT_BLOCK = 32;                       // rows of a wavefront
 constexpr int AT_ROWS = AT_WAVES * AT_BLOCK;       // rows of a workgroup
 constexpr int AT_TILE = 64;                        // rows that are in LDS at a time
 constexpr float AT_LOG2E = 1.44269504088896340736f;
+constexpr int64_t AT_MAX_STRIDE = 1 << 26;         // of positions, in numbers: 31 strides are less than 2^32 bytes
 constexpr int AT_NEAR_OFFSETS = 2048;              // offsets of documents that a workgroup looks through in LDS
 constexpr float AT_LN2 = 0.69314718055994530942f;
 
@@ -108,13 +109,25 @@ __device__ __forceinline__ int at_turn(int r)
 
 // Asynchronous loads into LDS: the wavefront's lanes bring BYTES each, which land behind each other from `to` on (the same for all of them).  Written
 // out, since for the builtin the compiler has every later read from LDS wait for all of them, also of the tile that is complete; at_arrived waits.
-// (There are no registers that such a load writes.)
+// (There are no registers that such a load writes.)  Two forms: an address a lane, and one for all with an offset in bytes a lane, which takes a third of
+// the registers.
+__device__ __forceinline__ uint32_t at_place_of(const void* to)
+{
+    return (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)to);
+}
 template <int BYTES>
 __device__ __forceinline__ void at_load_to_lds(const void* from, const void* to)
 {
-    const uint32_t place = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)to);
-    if constexpr (BYTES == 16) asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(place) : "memory", "m0");
-    else asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(from), "s"(place) : "memory", "m0");
+    if constexpr (BYTES == 16) asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(at_place_of(to)) : "memory", "m0");
+    else asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(from), "s"(at_place_of(to)) : "memory", "m0");
+}
+__device__ __forceinline__ uint64_t at_scalar(uint64_t v)             // the same for all lanes
+{
+    return (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)v);
+}
+__device__ __forceinline__ void at_load_to_lds(uint64_t base, uint32_t offset, const void* to)
+{
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(base), "s"(at_place_of(to)) : "memory", "m0");
 }
 
 // A lane's part in bringing tiles of ROWS rows of a tensor: the same pieces of every tile.
@@ -130,22 +143,24 @@ struct Bring {
         piece = (lane % PIECES) ^ at_turn<D>(row);
         there = piece * 8 < dim;
     }
-    // Where the lane's piece of a tile's first rows is, relative to the tile's first row.
-    __device__ __forceinline__ int64_t offset(int64_t stride) const { return row * stride + piece * 8; }
+    // Where the lane's piece of a tile's first rows is, in bytes behind the tile's first row (a lane's row is one of 32: strides are at most AT_MAX_STRIDE).
+    __device__ __forceinline__ uint32_t offset(int64_t stride) const { return 2 * ((uint32_t)row * (uint32_t)stride + (uint32_t)piece * 8); }
     // Rows first .. first + ROWS - 1 of the tensor that begins at `from`, no further than row `last`.
-    __device__ __forceinline__ void operator()(const Bf16* from, int64_t stride, int64_t offset, int first, int last, char* tile) const
+    __device__ __forceinline__ void operator()(const Bf16* from, int64_t stride, uint32_t offset, int first, int last, char* tile) const
     {
         if (!there) return;
         if (first + ROWS <= last + 1) {
-            const Bf16* base = from + first * stride;
+            const uint64_t base = at_scalar(reinterpret_cast<uint64_t>(from + first * stride)), step = at_scalar(2 * STEP * (uint64_t)stride);
 #pragma unroll
-            for (int j = 0; j < LOADS; ++j) one(base + j * STEP * stride + offset, tile, j);
+            for (int j = 0; j < LOADS; ++j) at_load_to_lds(base + j * step, offset, tile + (j * AT_WAVES + wave) * 1024);
         } else {
+            int r = first + row, p = piece * 8;
+            asm volatile("" : "+v"(r), "+v"(p));        // (nothing of this is kept for the next tile)
 #pragma unroll
-            for (int j = 0; j < LOADS; ++j) one(from + (int64_t)min(first + j * STEP + row, last) * stride + piece * 8, tile, j);
+            for (int j = 0; j < LOADS; ++j)
+                at_load_to_lds<16>(from + (int64_t)min(r + j * STEP, last) * stride + p, tile + (j * AT_WAVES + wave) * 1024);
         }
     }
-    __device__ __forceinline__ void one(const Bf16* p, char* tile, int j) const { at_load_to_lds<16>(p, tile + (j * AT_WAVES + wave) * 1024); }
 };
 
 // 32 binary32 numbers of a lane half each, to places behind one another.
@@ -256,9 +271,11 @@ struct Noted {
 template <int D, int ROWS = AT_TILE>
 __device__ __forceinline__ void at_make_finite(char* tile, int wave, uint32_t (&noted)[2])
 {
+    int lane = threadIdx.x & 63;
+    asm volatile("" : "+v"(lane));                      // (as above)
 #pragma unroll
     for (int j = 0; j < Bring<D, ROWS>::LOADS; ++j) {
-        const int at = (j * AT_WAVES + wave) * 64 + (threadIdx.x & 63);
+        const int at = (j * AT_WAVES + wave) * 64 + lane;
         sc_vec w = *reinterpret_cast<const sc_vec*>(tile + at * 16);
         uint32_t found = 0;
 #pragma unroll
@@ -450,7 +467,9 @@ __device__ __forceinline__ void at_clear(char* lds, int bytes, int dim)
 template <int D>
 __device__ __forceinline__ void at_store(char* place, Bf16* first, int64_t stride, int rows, int dim, const at_acc (&v)[D / 32], float factor, bool zero)
 {
-    const int lane = threadIdx.x & 63, half = lane / 32, r = lane & 31;
+    int lane = threadIdx.x & 63;
+    asm volatile("" : "+v"(lane));                      // (nothing is kept for this over the tiles)
+    const int half = lane / 32, r = lane & 31;
     char* const mine = place + r * D * 2 + half * 8;
     const int turn = at_turn<D>(r);
 #pragma unroll
@@ -530,7 +549,7 @@ __global__ void __launch_bounds__(AT_TPB, 2) rb_attend_kernel(AttentionArgs a)
     at_clear<D>(&lds[0][0][0], sizeof(lds), a.dim);
     const Bring<D> bring(wave, a.dim);
     const Reads<D> reads;
-    const int64_t k_offset = bring.offset(a.k.token), v_offset = bring.offset(a.v.token);
+    const uint32_t k_offset = bring.offset(a.k.token), v_offset = bring.offset(a.v.token);
     at_acc o[D / 32]{};
     float m = sc_neg_inf(), l = 0.0f;               // maximum (base 2), and this lane's part of the sum
 
@@ -758,7 +777,7 @@ __global__ void __launch_bounds__(AT_TPB, 2) rb_attend_grad_q_kernel(AttentionAr
     const Bring<D, ROWS> bring(wave, a.dim);
     const Bring<D> bring_own(wave, a.dim);
     const Reads<D> reads;
-    const int64_t k_offset = bring.offset(a.k.token), v_offset = bring.offset(a.v.token);
+    const uint32_t k_offset = bring.offset(a.k.token), v_offset = bring.offset(a.v.token);
     at_bf8 q[D / 16];
     at_acc dq[D / 32]{}, pk[D / 32]{};
     float off = 0.0f;
@@ -870,7 +889,7 @@ __global__ void __launch_bounds__(AT_TPB, 2) rb_attend_grad_kv_kernel(AttentionA
     const Bring<D, ROWS> bring(wave, a.dim);
     const Bring<D> bring_own(wave, a.dim);
     const Reads<D> reads;
-    const int64_t q_offset = bring.offset(a.q.token), g_offset = bring.offset(a.grad_out.token);
+    const uint32_t q_offset = bring.offset(a.q.token), g_offset = bring.offset(a.grad_out.token);
     auto fetch = [&](int head, int first, int buffer) {
         bring(a.q.at(0, head), a.q.token, q_offset, first, last, lds[buffer][0]);
         bring(a.grad_out.at(0, head), a.grad_out.token, g_offset, first, last, lds[buffer][1]);

@@ -228,14 +228,14 @@ def test_offsets_that_cannot_be():
 
 
 def test_positions_far_apart():
-    """Offsets beyond 32 bits: positions 2^27 + 8 elements apart, heads 2^32 apart."""
-    tokens, heads, dim = 40, 2, 64
+    """Offsets beyond 32 bits: positions as far apart as they may be, 2^26 elements, heads 2^32 and more apart."""
+    tokens, heads, dim = 70, 2, 64
     q, k, v, d = tensors(tokens, heads, heads, dim, layout="own")
     a = rb.DocumentAttention(heads, dim, max_tokens=tokens)
-    docs = documents([0, 17, 40])
+    docs = documents([0, 17, 70])
     near = a.forward(q, k, v, docs)
     grads = a.grad(q, k, v, docs, near.out, near.lse, d)
-    stride, head = (1 << 27) + 8, (1 << 32) + (1 << 31)
+    stride, head = 1 << 26, (1 << 32) + (1 << 31) + 8
     store = torch.empty((tokens - 1) * stride + head + dim, dtype=BF16, device="cuda")
     far = store.as_strided((tokens, heads, dim), (stride, head, 1))
     for which in range(3):
