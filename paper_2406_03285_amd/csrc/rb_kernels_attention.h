@@ -111,23 +111,25 @@ __device__ __forceinline__ int at_turn(int r)
 // out, since for the builtin the compiler has every later read from LDS wait for all of them, also of the tile that is complete; at_arrived waits.
 // (There are no registers that such a load writes.)  Two forms: an address a lane, and one for all with an offset in bytes a lane, which takes a third of
 // the registers.
-__device__ __forceinline__ uint32_t at_place_of(const void* to)
+__device__ __forceinline__ uint32_t at_place_of(const void* to)       // as LDS counts, the same for all lanes
 {
     return (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)to);
 }
-template <int BYTES>
-__device__ __forceinline__ void at_load_to_lds(const void* from, const void* to)
-{
-    if constexpr (BYTES == 16) asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(at_place_of(to)) : "memory", "m0");
-    else asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(from), "s"(at_place_of(to)) : "memory", "m0");
-}
-__device__ __forceinline__ uint64_t at_scalar(uint64_t v)             // the same for all lanes
+__device__ __forceinline__ uint64_t at_scalar(uint64_t v)
 {
     return (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)v);
 }
-__device__ __forceinline__ void at_load_to_lds(uint64_t base, uint32_t offset, const void* to)
+template <int BYTES>
+__device__ __forceinline__ void at_load_to_lds(const void* from, uint32_t to)
 {
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(base), "s"(at_place_of(to)) : "memory", "m0");
+    to = (uint32_t)__builtin_amdgcn_readfirstlane((int)to);
+    if constexpr (BYTES == 16) asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(to) : "memory", "m0");
+    else asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(from), "s"(to) : "memory", "m0");
+}
+__device__ __forceinline__ void at_load_to_lds(uint64_t base, uint32_t offset, uint32_t to)
+{
+    to = (uint32_t)__builtin_amdgcn_readfirstlane((int)to);
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(base), "s"(to) : "memory", "m0");
 }
 
 // A lane's part in bringing tiles of ROWS rows of a tensor: the same pieces of every tile.
@@ -144,9 +146,14 @@ struct Bring {
         there = piece * 8 < dim;
     }
     // Where the lane's piece of a tile's first rows is, in bytes behind the tile's first row (a lane's row is one of 32: strides are at most AT_MAX_STRIDE).
-    __device__ __forceinline__ uint32_t offset(int64_t stride) const { return 2 * ((uint32_t)row * (uint32_t)stride + (uint32_t)piece * 8); }
+    __device__ __forceinline__ uint32_t offset(int64_t stride) const
+    {
+        uint32_t bytes = 2 * ((uint32_t)row * (uint32_t)stride + (uint32_t)piece * 8);
+        asm volatile("" : "+v"(bytes));                 // (one register, and not half of a product's two)
+        return bytes;
+    }
     // Rows first .. first + ROWS - 1 of the tensor that begins at `from`, no further than row `last`.
-    __device__ __forceinline__ void operator()(const Bf16* from, int64_t stride, uint32_t offset, int first, int last, char* tile) const
+    __device__ __forceinline__ void operator()(const Bf16* from, int64_t stride, uint32_t offset, int first, int last, uint32_t tile) const
     {
         if (!there) return;
         if (first + ROWS <= last + 1) {
@@ -164,7 +171,7 @@ struct Bring {
 };
 
 // 32 binary32 numbers of a lane half each, to places behind one another.
-__device__ __forceinline__ void at_bring_numbers(const float* from, int first, int last, float* to)
+__device__ __forceinline__ void at_bring_numbers(const float* from, int first, int last, uint32_t to)
 {
     at_load_to_lds<4>(from + min(first + (int)(threadIdx.x & 31), last), to);
 }
@@ -224,10 +231,10 @@ __device__ __forceinline__ void at_own(const Reads<D>& reads, const char (&tiles
 }
 // The workgroup's 128 rows into two tiles.
 template <int D>
-__device__ __forceinline__ void at_bring_own(const Bring<D>& bring, const Bf16* from, int64_t stride, int tile, int last, char (&tiles)[2][AT_TILE * D * 2])
+__device__ __forceinline__ void at_bring_own(const Bring<D>& bring, const Bf16* from, int64_t stride, int tile, int last, uint32_t tiles)
 {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) bring(from, stride, bring.offset(stride), min(tile * AT_ROWS + i * AT_TILE, last), last, tiles[i]);
+    for (int i = 0; i < 2; ++i) bring(from, stride, bring.offset(stride), min(tile * AT_ROWS + i * AT_TILE, last), last, tiles + i * AT_TILE * D * 2);
 }
 
 // sum[n] += columns of the tile's rows 16 (c0 + c) .. times factors[c], for the head's numbers 32 n ..  AHEAD: the next columns are on their way while the last
@@ -382,7 +389,8 @@ __device__ __forceinline__ void at_place(int id, int tiles, int heads, int inner
         t = id / heads;
         head = id - t * heads;
     }
-    tile = UP ? t : tiles - 1 - t;             // (the turn's, where tiles are ranked)
+    tile = __builtin_amdgcn_readfirstlane(UP ? t : tiles - 1 - t);             // (the turn's, where tiles are ranked)
+    head = __builtin_amdgcn_readfirstlane(head);
 }
 
 // What rows see: all of it lies in [lo, hi), and [all_lo, all_hi) is seen by every row that sees anything.  Intervals of rows behind one another rise, so the
@@ -511,10 +519,12 @@ __global__ void __launch_bounds__(AT_TPB, 2) rb_attend_kernel(AttentionArgs a)
 {
     __shared__ __align__(1024) char lds[2][2][AT_TILE * D * 2];
     __shared__ Noted noted;
+    constexpr uint32_t BYTES = AT_TILE * D * 2;
+    const uint32_t place = at_place_of(&lds[0][0][0]);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x & 63, half = lane / 32;
     int tile, head;
     at_place<false>(blockIdx.x, a.tiles, a.heads, a.inner, tile, head);
-    const int kv = head / a.group;
+    const int kv = __builtin_amdgcn_readfirstlane(head / a.group);
     // what the workgroup's rows see, in LDS before the tiles come
     Span* const spans = reinterpret_cast<Span*>(&lds[0][0][0]);
     if (a.spans == nullptr) {
@@ -637,9 +647,9 @@ __global__ void __launch_bounds__(AT_TPB, 2) rb_attend_kernel(AttentionArgs a)
 
     const int count = all.tiles(AT_TILE);
     if (count > 0) {
-        at_bring_own<D>(bring, a.q.at(0, head), a.q.token, tile, last, lds[1]);
-        bring(keys, a.k.token, k_offset, all.lo, last, lds[0][0]);
-        bring(values, a.v.token, v_offset, all.lo, last, lds[0][1]);
+        at_bring_own<D>(bring, a.q.at(0, head), a.q.token, tile, last, place + 2 * BYTES);
+        bring(keys, a.k.token, k_offset, all.lo, last, place);
+        bring(values, a.v.token, v_offset, all.lo, last, place + BYTES);
         at_arrived();
         at_own<D>(reads, lds[1], wave, q);
         at_wait_for_all();
@@ -649,8 +659,8 @@ __global__ void __launch_bounds__(AT_TPB, 2) rb_attend_kernel(AttentionArgs a)
         at_arrived();
         if (threadIdx.x < 2) noted.rows[now ^ 1][threadIdx.x] = 0;
         if (i + 1 < count) {
-            bring(keys, a.k.token, k_offset, first + AT_TILE, last, lds[now ^ 1][0]);
-            bring(values, a.v.token, v_offset, first + AT_TILE, last, lds[now ^ 1][1]);
+            bring(keys, a.k.token, k_offset, first + AT_TILE, last, place + (now ^ 1) * 2 * BYTES);
+            bring(values, a.v.token, v_offset, first + AT_TILE, last, place + (now ^ 1) * 2 * BYTES + BYTES);
         }
         const bool all_see = all.whole(first);
         if (!all_see) {
@@ -758,11 +768,13 @@ __global__ void __launch_bounds__(AT_TPB, 2) rb_attend_grad_q_kernel(AttentionAr
     __shared__ __align__(1024) char lds[2][2][ROWS * D * 2];           // keys and values; first the workgroup's queries
     __shared__ __align__(1024) char own[AT_ROWS / AT_TILE][AT_TILE * D * 2];       // the gradients of the workgroup's results
     __shared__ Noted noted;
+    constexpr uint32_t BYTES = ROWS * D * 2;
+    const uint32_t place = at_place_of(&lds[0][0][0]), place_own = at_place_of(&own[0][0]);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x & 63, half = lane / 32;
     int tile, head;
     at_place<false>(blockIdx.x, a.tiles, a.heads, a.inner, tile, head);
     if (a.ranked) tile = at_ranked_by_spans<false>(a.spans, a.tiles - 1 - tile, a.tiles, a.tokens, &lds[0][0][0]);
-    const int kv = head / a.group;
+    const int kv = __builtin_amdgcn_readfirstlane(head / a.group);
     const Reach all = at_reach<false>(a.spans, tile * AT_ROWS, a.tokens);
     const int row = tile * AT_ROWS + wave * AT_BLOCK + (lane & 31);
     const Span mine = row < a.tokens ? a.spans[row].sees : Span{0, 0};
@@ -791,26 +803,31 @@ __global__ void __launch_bounds__(AT_TPB, 2) rb_attend_grad_q_kernel(AttentionAr
             s = at_mma(reads.rows(kt, 0, n), q[n], s);
             dp = at_mma(reads.rows(vt, 0, n), reads.rows(own[wave / 2], wave % 2, n), dp);
         }
-        at_acc w;                                   // p, times the cap's slope
-        auto elements = [&](auto masked_) {
+        at_acc w;                                   // p; s: ds; both times the cap's slope, that is kept in dp meanwhile
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            const int key = 8 * (e / 4) + e % 4;
+            float p, slope;
+            at_weight<FORM>(a.score, s[e], SLOPES ? fmaf(slope2, fabsf(away - (float)key), lse2) : lse2, p, slope);
+            w[e] = p;
+            s[e] = p * (dp[e] - delta);
+            dp[e] = slope;
+        }
+        if (masked) {
+            asm volatile("");       // (a branch: few tiles need it)
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
-                const int key = 8 * (e / 4) + e % 4;
-                float p, slope;
-                at_weight<FORM>(a.score, s[e], SLOPES ? fmaf(slope2, fabsf(away - (float)key), lse2) : lse2, p, slope);
-                float ds = p * (dp[e] - delta);
-                if (masked_()) {
-                    const bool seen = key + 4 * half >= from && key + 4 * half < to;
-                    p = seen ? p : 0.0f;
-                    ds = seen ? ds : 0.0f;
-                }
-                off += ds;
-                s[e] = FORM == AT_PLAIN ? ds : ds * slope;
-                w[e] = FORM == AT_PLAIN ? p : p * slope;
+                const int key = 8 * (e / 4) + 4 * half + e % 4;
+                const bool seen = key >= from && key < to;
+                w[e] = seen ? w[e] : 0.0f;
+                s[e] = seen ? s[e] : 0.0f;
             }
-        };
-        if (masked) elements(std::true_type());
-        else elements(std::false_type());
+        }
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            off += s[e];
+            if (FORM != AT_PLAIN) s[e] *= dp[e], w[e] *= dp[e];
+        }
         const at_bf8 f[2] = {at_pack(s, 0), at_pack(s, 1)}, g[2] = {at_pack(w, 0), at_pack(w, 1)};
 #pragma unroll
         for (int c = 0; c < 2; ++c)
@@ -827,21 +844,21 @@ __global__ void __launch_bounds__(AT_TPB, 2) rb_attend_grad_q_kernel(AttentionAr
     if (count > 0) {
         static_assert(sizeof(lds) == sizeof(own), "queries fit where the keys will be");
         char(&queries)[2][AT_TILE * D * 2] = reinterpret_cast<char(&)[2][AT_TILE * D * 2]>(lds);
-        at_bring_own<D>(bring_own, a.grad_out.at(0, head), a.grad_out.token, tile, last, own);
-        at_bring_own<D>(bring_own, a.q.at(0, head), a.q.token, tile, last, queries);
+        at_bring_own<D>(bring_own, a.grad_out.at(0, head), a.grad_out.token, tile, last, place_own);
+        at_bring_own<D>(bring_own, a.q.at(0, head), a.q.token, tile, last, place);
         at_arrived();
         at_own<D>(reads, queries, wave, q);
         at_wait_for_all();
-        bring(keys, a.k.token, k_offset, all.lo, last, lds[0][0]);
-        bring(values, a.v.token, v_offset, all.lo, last, lds[0][1]);
+        bring(keys, a.k.token, k_offset, all.lo, last, place);
+        bring(values, a.v.token, v_offset, all.lo, last, place + BYTES);
     }
     for (int i = 0; i < count; ++i) {
         const int first = all.lo + i * ROWS, now = i & 1;
         at_arrived();
         if (threadIdx.x < 2) noted.rows[now ^ 1][threadIdx.x] = 0;
         if (i + 1 < count) {
-            bring(keys, a.k.token, k_offset, first + ROWS, last, lds[now ^ 1][0]);
-            bring(values, a.v.token, v_offset, first + ROWS, last, lds[now ^ 1][1]);
+            bring(keys, a.k.token, k_offset, first + ROWS, last, place + (now ^ 1) * 2 * BYTES);
+            bring(values, a.v.token, v_offset, first + ROWS, last, place + (now ^ 1) * 2 * BYTES + BYTES);
         }
         if (!all.whole(first, ROWS)) {
             at_make_finite<D, ROWS>(lds[now][0], wave, noted.rows[now]);
@@ -870,12 +887,15 @@ __global__ void __launch_bounds__(AT_TPB, 2) rb_attend_grad_kv_kernel(AttentionA
     __shared__ __align__(1024) char lds[2][2][ROWS * D * 2];           // queries and their gradients; first the workgroup's keys
     __shared__ __align__(1024) char own[AT_ROWS / AT_TILE][AT_TILE * D * 2];       // the workgroup's values
     __shared__ Noted noted;
+    constexpr uint32_t BYTES = ROWS * D * 2;
+    const uint32_t place = at_place_of(&lds[0][0][0]), place_own = at_place_of(&own[0][0]);
     __shared__ __align__(1024) float numbers[2][AT_TILE];          // lse in base 2 and delta of the tile's queries
+    const uint32_t place_numbers = at_place_of(&numbers[0][0]);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x & 63, half = lane / 32;
     // one workgroup's share: a head of keys, and all of its queries or a part of them
     int tile, share;
     at_place<true>(blockIdx.x, a.tiles, a.shares, a.inner, tile, share);
-    const int parts = a.shares / (a.heads / a.group), kv = share / parts, part = share - kv * parts;
+    const int parts = __builtin_amdgcn_readfirstlane(a.shares / (a.heads / a.group)), kv = __builtin_amdgcn_readfirstlane(share / parts), part = share - kv * parts;
     if (a.ranked) tile = at_ranked_by_spans<true>(a.spans, tile, a.tiles, a.tokens, &lds[0][0][0]);
     const Reach all = at_reach<true>(a.spans, tile * AT_ROWS, a.tokens);
     const int row = tile * AT_ROWS + wave * AT_BLOCK + (lane & 31);
@@ -891,9 +911,9 @@ __global__ void __launch_bounds__(AT_TPB, 2) rb_attend_grad_kv_kernel(AttentionA
     const Reads<D> reads;
     const uint32_t q_offset = bring.offset(a.q.token), g_offset = bring.offset(a.grad_out.token);
     auto fetch = [&](int head, int first, int buffer) {
-        bring(a.q.at(0, head), a.q.token, q_offset, first, last, lds[buffer][0]);
-        bring(a.grad_out.at(0, head), a.grad_out.token, g_offset, first, last, lds[buffer][1]);
-        if (wave == 0) at_bring_numbers((lane < 32 ? a.lse2 : a.delta) + (int64_t)head * a.tokens, first, last, numbers[buffer]);
+        bring(a.q.at(0, head), a.q.token, q_offset, first, last, place + buffer * 2 * BYTES);
+        bring(a.grad_out.at(0, head), a.grad_out.token, g_offset, first, last, place + buffer * 2 * BYTES + BYTES);
+        if (wave == 0) at_bring_numbers((lane < 32 ? a.lse2 : a.delta) + (int64_t)head * a.tokens, first, last, place_numbers + buffer * AT_TILE * 4);
     };
     at_acc dk[D / 32]{}, dv[D / 32]{};
 
@@ -944,13 +964,13 @@ __global__ void __launch_bounds__(AT_TPB, 2) rb_attend_grad_kv_kernel(AttentionA
     bool lost = false;                              // seen by a query that is not finite, or whose gradient is not
     // tiles of queries, head by head; from where and how many
     const int tiles = all.tiles(ROWS);
-    const int from = (int)((int64_t)tiles * a.group * part / parts), skipped = tiles > 0 ? from / tiles : 0;
-    int head = kv * a.group + skipped, first = all.lo + (from - skipped * tiles) * ROWS, left = (int)((int64_t)tiles * a.group * (part + 1) / parts) - from;
+    const int from = __builtin_amdgcn_readfirstlane((int)((int64_t)tiles * a.group * part / parts)), skipped = tiles > 0 ? __builtin_amdgcn_readfirstlane(from / tiles) : 0;
+    int head = kv * a.group + skipped, first = all.lo + (from - skipped * tiles) * ROWS, left = __builtin_amdgcn_readfirstlane((int)((int64_t)tiles * a.group * (part + 1) / parts)) - from;
     if (left) {
         static_assert(sizeof(lds) == sizeof(own), "keys fit where the queries will be");
         char(&keys)[2][AT_TILE * D * 2] = reinterpret_cast<char(&)[2][AT_TILE * D * 2]>(lds);
-        at_bring_own<D>(bring_own, a.v.at(0, kv), a.v.token, tile, last, own);
-        at_bring_own<D>(bring_own, a.k.at(0, kv), a.k.token, tile, last, keys);
+        at_bring_own<D>(bring_own, a.v.at(0, kv), a.v.token, tile, last, place_own);
+        at_bring_own<D>(bring_own, a.k.at(0, kv), a.k.token, tile, last, place);
         at_arrived();
         at_own<D>(reads, keys, wave, k);
         at_wait_for_all();
@@ -984,10 +1004,10 @@ __global__ void __launch_bounds__(AT_TPB, 2) rb_attend_grad_kv_kernel(AttentionA
         return;
     }
     const int start = tile * AT_ROWS + wave * AT_BLOCK;
-    char* const place = &own[0][0] + wave * AT_BLOCK * D * 2;
+    char* const through = &own[0][0] + wave * AT_BLOCK * D * 2;
     at_wait_for_all();
-    at_store<D>(place, a.grad_k.at(start, kv), a.grad_k.token, a.tokens - start, a.dim, dk, lost ? sc_nan() : a.score.scale, empty);
-    at_store<D>(place, a.grad_v.at(start, kv), a.grad_v.token, a.tokens - start, a.dim, dv, lost ? sc_nan() : 1.0f, empty);
+    at_store<D>(through, a.grad_k.at(start, kv), a.grad_k.token, a.tokens - start, a.dim, dk, lost ? sc_nan() : a.score.scale, empty);
+    at_store<D>(through, a.grad_v.at(start, kv), a.grad_v.token, a.tokens - start, a.dim, dv, lost ? sc_nan() : 1.0f, empty);
 }
 
 // Gradients of keys and values from the parts' sums: a thread has four numbers of a row of one head.
