@@ -149,9 +149,11 @@ typedef struct rb_documents {
  *   s[j] = scale * (q[i] . k[j]);  s[j] = cap * tanh(s[j] / cap) with a cap;  s[j] -= slopes[h] * |i - j| with slopes (device, `heads` numbers; may be null)
  *   lse = log of the sum of e^s[j]                -> lse[h * tokens + i]  (may be null)
  *   out = sum of e^(s[j] - lse) v[j]              -> out, rounded to bfloat16
- * Products of bfloat16 numbers with sums in binary32; e^(s - max) is rounded to bfloat16 for the product with v, its sum is not.  Positions that belong to
- * no document have out 0 and lse -inf, and what lies there in q, k and v does not matter.  What a position does not see has no influence on it, infinities
- * and NaN included; an infinity in a v[j] that it sees makes out that infinity, a NaN NaN.  out overlaps nothing that is read.  tokens = 0 is a no-op.
+ * Products of bfloat16 numbers with sums in binary32; e^(s - max) is rounded to bfloat16 for the product with v, its sum is not.  With less than 128 positions a
+ * document in the mean (tokens < 128 * count) it is taken to 2^-17 of itself instead.  With a cap of up to 32 and more positions than that, scores are
+ * off by up to cap * 2^-22.  Positions that belong to no document have out 0 and lse -inf, and what lies there in q, k and v does not matter.  What a position
+ * does not see has no influence on it, infinities and NaN included; an infinity in a v[j] that it sees makes out that infinity (or NaN, where its weight is 0
+ * in binary32), a NaN NaN.  out overlaps nothing that is read.  tokens = 0 is a no-op.
  * RB_EINVAL: null or misaligned pointers, strides that do not fit, tokens < 0 or > max_tokens, documents' count < 0 or > RB_MAX_DOCUMENTS.
  * RB_ESTATE: not bound.
  */
@@ -162,7 +164,8 @@ int rb_attention_forward(rb_attention *a, const rb_heads *q, const rb_heads *k, 
  * Gradients with respect to q, k and v of a loss with the derivative grad_out of out; out and lse are rb_attention_forward's for the same arguments.  With p =
  * e^(s - lse), dp = grad_out[i] . v[j], ds = p * (dp - sum of p * dp), times the cap's slope and scale:
  *   grad_v[j] = sum over i of p grad_out[i],  grad_q[i] = sum over j of ds k[j],  grad_k[j] = sum over i of ds q[i]
- * (of keys and values over their heads of queries too), sums in binary32, p and ds rounded to bfloat16 for these products, results rounded to bfloat16.
+ * (of keys and values over their heads of queries too), sums in binary32, p and ds rounded to bfloat16 for these products (or taken to 2^-17 of themselves,
+ * as above), results rounded to bfloat16.  A position that sees one alone has a gradient of q of 0.
  * The sum of p * dp is made in binary32 from the first value grad_out[i] . out[i] on, so that out's rounding does not matter.
  * What a position does not see, or is not seen by, has no influence on its gradients; where it sees or is seen by a q, k, v or grad_out that is not finite, they
  * are not finite (which of their numbers is not specified).

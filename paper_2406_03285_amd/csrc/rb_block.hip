@@ -293,8 +293,7 @@ int rb_norm_destroy(rb_norm* n)
 struct rb_attention {
     int32_t heads, kv_heads, dim, max_tokens;
     bool causal;
-    ScoreOf score;
-    int form;                  // of the scores
+    float scale, cap;
     size_t off_lse2, off_delta, off_sums, bytes;
     char* ws;
 };
@@ -337,7 +336,18 @@ bool documents_fit(const rb_documents* d)
     return aligned(d->offsets, 8) && aligned(d->lengths, 8) && aligned(d->prefixes, 8);
 }
 
-AttentionArgs attention_args(const rb_attention* a, const rb_heads* q, const rb_heads* k, const rb_heads* v, int64_t tokens, const rb_documents* d, const float* slopes)
+// Documents of less than 128 positions in the mean have the forms for short documents (FINE), and their capped scores are exact near 0, too: AT_CAPPED's are off by up
+// to cap * 2^-22, which is a part in 10^6 of lse and less where it is of 128 positions.  (64 documents of 128, 16 heads of 128: forward 35 us by
+// these forms and 32 by the others, gradients 106 and 92; with a cap of 30 forward 39 and 33, gradients 113 and 97.)
+inline bool is_short(int64_t tokens, int64_t documents) { return tokens < 128 * documents; }
+inline int form_of(const rb_attention* a, bool fine) { return a->cap == 0.0f ? AT_PLAIN : a->cap <= AT_LOW_CAP && !fine ? AT_CAPPED : AT_HIGH_CAP; }
+ScoreOf score_of(const rb_attention* a, int form)
+{
+    if (form == AT_PLAIN) return ScoreOf{a->scale, a->scale * AT_LOG2E, 0.0f};
+    return ScoreOf{a->scale, a->cap * AT_LOG2E, a->scale / a->cap * (form == AT_CAPPED ? 2 * AT_LOG2E : 1.0f)};
+}
+
+AttentionArgs attention_args(const rb_attention* a, int form, const rb_heads* q, const rb_heads* k, const rb_heads* v, int64_t tokens, const rb_documents* d, const float* slopes)
 {
     AttentionArgs g{};
     g.q = rows_of(q);
@@ -346,7 +356,7 @@ AttentionArgs attention_args(const rb_attention* a, const rb_heads* q, const rb_
     g.documents = SpanArgs{d->offsets, d->lengths, d->prefixes, d->count, reinterpret_cast<Spans*>(a->ws), (int32_t)tokens, a->causal};
     g.spans = g.documents.spans;
     g.slopes = slopes;
-    g.score = a->score;
+    g.score = score_of(a, form);
     g.tokens = (int32_t)tokens;
     g.dim = a->dim;
     g.heads = a->heads;
@@ -357,17 +367,20 @@ AttentionArgs attention_args(const rb_attention* a, const rb_heads* q, const rb_
     return g;
 }
 
-// The kernel of a head's size, the scores' form and slopes: `of` is called with these three.
+// The kernel of a head's size, the scores' form and slopes: and whether documents are short: `of` is called with these four.
 template <typename Of>
-hipError_t by_form(const rb_attention* a, bool slopes, const Of& of)
+hipError_t by_form(const rb_attention* a, int form, bool slopes, bool fine, const Of& of)
 {
     auto with = [&](auto dim) {
         using Plain = std::integral_constant<int, AT_PLAIN>;
         using Capped = std::integral_constant<int, AT_CAPPED>;
         using HighCap = std::integral_constant<int, AT_HIGH_CAP>;
-        if (a->form == AT_PLAIN) return slopes ? of(dim, Plain(), std::true_type()) : of(dim, Plain(), std::false_type());
-        if (a->form == AT_CAPPED) return slopes ? of(dim, Capped(), std::true_type()) : of(dim, Capped(), std::false_type());
-        return of(dim, HighCap(), std::true_type());       // (slopes of 0)
+        using Yes = std::true_type;
+        using No = std::false_type;
+        if (fine) return form == AT_PLAIN ? of(dim, Plain(), Yes(), Yes()) : of(dim, HighCap(), Yes(), Yes());       // (slopes of 0, and below)
+        if (form == AT_PLAIN) return slopes ? of(dim, Plain(), Yes(), No()) : of(dim, Plain(), No(), No());
+        if (form == AT_CAPPED) return slopes ? of(dim, Capped(), Yes(), No()) : of(dim, Capped(), No(), No());
+        return of(dim, HighCap(), Yes(), No());
     };
     return a->dim <= 64 ? with(std::integral_constant<int, 64>()) : with(std::integral_constant<int, 128>());
 }
@@ -390,10 +403,8 @@ int rb_attention_create(rb_attention** out, int64_t heads, int64_t kv_heads, int
     a->dim = (int32_t)head_dim;
     a->max_tokens = (int32_t)max_tokens;
     a->causal = causal != 0;
-    a->form = cap == 0.0f ? AT_PLAIN : cap <= AT_LOW_CAP ? AT_CAPPED : AT_HIGH_CAP;
-    a->score.scale = scale;
-    a->score.to_log2 = (cap == 0.0f ? scale : cap) * AT_LOG2E;
-    a->score.to_tanh = cap == 0.0f ? 0.0f : scale / cap * (a->form == AT_CAPPED ? 2 * AT_LOG2E : 1.0f);
+    a->scale = scale;
+    a->cap = cap;
     size_t off = round_up((size_t)max_tokens * sizeof(Spans), 256);
     a->off_lse2 = off; off += round_up((size_t)heads * (size_t)max_tokens * sizeof(float), 256);
     a->off_delta = off; off += round_up((size_t)heads * (size_t)max_tokens * sizeof(float), 256);
@@ -428,7 +439,9 @@ int rb_attention_forward(rb_attention* a, const rb_heads* q, const rb_heads* k, 
     if (!a->ws) return RB_ESTATE;
     if (tokens == 0) return RB_OK;
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
-    AttentionArgs g = attention_args(a, q, k, v, tokens, documents, slopes);
+    const bool fine = is_short(tokens, documents->count);
+    const int form = form_of(a, fine);
+    AttentionArgs g = attention_args(a, form, q, k, v, tokens, documents, slopes);
     g.out = rows_of(out);
     g.lse = lse;
     // one launch where a workgroup can look through the documents itself (9 documents of 160 positions: 11.3 -> 7.9 us)
@@ -436,8 +449,8 @@ int rb_attention_forward(rb_attention* a, const rb_heads* q, const rb_heads* k, 
     if (documents->count < AT_NEAR_OFFSETS) g.spans = nullptr;       // (with many documents tiles take turns as they lie)
     else e = launch(rb_spans_kernel, dim3((unsigned)(tokens + AT_TPB - 1) / AT_TPB), AT_TPB, 0, st, g.documents);
     if (e == hipSuccess)
-        e = by_form(a, slopes != nullptr, [&](auto dim, auto form, auto lowered) {
-            return launch(rb_attend_kernel<dim(), form(), lowered()>, dim3((unsigned)(g.tiles * g.heads)), AT_TPB, 0, st, g);
+        e = by_form(a, form, slopes != nullptr, fine, [&](auto dim, auto scores, auto lowered, auto rests) {
+            return launch(rb_attend_kernel<dim(), scores(), lowered(), rests()>, dim3((unsigned)(g.tiles * g.heads)), AT_TPB, 0, st, g);
         });
     return e == hipSuccess ? RB_OK : RB_EHIP;
 }
@@ -452,7 +465,9 @@ int rb_attention_grad(rb_attention* a, const rb_heads* q, const rb_heads* k, con
     if (!a->ws) return RB_ESTATE;
     if (tokens == 0) return RB_OK;
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
-    AttentionArgs g = attention_args(a, q, k, v, tokens, documents, slopes);
+    const bool fine = is_short(tokens, documents->count);
+    const int form = form_of(a, fine);
+    AttentionArgs g = attention_args(a, form, q, k, v, tokens, documents, slopes);
     float *const lse2 = reinterpret_cast<float*>(a->ws + a->off_lse2), *const delta = reinterpret_cast<float*>(a->ws + a->off_delta);
     g.out = rows_of(out);
     g.lse = const_cast<float*>(lse);
@@ -462,7 +477,7 @@ int rb_attention_grad(rb_attention* a, const rb_heads* q, const rb_heads* k, con
     g.grad_v = rows_of(grad_v);
     g.lse2 = lse2;
     g.delta = delta;
-    g.lse_less = a->form == AT_CAPPED ? a->score.to_log2 : 0.0f;
+    g.lse_less = form == AT_CAPPED ? g.score.to_log2 : 0.0f;
     const int parts = key_parts(a, tokens, documents->count);
     AttentionArgs of_keys = g;
     of_keys.shares = a->kv_heads * parts;
@@ -472,11 +487,11 @@ int rb_attention_grad(rb_attention* a, const rb_heads* q, const rb_heads* k, con
     const dim3 delta_grid((unsigned)blocks, (unsigned)std::min<int64_t>((a->heads + AT_ONCE - 1) / AT_ONCE, (1024 + blocks - 1) / blocks));
     hipError_t e = launch(rb_attend_delta_kernel, delta_grid, AT_TPB, 0, st, g, lse2);
     if (e == hipSuccess)
-        e = by_form(a, slopes != nullptr, [&](auto dim, auto form, auto lowered) {
+        e = by_form(a, form, slopes != nullptr, fine, [&](auto dim, auto scores, auto lowered, auto rests) {
             // (of queries first: it makes delta exact)
-            hipError_t r = launch(rb_attend_grad_q_kernel<dim(), form(), lowered()>, dim3((unsigned)(g.tiles * g.heads)), AT_TPB, 0, st, g);
+            hipError_t r = launch(rb_attend_grad_q_kernel<dim(), scores(), lowered(), rests()>, dim3((unsigned)(g.tiles * g.heads)), AT_TPB, 0, st, g);
             if (r == hipSuccess)
-                r = launch(rb_attend_grad_kv_kernel<dim(), form(), lowered()>, dim3((unsigned)(g.tiles * of_keys.shares)), AT_TPB, 0, st, of_keys);
+                r = launch(rb_attend_grad_kv_kernel<dim(), scores(), lowered(), rests()>, dim3((unsigned)(g.tiles * of_keys.shares)), AT_TPB, 0, st, of_keys);
             if (r == hipSuccess && parts > 1) {
                 const int64_t threads = (int64_t)a->kv_heads * tokens * (2 * dim() / 4);
                 r = launch(rb_attend_join_kernel<dim()>, dim3((unsigned)std::min<int64_t>((threads + AT_TPB - 1) / AT_TPB, 1 << 16)), AT_TPB, 0, st, of_keys);

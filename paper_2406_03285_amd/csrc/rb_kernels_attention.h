@@ -222,6 +222,30 @@ __device__ __forceinline__ at_bf8 at_pack(const at_acc& v, int c)
     return __builtin_bit_cast(at_bf8, w);
 }
 
+// What that rounding left, rounded: both together are the elements to within 2^-17 of each.
+__device__ __forceinline__ at_bf8 at_pack_rest(const at_acc& v, const at_bf8& rounded, int c)
+{
+    const sc_vec r = __builtin_bit_cast(sc_vec, rounded);
+    sc_vec w;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = sc_bf16_pair(v[8 * c + 2 * i] - __uint_as_float(r[i] << 16), v[8 * c + 2 * i + 1] - __uint_as_float(r[i] & 0xffff0000u));
+    return __builtin_bit_cast(at_bf8, w);
+}
+// sum + the eight numbers of an operand, two at a time.  (Each pair through a register of its own: from within the operand's the compiler takes the first pair
+// four times.)
+__device__ __forceinline__ float at_sum(const at_bf8& v, float sum)
+{
+    typedef __bf16 at_bf2 __attribute__((ext_vector_type(2)));
+    const sc_vec w = __builtin_bit_cast(sc_vec, v);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        uint32_t pair = w[i];
+        asm volatile("" : "+v"(pair));
+        sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(at_bf2, pair), __builtin_bit_cast(at_bf2, 0x3f803f80u), sum, false);
+    }
+    return sum;
+}
+
 // The wavefront's 32 of the workgroup's 128 rows in two tiles, as operands.
 template <int D>
 __device__ __forceinline__ void at_own(const Reads<D>& reads, const char (&tiles)[2][AT_TILE * D * 2], int wave, at_bf8 (&f)[D / 16])
@@ -316,6 +340,10 @@ __device__ __forceinline__ uint64_t at_noted(const uint32_t (&noted)[2], int fro
 // most: less than what rounding e^score to bfloat16 puts in for caps of up to 32, where more is not worth it.  There the cap is also the maximum
 // that the softmax needs: e^(score - cap) is at least e^-64 for what lies next to a position, and its sums are normal numbers.  Larger caps have
 // scores that are exact near 0, too, and a running maximum.
+//
+// Short documents.  p and ds are rounded to bfloat16 for the products over positions.  The errors of many positions are as independent as those of the results'
+// own rounding, and as large.  Of a handful of positions they may be twice as large, so there (FINE) what the rounding left is multiplied too: an error
+// of 2^-17, for products that cost nothing where a launch has a few tiles of positions.
 enum { AT_PLAIN = 0, AT_CAPPED = 1, AT_HIGH_CAP = 2 };
 constexpr float AT_LOW_CAP = 32.0f;
 
@@ -430,7 +458,7 @@ __device__ __forceinline__ Reach at_reach(const Spans* spans, int first, int tok
 }
 
 // The tile whose turn it is where there are several documents: the one with the turn's place among all, by what its rows see (or are seen by), the longest first.
-// `lengths`: of all tiles, one a thread (at most AT_RANKED; 24 documents in 8192 positions: 87 -> us).
+// `lengths`: of all tiles, one a thread (at most AT_RANKED; 24 documents in 8192 positions, 16 heads of 128: 87 -> 77 us).
 constexpr int AT_RANKED = AT_TPB;
 __device__ __forceinline__ int at_ranked(int turn, int tiles, int length, char* lds)
 {
@@ -514,7 +542,7 @@ __device__ __forceinline__ void at_store_sum(float* row, const at_acc (&v)[D / 3
 
 // ---- forward -------------------------------------------------------------------
 
-template <int D, int FORM, bool SLOPES>
+template <int D, int FORM, bool SLOPES, bool FINE>
 __global__ void __launch_bounds__(AT_TPB, 2) rb_attend_kernel(AttentionArgs a)
 {
     __shared__ __align__(1024) char lds[2][2][AT_TILE * D * 2];
@@ -643,6 +671,11 @@ __global__ void __launch_bounds__(AT_TPB, 2) rb_attend_kernel(AttentionArgs a)
             p[2 * b + 1] = at_pack(s[b], 1);
         }
         at_add<D, 4, true>(o, p, reads, vt, 0);
+        if constexpr (FINE) {
+#pragma unroll
+            for (int c = 0; c < 4; ++c) p[c] = at_pack_rest(s[c / 2], p[c], c % 2);
+            at_add<D, 4, true>(o, p, reads, vt, 0);
+        }
     };
 
     const int count = all.tiles(AT_TILE);
@@ -662,7 +695,7 @@ __global__ void __launch_bounds__(AT_TPB, 2) rb_attend_kernel(AttentionArgs a)
             bring(keys, a.k.token, k_offset, first + AT_TILE, last, place + (now ^ 1) * 2 * BYTES);
             bring(values, a.v.token, v_offset, first + AT_TILE, last, place + (now ^ 1) * 2 * BYTES + BYTES);
         }
-        const bool all_see = all.whole(first);
+        const bool all_see = !FINE && all.whole(first);       // (what rounding leaves may be 0 or negative, too)
         if (!all_see) {
             at_make_finite<D>(lds[now][1], wave, noted.rows[now]);
             at_wait_for_all();
@@ -760,8 +793,9 @@ __device__ __forceinline__ void at_weight(const ScoreOf& of, float product, floa
 // bfloat16 puts an error of p times 2^-9 |grad_out . out| into it (5 times what rounding the results does, in short documents).  So delta is summed up again from
 // p dp, unrounded, as its difference `off` from that first value; and since that is known at the end only, sums of p k are kept beside those of
 // ds k: the gradient is the sum of p (dp - first - off) k.  The keys' kernel gets the better delta.  (A fourth product beside three, that shares its operand; a
-// pass of its own over the keys would be two.)
-template <int D, int FORM, bool SLOPES>
+// pass of its own over the keys would be two.)  What is taken away is not the sum of ds itself but that of what they were rounded to: then of a rounding's
+// error e the gradient gets e (k - mean of k) and not e k, where keys may lie around a mean that is larger than what they differ by.
+template <int D, int FORM, bool SLOPES, bool FINE>
 __global__ void __launch_bounds__(AT_TPB, 2) rb_attend_grad_q_kernel(AttentionArgs a)
 {
     constexpr int ROWS = AT_BLOCK;                  // keys at a time
@@ -792,7 +826,7 @@ __global__ void __launch_bounds__(AT_TPB, 2) rb_attend_grad_q_kernel(AttentionAr
     const uint32_t k_offset = bring.offset(a.k.token), v_offset = bring.offset(a.v.token);
     at_bf8 q[D / 16];
     at_acc dq[D / 32]{}, pk[D / 32]{};
-    float off = 0.0f;
+    float off = 0.0f, by = 0.0f;                    // by: what the rounded ds add up to, of capped scores less what they would unrounded
 
     auto step = [&](bool masked, int first, const char* kt, const char* vt) {
         const int from = mine.lo - first, to = mine.hi - first;
@@ -827,16 +861,22 @@ __global__ void __launch_bounds__(AT_TPB, 2) rb_attend_grad_q_kernel(AttentionAr
         for (int e = 0; e < 16; ++e) {
             off += s[e];
             if (FORM != AT_PLAIN) s[e] *= dp[e], w[e] *= dp[e];
+            if (FORM != AT_PLAIN && !FINE) by -= s[e];
         }
         const at_bf8 f[2] = {at_pack(s, 0), at_pack(s, 1)}, g[2] = {at_pack(w, 0), at_pack(w, 1)};
+        if constexpr (!FINE) by = at_sum(f[1], at_sum(f[0], by));
 #pragma unroll
-        for (int c = 0; c < 2; ++c)
+        for (int c = 0; c < 2; ++c) {
+            at_bf8 rest;
+            if constexpr (FINE) rest = at_pack_rest(s, f[c], c);
 #pragma unroll
             for (int n = 0; n < D / 32; ++n) {
                 const at_bf8 column = reads.columns(kt, n, c);
                 dq[n] = at_mma(column, f[c], dq[n]);
                 pk[n] = at_mma(column, g[c], pk[n]);
+                if constexpr (FINE) dq[n] = at_mma(column, rest, dq[n]);
             }
+        }
     };
 
     bool lost = false;                              // the row sees a key that is not finite
@@ -868,19 +908,22 @@ __global__ void __launch_bounds__(AT_TPB, 2) rb_attend_grad_q_kernel(AttentionAr
         if (reach.meets(first, ROWS)) step(!reach.whole(first, ROWS), first, lds[now][0], lds[now][1]);
     }
     off += sc_xor<32>(off);
+    by += sc_xor<32>(by);
     const bool empty = mine.lo >= mine.hi;
     if (half == 0 && row < a.tokens && !empty) a.delta[(int64_t)head * a.tokens + row] = delta + off;
+    const float aside = FINE ? off : FORM == AT_PLAIN ? by : off + by;
 #pragma unroll
     for (int n = 0; n < D / 32; ++n)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) dq[n][e] = fmaf(-off, pk[n][e], dq[n][e]);
+        for (int e = 0; e < 16; ++e) dq[n][e] = fmaf(-aside, pk[n][e], dq[n][e]);
+    const bool alone = mine.hi - mine.lo == 1;      // one key has the weight 1 whatever its score is: no gradient, and no rounding of one
     const int start = tile * AT_ROWS + wave * AT_BLOCK;
     at_wait_for_all();
-    at_store<D>(&lds[0][0][0] + wave * AT_BLOCK * D * 2, a.grad_q.at(start, head), a.grad_q.token, a.tokens - start, a.dim, dq, lost ? sc_nan() : a.score.scale, empty);
+    at_store<D>(&lds[0][0][0] + wave * AT_BLOCK * D * 2, a.grad_q.at(start, head), a.grad_q.token, a.tokens - start, a.dim, dq, lost ? sc_nan() : alone ? 0.0f : a.score.scale, empty);
 }
 
 // Of keys and values: a workgroup has 128 of one head, and goes through the queries of all the heads that read it.
-template <int D, int FORM, bool SLOPES>
+template <int D, int FORM, bool SLOPES, bool FINE>
 __global__ void __launch_bounds__(AT_TPB, 2) rb_attend_grad_kv_kernel(AttentionArgs a)
 {
     constexpr int ROWS = AT_BLOCK;                  // queries at a time
@@ -957,7 +1000,16 @@ __global__ void __launch_bounds__(AT_TPB, 2) rb_attend_grad_kv_kernel(AttentionA
             }
             const at_bf8 p[2] = {at_pack(s, 0), at_pack(s, 1)}, ds[2] = {at_pack(dp, 0), at_pack(dp, 1)};
             at_add<D, 2, false>(dv, p, reads, gt, 0);
+            if constexpr (FINE) {
+                const at_bf8 rest[2] = {at_pack_rest(s, p[0], 0), at_pack_rest(s, p[1], 1)};
+                at_add<D, 2, false>(dv, rest, reads, gt, 0);
+                __builtin_amdgcn_sched_barrier(0);
+            }
             at_add<D, 2, false>(dk, ds, reads, qt, 0);
+            if constexpr (FINE) {
+                const at_bf8 rest[2] = {at_pack_rest(dp, ds[0], 0), at_pack_rest(dp, ds[1], 1)};
+                at_add<D, 2, false>(dk, rest, reads, qt, 0);
+            }
         }
     };
 
@@ -996,17 +1048,23 @@ __global__ void __launch_bounds__(AT_TPB, 2) rb_attend_grad_kv_kernel(AttentionA
         first = next;
     }
     const bool empty = mine.lo >= mine.hi;
+    bool alone = false;                             // (the key's only query sees nothing else, see there)
+    if (mine.hi - mine.lo == 1) {
+        const Span sees = a.spans[row].sees;
+        alone = sees.hi - sees.lo == 1;
+    }
+    const float factor = lost ? sc_nan() : alone ? 0.0f : a.score.scale;
     if (a.sums) {
         if (row >= a.tokens) return;
         float* const to = a.sums + ((int64_t)share * a.tokens + row) * (2 * D);
-        at_store_sum<D>(to, dk, lost ? sc_nan() : a.score.scale, empty);
+        at_store_sum<D>(to, dk, factor, empty);
         at_store_sum<D>(to + D, dv, lost ? sc_nan() : 1.0f, empty);
         return;
     }
     const int start = tile * AT_ROWS + wave * AT_BLOCK;
     char* const through = &own[0][0] + wave * AT_BLOCK * D * 2;
     at_wait_for_all();
-    at_store<D>(through, a.grad_k.at(start, kv), a.grad_k.token, a.tokens - start, a.dim, dk, lost ? sc_nan() : a.score.scale, empty);
+    at_store<D>(through, a.grad_k.at(start, kv), a.grad_k.token, a.tokens - start, a.dim, dk, factor, empty);
     at_store<D>(through, a.grad_v.at(start, kv), a.grad_v.token, a.tokens - start, a.dim, dv, lost ? sc_nan() : 1.0f, empty);
 }
 

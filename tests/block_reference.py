@@ -185,6 +185,8 @@ def attend_grad(q, k, v, out, lse, grad_out, scale, cap, slopes, mask):
     off_w = rounded(p, off_p)
     off_of_q = rounded(ds.abs() + aside, off_ds + off_aside) + rounded(aside, off_aside)
     off_of_k = rounded(ds, off_ds)
+    # ... as the sum of what was rounded, which the roundings move by no more than all of them, times p k
+    off_of_q = off_of_q + (1 + BF16_HALF) * rounded(p * slope, off_p * slope + off_slope * p + p * slope) * (rounded(ds.abs() + aside, off_ds + off_aside) - off_ds).sum(2, keepdim=True)
     many = (tokens * heads + 16) * u
     def joined(x):
         return x.unflatten(1, (kv, heads // kv)).sum(2)

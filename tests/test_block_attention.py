@@ -97,6 +97,75 @@ def test_documents_prefixes_and_gaps(causal, prefix, gaps, cap, slopes, dim):
     check(*tensors(317, 4, 2, dim, seed=5), MANY, lengths, prefixes, causal, cap, slopes)
 
 
+@pytest.mark.parametrize("dim", [40, 64, 72, 128])
+@pytest.mark.parametrize("slopes", [False, True])
+@pytest.mark.parametrize("causal,prefixes,lengths", [(True, None, None), (False, None, [260, 0, 150]), (True, [70, 5, 400], None)])
+def test_capped_scores_of_long_documents(causal, prefixes, lengths, slopes, dim):
+    """Documents of 128 positions and more in the mean have a form of capped scores of their own (up to a cap of 32)."""
+    for cap in (3.0, 32.0):
+        check(*tensors(431, 4, 2, dim, seed=6), [0, 270, 271, 431], lengths, prefixes, causal, cap, slopes)
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("cap", [0.0, 2.0, 30.0, 100.0])
+def test_one_key_is_taken_as_it_is(cap, dim):
+    """Where a position sees nothing but itself, out is v and lse is the score: a few roundings of the score away, not of the cap."""
+    tokens, heads, scale = 41, 2, dim ** -0.5
+    q, k, v, _ = tensors(tokens, heads, heads, dim, seed=9)
+    a = rb.DocumentAttention(heads, dim, max_tokens=tokens, cap=cap)
+    got = a.forward(q, k, v, documents(list(range(tokens + 1))))
+    assert torch.equal(got.out, v)
+    mask = torch.eye(tokens, dtype=torch.bool)
+    q64, k64 = ref.to64(q), ref.to64(k)
+    plain, _, off = ref.scores(q64, k64, scale, 0.0, None, mask)
+    at = range(tokens)
+    s, off = plain[:, at, at], off[:, at, at]
+    want = cap * torch.tanh(s / cap) if cap else s
+    # (the cap's slope is at most 1; tanh and its factors: 16 roundings)
+    assert ((ref.to64(got.lse) - want).abs() <= off + 16 * ref.F32_HALF * want.abs()).all()
+
+
+@pytest.mark.parametrize("slopes", [False, True])
+@pytest.mark.parametrize("heads,kv", [(2, 2), (8, 2)])
+def test_one_key_has_no_gradient(heads, kv, slopes):
+    """Documents of one position: its weight is 1 whatever its score is, so q and k have gradients of 0, and v that of out."""
+    tokens, dim = 9, 128
+    q, k, v, d = tensors(tokens, heads, kv, dim, seed=2)
+    a = rb.DocumentAttention(heads, dim, kv, max_tokens=tokens)
+    docs, low = documents(list(range(tokens + 1))), slopes_of(heads) if slopes else None
+    got = a.forward(q, k, v, docs, slopes=low)
+    grad_q, grad_k, grad_v = a.grad(q, k, v, docs, got.out, got.lse, d, slopes=low)
+    assert (grad_q == 0).all() and (grad_k == 0).all()
+    want = ref.to64(d).unflatten(1, (kv, heads // kv)).sum(2)
+    # (weights of 1 within what lse is off by, a sum of some heads, a rounding)
+    size = ref.to64(d).abs().unflatten(1, (kv, heads // kv)).sum(2)
+    assert ((ref.to64(grad_v) - want).abs() <= want.abs() * ref.BF16_HALF + size * (ref.BF16_HALF + 2.0 ** -16)).all()
+    q[4, 1, 5] = NAN
+    got = a.forward(q, k, v, docs, slopes=low)
+    grad_q, grad_k, _ = a.grad(q, k, v, docs, got.out, got.lse, d, slopes=low)
+    assert grad_q[4, 1].isnan().all() and (grad_q[[0, 3, 5, 8]] == 0).all() and (grad_k[[0, 3, 5, 8]] == 0).all()
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("small", [1, 8])
+def test_infinities_in_tiles_that_are_seen_whole(small, dim):
+    """One long document, alone or with some of one position behind it (the forms for short ones): who sees an infinity has it, and nothing else is changed."""
+    tokens = 256 + small
+    q, k, v, _ = tensors(tokens, 2, 2, dim, seed=4, layout="own")
+    a = rb.DocumentAttention(2, dim, max_tokens=tokens, causal=False)
+    docs = documents([0] + list(range(256, tokens + 1)))
+    want = a.forward(q, k, v, docs).out.clone()
+    v[5, 0, 3] = INF
+    v[70, 1, 4] = -INF
+    v[71, 1, 5] = NAN
+    got = a.forward(q, k, v, docs).out
+    want[:256, 0, 3] = INF
+    want[:256, 1, 4] = -INF
+    assert got[:256, 1, 5].isnan().all()
+    got[:256, 1, 5] = want[:256, 1, 5]
+    assert torch.equal(got, want)
+
+
 def test_no_documents_and_documents_that_are_all_empty():
     q, k, v, d = tensors(70, 2, 2, 64)
     check(q, k, v, d, [0])
