@@ -94,16 +94,18 @@ hipError_t norm_forward(const NormArgs& a, hipStream_t st)
 
 template <int N> using Int = std::integral_constant<int, N>;
 
-// Lanes of a row and pieces of a lane, by the row's length, which ends in the last part: `of` is called with both.
+// Lanes of a row and pieces of a lane, by the row's length, which ends in the last part: `of` is called with both.  Few lanes have few exchanges to a sum (2^25
+// numbers of bfloat16 with residual and dropout: rows of 256 55 us with 16 lanes and 109 with 64, of 512 53 with 32 and 57 with 64), many have few
+// registers to a lane (2048: 57 with 128, 64 with 64; 8192: 53 with 512 and 70 with 256).
 template <typename Of>
 auto forward_by_width(int32_t width, const Of& of)
 {
     if (width <= 128) return of(Int<16>(), Int<1>());
     if (width <= 256) return of(Int<16>(), Int<2>());
-    if (width <= 512) return of(Int<64>(), Int<1>());
+    if (width <= 512) return of(Int<32>(), Int<2>());
     if (width <= 1024) return of(Int<64>(), Int<2>());
     if (width <= 1536) return of(Int<64>(), Int<3>());
-    if (width <= 2048) return of(Int<64>(), Int<4>());
+    if (width <= 2048) return of(Int<128>(), Int<2>());
     if (width <= 4096) return of(Int<256>(), Int<2>());
     if (width <= 6144) return of(Int<256>(), Int<3>());
     if (width <= 8192) return of(Int<512>(), Int<2>());
@@ -111,17 +113,20 @@ auto forward_by_width(int32_t width, const Of& of)
     if (width <= 24576) return of(Int<1024>(), Int<3>());
     return of(Int<1024>(), Int<4>());
 }
-// The gradients' sums and rows ahead take more registers: fewer pieces of a lane, of binary32 all the more.
+// The gradients' sums and rows ahead take more registers: fewer pieces of a lane, of binary32 all the more.  (The same 2^25 numbers: rows of 384 78 us with 16
+// lanes and 135 with 64; 512 81 with 32 and 108 with 64; 1536 80 with 64 and 141 with 256; 2048 84 with 128, 115 with 256 and 117 with 64; 8192 86 with 512
+// and 125 with 256.)
 template <typename Of>
 auto grad_by_width(int32_t width, const Of& of)
 {
     if (width <= 128) return of(Bf16(), Int<16>(), Int<1>());
     if (width <= 256) return of(Bf16(), Int<16>(), Int<2>());
     if (width <= 384) return of(Bf16(), Int<16>(), Int<3>());
-    if (width <= 512) return of(Bf16(), Int<64>(), Int<1>());
+    if (width <= 512) return of(Bf16(), Int<32>(), Int<2>());
+    if (width <= 768) return of(Bf16(), Int<32>(), Int<3>());
     if (width <= 1024) return of(Bf16(), Int<64>(), Int<2>());
     if (width <= 1536) return of(Bf16(), Int<64>(), Int<3>());
-    if (width <= 2048) return of(Bf16(), Int<256>(), Int<1>());
+    if (width <= 2048) return of(Bf16(), Int<128>(), Int<2>());
     if (width <= 4096) return of(Bf16(), Int<256>(), Int<2>());
     if (width <= 6144) return of(Bf16(), Int<256>(), Int<3>());
     if (width <= 8192) return of(Bf16(), Int<512>(), Int<2>());
@@ -135,9 +140,9 @@ auto grad_by_width_wide(int32_t width, const Of& of)
 {
     if (width <= 128) return of(float(), Int<16>(), Int<1>());
     if (width <= 256) return of(float(), Int<16>(), Int<2>());
-    if (width <= 512) return of(float(), Int<64>(), Int<1>());
+    if (width <= 512) return of(float(), Int<32>(), Int<2>());
     if (width <= 1024) return of(float(), Int<64>(), Int<2>());
-    if (width <= 2048) return of(float(), Int<256>(), Int<1>());
+    if (width <= 2048) return of(float(), Int<128>(), Int<2>());
     if (width <= 4096) return of(float(), Int<256>(), Int<2>());
     if (width <= 8192) return of(float(), Int<512>(), Int<2>());
     if (width <= 12288) return of(float(), Int<512>(), Int<3>());
@@ -303,12 +308,14 @@ namespace {
 // Workgroups that the gradients of keys and values are cut into at least.
 constexpr int64_t AT_KEY_GROUPS = 512, AT_MAX_PARTS = 16;
 
-// Into how many parts the queries of a head of keys are cut: until all units have two workgroups; and twice as many where documents are long and causal
-// (by their mean length), since the first keys' workgroups take twice the mean.
+// Into how many parts the queries of a head of keys are cut: until all units have two workgroups, and twice as many where some have much more to do than others.
+// That is so for the first keys of what is causal, and in documents of several lengths.  (Gradients of 16 heads of 128 to 8, once and twice as many: one causal
+// document of 8192 1395 and 1150 us, not causal 2065 and 2100; 24 documents of any lengths in 8192 260 and 228, 8 of them 574 and 433, not causal 687 and
+// 515.  The price is paid by documents of the same length, 24 of 341: 157 and 183, and by short ones, which have no such differences.)
 inline int key_parts(const rb_attention* a, int64_t tokens, int64_t documents)
 {
     const int64_t groups = (tokens + AT_ROWS - 1) / AT_ROWS * a->kv_heads;
-    const int64_t wanted = a->causal && tokens >= documents * 2048 ? 2 * AT_KEY_GROUPS : AT_KEY_GROUPS;
+    const int64_t wanted = (a->causal || documents > 1) && tokens >= documents * 160 ? 2 * AT_KEY_GROUPS : AT_KEY_GROUPS;
     // (a part of less than 4 tiles of queries would not be worth its sums)
     const int64_t most = std::min<int64_t>(AT_MAX_PARTS, std::max<int64_t>(1, tokens / std::max<int64_t>(documents, 1) * (a->heads / a->kv_heads) / (4 * AT_BLOCK)));
     return (int)std::min<int64_t>(most, (wanted + groups - 1) / groups);
@@ -363,7 +370,9 @@ AttentionArgs attention_args(const rb_attention* a, int form, const rb_heads* q,
     g.group = a->heads / a->kv_heads;
     g.tiles = (int32_t)((tokens + AT_ROWS - 1) / AT_ROWS);
     g.inner = inner_heads(a->heads, g.group);
-    g.ranked = d->count > 1 && tokens >= 192 * d->count && g.tiles > 1 && g.tiles <= AT_RANKED;
+    // (documents of any lengths in 8192 positions, 16 heads of 128: 24 of them, forward 59 -> 58 us and gradients 267 -> 258, 42 of them 57.5 -> 53 and 245 -> 234; 64
+    // of 128 each lose by it: 30 -> 35 and 87 -> 95)
+    g.ranked = d->count > 1 && tokens >= 160 * d->count && g.tiles > 1 && g.tiles <= AT_RANKED;
     return g;
 }
 

@@ -232,10 +232,8 @@ __device__ __forceinline__ void nm_sum(float (&v)[N], float* places)
         v[i] += sc_xor<2>(v[i]);
         v[i] += sc_xor<4>(v[i]);
         v[i] += sc_xor<8>(v[i]);
-        if (LANES >= 64) {
-            v[i] += sc_xor<16>(v[i]);
-            v[i] += sc_xor<32>(v[i]);
-        }
+        if (LANES >= 32) v[i] += sc_xor<16>(v[i]);
+        if (LANES >= 64) v[i] += sc_xor<32>(v[i]);
     }
     if (LANES > 64) {
         constexpr int WAVES = LANES / 64;
@@ -247,7 +245,7 @@ __device__ __forceinline__ void nm_sum(float (&v)[N], float* places)
         for (int i = 0; i < N; ++i) {
             v[i] = 0.0f;
 #pragma unroll
-            for (int w = 0; w < WAVES; ++w) v[i] += places[w * N + i];
+            for (int w = 0; w < WAVES; ++w) v[i] += places[(threadIdx.x / LANES * WAVES + w) * N + i];
         }
     }
 }
