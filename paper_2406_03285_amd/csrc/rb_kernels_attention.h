@@ -542,6 +542,12 @@ __device__ __forceinline__ void at_store_sum(float* row, const at_acc (&v)[D / 3
 
 // ---- forward -------------------------------------------------------------------
 
+// A workgroup has 128 queries of one head, 32 a wavefront, and goes through the keys that they see, 64 at a time, with the next 64 keys and values on their
+// way into the other half of LDS.  One pass: p = e^(s - m) with the running maximum m, l the sum of p, o the sum of p v; o and l are scaled where m
+// has grown by more than 2^8.  Two workgroups a unit (256 registers a lane, 64 KB of LDS): while a wavefront makes its softmax, another one multiplies.
+// Bound by the matrix instructions and the softmax's vector instructions beside them: 16 heads of 128 that see all of 8192 positions 527 us, 1.04 PFLOP/s (a large
+// product of the library runs at 1.3); one document of 16384 with 8 heads 620 us causal, 665 with capped scores; 24 documents of any lengths in 8192 positions
+// 58 us, half of it starts, ends and tiles that are masked in part.  64 documents of 128 30 us.
 template <int D, int FORM, bool SLOPES, bool FINE>
 __global__ void __launch_bounds__(AT_TPB, 2) rb_attend_kernel(AttentionArgs a)
 {
@@ -735,7 +741,7 @@ __global__ void __launch_bounds__(AT_TPB, 2) rb_attend_kernel(AttentionArgs a)
 // ---- gradients -----------------------------------------------------------------
 
 // What the gradients need: the positions' intervals, and of every row of every head lse in base 2 and the sum of grad_out * out.  A workgroup has 16 positions, 16
-// lanes each, and goes through its part of the heads, four at a time.
+// lanes each, and goes through its part of the heads, four at a time.  (Reads both once: 8192 positions of 16 heads of 128 20 us, 3.3 TB/s.)
 constexpr int AT_POSITIONS = AT_TPB / 16, AT_ONCE = 4;
 __global__ void __launch_bounds__(AT_TPB) rb_attend_delta_kernel(AttentionArgs a, float* lse2)
 {
@@ -795,6 +801,9 @@ __device__ __forceinline__ void at_weight(const ScoreOf& of, float product, floa
 // ds k: the gradient is the sum of p (dp - first - off) k.  The keys' kernel gets the better delta.  (A fourth product beside three, that shares its operand; a
 // pass of its own over the keys would be two.)  What is taken away is not the sum of ds itself but that of what they were rounded to: then of a rounding's
 // error e the gradient gets e (k - mean of k) and not e k, where keys may lie around a mean that is larger than what they differ by.
+//
+// The queries' gradients of the results stay in LDS (q is in registers), 32 keys at a time leave room for two workgroups a unit.  One document of 8192, 16 heads of
+// 128: 550 us, four products at 1.0 PFLOP/s.
 template <int D, int FORM, bool SLOPES, bool FINE>
 __global__ void __launch_bounds__(AT_TPB, 2) rb_attend_grad_q_kernel(AttentionArgs a)
 {
@@ -922,7 +931,9 @@ __global__ void __launch_bounds__(AT_TPB, 2) rb_attend_grad_q_kernel(AttentionAr
     at_store<D>(&lds[0][0][0] + wave * AT_BLOCK * D * 2, a.grad_q.at(start, head), a.grad_q.token, a.tokens - start, a.dim, dq, lost ? sc_nan() : alone ? 0.0f : a.score.scale, empty);
 }
 
-// Of keys and values: a workgroup has 128 of one head, and goes through the queries of all the heads that read it.
+// Of keys and values: a workgroup has 128 of one head, and goes through the queries of all the heads that read it, or of a part of these (key_parts) whose sums
+// then go to memory unrounded and are added up by the next kernel, in the same order every time.  One document of 8192, 16 heads of 128 to 8: 560 us, four
+// products at 1.0 PFLOP/s, and 25 us for the parts' sums.
 template <int D, int FORM, bool SLOPES, bool FINE>
 __global__ void __launch_bounds__(AT_TPB, 2) rb_attend_grad_kv_kernel(AttentionArgs a)
 {
@@ -1068,7 +1079,8 @@ __global__ void __launch_bounds__(AT_TPB, 2) rb_attend_grad_kv_kernel(AttentionA
     at_store<D>(through, a.grad_v.at(start, kv), a.grad_v.token, a.tokens - start, a.dim, dv, lost ? sc_nan() : 1.0f, empty);
 }
 
-// Gradients of keys and values from the parts' sums: a thread has four numbers of a row of one head.
+// Gradients of keys and values from the parts' sums: a thread has four numbers of a row of one head.  Bound by what it reads (two parts of 8192 rows of 8 heads of
+// 128 in binary32, 134 MB, 25 us).
 template <int D>
 __global__ void __launch_bounds__(AT_TPB) rb_attend_join_kernel(AttentionArgs a)
 {

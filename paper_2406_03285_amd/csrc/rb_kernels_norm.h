@@ -180,6 +180,8 @@ struct DropoutArgs {
     Drop drop;
 };
 
+// A thread has eight numbers, that is one draw: ten rounds of two multiplications hide behind the reading.  Short rows share a workgroup; long grids go round.
+// Bound by HBM: 8191 x 10007 bfloat16 63.5 us, 5.2 TB/s, what a copy reaches.  Of 128 x 192 binary32 the launch (2.9 us of a call's 5.4).
 template <typename T>
 __global__ void __launch_bounds__(NM_TPB) rb_dropout_kernel(DropoutArgs a)
 {
@@ -275,6 +277,8 @@ constexpr int nm_waves(int lanes, int parts)
 // A workgroup goes through rows that are the grid's width apart; the next row is on its way while one is worked on.  What is kept of a row is as it lies in
 // memory (the sum is rounded to that type anyway).  SUMMED: there is a residual or dropout.  The sum is stored when all of the row has been read (a lane that
 // has numbers of another one reads them in its own time).
+// Bound by HBM: 8192 x 8192 bfloat16 with residual and dropout 111 us (4.85 TB/s; 152 before the next row was on its way meanwhile), 5120 x 2048 binary32 alone 17.3 us
+// (4.85 TB/s).  One row: the launch and one chain of reading, sums and writing, 3.0 us of a call's 6.3.
 template <typename T, int LANES, int PARTS, bool SUMMED>
 __global__ void __launch_bounds__(nm_threads(LANES), nm_waves<T>(LANES, PARTS)) rb_norm_kernel(NormArgs a)
 {
@@ -398,6 +402,8 @@ struct NormGradArgs {
 
 // As forward; the gradients of the next row's y and that row are on their way while one is worked on.  SUMS: the weights' gradients are summed on the way (of rows
 // that leave room for the sums).
+// Bound by HBM where rows are of 1024 to 8192: 16384 x 4096 bfloat16 with residual and dropout 140 us of the call's 150 (4.8 TB/s).  Where there are few or
+// short rows, by the sums between lanes (65536 x 512 81 us, 4.1 TB/s); of more than 8192, by the registers (4096 x 16384 226 us, 3 TB/s).
 template <typename T, int LANES, int PARTS>
 __global__ void __launch_bounds__(nm_threads(LANES), LANES > 512 ? 4 : NM_SUM_WAVES) rb_norm_grad_kernel(NormGradArgs a)
 {
@@ -558,7 +564,8 @@ __global__ void __launch_bounds__(NM_TPB) rb_norm_columns_kernel(NormGradArgs a)
         }
 }
 
-// The workgroups' sums together: 64 columns of a workgroup, 16 parts of the groups for each.
+// The workgroups' sums together: 64 columns of a workgroup, 16 parts of the groups for each.  (4096 columns of 512 groups 9.5 us, 128 workgroups that wait for
+// memory; kept with the first kernel's atomics instead, results would depend on the order.)
 template <typename W>
 __global__ void __launch_bounds__(1024) rb_norm_join_kernel(const float* sums, int groups, int width, W* grad_weight, W* grad_bias)
 {
