@@ -544,9 +544,11 @@ __device__ __forceinline__ void at_store_sum(float* row, const at_acc (&v)[D / 3
 
 // A workgroup has 128 queries of one head, 32 a wavefront, and goes through the keys that they see, 64 at a time, with the next 64 keys and values on their
 // way into the other half of LDS.  One pass: p = e^(s - m) with the running maximum m, l the sum of p, o the sum of p v; o and l are scaled where m
-// has grown by more than 2^8.  Two workgroups a unit (256 registers a lane, 64 KB of LDS): while a wavefront makes its softmax, another one multiplies.
-// Bound by the matrix instructions and the softmax's vector instructions beside them: 16 heads of 128 that see all of 8192 positions 527 us, 1.04 PFLOP/s (a large
-// product of the library runs at 1.3); one document of 16384 with 8 heads 620 us causal, 665 with capped scores; 24 documents of any lengths in 8192 positions
+// has grown by more than 2^8.  Two workgroups a unit (256 registers a lane, 64 KB of LDS): while a wavefront makes its softmax, another one multiplies.  That
+// they do not do both at the same time is what the wavefronts' priorities are for: scores and softmax go before the second product (not causal 506 us without,
+// 482 with both products before the softmax, 474 so; capped scores 643, 644 and 566).
+// Bound by the matrix instructions and the softmax's vector instructions beside them: 16 heads of 128 that see all of 8192 positions 494 us, 1.11 PFLOP/s (a large
+// product of the library runs at 1.3); one document of 16384 with 8 heads 574 us causal, 604 with capped scores; 24 documents of any lengths in 8192 positions
 // 58 us, half of it starts, ends and tiles that are masked in part.  64 documents of 128 30 us.
 template <int D, int FORM, bool SLOPES, bool FINE>
 __global__ void __launch_bounds__(AT_TPB, 2) rb_attend_kernel(AttentionArgs a)
@@ -598,6 +600,7 @@ __global__ void __launch_bounds__(AT_TPB, 2) rb_attend_kernel(AttentionArgs a)
     float m = sc_neg_inf(), l = 0.0f;               // maximum (base 2), and this lane's part of the sum
 
     auto step = [&](bool masked, int first, const char* kt, const char* vt) {
+        __builtin_amdgcn_s_setprio(1);              // (see above)
         at_acc s[2]{};
         at_bf8 f[2][2][2];                          // pieces of the keys, two ahead
 #pragma unroll
@@ -676,6 +679,7 @@ __global__ void __launch_bounds__(AT_TPB, 2) rb_attend_kernel(AttentionArgs a)
             p[2 * b] = at_pack(s[b], 0);
             p[2 * b + 1] = at_pack(s[b], 1);
         }
+        __builtin_amdgcn_s_setprio(0);
         at_add<D, 4, true>(o, p, reads, vt, 0);
         if constexpr (FINE) {
 #pragma unroll
@@ -840,6 +844,7 @@ __global__ void __launch_bounds__(AT_TPB, 2) rb_attend_grad_q_kernel(AttentionAr
     auto step = [&](bool masked, int first, const char* kt, const char* vt) {
         const int from = mine.lo - first, to = mine.hi - first;
         const float away = (float)(row - first - 4 * half);
+        __builtin_amdgcn_s_setprio(0);
         at_acc s{}, dp{};
 #pragma unroll
         for (int n = 0; n < D / 16; ++n) {
@@ -873,6 +878,7 @@ __global__ void __launch_bounds__(AT_TPB, 2) rb_attend_grad_q_kernel(AttentionAr
             if (FORM != AT_PLAIN && !FINE) by -= s[e];
         }
         const at_bf8 f[2] = {at_pack(s, 0), at_pack(s, 1)}, g[2] = {at_pack(w, 0), at_pack(w, 1)};
+        __builtin_amdgcn_s_setprio(1);              // (as in the forward pass: wavefronts take turns)
         if constexpr (!FINE) by = at_sum(f[1], at_sum(f[0], by));
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
@@ -977,6 +983,7 @@ __global__ void __launch_bounds__(AT_TPB, 2) rb_attend_grad_kv_kernel(AttentionA
         const int from = mine.lo - first, to = mine.hi - first;
         const float away = (float)(row - first - 4 * half);
         {
+            __builtin_amdgcn_s_setprio(0);
             at_acc s{}, dp{};
 #pragma unroll
             for (int n = 0; n < D / 16; ++n) {
@@ -1010,6 +1017,7 @@ __global__ void __launch_bounds__(AT_TPB, 2) rb_attend_grad_kv_kernel(AttentionA
                 }
             }
             const at_bf8 p[2] = {at_pack(s, 0), at_pack(s, 1)}, ds[2] = {at_pack(dp, 0), at_pack(dp, 1)};
+            __builtin_amdgcn_s_setprio(1);
             at_add<D, 2, false>(dv, p, reads, gt, 0);
             if constexpr (FINE) {
                 const at_bf8 rest[2] = {at_pack_rest(s, p[0], 0), at_pack_rest(s, p[1], 1)};
