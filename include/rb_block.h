@@ -129,7 +129,7 @@ int rb_attention_query(const rb_attention *a, size_t *workspace_bytes);
 int rb_attention_bind(rb_attention *a, void *workspace);
 
 /* Rows of heads on the device: head h of position t begins t * token_stride + h * head_stride elements behind `data`.  All are multiples of 16 bytes; strides
- * are not negative, of what is written at least head_dim, and token_stride is at most 2^26. */
+ * are not negative, token_stride is at most 2^26; what is written lies row by row or head by head, no two rows of heads overlap. */
 typedef struct rb_heads {
     void *data;
     int64_t token_stride, head_stride;

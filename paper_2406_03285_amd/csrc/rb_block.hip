@@ -329,11 +329,16 @@ inline int inner_heads(int64_t heads, int64_t group)
     return (int)(of_die % group == 0 ? group : group % of_die == 0 ? of_die : 1);
 }
 
-bool heads_fit(const rb_attention* a, const rb_heads* t, bool written)
+bool heads_fit(const rb_heads* t)
 {
     if (!t || !t->data || !aligned(t->data, 16) || t->token_stride % 8 != 0 || t->head_stride % 8 != 0) return false;
-    if (t->token_stride < 0 || t->head_stride < 0 || t->token_stride > AT_MAX_STRIDE || t->head_stride > (int64_t(1) << 48)) return false;
-    return !written || (t->token_stride >= a->dim && t->head_stride >= a->dim);
+    return t->token_stride >= 0 && t->head_stride >= 0 && t->token_stride <= AT_MAX_STRIDE && t->head_stride <= (int64_t(1) << 48);
+}
+// What is written: no two of its rows may share a number.
+bool heads_apart(const rb_attention* a, const rb_heads* t, int64_t tokens, int64_t heads)
+{
+    if (!heads_fit(t) || t->token_stride < a->dim || t->head_stride < a->dim) return false;
+    return tokens <= 1 || heads <= 1 || t->token_stride >= (heads - 1) * t->head_stride + a->dim || t->head_stride >= (tokens - 1) * t->token_stride + a->dim;
 }
 HeadRows rows_of(const rb_heads* t) { return HeadRows{static_cast<Bf16*>(t->data), t->token_stride, t->head_stride}; }
 
@@ -444,7 +449,7 @@ int rb_attention_forward(rb_attention* a, const rb_heads* q, const rb_heads* k, 
                          const float* slopes, const rb_heads* out, float* lse, void* hip_stream)
 {
     if (!a || tokens < 0 || tokens > a->max_tokens || !documents_fit(documents) || !aligned(slopes, 4) || !aligned(lse, 4)) return RB_EINVAL;
-    if (!heads_fit(a, q, false) || !heads_fit(a, k, false) || !heads_fit(a, v, false) || !heads_fit(a, out, true)) return RB_EINVAL;
+    if (!heads_fit(q) || !heads_fit(k) || !heads_fit(v) || !heads_apart(a, out, tokens, a->heads)) return RB_EINVAL;
     if (!a->ws) return RB_ESTATE;
     if (tokens == 0) return RB_OK;
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
@@ -469,8 +474,8 @@ int rb_attention_grad(rb_attention* a, const rb_heads* q, const rb_heads* k, con
                       const rb_heads* grad_v, void* hip_stream)
 {
     if (!a || tokens < 0 || tokens > a->max_tokens || !documents_fit(documents) || !aligned(slopes, 4) || !lse || !aligned(lse, 4)) return RB_EINVAL;
-    if (!heads_fit(a, q, false) || !heads_fit(a, k, false) || !heads_fit(a, v, false) || !heads_fit(a, out, false) || !heads_fit(a, grad_out, false)) return RB_EINVAL;
-    if (!heads_fit(a, grad_q, true) || !heads_fit(a, grad_k, true) || !heads_fit(a, grad_v, true)) return RB_EINVAL;
+    if (!heads_fit(q) || !heads_fit(k) || !heads_fit(v) || !heads_fit(out) || !heads_fit(grad_out)) return RB_EINVAL;
+    if (!heads_apart(a, grad_q, tokens, a->heads) || !heads_apart(a, grad_k, tokens, a->kv_heads) || !heads_apart(a, grad_v, tokens, a->kv_heads)) return RB_EINVAL;
     if (!a->ws) return RB_ESTATE;
     if (tokens == 0) return RB_OK;
     hipStream_t st = static_cast<hipStream_t>(hip_stream);

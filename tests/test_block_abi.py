@@ -116,7 +116,7 @@ def test_attention_calls_refuse():
     bad_docs = (None, rb.RbDocuments(None, P, P, 5), rb.RbDocuments(P + 4, P, P, 5), rb.RbDocuments(P, P + 4, P, 5), rb.RbDocuments(P, P, P + 4, 5),
                 rb.RbDocuments(P, P, P, -1), rb.RbDocuments(P, P, P, rb.RB_MAX_DOCUMENTS + 1))
     read = (None, heads(None), heads(P + 8), heads(P, 508), heads(P, 512, 60), heads(P, -512), heads(P, 512, -64), heads(P, 1 << 40), heads(P, 512, 1 << 50))
-    written = read + (heads(P, 56), heads(P, 512, 56), heads(P, 0))
+    written = read + (heads(P, 56), heads(P, 512, 56), heads(P, 0), heads(P, 64, 64), heads(P, 72, 64), heads(P, 64, 9 * 64 - 8))
     good = dict(a=a, q=heads(P), k=heads(2 * P), v=heads(3 * P), tokens=10, documents=docs, slopes=P, out=heads(4 * P), lse=5 * P)
     assert rb.rb_attention_forward(*good.values(), STREAM) == rb.RB_ESTATE         # never bound
     refused(rb.rb_attention_forward, good, (
