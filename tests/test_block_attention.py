@@ -106,6 +106,15 @@ def test_capped_scores_of_long_documents(causal, prefixes, lengths, slopes, dim)
         check(*tensors(431, 4, 2, dim, seed=6), [0, 270, 271, 431], lengths, prefixes, causal, cap, slopes)
 
 
+@pytest.mark.parametrize("dim", [64, 72, 128])
+@pytest.mark.parametrize("cap,slopes", [(0.0, False), (0.0, True), (4.0, True), (50.0, False)])
+@pytest.mark.parametrize("causal,prefix,gaps", [(True, False, False), (True, True, True), (False, False, True), (False, False, False)])
+def test_longer_documents(causal, prefix, gaps, cap, slopes, dim):
+    """Documents of more than 160 positions in the mean, one of them of one position and one of none: tiles take turns by length."""
+    offsets = [0, 1, 330, 330, 690]
+    check(*tensors(700, 4, 2, dim, seed=8), offsets, [1, 300, 0, 355] if gaps else None, [0, 100, 7, 1000] if prefix else None, causal, cap, slopes)
+
+
 @pytest.mark.parametrize("dim", [64, 128])
 @pytest.mark.parametrize("cap", [0.0, 2.0, 30.0, 100.0])
 def test_one_key_is_taken_as_it_is(cap, dim):
@@ -123,6 +132,23 @@ def test_one_key_is_taken_as_it_is(cap, dim):
     want = cap * torch.tanh(s / cap) if cap else s
     # (the cap's slope is at most 1; tanh and its factors: 16 roundings)
     assert ((ref.to64(got.lse) - want).abs() <= off + 16 * ref.F32_HALF * want.abs()).all()
+
+
+@pytest.mark.parametrize("dim,heads,kv,cap", [(16, 4, 2, 0.0), (64, 2, 2, 30.0), (128, 3, 1, 0.0)])
+def test_short_documents_are_as_exact_as_their_results_rounding(dim, heads, kv, cap):
+    """In the mean: what p and ds are off by, 2^-17 of themselves, is nothing beside the results' 2^-9 (one in 2^15 of its square, and rounded to the other side
+    for as many); with p and ds in bfloat16 errors would be 1.4 times as large."""
+    offsets = [0, 2, 4, 9, 10, 26, 29, 60]
+    q, k, v, d = tensors(60, heads, kv, dim, seed=12)
+    a = rb.DocumentAttention(heads, dim, kv, max_tokens=60, cap=cap)
+    docs, mask, scale = documents(offsets), ref.seen(60, offsets), dim ** -0.5
+    got = a.forward(q, k, v, docs)
+    grads = a.grad(q, k, v, docs, got.out, got.lse, d)
+    q64, k64, v64, d64 = (ref.to64(x) for x in (q, k, v, d))
+    out, lse, _, _ = ref.attend(q64, k64, v64, scale, cap, None, mask)
+    want, _ = ref.attend_grad(q64, k64, v64, out, lse, d64, scale, cap, None, mask)
+    for name, have, exact in zip(("out", *"qkv"), (got.out, *grads), (out, *want)):
+        assert (ref.to64(have) - exact).norm() <= 1.05 * (exact.to(BF16).double() - exact).norm(), name
 
 
 @pytest.mark.parametrize("slopes", [False, True])
@@ -186,14 +212,17 @@ def test_large_and_small_scores(scale, cap, size):
     check(q, k, v, d, [0, 100, 130], scale=scale, cap=cap)
 
 
+@pytest.mark.parametrize("cap", [0.0, 20.0])
+@pytest.mark.parametrize("times", [1, 4])
 @pytest.mark.parametrize("dim", [64, 72, 128])
-def test_what_lies_in_masked_places_does_not_matter(dim):
+def test_what_lies_in_masked_places_does_not_matter(dim, times, cap):
     """NaN and infinities behind the documents, in gaps, in other documents and in positions to come; results as if they were 0."""
-    offsets, lengths = [0, 50, 130, 190], [40, 80, 55]
-    q, k, v, d = tensors(200, 2, 1, dim, layout="own")
-    a = rb.DocumentAttention(2, dim, 1, max_tokens=200)
+    n = times                                        # (documents of less and of more than 128 positions in the mean)
+    offsets, lengths = [0, 50 * n, 130 * n, 190 * n], [40 * n, 80 * n, 55 * n]
+    q, k, v, d = tensors(200 * n, 2, 1, dim, layout="own")
+    a = rb.DocumentAttention(2, dim, 1, max_tokens=200 * n, cap=cap)
     docs = documents(offsets, lengths)
-    nobody = ~ref.seen(200, offsets, lengths).any(1)
+    nobody = ~ref.seen(200 * n, offsets, lengths).any(1)
     want = a.forward(q, k, v, docs)
     grads = a.grad(q, k, v, docs, want.out, want.lse, d)
     for bad in (NAN, INF, -INF):
@@ -205,31 +234,31 @@ def test_what_lies_in_masked_places_does_not_matter(dim):
         for x, y in zip(a.grad(q2, k2, v2, docs, o2, want.lse, d2), grads):
             assert torch.equal(x, y)
         # the second document is not a number: the others do not know
-        others = torch.ones(200, dtype=torch.bool)
-        others[50:130] = False
+        others = torch.ones(200 * n, dtype=torch.bool)
+        others[50 * n:130 * n] = False
         q2, k2, v2, d2, o2 = (x.clone() for x in (q, k, v, d, want.out))
         for x in (q2, k2, v2, d2, o2):
-            x[50:130] = bad
+            x[50 * n:130 * n] = bad
         got = a.forward(q2, k2, v2, docs)
         assert torch.equal(got.out[others], want.out[others]) and torch.equal(got.lse[:, others], want.lse[:, others])
         for x, y in zip(a.grad(q2, k2, v2, docs, o2, want.lse, d2), grads):
             assert torch.equal(x[others], y[others])
         # one position of it: what lies before does not know, what lies behind and sees it does
         v2 = v.clone()
-        v2[100, 0, 3] = bad
+        v2[100 * n, 0, 3] = bad
         got = a.forward(q, k, v2, docs).out
-        assert torch.equal(got[:100], want.out[:100]) and torch.equal(got[130:], want.out[130:])
-        column = got[100:130, :, 3]
+        assert torch.equal(got[:100 * n], want.out[:100 * n]) and torch.equal(got[130 * n:], want.out[130 * n:])
+        column = got[100 * n:130 * n, :, 3]
         assert torch.isnan(column).all() if bad != bad else (column == bad).all()
         keep = [c for c in range(dim) if c != 3]
         assert torch.equal(got[:, :, keep], want.out[:, :, keep])
         q2, d2 = q.clone(), d.clone()                    # a query's row: the keys behind it do not know
-        q2[70, 1] = bad
-        d2[70, 1] = bad
+        q2[70 * n, 1] = bad
+        d2[70 * n, 1] = bad
         g = a.grad(q2, k, v, docs, want.out, want.lse, d2)
         for x, y in zip(g, grads):
-            assert torch.equal(x[71:], y[71:]) and torch.equal(x[:50], y[:50])
-        assert torch.equal(g[0][50:70], grads[0][50:70]) and not torch.isfinite(g[2][50:71].float()).any()
+            assert torch.equal(x[70 * n + 1:], y[70 * n + 1:]) and torch.equal(x[:50 * n], y[:50 * n])
+        assert torch.equal(g[0][50 * n:70 * n], grads[0][50 * n:70 * n]) and not torch.isfinite(g[2][50 * n:70 * n + 1].float()).any()
 
 
 def test_rows_that_are_not_numbers():

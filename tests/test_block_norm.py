@@ -75,7 +75,7 @@ def check(x, residual, drop, weight, bias, eps=1e-5):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
-@pytest.mark.parametrize("width", [1, 2, 7, 8, 9, 63, 64, 127, 128, 129, 200, 511, 512, 513, 1000, 1024, 1025, 1536, 1537, 2047, 2048, 2049, 4096, 4097, 5003, 6144, 6145,
+@pytest.mark.parametrize("width", [1, 2, 7, 8, 9, 63, 64, 127, 128, 129, 200, 257, 384, 385, 511, 512, 513, 767, 768, 769, 1000, 1024, 1025, 1536, 1537, 2047, 2048, 2049, 4096, 4097, 5003, 6144, 6145,
                                    8192, 8193, 10007, 12289, 16383, 16385, 24576, 24577, 32763, 32768])
 def test_rows_of_any_length(width, dtype):
     w, b = weights(width, F32)
@@ -111,13 +111,13 @@ def test_rows_that_lie_anyhow(pad, offset, dtype):
 
 @pytest.mark.parametrize("rows", [1, 15, 16, 17, 511, 513, 4099, 20011])
 def test_any_number_of_rows(rows):
-    for width in (24, 300):
+    for width in (24, 300, 700, 2000):
         w, b = weights(width, F32)
         check(make(rows, width, BF16), make(rows, width, BF16, seed=1), D, w, b)
 
 
 def test_many_rows_of_every_form():
-    for width, rows in ((1024, 3001), (2048, 2500), (4096, 1300), (8000, 700), (20000, 600)):
+    for width, rows in ((512, 9001), (700, 8003), (1024, 3001), (2048, 2500), (4096, 1300), (8000, 700), (20000, 600)):
         w, b = weights(width, F32)
         check(make(rows, width, F32), None, None, w, b)
 
