@@ -402,8 +402,8 @@ struct NormGradArgs {
 
 // As forward; the gradients of the next row's y and that row are on their way while one is worked on.  SUMS: the weights' gradients are summed on the way (of rows
 // that leave room for the sums).
-// Bound by HBM where rows are of 1024 to 8192: 16384 x 4096 bfloat16 with residual and dropout 140 us of the call's 150 (4.8 TB/s).  Where there are few or
-// short rows, by the sums between lanes (65536 x 512 81 us, 4.1 TB/s); of more than 8192, by the registers (4096 x 16384 226 us, 3 TB/s).
+// Bound by HBM where rows are of 1024 to 8192: 16384 x 4096 bfloat16 with residual and dropout 140 us of the call's 144 (4.8 TB/s).  Where there are few or
+// short rows, by the sums between lanes (65536 x 512 72 us, 4.7 TB/s; 65536 x 100 29 us, 2.3 TB/s); of more than 8192, by the registers (4096 x 16384 226 us, 3 TB/s).
 template <typename T, int LANES, int PARTS>
 __global__ void __launch_bounds__(nm_threads(LANES), LANES > 512 ? 4 : NM_SUM_WAVES) rb_norm_grad_kernel(NormGradArgs a)
 {
@@ -564,8 +564,8 @@ __global__ void __launch_bounds__(NM_TPB) rb_norm_columns_kernel(NormGradArgs a)
         }
 }
 
-// The workgroups' sums together: 64 columns of a workgroup, 16 parts of the groups for each.  (4096 columns of 512 groups 9.5 us, 128 workgroups that wait for
-// memory; kept with the first kernel's atomics instead, results would depend on the order.)
+// The workgroups' sums together: 64 columns of a workgroup, 16 parts of the groups for each, 16 groups on their way at a time (4096 columns of 512 groups 9.5 us
+// one by one, 4.5 so: 3.7 TB/s, mostly from the last cache).  Kept with the first kernel's atomics instead, results would depend on the order.
 template <typename W>
 __global__ void __launch_bounds__(1024) rb_norm_join_kernel(const float* sums, int groups, int width, W* grad_weight, W* grad_bias)
 {
@@ -574,8 +574,16 @@ __global__ void __launch_bounds__(1024) rb_norm_join_kernel(const float* sums, i
     if (!to) return;
     const int column = blockIdx.x * 64 + (threadIdx.x & 63), part = threadIdx.x / 64;
     float s = 0.0f;
-    if (column < width)
-        for (int g = part; g < groups; g += 16) s += sums[((int64_t)blockIdx.y * groups + g) * width + column];
+    if (column < width) {
+        const float* const from = sums + (int64_t)blockIdx.y * groups * width + column;
+        for (int first = part; first < groups; first += 16 * 16) {
+            float v[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) v[i] = from[(int64_t)min(first + 16 * i, groups - 1) * width];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s += first + 16 * i < groups ? v[i] : 0.0f;
+        }
+    }
     parts[part][threadIdx.x & 63] = s;
     __syncthreads();
     if (part != 0 || column >= width) return;
