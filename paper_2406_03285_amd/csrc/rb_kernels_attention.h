@@ -339,7 +339,7 @@ __device__ __forceinline__ uint64_t at_noted(const uint32_t (&noted)[2], int fro
 // All in base 2.  With r = 1 / (1 + e^2x), tanh x = 1 - 2 r to within 2^-22 (and its slope 4 r (1 - r)), so that a capped score is off by cap * 2^-22 at
 // most: less than what rounding e^score to bfloat16 puts in for caps of up to 32, where more is not worth it.  There the cap is also the maximum
 // that the softmax needs: e^(score - cap) is at least e^-64 for what lies next to a position, and its sums are normal numbers.  Larger caps have
-// scores that are exact near 0, too, and a running maximum.
+// scores that are exact near 0, too, and a running maximum.  (16384 positions, 8 heads of 128: a cap of 30 590 us and gradients 2335, one of 33 912 and 2785.)
 //
 // Short documents.  p and ds are rounded to bfloat16 for the products over positions.  The errors of many positions are as independent as those of the results'
 // own rounding, and as large.  Of a handful of positions they may be twice as large, so there (FINE) what the rounding left is multiplied too: an error
