@@ -339,7 +339,8 @@ __device__ __forceinline__ uint64_t at_noted(const uint32_t (&noted)[2], int fro
 // All in base 2.  With r = 1 / (1 + e^2x), tanh x = 1 - 2 r to within 2^-22 (and its slope 4 r (1 - r)), so that a capped score is off by cap * 2^-22 at
 // most: less than what rounding e^score to bfloat16 puts in for caps of up to 32, where more is not worth it.  There the cap is also the maximum
 // that the softmax needs: e^(score - cap) is at least e^-64 for what lies next to a position, and its sums are normal numbers.  Larger caps have
-// scores that are exact near 0, too, and a running maximum.  (16384 positions, 8 heads of 128: a cap of 30 590 us and gradients 2335, one of 33 912 and 2785.)
+// scores that are exact near 0, too, and a running maximum; a slope below 0 raises scores beyond any cap and has one as well.  (16384 positions, 8 heads of 128: a
+// cap of 30 590 us and gradients 2335, one of 33 912 and 2785.)
 //
 // Short documents.  p and ds are rounded to bfloat16 for the products over positions.  The errors of many positions are as independent as those of the results'
 // own rounding, and as large.  Of a handful of positions they may be twice as large, so there (FINE) what the rounding left is multiplied too: an error
@@ -597,7 +598,11 @@ __global__ void __launch_bounds__(AT_TPB, 2) rb_attend_kernel(AttentionArgs a)
     const Reads<D> reads;
     const uint32_t k_offset = bring.offset(a.k.token), v_offset = bring.offset(a.v.token);
     at_acc o[D / 32]{};
-    float m = sc_neg_inf(), l = 0.0f;               // maximum (base 2), and this lane's part of the sum
+    // capped scores need no maximum, but where a slope below 0 raises what is far away (16384 positions, 8 heads of 128, a cap of 30, slopes above 0: 584 us, with a
+    // maximum 736)
+    constexpr bool MAY_RISE = FORM == AT_CAPPED && SLOPES;
+    const bool moves = FORM != AT_CAPPED || (MAY_RISE && __builtin_amdgcn_readfirstlane(slope2 < 0.0f));
+    float m = moves ? sc_neg_inf() : 0.0f, l = 0.0f;               // maximum (base 2), and this lane's part of the sum
 
     auto step = [&](bool masked, int first, const char* kt, const char* vt) {
         __builtin_amdgcn_s_setprio(1);              // (see above)
@@ -647,7 +652,7 @@ __global__ void __launch_bounds__(AT_TPB, 2) rb_attend_kernel(AttentionArgs a)
                 }
         }
         float base = 0.0f;
-        if (FORM != AT_CAPPED) {
+        if (moves) {
             float most = sc_neg_inf();
 #pragma unroll
             for (int b = 0; b < 2; ++b)
@@ -673,7 +678,7 @@ __global__ void __launch_bounds__(AT_TPB, 2) rb_attend_kernel(AttentionArgs a)
         for (int b = 0; b < 2; ++b) {
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
-                s[b][e] = __builtin_amdgcn_exp2f(!SCORED ? fmaf(s[b][e], a.score.to_log2, -base) : FORM == AT_CAPPED ? s[b][e] : s[b][e] - base);
+                s[b][e] = __builtin_amdgcn_exp2f(!SCORED ? fmaf(s[b][e], a.score.to_log2, -base) : FORM == AT_CAPPED && !MAY_RISE ? s[b][e] : s[b][e] - base);
                 l += s[b][e];
             }
             p[2 * b] = at_pack(s[b], 0);
@@ -739,7 +744,7 @@ __global__ void __launch_bounds__(AT_TPB, 2) rb_attend_kernel(AttentionArgs a)
     at_wait_for_all();                              // (the tiles are read)
     at_store<D>(&lds[0][0][0] + wave * AT_BLOCK * D * 2, a.out.at(start, head), a.out.token, a.tokens - start, a.dim, o, 1.0f / l, empty);
     if (a.lse && half == 0 && row < a.tokens)
-        a.lse[(int64_t)head * a.tokens + row] = empty ? sc_neg_inf() : ((FORM == AT_CAPPED ? a.score.to_log2 : m) + __log2f(l)) * AT_LN2;
+        a.lse[(int64_t)head * a.tokens + row] = empty ? sc_neg_inf() : ((FORM == AT_CAPPED ? a.score.to_log2 + m : m) + __log2f(l)) * AT_LN2;
 }
 
 // ---- gradients -----------------------------------------------------------------

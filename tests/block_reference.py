@@ -131,7 +131,7 @@ def scores(q, k, scale, cap, slopes, mask):
     if slopes is not None:
         i = torch.arange(q.shape[0], dtype=torch.float64)
         b = slopes[:, None, None] * (i[:, None] - i[None]).abs()
-        off = off + 4 * u * b
+        off = off + 4 * u * b.abs()
         s = s - b
     off = off + 6 * u * (s.abs() + 1)
     return torch.where(mask, s, -np.inf), slope, torch.where(mask, off, 0.0)
@@ -166,7 +166,9 @@ def attend_grad(q, k, v, out, lse, grad_out, scale, cap, slopes, mask):
     s, slope, off_s = scores(q, k, scale, cap, slopes, mask)
     lse = torch.where(mask.any(1), lse, 0.0)
     p = torch.where(mask, (s - lse[:, :, None]).exp(), 0.0)
-    off_p = p * (2 * off_s + 4 * u * (lse.abs()[:, :, None] + 1))
+    # what is less than binary32's least normal number, 2^-126, may be 0: a weight, ds, and what they were rounded to
+    least = torch.where(mask, 2.0 ** -126, 0.0)
+    off_p = p * (2 * off_s + 4 * u * (lse.abs()[:, :, None] + 1)) + least
     dp, dp_size = torch.einsum("ihd,jhd->hij", grad_out, v), torch.einsum("ihd,jhd->hij", grad_out.abs(), v.abs())
     first, first_size = (grad_out * out).sum(2).t()[:, :, None], (grad_out * out).abs().sum(2).t()[:, :, None]
     # sum of p (dp - first) over what is seen, p as it was computed: the weights add up to 1 only within the bound of lse, which makes of `first` no more than that
@@ -181,7 +183,7 @@ def attend_grad(q, k, v, out, lse, grad_out, scale, cap, slopes, mask):
     aside = p * away.abs() * slope                     # what is added to ds before it is rounded, and taken away again
     off_aside = (off_p * slope + off_slope * p) * away.abs() + 4 * u * aside
     def rounded(x, off):           # x was rounded to bfloat16
-        return off * (1 + BF16_HALF) + x.abs() * BF16_HALF
+        return off * (1 + BF16_HALF) + x.abs() * BF16_HALF + least
     off_w = rounded(p, off_p)
     off_of_q = rounded(ds.abs() + aside, off_ds + off_aside) + rounded(aside, off_aside)
     off_of_k = rounded(ds, off_ds)
