@@ -937,7 +937,8 @@ __global__ void __launch_bounds__(AT_TPB, 2) rb_attend_grad_q_kernel(AttentionAr
     off += sc_xor<32>(off);
     by += sc_xor<32>(by);
     const bool empty = mine.lo >= mine.hi;
-    if (half == 0 && row < a.tokens && !empty) a.delta[(int64_t)head * a.tokens + row] = delta + off;
+    // (of a row that sees a key that is not finite `off` is made of scores without its numbers: the first value stays)
+    if (half == 0 && row < a.tokens && !empty && !lost) a.delta[(int64_t)head * a.tokens + row] = delta + off;
     const float aside = FINE ? off : FORM == AT_PLAIN ? by : off + by;
 #pragma unroll
     for (int n = 0; n < D / 32; ++n)
