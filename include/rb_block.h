@@ -99,7 +99,8 @@ int rb_norm_forward(rb_norm *n, const rb_rows *x, const rb_rows *residual, const
  *   d = rstd * (g - mean(g) - h * mean(g * h)) + grad_total   -> grad_sum: the gradient of the sum, so of the residual (and of x without drop), rounded to dtype
  *   dropout(d)                                                -> grad_x, rounded to dtype (needed with drop, null without)
  *   sum over the rows of grad_y * h, of grad_y                -> grad_weight, grad_bias (each may be null), `width` elements of weight_dtype
- * mean and rstd are rb_norm_forward's for this total.  grad_sum or grad_x may be grad_y or grad_total, but not both the same (same pointer and stride);
+ * mean and rstd are rb_norm_forward's for this total; what rounding the mean to one number has left is made again from total (of rows far from 0 it may be as large
+ * as what they differ by).  grad_sum or grad_x may be grad_y or grad_total, but not both the same (same pointer and stride);
  * otherwise what is written overlaps nothing.  rows = 0: grad_weight and grad_bias become 0.
  * RB_EINVAL: as above; drop without grad_x or grad_x without drop.  RB_ESTATE: not bound.
  */

@@ -268,15 +268,29 @@ int rb_norm_grad(rb_norm* n, const rb_rows* grad_y, const rb_rows* total, const 
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     hipError_t e = hipSuccess;
     const unsigned groups = grad_form(n, [&](auto, auto lanes, auto) { return norm_groups(rows, std::min(lanes(), 512), NM_SUM_WAVES); });
-    if (wanted && n->width > NM_FUSED_WIDTH) {       // (before grad_y may be overwritten)
-        const dim3 grid(groups, (unsigned)(n->width + NM_TPB * NM_PIECE - 1) / (NM_TPB * NM_PIECE));
-        if (rows > 0) e = n->dtype == RB_F32 ? launch(rb_norm_columns_kernel<float>, grid, NM_TPB, 0, st, a) : launch(rb_norm_columns_kernel<Bf16>, grid, NM_TPB, 0, st, a);
+    const dim3 columns_grid(groups, (unsigned)(n->width + NM_TPB * NM_PIECE - 1) / (NM_TPB * NM_PIECE));
+    auto columns = [&] { return n->dtype == RB_F32 ? launch(rb_norm_columns_kernel<float>, columns_grid, NM_TPB, 0, st, a) : launch(rb_norm_columns_kernel<Bf16>, columns_grid, NM_TPB, 0, st, a); };
+    // long rows: their weights' gradients come from another kernel, which needs grad_y and what the rows have beside their means: behind the first kernel, that makes
+    // the latter on its way, or before it where it overwrites grad_y
+    const bool apart = wanted && rows > 0 && n->width > NM_FUSED_WIDTH, before = apart && (grad_sum->data == grad_y->data || (drop && grad_x->data == grad_y->data));
+    if (apart) {
+        constexpr int64_t GROUPS = NM_MAX_GROUPS / 2;       // (of workgroups of 512 threads; the workspace's second half is free)
+        static_assert(2 * GROUPS * (NM_FUSED_WIDTH + 1) >= RB_MAX_NORM_ROWS, "a number a row");
+        a.rests = n->sums + 2 * GROUPS * n->width;
+    }
+    if (before) {
+        e = grad_form(n, [&](auto type, auto lanes, auto parts) {
+            if constexpr (lanes() > 512) return launch(rb_norm_rests_kernel<decltype(type), lanes(), parts()>, dim3(norm_groups(rows, lanes(), 8)), nm_threads(lanes()), 0, st, a);
+            return hipSuccess;
+        });
+        if (e == hipSuccess) e = columns();
     }
     if (e == hipSuccess && rows > 0)
         e = grad_form(n, [&](auto type, auto lanes, auto parts) {
             const dim3 grid(lanes() <= 512 ? groups : norm_groups(rows, lanes(), 4));
             return launch(rb_norm_grad_kernel<decltype(type), lanes(), parts()>, grid, nm_threads(lanes()), 0, st, a);
         });
+    if (apart && !before && e == hipSuccess) e = columns();
     if (e == hipSuccess && wanted) {
         const dim3 grid((unsigned)(n->width + 63) / 64, 2);
         e = n->weight_dtype == RB_F32

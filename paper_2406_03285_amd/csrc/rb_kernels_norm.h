@@ -390,11 +390,20 @@ __global__ void __launch_bounds__(nm_threads(LANES), nm_waves<T>(LANES, PARTS)) 
 
 constexpr int NM_SUM_WAVES = 2;
 
+// What a row has beside its mean, from the sum of the differences: half a step of the mean at most.  (More would be what that sum's own roundings leave, which
+// rows near 0 are better without.)
+__device__ __forceinline__ float nm_rest(float sum, int width, float mean)
+{
+    const float most = fabsf(mean) * 0x1p-24f;
+    return fminf(fmaxf(sum / (float)width, -most), most);
+}
+
 struct NormGradArgs {
     const void *grad_y, *total, *grad_total, *weight;
     const float *mean, *rstd;
     void *grad_sum, *grad_x;
     float* sums;                       // [2][groups][width]: of the weight's and of the bias's gradient
+    float* rests;                      // [rows]: what the rows have beside `mean`, for rb_norm_columns_kernel; null: not wanted
     int64_t grad_y_stride, total_stride, grad_total_stride, grad_sum_stride, grad_x_stride;
     int32_t rows, width;
     bool wide_weights, drops;
@@ -404,14 +413,18 @@ struct NormGradArgs {
 // As forward; the gradients of the next row's y and that row are on their way while one is worked on.  SUMS: the weights' gradients are summed on the way (of rows
 // that leave room for the sums).
 // Bound by HBM where rows are of 1024 to 8192: 16384 x 4096 bfloat16 with residual and dropout 140 us of the call's 144 (4.8 TB/s).  Where there are few or
-// short rows, by the sums between lanes (65536 x 512 72 us, 4.7 TB/s; 65536 x 100 29 us, 2.3 TB/s); of more than 8192, by the registers (4096 x 16384 226 us, 3 TB/s).
+// short rows, by the sums between lanes (65536 x 512 72 us, 4.7 TB/s; 65536 x 100 30 us, 2.2 TB/s); of more than 8192, by the registers (4096 x 16384 196 us, 3.4 TB/s).
+//
+// `mean` is one number, so of rows far from 0 half a step of it may be as large as what the rows differ by (a mean of 10^4 with a deviation of 10^-3: h off by 0.15).
+// The forward pass normalises with the mean as two numbers; the second one, `rest`, is made again here, as a third sum over the row, and h is that of the forward
+// pass.  The sums of g h are made without it and put right: sum of g (h - rest rstd).
 template <typename T, int LANES, int PARTS>
 __global__ void __launch_bounds__(nm_threads(LANES), LANES > 512 ? 4 : NM_SUM_WAVES) rb_norm_grad_kernel(NormGradArgs a)
 {
     constexpr bool SUMS = LANES <= 512;
     constexpr int TPB = nm_threads(LANES), ROWS = TPB / LANES;
     constexpr bool KEPT = SUMS && PARTS * sizeof(T) <= (sizeof(T) == 2 ? 6 : 8);       // weights stay in registers between rows
-    __shared__ float places[2][32];
+    __shared__ float places[2][48];
     const Row<LANES, PARTS> of(a.width, threadIdx.x % LANES);
     const int line = threadIdx.x / LANES;
     Piece<T> next_y[PARTS], next_t[PARTS];
@@ -446,13 +459,13 @@ __global__ void __launch_bounds__(nm_threads(LANES), LANES > 512 ? 4 : NM_SUM_WA
 #pragma unroll
             for (int p = 0; p < PARTS; ++p) of.load(static_cast<const T*>(a.grad_total) + row * a.grad_total_stride, p, more[p]);
         }
-        float sum[2] = {0.0f, 0.0f};
-        auto part = [&](int p, float (&g)[8], float (&h)[8]) {       // grad_y * weight and the normalised row
+        float sum[3] = {0.0f, 0.0f, 0.0f};
+        auto part = [&](int p, float rest, float (&g)[8], float (&h)[8]) {       // grad_y * weight and the normalised row
             float ww[8];
             if constexpr (!KEPT) of.weights(a.weight, a.wide_weights, p, ww);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                h[i] = (t[p].get(i) - mean) * rstd;
+                h[i] = (t[p].get(i) - mean - rest) * rstd;
                 if constexpr (KEPT) g[i] = y[p].get(i) * w[p][i];
                 else g[i] = y[p].get(i) * ww[i];
             }
@@ -462,17 +475,13 @@ __global__ void __launch_bounds__(nm_threads(LANES), LANES > 512 ? 4 : NM_SUM_WA
             float g[8], h[8];
             y[p] = next_y[p];
             t[p] = next_t[p];
-            part(p, g, h);
+            part(p, 0.0f, g, h);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const bool counts = of.counts(p, i);
-                if constexpr (SUMS) {
-                    const bool adds = counts && (ROWS == 1 || mine);
-                    gw[p][i] += adds ? y[p].get(i) * h[i] : 0.0f;
-                    gb[p][i] += adds ? y[p].get(i) : 0.0f;
-                }
                 sum[0] += counts ? g[i] : 0.0f;
                 sum[1] += counts ? g[i] * h[i] : 0.0f;
+                sum[2] += counts ? t[p].get(i) - mean : 0.0f;
             }
             y[p].keep();
             t[p].keep();
@@ -481,11 +490,21 @@ __global__ void __launch_bounds__(nm_threads(LANES), LANES > 512 ? 4 : NM_SUM_WA
         if (first + (int64_t)gridDim.x * ROWS < a.rows) fetch(row_of(first + (int64_t)gridDim.x * ROWS));
         if (a.grad_total) more[PARTS - 1].keep();          // (has been read before any lane may write there)
         nm_sum<LANES>(sum, places[turn]);
-        const float c0 = sum[0] / (float)a.width, c1 = sum[1] / (float)a.width;
+        const float rest = nm_rest(sum[2], a.width, mean);
+        const float c0 = sum[0] / (float)a.width, c1 = fmaf(-rest * rstd, sum[0], sum[1]) / (float)a.width;
+        if (!SUMS && a.rests && threadIdx.x == 0) a.rests[row] = rest;
 #pragma unroll
         for (int p = 0; p < PARTS; ++p) {
             float g[8], h[8], d[8];
-            part(p, g, h);
+            part(p, rest, g, h);
+            if constexpr (SUMS) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const bool adds = of.counts(p, i) && (ROWS == 1 || mine);
+                    gw[p][i] += adds ? y[p].get(i) * h[i] : 0.0f;
+                    gb[p][i] += adds ? y[p].get(i) : 0.0f;
+                }
+            }
 #pragma unroll
             for (int i = 0; i < 8; ++i) d[i] = rstd * (g[i] - c0 - h[i] * c1);
             if (a.grad_total) {
@@ -538,6 +557,29 @@ __global__ void __launch_bounds__(nm_threads(LANES), LANES > 512 ? 4 : NM_SUM_WA
     }
 }
 
+// What rows have beside their means, as rb_norm_grad_kernel makes it (the same sums in the same order), where the next kernel has to come before that one.
+template <typename T, int LANES, int PARTS>
+__global__ void __launch_bounds__(nm_threads(LANES), 4) rb_norm_rests_kernel(NormGradArgs a)
+{
+    static_assert(LANES == nm_threads(LANES), "a row a workgroup");
+    __shared__ float places[2][48];
+    const Row<LANES, PARTS> of(a.width, threadIdx.x);
+    int turn = 0;
+    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x, turn ^= 1) {
+        const float mean = a.mean[row];
+        Piece<T> t[PARTS];
+#pragma unroll
+        for (int p = 0; p < PARTS; ++p) of.load(static_cast<const T*>(a.total) + row * a.total_stride, p, t[p]);
+        float sum[1] = {0.0f};
+#pragma unroll
+        for (int p = 0; p < PARTS; ++p)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum[0] += of.counts(p, i) ? t[p].get(i) - mean : 0.0f;
+        nm_sum<LANES>(sum, places[turn]);
+        if (threadIdx.x == 0) a.rests[row] = nm_rest(sum[0], a.width, mean);
+    }
+}
+
 // The weights' gradients of rows too long for the sums to stay in registers beside them: a workgroup has 2048 columns of some rows.
 template <typename T>
 __global__ void __launch_bounds__(NM_TPB) rb_norm_columns_kernel(NormGradArgs a)
@@ -547,13 +589,13 @@ __global__ void __launch_bounds__(NM_TPB) rb_norm_columns_kernel(NormGradArgs a)
     const int last = min(column, a.width - NM_PIECE);          // (the row's last piece as Row says)
     float gw[8] = {}, gb[8] = {};
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
-        const float mean = a.mean[row], rstd = a.rstd[row];
+        const float mean = a.mean[row], rest = a.rests[row], rstd = a.rstd[row];
         Piece<T> y, t;
         y.load(static_cast<const T*>(a.grad_y) + row * a.grad_y_stride + last);
         t.load(static_cast<const T*>(a.total) + row * a.total_stride + last);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            gw[i] = fmaf(y.get(i), (t.get(i) - mean) * rstd, gw[i]);
+            gw[i] = fmaf(y.get(i), (t.get(i) - mean - rest) * rstd, gw[i]);
             gb[i] += y.get(i);
         }
     }
