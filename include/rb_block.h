@@ -152,7 +152,7 @@ typedef struct rb_documents {
  *   out = sum of e^(s[j] - lse) v[j]              -> out, rounded to bfloat16
  * Products of bfloat16 numbers with sums in binary32; e^(s - max) is rounded to bfloat16 for the product with v, its sum is not.  With less than 128 positions a
  * document in the mean (tokens < 128 * count) it is taken to 2^-17 of itself instead.  With a cap of up to 32 and more positions than that, scores are
- * off by up to cap * 2^-22.  Positions that belong to no document have out 0 and lse -inf, and what lies there in q, k and v does not matter.  What a position
+ * off by up to cap * 2^-21; other capped scores are within 2^-20 of themselves.  Positions that belong to no document have out 0 and lse -inf, and what lies there in q, k and v does not matter.  What a position
  * does not see has no influence on it, infinities and NaN included; an infinity in a v[j] that it sees makes out that infinity (or NaN, where its weight is 0
  * in binary32), a NaN NaN.  out overlaps nothing that is read.  tokens = 0 is a no-op.
  * RB_EINVAL: null or misaligned pointers, strides that do not fit, tokens < 0 or > max_tokens, documents' count < 0 or > RB_MAX_DOCUMENTS.

@@ -363,7 +363,7 @@ bool documents_fit(const rb_documents* d)
 }
 
 // Documents of less than 128 positions in the mean have the forms for short documents (FINE), and their capped scores are exact near 0, too: AT_CAPPED's are off by up
-// to cap * 2^-22, which is a part in 10^6 of lse and less where it is of 128 positions.  (64 documents of 128, 16 heads of 128: forward 35 us by
+// to cap * 2^-21, which is some parts in 10^6 of lse and less where it is of 128 positions.  (64 documents of 128, 16 heads of 128: forward 35 us by
 // these forms and 32 by the others, gradients 106 and 92; with a cap of 30 forward 39 and 33, gradients 113 and 97.)
 inline bool is_short(int64_t tokens, int64_t documents) { return tokens < 128 * documents; }
 inline int form_of(const rb_attention* a, bool fine) { return a->cap == 0.0f ? AT_PLAIN : a->cap <= AT_LOW_CAP && !fine ? AT_CAPPED : AT_HIGH_CAP; }

@@ -336,7 +336,7 @@ __device__ __forceinline__ uint64_t at_noted(const uint32_t (&noted)[2], int fro
 
 // ---- scores ------------------------------------------------------------------
 //
-// All in base 2.  With r = 1 / (1 + e^2x), tanh x = 1 - 2 r to within 2^-22 (and its slope 4 r (1 - r)), so that a capped score is off by cap * 2^-22 at
+// All in base 2.  With r = 1 / (1 + e^2x), tanh x = 1 - 2 r to within 2^-21 (and its slope 4 r (1 - r)), so that a capped score is off by cap * 2^-21 at
 // most: less than what rounding e^score to bfloat16 puts in for caps of up to 32, where more is not worth it.  There the cap is also the maximum
 // that the softmax needs: e^(score - cap) is at least e^-64 for what lies next to a position, and its sums are normal numbers.  Larger caps have
 // scores that are exact near 0, too, and a running maximum; a slope below 0 raises scores beyond any cap and has one as well.  (16384 positions, 8 heads of 128: a
@@ -354,14 +354,16 @@ struct ScoreOf {
     float to_tanh;             // 2 log2 e scale / cap: 2^(to_tanh * product) = e^2x; of a high cap: scale / cap
 };
 
-// tanh within some 2^-23 of itself (its series near 0: x^9 left out, 2^-32 of it at 1/8).
+// tanh within 2^-21 of itself (eight half steps): below 0.4 by a polynomial, x + x^3 times one of three terms in x^2 that is nearest to tanh there (2^-23, and 2^-22.2 with
+// its roundings); from there on 1 - 2 r, where an exponential and a reciprocal that are off by their last bits put 2^-21 into 0.38.  (The polynomial with one
+// term more, up to 0.5, would be within 2^-21.4, and costs 2.5 % of 16384 positions with a cap of 33.)
 __device__ __forceinline__ float at_tanh(float x)
 {
     const float x2 = x * x;
-    const float near = x * fmaf(x2, fmaf(x2, fmaf(x2, -17.0f / 315, 2.0f / 15), -1.0f / 3), 1.0f);
+    const float near = x * fmaf(x2, fmaf(x2, fmaf(x2, -0.0478118619f, 0.1327802241f), -0.3333190084f), 1.0f);
     const float e = __builtin_amdgcn_exp2f(x * (2 * AT_LOG2E));
     const float far = 1.0f - 2.0f * __builtin_amdgcn_rcpf(e + 1.0f);
-    return fabsf(x) < 0.125f ? near : far;
+    return fabsf(x) < 0.4f ? near : far;
 }
 
 // A score (of AT_CAPPED: less the cap) in base 2, and the cap's slope.

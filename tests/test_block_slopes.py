@@ -41,3 +41,24 @@ def test_one_weight_of_many(cap):
     # the sum's size is rounded some times
     assert ((ref.to64(got.lse) - want).abs() <= 1e-4 + 8 * ref.F32_HALF * want.abs())[:, at].all()
     assert torch.isfinite(got.out.float()).all() and torch.isfinite(got.lse).all()
+
+
+@pytest.mark.parametrize("cap", [16.0, 64.0, 4096.0])
+def test_capped_scores_are_exact_to_some_of_their_own_half_steps(cap):
+    """Documents of one position, whose lse is the score: of any size beside the cap.  The product (of two numbers, with 1 and 2^-8) and its quotient by a power of two
+    are exact; tanh is within eight half steps, log2 e times the cap and ln 2 are two of each a constant's and a product's."""
+    tokens, dim = 30000, 8
+    g = torch.Generator().manual_seed(3)
+    x = torch.empty(tokens, dtype=torch.float64).uniform_(0.01, 0.6, generator=g)
+    x[20000:] = torch.empty(10000, dtype=torch.float64).uniform_(0.1, 3.0, generator=g)
+    x = x * (1 - 2 * (torch.arange(tokens) % 2)) * cap
+    q, k = (torch.zeros((tokens, 1, dim), dtype=torch.bfloat16) for _ in range(2))
+    q[:, 0, 0] = x.to(torch.bfloat16)
+    q[:, 0, 1] = ((x - q[:, 0, 0].double()) * 256).to(torch.bfloat16)
+    k[:, 0, 0], k[:, 0, 1] = 1.0, 2.0 ** -8
+    a = rb.DocumentAttention(1, dim, max_tokens=tokens, scale=1.0, cap=cap)
+    got = a.forward(q.cuda(), k.cuda(), k.cuda(), plain.documents(list(range(tokens + 1))))
+    s = ref.to64(q[:, 0, 0]) + ref.to64(q[:, 0, 1]) / 256
+    want = cap * torch.tanh(s / cap)
+    d = (ref.to64(got.lse)[0] - want).abs() / want.abs()
+    assert (d <= 12 * ref.F32_HALF).all(), float(d.max()) / ref.F32_HALF
