@@ -119,7 +119,8 @@ typedef struct rb_attention rb_attention;
  * numbers each, for up to max_tokens positions.  causal != 0: a position does not see what is behind it, but for its document's prefix.
  * scale multiplies the products; cap > 0: scores are cap * tanh(score / cap), cap = 0: as they are.  Host-only.
  * RB_EINVAL: null out, heads < 1 or > RB_MAX_HEADS, kv_heads < 1 or no divisor of heads, head_dim < 8, > RB_MAX_HEAD_DIM or no multiple of 8,
- * max_tokens < 1, > RB_MAX_TOKENS or more than RB_MAX_HEAD_ROWS with the heads, scale not positive and finite, cap negative or not finite.
+ * max_tokens < 1, > RB_MAX_TOKENS or more than RB_MAX_HEAD_ROWS with the heads, scale not positive and finite, cap negative or not finite,
+ * scale * log2 e, cap * log2 e or scale / cap beyond binary32's normal numbers (of scale / cap a third of the largest).
  */
 int rb_attention_create(rb_attention **out, int64_t heads, int64_t kv_heads, int64_t head_dim, int64_t max_tokens, int32_t causal, float scale, float cap);
 

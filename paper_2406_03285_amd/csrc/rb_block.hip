@@ -424,6 +424,8 @@ int rb_attention_create(rb_attention** out, int64_t heads, int64_t kv_heads, int
     if (heads < 1 || heads > RB_MAX_HEADS || kv_heads < 1 || heads % kv_heads != 0) return RB_EINVAL;
     if (head_dim < 8 || head_dim > RB_MAX_HEAD_DIM || head_dim % 8 != 0 || max_tokens < 1 || max_tokens > RB_MAX_TOKENS || heads * max_tokens > RB_MAX_HEAD_ROWS) return RB_EINVAL;
     if (!std::isfinite(scale) || !(scale > 0.0f) || !std::isfinite(cap) || cap < 0.0f) return RB_EINVAL;
+    // (what the kernels multiply by; a quotient below binary32's normal numbers would have lost bits)
+    if (!std::isfinite(scale * AT_LOG2E) || !std::isfinite(cap * AT_LOG2E) || (cap > 0.0f && (!std::isfinite(2 * AT_LOG2E * (scale / cap)) || !std::isnormal(scale / cap)))) return RB_EINVAL;
     rb_attention* a = new (std::nothrow) rb_attention();
     if (!a) return RB_ENOMEM;
     a->heads = (int32_t)heads;
