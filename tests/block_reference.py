@@ -129,7 +129,7 @@ def scores(q, k, scale, cap, slopes, mask):
         s, slope = cap * t, 1 - t * t
         off = off + 8 * cap * u
     if slopes is not None:
-        i = torch.arange(q.shape[0], dtype=torch.float64)
+        i = torch.arange(q.shape[0], dtype=torch.float64, device=q.device)
         b = slopes[:, None, None] * (i[:, None] - i[None]).abs()
         off = off + 4 * u * b.abs()
         s = s - b
