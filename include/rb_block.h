@@ -40,7 +40,8 @@ extern "C" {
  *   counter = (i, 2^31 + j / 8, step's low half, step's high half), key = (seed's low half, seed's high half),
  * a function of (seed, step, row, column) alone: nothing is stored, the gradient's call is the same call on the gradients, and what rows lie
  * apart by, their type and who else is in the mini-batch do not matter.  The buffer's draws (rb.h) use other counters: one seed may serve both.
- * Layers of one training step have a `step` (or a seed) of their own each.
+ * Layers of one training step have a `step` (or a seed) of their own each.  seed and step are read when a call is made: one that was captured into a graph
+ * drops the same elements in every replay.  A graph that trains leaves dropout's calls out, is captured anew, or has p = 0.
  */
 typedef struct rb_drop {
     double p;              /* 0 <= p <= 1; 1: nothing stays                          */
@@ -124,7 +125,8 @@ typedef struct rb_attention rb_attention;
  */
 int rb_attention_create(rb_attention **out, int64_t heads, int64_t kv_heads, int64_t head_dim, int64_t max_tokens, int32_t causal, float scale, float cap);
 
-/* Bytes of workspace rb_attention_bind wants. */
+/* Bytes of workspace rb_attention_bind wants: 16 a position, 8 a position and head of queries, and what the gradients' parts may need at most, 64 KB (heads of up to
+ * 64 numbers; else 128 KB) for each 128 positions of a head of keys times 16, no more than 2048 such (256 MiB).  The forward pass uses the positions' alone. */
 int rb_attention_query(const rb_attention *a, size_t *workspace_bytes);
 
 /* Attach the workspace (device, 256-byte aligned); nothing is enqueued.  It stays borrowed until rb_attention_destroy or the next bind. */
@@ -140,7 +142,9 @@ typedef struct rb_heads {
 /* Documents on the device.  Document d begins at position offsets[d] and ends before offsets[d + 1], or lengths[d] positions behind its begin if that is
  * nearer (lengths may be null: all positions).  The first prefixes[d] positions of a document are seen by all of it (null: none; means something only if
  * causal).  offsets: count + 1 numbers, none smaller than the one before.  What cannot be (offsets that fall, numbers outside of the positions, negative lengths)
- * is cut to the positions there are: which results such a call has is not specified, but it reads and writes nothing else. */
+ * is cut to the positions there are: which results such a call has is not specified, but it reads and writes nothing else.
+ * The host sees `count` alone, so that is what chooses between the forms below, and documents of no positions count: offsets that are padded to a fixed number
+ * with many of them make long documents be taken for short ones, which costs time (and precision only gains). */
 typedef struct rb_documents {
     const int64_t *offsets, *lengths, *prefixes;
     int64_t count;
@@ -152,9 +156,9 @@ typedef struct rb_documents {
  *   lse = log of the sum of e^s[j]                -> lse[h * tokens + i]  (may be null)
  *   out = sum of e^(s[j] - lse) v[j]              -> out, rounded to bfloat16
  * Products of bfloat16 numbers with sums in binary32; e^(s - max) is rounded to bfloat16 for the product with v, its sum is not.  With less than 128 positions a
- * document in the mean (tokens < 128 * count) it is taken to 2^-17 of itself instead.  With a cap of up to 32 and more positions than that, scores are
+ * document in the mean (tokens < 128 * count) it is taken to 2^-17 of itself instead.  slopes may have either sign.  With a cap of up to 32 and more positions than that, scores are
  * off by up to cap * 2^-21; other capped scores are within 2^-20 of themselves.  Positions that belong to no document have out 0 and lse -inf, and what lies there in q, k and v does not matter.  What a position
- * does not see has no influence on it, infinities and NaN included; an infinity in a v[j] that it sees makes out that infinity (or NaN, where its weight is 0
+ * does not see has no influence on it (but for how many positions and documents there are, which choose the form), infinities and NaN included; an infinity in a v[j] that it sees makes out that infinity (or NaN, where its weight is 0
  * in binary32), a NaN NaN.  out overlaps nothing that is read.  tokens = 0 is a no-op.
  * RB_EINVAL: null or misaligned pointers, strides that do not fit, tokens < 0 or > max_tokens, documents' count < 0 or > RB_MAX_DOCUMENTS.
  * RB_ESTATE: not bound.
@@ -169,8 +173,9 @@ int rb_attention_forward(rb_attention *a, const rb_heads *q, const rb_heads *k, 
  * (of keys and values over their heads of queries too), sums in binary32, p and ds rounded to bfloat16 for these products (or taken to 2^-17 of themselves,
  * as above), results rounded to bfloat16.  A position that sees one alone has a gradient of q of 0.
  * The sum of p * dp is made in binary32 from the first value grad_out[i] . out[i] on, so that out's rounding does not matter.
- * What a position does not see, or is not seen by, has no influence on its gradients; where it sees or is seen by a q, k, v or grad_out that is not finite, they
- * are not finite (which of their numbers is not specified).
+ * A position's gradients come of what it sees and of the positions that see it, with what these see; nothing else has an influence.  Where it sees or is seen by a
+ * q, k, v or grad_out that is not finite, or one of the positions that see it has an out that is not finite, they are not finite (which of their numbers
+ * is not specified).  An infinite k without weight (a score of -inf) matters to itself and to the gradients of q of who sees it, to no other.
  * Positions that belong to no document have gradients 0.  What is written overlaps nothing.  (The slopes have no gradient.)
  * RB_EINVAL, RB_ESTATE: as above.
  */

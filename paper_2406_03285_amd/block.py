@@ -170,7 +170,8 @@ class _Structures:
 # ---- dropout -------------------------------------------------------------------
 
 class Drop(NamedTuple):
-    """Dropout with probability p; the mask is a function of seed, step, row and column.  Every layer of a training step has a step (or a seed) of its own."""
+    """Dropout with probability p; the mask is a function of seed, step, row and column.  Every layer of a training step has a step (or a seed) of its own.  Both are
+    numbers of the host: a call that was captured into a graph has the same mask in every replay."""
     p: float
     seed: int
     step: int
@@ -262,7 +263,8 @@ _M64 = 2 ** 64 - 1
 
 
 class LayerNorm(_OnStream):
-    """Layer norm of rows, alone or of residual + dropout(x), and its gradients.  One handle serves all layers of a width (it holds no weights).
+    """Layer norm of rows, alone or of residual + dropout(x), and its gradients.  One handle serves all layers of a width (it holds no weights), and one host thread
+    at a time.
 
     norm = LayerNorm(1024, torch.bfloat16, weight_dtype=torch.float32)
     o = norm.forward(x, weight, bias, residual=r, drop=Drop(0.1, seed, step))      # Normed; x, r [rows, width], rows may be strided
@@ -413,7 +415,8 @@ class _Norm(torch.autograd.Function):
 
 class Documents(NamedTuple):
     """Where the documents of packed rows lie, int64 on the device: document d begins at position offsets[d] and ends before offsets[d + 1] (or after lengths[d]
-    positions); all of it sees its first prefixes[d] positions."""
+    positions); all of it sees its first prefixes[d] positions.  Empty documents are documents: with more than one for each 128 positions (padded offsets) a call
+    takes the forms for short ones, which are slower for long ones."""
     offsets: torch.Tensor                      # [documents + 1]
     lengths: Optional[torch.Tensor] = None     # [documents]
     prefixes: Optional[torch.Tensor] = None    # [documents]
@@ -434,7 +437,7 @@ _NO_HEADS = (0, 0, 0) * 4
 
 
 class DocumentAttention(_OnStream):
-    """Attention of packed documents, and its gradients.  One handle serves all layers of a form.
+    """Attention of packed documents, and its gradients.  One handle serves all layers of a form, and one host thread at a time.
 
     attention = DocumentAttention(16, 128, kv_heads=4, max_tokens=8192)            # bfloat16; causal, no cap
     documents = Documents(torch.tensor([0, 700, 1500], device="cuda"))

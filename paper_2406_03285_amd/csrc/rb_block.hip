@@ -95,8 +95,8 @@ hipError_t norm_forward(const NormArgs& a, hipStream_t st)
 template <int N> using Int = std::integral_constant<int, N>;
 
 // Lanes of a row and pieces of a lane, by the row's length, which ends in the last part: `of` is called with both.  Few lanes have few exchanges to a sum (2^25
-// numbers of bfloat16 with residual and dropout: rows of 256 55 us with 16 lanes and 109 with 64, of 512 53 with 32 and 57 with 64), many have few
-// registers to a lane (2048: 57 with 128, 64 with 64; 8192: 53 with 512 and 70 with 256).
+// numbers of bfloat16 with residual and dropout: rows of 256 51 us with 16 lanes and 96 with 64, of 512 50 with 32 and 54 with 64), many have few
+// registers to a lane (2048: 56 with 128, 62 with 64; 8192: 54 with 512 and 66 with 256).
 template <typename Of>
 auto forward_by_width(int32_t width, const Of& of)
 {
@@ -113,9 +113,9 @@ auto forward_by_width(int32_t width, const Of& of)
     if (width <= 24576) return of(Int<1024>(), Int<3>());
     return of(Int<1024>(), Int<4>());
 }
-// The gradients' sums and rows ahead take more registers: fewer pieces of a lane, of binary32 all the more.  (The same 2^25 numbers: rows of 384 78 us with 16
-// lanes and 135 with 64; 512 81 with 32 and 108 with 64; 1536 80 with 64 and 141 with 256; 2048 84 with 128, 115 with 256 and 117 with 64; 8192 86 with 512
-// and 125 with 256.)
+// The gradients' sums and rows ahead take more registers: fewer pieces of a lane, of binary32 all the more.  (The same 2^25 numbers: rows of 384 70 us with 16
+// lanes and 149 with 64; 512 72 with 32 and 121 with 64; 1536 71 with 64 and 161 with 256; 2048 76 with 128, 130 with 256 and 78 with 64; 8192 82 with 512
+// and 110 with 256.)
 template <typename Of>
 auto grad_by_width(int32_t width, const Of& of)
 {
@@ -324,8 +324,8 @@ constexpr int64_t AT_KEY_GROUPS = 512, AT_MAX_PARTS = 16;
 
 // Into how many parts the queries of a head of keys are cut: until all units have two workgroups, and twice as many where some have much more to do than others.
 // That is so for the first keys of what is causal, and in documents of several lengths.  (Gradients of 16 heads of 128 to 8, once and twice as many: one causal
-// document of 8192 1395 and 1150 us, not causal 2065 and 2100; 24 documents of any lengths in 8192 260 and 228, 8 of them 574 and 433, not causal 687 and
-// 515.  The price is paid by documents of the same length, 24 of 341: 157 and 183, and by short ones, which have no such differences.)
+// document of 8192 1347 and 1080 us, not causal 1985 and 2027; 24 documents of any lengths in 8192 306 and 241, 8 of them 468 and 352, not causal 690 and
+// 563.  The price is paid by documents of the same length, 24 of 341: 156 and 182, and by short ones, which have no such differences.)
 inline int key_parts(const rb_attention* a, int64_t tokens, int64_t documents)
 {
     const int64_t groups = (tokens + AT_ROWS - 1) / AT_ROWS * a->kv_heads;
@@ -364,7 +364,7 @@ bool documents_fit(const rb_documents* d)
 
 // Documents of less than 128 positions in the mean have the forms for short documents (FINE), and their capped scores are exact near 0, too: AT_CAPPED's are off by up
 // to cap * 2^-21, which is some parts in 10^6 of lse and less where it is of 128 positions.  (64 documents of 128, 16 heads of 128: forward 35 us by
-// these forms and 32 by the others, gradients 106 and 92; with a cap of 30 forward 39 and 33, gradients 113 and 97.)
+// these forms and 33 by the others, gradients 122 and 104; with a cap of 30 forward 40 and 34, gradients 135 and 110.)
 inline bool is_short(int64_t tokens, int64_t documents) { return tokens < 128 * documents; }
 inline int form_of(const rb_attention* a, bool fine) { return a->cap == 0.0f ? AT_PLAIN : a->cap <= AT_LOW_CAP && !fine ? AT_CAPPED : AT_HIGH_CAP; }
 ScoreOf score_of(const rb_attention* a, int form)
@@ -389,8 +389,8 @@ AttentionArgs attention_args(const rb_attention* a, int form, const rb_heads* q,
     g.group = a->heads / a->kv_heads;
     g.tiles = (int32_t)((tokens + AT_ROWS - 1) / AT_ROWS);
     g.inner = inner_heads(a->heads, g.group);
-    // (documents of any lengths in 8192 positions, 16 heads of 128: 24 of them, forward 59 -> 58 us and gradients 267 -> 258, 42 of them 57.5 -> 53 and 245 -> 234; 64
-    // of 128 each lose by it: 30 -> 35 and 87 -> 95)
+    // (documents of any lengths in 8192 positions, 16 heads of 128: 24 of them, forward 74 -> 60 us and gradients 313 -> 241, 42 of them 49 -> 46 and 198 -> 189; 64
+    // of 128 each lose by it: 33 -> 39 and 104 -> 112)
     g.ranked = d->count > 1 && tokens >= 160 * d->count && g.tiles > 1 && g.tiles <= AT_RANKED;
     return g;
 }
@@ -474,7 +474,7 @@ int rb_attention_forward(rb_attention* a, const rb_heads* q, const rb_heads* k, 
     AttentionArgs g = attention_args(a, form, q, k, v, tokens, documents, slopes);
     g.out = rows_of(out);
     g.lse = lse;
-    // one launch where a workgroup can look through the documents itself (9 documents of 160 positions: 11.3 -> 7.9 us)
+    // one launch where a workgroup can look through the documents itself (9 documents in 160 positions: 10.2 to 12.7 us in two, 8.4 in one)
     hipError_t e = hipSuccess;
     if (documents->count < AT_NEAR_OFFSETS) g.spans = nullptr;       // (with many documents tiles take turns as they lie)
     else e = launch(rb_spans_kernel, dim3((unsigned)(tokens + AT_TPB - 1) / AT_TPB), AT_TPB, 0, st, g.documents);

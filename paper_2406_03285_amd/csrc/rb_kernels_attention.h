@@ -340,7 +340,7 @@ __device__ __forceinline__ uint64_t at_noted(const uint32_t (&noted)[2], int fro
 // most: less than what rounding e^score to bfloat16 puts in for caps of up to 32, where more is not worth it.  There the cap is also the maximum
 // that the softmax needs: e^(score - cap) is at least e^-64 for what lies next to a position, and its sums are normal numbers.  Larger caps have
 // scores that are exact near 0, too, and a running maximum; a slope below 0 raises scores beyond any cap and has one as well.  (16384 positions, 8 heads of 128: a
-// cap of 30 590 us and gradients 2335, one of 33 912 and 2785.)
+// cap of 30 613 us and gradients 2424, one of 33 926 and 2905.)
 //
 // Short documents.  p and ds are rounded to bfloat16 for the products over positions.  The errors of many positions are as independent as those of the results'
 // own rounding, and as large.  Of a handful of positions they may be twice as large, so there (FINE) what the rounding left is multiplied too: an error
@@ -461,7 +461,7 @@ __device__ __forceinline__ Reach at_reach(const Spans* spans, int first, int tok
 }
 
 // The tile whose turn it is where there are several documents: the one with the turn's place among all, by what its rows see (or are seen by), the longest first.
-// `lengths`: of all tiles, one a thread (at most AT_RANKED; 24 documents in 8192 positions, 16 heads of 128: 87 -> 77 us).
+// `lengths`: of all tiles, one a thread (at most AT_RANKED; 24 documents in 8192 positions, 16 heads of 128: 74 -> 60 us).
 constexpr int AT_RANKED = AT_TPB;
 __device__ __forceinline__ int at_ranked(int turn, int tiles, int length, char* lds)
 {
@@ -548,11 +548,11 @@ __device__ __forceinline__ void at_store_sum(float* row, const at_acc (&v)[D / 3
 // A workgroup has 128 queries of one head, 32 a wavefront, and goes through the keys that they see, 64 at a time, with the next 64 keys and values on their
 // way into the other half of LDS.  One pass: p = e^(s - m) with the running maximum m, l the sum of p, o the sum of p v; o and l are scaled where m
 // has grown by more than 2^8.  Two workgroups a unit (256 registers a lane, 64 KB of LDS): while a wavefront makes its softmax, another one multiplies.  That
-// they do not do both at the same time is what the wavefronts' priorities are for: scores and softmax go before the second product (not causal 506 us without,
-// 482 with both products before the softmax, 474 so; capped scores 643, 644 and 566).
-// Bound by the matrix instructions and the softmax's vector instructions beside them: 16 heads of 128 that see all of 8192 positions 494 us, 1.11 PFLOP/s (a large
-// product of the library runs at 1.3); one document of 16384 with 8 heads 574 us causal, 604 with capped scores; 24 documents of any lengths in 8192 positions
-// 58 us, half of it starts, ends and tiles that are masked in part.  64 documents of 128 30 us.
+// they do not do both at the same time is what the wavefronts' priorities are for: scores and softmax go before the second product (16 heads of 128 that see all of 8192 positions
+// 526 us without, 503 with both products before the softmax, 497 so; 16384 positions, 8 heads, a cap of 30: 662, 661 and 602).
+// Bound by the matrix instructions and the softmax's vector instructions beside them: the 497 us are 1.11 PFLOP/s (a large product of the library runs at 1.3); one
+// document of 16384 with 8 heads 510 us causal, 602 with capped scores; 24 documents of any lengths in 8192 positions 60 us, half of it starts, ends and
+// tiles that are masked in part.  64 documents of 128 33 us.
 template <int D, int FORM, bool SLOPES, bool FINE>
 __global__ void __launch_bounds__(AT_TPB, 2) rb_attend_kernel(AttentionArgs a)
 {
@@ -821,7 +821,7 @@ __device__ __forceinline__ void at_weight(const ScoreOf& of, float product, floa
 // error e the gradient gets e (k - mean of k) and not e k, where keys may lie around a mean that is larger than what they differ by.
 //
 // The queries' gradients of the results stay in LDS (q is in registers), 32 keys at a time leave room for two workgroups a unit.  One document of 8192, 16 heads of
-// 128: 550 us, four products at 1.0 PFLOP/s.
+// 128: 510 us of a call's 1080, four products at 1.08 PFLOP/s.
 template <int D, int FORM, bool SLOPES, bool FINE>
 __global__ void __launch_bounds__(AT_TPB, 2) rb_attend_grad_q_kernel(AttentionArgs a)
 {
@@ -953,8 +953,8 @@ __global__ void __launch_bounds__(AT_TPB, 2) rb_attend_grad_q_kernel(AttentionAr
 }
 
 // Of keys and values: a workgroup has 128 of one head, and goes through the queries of all the heads that read it, or of a part of these (key_parts) whose sums
-// then go to memory unrounded and are added up by the next kernel, in the same order every time.  One document of 8192, 16 heads of 128 to 8: 560 us, four
-// products at 1.0 PFLOP/s, and 25 us for the parts' sums.
+// then go to memory unrounded and are added up by the next kernel, in the same order every time.  One document of 8192, 16 heads of 128 to 8: 530 us of a
+// call's 1080, four products at 1.04 PFLOP/s, and 25 us for the parts' sums.
 template <int D, int FORM, bool SLOPES, bool FINE>
 __global__ void __launch_bounds__(AT_TPB, 2) rb_attend_grad_kv_kernel(AttentionArgs a)
 {

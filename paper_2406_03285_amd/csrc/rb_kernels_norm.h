@@ -181,7 +181,7 @@ struct DropoutArgs {
 };
 
 // A thread has eight numbers, that is one draw: ten rounds of two multiplications hide behind the reading.  Short rows share a workgroup; long grids go round.
-// Bound by HBM: 8191 x 10007 bfloat16 63.5 us, 5.2 TB/s, what a copy reaches.  Of 128 x 192 binary32 the launch (2.9 us of a call's 5.4).
+// Bound by HBM: 8191 x 10007 bfloat16 63.3 us, 5.2 TB/s, what a copy reaches.  Of 128 x 192 binary32 the launch (3.0 us of a call's 5.7).
 template <typename T>
 __global__ void __launch_bounds__(NM_TPB) rb_dropout_kernel(DropoutArgs a)
 {
@@ -266,7 +266,7 @@ struct NormArgs {
 };
 
 // Wavefronts that share a SIMD, so how many workgroups of how many threads a grid that fills the chip once has.  More hide more of memory's latency until a row and the
-// next one no longer fit their registers (forward, one less each: 8192 x 8192 bfloat16 127 -> 142 us, 13000 x 5003 153 -> 172; one more: 153 -> 168).
+// next one no longer fit their registers (forward, one less each: 8192 x 8192 bfloat16 118 -> 129 us, 13000 x 5003 153 -> 171; one more: 118 -> 158, 153 -> 169).
 constexpr int nm_threads(int lanes) { return lanes > NM_TPB ? lanes : NM_TPB; }
 template <typename T>
 constexpr int nm_waves(int lanes, int parts)
@@ -278,8 +278,8 @@ constexpr int nm_waves(int lanes, int parts)
 // A workgroup goes through rows that are the grid's width apart; the next row is on its way while one is worked on.  What is kept of a row is as it lies in
 // memory (the sum is rounded to that type anyway).  SUMMED: there is a residual or dropout.  The sum is stored when all of the row has been read (a lane that
 // has numbers of another one reads them in its own time).
-// Bound by HBM: 8192 x 8192 bfloat16 with residual and dropout 111 us (4.85 TB/s; 152 before the next row was on its way meanwhile), 5120 x 2048 binary32 alone 17.3 us
-// (4.85 TB/s).  One row: the launch and one chain of reading, sums and writing, 3.0 us of a call's 6.3.
+// Bound by HBM: 8192 x 8192 bfloat16 with residual and dropout 110 us (4.9 TB/s), or 118 where one call follows another at once and the clock falls;
+// 5120 x 2048 binary32 alone 17.3 us (4.85 TB/s).  One row: the launch and one chain of reading, sums and writing, 3.0 us of a call's 6.1.
 template <typename T, int LANES, int PARTS, bool SUMMED>
 __global__ void __launch_bounds__(nm_threads(LANES), nm_waves<T>(LANES, PARTS)) rb_norm_kernel(NormArgs a)
 {
@@ -412,8 +412,9 @@ struct NormGradArgs {
 
 // As forward; the gradients of the next row's y and that row are on their way while one is worked on.  SUMS: the weights' gradients are summed on the way (of rows
 // that leave room for the sums).
-// Bound by HBM where rows are of 1024 to 8192: 16384 x 4096 bfloat16 with residual and dropout 140 us of the call's 144 (4.8 TB/s).  Where there are few or
-// short rows, by the sums between lanes (65536 x 512 72 us, 4.7 TB/s; 65536 x 100 30 us, 2.2 TB/s); of more than 8192, by the registers (4096 x 16384 196 us, 3.4 TB/s).
+// Bound by HBM where rows are of 1024 to 8192: 16384 x 4096 bfloat16 with residual and dropout 140 us of the call's 145 (4.8 TB/s).  Where there are few or
+// short rows, by the sums between lanes (65536 x 512 73 us, 4.6 TB/s; 65536 x 100 30 us, 2.1 TB/s); of more than 8192, by the registers (4096 x 16384 196 us, 3.4 TB/s), of more
+// than 16384 by reading grad_y and total twice, too (4096 x 32768 634 us, 2.1 TB/s).
 //
 // `mean` is one number, so of rows far from 0 half a step of it may be as large as what the rows differ by (a mean of 10^4 with a deviation of 10^-3: h off by 0.15).
 // The forward pass normalises with the mean as two numbers; the second one, `rest`, is made again here, as a third sum over the row, and h is that of the forward
