@@ -77,3 +77,32 @@ def test_gradients_of_many_far_rows_with_dropout(width):
     into = rb.NormGrads(gt2, gy2, torch.empty_like(w), torch.empty_like(w))
     n.grad(gy2, x, w, o.mean, o.rstd, grad_total=gt2, drop=d, out=into)
     assert all(torch.equal(a, b) for a, b in zip(into, g))
+
+
+@pytest.mark.parametrize("width", [2000, 20000])
+def test_captured_gradients_of_far_rows_are_the_eager_ones(width):
+    """Apart from the gradient that arrives and in its place, several replays, the program's own work between them."""
+    x, gy, gt = far_rows(width)
+    w = torch.ones(width, device="cuda")
+    n = rb.LayerNorm(width, F32, eps=EPS)
+    o = n.forward(x, w)
+    kept, gy2, gw2 = n.gradients(7), torch.empty_like(gy), torch.empty_like(w)
+
+    def step():
+        n.grad(gy, x, w, o.mean, o.rstd, grad_total=gt, out=kept)
+        gy2.copy_(gy)
+        n.grad(gy2, x, w, o.mean, o.rstd, grad_total=gt, out=rb.NormGrads(gy2, None, gw2, None))
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for turn in range(4):
+        gy.copy_(torch.randn(gy.shape, generator=torch.Generator("cuda").manual_seed(turn), device="cuda"))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in (kept.total, kept.weight, kept.bias, gy2, gw2)]
+        want = n.grad(gy, x, w, o.mean, o.rstd, grad_total=gt)
+        for a, b in zip(got, (want.total, want.weight, want.bias, want.total, want.weight)):
+            assert torch.equal(a, b), turn
+        torch.cuda.synchronize()
